@@ -506,6 +506,183 @@ snn_status_t snn_adamw_step(int64_t n, float* w, void* w_bf16, const float* grad
                             snn_stream_t stream);
 
 /*
+ * Leaky attention: linear attention with a decay for each head.  The state
+ * of a head is a matrix that leaks as the membrane of Eq. (2) does, charged
+ * by the outer product of a key and a value and read by a query:
+ *   S_t = beta_h S_{t-1} + k_t v_t^T        (Dk x Dv, fp32)
+ *   o_t = scale * S_t^T q_t
+ * (the paper has no such layer; beta_h is its decay with a matrix for u).
+ *
+ * Tensors are [B, T, heads, D] with D contiguous and any other strides
+ * (snn_bthd, in elements), so that q, k and v may be parts of one
+ * projection's rows and [T, B, ...] spike trains are read in place.  There
+ * are H query heads and Hk key/value heads, Hk dividing H: query head h
+ * reads key/value head h / (H / Hk), and a shared head's gradient is the sum
+ * over its query heads.
+ */
+typedef struct snn_attn_desc {
+  int64_t B, T, H, Hk;  /* sequences, tokens, query heads, key/value heads     */
+  int64_t Dk, Dv;       /* widths of q/k and of v/o: multiples of 8, 8 .. 128  */
+  int32_t dtype;        /* of q, k, v, o and their gradients: SNN_BF16/SNN_F16 */
+  float scale;          /* finite; not 0 for the backward                      */
+  uint32_t reserved[2]; /* must be 0                                           */
+} snn_attn_desc;
+
+/* A [B, T, heads, D] tensor on the device: element (b, t, h, d) at
+ * data[b*stride_b + t*stride_t + h*stride_h + d].  data 16-byte aligned;
+ * strides positive multiples of 8 (SNN_ERR_ALIGNMENT otherwise; the stride
+ * of an extent of 1 is not looked at). */
+typedef struct snn_bthd {
+  void* data;
+  int64_t stride_b, stride_t, stride_h;
+} snn_bthd;
+
+/* sizeof(snn_attn_desc) as compiled into the library (ABI check). */
+size_t snn_attn_desc_size(void);
+
+/* Bytes of device workspace of snn_leaky_attn_fwd (backward = 0) or of
+ * snn_leaky_attn_bwd (backward != 0; enough for the forward too).  0 for an
+ * invalid desc. */
+size_t snn_leaky_attn_workspace_bytes(const snn_attn_desc* desc, int backward);
+
+/*
+ * Forward over whole sequences (prompts, training).
+ *   q, k, v    as above                  o (out) [B, T, H, Dv]
+ *   beta       fp32 [H], 0 <= beta <= 1
+ *   seq_lens   int32 [B] or NULL: sequence b has its first seq_lens[b]
+ *              tokens (clamped to 0 .. T; NULL: all T).  Later places are
+ *              not read into any result, whatever they hold (NaN
+ *              included); their outputs are zero.
+ *   state_in   fp32 [slots, H, Dk, Dv] or NULL (zeros): S before the first token
+ *   state_out  fp32 [slots, H, Dk, Dv] or NULL: S after the last one (equal to
+ *              state_in's for an empty sequence).  May be state_in itself.
+ *   slots      int32 [B] or NULL: the place of sequence b's state in state_in and
+ *              state_out (NULL: b).  A place outside 0 .. num_slots-1 means
+ *              no state: zeros in, nothing written.  Places of one call
+ *              must differ where state_out is given.
+ *   ws         snn_leaky_attn_workspace_bytes(desc, 0) bytes, 16-byte aligned
+ *              (its first 256 bytes are the status word of snn_workspace_status)
+ * Products run on the tensor cores with fp32 accumulation; the state is kept
+ * in fp32 between chunks.  Valid tokens must be finite: an infinity or NaN
+ * there reaches every token of its sequence and head, earlier ones of its
+ * chunk included.
+ */
+snn_status_t snn_leaky_attn_fwd(const snn_attn_desc* desc, const snn_bthd* q, const snn_bthd* k,
+                                const snn_bthd* v, const float* beta, const int32_t* seq_lens,
+                                const float* state_in, float* state_out, const int32_t* slots,
+                                int64_t num_slots, const snn_bthd* o, void* ws, size_t ws_bytes,
+                                snn_stream_t stream);
+
+/*
+ * Backward: gradients of the forward's inputs (beta is a fixed schedule over
+ * the heads and has none).
+ *   grad_o           [B, T, H, Dv]
+ *   grad_state_out   fp32 [B, H, Dk, Dv] or NULL (zeros)
+ *   grad_q [B, T, H, Dk], grad_k [B, T, Hk, Dk], grad_v [B, T, Hk, Dv] (out);
+ *              zero in places at and past seq_lens[b]
+ *   grad_state_in    fp32 [B, H, Dk, Dv] (out) or NULL.  Must not be grad_state_out.
+ *   state_in   fp32 [B, H, Dk, Dv] or NULL, as in the forward (place b for sequence b)
+ *   ws         snn_leaky_attn_workspace_bytes(desc, 1) bytes
+ * The three gradients are the forward's recurrence with the tensors' roles
+ * changed, two of them backwards in time:
+ *   grad_q = fwd(grad_o, v, k);  grad_v = rev(k, q, grad_o);  grad_k = rev(v, grad_o, q).
+ * Results do not depend on the order in which blocks run (no atomics).
+ */
+snn_status_t snn_leaky_attn_bwd(const snn_attn_desc* desc, const snn_bthd* q, const snn_bthd* k,
+                                const snn_bthd* v, const float* beta, const int32_t* seq_lens,
+                                const float* state_in, const snn_bthd* grad_o,
+                                const float* grad_state_out, const snn_bthd* grad_q,
+                                const snn_bthd* grad_k, const snn_bthd* grad_v,
+                                float* grad_state_in, void* ws, size_t ws_bytes,
+                                snn_stream_t stream);
+
+/*
+ * One token for each of B sequences (decoding): state places are updated in
+ * place, S <- beta_h S + k v^T, and o = scale * S^T q.
+ *   desc    T = 1 (stride_t is not looked at)
+ *   state   fp32 [num_slots, H, Dk, Dv] (in/out)
+ *   slots   int32 [B] or NULL (sequence b at place b; num_slots >= B then).  A place
+ *           outside 0 .. num_slots-1 is an empty place of the batch: its o is
+ *           zero and no state changes.  Places of one call must differ.
+ */
+snn_status_t snn_leaky_attn_step(const snn_attn_desc* desc, const snn_bthd* q, const snn_bthd* k,
+                                 const snn_bthd* v, const float* beta, float* state,
+                                 const int32_t* slots, int64_t num_slots, const snn_bthd* o,
+                                 snn_stream_t stream);
+
+/*
+ * Block norms: the norm after a block, its gate and residual scale, the
+ * residual sum, and the norm before the next block, in one pass.  Per row of
+ * N channels:
+ *   n  = a * rsqrt(mean of a^2 over each group + eps) * w_post
+ *   r' = r + res_scale * n * act(z)
+ *   y  = r' * rsqrt(mean of r'^2 + eps) * w_pre
+ * with act the identity (SNN_GATE_NONE), sigmoid(z) or z * sigmoid(z).  All
+ * arithmetic is fp32; y is taken from r' before r' is rounded to its type.
+ * Without a (NULL) only y = norm(r) w_pre is computed: the norm before the
+ * first block.  Without w_pre (NULL) only r' is: the last block.
+ */
+typedef enum { SNN_GATE_NONE = 0, SNN_GATE_SIGMOID = 1, SNN_GATE_SILU = 2 } snn_gate_t;
+
+typedef struct snn_norm_desc {
+  int64_t M, N;         /* rows, channels (N <= 8192)                          */
+  int64_t group;        /* channels per group of the norm of a: 0 or N for the
+                           whole row, or 8, 16, 32, 64, 128 or 256 dividing N
+                           (a head's width)                                    */
+  int32_t dtype;        /* snn_dtype_t of a, z, y and their gradients          */
+  int32_t res_dtype;    /* of r, r' and their gradients: dtype or SNN_F32      */
+  int32_t gate;         /* snn_gate_t                                          */
+  float eps;            /* > 0                                                 */
+  uint32_t reserved[2]; /* must be 0                                           */
+} snn_norm_desc;
+
+/* A [M, N] matrix on the device with contiguous rows ld >= N elements apart;
+ * data 16-byte aligned.  NULL where a tensor is absent. */
+typedef struct snn_rows {
+  void* data;
+  int64_t ld;
+} snn_rows;
+
+/* sizeof(snn_norm_desc) as compiled into the library (ABI check). */
+size_t snn_norm_desc_size(void);
+
+/* Bytes of device workspace of snn_block_norm_bwd (partial sums of the
+ * parameter gradients); 0 for a bad shape. */
+size_t snn_block_norm_workspace_bytes(int64_t M, int64_t N);
+
+/*
+ * Forward.  w_post, res_scale (NULL: ones) and w_pre are fp32 [N].
+ *   r_out  (out) r'; NULL when a is NULL.  May be r itself.
+ *   y      (out); NULL when w_pre is NULL
+ * z is given exactly when gate is not SNN_GATE_NONE.  Rows whose N and ld are
+ * whole 16-byte vectors move in vectors; others element by element, where a
+ * group must be the whole row (SNN_ERR_UNSUPPORTED otherwise).
+ */
+snn_status_t snn_block_norm_fwd(const snn_norm_desc* desc, const snn_rows* r, const snn_rows* a,
+                                const snn_rows* z, const float* w_post, const float* res_scale,
+                                const float* w_pre, const snn_rows* r_out, const snn_rows* y,
+                                snn_stream_t stream);
+
+/*
+ * Backward from the stored r' (the norms' factors are recomputed):
+ *   d      = grad_r_out + rstd (g - y' mean(g y')),  g = grad_y w_pre, y' = r' rstd
+ *   grad_r = d,  grad_z = d res_scale n act'(z),  grad_a through the norm of a
+ *   grad_w_post, grad_scale, grad_w_pre  fp32 [N], summed over the rows in a
+ *          fixed order (the same bits on every call)
+ * grad_r_out and grad_y may be NULL (zeros; not both, and grad_y is given only with
+ * w_pre); every output may be NULL.  Without a: only grad_r and grad_w_pre.
+ * grad_r may be grad_r_out, grad_a may be grad_y.
+ *   ws     snn_block_norm_workspace_bytes(M, N) bytes, 16-byte aligned
+ */
+snn_status_t snn_block_norm_bwd(const snn_norm_desc* desc, const snn_rows* r_out,
+                                const snn_rows* a, const snn_rows* z, const float* w_post,
+                                const float* res_scale, const float* w_pre,
+                                const snn_rows* grad_r_out, const snn_rows* grad_y,
+                                const snn_rows* grad_r, const snn_rows* grad_a,
+                                const snn_rows* grad_z, float* grad_w_post, float* grad_scale,
+                                float* grad_w_pre, void* ws, size_t ws_bytes, snn_stream_t stream);
+
+/*
  * Leaky BPTT that allocates nothing (no counterpart in the paper; it exists
  * for callers of this library that cannot allocate device memory: hosts
  * whose device memory is budgeted by another runtime, real-time loops that

@@ -1,0 +1,139 @@
+// Leaky attention, one token for each sequence of a batch (decoding):
+//   S <- beta S + k v^T,   o = scale S^T q
+// on fp32 states [num_slots, H, Dk, Dv] updated in place.  Each state element is
+// read and written once (8 bytes for 4 flops), so the bound is HBM: a block
+// takes one head's state, every thread starts all its 16-byte loads before
+// the first use, and the sums over the state's rows meet in shared memory.
+#include <cuda_bf16.h>
+#include <cuda_fp16.h>
+#include <cuda_runtime.h>
+
+#include <cmath>
+
+#include "launch.cuh"
+#include "leaky_attn.cuh"
+#include "leaky_attn_host.cuh"
+#include "snn_device.cuh"
+
+namespace snn {
+namespace attn {
+
+constexpr int kStepThreads = 256;
+
+struct StepArgs {
+  Tensor q, k, v, o;
+  const float* beta;
+  float* state;
+  const int32_t* slots;
+  int64_t num_slots;
+  int H, Dk, Dv;
+  float scale;
+};
+
+// LANES: threads across a state row, four columns each (LANES * 4 >= Dv)
+template <typename T, int LANES>
+__global__ void __launch_bounds__(kStepThreads) attn_step(const StepArgs g) {
+  constexpr int kRows = kStepThreads / LANES;    // rows in one pass of the block
+  constexpr int kPass = (kMaxD + kRows - 1) / kRows;
+  __shared__ float sq[kMaxD], sk[kMaxD];
+  __shared__ float4 part[kRows][LANES];
+  grid_dep_wait();
+  const int b = blockIdx.x / g.H, h = blockIdx.x % g.H;
+  const int lane = threadIdx.x % LANES, row = threadIdx.x / LANES, col = lane * 4;
+  T* po = static_cast<T*>(g.o.data) + b * g.o.sb + h * g.o.sh;
+  const int64_t place = g.slots ? (int64_t)g.slots[b] : (int64_t)b;
+  const bool live = col < g.Dv;
+  if (place < 0 || place >= g.num_slots) {  // an empty place of the batch
+    if (row == 0 && live) {
+      const float z[4] = {0.f, 0.f, 0.f, 0.f};
+      Elem<T>::store4(po + col, z);
+    }
+    return;
+  }
+  float* st = g.state + (place * g.H + h) * (int64_t)g.Dk * g.Dv + col;
+  float4 s[kPass];
+#pragma unroll
+  for (int i = 0; i < kPass; ++i) {
+    const int r = row + i * kRows;
+    if (live && r < g.Dk) s[i] = *reinterpret_cast<const float4*>(st + (int64_t)r * g.Dv);
+  }
+  if (threadIdx.x < g.Dk) {
+    sq[threadIdx.x] = Elem<T>::load1(static_cast<const T*>(g.q.data) + b * g.q.sb + h * g.q.sh + threadIdx.x);
+    sk[threadIdx.x] = Elem<T>::load1(static_cast<const T*>(g.k.data) + b * g.k.sb +
+                                     (h / g.k.group) * g.k.sh + threadIdx.x);
+  }
+  float v[4] = {0.f, 0.f, 0.f, 0.f};
+  if (live) Elem<T>::load4(static_cast<const T*>(g.v.data) + b * g.v.sb + (h / g.v.group) * g.v.sh + col, v);
+  const float beta = g.beta[h];
+  __syncthreads();
+  float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+  for (int i = 0; i < kPass; ++i) {
+    const int r = row + i * kRows;
+    if (live && r < g.Dk) {
+      const float kr = sk[r], qr = sq[r];
+      s[i].x = fmaf(kr, v[0], beta * s[i].x);
+      s[i].y = fmaf(kr, v[1], beta * s[i].y);
+      s[i].z = fmaf(kr, v[2], beta * s[i].z);
+      s[i].w = fmaf(kr, v[3], beta * s[i].w);
+      *reinterpret_cast<float4*>(st + (int64_t)r * g.Dv) = s[i];
+      o.x = fmaf(qr, s[i].x, o.x);
+      o.y = fmaf(qr, s[i].y, o.y);
+      o.z = fmaf(qr, s[i].z, o.z);
+      o.w = fmaf(qr, s[i].w, o.w);
+    }
+  }
+  part[row][lane] = o;
+  __syncthreads();
+  if (row == 0 && live) {
+    for (int i = 1; i < kRows; ++i) {
+      const float4 p = part[i][lane];
+      o.x += p.x;
+      o.y += p.y;
+      o.z += p.z;
+      o.w += p.w;
+    }
+    const float out[4] = {g.scale * o.x, g.scale * o.y, g.scale * o.z, g.scale * o.w};
+    Elem<T>::store4(po + col, out);
+  }
+}
+
+template <typename T>
+cudaError_t launch_step(const StepArgs& g, int64_t blocks, cudaStream_t st) {
+  const dim3 grid((unsigned)blocks), block(kStepThreads);
+  if (g.Dv <= 32) return launch_pdl(attn_step<T, 8>, grid, block, 0, st, g);
+  if (g.Dv <= 64) return launch_pdl(attn_step<T, 16>, grid, block, 0, st, g);
+  return launch_pdl(attn_step<T, 32>, grid, block, 0, st, g);
+}
+
+}  // namespace attn
+}  // namespace snn
+
+using namespace snn::attn;
+
+extern "C" snn_status_t snn_leaky_attn_step(const snn_attn_desc* desc, const snn_bthd* q,
+                                            const snn_bthd* k, const snn_bthd* v, const float* beta,
+                                            float* state, const int32_t* slots, int64_t num_slots,
+                                            const snn_bthd* o, snn_stream_t stream) {
+  snn_status_t s = check_desc(desc);
+  if (s != SNN_OK) return s;
+  if (desc->T != 1) return SNN_ERR_INVALID_ARG;
+  const snn_bthd* x[4] = {q, k, v, o};
+  const int64_t heads[4] = {desc->H, desc->Hk, desc->Hk, desc->H};
+  for (int i = 0; i < 4; ++i)
+    if ((s = check_tensor(desc, x[i], heads[i])) != SNN_OK) return s;
+  if (!beta || !state || num_slots < 0) return SNN_ERR_INVALID_ARG;
+  if (!slots && num_slots < desc->B) return SNN_ERR_INVALID_ARG;
+  const void* ptrs[3] = {beta, state, slots};
+  for (const void* p : ptrs)
+    if (!aligned16(p)) return SNN_ERR_ALIGNMENT;
+  if (desc->B == 0) return SNN_OK;
+  const int G = (int)(desc->H / desc->Hk);
+  StepArgs g{tensor(q, 1), tensor(k, G), tensor(v, G), tensor(o, 1), beta, state, slots, num_slots,
+             (int)desc->H, (int)desc->Dk, (int)desc->Dv, desc->scale};
+  cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
+  const int64_t blocks = desc->B * desc->H;
+  const cudaError_t e = desc->dtype == SNN_BF16 ? launch_step<__nv_bfloat16>(g, blocks, st)
+                                                : launch_step<__half>(g, blocks, st);
+  return e == cudaSuccess ? SNN_OK : SNN_ERR_CUDA;
+}

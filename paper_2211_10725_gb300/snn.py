@@ -26,6 +26,8 @@ STATUS_NAMES = {0: "SNN_OK", 1: "SNN_ERR_INVALID_ARG", 2: "SNN_ERR_ALIGNMENT",
                 3: "SNN_ERR_UNSUPPORTED", 4: "SNN_ERR_WORKSPACE", 5: "SNN_ERR_CUDA",
                 6: "SNN_ERR_TIMEOUT"}
 DTYPE_CODE = {W.F32: 0, W.BF16: 1, W.F16: 2}
+_TORCH_DTYPE_CODE = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
+GATE_CODE = {"none": 0, "sigmoid": 1, "silu": 2}
 RESET_CODE = {"subtract": 0, "zero": 1, "none": 2}
 SG_CODE = {"fast_sigmoid": 0, "atan": 1}
 PMODE_CODE = {"scalar": 0, "per_neuron": 1, "per_channel": 2}
@@ -55,6 +57,35 @@ class ScanDesc(ctypes.Structure):
         ("wait_limit_ns", ctypes.c_int64), ("debug_flags", ctypes.c_uint32),
         ("reserved1", ctypes.c_uint32),
     ]
+
+
+class AttnDesc(ctypes.Structure):
+    """Mirror of snn_attn_desc."""
+    _fields_ = [
+        ("B", ctypes.c_int64), ("T", ctypes.c_int64), ("H", ctypes.c_int64),
+        ("Hk", ctypes.c_int64), ("Dk", ctypes.c_int64), ("Dv", ctypes.c_int64),
+        ("dtype", ctypes.c_int32), ("scale", ctypes.c_float), ("reserved", ctypes.c_uint32 * 2),
+    ]
+
+
+class Bthd(ctypes.Structure):
+    """Mirror of snn_bthd."""
+    _fields_ = [("data", ctypes.c_void_p), ("stride_b", ctypes.c_int64),
+                ("stride_t", ctypes.c_int64), ("stride_h", ctypes.c_int64)]
+
+
+class NormDesc(ctypes.Structure):
+    """Mirror of snn_norm_desc."""
+    _fields_ = [
+        ("M", ctypes.c_int64), ("N", ctypes.c_int64), ("group", ctypes.c_int64),
+        ("dtype", ctypes.c_int32), ("res_dtype", ctypes.c_int32), ("gate", ctypes.c_int32),
+        ("eps", ctypes.c_float), ("reserved", ctypes.c_uint32 * 2),
+    ]
+
+
+class Rows(ctypes.Structure):
+    """Mirror of snn_rows."""
+    _fields_ = [("data", ctypes.c_void_p), ("ld", ctypes.c_int64)]
 
 
 _P = ctypes.c_void_p
@@ -94,6 +125,16 @@ _SIGS = {
                          ctypes.c_int),
     "snn_rate_ce_leaky_bwd": ([ctypes.POINTER(ScanDesc)] + [ctypes.c_int64] * 3 + [_P] * 10
                               + [ctypes.c_size_t, _P], ctypes.c_int),
+    "snn_attn_desc_size": ([], ctypes.c_size_t),
+    "snn_leaky_attn_workspace_bytes": ([_P, ctypes.c_int], ctypes.c_size_t),
+    "snn_leaky_attn_fwd": ([_P] * 9 + [ctypes.c_int64] + [_P] * 2 + [ctypes.c_size_t, _P],
+                           ctypes.c_int),
+    "snn_leaky_attn_bwd": ([_P] * 14 + [ctypes.c_size_t, _P], ctypes.c_int),
+    "snn_leaky_attn_step": ([_P] * 7 + [ctypes.c_int64, _P, _P], ctypes.c_int),
+    "snn_norm_desc_size": ([], ctypes.c_size_t),
+    "snn_block_norm_workspace_bytes": ([ctypes.c_int64] * 2, ctypes.c_size_t),
+    "snn_block_norm_fwd": ([_P] * 10, ctypes.c_int),
+    "snn_block_norm_bwd": ([_P] * 16 + [ctypes.c_size_t, _P], ctypes.c_int),
     "snn_adamw_step": ([ctypes.c_int64] + [_P] * 5 + [ctypes.c_float] * 5 + [ctypes.c_int64] +
                        [_P, _P], ctypes.c_int),
 }
@@ -439,6 +480,176 @@ def snn_maxpool2_bwd_nhwc(dY, idx, dX, stream=None):
     M, H, W_, C = dX.shape
     _check(load_library().snn_maxpool2_bwd_nhwc(M, H, W_, C, _ptr(dY), _ptr(idx), _ptr(dX),
                                                 _stream(stream)), "snn_maxpool2_bwd_nhwc")
+
+
+def _attn_desc(where, B, T, H, Hk, Dk, Dv, dtype, scale) -> AttnDesc:
+    code = _TORCH_DTYPE_CODE.get(dtype)
+    if code is None:
+        raise ValueError(f"{where}: dtype {dtype}")
+    return AttnDesc(B, T, H, Hk, Dk, Dv, code, scale)
+
+
+def _bthd(where, name, t, shape, dtype):
+    """A [B, T, heads, D] tensor (a [B, heads, D] one for a single token) with
+    contiguous D."""
+    if tuple(t.shape) != tuple(shape) or t.dtype != dtype or not t.is_cuda:
+        raise ValueError(f"{where}: {name} must be a CUDA {dtype} tensor of shape {tuple(shape)}")
+    st = t.stride()
+    if st[-1] != 1 and t.shape[-1] > 1:
+        raise ValueError(f"{where}: {name} must have a contiguous last dimension")
+    return ctypes.byref(Bthd(t.data_ptr(), st[0], st[1] if len(st) == 4 else 0, st[-2]))
+
+
+def _flat(where, name, t, shape, dtype):
+    """Pointer of a contiguous tensor of the given shape and type, or None."""
+    if t is None:
+        return None
+    if tuple(t.shape) != tuple(shape) or t.dtype != dtype or not t.is_contiguous() or not t.is_cuda:
+        raise ValueError(f"{where}: {name} must be a contiguous CUDA {dtype} tensor of shape "
+                         f"{tuple(shape)}")
+    return t.data_ptr()
+
+
+def snn_leaky_attn_workspace_bytes(B, T, H, Hk, Dk, Dv, backward=False) -> int:
+    d = AttnDesc(B, T, H, Hk, Dk, Dv, 1, 1.0)
+    return load_library().snn_leaky_attn_workspace_bytes(ctypes.byref(d), 1 if backward else 0)
+
+
+def _state_places(where, slots, B, states):
+    """(slots pointer, number of places) of the fp32 [places, H, Dk, Dv] states."""
+    places = [s.shape[0] for s in states if s is not None]
+    n = places[0] if places else B
+    if slots is None:
+        if n != B:
+            raise ValueError(f"{where}: without slots the states have one place per sequence")
+        return None, n
+    return _flat(where, "slots", slots, (B,), torch.int32), n
+
+
+def snn_leaky_attn_fwd(q, k, v, beta, o, ws, scale=1.0, seq_lens=None, state_in=None,
+                       state_out=None, slots=None, stream=None):
+    """Leaky attention over whole sequences, S_t = beta_h S_{t-1} + k_t v_t^T and
+    o_t = scale S_t^T q_t: q [B, T, H, Dk], k [B, T, Hk, Dk], v [B, T, Hk, Dv],
+    o [B, T, H, Dv] (bf16 or fp16, any strides with contiguous D), beta fp32
+    [H].  seq_lens int32 [B]; state_in and state_out fp32 [places, H, Dk, Dv]
+    with slots int32 [B] naming each sequence's place (default b; outside the
+    range: no state).  ws: snn_leaky_attn_workspace_bytes of the shape."""
+    w = "snn_leaky_attn_fwd"
+    (B, T, H, Dk), Hk, Dv, dt = q.shape, k.shape[2], v.shape[-1], q.dtype
+    d = _attn_desc(w, B, T, H, Hk, Dk, Dv, dt, scale)
+    if state_in is not None and state_out is not None and len(state_in) != len(state_out):
+        raise ValueError(f"{w}: state_in and state_out differ in places")
+    ps, n = _state_places(w, slots, B, (state_in, state_out))
+    _check(load_library().snn_leaky_attn_fwd(
+        ctypes.byref(d), _bthd(w, "q", q, (B, T, H, Dk), dt), _bthd(w, "k", k, (B, T, Hk, Dk), dt),
+        _bthd(w, "v", v, (B, T, Hk, Dv), dt), _flat(w, "beta", beta, (H,), torch.float32),
+        _flat(w, "seq_lens", seq_lens, (B,), torch.int32),
+        _flat(w, "state_in", state_in, (n, H, Dk, Dv), torch.float32),
+        _flat(w, "state_out", state_out, (n, H, Dk, Dv), torch.float32), ps, n,
+        _bthd(w, "o", o, (B, T, H, Dv), dt), _ptr(ws), ws.numel() * ws.element_size(),
+        _stream(stream)), w)
+
+
+def snn_leaky_attn_bwd(q, k, v, beta, grad_o, grad_q, grad_k, grad_v, ws, scale=1.0,
+                       seq_lens=None, state_in=None, grad_state_out=None, grad_state_in=None,
+                       stream=None):
+    """Gradients of snn_leaky_attn_fwd (states [B, H, Dk, Dv], in sequence
+    order); ws: snn_leaky_attn_workspace_bytes(..., backward=True)."""
+    w = "snn_leaky_attn_bwd"
+    (B, T, H, Dk), Hk, Dv, dt = q.shape, k.shape[2], v.shape[-1], q.dtype
+    d = _attn_desc(w, B, T, H, Hk, Dk, Dv, dt, scale)
+    qs, ks, vs, os = (B, T, H, Dk), (B, T, Hk, Dk), (B, T, Hk, Dv), (B, T, H, Dv)
+    state = lambda name, t: _flat(w, name, t, (B, H, Dk, Dv), torch.float32)
+    _check(load_library().snn_leaky_attn_bwd(
+        ctypes.byref(d), _bthd(w, "q", q, qs, dt), _bthd(w, "k", k, ks, dt),
+        _bthd(w, "v", v, vs, dt), _flat(w, "beta", beta, (H,), torch.float32),
+        _flat(w, "seq_lens", seq_lens, (B,), torch.int32), state("state_in", state_in),
+        _bthd(w, "grad_o", grad_o, os, dt), state("grad_state_out", grad_state_out),
+        _bthd(w, "grad_q", grad_q, qs, dt), _bthd(w, "grad_k", grad_k, ks, dt),
+        _bthd(w, "grad_v", grad_v, vs, dt), state("grad_state_in", grad_state_in), _ptr(ws),
+        ws.numel() * ws.element_size(), _stream(stream)), w)
+
+
+def snn_leaky_attn_step(q, k, v, beta, state, o, scale=1.0, slots=None, stream=None):
+    """One token of each sequence (decoding): q [B, H, Dk], k [B, Hk, Dk],
+    v [B, Hk, Dv], o [B, H, Dv]; state fp32 [places, H, Dk, Dv] is updated in
+    place at slots (int32 [B]; default b; outside the range: an empty place of
+    the batch, whose o is zero)."""
+    w = "snn_leaky_attn_step"
+    (B, H, Dk), Hk, Dv, dt = q.shape, k.shape[1], v.shape[-1], q.dtype
+    d = _attn_desc(w, B, 1, H, Hk, Dk, Dv, dt, scale)
+    n = state.shape[0]
+    _check(load_library().snn_leaky_attn_step(
+        ctypes.byref(d), _bthd(w, "q", q, (B, H, Dk), dt), _bthd(w, "k", k, (B, Hk, Dk), dt),
+        _bthd(w, "v", v, (B, Hk, Dv), dt), _flat(w, "beta", beta, (H,), torch.float32),
+        _flat(w, "state", state, (n, H, Dk, Dv), torch.float32),
+        _flat(w, "slots", slots, (B,), torch.int32), n, _bthd(w, "o", o, (B, H, Dv), dt),
+        _stream(stream)), w)
+
+
+def snn_block_norm_workspace_bytes(M: int, N: int) -> int:
+    return load_library().snn_block_norm_workspace_bytes(M, N)
+
+
+def _norm_desc(where, M, N, group, dtype, res_dtype, gate, eps) -> NormDesc:
+    for dt in (dtype, res_dtype):
+        if dt not in _TORCH_DTYPE_CODE:
+            raise ValueError(f"{where}: dtype {dt}")
+    if gate not in GATE_CODE:
+        raise ValueError(f"{where}: gate {gate!r}")
+    return NormDesc(M, N, group, _TORCH_DTYPE_CODE[dtype], _TORCH_DTYPE_CODE[res_dtype],
+                    GATE_CODE[gate], eps)
+
+
+def _rows(where, name, t, shape, dtype):
+    if t is None:
+        return None
+    if tuple(t.shape) != shape or t.dtype != dtype or not t.is_cuda:
+        raise ValueError(f"{where}: {name} must be a CUDA {dtype} tensor of shape {shape}")
+    if t.stride(1) != 1 and shape[1] > 1:
+        raise ValueError(f"{where}: {name} must have contiguous rows")
+    return ctypes.byref(Rows(t.data_ptr(), t.stride(0)))
+
+
+def snn_block_norm_fwd(r, a, z, w_post, res_scale, w_pre, r_out, y, eps=1e-6, group=0,
+                       gate="none", stream=None):
+    """r_out = r + res_scale * norm(a) w_post * act(z) and y = norm(r_out)
+    w_pre over the rows of [M, N] matrices (rows any stride apart).  a None:
+    y = norm(r) w_pre alone; w_pre None: no y.  group: channels per norm of a
+    (0: the row); gate: "none", "sigmoid" or "silu" of z."""
+    w = "snn_block_norm_fwd"
+    shape = tuple(r.shape)
+    io = a.dtype if a is not None else y.dtype if y is not None else r.dtype
+    d = _norm_desc(w, *shape, group, io, r.dtype, gate, eps)
+    rows = lambda name, t, dt: _rows(w, name, t, shape, dt)
+    par = lambda name, t: _flat(w, name, t, shape[1:], torch.float32)
+    _check(load_library().snn_block_norm_fwd(
+        ctypes.byref(d), rows("r", r, r.dtype), rows("a", a, io), rows("z", z, io),
+        par("w_post", w_post), par("res_scale", res_scale), par("w_pre", w_pre),
+        rows("r_out", r_out, r.dtype), rows("y", y, io), _stream(stream)), w)
+
+
+def snn_block_norm_bwd(r_out, a, z, w_post, res_scale, w_pre, grad_r_out, grad_y, grad_r, grad_a,
+                       grad_z, grad_w_post, grad_scale, grad_w_pre, ws, eps=1e-6, group=0,
+                       gate="none", stream=None):
+    """Gradients of snn_block_norm_fwd from its stored r_out; grad_r_out or
+    grad_y None stands for zeros, an output None is not computed.  ws:
+    snn_block_norm_workspace_bytes(M, N) (None without parameter gradients)."""
+    w = "snn_block_norm_bwd"
+    res = r_out if r_out is not None else grad_r_out
+    shape = tuple(res.shape)
+    io = a.dtype if a is not None else grad_y.dtype if grad_y is not None else res.dtype
+    d = _norm_desc(w, *shape, group, io, res.dtype, gate, eps)
+    rows = lambda name, t, dt: _rows(w, name, t, shape, dt)
+    par = lambda name, t: _flat(w, name, t, shape[1:], torch.float32)
+    _check(load_library().snn_block_norm_bwd(
+        ctypes.byref(d), rows("r_out", r_out, res.dtype), rows("a", a, io), rows("z", z, io),
+        par("w_post", w_post), par("res_scale", res_scale), par("w_pre", w_pre),
+        rows("grad_r_out", grad_r_out, res.dtype), rows("grad_y", grad_y, io),
+        rows("grad_r", grad_r, res.dtype), rows("grad_a", grad_a, io), rows("grad_z", grad_z, io),
+        par("grad_w_post", grad_w_post), par("grad_scale", grad_scale),
+        par("grad_w_pre", grad_w_pre), _ptr(ws),
+        ws.numel() * ws.element_size() if ws is not None else 0, _stream(stream)), w)
 
 
 # ---------------------------------------------------------------------------
