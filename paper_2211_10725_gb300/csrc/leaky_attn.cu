@@ -7,88 +7,16 @@
 #include <cuda_runtime.h>
 
 #include <cmath>
-#include <cstring>
+#include <type_traits>
 
 #include "launch.cuh"
 #include "leaky_attn.cuh"
+#include "leaky_attn_chunks.cuh"
 #include "leaky_attn_host.cuh"
 #include "scan_host.cuh"
 
 namespace snn {
 namespace attn {
-
-constexpr int kTokThreads = 128;
-constexpr int kTokCols = 32;  // columns of the state one block keeps
-
-// Token by token: a block keeps a [Da, 32] strip of one head's state, 32
-// rows of one column in each thread's registers.
-template <typename T>
-__global__ void __launch_bounds__(kTokThreads) attn_tokens(const Args g) {
-  grid_dep_wait();
-  __shared__ float sa[kMaxD], sb[kMaxD], part[4][kTokCols];
-  const Role& r = g.role[blockIdx.z];
-  const int b = blockIdx.x / g.H, h = blockIdx.x % g.H;
-  const int col = blockIdx.y * kTokCols + (threadIdx.x & 31), row0 = (threadIdx.x >> 5) * 32;
-  const int len = seq_len(g, b);
-  const bool live = col < r.Dc;
-  const float beta = g.beta[h];
-  const T* pa = static_cast<const T*>(r.a.data) + b * r.a.sb + (h / r.a.group) * r.a.sh;
-  const T* pb = static_cast<const T*>(r.b.data) + b * r.b.sb + (h / r.b.group) * r.b.sh;
-  const T* pc = static_cast<const T*>(r.c.data) + b * r.c.sb + (h / r.c.group) * r.c.sh;
-  const int64_t out0 = b * r.out.sb + (h / r.out.group) * r.out.sh;
-  const int64_t so = (r.s_in || r.s_out) ? state_offset(g, b, h) : -1;
-  const int64_t srow = r.s_trans ? 1 : g.Dv, scol = r.s_trans ? g.Dv : 1;
-  const float in_scale = r.rev ? 1.0f / g.scale : 1.0f;
-  float E[32], R[32];
-#pragma unroll
-  for (int i = 0; i < 32; ++i) {
-    const bool in = live && row0 + i < r.Da && r.s_in && so >= 0;
-    R[i] = in ? r.s_in[so + (row0 + i) * srow + col * scol] * in_scale : 0.0f;
-    E[i] = r.rev ? R[i] : beta * R[i];
-  }
-  for (int n = 0; n < len; ++n) {
-    const int64_t t = r.rev ? len - 1 - n : n;
-    __syncthreads();
-    if (threadIdx.x < r.Da) {
-      sa[threadIdx.x] = (float)pa[t * r.a.st + threadIdx.x];
-      sb[threadIdx.x] = (float)pb[t * r.b.st + threadIdx.x];
-    }
-    __syncthreads();
-    const float c = live ? (float)pc[t * r.c.st + col] : 0.0f;
-    float o = 0.0f;
-#pragma unroll
-    for (int i = 0; i < 32; ++i) {
-      if (row0 + i < r.Da) {
-        R[i] = fmaf(sb[row0 + i], c, E[i]);
-        o = fmaf(sa[row0 + i], R[i], o);
-        E[i] = beta * R[i];
-      }
-    }
-    part[threadIdx.x >> 5][threadIdx.x & 31] = o;
-    __syncthreads();
-    if (threadIdx.x < 32 && live) {
-      const float v = g.scale * (part[0][threadIdx.x] + part[1][threadIdx.x] +
-                                 part[2][threadIdx.x] + part[3][threadIdx.x]);
-      const int64_t at = out0 + t * r.out.st + col;
-      if (r.out_f32) static_cast<float*>(r.out.data)[at] = v;
-      else static_cast<T*>(r.out.data)[at] = T(v);
-    }
-  }
-  if (threadIdx.x < 32 && live) {
-    for (int64_t t = len; t < g.T; ++t) {
-      const int64_t at = out0 + t * r.out.st + col;
-      if (r.out_f32) static_cast<float*>(r.out.data)[at] = 0.0f;
-      else static_cast<T*>(r.out.data)[at] = T(0.0f);
-    }
-  }
-  if (r.s_out && so >= 0 && live) {
-#pragma unroll
-    for (int i = 0; i < 32; ++i) {
-      if (row0 + i < r.Da)
-        r.s_out[so + (row0 + i) * srow + col * scol] = r.rev ? E[i] * g.scale : R[i];
-    }
-  }
-}
 
 // out[b, t, hk, :] = sum over the group's query heads, in head order, of the
 // fp32 shares part[b, t, h, :], rounded once.
@@ -120,12 +48,103 @@ __global__ void __launch_bounds__(256) sum_group(const float* __restrict__ part,
 // Host side
 // ---------------------------------------------------------------------------
 
+// How a run of `nroles` roles over B*H heads cuts T tokens into segments.
+// Every block costs its chunks and about kStart chunks of set-up; a segmented
+// run adds a launch over the segments (update products only, about half of a
+// chunk's time) and a sum of the earlier segments' states in each block.  The
+// count that ends soonest is taken, with full waves of kSlots resident blocks.
+// A function of the shapes alone, so that a shape always sums in the same
+// order.
+struct Plan {
+  int nseg = 1, seg_tokens = kChunk;
+};
+constexpr int kMaxSeg = 64;
+inline int tile(int64_t D) { return D <= 64 ? 64 : 128; }
+
+Plan plan(const snn_attn_desc* d, int nroles) {
+  const int64_t chunks = ceil_div(d->T, kChunk), heads = d->B * d->H * nroles;
+  const int64_t slots = tile(d->Dk) + tile(d->Dv) == 128 ? 152 * 4 : 152 * 2;
+  constexpr double kStart = 2.0, kHalf = 0.5, kSum = 0.1;
+  Plan best;
+  double best_cost = 0.0;
+  for (int64_t s = 1; s <= kMaxSeg && s <= (chunks > 1 ? chunks : 1); ++s) {
+    const int64_t per = chunks > 0 ? ceil_div(chunks, s) : 1;
+    const int64_t n = chunks > 0 ? ceil_div(chunks, per) : 1;
+    const double waves = (double)ceil_div(heads * n, slots);
+    double cost = waves * (kStart + per);
+    if (n > 1) cost += waves * (kStart + kHalf * per) + kSum * n;
+    if (s == 1 || cost < best_cost) {
+      best_cost = cost;
+      best.nseg = (int)n;
+      best.seg_tokens = (int)(per * kChunk);
+    }
+  }
+  return best;
+}
+
+size_t segment_bytes(const snn_attn_desc* d, int nroles) {
+  const Plan pl = plan(d, nroles);
+  if (pl.nseg == 1) return 0;
+  return round256((size_t)(d->B * d->H * nroles) * pl.nseg * tile(d->Dk) * tile(d->Dv) * sizeof(float));
+}
+
+// Map of a [B, T, heads, D] tensor read or written as boxes of 64 tokens x 64
+// elements of one head; tokens past T and elements past D read as zero and
+// are not written.
+bool make_map_bthd(CUtensorMap* map, const Tensor& x, const Args& g, int heads, int D, bool bf16) {
+  auto fn = gemm::encode_fn();
+  if (!fn) return false;
+  const cuuint64_t dims[4] = {(cuuint64_t)D, (cuuint64_t)g.T, (cuuint64_t)heads, (cuuint64_t)g.B};
+  // the stride of an extent of 1 is never stepped over: any valid value
+  auto bytes = [&](int64_t extent, int64_t stride) { return (cuuint64_t)(extent == 1 ? 16 : 2 * stride); };
+  const cuuint64_t strides[3] = {bytes(g.T, x.st), bytes(heads, x.sh), bytes(g.B, x.sb)};
+  const cuuint32_t box[4] = {64u, (cuuint32_t)kChunk, 1u, 1u};
+  const cuuint32_t estr[4] = {1, 1, 1, 1};
+  return fn(map, bf16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 4, x.data,
+            dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
+            CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+template <typename T, int DA, int DC>
+cudaError_t launch_tile(ChunkArgs& p, cudaStream_t st) {
+  using C = Cfg<DA, DC>;
+  const cudaError_t e = ensure_smem((const void*)attn_chunks<T, DA, DC>, C::kSmem);
+  if (e != cudaSuccess) return e;
+  const int64_t blocks = (int64_t)p.g.B * p.g.H * p.nseg * p.g.nroles;
+  if (p.nseg > 1) {
+    p.states_only = 1;
+    const cudaError_t es = launch_pdl(attn_chunks<T, DA, DC>, dim3((unsigned)blocks), dim3(C::kThreads),
+                                      C::kSmem, st, p);
+    if (es != cudaSuccess) return es;
+    p.states_only = 0;
+  }
+  return launch_pdl(attn_chunks<T, DA, DC>, dim3((unsigned)blocks), dim3(C::kThreads), C::kSmem, st, p);
+}
+
 template <typename T>
-cudaError_t launch(const Args& g, cudaStream_t st) {
-  int cols = 0;
-  for (int i = 0; i < g.nroles; ++i) cols = g.role[i].Dc > cols ? g.role[i].Dc : cols;
-  const dim3 grid((unsigned)(g.B * g.H), (unsigned)((cols + kTokCols - 1) / kTokCols), (unsigned)g.nroles);
-  return launch_pdl(attn_tokens<T>, grid, dim3(kTokThreads), 0, st, g);
+cudaError_t launch(const Args& g, const Plan& pl, float* seg_state, cudaStream_t st) {
+  ChunkArgs p = {};
+  p.g = g;
+  p.nseg = pl.nseg;
+  p.seg_tokens = pl.seg_tokens;
+  p.seg_state = seg_state;
+  constexpr bool bf = std::is_same<T, __nv_bfloat16>::value;
+  for (int i = 0; i < g.nroles && g.T > 0; ++i) {
+    const Role& r = g.role[i];
+    if (!make_map_bthd(&p.map[i].a, r.a, g, g.H / r.a.group, r.Da, bf) ||
+        !make_map_bthd(&p.map[i].b, r.b, g, g.H / r.b.group, r.Da, bf) ||
+        !make_map_bthd(&p.map[i].c, r.c, g, g.H / r.c.group, r.Dc, bf) ||
+        (!r.out_f32 && !make_map_bthd(&p.map[i].out, r.out, g, g.H / r.out.group, r.Dc, bf)))
+      return cudaErrorInvalidValue;
+  }
+  const int da = tile(g.role[0].Da), dc = tile(g.role[0].Dc);
+  if (da == 64) return dc == 64 ? launch_tile<T, 64, 64>(p, st) : launch_tile<T, 64, 128>(p, st);
+  return dc == 64 ? launch_tile<T, 128, 64>(p, st) : launch_tile<T, 128, 128>(p, st);
+}
+
+cudaError_t launch(const snn_attn_desc* d, const Args& g, const Plan& pl, float* seg_state, cudaStream_t st) {
+  return d->dtype == SNN_BF16 ? launch<__nv_bfloat16>(g, pl, seg_state, st)
+                              : launch<__half>(g, pl, seg_state, st);
 }
 
 template <typename T>
@@ -164,7 +183,11 @@ size_t snn_attn_desc_size(void) { return sizeof(snn_attn_desc); }
 
 size_t snn_leaky_attn_workspace_bytes(const snn_attn_desc* desc, int backward) {
   if (check_desc(desc) != SNN_OK) return 0;
-  return 256 + (backward ? share_bytes(desc, desc->Dk) + share_bytes(desc, desc->Dv) : 0);
+  const size_t fwd = segment_bytes(desc, 1);
+  if (!backward) return 256 + fwd;
+  const size_t bwd =
+      segment_bytes(desc, 3) + share_bytes(desc, desc->Dk) + share_bytes(desc, desc->Dv);
+  return 256 + (fwd > bwd ? fwd : bwd);
 }
 
 snn_status_t snn_leaky_attn_fwd(const snn_attn_desc* desc, const snn_bthd* q, const snn_bthd* k,
@@ -199,7 +222,7 @@ snn_status_t snn_leaky_attn_fwd(const snn_attn_desc* desc, const snn_bthd* q, co
   r.s_in = state_in;
   r.s_out = state_out;
   cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
-  const cudaError_t e = desc->dtype == SNN_BF16 ? launch<__nv_bfloat16>(g, st) : launch<__half>(g, st);
+  const cudaError_t e = launch(desc, g, plan(desc, 1), reinterpret_cast<float*>(static_cast<unsigned char*>(ws) + 256), st);
   return e == cudaSuccess ? SNN_OK : SNN_ERR_CUDA;
 }
 
@@ -228,6 +251,8 @@ snn_status_t snn_leaky_attn_bwd(const snn_attn_desc* desc, const snn_bthd* q, co
   g.num_slots = desc->B;
   g.nroles = 3;
   unsigned char* at = static_cast<unsigned char*>(ws) + 256;
+  float* seg_state = reinterpret_cast<float*>(at);
+  at += segment_bytes(desc, 3);
   float* share_k = reinterpret_cast<float*>(at);
   float* share_v = reinterpret_cast<float*>(at + share_bytes(desc, desc->Dk));
   auto share = [&](float* p, int64_t D) {
@@ -247,17 +272,7 @@ snn_status_t snn_leaky_attn_bwd(const snn_attn_desc* desc, const snn_bthd* q, co
   rq.Dc = g.Dk;
   rq.s_in = state_in;
   rq.s_trans = 1;
-  snn::attn::Role& rv = g.role[1];
-  rv.a = tensor(k, G);
-  rv.b = tensor(q, 1);
-  rv.c = tensor(grad_o, 1);
-  rv.out = G == 1 ? tensor(grad_v, 1) : share(share_v, desc->Dv);
-  rv.Da = g.Dk;
-  rv.Dc = g.Dv;
-  rv.rev = 1;
-  rv.s_in = grad_state_out;
-  rv.s_out = grad_state_in;
-  snn::attn::Role& rk = g.role[2];
+  snn::attn::Role& rk = g.role[1];
   rk.a = tensor(v, G);
   rk.b = tensor(grad_o, 1);
   rk.c = tensor(q, 1);
@@ -267,10 +282,32 @@ snn_status_t snn_leaky_attn_bwd(const snn_attn_desc* desc, const snn_bthd* q, co
   rk.rev = 1;
   rk.s_in = grad_state_out;
   rk.s_trans = 1;
+  snn::attn::Role& rv = g.role[2];
+  rv.a = tensor(k, G);
+  rv.b = tensor(q, 1);
+  rv.c = tensor(grad_o, 1);
+  rv.out = G == 1 ? tensor(grad_v, 1) : share(share_v, desc->Dv);
+  rv.Da = g.Dk;
+  rv.Dc = g.Dv;
+  rv.rev = 1;
+  rv.s_in = grad_state_out;
+  rv.s_out = grad_state_in;
   rv.out_f32 = rk.out_f32 = G > 1;
   cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
   const bool bf = desc->dtype == SNN_BF16;
-  cudaError_t e = bf ? launch<__nv_bfloat16>(g, st) : launch<__half>(g, st);
+  const Plan pl = plan(desc, 3);
+  cudaError_t e;
+  if (tile(desc->Dk) == tile(desc->Dv)) {
+    e = launch(desc, g, pl, seg_state, st);
+  } else {  // the first two roles have the widths the other way round
+    Args gv = g;
+    gv.role[0] = rv;
+    gv.nroles = 1;
+    g.nroles = 2;
+    e = launch(desc, g, pl, seg_state, st);
+    if (e == cudaSuccess)
+      e = launch(desc, gv, pl, seg_state + (size_t)(desc->B * desc->H * 2) * pl.nseg * 64 * 128, st);
+  }
   if (e == cudaSuccess && G > 1 && desc->T > 0) {
     e = bf ? launch_sum<__nv_bfloat16>(desc, share_k, grad_k, g.Dk, st)
            : launch_sum<__half>(desc, share_k, grad_k, g.Dk, st);

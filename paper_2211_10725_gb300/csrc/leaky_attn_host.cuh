@@ -21,7 +21,7 @@ inline snn_status_t check_desc(const snn_attn_desc* d) {
   if (d->dtype == SNN_F32 || d->Dk % 8 || d->Dv % 8 || d->Dk > kMaxD || d->Dv > kMaxD)
     return SNN_ERR_UNSUPPORTED;
   // block and token indexes are 32-bit
-  constexpr int64_t kMost = int64_t(1) << 30;
+  constexpr int64_t kMost = int64_t(1) << 22;
   if (d->T > kMost || d->B > kMost || d->H > kMost || d->B * d->H > kMost) return SNN_ERR_UNSUPPORTED;
   return SNN_OK;
 }
