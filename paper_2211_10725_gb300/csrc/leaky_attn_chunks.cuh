@@ -3,26 +3,30 @@
 // With E the state a chunk starts from, already decayed to its first token,
 // the recurrence over n <= 64 tokens is four products (i, j count tokens in
 // the direction of time of the role, see leaky_attn.cuh):
-//   scores  s_ij = a_i . b_j                                [64 x 64]
-//   inter   (scale beta^i a_i) E                            [64 x Dc]
-//   intra   + sum_{j <= i} (scale beta^(i-j) s_ij) c_j      [64 x Dc], same accumulator
-//   update  E <- beta^n E + sum_j b_j (beta^(n-j) c_j)^T    [Da x Dc]
+//   scores  s_ij = a_i . b_j                                          [64 x 64]
+//   inter   X = (scale beta^i) E^T a_i                                [Dc x 64]
+//   intra   O = X + sum_{j <= i} (scale beta^(i-j) s_ij) c_j          [Dc x 64]
+//   update  E^T <- beta^n E^T + sum_j (beta^(n-j) c_j) b_j^T          [Dc x Da]
 // A block walks the chunks of one head in order with E in fp32 registers, so
-// every token is read once and the state never leaves the SM.  Operands land
-// by TMA as 64-token, 64-element boxes (128-byte swizzle); the same box of b
-// is the K-major operand of the scores and the MN-major one of the update.
-// Per chunk one thread issues the MMAs in two groups with the block's work
-// between: the decayed scores, queries and values go back to shared memory as
-// 16-bit operands; then the state is updated from its accumulator while the
-// intra product runs, and the output leaves by TMA.  Two blocks (128-wide
-// heads) or four (64-wide) share an SM and fill each other's waits; 64-token
-// chunks are what lets two 112 KB working sets fit.
+// every token is read once and the state never leaves the SM.  The last three
+// products are taken transposed, with the Dc channels as the rows: a 128-wide
+// head then fills the tensor core's 128 rows although a chunk has 64 tokens,
+// and the state's 16-bit copy is an operand in tensor memory (in shared
+// memory for a 64-wide head).  Operands land by TMA as 64-token, 64-element
+// boxes (128-byte swizzle); the same box of b is the K-major operand of the
+// scores and the MN-major one of the update.  Per chunk one thread issues the
+// MMAs in two groups, with the block's work between: the decayed scores and
+// values go back to shared memory as 16-bit operands, the inter product is
+// decayed in place; then the output leaves by TMA and the state is updated.
+// Two blocks (128-wide heads) or four (64-wide) share an SM and fill each
+// other's waits; 64-token chunks are what lets two working sets fit.
 //
-// Roundings to 16 bits: the operands (decayed scores, queries, values and the
-// state's copy) and the output.  The state itself is a sum of fp32
-// accumulators; where it is an output, the decayed values are split into two
-// 16-bit parts and multiplied twice, so it keeps 16 bits or more per term.
-// The state's copy is bf16 even for fp16 tensors, for its range.
+// Roundings to 16 bits: the decayed scores, the state's copy and the output.
+// The decayed values are two 16-bit parts each (v w = hi + lo with products
+// and residuals exact in packed 16-bit arithmetic), multiplied in turn, so a
+// state keeps 16 bits or more of each term; where a bf16 state is an output, a
+// third part makes them 24.  fp16 has not the range of a sum of products: its
+// state copy is scaled by a power of two.
 //
 // Few heads and many tokens: the tokens are cut into segments, a first launch
 // finds each segment's own contribution to the state (update products only),
@@ -63,18 +67,24 @@ struct ChunkArgs {
 template <int DA, int DC>
 struct Cfg {
   static constexpr int kThreads = (DA == 128 || DC == 128) ? 256 : 128;
-  static constexpr int kHalves = kThreads / 128;  // column halves of an accumulator
-  static constexpr int kCols = DC / kHalves;      // columns of c/out a warp covers
-  static constexpr int kRowHalves = DA / 64;      // 16-lane halves of the state accumulator
-  static constexpr int kState = kRowHalves * kCols / 2;  // state floats of a thread
+  static constexpr int kHalves = kThreads / 128;   // column halves of an accumulator
+  static constexpr int kRowHalves = DC / 64;       // 16-lane halves of a warp's channels
+  static constexpr int kCols = DA / kHalves;       // state columns of a warp
+  static constexpr int kToks = kChunk / kHalves;   // tokens (score columns) of a warp
   static constexpr int kABytes = kChunk * DA * 2;
   static constexpr int kCBytes = kChunk * DC * 2;
-  static constexpr int kEBytes = DA * DC * 2;
-  static constexpr int kQBytes = kABytes > kCBytes ? kABytes : kCBytes;  // a, then values' low parts
-  static constexpr int kOutBytes = kCBytes;       // >= the 8 KB of the decayed scores
-  static constexpr int kTail = 1024;              // barriers, tables
-  static constexpr size_t kSmem = kQBytes + kABytes + 2 * kCBytes + kEBytes + kOutBytes + kTail;
-  static constexpr uint32_t kTmemCols = 2 * DC;   // scores/output, state update
+  static constexpr bool kStateTmem = DC == 128;    // where the state's 16-bit copy is
+  static constexpr int kEBytes = kStateTmem ? 0 : DA * DC * 2;
+  // the values' low parts: a buffer of their own, or (64 x 64, where it would
+  // cost the fourth block of an SM) the place of a once it has been used
+  static constexpr bool kLowInA = DA == 64 && DC == 64;
+  static constexpr int kLowBytes = kLowInA ? 0 : kCBytes;
+  static constexpr int kOutBytes = kCBytes;        // decayed scores (8 KB), then the output
+  static constexpr int kTail = 2048;               // barriers, tables
+  static constexpr size_t kSmem =
+      2 * kABytes + 2 * kCBytes + kLowBytes + kEBytes + kOutBytes + kTail;
+  // tensor memory: output, update (scores in its first 64 columns), state
+  static constexpr uint32_t kTmemCols = kStateTmem ? 256 : (DA == 64 ? 128 : 256);
   static constexpr int kBlocksPerSm = kThreads == 128 ? 4 : 2;
 };
 
@@ -148,6 +158,90 @@ __device__ __forceinline__ void tmem_st_rows(uint32_t taddr, const float (&v)[32
       : "memory");
 }
 
+// 16 lanes x 4*N/2 32-bit columns from registers: register 2k + r of lane l
+// goes to row l/4 + 8r, column 4k + l%4 (pairs of 16-bit values of an operand).
+__device__ __forceinline__ void tmem_st_pairs(uint32_t taddr, const uint32_t (&v)[8]) {
+  asm volatile(
+      "tcgen05.st.sync.aligned.16x128b.x4.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"r"(taddr),
+      "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]), "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7])
+      : "memory");
+}
+__device__ __forceinline__ void tmem_st_pairs(uint32_t taddr, const uint32_t (&v)[16]) {
+  asm volatile(
+      "tcgen05.st.sync.aligned.16x128b.x8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, "
+      "%12, %13, %14, %15, %16};" ::"r"(taddr),
+      "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]), "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7]),
+      "r"(v[8]), "r"(v[9]), "r"(v[10]), "r"(v[11]), "r"(v[12]), "r"(v[13]), "r"(v[14]), "r"(v[15])
+      : "memory");
+}
+__device__ __forceinline__ void tmem_wait_st() {
+  asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
+}
+
+// Four 8x8 blocks of 16-bit values, transposed into shared memory: lane l
+// gives the address of row l%8 of block l/8.
+__device__ __forceinline__ void stmatrix_t(void* row, uint32_t r0, uint32_t r1, uint32_t r2,
+                                           uint32_t r3) {
+  asm volatile("stmatrix.sync.aligned.m8n8.x4.trans.shared.b16 [%0], {%1, %2, %3, %4};" ::"r"(
+                   smem_u32(row)),
+               "r"(r0), "r"(r1), "r"(r2), "r"(r3)
+               : "memory");
+}
+
+// D (tensor memory) [+]= A (tensor memory, K-major) * B (shared memory)
+__device__ __forceinline__ void tc_mma_ts(uint32_t tmem_d, uint32_t tmem_a, uint64_t bdesc,
+                                          uint32_t idesc, uint32_t accumulate) {
+  asm volatile(
+      "{\n\t.reg .pred p;\n\t"
+      "setp.ne.b32 p, %4, 0;\n\t"
+      "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}" ::"r"(tmem_d),
+      "r"(tmem_a), "l"(bdesc), "r"(idesc), "r"(accumulate)
+      : "memory");
+}
+
+// v w = hi + lo in packed 16-bit arithmetic, for a weight in two parts: the
+// residual of hi is exact (a product of two significands is twice as wide).
+__device__ __forceinline__ void split_product(__nv_bfloat162 v, __nv_bfloat162 w1, __nv_bfloat162 w2,
+                                              __nv_bfloat162& hi, __nv_bfloat162& lo) {
+  hi = __hmul2_rn(v, w1);
+  lo = __hfma2(v, w2, __hfma2(v, w1, __hneg2(hi)));
+}
+__device__ __forceinline__ void split_product(__half2 v, __half2 w1, __half2 w2, __half2& hi, __half2& lo) {
+  hi = __hmul2_rn(v, w1);
+  lo = __hfma2(v, w2, __hfma2(v, w1, __hneg2(hi)));
+}
+
+template <typename T>
+struct Pair;
+template <>
+struct Pair<__nv_bfloat16> {
+  using type = __nv_bfloat162;
+};
+template <>
+struct Pair<__half> {
+  using type = __half2;
+};
+
+// x^n for n >= 0 as an unevaluated sum of two floats (about 46 bits), by
+// squaring: the tables' powers come out correctly rounded or next to it.
+struct Two {
+  float hi, lo;
+};
+__device__ __forceinline__ Two mul(Two a, Two b) {
+  const float p = a.hi * b.hi;
+  const float e = fmaf(a.hi, b.lo, fmaf(a.lo, b.hi, fmaf(a.hi, b.hi, -p)));
+  const float s = p + e;
+  return Two{s, e - (s - p)};
+}
+__device__ __forceinline__ float power(float x, int n) {
+  Two v{1.0f, 0.0f}, s{x, 0.0f};
+  for (; n > 0; n >>= 1) {
+    if (n & 1) v = mul(v, s);
+    s = mul(s, s);
+  }
+  return v.hi;
+}
+
 // MN-major descriptor whose next 64 elements along MN are box_bytes on.
 __device__ __forceinline__ uint64_t sdesc_mn(const void* tile, uint32_t box_bytes) {
   uint64_t d = gemm::sdesc_sw128(tile);
@@ -173,22 +267,26 @@ template <typename T, int DA, int DC>
 __global__ void __launch_bounds__(Cfg<DA, DC>::kThreads, Cfg<DA, DC>::kBlocksPerSm)
     attn_chunks(const __grid_constant__ ChunkArgs p) {
   using C = Cfg<DA, DC>;
+  using T2 = typename Pair<T>::type;
   constexpr int NT = C::kThreads;
   constexpr bool kHalf = std::is_same<T, __half>::value;
   extern __shared__ __align__(1024) unsigned char smem[];
   unsigned char* sA = smem;
-  unsigned char* sB = sA + C::kQBytes;
+  unsigned char* sB = sA + C::kABytes;
   unsigned char* sC = sB + C::kABytes;
-  unsigned char* sW = sC + C::kCBytes;   // decayed values
-  unsigned char* sE = sW + C::kCBytes;   // the state's copy
-  unsigned char* sP = sE + C::kEBytes;   // decayed scores, then the output
+  unsigned char* sW = sC + C::kCBytes;                    // decayed values, high parts
+  unsigned char* sL = C::kLowInA ? sA : sW + C::kCBytes;  // low parts
+  unsigned char* sE = sW + C::kCBytes + C::kLowBytes;     // the state's copy (64-wide heads)
+  unsigned char* sP = sE + C::kEBytes;                    // decayed scores, then the output
   uint64_t* bar = reinterpret_cast<uint64_t*>(sP + C::kOutBytes);
   uint64_t *bar_a = bar, *bar_b = bar + 1, *bar_c = bar + 2, *bar_s = bar + 3, *bar_u = bar + 4,
            *bar_o = bar + 5, *bar_x = bar + 6;
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bar + 7);
   unsigned* top = reinterpret_cast<unsigned*>(bar + 8);  // [2] bits of the state's largest element
-  float* pw = reinterpret_cast<float*>(bar + 10);  // beta^n, n = 0 .. 64
-  float* lag = pw + 68;  // [128] weight of token j at token i, at i - j + 64
+  float* seg_decay = reinterpret_cast<float*>(bar + 9);
+  T2* wt = reinterpret_cast<T2*>(bar + 10);       // [65][2] beta^n in two 16-bit parts
+  float* pw = reinterpret_cast<float*>(wt + 132);  // [65] beta^n
+  float* lag = pw + 68;  // [128] scaled weight of token j at token i, at i - j + 64
 
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const int quad = warp & 3, half = warp >> 2;
@@ -254,28 +352,31 @@ __global__ void __launch_bounds__(Cfg<DA, DC>::kThreads, Cfg<DA, DC>::kBlocksPer
     load_c(0);
   }
 
-  // powers of the decay, in fp64 by squaring: each one correctly rounded
-  const double beta = (double)g.beta[h];
-  auto power = [&](int n) {
-    double v = 1.0, s = beta;
-    for (; n > 0; n >>= 1, s *= s)
-      if (n & 1) v *= s;
-    return v;
-  };
-  if (tid <= kChunk) pw[tid] = (float)power(tid);
+  if (tid <= kChunk + 1) {
+    const float w = power(g.beta[h], tid <= kChunk ? tid : p.seg_tokens);
+    if (tid <= kChunk) {
+      const T hi = T(w), lo = T(w - (float)hi);
+      pw[tid] = w;
+      wt[2 * tid] = T2(hi, hi);
+      wt[2 * tid + 1] = T2(lo, lo);
+    } else {
+      *seg_decay = w;
+    }
+  }
   __syncthreads();
   if (tid < 128) {
     const int n = rev ? 64 - tid : tid - 64;
     lag[tid] = n >= 0 ? scale * pw[n] : 0.0f;
   }
 
-  // this thread's part of the state: rows erow + 16*rh (+8), columns ecol + 8k (+1)
+  // this thread's part of the transposed state: channels erow + 16*rh (+8) of
+  // c, columns ecol + 8k (+1) of a and b
   const int erow = (C::kRowHalves == 2 ? 32 : 16) * quad + (lane >> 2);
   const int ecol = half * C::kCols + 2 * (lane & 3);
   float E[C::kRowHalves][C::kCols / 2];
   const int64_t so = (r.s_in || r.s_out) ? state_offset(g, b, h) : -1;
-  const int64_t s_row = r.s_trans ? 1 : g.Dv, s_col = r.s_trans ? g.Dv : 1;
-  auto each_state = [&](auto f) {  // f(value, row, column) over the thread's part
+  const int64_t s_row = r.s_trans ? g.Dv : 1, s_col = r.s_trans ? 1 : g.Dv;
+  auto each_state = [&](auto f) {  // f(value, channel, column) over the thread's part
 #pragma unroll
     for (int rh = 0; rh < C::kRowHalves; ++rh)
 #pragma unroll
@@ -294,42 +395,38 @@ __global__ void __launch_bounds__(Cfg<DA, DC>::kThreads, Cfg<DA, DC>::kBlocksPer
         s4[(rh * (C::kCols / 8) + i / 4) * NT + tid] =
             make_float4(E[rh][i], E[rh][i + 1], E[rh][i + 2], E[rh][i + 3]);
   };
+  each_state([&](float& e, int, int) { e = 0.0f; });
   if (order == 0 && (p.nseg == 1 || states_only)) {
-    const float f = rev ? 1.0f / scale : (len > 0 ? pw[1] : 1.0f);
-    const float* s_in = so >= 0 ? r.s_in : nullptr;
-    each_state([&](float& e, int y, int x) {
-      e = s_in && y < Da && x < Dc ? f * s_in[so + y * s_row + x * s_col] : 0.0f;
-    });
+    if (r.s_in && so >= 0) {
+      const float f = rev ? 1.0f / scale : (len > 0 ? pw[1] : 1.0f);
+      const float* s_in = r.s_in + so;
+      each_state([&](float& e, int y, int x) {
+        if (y < Dc && x < Da) e = f * s_in[y * s_row + x * s_col];
+      });
+    }
     if (states_only) store_segment(0);  // kept apart: the caller's state may be overwritten in place
-  } else {
-    each_state([&](float& e, int, int) { e = 0.0f; });
-    if (!states_only && active) {
-      const float decay = (float)power(p.seg_tokens);
-      for (int m = order == 0 ? 0 : 1; m <= order; ++m) {
-        const float4* s4 = reinterpret_cast<const float4*>(seg0 + m * kSegFloats);
+  } else if (!states_only && active) {
+    const float decay = *seg_decay;
+    for (int m = order == 0 ? 0 : 1; m <= order; ++m) {
+      const float4* s4 = reinterpret_cast<const float4*>(seg0 + m * kSegFloats);
 #pragma unroll
-        for (int rh = 0; rh < C::kRowHalves; ++rh)
+      for (int rh = 0; rh < C::kRowHalves; ++rh)
 #pragma unroll
-          for (int i = 0; i < C::kCols / 2; i += 4) {
-            const float4 v = s4[(rh * (C::kCols / 8) + i / 4) * NT + tid];
-            E[rh][i] = fmaf(E[rh][i], decay, v.x);
-            E[rh][i + 1] = fmaf(E[rh][i + 1], decay, v.y);
-            E[rh][i + 2] = fmaf(E[rh][i + 2], decay, v.z);
-            E[rh][i + 3] = fmaf(E[rh][i + 3], decay, v.w);
-          }
-      }
+        for (int i = 0; i < C::kCols / 2; i += 4) {
+          const float4 v = s4[(rh * (C::kCols / 8) + i / 4) * NT + tid];
+          E[rh][i] = fmaf(E[rh][i], decay, v.x);
+          E[rh][i + 1] = fmaf(E[rh][i + 1], decay, v.y);
+          E[rh][i + 2] = fmaf(E[rh][i + 2], decay, v.z);
+          E[rh][i + 3] = fmaf(E[rh][i + 3], decay, v.w);
+        }
     }
   }
 
-  // two neighbouring 16-bit values of this lane into row y, 16-byte piece
-  // `piece`, of a tile of 128-byte swizzled rows
-  auto put = [&](unsigned char* tile, int y, int piece, float v0, float v1) {
-    *reinterpret_cast<uint32_t*>(tile + y * 128 + ((piece ^ (y & 7)) << 4) + (lane & 3) * 4) =
-        Elem<T>::from2(v0, v1);
-  };
-  // The state's copy, Da rows of 64-column boxes.  fp16 has not the range of
-  // a sum of products: its copy is scaled by the power of two that brings the
-  // largest element to 2^10 .. 2^11, and e_back undoes it.
+  const uint32_t t_quad = (uint32_t)(quad * 32) << 16;
+  const uint32_t t_out = tmem, t_upd = tmem + kChunk, t_state = tmem + kChunk + DA;
+  // The state's 16-bit copy.  fp16 has not the range of a sum of products: its
+  // copy is scaled by the power of two that brings the largest element to
+  // 2^10 .. 2^11, and e_back undoes it.
   float e_back = 1.0f;
   auto put_state = [&](int slot) {
     float f = 1.0f;
@@ -348,27 +445,34 @@ __global__ void __launch_bounds__(Cfg<DA, DC>::kThreads, Cfg<DA, DC>::kBlocksPer
     }
 #pragma unroll
     for (int rh = 0; rh < C::kRowHalves; ++rh) {
+      uint32_t v[C::kCols / 4];
 #pragma unroll
-      for (int k = 0; k < C::kCols / 8; ++k) {
-        const int x = half * C::kCols + 8 * k, y = erow + 16 * rh;
-        unsigned char* tile = sE + (x >> 6) * (DA * 128);
-        const float* e = &E[rh][4 * k];
-        put(tile, y, (x & 63) >> 3, kHalf ? f * e[0] : e[0], kHalf ? f * e[1] : e[1]);
-        put(tile, y + 8, (x & 63) >> 3, kHalf ? f * e[2] : e[2], kHalf ? f * e[3] : e[3]);
+      for (int i = 0; i < C::kCols / 4; ++i)
+        v[i] = kHalf ? Elem<T>::from2(f * E[rh][2 * i], f * E[rh][2 * i + 1])
+                     : Elem<T>::from2(E[rh][2 * i], E[rh][2 * i + 1]);
+      if constexpr (C::kStateTmem) {
+        tmem_st_pairs(t_state + t_quad + ((uint32_t)(16 * rh) << 16) + half * (C::kCols / 2), v);
+      } else {  // rows of Da: 64-column boxes of DC 128-byte rows
+#pragma unroll
+        for (int i = 0; i < C::kCols / 4; ++i) {
+          const int x = half * C::kCols + 8 * (i >> 1), y = erow + 8 * (i & 1);
+          *reinterpret_cast<uint32_t*>(sE + (x >> 6) * (DC * 128) + y * 128 +
+                                       ((((x & 63) >> 3) ^ (y & 7)) << 4) + (lane & 3) * 4) = v[i];
+        }
       }
     }
+    if constexpr (C::kStateTmem) tmem_wait_st();
   };
+  __syncwarp();
   if (!states_only && n_chunks > 0) {
     put_state(0);
     gemm::fence_async_smem();
+    gemm::tc_fence_before();
     __syncthreads();
   }
 
-  const uint32_t t_acc = tmem + ((uint32_t)(quad * 32) << 16);  // scores, then the output
-  const uint32_t t_upd = t_acc + DC + half * C::kCols;          // inter product, then the update
-  const int y0 = 16 * quad + (lane >> 2);                       // this lane's tokens: y0, y0 + 8
-  // two 16-bit parts of a bf16 value carry 16 bits of it; where the state is
-  // an output, a third one makes them 24 (two of an fp16 value carry 22)
+  const int y0 = 16 * quad + (lane >> 2);            // this lane's score rows: y0, y0 + 8
+  const int tok = half * C::kToks + 2 * (lane & 3);  // its output tokens: tok + 8k (+1)
   const bool third = !kHalf && r.s_out;
   uint32_t u_phase = 0;
   int fail = 0, it = 0;
@@ -387,89 +491,94 @@ __global__ void __launch_bounds__(Cfg<DA, DC>::kThreads, Cfg<DA, DC>::kBlocksPer
         fail |= !gemm::mbar_wait_poll(bar_b, par, kWaitNs);
         gemm::tc_fence_after();
         constexpr uint32_t id_s = idesc<T>(kChunk, kChunk, false, false);
-        constexpr uint32_t id_x = idesc<T>(kChunk, DC, false, true);
+        constexpr uint32_t id_x = idesc<T>(DC, kChunk, false, false);
 #pragma unroll
         for (int kk = 0; kk < DA / 16; ++kk) {
           const int off = (kk / 4) * kBoxBytes + (kk % 4) * 32;
-          gemm::tc_mma(tmem, gemm::sdesc_sw128(sA + off), gemm::sdesc_sw128(sB + off), id_s, kk != 0);
+          gemm::tc_mma(t_upd, gemm::sdesc_sw128(sA + off), gemm::sdesc_sw128(sB + off), id_s, kk != 0);
         }
-bulk_wait_read_all();  // the last output has left sP
         gemm::tc_commit(bar_s);
 #pragma unroll
-        for (int kk = 0; kk < DA / 16; ++kk)
-          gemm::tc_mma(tmem + DC, gemm::sdesc_sw128(sA + (kk / 4) * kBoxBytes + (kk % 4) * 32),
-                       sdesc_mn(sE + kk * 2048, DA * 128), id_x, kk != 0);
+        for (int kk = 0; kk < DA / 16; ++kk) {
+          const uint64_t q = gemm::sdesc_sw128(sA + (kk / 4) * kBoxBytes + (kk % 4) * 32);
+          if constexpr (C::kStateTmem)
+            tc_mma_ts(t_out, t_state + 8 * kk, q, id_x, kk != 0);
+          else
+            gemm::tc_mma(t_out, gemm::sdesc_sw128(sE + (kk / 4) * (DC * 128) + (kk % 4) * 32), q, id_x, kk != 0);
+        }
+        bulk_wait_read_all();  // the last output has left sP
         gemm::tc_commit(bar_x);
       }
       __syncwarp();
     }
+
+    // decayed values in two parts
     fail |= wait_all(bar_c, par);
     if (states_only) fail |= wait_all(bar_b, par);
-    // 16-bit part `PART` of the decayed values: what the parts before left of them
-    auto put_values = [&](auto part, unsigned char* to) {
-      constexpr int kPart = decltype(part)::value;
+    constexpr int kPieces = C::kCBytes / 16 / NT;
+    uint4 low[kPieces];
 #pragma unroll
-      for (int i = 0; i < C::kCBytes / 16 / NT; ++i) {
-        const int piece = i * NT + tid, y = (piece >> 3) & 63;
-        float v[8], left[8];
-        Elem<T>::load8(reinterpret_cast<const T*>(sC) + piece * 8, v);
-        if (n < kChunk && y >= n) {
+    for (int i = 0; i < kPieces; ++i) {
+      const int piece = i * NT + tid, y = (piece >> 3) & 63;
+      uint4 v = reinterpret_cast<const uint4*>(sC)[piece], hi;
+      if (n < kChunk && y >= n) v = make_uint4(0, 0, 0, 0);
+      const int at = max(0, rev ? y + 1 : ex - y);
+      const T2 w1 = wt[2 * at], w2 = wt[2 * at + 1];
+      const T2* vp = reinterpret_cast<const T2*>(&v);
+      T2 *hp = reinterpret_cast<T2*>(&hi), *lp = reinterpret_cast<T2*>(&low[i]);
 #pragma unroll
-          for (int e = 0; e < 8; ++e) v[e] = 0.0f;
-        }
-        const float w = pw[max(0, rev ? y + 1 : ex - y)];
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          left[e] = v[e] * w;
-          if (kPart > 0) left[e] = fmaf(v[e], w, -(float)T(left[e]));
-          if (kPart > 1) left[e] -= (float)T(left[e]);
-        }
-        Elem<T>::store8(reinterpret_cast<T*>(to) + piece * 8, left);
-      }
-    };
-    using Part0 = std::integral_constant<int, 0>;
-    using Part1 = std::integral_constant<int, 1>;
-    using Part2 = std::integral_constant<int, 2>;
-    put_values(Part0(), sW);
+      for (int e = 0; e < 4; ++e) split_product(vp[e], w1, w2, hp[e], lp[e]);
+      reinterpret_cast<uint4*>(sW)[piece] = hi;
+      if (!C::kLowInA) reinterpret_cast<uint4*>(sL)[piece] = low[i];
+    }
+
     if (!states_only) {
+      // decayed scores; the first token's wait for the inter product is what
+      // frees sP of the last output
       fail |= wait_all(bar_s, par);
       gemm::tc_fence_after();
-      // decayed scores
+      float s[C::kToks / 2];
+      tmem_ld_rows(t_upd + t_quad + half * C::kToks, s);
+      const int x0 = half * C::kToks;
+      const float* w = lag + 64 + y0 - x0 - 2 * (lane & 3);
 #pragma unroll
-      for (int cc = 0; cc < kChunk / C::kHalves; cc += 32) {
-        const int x0 = half * (kChunk / C::kHalves) + cc;
-        float s[16];
-        tmem_ld_rows(t_acc + x0, s);
-        const float* w = lag + 64 + y0 - x0 - 2 * (lane & 3);
+      for (int i = 0; i < C::kToks / 2; ++i) s[i] *= w[8 * ((i >> 1) & 1) - 8 * (i >> 2) - (i & 1)];
+      if (n < kChunk) {  // places past the sequence hold anything
 #pragma unroll
-        for (int i = 0; i < 16; ++i) s[i] *= w[8 * ((i >> 1) & 1) - 8 * (i >> 2) - (i & 1)];
-        if (n < kChunk) {  // places past the sequence hold anything
-#pragma unroll
-          for (int i = 0; i < 16; ++i)
-            if (max(y0 + 8 * ((i >> 1) & 1), x0 + 2 * (lane & 3) + 8 * (i >> 2) + (i & 1)) >= n) s[i] = 0.0f;
-        }
-#pragma unroll
-        for (int k = 0; k < 4; ++k) {
-          put(sP, y0, (x0 >> 3) + k, s[4 * k], s[4 * k + 1]);
-          put(sP, y0 + 8, (x0 >> 3) + k, s[4 * k + 2], s[4 * k + 3]);
-        }
+        for (int i = 0; i < C::kToks / 2; ++i)
+          if (max(y0 + 8 * ((i >> 1) & 1), x0 + 2 * (lane & 3) + 8 * (i >> 2) + (i & 1)) >= n) s[i] = 0.0f;
       }
       fail |= wait_all(bar_x, par);
       gemm::tc_fence_after();
-      // the inter product, decayed, is what the intra product adds to; the
-      // scores lie in its columns, so both halves have to have read them
-      if (C::kHalves == 2) asm volatile("bar.sync %0, 64;" ::"r"(1 + quad) : "memory");
-      {
-        float x[C::kCols / 2];
-        tmem_ld_rows(t_upd, x);
-        const float f0 = e_back * lag[64 + (rev ? y0 + 1 - n : y0)];
-        const float f1 = e_back * lag[64 + (rev ? y0 + 9 - n : y0 + 8)];
 #pragma unroll
-        for (int i = 0; i < C::kCols / 2; ++i) x[i] *= (i & 2) ? f1 : f0;
-        tmem_st_rows(t_acc + half * C::kCols, x);
+      for (int k = 0; k < C::kToks / 8; ++k) {
+        unsigned char* to = sP + y0 * 128 + ((((x0 >> 3) + k) ^ (y0 & 7)) << 4) + (lane & 3) * 4;
+        *reinterpret_cast<uint32_t*>(to) = Elem<T>::from2(s[4 * k], s[4 * k + 1]);
+        *reinterpret_cast<uint32_t*>(to + 1024) = Elem<T>::from2(s[4 * k + 2], s[4 * k + 3]);
+      }
+      if (!C::kLowInA && tid == 32 && more) load_a(it + 1);
+      __syncwarp();
+      // the inter product, decayed, is what the intra product adds to
+      float f[C::kToks / 4];
+#pragma unroll
+      for (int i = 0; i < C::kToks / 4; ++i) {
+        const int y = tok + 8 * (i >> 1) + (i & 1);
+        f[i] = e_back * lag[64 + (rev ? y + 1 - n : y)];
+      }
+#pragma unroll
+      for (int rh = 0; rh < C::kRowHalves; ++rh) {
+        float x[C::kToks / 2];
+        const uint32_t at = t_out + t_quad + ((uint32_t)(16 * rh) << 16) + half * C::kToks;
+        tmem_ld_rows(at, x);
+#pragma unroll
+        for (int i = 0; i < C::kToks / 2; ++i) x[i] *= f[2 * (i >> 2) + (i & 1)];
+        tmem_st_rows(at, x);
       }
     }
-    put_values(Part1(), sA);  // the scores and the inter product have read a
+    if (C::kLowInA) {
+#pragma unroll
+      for (int i = 0; i < kPieces; ++i) reinterpret_cast<uint4*>(sL)[i * NT + tid] = low[i];
+    }
     if (n < kChunk) {  // clear the places past the sequence
       const uint4 z = make_uint4(0, 0, 0, 0);
       for (int i = tid; i < C::kABytes / 16; i += NT)
@@ -482,30 +591,80 @@ bulk_wait_read_all();  // the last output has left sP
     if (__syncthreads_or(fail)) break;
 
     auto update = [&](const unsigned char* values, uint32_t accumulate) {
-      constexpr uint32_t id = idesc<T>(DA, DC, true, true);
+      constexpr uint32_t id = idesc<T>(DC, DA, true, true);
 #pragma unroll
       for (int kk = 0; kk < kChunk / 16; ++kk)
-        gemm::tc_mma(tmem + DC, sdesc_mn(sB + kk * 2048, kBoxBytes),
-                     sdesc_mn(values + kk * 2048, kBoxBytes), id, accumulate | (kk != 0));
+        gemm::tc_mma(t_upd, sdesc_mn(values + kk * 2048, kBoxBytes), sdesc_mn(sB + kk * 2048, kBoxBytes),
+                     id, accumulate | (kk != 0));
     };
     if (tid == 0) {
       gemm::tc_fence_after();
-      update(sW, 0);
-      update(sA, 1);
-      gemm::tc_commit(bar_u);
       if (!states_only) {
-        constexpr uint32_t id = idesc<T>(kChunk, DC, false, true);
+        constexpr uint32_t id = idesc<T>(DC, kChunk, true, false);
 #pragma unroll
         for (int kk = 0; kk < kChunk / 16; ++kk)
-          gemm::tc_mma(tmem, gemm::sdesc_sw128(sP + kk * 32), sdesc_mn(sC + kk * 2048, kBoxBytes), id, 1);
+          gemm::tc_mma(t_out, sdesc_mn(sC + kk * 2048, kBoxBytes), gemm::sdesc_sw128(sP + kk * 32), id, 1);
         gemm::tc_commit(bar_o);
       }
+      update(sW, 0);
+      update(sL, 1);
+      gemm::tc_commit(bar_u);
     }
     __syncwarp();
+
+    if (!states_only) {
+      fail |= wait_all(bar_o, par);
+      gemm::tc_fence_after();
+      if (tid == 96 && more && !third) load_c(it + 1);
+      __syncwarp();
+#pragma unroll
+      for (int rh = 0; rh < C::kRowHalves; ++rh) {
+        float o[C::kToks / 2];
+        tmem_ld_rows(t_out + t_quad + ((uint32_t)(16 * rh) << 16) + half * C::kToks, o);
+        if (n < kChunk) {
+#pragma unroll
+          for (int i = 0; i < C::kToks / 2; ++i)
+            if (tok + 8 * (i >> 2) + (i & 1) >= n) o[i] = 0.0f;
+        }
+        if (out_f32) {
+          const int y = erow + 16 * rh;
+          float* d = static_cast<float*>(r.out.data) + b * r.out.sb + h * r.out.sh + y;
+#pragma unroll
+          for (int i = 0; i < C::kToks / 2; ++i) {
+            const int t = t0 + tok + 8 * (i >> 2) + (i & 1), c = 8 * ((i >> 1) & 1);
+            if (t < T_all && y + c < Dc) d[t * r.out.st + c] = o[i];
+          }
+        } else {
+          // tokens as rows again: blocks (channels, +8) x (tokens 16j, 16j + 8)
+          const int x = (erow - (lane >> 2)) + 16 * rh;  // the warp's first channel
+          unsigned char* tile = sP + (x >> 6) * kBoxBytes;
+#pragma unroll
+          for (int j = 0; j < C::kToks / 16; ++j) {
+            const int y = half * C::kToks + 16 * j + 8 * (lane >> 4) + (lane & 7);
+            const int piece = ((x & 63) >> 3) + ((lane >> 3) & 1);
+            stmatrix_t(tile + y * 128 + ((piece ^ (y & 7)) << 4),
+                       Elem<T>::from2(o[8 * j], o[8 * j + 1]), Elem<T>::from2(o[8 * j + 2], o[8 * j + 3]),
+                       Elem<T>::from2(o[8 * j + 4], o[8 * j + 5]), Elem<T>::from2(o[8 * j + 6], o[8 * j + 7]));
+          }
+        }
+      }
+    }
+
     fail |= wait_all(bar_u, u_phase);
     u_phase ^= 1;
-    if (third) {
-      put_values(Part2(), sW);
+    if (third) {  // what the two parts left of the decayed values
+#pragma unroll
+      for (int i = 0; i < kPieces; ++i) {
+        const int piece = i * NT + tid, y = (piece >> 3) & 63;
+        float v[8], hi[8], lo[8];
+        Elem<T>::load8(reinterpret_cast<const T*>(sC) + piece * 8, v);
+        Elem<T>::load8(reinterpret_cast<const T*>(sW) + piece * 8, hi);
+        Elem<T>::load8(reinterpret_cast<const T*>(sL) + piece * 8, lo);
+        const float w = pw[max(0, rev ? y + 1 : ex - y)];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e] = fmaf(v[e], w, -hi[e]) - lo[e];
+        Elem<T>::store8(reinterpret_cast<T*>(sW) + piece * 8, v);
+      }
       gemm::fence_async_smem();
       if (__syncthreads_or(fail)) break;
       if (tid == 0) {
@@ -517,60 +676,25 @@ bulk_wait_read_all();  // the last output has left sP
       u_phase ^= 1;
     }
     gemm::tc_fence_after();
-    if (tid == 32 && more) load_a(it + 1);
+    if (C::kLowInA && tid == 32 && more) load_a(it + 1);
     if (tid == 64 && more) load_b(it + 1);
+    if (tid == 96 && more && third && !states_only) load_c(it + 1);
     __syncwarp();
     const float decay = pw[ex];
 #pragma unroll
     for (int rh = 0; rh < C::kRowHalves; ++rh) {
       float u[C::kCols / 2];
-      tmem_ld_rows(t_upd + ((uint32_t)(16 * rh) << 16), u);
+      tmem_ld_rows(t_upd + t_quad + ((uint32_t)(16 * rh) << 16) + half * C::kCols, u);
 #pragma unroll
       for (int i = 0; i < C::kCols / 2; ++i) E[rh][i] = fmaf(decay, E[rh][i], u[i]);
     }
-    if (states_only) {
-      // the accumulator and the values are free once every thread is here
-      gemm::tc_fence_before();
-      if (__syncthreads_or(fail)) break;
-      if (tid == 96 && more) load_c(it + 1);
-      continue;
-    }
-    if (more) put_state((it + 1) & 1);
-
-    fail |= wait_all(bar_o, par);
-    gemm::tc_fence_after();
-    if (tid == 96 && more) load_c(it + 1);
-    __syncwarp();
-    {
-      float o[C::kCols / 2];
-      tmem_ld_rows(t_acc + half * C::kCols, o);
-      if (n < kChunk) {
-#pragma unroll
-        for (int i = 0; i < C::kCols / 2; ++i)
-          if (y0 + 8 * ((i >> 1) & 1) >= n) o[i] = 0.0f;
-      }
-      if (out_f32) {
-        float* d = static_cast<float*>(r.out.data) + b * r.out.sb + (int64_t)(t0 + y0) * r.out.st + h * r.out.sh;
-#pragma unroll
-        for (int i = 0; i < C::kCols / 2; i += 2) {
-          const int y = 8 * ((i >> 1) & 1), x = ecol + 8 * (i >> 2);
-          if (t0 + y0 + y < T_all && x < Dc)
-            *reinterpret_cast<float2*>(d + y * r.out.st + x) = make_float2(o[i], o[i + 1]);
-        }
-      } else {
-#pragma unroll
-        for (int k = 0; k < C::kCols / 8; ++k) {
-          const int x = half * C::kCols + 8 * k;
-          unsigned char* tile = sP + (x >> 6) * kBoxBytes;
-          put(tile, y0, (x & 63) >> 3, o[4 * k], o[4 * k + 1]);
-          put(tile, y0 + 8, (x & 63) >> 3, o[4 * k + 2], o[4 * k + 3]);
-        }
-      }
-    }
+    if (!states_only && more) put_state((it + 1) & 1);
     gemm::fence_async_smem();
     gemm::tc_fence_before();
     if (__syncthreads_or(fail)) break;
-    if (tid == 0 && !out_f32) {
+    if (states_only) {
+      if (tid == 96 && more) load_c(it + 1);
+    } else if (tid == 0 && !out_f32) {
 #pragma unroll
       for (int x = 0; x < DC / 64; ++x)
         tma_store_4d(&maps.out, sP + x * kBoxBytes, 64 * x, t0, ho, b);
@@ -594,7 +718,7 @@ bulk_wait_read_all();  // the last output has left sP
     const float f = rev ? scale : 1.0f;
     float* s_out = r.s_out + so;
     each_state([&](float& e, int y, int x) {
-      if (y < Da && x < Dc) s_out[y * s_row + x * s_col] = f * e;
+      if (y < Dc && x < Da) s_out[y * s_row + x * s_col] = f * e;
     });
   }
   if (!states_only) {
