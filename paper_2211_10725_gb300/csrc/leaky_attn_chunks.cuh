@@ -79,10 +79,13 @@ struct Cfg {
   // cost the fourth block of an SM) the place of a once it has been used
   static constexpr bool kLowInA = DA == 64 && DC == 64;
   static constexpr int kLowBytes = kLowInA ? 0 : kCBytes;
-  static constexpr int kOutBytes = kCBytes;        // decayed scores (8 KB), then the output
-  static constexpr int kTail = 2048;               // barriers, tables
+  // the decayed scores' buffer is the output's as well where smem is short
+  static constexpr bool kSharedOut = kLowInA;
+  static constexpr int kScoreBytes = kSharedOut ? 0 : kBoxBytes;
+  static constexpr int kOutBytes = kCBytes;
+  static constexpr int kTail = 1024;               // barriers, tables
   static constexpr size_t kSmem =
-      2 * kABytes + 2 * kCBytes + kLowBytes + kEBytes + kOutBytes + kTail;
+      2 * kABytes + 2 * kCBytes + kLowBytes + kEBytes + kScoreBytes + kOutBytes + kTail;
   // tensor memory: output, update (scores in its first 64 columns), state
   static constexpr uint32_t kTmemCols = kStateTmem ? 256 : (DA == 64 ? 128 : 256);
   static constexpr int kBlocksPerSm = kThreads == 128 ? 4 : 2;
@@ -188,14 +191,44 @@ __device__ __forceinline__ void stmatrix_t(void* row, uint32_t r0, uint32_t r1, 
                : "memory");
 }
 
-// D (tensor memory) [+]= A (tensor memory, K-major) * B (shared memory)
-__device__ __forceinline__ void tc_mma_ts(uint32_t tmem_d, uint32_t tmem_a, uint64_t bdesc,
-                                          uint32_t idesc, uint32_t accumulate) {
+// One lane of a whole warp.
+__device__ __forceinline__ uint32_t elect_one() {
+  uint32_t e;
   asm volatile(
-      "{\n\t.reg .pred p;\n\t"
-      "setp.ne.b32 p, %4, 0;\n\t"
-      "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}" ::"r"(tmem_d),
-      "r"(tmem_a), "l"(bdesc), "r"(idesc), "r"(accumulate)
+      "{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.u32 %0, 1, 0, p;\n\t}"
+      : "=r"(e));
+  return e;
+}
+
+// MMAs and commits of the elected lane, written for the whole warp: the
+// operands stay uniform across it, which the instruction wants (a lane of its
+// own would move each descriptor between register files, about 75 cycles an
+// MMA).  D (tensor memory) [+]= A * B with A and B in shared memory (ss) or A in
+// tensor memory, K-major (ts).
+__device__ __forceinline__ void mma_ss(uint32_t e, uint32_t d, uint64_t a, uint64_t b, uint32_t idesc,
+                                       uint32_t accumulate) {
+  asm volatile(
+      "{\n\t.reg .pred p, q;\n\t"
+      "setp.ne.b32 p, %4, 0;\n\tsetp.ne.b32 q, %5, 0;\n\t"
+      "@q tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}" ::"r"(d),
+      "l"(a), "l"(b), "r"(idesc), "r"(accumulate), "r"(e)
+      : "memory");
+}
+__device__ __forceinline__ void mma_ts(uint32_t e, uint32_t d, uint32_t a, uint64_t b, uint32_t idesc,
+                                       uint32_t accumulate) {
+  asm volatile(
+      "{\n\t.reg .pred p, q;\n\t"
+      "setp.ne.b32 p, %4, 0;\n\tsetp.ne.b32 q, %5, 0;\n\t"
+      "@q tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}" ::"r"(d),
+      "r"(a), "l"(b), "r"(idesc), "r"(accumulate), "r"(e)
+      : "memory");
+}
+__device__ __forceinline__ void mma_commit(uint32_t e, uint64_t* bar) {
+  asm volatile(
+      "{\n\t.reg .pred q;\n\tsetp.ne.b32 q, %1, 0;\n\t"
+      "@q tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];\n\t}" ::"r"(
+          smem_u32(bar)),
+      "r"(e)
       : "memory");
 }
 
@@ -269,6 +302,7 @@ __global__ void __launch_bounds__(Cfg<DA, DC>::kThreads, Cfg<DA, DC>::kBlocksPer
   using C = Cfg<DA, DC>;
   using T2 = typename Pair<T>::type;
   constexpr int NT = C::kThreads;
+  constexpr int kStorer = C::kSharedOut ? 0 : NT - 32;  // thread that issues and awaits the output's copies
   constexpr bool kHalf = std::is_same<T, __half>::value;
   extern __shared__ __align__(1024) unsigned char smem[];
   unsigned char* sA = smem;
@@ -277,18 +311,20 @@ __global__ void __launch_bounds__(Cfg<DA, DC>::kThreads, Cfg<DA, DC>::kBlocksPer
   unsigned char* sW = sC + C::kCBytes;                    // decayed values, high parts
   unsigned char* sL = C::kLowInA ? sA : sW + C::kCBytes;  // low parts
   unsigned char* sE = sW + C::kCBytes + C::kLowBytes;     // the state's copy (64-wide heads)
-  unsigned char* sP = sE + C::kEBytes;                    // decayed scores, then the output
-  uint64_t* bar = reinterpret_cast<uint64_t*>(sP + C::kOutBytes);
+  unsigned char* sP = sE + C::kEBytes;                    // decayed scores
+  unsigned char* sO = sP + C::kScoreBytes;                // the output
+  uint64_t* bar = reinterpret_cast<uint64_t*>(sO + C::kOutBytes);
   uint64_t *bar_a = bar, *bar_b = bar + 1, *bar_c = bar + 2, *bar_s = bar + 3, *bar_u = bar + 4,
            *bar_o = bar + 5, *bar_x = bar + 6;
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bar + 7);
   unsigned* top = reinterpret_cast<unsigned*>(bar + 8);  // [2] bits of the state's largest element
   float* seg_decay = reinterpret_cast<float*>(bar + 9);
-  T2* wt = reinterpret_cast<T2*>(bar + 10);       // [65][2] beta^n in two 16-bit parts
-  float* pw = reinterpret_cast<float*>(wt + 132);  // [65] beta^n
-  float* lag = pw + 68;  // [128] scaled weight of token j at token i, at i - j + 64
+  // beta^n at 64 + n (64 - n for a role backwards in time), n = 0 .. 64; zeros
+  // on the other side: the weight of token j at token i, at i - j + 64
+  float* lag = reinterpret_cast<float*>(bar + 10);  // [129]
+  T2* wt = reinterpret_cast<T2*>(lag + 129);        // [65] beta^n in two 16-bit parts
 
-  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  const int tid = threadIdx.x, warp = __shfl_sync(0xffffffffu, tid >> 5, 0), lane = tid & 31;
   const int quad = warp & 3, half = warp >> 2;
   const Args& g = p.g;
   const int role = blockIdx.x % g.nroles;
@@ -356,18 +392,15 @@ __global__ void __launch_bounds__(Cfg<DA, DC>::kThreads, Cfg<DA, DC>::kBlocksPer
     const float w = power(g.beta[h], tid <= kChunk ? tid : p.seg_tokens);
     if (tid <= kChunk) {
       const T hi = T(w), lo = T(w - (float)hi);
-      pw[tid] = w;
-      wt[2 * tid] = T2(hi, hi);
-      wt[2 * tid + 1] = T2(lo, lo);
+      wt[tid] = T2(hi, lo);
+      if (tid > 0) lag[rev ? 64 + tid : 64 - tid] = 0.0f;
+      lag[rev ? 64 - tid : 64 + tid] = w;
     } else {
       *seg_decay = w;
     }
   }
   __syncthreads();
-  if (tid < 128) {
-    const int n = rev ? 64 - tid : tid - 64;
-    lag[tid] = n >= 0 ? scale * pw[n] : 0.0f;
-  }
+  auto decay_of = [&](int n) { return lag[rev ? 64 - n : 64 + n]; };  // beta^n
 
   // this thread's part of the transposed state: channels erow + 16*rh (+8) of
   // c, columns ecol + 8k (+1) of a and b
@@ -398,7 +431,7 @@ __global__ void __launch_bounds__(Cfg<DA, DC>::kThreads, Cfg<DA, DC>::kBlocksPer
   each_state([&](float& e, int, int) { e = 0.0f; });
   if (order == 0 && (p.nseg == 1 || states_only)) {
     if (r.s_in && so >= 0) {
-      const float f = rev ? 1.0f / scale : (len > 0 ? pw[1] : 1.0f);
+      const float f = rev ? 1.0f / scale : (len > 0 ? decay_of(1) : 1.0f);
       const float* s_in = r.s_in + so;
       each_state([&](float& e, int y, int x) {
         if (y < Dc && x < Da) e = f * s_in[y * s_row + x * s_col];
@@ -484,32 +517,34 @@ __global__ void __launch_bounds__(Cfg<DA, DC>::kThreads, Cfg<DA, DC>::kBlocksPer
     const int ex = n - (last ? 1 : 0);
     const bool more = it + 1 < n_chunks;
 
-    if (!states_only) {
-      if (tid == 0) {
-        if (kHalf) top[(it + 1) & 1] = 0u;
-        fail |= !gemm::mbar_wait_poll(bar_a, par, kWaitNs);
-        fail |= !gemm::mbar_wait_poll(bar_b, par, kWaitNs);
-        gemm::tc_fence_after();
-        constexpr uint32_t id_s = idesc<T>(kChunk, kChunk, false, false);
-        constexpr uint32_t id_x = idesc<T>(DC, kChunk, false, false);
+    if (!states_only && warp == 0) {
+      if (kHalf && lane == 0) top[(it + 1) & 1] = 0u;
+      fail |= wait_all(bar_a, par);
+      fail |= wait_all(bar_b, par);
+      gemm::tc_fence_after();
+      const uint32_t e = elect_one();
+      constexpr uint32_t id_s = idesc<T>(kChunk, kChunk, false, false);
+      constexpr uint32_t id_x = idesc<T>(DC, kChunk, false, false);
 #pragma unroll
-        for (int kk = 0; kk < DA / 16; ++kk) {
-          const int off = (kk / 4) * kBoxBytes + (kk % 4) * 32;
-          gemm::tc_mma(t_upd, gemm::sdesc_sw128(sA + off), gemm::sdesc_sw128(sB + off), id_s, kk != 0);
-        }
-        gemm::tc_commit(bar_s);
-#pragma unroll
-        for (int kk = 0; kk < DA / 16; ++kk) {
-          const uint64_t q = gemm::sdesc_sw128(sA + (kk / 4) * kBoxBytes + (kk % 4) * 32);
-          if constexpr (C::kStateTmem)
-            tc_mma_ts(t_out, t_state + 8 * kk, q, id_x, kk != 0);
-          else
-            gemm::tc_mma(t_out, gemm::sdesc_sw128(sE + (kk / 4) * (DC * 128) + (kk % 4) * 32), q, id_x, kk != 0);
-        }
-        bulk_wait_read_all();  // the last output has left sP
-        gemm::tc_commit(bar_x);
+      for (int kk = 0; kk < DA / 16; ++kk) {
+        const int off = (kk / 4) * kBoxBytes + (kk % 4) * 32;
+        mma_ss(e, t_upd, gemm::sdesc_sw128(sA + off), gemm::sdesc_sw128(sB + off), id_s, kk != 0);
       }
-      __syncwarp();
+      mma_commit(e, bar_s);
+#pragma unroll
+      for (int kk = 0; kk < DA / 16; ++kk) {
+        const uint64_t q = gemm::sdesc_sw128(sA + (kk / 4) * kBoxBytes + (kk % 4) * 32);
+        if constexpr (C::kStateTmem)
+          mma_ts(e, t_out, t_state + 8 * kk, q, id_x, kk != 0);
+        else
+          mma_ss(e, t_out, gemm::sdesc_sw128(sE + (kk / 4) * (DC * 128) + (kk % 4) * 32), q, id_x, kk != 0);
+      }
+      if (C::kSharedOut) {
+        if (lane == 0) bulk_wait_read_all();  // the last output has left the scores' buffer
+        __syncwarp();
+        asm volatile("" ::: "memory");
+      }
+      mma_commit(e, bar_x);
     }
 
     // decayed values in two parts
@@ -523,7 +558,7 @@ __global__ void __launch_bounds__(Cfg<DA, DC>::kThreads, Cfg<DA, DC>::kBlocksPer
       uint4 v = reinterpret_cast<const uint4*>(sC)[piece], hi;
       if (n < kChunk && y >= n) v = make_uint4(0, 0, 0, 0);
       const int at = max(0, rev ? y + 1 : ex - y);
-      const T2 w1 = wt[2 * at], w2 = wt[2 * at + 1];
+      const T2 w = wt[at], w1 = T2(w.x, w.x), w2 = T2(w.y, w.y);
       const T2* vp = reinterpret_cast<const T2*>(&v);
       T2 *hp = reinterpret_cast<T2*>(&hi), *lp = reinterpret_cast<T2*>(&low[i]);
 #pragma unroll
@@ -533,8 +568,7 @@ __global__ void __launch_bounds__(Cfg<DA, DC>::kThreads, Cfg<DA, DC>::kBlocksPer
     }
 
     if (!states_only) {
-      // decayed scores; the first token's wait for the inter product is what
-      // frees sP of the last output
+      // decayed scores
       fail |= wait_all(bar_s, par);
       gemm::tc_fence_after();
       float s[C::kToks / 2];
@@ -542,20 +576,21 @@ __global__ void __launch_bounds__(Cfg<DA, DC>::kThreads, Cfg<DA, DC>::kBlocksPer
       const int x0 = half * C::kToks;
       const float* w = lag + 64 + y0 - x0 - 2 * (lane & 3);
 #pragma unroll
-      for (int i = 0; i < C::kToks / 2; ++i) s[i] *= w[8 * ((i >> 1) & 1) - 8 * (i >> 2) - (i & 1)];
+      for (int i = 0; i < C::kToks / 2; ++i) s[i] = s[i] * scale * w[8 * ((i >> 1) & 1) - 8 * (i >> 2) - (i & 1)];
       if (n < kChunk) {  // places past the sequence hold anything
 #pragma unroll
         for (int i = 0; i < C::kToks / 2; ++i)
           if (max(y0 + 8 * ((i >> 1) & 1), x0 + 2 * (lane & 3) + 8 * (i >> 2) + (i & 1)) >= n) s[i] = 0.0f;
       }
-      fail |= wait_all(bar_x, par);
-      gemm::tc_fence_after();
+      if (C::kSharedOut) fail |= wait_all(bar_x, par);
 #pragma unroll
       for (int k = 0; k < C::kToks / 8; ++k) {
         unsigned char* to = sP + y0 * 128 + ((((x0 >> 3) + k) ^ (y0 & 7)) << 4) + (lane & 3) * 4;
         *reinterpret_cast<uint32_t*>(to) = Elem<T>::from2(s[4 * k], s[4 * k + 1]);
         *reinterpret_cast<uint32_t*>(to + 1024) = Elem<T>::from2(s[4 * k + 2], s[4 * k + 3]);
       }
+      if (!C::kSharedOut) fail |= wait_all(bar_x, par);
+      gemm::tc_fence_after();
       if (!C::kLowInA && tid == 32 && more) load_a(it + 1);
       __syncwarp();
       // the inter product, decayed, is what the intra product adds to
@@ -563,7 +598,7 @@ __global__ void __launch_bounds__(Cfg<DA, DC>::kThreads, Cfg<DA, DC>::kBlocksPer
 #pragma unroll
       for (int i = 0; i < C::kToks / 4; ++i) {
         const int y = tok + 8 * (i >> 1) + (i & 1);
-        f[i] = e_back * lag[64 + (rev ? y + 1 - n : y)];
+        f[i] = e_back * scale * lag[64 + (rev ? y + 1 - n : y)];
       }
 #pragma unroll
       for (int rh = 0; rh < C::kRowHalves; ++rh) {
@@ -586,31 +621,32 @@ __global__ void __launch_bounds__(Cfg<DA, DC>::kThreads, Cfg<DA, DC>::kBlocksPer
       for (int i = tid; i < C::kCBytes / 16; i += NT)
         if (((i >> 3) & 63) >= n) reinterpret_cast<uint4*>(sC)[i] = z;
     }
+    if (!C::kSharedOut && tid == kStorer) bulk_wait_read_all();  // the last output has left sO
     gemm::fence_async_smem();
     gemm::tc_fence_before();
     if (__syncthreads_or(fail)) break;
 
-    auto update = [&](const unsigned char* values, uint32_t accumulate) {
+    auto update = [&](uint32_t e, const unsigned char* values, uint32_t accumulate) {
       constexpr uint32_t id = idesc<T>(DC, DA, true, true);
 #pragma unroll
       for (int kk = 0; kk < kChunk / 16; ++kk)
-        gemm::tc_mma(t_upd, sdesc_mn(values + kk * 2048, kBoxBytes), sdesc_mn(sB + kk * 2048, kBoxBytes),
-                     id, accumulate | (kk != 0));
+        mma_ss(e, t_upd, sdesc_mn(values + kk * 2048, kBoxBytes), sdesc_mn(sB + kk * 2048, kBoxBytes), id,
+               accumulate | (kk != 0));
     };
-    if (tid == 0) {
+    if (warp == 0) {
       gemm::tc_fence_after();
+      const uint32_t e = elect_one();
       if (!states_only) {
         constexpr uint32_t id = idesc<T>(DC, kChunk, true, false);
 #pragma unroll
         for (int kk = 0; kk < kChunk / 16; ++kk)
-          gemm::tc_mma(t_out, sdesc_mn(sC + kk * 2048, kBoxBytes), gemm::sdesc_sw128(sP + kk * 32), id, 1);
-        gemm::tc_commit(bar_o);
+          mma_ss(e, t_out, sdesc_mn(sC + kk * 2048, kBoxBytes), gemm::sdesc_sw128(sP + kk * 32), id, 1);
+        mma_commit(e, bar_o);
       }
-      update(sW, 0);
-      update(sL, 1);
-      gemm::tc_commit(bar_u);
+      update(e, sW, 0);
+      update(e, sL, 1);
+      mma_commit(e, bar_u);
     }
-    __syncwarp();
 
     if (!states_only) {
       fail |= wait_all(bar_o, par);
@@ -637,7 +673,7 @@ __global__ void __launch_bounds__(Cfg<DA, DC>::kThreads, Cfg<DA, DC>::kBlocksPer
         } else {
           // tokens as rows again: blocks (channels, +8) x (tokens 16j, 16j + 8)
           const int x = (erow - (lane >> 2)) + 16 * rh;  // the warp's first channel
-          unsigned char* tile = sP + (x >> 6) * kBoxBytes;
+          unsigned char* tile = sO + (x >> 6) * kBoxBytes;
 #pragma unroll
           for (int j = 0; j < C::kToks / 16; ++j) {
             const int y = half * C::kToks + 16 * j + 8 * (lane >> 4) + (lane & 7);
@@ -660,18 +696,18 @@ __global__ void __launch_bounds__(Cfg<DA, DC>::kThreads, Cfg<DA, DC>::kBlocksPer
         Elem<T>::load8(reinterpret_cast<const T*>(sC) + piece * 8, v);
         Elem<T>::load8(reinterpret_cast<const T*>(sW) + piece * 8, hi);
         Elem<T>::load8(reinterpret_cast<const T*>(sL) + piece * 8, lo);
-        const float w = pw[max(0, rev ? y + 1 : ex - y)];
+        const float w = decay_of(max(0, rev ? y + 1 : ex - y));
 #pragma unroll
         for (int e = 0; e < 8; ++e) v[e] = fmaf(v[e], w, -hi[e]) - lo[e];
         Elem<T>::store8(reinterpret_cast<T*>(sW) + piece * 8, v);
       }
       gemm::fence_async_smem();
       if (__syncthreads_or(fail)) break;
-      if (tid == 0) {
-        update(sW, 1);
-        gemm::tc_commit(bar_u);
+      if (warp == 0) {
+        const uint32_t e = elect_one();
+        update(e, sW, 1);
+        mma_commit(e, bar_u);
       }
-      __syncwarp();
       fail |= wait_all(bar_u, u_phase);
       u_phase ^= 1;
     }
@@ -680,7 +716,7 @@ __global__ void __launch_bounds__(Cfg<DA, DC>::kThreads, Cfg<DA, DC>::kBlocksPer
     if (tid == 64 && more) load_b(it + 1);
     if (tid == 96 && more && third && !states_only) load_c(it + 1);
     __syncwarp();
-    const float decay = pw[ex];
+    const float decay = decay_of(ex);
 #pragma unroll
     for (int rh = 0; rh < C::kRowHalves; ++rh) {
       float u[C::kCols / 2];
@@ -694,10 +730,10 @@ __global__ void __launch_bounds__(Cfg<DA, DC>::kThreads, Cfg<DA, DC>::kBlocksPer
     if (__syncthreads_or(fail)) break;
     if (states_only) {
       if (tid == 96 && more) load_c(it + 1);
-    } else if (tid == 0 && !out_f32) {
+    } else if (tid == kStorer && !out_f32) {
 #pragma unroll
       for (int x = 0; x < DC / 64; ++x)
-        tma_store_4d(&maps.out, sP + x * kBoxBytes, 64 * x, t0, ho, b);
+        tma_store_4d(&maps.out, sO + x * kBoxBytes, 64 * x, t0, ho, b);
       gemm::bulk_commit();
     }
   }
@@ -731,7 +767,7 @@ __global__ void __launch_bounds__(Cfg<DA, DC>::kThreads, Cfg<DA, DC>::kBlocksPer
       *reinterpret_cast<uint4*>(o + ((from + i / pieces) * r.out.st + (i % pieces) * per) * es) =
           make_uint4(0, 0, 0, 0);
   }
-  if (tid == 0) gemm::bulk_wait_all();
+  if (tid == kStorer) gemm::bulk_wait_all();
   gemm::tc_fence_before();
   __syncthreads();
   if (warp == 0) {
