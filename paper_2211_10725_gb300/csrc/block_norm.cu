@@ -9,11 +9,13 @@
 //   grad_a = rstd_a (m - h mean_group(m h)),  h = a rstd_a,  m = d s act(z) w_post
 //   grad_w_post = sum d s act(z) h;  grad_s = sum d n act(z);  grad_w_pre = sum grad_y e
 // Every tensor is read and written once: the bound is HBM.  A row stays in
-// the registers of one warp (short rows) or one block; the parameters and
-// their gradients' partial sums stay in the registers of the thread that owns
-// the columns, over all the rows its block takes, so the sums over rows need
-// one [blocks, 3, N] array of partials and a second kernel that adds them in
-// block order (no atomics: the same bits on every call).
+// the registers of one warp (short rows) or one block, eight channels to a
+// thread; blocks stay on the GPU and take rows in turn, with the next row's
+// loads in flight while the sums of the present one meet.  The parameters'
+// gradients gather in the registers (long rows: in shared memory) of the
+// thread that owns the channels over all the rows of its block, so the sums
+// over rows need one [blocks, 3, N] array of partials and a second kernel
+// that adds them in block order (no atomics: the same bits on every call).
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 #include <cuda_runtime.h>
@@ -22,6 +24,7 @@
 #include <cstdint>
 
 #include "launch.cuh"
+#include "scan_host.cuh"
 #include "snn.h"
 #include "snn_device.cuh"
 
@@ -29,10 +32,8 @@ namespace snn {
 namespace norm {
 
 constexpr int64_t kMaxN = 8192;
-constexpr int kMaxThreads = 512;
-// Blocks whose partial sums of the parameter gradients are added: a
-// constant, so that a shape always sums in the same order.
-constexpr int64_t kBwdBlocks = 304;
+constexpr int kSms = 152;
+constexpr int E = 8;  // channels of a thread
 
 struct Rows {
   void* data;
@@ -49,44 +50,50 @@ struct Args {
   float* part;                // [blocks][3][N]
 };
 
-__device__ __forceinline__ float sigmoidf_(float z) { return 1.0f / (1.0f + __expf(-z)); }
+__device__ __forceinline__ float sigmoidf_(float z) { return __fdividef(1.0f, 1.0f + __expf(-z)); }
 
-// Element e of thread t's share of a row: eight consecutive ones per vector
+// A thread's share of a row as it lies in memory: eight consecutive channels
 // (VEC), else every TPR-th.
-template <bool VEC, int TPR>
-__device__ __forceinline__ int column(int t, int e) {
-  return VEC ? ((e >> 3) * TPR + t) * 8 + (e & 7) : e * TPR + t;
-}
+template <typename T, bool VEC, int TPR>
+struct Share {
+  static constexpr int kWords = E * sizeof(T) / 16;
+  uint4 w[VEC ? kWords : 1];
+  T x[VEC ? 1 : E];
 
-template <typename T, bool VEC, int TPR, int E>
-__device__ __forceinline__ void load_row(const Rows& x, int64_t row, int N, int t, float v[E]) {
-  const T* p = static_cast<const T*>(x.data) + row * x.ld;
-  if constexpr (VEC) {
+  __device__ __forceinline__ void load(const Rows& m, int64_t row, int N, int t) {
+    const T* p = static_cast<const T*>(m.data) + row * m.ld;
+    if constexpr (VEC) {
+      if (t * E < N) {
 #pragma unroll
-    for (int j = 0; j < E / 8; ++j) {
-      const int c = (j * TPR + t) * 8;
-      if (c < N) {
-        Elem<T>::load8(p + c, v + 8 * j);
+        for (int i = 0; i < kWords; ++i) w[i] = reinterpret_cast<const uint4*>(p + t * E)[i];
+      }
+    } else {
+#pragma unroll
+      for (int e = 0; e < E; ++e)
+        if (e * TPR + t < N) x[e] = p[e * TPR + t];
+    }
+  }
+  // in 32 bits, zero past N
+  __device__ __forceinline__ void get(int N, int t, float v[E]) const {
+    if constexpr (VEC) {
+      if (t * E < N) {
+        Elem<T>::load8(reinterpret_cast<const T*>(w), v);
       } else {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) v[8 * j + i] = 0.0f;
+        for (int e = 0; e < E; ++e) v[e] = 0.0f;
       }
-    }
-  } else {
+    } else {
 #pragma unroll
-    for (int e = 0; e < E; ++e) v[e] = e * TPR + t < N ? Elem<T>::load1(p + e * TPR + t) : 0.0f;
+      for (int e = 0; e < E; ++e) v[e] = e * TPR + t < N ? (float)x[e] : 0.0f;
+    }
   }
-}
+};
 
-template <typename T, bool VEC, int TPR, int E>
-__device__ __forceinline__ void store_row(const Rows& x, int64_t row, int N, int t, const float v[E]) {
-  T* p = static_cast<T*>(x.data) + row * x.ld;
+template <typename T, bool VEC, int TPR>
+__device__ __forceinline__ void store_row(const Rows& m, int64_t row, int N, int t, const float v[E]) {
+  T* p = static_cast<T*>(m.data) + row * m.ld;
   if constexpr (VEC) {
-#pragma unroll
-    for (int j = 0; j < E / 8; ++j) {
-      const int c = (j * TPR + t) * 8;
-      if (c < N) Elem<T>::store8(p + c, v + 8 * j);
-    }
+    if (t * E < N) Elem<T>::store8(p + t * E, v);
   } else {
 #pragma unroll
     for (int e = 0; e < E; ++e)
@@ -95,37 +102,53 @@ __device__ __forceinline__ void store_row(const Rows& x, int64_t row, int N, int
 }
 
 // A parameter's share (ones where it is absent, zero past N).
-template <bool VEC, int TPR, int E>
+template <bool VEC, int TPR>
 __device__ __forceinline__ void load_param(const float* p, int N, int t, float v[E]) {
+  if (VEC && p && t * E < N) {
+    Elem<float>::load8(p + t * E, v);
+    return;
+  }
 #pragma unroll
   for (int e = 0; e < E; ++e) {
-    const int c = column<VEC, TPR>(t, e);
+    const int c = VEC ? t * E + e : e * TPR + t;
     v[e] = c < N ? (p ? p[c] : 1.0f) : 0.0f;
   }
 }
 
-// Sums of two values over the TPR threads of a row; every thread gets them.
+// Sums of K values over the TPR threads of a row; every thread gets them.
+// Successive sums alternate between two scratch buffers, so one barrier a sum
+// is enough: a warp cannot be two sums ahead.
 template <int TPR>
-__device__ __forceinline__ float2 row_sum(float2 v, float2* scratch) {
+struct RowSum {
+  float4 (*scratch)[32];  // [2][warps]
+  int turn = 0;
+  template <int K>
+  __device__ __forceinline__ void operator()(float (&v)[K]) {
 #pragma unroll
-  for (int o = 16; o > 0; o >>= 1) {
-    v.x += __shfl_xor_sync(0xffffffffu, v.x, o);
-    v.y += __shfl_xor_sync(0xffffffffu, v.y, o);
-  }
-  if constexpr (TPR > 32) {
-    constexpr int W = TPR / 32;
-    __syncthreads();  // the last call's reads are done
-    if ((threadIdx.x & 31) == 0) scratch[threadIdx.x >> 5] = v;
-    __syncthreads();
-    v = scratch[0];
+    for (int o = 16; o > 0; o >>= 1)
 #pragma unroll
-    for (int w = 1; w < W; ++w) {
-      v.x += scratch[w].x;
-      v.y += scratch[w].y;
+      for (int k = 0; k < K; ++k) v[k] += __shfl_xor_sync(0xffffffffu, v[k], o);
+    if constexpr (TPR > 32) {
+      constexpr int W = TPR / 32;
+      float4* s = scratch[turn];
+      turn ^= 1;
+      if ((threadIdx.x & 31) == 0)
+        s[threadIdx.x >> 5] = make_float4(v[0], K > 1 ? v[K > 1] : 0.f, K > 2 ? v[K > 2 ? 2 : 0] : 0.f, 0.f);
+      __syncthreads();
+      float4 a = s[0];
+#pragma unroll
+      for (int w = 1; w < W; ++w) {
+        const float4 x = s[w];
+        a.x += x.x;
+        if (K > 1) a.y += x.y;
+        if (K > 2) a.z += x.z;
+      }
+      v[0] = a.x;
+      if (K > 1) v[K > 1] = a.y;
+      if (K > 2) v[K > 2 ? 2 : 0] = a.z;
     }
   }
-  return v;
-}
+};
 
 // Sum over the group of `lanes` neighbouring threads that a vector lies in.
 __device__ __forceinline__ float group_sum(float v, int lanes) {
@@ -133,220 +156,282 @@ __device__ __forceinline__ float group_sum(float v, int lanes) {
   return v;
 }
 
-// Factor 1/rms of every element of a: over the row, or over its group (VEC;
-// each of a thread's vectors lies in one group of group/8 threads).
-template <int E>
-struct Factors {
-  float f[E / 8];
-  __device__ __forceinline__ float at(int e) const { return f[e >> 3]; }
-};
+template <int TPR>
+constexpr int kBlockThreads = TPR == 32 ? 256 : TPR;  // short rows: eight warps, a row each
 
-template <typename T, typename R, bool VEC, int TPR, int E>
-__global__ void __launch_bounds__(TPR < 256 ? 256 : TPR) norm_fwd(const Args g) {
-  constexpr int kRowsPerBlock = TPR == 32 ? 8 : 1;
-  __shared__ float2 scratch[TPR / 32];
+// Registers: two blocks of 512 threads (or as many smaller ones) on an SM,
+// one of 1024.
+template <typename T, typename R, bool VEC, int TPR>
+__global__ void __launch_bounds__(kBlockThreads<TPR>, 1024 / kBlockThreads<TPR>) norm_fwd(const Args g) {
+  __shared__ float4 scratch[2][32];
   grid_dep_wait();
-  const int t = threadIdx.x % TPR;
-  const int64_t row0 = (int64_t)blockIdx.x * kRowsPerBlock + threadIdx.x / TPR;
-  const bool whole = g.group == g.N;
-  const float inv_n = 1.0f / (float)g.N, inv_g = 1.0f / (float)g.group;
-  for (int64_t row = row0; row < g.M; row += (int64_t)gridDim.x * kRowsPerBlock) {
-    float x[E], w[E];
-    load_row<R, VEC, TPR, E>(g.r, row, g.N, t, x);
-    if (g.a.data) {
-      float a[E];
-      load_row<T, VEC, TPR, E>(g.a, row, g.N, t, a);
-      Factors<E> rs;
-      if (whole) {
-        float2 ss = make_float2(0.f, 0.f);
+  constexpr int kTeams = kBlockThreads<TPR> / TPR;
+  const int t = threadIdx.x % TPR, N = g.N;
+  const int64_t step = (int64_t)gridDim.x * kTeams;
+  int64_t row = (int64_t)blockIdx.x * kTeams + threadIdx.x / TPR;
+  const bool whole = g.group == N, block = g.a.data != nullptr, gated = g.z.data != nullptr;
+  const float inv_n = 1.0f / (float)N, inv_g = 1.0f / (float)g.group;
+  RowSum<TPR> row_sum{scratch};
+  float w_post[E], w_pre[E];
+  load_param<VEC, TPR>(g.w_pre, N, t, w_pre);
+  if (block) {  // s n act(z): the two factors of a channel as one
+    float sc[E];
+    load_param<VEC, TPR>(g.w_post, N, t, w_post);
+    load_param<VEC, TPR>(g.scale, N, t, sc);
 #pragma unroll
-        for (int e = 0; e < E; ++e) ss.x = fmaf(a[e], a[e], ss.x);
-        ss = row_sum<TPR>(ss, scratch);
+    for (int e = 0; e < E; ++e) w_post[e] *= sc[e];
+  }
+  Share<R, VEC, TPR> r;
+  Share<T, VEC, TPR> a, z;
+  auto fetch = [&](int64_t i) {
+    r.load(g.r, i, N, t);
+    if (block) a.load(g.a, i, N, t);
+    if (gated) z.load(g.z, i, N, t);
+  };
+  if (row < g.M) fetch(row);
+  for (; row < g.M; row += step) {
+    float x[E], u[E], sg[E];
+    r.get(N, t, x);
+    if (block) a.get(N, t, u);
+    if (gated) z.get(N, t, sg);
+    if (row + step < g.M) fetch(row + step);
+    if (block) {
+      float ss[1] = {0.0f};
 #pragma unroll
-        for (int j = 0; j < E / 8; ++j) rs.f[j] = rsqrtf(fmaf(ss.x, inv_n, g.eps));
-      } else {
+      for (int e = 0; e < E; ++e) ss[0] = fmaf(u[e], u[e], ss[0]);
+      if (whole) row_sum(ss);
+      else ss[0] = group_sum(ss[0], g.group >> 3);
+      const float rstd = rsqrtf(fmaf(ss[0], whole ? inv_n : inv_g, g.eps));
 #pragma unroll
-        for (int j = 0; j < E / 8; ++j) {
-          float ss = 0.f;
-#pragma unroll
-          for (int i = 0; i < 8; ++i) ss = fmaf(a[8 * j + i], a[8 * j + i], ss);
-          rs.f[j] = rsqrtf(fmaf(group_sum(ss, g.group >> 3), inv_g, g.eps));
+      for (int e = 0; e < E; ++e) {
+        u[e] = u[e] * rstd * w_post[e];
+        if (gated) {
+          const float s = sigmoidf_(sg[e]);
+          u[e] *= g.gate == SNN_GATE_SILU ? sg[e] * s : s;
         }
+        x[e] += u[e];
       }
-      load_param<VEC, TPR, E>(g.w_post, g.N, t, w);
-#pragma unroll
-      for (int e = 0; e < E; ++e) a[e] = a[e] * rs.at(e) * w[e];
-      load_param<VEC, TPR, E>(g.scale, g.N, t, w);
-      if (g.z.data) {
-        float z[E];
-        load_row<T, VEC, TPR, E>(g.z, row, g.N, t, z);
-#pragma unroll
-        for (int e = 0; e < E; ++e) {
-          const float sg = sigmoidf_(z[e]);
-          a[e] *= g.gate == SNN_GATE_SILU ? z[e] * sg : sg;
-        }
-      }
-#pragma unroll
-      for (int e = 0; e < E; ++e) x[e] = fmaf(w[e], a[e], x[e]);
-      store_row<R, VEC, TPR, E>(g.ro, row, g.N, t, x);
+      store_row<R, VEC, TPR>(g.ro, row, N, t, x);
     }
     if (g.y.data) {
-      float2 ss = make_float2(0.f, 0.f);
+      float ss[1] = {0.0f};
 #pragma unroll
-      for (int e = 0; e < E; ++e) ss.x = fmaf(x[e], x[e], ss.x);
-      ss = row_sum<TPR>(ss, scratch);
-      const float rstd = rsqrtf(fmaf(ss.x, inv_n, g.eps));
-      load_param<VEC, TPR, E>(g.w_pre, g.N, t, w);
+      for (int e = 0; e < E; ++e) ss[0] = fmaf(x[e], x[e], ss[0]);
+      row_sum(ss);
+      const float rstd = rsqrtf(fmaf(ss[0], inv_n, g.eps));
 #pragma unroll
-      for (int e = 0; e < E; ++e) x[e] = x[e] * rstd * w[e];
-      store_row<T, VEC, TPR, E>(g.y, row, g.N, t, x);
+      for (int e = 0; e < E; ++e) x[e] = x[e] * rstd * w_pre[e];
+      store_row<T, VEC, TPR>(g.y, row, N, t, x);
     }
   }
 }
 
-template <typename T, typename R, bool VEC, int TPR, int E>
-__global__ void __launch_bounds__(TPR < 256 ? 256 : TPR) norm_bwd(const Args g) {
-  constexpr int kRowsPerBlock = TPR == 32 ? 8 : 1;
-  __shared__ float2 scratch[TPR / 32];
-  grid_dep_wait();
-  const int t = threadIdx.x % TPR;
-  const int64_t row0 = (int64_t)blockIdx.x * kRowsPerBlock + threadIdx.x / TPR;
-  const bool whole = g.group == g.N;
-  const float inv_n = 1.0f / (float)g.N, inv_g = 1.0f / (float)g.group;
-  float d_post[E], d_scale[E], d_pre[E];
+// The parameters' gradients of a thread's channels over its rows: in registers,
+// or (ROW in shared memory, [3][E / 4][threads] float4) for long rows.
+template <bool SMEM, int THREADS>
+struct Gather {
+  float v[SMEM ? 1 : 3][E];
+  __device__ __forceinline__ float4* at(int k, int i) {
+    extern __shared__ float4 gather_smem[];
+    return gather_smem + (k * (E / 4) + i) * THREADS + threadIdx.x;
+  }
+  __device__ __forceinline__ void clear() {
+    if constexpr (SMEM) {
 #pragma unroll
-  for (int e = 0; e < E; ++e) d_post[e] = d_scale[e] = d_pre[e] = 0.0f;
-  for (int64_t row = row0; row < g.M; row += (int64_t)gridDim.x * kRowsPerBlock) {
-    float d[E], w[E];
-    if (g.gro.data) {
-      load_row<R, VEC, TPR, E>(g.gro, row, g.N, t, d);
+      for (int k = 0; k < 3; ++k)
+        for (int i = 0; i < E / 4; ++i) *at(k, i) = make_float4(0.f, 0.f, 0.f, 0.f);
+    } else {
+#pragma unroll
+      for (int k = 0; k < 3; ++k)
+        for (int e = 0; e < E; ++e) v[k][e] = 0.0f;
+    }
+  }
+  __device__ __forceinline__ void add(int k, const float (&a)[E], const float (&b)[E]) {  // += a b
+    if constexpr (SMEM) {
+#pragma unroll
+      for (int i = 0; i < E / 4; ++i) {
+        float4 s = *at(k, i);
+        s.x = fmaf(a[4 * i], b[4 * i], s.x);
+        s.y = fmaf(a[4 * i + 1], b[4 * i + 1], s.y);
+        s.z = fmaf(a[4 * i + 2], b[4 * i + 2], s.z);
+        s.w = fmaf(a[4 * i + 3], b[4 * i + 3], s.w);
+        *at(k, i) = s;
+      }
+    } else {
+#pragma unroll
+      for (int e = 0; e < E; ++e) v[k][e] = fmaf(a[e], b[e], v[k][e]);
+    }
+  }
+  __device__ __forceinline__ void get(int k, float (&a)[E]) {
+    if constexpr (SMEM) {
+#pragma unroll
+      for (int i = 0; i < E / 4; ++i) {
+        const float4 s = *at(k, i);
+        a[4 * i] = s.x;
+        a[4 * i + 1] = s.y;
+        a[4 * i + 2] = s.z;
+        a[4 * i + 3] = s.w;
+      }
+    } else {
+#pragma unroll
+      for (int e = 0; e < E; ++e) a[e] = v[k][e];
+    }
+  }
+};
+
+template <typename T, typename R, bool VEC, int TPR>
+__global__ void __launch_bounds__(kBlockThreads<TPR>, TPR == 1024 ? 1 : 512 / kBlockThreads<TPR>)
+    norm_bwd(const Args g) {
+  __shared__ float4 scratch[2][32];
+  grid_dep_wait();
+  constexpr int kTeams = kBlockThreads<TPR> / TPR;
+  const int t = threadIdx.x % TPR, team = threadIdx.x / TPR, N = g.N;
+  const int64_t step = (int64_t)gridDim.x * kTeams;
+  int64_t row = (int64_t)blockIdx.x * kTeams + team;
+  const bool whole = g.group == N, block = g.a.data != nullptr, gated = g.z.data != nullptr;
+  const bool pre = g.gy.data != nullptr, through = g.gro.data != nullptr;
+  const float inv_n = 1.0f / (float)N, inv_g = 1.0f / (float)g.group;
+  RowSum<TPR> row_sum{scratch};
+  Gather<TPR == 1024, TPR> sums;  // of w_post, the residual scale, w_pre
+  sums.clear();
+  Share<R, VEC, TPR> ro, gro;
+  Share<T, VEC, TPR> gy, a, z;
+  auto fetch = [&](int64_t i) {
+    if (pre) ro.load(g.ro, i, N, t);
+    if (pre) gy.load(g.gy, i, N, t);
+    if (through) gro.load(g.gro, i, N, t);
+    if (block) a.load(g.a, i, N, t);
+    if (gated) z.load(g.z, i, N, t);
+  };
+  // long rows have not the registers to hold a row ahead
+  constexpr bool kAhead = TPR < 1024;
+  if (kAhead && row < g.M) fetch(row);
+  for (; row < g.M; row += step) {
+    if (!kAhead) fetch(row);
+    float d[E], x[E], gw[E], h[E], zz[E], w[E];
+    if (pre) ro.get(N, t, x);
+    if (pre) gy.get(N, t, gw);
+    if (block) a.get(N, t, h);
+    if (gated) z.get(N, t, zz);
+    if (through) {
+      gro.get(N, t, d);
     } else {
 #pragma unroll
       for (int e = 0; e < E; ++e) d[e] = 0.0f;
     }
-    if (g.gy.data) {
-      float x[E], gy[E];
-      load_row<R, VEC, TPR, E>(g.ro, row, g.N, t, x);
-      load_row<T, VEC, TPR, E>(g.gy, row, g.N, t, gy);
-      load_param<VEC, TPR, E>(g.w_pre, g.N, t, w);
-      float2 ss = make_float2(0.f, 0.f);
+    if (kAhead && row + step < g.M) fetch(row + step);
+    float ss[3] = {0.0f, 0.0f, 0.0f};  // of r'^2, grad_y w_pre r', a^2
+    if (pre) {
+      load_param<VEC, TPR>(g.w_pre, N, t, w);
 #pragma unroll
       for (int e = 0; e < E; ++e) {
-        ss.x = fmaf(x[e], x[e], ss.x);
-        ss.y = fmaf(gy[e] * w[e], x[e], ss.y);
-      }
-      ss = row_sum<TPR>(ss, scratch);
-      const float rstd = rsqrtf(fmaf(ss.x, inv_n, g.eps));
-      const float mean = ss.y * rstd * inv_n;  // mean of (grad_y w_pre) e
-#pragma unroll
-      for (int e = 0; e < E; ++e) {
-        const float h = x[e] * rstd;
-        d[e] = fmaf(rstd, fmaf(-h, mean, gy[e] * w[e]), d[e]);
-        d_pre[e] = fmaf(gy[e], h, d_pre[e]);
+        ss[0] = fmaf(x[e], x[e], ss[0]);
+        ss[1] = fmaf(gw[e] * w[e], x[e], ss[1]);
       }
     }
-    if (g.gr.data) store_row<R, VEC, TPR, E>(g.gr, row, g.N, t, d);
-    if (!g.a.data) continue;
-    float a[E], sc[E];
-    load_row<T, VEC, TPR, E>(g.a, row, g.N, t, a);
-    load_param<VEC, TPR, E>(g.w_post, g.N, t, w);
-    load_param<VEC, TPR, E>(g.scale, g.N, t, sc);
-    Factors<E> rs;
-    float2 ss = make_float2(0.f, 0.f);
+    if (block) {
 #pragma unroll
-    for (int e = 0; e < E; ++e) ss.x = fmaf(a[e], a[e], ss.x);
-    if (whole) {
-      ss = row_sum<TPR>(ss, scratch);
-#pragma unroll
-      for (int j = 0; j < E / 8; ++j) rs.f[j] = rsqrtf(fmaf(ss.x, inv_n, g.eps));
-    } else {
-#pragma unroll
-      for (int j = 0; j < E / 8; ++j) {
-        float q = 0.f;
-#pragma unroll
-        for (int i = 0; i < 8; ++i) q = fmaf(a[8 * j + i], a[8 * j + i], q);
-        rs.f[j] = rsqrtf(fmaf(group_sum(q, g.group >> 3), inv_g, g.eps));
-      }
+      for (int e = 0; e < E; ++e) ss[2] = fmaf(h[e], h[e], ss[2]);
+      if (!whole) ss[2] = group_sum(ss[2], g.group >> 3);
     }
-    // a <- h = a rstd_a;  d <- m = d s act w_post
-    if (g.z.data) {
-      float z[E];
-      load_row<T, VEC, TPR, E>(g.z, row, g.N, t, z);
+    const float in_group = ss[2];
+    row_sum(ss);
+    if (pre) {
+      const float rstd = rsqrtf(fmaf(ss[0], inv_n, g.eps));
+      const float mean = ss[1] * rstd * inv_n;  // mean of (grad_y w_pre) y'
 #pragma unroll
-      for (int e = 0; e < E; ++e) {
-        const float sg = sigmoidf_(z[e]);
-        const float act = g.gate == SNN_GATE_SILU ? z[e] * sg : sg;
-        const float slope = g.gate == SNN_GATE_SILU ? sg * fmaf(z[e], 1.0f - sg, 1.0f) : sg * (1.0f - sg);
-        a[e] *= rs.at(e);
-        const float n = a[e] * w[e];
-        z[e] = d[e] * sc[e] * n * slope;
-        d_scale[e] = fmaf(d[e], n * act, d_scale[e]);
-        const float dn = d[e] * sc[e] * act;
-        d_post[e] = fmaf(dn, a[e], d_post[e]);
-        d[e] = dn * w[e];
-      }
-      if (g.gz.data) store_row<T, VEC, TPR, E>(g.gz, row, g.N, t, z);
-    } else {
+      for (int e = 0; e < E; ++e) x[e] *= rstd;  // y'
+      sums.add(2, gw, x);
 #pragma unroll
-      for (int e = 0; e < E; ++e) {
-        a[e] *= rs.at(e);
-        d_scale[e] = fmaf(d[e], a[e] * w[e], d_scale[e]);
-        const float dn = d[e] * sc[e];
-        d_post[e] = fmaf(dn, a[e], d_post[e]);
-        d[e] = dn * w[e];
-      }
+      for (int e = 0; e < E; ++e) d[e] = fmaf(rstd, fmaf(-x[e], mean, gw[e] * w[e]), d[e]);
     }
+    if (g.gr.data) store_row<R, VEC, TPR>(g.gr, row, N, t, d);
+    if (!block) continue;
+    const float rstd_a = rsqrtf(whole ? fmaf(ss[2], inv_n, g.eps) : fmaf(in_group, inv_g, g.eps));
+    load_param<VEC, TPR>(g.w_post, N, t, w);
+    load_param<VEC, TPR>(g.scale, N, t, gw);
+#pragma unroll
+    for (int e = 0; e < E; ++e) {
+      h[e] *= rstd_a;
+      float act = 1.0f, slope = 0.0f;
+      if (gated) {
+        const float s = sigmoidf_(zz[e]);
+        act = g.gate == SNN_GATE_SILU ? zz[e] * s : s;
+        slope = g.gate == SNN_GATE_SILU ? s * fmaf(zz[e], 1.0f - s, 1.0f) : s * (1.0f - s);
+      }
+      const float n = h[e] * w[e];
+      zz[e] = d[e] * gw[e] * n * slope;  // grad_z
+      x[e] = n * act;
+      gw[e] *= d[e] * act;               // gradient of n
+    }
+    sums.add(1, d, x);
+    sums.add(0, gw, h);
+    if (g.gz.data) store_row<T, VEC, TPR>(g.gz, row, N, t, zz);
     if (!g.ga.data) continue;
-    if (whole) {
-      ss = make_float2(0.f, 0.f);
+    float q[1] = {0.0f};
 #pragma unroll
-      for (int e = 0; e < E; ++e) ss.x = fmaf(d[e], a[e], ss.x);
-      ss = row_sum<TPR>(ss, scratch);
-#pragma unroll
-      for (int e = 0; e < E; ++e) d[e] = rs.at(e) * fmaf(-a[e], ss.x * inv_n, d[e]);
-    } else {
-#pragma unroll
-      for (int j = 0; j < E / 8; ++j) {
-        float q = 0.f;
-#pragma unroll
-        for (int i = 0; i < 8; ++i) q = fmaf(d[8 * j + i], a[8 * j + i], q);
-        q = group_sum(q, g.group >> 3) * inv_g;
-#pragma unroll
-        for (int i = 0; i < 8; ++i) d[8 * j + i] = rs.f[j] * fmaf(-a[8 * j + i], q, d[8 * j + i]);
-      }
+    for (int e = 0; e < E; ++e) {
+      gw[e] *= w[e];
+      q[0] = fmaf(gw[e], h[e], q[0]);
     }
-    store_row<T, VEC, TPR, E>(g.ga, row, g.N, t, d);
+    if (whole) row_sum(q);
+    else q[0] = group_sum(q[0], g.group >> 3);
+    const float mean = q[0] * (whole ? inv_n : inv_g);
+#pragma unroll
+    for (int e = 0; e < E; ++e) gw[e] = rstd_a * fmaf(-h[e], mean, gw[e]);
+    store_row<T, VEC, TPR>(g.ga, row, N, t, gw);
   }
   if (!g.part) return;
-  // one row of partials per row team
-  float* p = g.part + ((int64_t)blockIdx.x * kRowsPerBlock + threadIdx.x / TPR) * 3 * g.N;
+  float* p = g.part + (int64_t)blockIdx.x * 3 * N;
+  if constexpr (kTeams > 1) {  // the block's teams, in order
+    __shared__ float all[kTeams][3][TPR * E];
 #pragma unroll
-  for (int e = 0; e < E; ++e) {
-    const int c = column<VEC, TPR>(t, e);
-    if (c < g.N) {
-      p[c] = d_post[e];
-      p[g.N + c] = d_scale[e];
-      p[2 * g.N + c] = d_pre[e];
+    for (int k = 0; k < 3; ++k) {
+      float v[E];
+      sums.get(k, v);
+#pragma unroll
+      for (int e = 0; e < E; ++e) all[team][k][VEC ? t * E + e : e * TPR + t] = v[e];
+    }
+    __syncthreads();
+    for (int i = threadIdx.x; i < 3 * N; i += kBlockThreads<TPR>) {
+      const int k = i / N, c = i - k * N;
+      float v = all[0][k][c];
+#pragma unroll
+      for (int j = 1; j < kTeams; ++j) v += all[j][k][c];
+      p[i] = v;
+    }
+  } else {
+#pragma unroll
+    for (int k = 0; k < 3; ++k) {
+      float v[E];
+      sums.get(k, v);
+#pragma unroll
+      for (int e = 0; e < E; ++e) {
+        const int c = VEC ? t * E + e : e * TPR + t;
+        if (c < N) p[k * N + c] = v[e];
+      }
     }
   }
 }
 
-// Column sums of the partials, in row order within each of 8 slices, then
-// over the slices in order.
-__global__ void __launch_bounds__(256) norm_sum(const float* __restrict__ part, int rows, int N,
-                                                float* o0, float* o1, float* o2) {
-  __shared__ float s[8][32];
+// Column sums of the partials: 32 columns a block, the rows in 32 slices (every
+// 32nd row, in order), then the slices in order.
+__global__ void __launch_bounds__(1024) norm_sum(const float* __restrict__ part, int rows, int N,
+                                                 float* o0, float* o1, float* o2) {
+  __shared__ float s[32][33];
   grid_dep_wait();
   const int64_t c = (int64_t)blockIdx.x * 32 + (threadIdx.x & 31);
   const int slice = threadIdx.x >> 5;
   const int64_t width = 3 * (int64_t)N;
   float v = 0.0f;
-  if (c < width)
-    for (int i = slice; i < rows; i += 8) v += part[i * width + c];
+  if (c < width) {
+#pragma unroll 4
+    for (int i = slice; i < rows; i += 32) v += part[i * width + c];
+  }
   s[slice][threadIdx.x & 31] = v;
   __syncthreads();
   if (slice || c >= width) return;
-  for (int i = 1; i < 8; ++i) v += s[i][threadIdx.x];
+  for (int i = 1; i < 32; ++i) v += s[i][threadIdx.x];
   float* o = c < N ? o0 : (c < 2 * (int64_t)N ? o1 : o2);
   if (o) o[c % N] = v;
 }
@@ -358,11 +443,19 @@ __global__ void __launch_bounds__(256) norm_sum(const float* __restrict__ part, 
 bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
 int64_t least(int64_t a, int64_t b) { return a < b ? a : b; }
 
-int64_t bwd_teams(int64_t M, int64_t N) {
-  // one team of 32 threads per row up to 256 channels, eight teams a block
-  if (N <= 256) return least(kBwdBlocks, (M + 7) / 8) * 8;
-  return least(kBwdBlocks, M);
+// Threads of a row, eight channels each.
+int row_threads(int64_t N) {
+  return N <= 256 ? 32 : N <= 1024 ? 128 : N <= 2048 ? 256 : N <= 4096 ? 512 : 1024;
 }
+
+// Blocks for M rows with `threads` of them on an SM; from the shape alone, so
+// that a shape always sums in the same order.
+int64_t blocks_for(int64_t M, int64_t N, int threads) {
+  const int tpr = row_threads(N), block = tpr == 32 ? 256 : tpr;
+  const int64_t resident = (int64_t)kSms * (threads > block ? threads / block : 1);
+  return least(resident, tpr == 32 ? (M + 7) / 8 : M);
+}
+int64_t bwd_blocks(int64_t M, int64_t N) { return blocks_for(M, N, 512); }
 
 snn_status_t check_desc(const snn_norm_desc* d) {
   if (!d || d->reserved[0] || d->reserved[1]) return SNN_ERR_INVALID_ARG;
@@ -402,22 +495,25 @@ struct Launch {
   cudaStream_t st;
 };
 
-template <typename T, typename R, bool VEC, int TPR, int E>
+template <typename T, typename R, bool VEC, int TPR>
 cudaError_t launch_tpr(const Launch& l) {
-  const dim3 block(TPR == 32 ? 256 : TPR);
-  if (l.bwd) return launch_pdl(norm_bwd<T, R, VEC, TPR, E>, dim3((unsigned)l.blocks), block, 0, l.st, l.g);
-  return launch_pdl(norm_fwd<T, R, VEC, TPR, E>, dim3((unsigned)l.blocks), block, 0, l.st, l.g);
+  const dim3 grid((unsigned)l.blocks), block(kBlockThreads<TPR>);
+  if (!l.bwd) return launch_pdl(norm_fwd<T, R, VEC, TPR>, grid, block, 0, l.st, l.g);
+  const size_t smem = TPR == 1024 ? 3 * E * sizeof(float) * TPR : 0;
+  const cudaError_t e = ensure_smem((const void*)norm_bwd<T, R, VEC, TPR>, smem);
+  if (e != cudaSuccess) return e;
+  return launch_pdl(norm_bwd<T, R, VEC, TPR>, grid, block, smem, l.st, l.g);
 }
 
-// Threads of a row: eight elements each, sixteen above 4096 channels.
 template <typename T, typename R, bool VEC>
 cudaError_t launch_vec(const Launch& l) {
-  const int N = l.g.N;
-  if (N <= 256) return launch_tpr<T, R, VEC, 32, 8>(l);
-  if (N <= 1024) return launch_tpr<T, R, VEC, 128, 8>(l);
-  if (N <= 2048) return launch_tpr<T, R, VEC, 256, 8>(l);
-  if (N <= 4096) return launch_tpr<T, R, VEC, 512, 8>(l);
-  return launch_tpr<T, R, VEC, 512, 16>(l);
+  switch (row_threads(l.g.N)) {
+    case 32: return launch_tpr<T, R, VEC, 32>(l);
+    case 128: return launch_tpr<T, R, VEC, 128>(l);
+    case 256: return launch_tpr<T, R, VEC, 256>(l);
+    case 512: return launch_tpr<T, R, VEC, 512>(l);
+    default: return launch_tpr<T, R, VEC, 1024>(l);
+  }
 }
 
 template <typename T, typename R>
@@ -465,7 +561,7 @@ size_t snn_norm_desc_size(void) { return sizeof(snn_norm_desc); }
 
 size_t snn_block_norm_workspace_bytes(int64_t M, int64_t N) {
   if (M < 0 || N < 1 || N > kMaxN) return 0;
-  const size_t b = (size_t)bwd_teams(M, N) * 3 * (size_t)N * sizeof(float);
+  const size_t b = (size_t)bwd_blocks(M, N) * 3 * (size_t)N * sizeof(float);
   return b < 256 ? 256 : b;
 }
 
@@ -490,8 +586,7 @@ snn_status_t snn_block_norm_fwd(const snn_norm_desc* desc, const snn_rows* r, co
       (s = take(desc, z, io, &g.z, &vec)) != SNN_OK || (s = take(desc, r_out, res, &g.ro, &vec)) != SNN_OK ||
       (s = take(desc, y, io, &g.y, &vec)) != SNN_OK || (s = finish(desc, &vec)) != SNN_OK)
     return s;
-  const int64_t teams = desc->N <= 256 ? (desc->M + 7) / 8 : desc->M;
-  const Launch l{g, false, least(teams, 152 * 32), reinterpret_cast<cudaStream_t>(stream)};
+  const Launch l{g, false, blocks_for(desc->M, desc->N, 1024), reinterpret_cast<cudaStream_t>(stream)};
   return launch(desc, l, vec) == cudaSuccess ? SNN_OK : SNN_ERR_CUDA;
 }
 
@@ -529,16 +624,16 @@ snn_status_t snn_block_norm_bwd(const snn_norm_desc* desc, const snn_rows* r_out
       (s = finish(desc, &vec)) != SNN_OK)
     return s;
   cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
-  const int64_t teams = bwd_teams(desc->M, desc->N);
+  const int64_t blocks = bwd_blocks(desc->M, desc->N);
   cudaError_t e = cudaSuccess;
   if (desc->M > 0) {
     g.part = params ? static_cast<float*>(ws) : nullptr;
-    const Launch l{g, true, desc->N <= 256 ? teams / 8 : teams, st};
+    const Launch l{g, true, blocks, st};
     e = launch(desc, l, vec);
   }
   if (e == cudaSuccess && params)
-    e = snn::launch_pdl(norm_sum, dim3((unsigned)((3 * desc->N + 31) / 32)), dim3(256), 0, st,
-                        static_cast<const float*>(ws), (int)teams, (int)desc->N, grad_w_post,
+    e = snn::launch_pdl(norm_sum, dim3((unsigned)((3 * desc->N + 31) / 32)), dim3(1024), 0, st,
+                        static_cast<const float*>(ws), (int)blocks, (int)desc->N, grad_w_post,
                         grad_scale, grad_w_pre);
   return e == cudaSuccess ? SNN_OK : SNN_ERR_CUDA;
 }
