@@ -9,6 +9,7 @@ fallback implementation.
 from __future__ import annotations
 
 import ctypes
+import functools
 import os
 import re
 from typing import Optional
@@ -182,9 +183,15 @@ def _ptr(t) -> Optional[int]:
     return t.data_ptr()
 
 
+# handle of a device's current stream, without the Stream object around it
+# (building one costs more than a small kernel takes)
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (
+    lambda device: torch.cuda.current_stream(device).cuda_stream)
+
+
 def _stream(stream) -> Optional[int]:
     if stream is None:
-        return torch.cuda.current_stream().cuda_stream
+        return _raw_stream(torch.cuda.current_device())
     if isinstance(stream, int):
         return stream
     return stream.cuda_stream
@@ -482,6 +489,7 @@ def snn_maxpool2_bwd_nhwc(dY, idx, dX, stream=None):
                                                 _stream(stream)), "snn_maxpool2_bwd_nhwc")
 
 
+@functools.lru_cache(maxsize=1024)
 def _attn_desc(where, B, T, H, Hk, Dk, Dv, dtype, scale) -> AttnDesc:
     code = _TORCH_DTYPE_CODE.get(dtype)
     if code is None:
@@ -489,27 +497,53 @@ def _attn_desc(where, B, T, H, Hk, Dk, Dv, dtype, scale) -> AttnDesc:
     return AttnDesc(B, T, H, Hk, Dk, Dv, code, scale)
 
 
-def _bthd(where, name, t, shape, dtype):
-    """A [B, T, heads, D] tensor (a [B, heads, D] one for a single token) with
-    contiguous D."""
-    if tuple(t.shape) != tuple(shape) or t.dtype != dtype or not t.is_cuda:
-        raise ValueError(f"{where}: {name} must be a CUDA {dtype} tensor of shape {tuple(shape)}")
-    st = t.stride()
-    if st[-1] != 1 and t.shape[-1] > 1:
-        raise ValueError(f"{where}: {name} must have a contiguous last dimension")
-    return ctypes.byref(Bthd(t.data_ptr(), st[0], st[1] if len(st) == 4 else 0, st[-2]))
+class _Strided:
+    """The snn_bthd or snn_rows structures of one call, as one array of 64-bit
+    words (both structures are a pointer and 64-bit strides)."""
+    __slots__ = ("where", "dtype", "words", "array")
+
+    def __init__(self, where):
+        self.where, self.words = where, []
+
+    def bthd(self, name, t, shape, dtype):
+        """Place of a [B, T, heads, D] tensor (a [B, heads, D] one for a single
+        token) with contiguous D."""
+        if t.shape != shape or t.dtype != dtype or not t.is_cuda:
+            raise ValueError(f"{self.where}: {name} must be a CUDA {dtype} tensor of shape {shape}")
+        st = t.stride()
+        if st[-1] != 1 and shape[-1] > 1:
+            raise ValueError(f"{self.where}: {name} must have a contiguous last dimension")
+        self.words += (t.data_ptr(), st[0], st[1], st[-2])
+
+    def rows(self, name, t, shape, dtype):
+        """Place of an [M, N] matrix with contiguous rows, or of None."""
+        if t is None:
+            self.words += (0, 0)
+            return
+        if t.shape != shape or t.dtype != dtype or not t.is_cuda:
+            raise ValueError(f"{self.where}: {name} must be a CUDA {dtype} tensor of shape {shape}")
+        ld, inner = t.stride()
+        if inner != 1 and shape[1] > 1:
+            raise ValueError(f"{self.where}: {name} must have contiguous rows")
+        self.words += (t.data_ptr(), ld)
+
+    def pointers(self, words):
+        """Addresses of the structures, of `words` words each."""
+        self.array = (ctypes.c_int64 * len(self.words))(*self.words)
+        at = ctypes.addressof(self.array)
+        return range(at, at + 8 * len(self.words), 8 * words)
 
 
 def _flat(where, name, t, shape, dtype):
     """Pointer of a contiguous tensor of the given shape and type, or None."""
     if t is None:
         return None
-    if tuple(t.shape) != tuple(shape) or t.dtype != dtype or not t.is_contiguous() or not t.is_cuda:
-        raise ValueError(f"{where}: {name} must be a contiguous CUDA {dtype} tensor of shape "
-                         f"{tuple(shape)}")
+    if t.shape != shape or t.dtype != dtype or not t.is_contiguous() or not t.is_cuda:
+        raise ValueError(f"{where}: {name} must be a contiguous CUDA {dtype} tensor of shape {shape}")
     return t.data_ptr()
 
 
+@functools.lru_cache(maxsize=1024)
 def snn_leaky_attn_workspace_bytes(B, T, H, Hk, Dk, Dv, backward=False) -> int:
     d = AttnDesc(B, T, H, Hk, Dk, Dv, 1, 1.0)
     return load_library().snn_leaky_attn_workspace_bytes(ctypes.byref(d), 1 if backward else 0)
@@ -540,14 +574,18 @@ def snn_leaky_attn_fwd(q, k, v, beta, o, ws, scale=1.0, seq_lens=None, state_in=
     if state_in is not None and state_out is not None and len(state_in) != len(state_out):
         raise ValueError(f"{w}: state_in and state_out differ in places")
     ps, n = _state_places(w, slots, B, (state_in, state_out))
+    x = _Strided(w)
+    x.bthd("q", q, (B, T, H, Dk), dt)
+    x.bthd("k", k, (B, T, Hk, Dk), dt)
+    x.bthd("v", v, (B, T, Hk, Dv), dt)
+    x.bthd("o", o, (B, T, H, Dv), dt)
+    pq, pk, pv, po = x.pointers(4)
     _check(load_library().snn_leaky_attn_fwd(
-        ctypes.byref(d), _bthd(w, "q", q, (B, T, H, Dk), dt), _bthd(w, "k", k, (B, T, Hk, Dk), dt),
-        _bthd(w, "v", v, (B, T, Hk, Dv), dt), _flat(w, "beta", beta, (H,), torch.float32),
+        ctypes.byref(d), pq, pk, pv, _flat(w, "beta", beta, (H,), torch.float32),
         _flat(w, "seq_lens", seq_lens, (B,), torch.int32),
         _flat(w, "state_in", state_in, (n, H, Dk, Dv), torch.float32),
-        _flat(w, "state_out", state_out, (n, H, Dk, Dv), torch.float32), ps, n,
-        _bthd(w, "o", o, (B, T, H, Dv), dt), _ptr(ws), ws.numel() * ws.element_size(),
-        _stream(stream)), w)
+        _flat(w, "state_out", state_out, (n, H, Dk, Dv), torch.float32), ps, n, po, _ptr(ws),
+        ws.numel() * ws.element_size(), _stream(stream)), w)
 
 
 def snn_leaky_attn_bwd(q, k, v, beta, grad_o, grad_q, grad_k, grad_v, ws, scale=1.0,
@@ -559,15 +597,17 @@ def snn_leaky_attn_bwd(q, k, v, beta, grad_o, grad_q, grad_k, grad_v, ws, scale=
     (B, T, H, Dk), Hk, Dv, dt = q.shape, k.shape[2], v.shape[-1], q.dtype
     d = _attn_desc(w, B, T, H, Hk, Dk, Dv, dt, scale)
     qs, ks, vs, os = (B, T, H, Dk), (B, T, Hk, Dk), (B, T, Hk, Dv), (B, T, H, Dv)
+    x = _Strided(w)
+    for name, t, shape in (("q", q, qs), ("k", k, ks), ("v", v, vs), ("grad_o", grad_o, os),
+                           ("grad_q", grad_q, qs), ("grad_k", grad_k, ks), ("grad_v", grad_v, vs)):
+        x.bthd(name, t, shape, dt)
+    pq, pk, pv, po, gq, gk, gv = x.pointers(4)
     state = lambda name, t: _flat(w, name, t, (B, H, Dk, Dv), torch.float32)
     _check(load_library().snn_leaky_attn_bwd(
-        ctypes.byref(d), _bthd(w, "q", q, qs, dt), _bthd(w, "k", k, ks, dt),
-        _bthd(w, "v", v, vs, dt), _flat(w, "beta", beta, (H,), torch.float32),
-        _flat(w, "seq_lens", seq_lens, (B,), torch.int32), state("state_in", state_in),
-        _bthd(w, "grad_o", grad_o, os, dt), state("grad_state_out", grad_state_out),
-        _bthd(w, "grad_q", grad_q, qs, dt), _bthd(w, "grad_k", grad_k, ks, dt),
-        _bthd(w, "grad_v", grad_v, vs, dt), state("grad_state_in", grad_state_in), _ptr(ws),
-        ws.numel() * ws.element_size(), _stream(stream)), w)
+        ctypes.byref(d), pq, pk, pv, _flat(w, "beta", beta, (H,), torch.float32),
+        _flat(w, "seq_lens", seq_lens, (B,), torch.int32), state("state_in", state_in), po,
+        state("grad_state_out", grad_state_out), gq, gk, gv, state("grad_state_in", grad_state_in),
+        _ptr(ws), ws.numel() * ws.element_size(), _stream(stream)), w)
 
 
 def snn_leaky_attn_step(q, k, v, beta, state, o, scale=1.0, slots=None, stream=None):
@@ -579,18 +619,24 @@ def snn_leaky_attn_step(q, k, v, beta, state, o, scale=1.0, slots=None, stream=N
     (B, H, Dk), Hk, Dv, dt = q.shape, k.shape[1], v.shape[-1], q.dtype
     d = _attn_desc(w, B, 1, H, Hk, Dk, Dv, dt, scale)
     n = state.shape[0]
+    x = _Strided(w)
+    x.bthd("q", q, (B, H, Dk), dt)
+    x.bthd("k", k, (B, Hk, Dk), dt)
+    x.bthd("v", v, (B, Hk, Dv), dt)
+    x.bthd("o", o, (B, H, Dv), dt)
+    pq, pk, pv, po = x.pointers(4)
     _check(load_library().snn_leaky_attn_step(
-        ctypes.byref(d), _bthd(w, "q", q, (B, H, Dk), dt), _bthd(w, "k", k, (B, Hk, Dk), dt),
-        _bthd(w, "v", v, (B, Hk, Dv), dt), _flat(w, "beta", beta, (H,), torch.float32),
+        ctypes.byref(d), pq, pk, pv, _flat(w, "beta", beta, (H,), torch.float32),
         _flat(w, "state", state, (n, H, Dk, Dv), torch.float32),
-        _flat(w, "slots", slots, (B,), torch.int32), n, _bthd(w, "o", o, (B, H, Dv), dt),
-        _stream(stream)), w)
+        _flat(w, "slots", slots, (B,), torch.int32), n, po, _stream(stream)), w)
 
 
+@functools.lru_cache(maxsize=1024)
 def snn_block_norm_workspace_bytes(M: int, N: int) -> int:
     return load_library().snn_block_norm_workspace_bytes(M, N)
 
 
+@functools.lru_cache(maxsize=1024)
 def _norm_desc(where, M, N, group, dtype, res_dtype, gate, eps) -> NormDesc:
     for dt in (dtype, res_dtype):
         if dt not in _TORCH_DTYPE_CODE:
@@ -601,16 +647,6 @@ def _norm_desc(where, M, N, group, dtype, res_dtype, gate, eps) -> NormDesc:
                     GATE_CODE[gate], eps)
 
 
-def _rows(where, name, t, shape, dtype):
-    if t is None:
-        return None
-    if tuple(t.shape) != shape or t.dtype != dtype or not t.is_cuda:
-        raise ValueError(f"{where}: {name} must be a CUDA {dtype} tensor of shape {shape}")
-    if t.stride(1) != 1 and shape[1] > 1:
-        raise ValueError(f"{where}: {name} must have contiguous rows")
-    return ctypes.byref(Rows(t.data_ptr(), t.stride(0)))
-
-
 def snn_block_norm_fwd(r, a, z, w_post, res_scale, w_pre, r_out, y, eps=1e-6, group=0,
                        gate="none", stream=None):
     """r_out = r + res_scale * norm(a) w_post * act(z) and y = norm(r_out)
@@ -618,15 +654,21 @@ def snn_block_norm_fwd(r, a, z, w_post, res_scale, w_pre, r_out, y, eps=1e-6, gr
     y = norm(r) w_pre alone; w_pre None: no y.  group: channels per norm of a
     (0: the row); gate: "none", "sigmoid" or "silu" of z."""
     w = "snn_block_norm_fwd"
-    shape = tuple(r.shape)
-    io = a.dtype if a is not None else y.dtype if y is not None else r.dtype
-    d = _norm_desc(w, *shape, group, io, r.dtype, gate, eps)
-    rows = lambda name, t, dt: _rows(w, name, t, shape, dt)
-    par = lambda name, t: _flat(w, name, t, shape[1:], torch.float32)
+    shape, res = r.shape, r.dtype
+    io = a.dtype if a is not None else y.dtype if y is not None else res
+    d = _norm_desc(w, *shape, group, io, res, gate, eps)
+    x = _Strided(w)
+    x.rows("r", r, shape, res)
+    x.rows("a", a, shape, io)
+    x.rows("z", z, shape, io)
+    x.rows("r_out", r_out, shape, res)
+    x.rows("y", y, shape, io)
+    pr, pa, pz, po, py = x.pointers(2)
+    n = shape[1:]
     _check(load_library().snn_block_norm_fwd(
-        ctypes.byref(d), rows("r", r, r.dtype), rows("a", a, io), rows("z", z, io),
-        par("w_post", w_post), par("res_scale", res_scale), par("w_pre", w_pre),
-        rows("r_out", r_out, r.dtype), rows("y", y, io), _stream(stream)), w)
+        ctypes.byref(d), pr, pa, pz, _flat(w, "w_post", w_post, n, torch.float32),
+        _flat(w, "res_scale", res_scale, n, torch.float32),
+        _flat(w, "w_pre", w_pre, n, torch.float32), po, py, _stream(stream)), w)
 
 
 def snn_block_norm_bwd(r_out, a, z, w_post, res_scale, w_pre, grad_r_out, grad_y, grad_r, grad_a,
@@ -636,19 +678,22 @@ def snn_block_norm_bwd(r_out, a, z, w_post, res_scale, w_pre, grad_r_out, grad_y
     grad_y None stands for zeros, an output None is not computed.  ws:
     snn_block_norm_workspace_bytes(M, N) (None without parameter gradients)."""
     w = "snn_block_norm_bwd"
-    res = r_out if r_out is not None else grad_r_out
-    shape = tuple(res.shape)
-    io = a.dtype if a is not None else grad_y.dtype if grad_y is not None else res.dtype
-    d = _norm_desc(w, *shape, group, io, res.dtype, gate, eps)
-    rows = lambda name, t, dt: _rows(w, name, t, shape, dt)
-    par = lambda name, t: _flat(w, name, t, shape[1:], torch.float32)
+    of = r_out if r_out is not None else grad_r_out
+    shape, res = of.shape, of.dtype
+    io = a.dtype if a is not None else grad_y.dtype if grad_y is not None else res
+    d = _norm_desc(w, *shape, group, io, res, gate, eps)
+    x = _Strided(w)
+    for name, t, dt in (("r_out", r_out, res), ("a", a, io), ("z", z, io),
+                        ("grad_r_out", grad_r_out, res), ("grad_y", grad_y, io),
+                        ("grad_r", grad_r, res), ("grad_a", grad_a, io), ("grad_z", grad_z, io)):
+        x.rows(name, t, shape, dt)
+    pr, pa, pz, gro, gy, gr, ga, gz = x.pointers(2)
+    n = shape[1:]
+    par = lambda name, t: _flat(w, name, t, n, torch.float32)
     _check(load_library().snn_block_norm_bwd(
-        ctypes.byref(d), rows("r_out", r_out, res.dtype), rows("a", a, io), rows("z", z, io),
-        par("w_post", w_post), par("res_scale", res_scale), par("w_pre", w_pre),
-        rows("grad_r_out", grad_r_out, res.dtype), rows("grad_y", grad_y, io),
-        rows("grad_r", grad_r, res.dtype), rows("grad_a", grad_a, io), rows("grad_z", grad_z, io),
-        par("grad_w_post", grad_w_post), par("grad_scale", grad_scale),
-        par("grad_w_pre", grad_w_pre), _ptr(ws),
+        ctypes.byref(d), pr, pa, pz, par("w_post", w_post), par("res_scale", res_scale),
+        par("w_pre", w_pre), gro, gy, gr, ga, gz, par("grad_w_post", grad_w_post),
+        par("grad_scale", grad_scale), par("grad_w_pre", grad_w_pre), _ptr(ws),
         ws.numel() * ws.element_size() if ws is not None else 0, _stream(stream)), w)
 
 
