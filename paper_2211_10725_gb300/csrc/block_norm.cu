@@ -7,14 +7,14 @@
 //   d      = grad_r' + rstd (g - e mean(g e))
 //   grad_r = d;  grad_z = d s n act'(z)
 //   grad_a = rstd_a (m - h mean_group(m h)),  h = a rstd_a,  m = d s act(z) w_post
-//   grad_w_post = sum d s act(z) h;  grad_s = sum d n act(z);  grad_w_pre = sum grad_y e
+//   grad_w_post = s G,  grad_s = w_post G  with  G = sum d act(z) h;  grad_w_pre = sum grad_y e
 // Every tensor is read and written once: the bound is HBM.  A row stays in
 // the registers of one warp (short rows) or one block, eight channels to a
 // thread; blocks stay on the GPU and take rows in turn, with the next row's
 // loads in flight while the sums of the present one meet.  The parameters'
 // gradients gather in the registers (long rows: in shared memory) of the
 // thread that owns the channels over all the rows of its block, so the sums
-// over rows need one [blocks, 3, N] array of partials and a second kernel
+// over rows need one [blocks, 2, N] array of partials and a second kernel
 // that adds them in block order (no atomics: the same bits on every call).
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
@@ -47,10 +47,25 @@ struct Args {
   Rows r, a, z, ro, y;        // forward
   Rows gro, gy, gr, ga, gz;   // backward (reads ro, a, z)
   const float *w_post, *scale, *w_pre;
-  float* part;                // [blocks][3][N]
+  float* part;                // [blocks][2][N]
 };
 
 __device__ __forceinline__ float sigmoidf_(float z) { return __fdividef(1.0f, 1.0f + __expf(-z)); }
+
+// Eight floats as one 32-byte access (p 32-byte aligned): two 16-byte ones
+// would each touch half of every 32-byte sector.
+__device__ __forceinline__ void load32(const float* p, uint4 w[2]) {
+  asm volatile("ld.global.v8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+               : "=r"(w[0].x), "=r"(w[0].y), "=r"(w[0].z), "=r"(w[0].w), "=r"(w[1].x), "=r"(w[1].y),
+                 "=r"(w[1].z), "=r"(w[1].w)
+               : "l"(p)
+               : "memory");
+}
+__device__ __forceinline__ void store32(float* p, const float v[8]) {
+  asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(p), "f"(v[0]),
+               "f"(v[1]), "f"(v[2]), "f"(v[3]), "f"(v[4]), "f"(v[5]), "f"(v[6]), "f"(v[7])
+               : "memory");
+}
 
 // A thread's share of a row as it lies in memory: eight consecutive channels
 // (VEC), else every TPR-th.
@@ -64,6 +79,8 @@ struct Share {
     const T* p = static_cast<const T*>(m.data) + row * m.ld;
     if constexpr (VEC) {
       if (t * E < N) {
+        if constexpr (sizeof(T) == 4) load32(reinterpret_cast<const float*>(p + t * E), w);
+        else
 #pragma unroll
         for (int i = 0; i < kWords; ++i) w[i] = reinterpret_cast<const uint4*>(p + t * E)[i];
       }
@@ -93,7 +110,10 @@ template <typename T, bool VEC, int TPR>
 __device__ __forceinline__ void store_row(const Rows& m, int64_t row, int N, int t, const float v[E]) {
   T* p = static_cast<T*>(m.data) + row * m.ld;
   if constexpr (VEC) {
-    if (t * E < N) Elem<T>::store8(p + t * E, v);
+    if (t * E < N) {
+      if constexpr (sizeof(T) == 4) store32(p + t * E, v);
+      else Elem<T>::store8(p + t * E, v);
+    }
   } else {
 #pragma unroll
     for (int e = 0; e < E; ++e)
@@ -120,7 +140,7 @@ __device__ __forceinline__ void load_param(const float* p, int N, int t, float v
 // is enough: a warp cannot be two sums ahead.
 template <int TPR>
 struct RowSum {
-  float4 (*scratch)[32];  // [2][warps]
+  float (*scratch)[3][32];  // [2][value][warp]
   int turn = 0;
   template <int K>
   __device__ __forceinline__ void operator()(float (&v)[K]) {
@@ -130,22 +150,22 @@ struct RowSum {
       for (int k = 0; k < K; ++k) v[k] += __shfl_xor_sync(0xffffffffu, v[k], o);
     if constexpr (TPR > 32) {
       constexpr int W = TPR / 32;
-      float4* s = scratch[turn];
+      float (*s)[32] = scratch[turn];
       turn ^= 1;
       if ((threadIdx.x & 31) == 0)
-        s[threadIdx.x >> 5] = make_float4(v[0], K > 1 ? v[K > 1] : 0.f, K > 2 ? v[K > 2 ? 2 : 0] : 0.f, 0.f);
-      __syncthreads();
-      float4 a = s[0];
 #pragma unroll
-      for (int w = 1; w < W; ++w) {
-        const float4 x = s[w];
-        a.x += x.x;
-        if (K > 1) a.y += x.y;
-        if (K > 2) a.z += x.z;
+        for (int k = 0; k < K; ++k) s[k][threadIdx.x >> 5] = v[k];
+      __syncthreads();
+#pragma unroll
+      for (int k = 0; k < K; ++k) {
+        float a = 0.0f;
+#pragma unroll
+        for (int w = 0; w < W; w += 4) {
+          const float4 x = *reinterpret_cast<const float4*>(&s[k][w]);
+          a += (x.x + x.y) + (x.z + x.w);
+        }
+        v[k] = a;
       }
-      v[0] = a.x;
-      if (K > 1) v[K > 1] = a.y;
-      if (K > 2) v[K > 2 ? 2 : 0] = a.z;
     }
   }
 };
@@ -163,7 +183,7 @@ constexpr int kBlockThreads = TPR == 32 ? 256 : TPR;  // short rows: eight warps
 // one of 1024.
 template <typename T, typename R, bool VEC, int TPR>
 __global__ void __launch_bounds__(kBlockThreads<TPR>, 1024 / kBlockThreads<TPR>) norm_fwd(const Args g) {
-  __shared__ float4 scratch[2][32];
+  __shared__ __align__(16) float scratch[2][3][32];
   grid_dep_wait();
   constexpr int kTeams = kBlockThreads<TPR> / TPR;
   const int t = threadIdx.x % TPR, N = g.N;
@@ -226,47 +246,30 @@ __global__ void __launch_bounds__(kBlockThreads<TPR>, 1024 / kBlockThreads<TPR>)
   }
 }
 
-// The parameters' gradients of a thread's channels over its rows: in registers,
-// or (ROW in shared memory, [3][E / 4][threads] float4) for long rows.
-template <bool SMEM, int THREADS>
-struct Gather {
-  float v[SMEM ? 1 : 3][E];
-  __device__ __forceinline__ float4* at(int k, int i) {
-    extern __shared__ float4 gather_smem[];
-    return gather_smem + (k * (E / 4) + i) * THREADS + threadIdx.x;
+// Two vectors of a thread's channels that live as long as its block: in
+// registers, or (long rows, whose threads have none to spare) in shared
+// memory, [4][E / 4][threads] float4 with the pair at FIRST.
+template <bool SMEM, int THREADS, int FIRST>
+struct Kept {
+  float v[SMEM ? 1 : 2][E];
+  __device__ __forceinline__ float4& at(int k, int i) {
+    extern __shared__ float4 kept_smem[];
+    return kept_smem[((FIRST + k) * (E / 4) + i) * THREADS + threadIdx.x];
   }
-  __device__ __forceinline__ void clear() {
+  __device__ __forceinline__ void set(int k, const float (&a)[E]) {
     if constexpr (SMEM) {
 #pragma unroll
-      for (int k = 0; k < 3; ++k)
-        for (int i = 0; i < E / 4; ++i) *at(k, i) = make_float4(0.f, 0.f, 0.f, 0.f);
+      for (int i = 0; i < E / 4; ++i) at(k, i) = make_float4(a[4 * i], a[4 * i + 1], a[4 * i + 2], a[4 * i + 3]);
     } else {
 #pragma unroll
-      for (int k = 0; k < 3; ++k)
-        for (int e = 0; e < E; ++e) v[k][e] = 0.0f;
-    }
-  }
-  __device__ __forceinline__ void add(int k, const float (&a)[E], const float (&b)[E]) {  // += a b
-    if constexpr (SMEM) {
-#pragma unroll
-      for (int i = 0; i < E / 4; ++i) {
-        float4 s = *at(k, i);
-        s.x = fmaf(a[4 * i], b[4 * i], s.x);
-        s.y = fmaf(a[4 * i + 1], b[4 * i + 1], s.y);
-        s.z = fmaf(a[4 * i + 2], b[4 * i + 2], s.z);
-        s.w = fmaf(a[4 * i + 3], b[4 * i + 3], s.w);
-        *at(k, i) = s;
-      }
-    } else {
-#pragma unroll
-      for (int e = 0; e < E; ++e) v[k][e] = fmaf(a[e], b[e], v[k][e]);
+      for (int e = 0; e < E; ++e) v[k][e] = a[e];
     }
   }
   __device__ __forceinline__ void get(int k, float (&a)[E]) {
     if constexpr (SMEM) {
 #pragma unroll
       for (int i = 0; i < E / 4; ++i) {
-        const float4 s = *at(k, i);
+        const float4 s = at(k, i);
         a[4 * i] = s.x;
         a[4 * i + 1] = s.y;
         a[4 * i + 2] = s.z;
@@ -277,12 +280,19 @@ struct Gather {
       for (int e = 0; e < E; ++e) a[e] = v[k][e];
     }
   }
+  __device__ __forceinline__ void add(int k, const float (&a)[E], const float (&b)[E]) {  // += a b
+    float s[E];
+    get(k, s);
+#pragma unroll
+    for (int e = 0; e < E; ++e) s[e] = fmaf(a[e], b[e], s[e]);
+    set(k, s);
+  }
 };
 
 template <typename T, typename R, bool VEC, int TPR>
 __global__ void __launch_bounds__(kBlockThreads<TPR>, TPR == 1024 ? 1 : 512 / kBlockThreads<TPR>)
     norm_bwd(const Args g) {
-  __shared__ float4 scratch[2][32];
+  __shared__ __align__(16) float scratch[2][3][32];
   grid_dep_wait();
   constexpr int kTeams = kBlockThreads<TPR> / TPR;
   const int t = threadIdx.x % TPR, team = threadIdx.x / TPR, N = g.N;
@@ -292,8 +302,24 @@ __global__ void __launch_bounds__(kBlockThreads<TPR>, TPR == 1024 ? 1 : 512 / kB
   const bool pre = g.gy.data != nullptr, through = g.gro.data != nullptr;
   const float inv_n = 1.0f / (float)N, inv_g = 1.0f / (float)g.group;
   RowSum<TPR> row_sum{scratch};
-  Gather<TPR == 1024, TPR> sums;  // of w_post, the residual scale, w_pre
-  sums.clear();
+  // 0: of d act(z) h, 1: of grad_y y';  0: w_pre, 1: s w_post
+  Kept<TPR == 1024, TPR, 0> sums;
+  Kept<TPR == 1024, TPR, 2> params;
+  {
+    float w[E], sc[E];
+    load_param<VEC, TPR>(g.w_pre, N, t, w);
+    params.set(0, w);
+    load_param<VEC, TPR>(g.w_post, N, t, w);
+    load_param<VEC, TPR>(g.scale, N, t, sc);
+#pragma unroll
+    for (int e = 0; e < E; ++e) {
+      w[e] *= sc[e];
+      sc[e] = 0.0f;
+    }
+    params.set(1, w);
+    sums.set(0, sc);
+    sums.set(1, sc);
+  }
   Share<R, VEC, TPR> ro, gro;
   Share<T, VEC, TPR> gy, a, z;
   auto fetch = [&](int64_t i) {
@@ -308,7 +334,7 @@ __global__ void __launch_bounds__(kBlockThreads<TPR>, TPR == 1024 ? 1 : 512 / kB
   if (kAhead && row < g.M) fetch(row);
   for (; row < g.M; row += step) {
     if (!kAhead) fetch(row);
-    float d[E], x[E], gw[E], h[E], zz[E], w[E];
+    float d[E], x[E], gw[E], h[E], zz[E];
     if (pre) ro.get(N, t, x);
     if (pre) gy.get(N, t, gw);
     if (block) a.get(N, t, h);
@@ -321,8 +347,9 @@ __global__ void __launch_bounds__(kBlockThreads<TPR>, TPR == 1024 ? 1 : 512 / kB
     }
     if (kAhead && row + step < g.M) fetch(row + step);
     float ss[3] = {0.0f, 0.0f, 0.0f};  // of r'^2, grad_y w_pre r', a^2
+    float w[E];
+    params.get(0, w);
     if (pre) {
-      load_param<VEC, TPR>(g.w_pre, N, t, w);
 #pragma unroll
       for (int e = 0; e < E; ++e) {
         ss[0] = fmaf(x[e], x[e], ss[0]);
@@ -332,83 +359,77 @@ __global__ void __launch_bounds__(kBlockThreads<TPR>, TPR == 1024 ? 1 : 512 / kB
     if (block) {
 #pragma unroll
       for (int e = 0; e < E; ++e) ss[2] = fmaf(h[e], h[e], ss[2]);
-      if (!whole) ss[2] = group_sum(ss[2], g.group >> 3);
     }
-    const float in_group = ss[2];
+    float in_group = 0.0f;
+    if (block && !whole) in_group = group_sum(ss[2], g.group >> 3);
     row_sum(ss);
     if (pre) {
       const float rstd = rsqrtf(fmaf(ss[0], inv_n, g.eps));
       const float mean = ss[1] * rstd * inv_n;  // mean of (grad_y w_pre) y'
 #pragma unroll
       for (int e = 0; e < E; ++e) x[e] *= rstd;  // y'
-      sums.add(2, gw, x);
+      sums.add(1, gw, x);
 #pragma unroll
       for (int e = 0; e < E; ++e) d[e] = fmaf(rstd, fmaf(-x[e], mean, gw[e] * w[e]), d[e]);
     }
     if (g.gr.data) store_row<R, VEC, TPR>(g.gr, row, N, t, d);
     if (!block) continue;
     const float rstd_a = rsqrtf(whole ? fmaf(ss[2], inv_n, g.eps) : fmaf(in_group, inv_g, g.eps));
-    load_param<VEC, TPR>(g.w_post, N, t, w);
-    load_param<VEC, TPR>(g.scale, N, t, gw);
+    float q[1] = {0.0f};
+    params.get(1, w);
 #pragma unroll
     for (int e = 0; e < E; ++e) {
       h[e] *= rstd_a;
-      float act = 1.0f, slope = 0.0f;
+      x[e] = d[e];
+      d[e] *= w[e];
       if (gated) {
         const float s = sigmoidf_(zz[e]);
-        act = g.gate == SNN_GATE_SILU ? zz[e] * s : s;
-        slope = g.gate == SNN_GATE_SILU ? s * fmaf(zz[e], 1.0f - s, 1.0f) : s * (1.0f - s);
+        const float act = g.gate == SNN_GATE_SILU ? zz[e] * s : s;
+        const float slope = g.gate == SNN_GATE_SILU ? s * fmaf(zz[e], 1.0f - s, 1.0f) : s * (1.0f - s);
+        zz[e] = d[e] * h[e] * slope;  // grad_z
+        x[e] *= act;
+        d[e] *= act;                  // m
       }
-      const float n = h[e] * w[e];
-      zz[e] = d[e] * gw[e] * n * slope;  // grad_z
-      x[e] = n * act;
-      gw[e] *= d[e] * act;               // gradient of n
+      q[0] = fmaf(d[e], h[e], q[0]);
     }
-    sums.add(1, d, x);
-    sums.add(0, gw, h);
+    sums.add(0, x, h);
     if (g.gz.data) store_row<T, VEC, TPR>(g.gz, row, N, t, zz);
     if (!g.ga.data) continue;
-    float q[1] = {0.0f};
-#pragma unroll
-    for (int e = 0; e < E; ++e) {
-      gw[e] *= w[e];
-      q[0] = fmaf(gw[e], h[e], q[0]);
-    }
     if (whole) row_sum(q);
     else q[0] = group_sum(q[0], g.group >> 3);
     const float mean = q[0] * (whole ? inv_n : inv_g);
 #pragma unroll
-    for (int e = 0; e < E; ++e) gw[e] = rstd_a * fmaf(-h[e], mean, gw[e]);
-    store_row<T, VEC, TPR>(g.ga, row, N, t, gw);
+    for (int e = 0; e < E; ++e) d[e] = rstd_a * fmaf(-h[e], mean, d[e]);
+    store_row<T, VEC, TPR>(g.ga, row, N, t, d);
   }
   if (!g.part) return;
-  float* p = g.part + (int64_t)blockIdx.x * 3 * N;
+  float* p = g.part + (int64_t)blockIdx.x * 2 * N;
   if constexpr (kTeams > 1) {  // the block's teams, in order
-    __shared__ float all[kTeams][3][TPR * E];
+    __shared__ float all[kTeams][2][TPR * E];
 #pragma unroll
-    for (int k = 0; k < 3; ++k) {
+    for (int k = 0; k < 2; ++k) {
       float v[E];
       sums.get(k, v);
 #pragma unroll
       for (int e = 0; e < E; ++e) all[team][k][VEC ? t * E + e : e * TPR + t] = v[e];
     }
     __syncthreads();
-    for (int i = threadIdx.x; i < 3 * N; i += kBlockThreads<TPR>) {
-      const int k = i / N, c = i - k * N;
-      float v = all[0][k][c];
+    for (int i = threadIdx.x; i < 2 * N; i += kBlockThreads<TPR>) {
+      const int k = i / N, at = i - k * N;
+      float v = all[0][k][at];
 #pragma unroll
-      for (int j = 1; j < kTeams; ++j) v += all[j][k][c];
+      for (int j = 1; j < kTeams; ++j) v += all[j][k][at];
       p[i] = v;
     }
   } else {
 #pragma unroll
-    for (int k = 0; k < 3; ++k) {
+    for (int k = 0; k < 2; ++k) {
       float v[E];
       sums.get(k, v);
 #pragma unroll
       for (int e = 0; e < E; ++e) {
-        const int c = VEC ? t * E + e : e * TPR + t;
-        if (c < N) p[k * N + c] = v[e];
+        const int at = VEC ? t * E + e : e * TPR + t;
+        if (at < N) p[k * N + at] = v[e];
       }
     }
   }
@@ -417,23 +438,27 @@ __global__ void __launch_bounds__(kBlockThreads<TPR>, TPR == 1024 ? 1 : 512 / kB
 // Column sums of the partials: 32 columns a block, the rows in 32 slices (every
 // 32nd row, in order), then the slices in order.
 __global__ void __launch_bounds__(1024) norm_sum(const float* __restrict__ part, int rows, int N,
-                                                 float* o0, float* o1, float* o2) {
+                                                 const float* w_post, const float* scale,
+                                                 float* g_post, float* g_scale, float* g_pre) {
   __shared__ float s[32][33];
   grid_dep_wait();
-  const int64_t c = (int64_t)blockIdx.x * 32 + (threadIdx.x & 31);
-  const int slice = threadIdx.x >> 5;
-  const int64_t width = 3 * (int64_t)N;
+  const int c = blockIdx.x * 32 + (threadIdx.x & 31);
+  const int slice = threadIdx.x >> 5, width = 2 * N;
   float v = 0.0f;
   if (c < width) {
 #pragma unroll 4
-    for (int i = slice; i < rows; i += 32) v += part[i * width + c];
+    for (int i = slice; i < rows; i += 32) v += part[(int64_t)i * width + c];
   }
   s[slice][threadIdx.x & 31] = v;
   __syncthreads();
   if (slice || c >= width) return;
   for (int i = 1; i < 32; ++i) v += s[i][threadIdx.x];
-  float* o = c < N ? o0 : (c < 2 * (int64_t)N ? o1 : o2);
-  if (o) o[c % N] = v;
+  if (c >= N) {
+    if (g_pre) g_pre[c - N] = v;
+  } else {
+    if (g_post) g_post[c] = scale ? scale[c] * v : v;
+    if (g_scale) g_scale[c] = w_post ? w_post[c] * v : v;
+  }
 }
 
 // ---------------------------------------------------------------------------
@@ -482,8 +507,8 @@ snn_status_t take(const snn_norm_desc* d, const snn_rows* x, int dtype, Rows* ou
   if (!data_of(x)) return SNN_OK;
   if (!aligned16(x->data)) return SNN_ERR_ALIGNMENT;
   if (d->M > 1 && (x->ld < d->N || x->ld > (int64_t(1) << 40))) return SNN_ERR_INVALID_ARG;
-  const int64_t per = dtype == SNN_F32 ? 4 : 8;
-  if (d->M > 1 && x->ld % per) *vec = false;
+  if (d->M > 1 && x->ld % 8) *vec = false;
+  if (dtype == SNN_F32 && (reinterpret_cast<uintptr_t>(x->data) & 31u)) *vec = false;
   *out = Rows{x->data, x->ld};
   return SNN_OK;
 }
@@ -499,7 +524,7 @@ template <typename T, typename R, bool VEC, int TPR>
 cudaError_t launch_tpr(const Launch& l) {
   const dim3 grid((unsigned)l.blocks), block(kBlockThreads<TPR>);
   if (!l.bwd) return launch_pdl(norm_fwd<T, R, VEC, TPR>, grid, block, 0, l.st, l.g);
-  const size_t smem = TPR == 1024 ? 3 * E * sizeof(float) * TPR : 0;
+  const size_t smem = TPR == 1024 ? 4 * E * sizeof(float) * TPR : 0;
   const cudaError_t e = ensure_smem((const void*)norm_bwd<T, R, VEC, TPR>, smem);
   if (e != cudaSuccess) return e;
   return launch_pdl(norm_bwd<T, R, VEC, TPR>, grid, block, smem, l.st, l.g);
@@ -561,7 +586,7 @@ size_t snn_norm_desc_size(void) { return sizeof(snn_norm_desc); }
 
 size_t snn_block_norm_workspace_bytes(int64_t M, int64_t N) {
   if (M < 0 || N < 1 || N > kMaxN) return 0;
-  const size_t b = (size_t)bwd_blocks(M, N) * 3 * (size_t)N * sizeof(float);
+  const size_t b = (size_t)bwd_blocks(M, N) * 2 * (size_t)N * sizeof(float);
   return b < 256 ? 256 : b;
 }
 
@@ -632,9 +657,9 @@ snn_status_t snn_block_norm_bwd(const snn_norm_desc* desc, const snn_rows* r_out
     e = launch(desc, l, vec);
   }
   if (e == cudaSuccess && params)
-    e = snn::launch_pdl(norm_sum, dim3((unsigned)((3 * desc->N + 31) / 32)), dim3(1024), 0, st,
-                        static_cast<const float*>(ws), (int)blocks, (int)desc->N, grad_w_post,
-                        grad_scale, grad_w_pre);
+    e = snn::launch_pdl(norm_sum, dim3((unsigned)((2 * desc->N + 31) / 32)), dim3(1024), 0, st,
+                        static_cast<const float*>(ws), (int)blocks, (int)desc->N, w_post,
+                        res_scale, grad_w_post, grad_scale, grad_w_pre);
   return e == cudaSuccess ? SNN_OK : SNN_ERR_CUDA;
 }
 
