@@ -106,17 +106,21 @@ bool make_map_bthd(CUtensorMap* map, const Tensor& x, const Args& g, int heads, 
 }
 
 template <typename T, int DA, int DC>
-cudaError_t launch_tile(ChunkArgs& p, cudaStream_t st) {
+cudaError_t launch_tile(const ChunkArgs& p, cudaStream_t st) {
   using C = Cfg<DA, DC>;
   const cudaError_t e = ensure_smem((const void*)attn_chunks<T, DA, DC>, C::kSmem);
   if (e != cudaSuccess) return e;
   const int64_t blocks = (int64_t)p.g.B * p.g.H * p.nseg * p.g.nroles;
   if (p.nseg > 1) {
-    p.states_only = 1;
-    const cudaError_t es = launch_pdl(attn_chunks<T, DA, DC>, dim3((unsigned)blocks), dim3(C::kThreads),
-                                      C::kSmem, st, p);
+    // a third part of the decayed values only where a bf16 state is an output
+    bool third = false;
+    for (int i = 0; i < p.g.nroles; ++i)
+      third = third || (p.g.role[i].s_out && std::is_same<T, __nv_bfloat16>::value);
+    const size_t smem = C::kSegSmem + (third ? C::kCBytes : 0);
+    cudaError_t es = ensure_smem((const void*)attn_segments<T, DA, DC>, smem);
+    if (es == cudaSuccess)
+      es = launch_pdl(attn_segments<T, DA, DC>, dim3((unsigned)blocks), dim3(C::kThreads), smem, st, p);
     if (es != cudaSuccess) return es;
-    p.states_only = 0;
   }
   return launch_pdl(attn_chunks<T, DA, DC>, dim3((unsigned)blocks), dim3(C::kThreads), C::kSmem, st, p);
 }

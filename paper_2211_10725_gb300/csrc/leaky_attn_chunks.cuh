@@ -28,9 +28,10 @@
 // third part makes them 24.  fp16 has not the range of a sum of products: its
 // state copy is scaled by a power of two.
 //
-// Few heads and many tokens: the tokens are cut into segments, a first launch
-// finds each segment's own contribution to the state (update products only),
-// and each segment then starts from the decayed sum of those before it.
+// Few heads and many tokens: the tokens are cut into segments, a first kernel
+// (attn_segments: update products only) finds each segment's own contribution
+// to the state, and each segment then starts from the decayed sum of those
+// before it.
 #pragma once
 
 #include <cuda.h>
@@ -60,7 +61,6 @@ struct ChunkArgs {
   RoleMaps map[kMaxRoles];
   int nseg;             // segments of a sequence
   int seg_tokens;       // tokens of a segment, a multiple of kChunk
-  int states_only;      // the first launch of a segmented run
   float* seg_state;     // [role][B*H][nseg] states in fragment order
 };
 
@@ -84,8 +84,13 @@ struct Cfg {
   static constexpr int kScoreBytes = kSharedOut ? 0 : kBoxBytes;
   static constexpr int kOutBytes = kCBytes;
   static constexpr int kTail = 1024;               // barriers, tables
+  // a's place, big enough to take a third part of the values after a's last use
+  static constexpr int kQBytes = kLowInA || kABytes > kCBytes ? kABytes : kCBytes;
   static constexpr size_t kSmem =
-      2 * kABytes + 2 * kCBytes + kLowBytes + kEBytes + kScoreBytes + kOutBytes + kTail;
+      kQBytes + kABytes + 2 * kCBytes + kLowBytes + kEBytes + kScoreBytes + kOutBytes + kTail;
+  // attn_segments: two stages of b and c, the parts of the decayed values
+  static constexpr size_t kSegSmem = 2 * (kABytes + kCBytes) + 2 * kCBytes + kTail;
+  static constexpr uint32_t kSegTmemCols = 2 * DA;
   // tensor memory: output, update (scores in its first 64 columns), state
   static constexpr uint32_t kTmemCols = kStateTmem ? 256 : (DA == 64 ? 128 : 256);
   static constexpr int kBlocksPerSm = kThreads == 128 ? 4 : 2;
@@ -296,6 +301,308 @@ __device__ __forceinline__ int wait_all(uint64_t* bar, uint32_t parity) {
   return fail;
 }
 
+// beta^n by direction: at 64 + n (64 - n for a role backwards in time), n = 0 ..
+// 64, zeros on the other side; and in two 16-bit parts.
+template <typename T>
+struct Decays {
+  float lag[2 * kChunk + 1];
+  typename Pair<T>::type parts[kChunk + 1];
+  float segment;  // beta^tokens of a segment
+
+  __device__ __forceinline__ void fill(float beta, bool rev, int seg_tokens, int tid) {
+    if (tid > kChunk + 1) return;
+    const float w = power(beta, tid <= kChunk ? tid : seg_tokens);
+    if (tid > kChunk) {
+      segment = w;
+      return;
+    }
+    const T hi = T(w);
+    parts[tid] = typename Pair<T>::type(hi, T(w - (float)hi));
+    if (tid > 0) lag[rev ? kChunk + tid : kChunk - tid] = 0.0f;
+    lag[rev ? kChunk - tid : kChunk + tid] = w;
+  }
+  __device__ __forceinline__ float of(int n, bool rev) const { return lag[rev ? kChunk - n : kChunk + n]; }
+};
+
+// Where a block is: which role, head and segment, and that segment's tokens.
+struct Place {
+  int role, seg, row, b, h;
+  int len;        // tokens of the sequence
+  int begin;      // first token of the segment
+  int tokens;     // tokens of it that exist
+  int chunks;
+  int last_seg;   // segment of the sequence's last token
+  int order;      // place of this segment in time, 0 .. last_seg
+
+  __device__ __forceinline__ explicit Place(const ChunkArgs& p) {
+    role = blockIdx.x % p.g.nroles;
+    seg = (blockIdx.x / p.g.nroles) % p.nseg;
+    row = blockIdx.x / (p.g.nroles * p.nseg);
+    b = row / p.g.H;
+    h = row % p.g.H;
+  }
+  __device__ __forceinline__ void measure(const ChunkArgs& p, bool rev) {
+    len = seq_len(p.g, b);
+    begin = seg * p.seg_tokens;
+    tokens = max(0, min(len, min(p.g.T, begin + p.seg_tokens)) - begin);
+    chunks = (tokens + kChunk - 1) / kChunk;
+    last_seg = len > 0 ? (len - 1) / p.seg_tokens : 0;
+    order = rev ? last_seg - seg : seg;
+  }
+  __device__ __forceinline__ int start(int it, bool rev) const {  // first token of chunk it in time
+    return begin + kChunk * (rev ? chunks - 1 - it : it);
+  }
+};
+
+// A thread's part of a head's transposed state: channels row + 16*rh (+8) of c,
+// columns col + 8k (+1) of a and b.
+template <int DA, int DC>
+struct State {
+  using C = Cfg<DA, DC>;
+  float e[C::kRowHalves][C::kCols / 2];
+  int row, col;
+
+  __device__ __forceinline__ State(int quad, int half, int lane)
+      : row((C::kRowHalves == 2 ? 32 : 16) * quad + (lane >> 2)), col(half * C::kCols + 2 * (lane & 3)) {
+    each([](float& x, int, int) { x = 0.0f; });
+  }
+  template <typename F>
+  __device__ __forceinline__ void each(F f) {  // f(value, channel, column)
+#pragma unroll
+    for (int rh = 0; rh < C::kRowHalves; ++rh)
+#pragma unroll
+      for (int i = 0; i < C::kCols / 2; ++i)
+        f(e[rh][i], row + 16 * rh + 8 * ((i >> 1) & 1), col + 8 * (i >> 2) + (i & 1));
+  }
+  // e = f * the caller's state (zeros where there is none)
+  __device__ __forceinline__ void load(const Args& g, const Role& r, int b, int h, float f) {
+    const int64_t so = r.s_in ? state_offset(g, b, h) : -1;
+    if (so < 0) return;
+    const float* s = r.s_in + so;
+    const int64_t sr = r.s_trans ? g.Dv : 1, sc = r.s_trans ? 1 : g.Dv;
+    each([&](float& x, int y, int c) {
+      if (y < r.Dc && c < r.Da) x = f * s[y * sr + c * sc];
+    });
+  }
+  __device__ __forceinline__ void store(const Args& g, const Role& r, int b, int h, float f) {
+    const int64_t so = state_offset(g, b, h);
+    if (so < 0) return;
+    float* s = r.s_out + so;
+    const int64_t sr = r.s_trans ? g.Dv : 1, sc = r.s_trans ? 1 : g.Dv;
+    each([&](float& x, int y, int c) {
+      if (y < r.Dc && c < r.Da) s[y * sr + c * sc] = f * x;
+    });
+  }
+  // segment states: four neighbouring registers of every thread in turn
+  __device__ __forceinline__ void put_segment(float* at, int tid) {
+#pragma unroll
+    for (int rh = 0; rh < C::kRowHalves; ++rh)
+#pragma unroll
+      for (int i = 0; i < C::kCols / 2; i += 4)
+        reinterpret_cast<float4*>(at)[(rh * (C::kCols / 8) + i / 4) * C::kThreads + tid] =
+            make_float4(e[rh][i], e[rh][i + 1], e[rh][i + 2], e[rh][i + 3]);
+  }
+  __device__ __forceinline__ void add_segment(const float* at, int tid, float decay) {  // e = decay e + it
+#pragma unroll
+    for (int rh = 0; rh < C::kRowHalves; ++rh)
+#pragma unroll
+      for (int i = 0; i < C::kCols / 2; i += 4) {
+        const float4 v =
+            reinterpret_cast<const float4*>(at)[(rh * (C::kCols / 8) + i / 4) * C::kThreads + tid];
+        e[rh][i] = fmaf(e[rh][i], decay, v.x);
+        e[rh][i + 1] = fmaf(e[rh][i + 1], decay, v.y);
+        e[rh][i + 2] = fmaf(e[rh][i + 2], decay, v.z);
+        e[rh][i + 3] = fmaf(e[rh][i + 3], decay, v.w);
+      }
+  }
+  // e = decay e + the update product in tensor memory
+  __device__ __forceinline__ void add_update(uint32_t at, float decay) {
+#pragma unroll
+    for (int rh = 0; rh < C::kRowHalves; ++rh) {
+      float u[C::kCols / 2];
+      tmem_ld_rows(at + ((uint32_t)(16 * rh) << 16), u);
+#pragma unroll
+      for (int i = 0; i < C::kCols / 2; ++i) e[rh][i] = fmaf(decay, e[rh][i], u[i]);
+    }
+  }
+};
+
+// The decayed values of a chunk: piece i of this thread, hi and lo parts.
+// `at` is the power of the decay (0 for a place past the sequence, whose
+// values count as zero).
+template <typename T>
+__device__ __forceinline__ void split_piece(const unsigned char* values, int piece, bool live,
+                                            typename Pair<T>::type w, uint4& hi, uint4& lo) {
+  using T2 = typename Pair<T>::type;
+  uint4 v = reinterpret_cast<const uint4*>(values)[piece];
+  if (!live) v = make_uint4(0, 0, 0, 0);
+  const T2 w1 = T2(w.x, w.x), w2 = T2(w.y, w.y);
+  const T2* vp = reinterpret_cast<const T2*>(&v);
+  T2 *hp = reinterpret_cast<T2*>(&hi), *lp = reinterpret_cast<T2*>(&lo);
+#pragma unroll
+  for (int e = 0; e < 4; ++e) split_product(vp[e], w1, w2, hp[e], lp[e]);
+}
+// What the two parts left of v w, to 16 bits.
+template <typename T>
+__device__ __forceinline__ uint4 third_part(const unsigned char* values, int piece, bool live, float w,
+                                            uint4 hi, uint4 lo) {
+  float v[8], a[8], b[8];
+  Elem<T>::load8(reinterpret_cast<const T*>(values) + piece * 8, v);
+  Elem<T>::load8(reinterpret_cast<const T*>(&hi), a);
+  Elem<T>::load8(reinterpret_cast<const T*>(&lo), b);
+#pragma unroll
+  for (int e = 0; e < 8; ++e) v[e] = live ? fmaf(v[e], w, -a[e]) - b[e] : 0.0f;
+  uint4 out;
+  Elem<T>::store8(reinterpret_cast<T*>(&out), v);
+  return out;
+}
+
+// Zero the places past the sequence's end in a tile of 128-byte rows.
+__device__ __forceinline__ void clear_rows(unsigned char* tile, int bytes, int n, int tid, int threads) {
+  for (int i = tid; i < bytes / 16; i += threads)
+    if (((i >> 3) & 63) >= n) reinterpret_cast<uint4*>(tile)[i] = make_uint4(0, 0, 0, 0);
+}
+
+// The first kernel of a segmented run: each segment's state after its own
+// tokens (the first one's from the caller's state, kept too, because that may
+// be overwritten in place).  Bound by the reads of b and c: their tiles have
+// two stages, and the state is updated from one accumulator while the next
+// chunk's products fill the other.
+template <typename T, int DA, int DC>
+__global__ void __launch_bounds__(Cfg<DA, DC>::kThreads, Cfg<DA, DC>::kBlocksPerSm)
+    attn_segments(const __grid_constant__ ChunkArgs p) {
+  using C = Cfg<DA, DC>;
+  constexpr int NT = C::kThreads;
+  constexpr bool kHalf = std::is_same<T, __half>::value;
+  constexpr int kStage = C::kABytes + C::kCBytes;
+  extern __shared__ __align__(1024) unsigned char smem[];
+  unsigned char* sW = smem + 2 * kStage;
+  unsigned char* sL = sW + C::kCBytes;
+  uint64_t* bar = reinterpret_cast<uint64_t*>(sL + C::kCBytes);  // [2] loads, [1] update
+  uint64_t* bar_u = bar + 2;
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bar + 3);
+  Decays<T>& decays = *reinterpret_cast<Decays<T>*>(bar + 4);
+  unsigned char* sT = sL + C::kCBytes + C::kTail;  // third parts, where there are any
+
+  const int tid = threadIdx.x, warp = __shfl_sync(0xffffffffu, tid >> 5, 0), lane = tid & 31;
+  const int quad = warp & 3, half = warp >> 2;
+  const Args& g = p.g;
+  Place at(p);
+  const Role& r = g.role[at.role];
+  const RoleMaps& maps = p.map[at.role];
+  const bool rev = r.rev != 0;
+  const int hb = at.h / r.b.group, hc = at.h / r.c.group;
+
+  if (tid == 0) {
+    for (int i = 0; i < 3; ++i) mbar_init(&bar[i], 1);
+    fence_barrier_init();
+  }
+  __syncwarp();
+  if (warp == 0) gemm::tmem_alloc(tmem_slot, C::kSegTmemCols);
+  gemm::tc_fence_before();
+  __syncthreads();
+  gemm::tc_fence_after();
+  const uint32_t tmem = *tmem_slot;
+  grid_dep_wait();
+
+  const float beta = g.beta[at.h];
+  at.measure(p, rev);
+  const bool wanted = at.seg <= at.last_seg && at.order < at.last_seg;  // something starts after it
+  const int n_chunks = wanted ? at.chunks : 0;
+  auto load = [&](int it) {
+    unsigned char* stage = smem + (it & 1) * kStage;
+    const int t0 = at.start(it, rev);
+    mbar_arrive_expect_tx(&bar[it & 1], kStage);
+#pragma unroll
+    for (int x = 0; x < DA / 64; ++x)
+      tma_load_4d(stage + x * kBoxBytes, &maps.b, 64 * x, t0, hb, at.b, &bar[it & 1]);
+#pragma unroll
+    for (int x = 0; x < DC / 64; ++x)
+      tma_load_4d(stage + C::kABytes + x * kBoxBytes, &maps.c, 64 * x, t0, hc, at.b, &bar[it & 1]);
+  };
+  if (tid == 0) {
+    if (n_chunks > 0) load(0);
+    if (n_chunks > 1) load(1);
+  }
+  decays.fill(beta, rev, p.seg_tokens, tid);
+  State<DA, DC> state(quad, half, lane);
+  float* const seg0 = p.seg_state + ((size_t)at.role * g.B * g.H + at.row) * p.nseg * (size_t)(DA * DC);
+  if (at.order == 0) {
+    state.load(g, r, at.b, at.h, rev ? 1.0f / g.scale : (at.len > 0 ? beta : 1.0f));
+    state.put_segment(seg0, tid);
+  }
+  __syncthreads();
+
+  const uint32_t t_upd = tmem + ((uint32_t)(quad * 32) << 16) + half * C::kCols;
+  const bool third = !kHalf && r.s_out;
+  int fail = 0, it = 0, n_last = 0;
+  for (; it < n_chunks; ++it) {
+    const int n = min(kChunk, at.len - at.start(it, rev));
+    unsigned char* sB = smem + (it & 1) * kStage;
+    unsigned char* sC = sB + C::kABytes;
+    if (it > 0) {  // the last products have read their operands
+      fail |= wait_all(bar_u, (it - 1) & 1);
+      if (tid == 32 && it + 1 < n_chunks) load(it + 1);
+      __syncwarp();
+    }
+    fail |= wait_all(&bar[it & 1], (it >> 1) & 1);
+#pragma unroll
+    for (int i = 0; i < C::kCBytes / 16 / NT; ++i) {
+      const int piece = i * NT + tid, y = (piece >> 3) & 63;
+      const int lag = max(0, rev ? y + 1 : n - y);
+      uint4 hi, lo;
+      split_piece<T>(sC, piece, y < n, decays.parts[lag], hi, lo);
+      reinterpret_cast<uint4*>(sW)[piece] = hi;
+      reinterpret_cast<uint4*>(sL)[piece] = lo;
+      if (third)
+        reinterpret_cast<uint4*>(sT)[piece] = third_part<T>(sC, piece, y < n, decays.of(lag, rev), hi, lo);
+    }
+    if (n < kChunk) clear_rows(sB, C::kABytes, n, tid, NT);
+    gemm::fence_async_smem();
+    gemm::tc_fence_before();
+    if (__syncthreads_or(fail)) break;
+    if (warp == 0) {
+      gemm::tc_fence_after();
+      const uint32_t e = elect_one();
+      constexpr uint32_t id = idesc<T>(DC, DA, true, true);
+#pragma unroll
+      for (int part = 0; part < 3; ++part) {
+        if (part == 2 && !third) continue;
+        const unsigned char* values = part == 0 ? sW : part == 1 ? sL : sT;
+#pragma unroll
+        for (int kk = 0; kk < kChunk / 16; ++kk)
+          mma_ss(e, tmem + (it & 1) * DA, sdesc_mn(values + kk * 2048, kBoxBytes),
+                 sdesc_mn(sB + kk * 2048, kBoxBytes), id, part | kk);
+      }
+      mma_commit(e, bar_u);
+    }
+    if (it > 0) {
+      gemm::tc_fence_after();
+      state.add_update(t_upd + ((it - 1) & 1) * DA, decays.of(n_last, rev));
+    }
+    n_last = n;
+  }
+  if (it < n_chunks) {  // a wait gave up: loads in flight land before the block may exit
+    if (fail) record_status(g.status, kStatusTimeout);
+    if (tid == 0)
+      for (int j = it; j < min(it + 2, n_chunks); ++j)
+        mbar_wait_bounded(&bar[j & 1], (j >> 1) & 1, gemm::kDrainWaitNs);
+  } else if (wanted) {
+    if (n_chunks > 0) {
+      if (wait_all(bar_u, (n_chunks - 1) & 1)) record_status(g.status, kStatusTimeout);
+      gemm::tc_fence_after();
+      state.add_update(t_upd + ((n_chunks - 1) & 1) * DA, decays.of(n_last, rev));
+    }
+    state.put_segment(seg0 + (size_t)(at.order + 1) * (DA * DC), tid);
+  }
+  gemm::tc_fence_before();
+  __syncthreads();
+  if (warp == 0) {
+    gemm::tc_fence_after();
+    gemm::tmem_dealloc(tmem, C::kSegTmemCols);
+  }
+}
+
 template <typename T, int DA, int DC>
 __global__ void __launch_bounds__(Cfg<DA, DC>::kThreads, Cfg<DA, DC>::kBlocksPerSm)
     attn_chunks(const __grid_constant__ ChunkArgs p) {
@@ -306,7 +613,7 @@ __global__ void __launch_bounds__(Cfg<DA, DC>::kThreads, Cfg<DA, DC>::kBlocksPer
   constexpr bool kHalf = std::is_same<T, __half>::value;
   extern __shared__ __align__(1024) unsigned char smem[];
   unsigned char* sA = smem;
-  unsigned char* sB = sA + C::kABytes;
+  unsigned char* sB = sA + C::kQBytes;
   unsigned char* sC = sB + C::kABytes;
   unsigned char* sW = sC + C::kCBytes;                    // decayed values, high parts
   unsigned char* sL = C::kLowInA ? sA : sW + C::kCBytes;  // low parts
@@ -318,24 +625,18 @@ __global__ void __launch_bounds__(Cfg<DA, DC>::kThreads, Cfg<DA, DC>::kBlocksPer
            *bar_o = bar + 5, *bar_x = bar + 6;
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bar + 7);
   unsigned* top = reinterpret_cast<unsigned*>(bar + 8);  // [2] bits of the state's largest element
-  float* seg_decay = reinterpret_cast<float*>(bar + 9);
-  // beta^n at 64 + n (64 - n for a role backwards in time), n = 0 .. 64; zeros
-  // on the other side: the weight of token j at token i, at i - j + 64
-  float* lag = reinterpret_cast<float*>(bar + 10);  // [129]
-  T2* wt = reinterpret_cast<T2*>(lag + 129);        // [65] beta^n in two 16-bit parts
+  Decays<T>& decays = *reinterpret_cast<Decays<T>*>(bar + 9);
 
   const int tid = threadIdx.x, warp = __shfl_sync(0xffffffffu, tid >> 5, 0), lane = tid & 31;
   const int quad = warp & 3, half = warp >> 2;
   const Args& g = p.g;
-  const int role = blockIdx.x % g.nroles;
-  const int seg = (blockIdx.x / g.nroles) % p.nseg;
-  const int row = blockIdx.x / (g.nroles * p.nseg);
-  const int b = row / g.H, h = row % g.H;
-  const Role& r = g.role[role];
-  const RoleMaps& maps = p.map[role];
-  const bool rev = r.rev != 0, out_f32 = r.out_f32 != 0, states_only = p.states_only != 0;
+  Place at(p);
+  const Role& r = g.role[at.role];
+  const RoleMaps& maps = p.map[at.role];
+  const bool rev = r.rev != 0, out_f32 = r.out_f32 != 0;
+  const int b = at.b, h = at.h;
   const int ha = h / r.a.group, hb = h / r.b.group, hc = h / r.c.group, ho = h / r.out.group;
-  const int Da = r.Da, Dc = r.Dc, T_all = g.T;
+  const int Dc = r.Dc, T_all = g.T;
   const float scale = g.scale;
 
   if (tid == 0) {
@@ -351,36 +652,28 @@ __global__ void __launch_bounds__(Cfg<DA, DC>::kThreads, Cfg<DA, DC>::kBlocksPer
   const uint32_t tmem = *tmem_slot;
   grid_dep_wait();
 
-  const int len = seq_len(g, b);
-  const int t_begin = seg * p.seg_tokens;
-  const int t_end = min(T_all, t_begin + p.seg_tokens);
-  const int last_seg = len > 0 ? (len - 1) / p.seg_tokens : 0;
-  const int order = rev ? last_seg - seg : seg;  // place of this segment in time
-  const int n_tok = max(0, min(len, t_end) - t_begin);
-  int n_chunks = (n_tok + kChunk - 1) / kChunk;
-  if (states_only && order >= last_seg) n_chunks = 0;  // nothing starts after this one
-  const bool active = seg <= last_seg;
-  const bool ends = !states_only && r.s_out && (rev ? seg == 0 : seg == last_seg);
+  const float beta = g.beta[h];
+  at.measure(p, rev);
+  const int n_chunks = at.chunks;
+  const bool ends = r.s_out && (rev ? at.seg == 0 : at.seg == at.last_seg);
 
-  auto chunk_start = [&](int it) { return t_begin + kChunk * (rev ? n_chunks - 1 - it : it); };
   auto load_a = [&](int it) {
-    if (states_only) return;
     mbar_arrive_expect_tx(bar_a, C::kABytes);
 #pragma unroll
     for (int x = 0; x < DA / 64; ++x)
-      tma_load_4d(sA + x * kBoxBytes, &maps.a, 64 * x, chunk_start(it), ha, b, bar_a);
+      tma_load_4d(sA + x * kBoxBytes, &maps.a, 64 * x, at.start(it, rev), ha, b, bar_a);
   };
   auto load_b = [&](int it) {
     mbar_arrive_expect_tx(bar_b, C::kABytes);
 #pragma unroll
     for (int x = 0; x < DA / 64; ++x)
-      tma_load_4d(sB + x * kBoxBytes, &maps.b, 64 * x, chunk_start(it), hb, b, bar_b);
+      tma_load_4d(sB + x * kBoxBytes, &maps.b, 64 * x, at.start(it, rev), hb, b, bar_b);
   };
   auto load_c = [&](int it) {
     mbar_arrive_expect_tx(bar_c, C::kCBytes);
 #pragma unroll
     for (int x = 0; x < DC / 64; ++x)
-      tma_load_4d(sC + x * kBoxBytes, &maps.c, 64 * x, chunk_start(it), hc, b, bar_c);
+      tma_load_4d(sC + x * kBoxBytes, &maps.c, 64 * x, at.start(it, rev), hc, b, bar_c);
   };
   if (tid == 0 && n_chunks > 0) {
     load_a(0);
@@ -388,71 +681,16 @@ __global__ void __launch_bounds__(Cfg<DA, DC>::kThreads, Cfg<DA, DC>::kBlocksPer
     load_c(0);
   }
 
-  if (tid <= kChunk + 1) {
-    const float w = power(g.beta[h], tid <= kChunk ? tid : p.seg_tokens);
-    if (tid <= kChunk) {
-      const T hi = T(w), lo = T(w - (float)hi);
-      wt[tid] = T2(hi, lo);
-      if (tid > 0) lag[rev ? 64 + tid : 64 - tid] = 0.0f;
-      lag[rev ? 64 - tid : 64 + tid] = w;
-    } else {
-      *seg_decay = w;
-    }
-  }
+  decays.fill(beta, rev, p.seg_tokens, tid);
   __syncthreads();
-  auto decay_of = [&](int n) { return lag[rev ? 64 - n : 64 + n]; };  // beta^n
-
-  // this thread's part of the transposed state: channels erow + 16*rh (+8) of
-  // c, columns ecol + 8k (+1) of a and b
-  const int erow = (C::kRowHalves == 2 ? 32 : 16) * quad + (lane >> 2);
-  const int ecol = half * C::kCols + 2 * (lane & 3);
-  float E[C::kRowHalves][C::kCols / 2];
-  const int64_t so = (r.s_in || r.s_out) ? state_offset(g, b, h) : -1;
-  const int64_t s_row = r.s_trans ? g.Dv : 1, s_col = r.s_trans ? 1 : g.Dv;
-  auto each_state = [&](auto f) {  // f(value, channel, column) over the thread's part
-#pragma unroll
-    for (int rh = 0; rh < C::kRowHalves; ++rh)
-#pragma unroll
-      for (int i = 0; i < C::kCols / 2; ++i)
-        f(E[rh][i], erow + 16 * rh + 8 * ((i >> 1) & 1), ecol + 8 * (i >> 2) + (i & 1));
-  };
-  // segment states: four neighbouring registers of every thread in turn
-  constexpr size_t kSegFloats = (size_t)DA * DC;
-  float* const seg0 = p.seg_state + ((size_t)role * g.B * g.H + row) * p.nseg * kSegFloats;
-  auto store_segment = [&](int place) {
-    float4* s4 = reinterpret_cast<float4*>(seg0 + place * kSegFloats);
-#pragma unroll
-    for (int rh = 0; rh < C::kRowHalves; ++rh)
-#pragma unroll
-      for (int i = 0; i < C::kCols / 2; i += 4)
-        s4[(rh * (C::kCols / 8) + i / 4) * NT + tid] =
-            make_float4(E[rh][i], E[rh][i + 1], E[rh][i + 2], E[rh][i + 3]);
-  };
-  each_state([&](float& e, int, int) { e = 0.0f; });
-  if (order == 0 && (p.nseg == 1 || states_only)) {
-    if (r.s_in && so >= 0) {
-      const float f = rev ? 1.0f / scale : (len > 0 ? decay_of(1) : 1.0f);
-      const float* s_in = r.s_in + so;
-      each_state([&](float& e, int y, int x) {
-        if (y < Dc && x < Da) e = f * s_in[y * s_row + x * s_col];
-      });
-    }
-    if (states_only) store_segment(0);  // kept apart: the caller's state may be overwritten in place
-  } else if (!states_only && active) {
-    const float decay = *seg_decay;
-    for (int m = order == 0 ? 0 : 1; m <= order; ++m) {
-      const float4* s4 = reinterpret_cast<const float4*>(seg0 + m * kSegFloats);
-#pragma unroll
-      for (int rh = 0; rh < C::kRowHalves; ++rh)
-#pragma unroll
-        for (int i = 0; i < C::kCols / 2; i += 4) {
-          const float4 v = s4[(rh * (C::kCols / 8) + i / 4) * NT + tid];
-          E[rh][i] = fmaf(E[rh][i], decay, v.x);
-          E[rh][i + 1] = fmaf(E[rh][i + 1], decay, v.y);
-          E[rh][i + 2] = fmaf(E[rh][i + 2], decay, v.z);
-          E[rh][i + 3] = fmaf(E[rh][i + 3], decay, v.w);
-        }
-    }
+  State<DA, DC> state(quad, half, lane);
+  const float* const seg0 =
+      p.seg_state + ((size_t)at.role * g.B * g.H + at.row) * p.nseg * (size_t)(DA * DC);
+  if (p.nseg == 1) {
+    state.load(g, r, b, h, rev ? 1.0f / scale : (at.len > 0 ? beta : 1.0f));
+  } else if (at.seg <= at.last_seg) {
+    for (int m = at.order == 0 ? 0 : 1; m <= at.order; ++m)
+      state.add_segment(seg0 + (size_t)m * (DA * DC), tid, decays.segment);
   }
 
   const uint32_t t_quad = (uint32_t)(quad * 32) << 16;
@@ -465,7 +703,7 @@ __global__ void __launch_bounds__(Cfg<DA, DC>::kThreads, Cfg<DA, DC>::kBlocksPer
     float f = 1.0f;
     if constexpr (kHalf) {
       float m = 0.0f;
-      each_state([&](float& e, int, int) { m = fmaxf(m, fabsf(e)); });
+      state.each([&](float& e, int, int) { m = fmaxf(m, fabsf(e)); });
       const unsigned bits = __reduce_max_sync(0xffffffffu, __float_as_uint(m));
       if (lane == 0) atomicMax(&top[slot], bits);
       __syncthreads();
@@ -481,14 +719,14 @@ __global__ void __launch_bounds__(Cfg<DA, DC>::kThreads, Cfg<DA, DC>::kBlocksPer
       uint32_t v[C::kCols / 4];
 #pragma unroll
       for (int i = 0; i < C::kCols / 4; ++i)
-        v[i] = kHalf ? Elem<T>::from2(f * E[rh][2 * i], f * E[rh][2 * i + 1])
-                     : Elem<T>::from2(E[rh][2 * i], E[rh][2 * i + 1]);
+        v[i] = kHalf ? Elem<T>::from2(f * state.e[rh][2 * i], f * state.e[rh][2 * i + 1])
+                     : Elem<T>::from2(state.e[rh][2 * i], state.e[rh][2 * i + 1]);
       if constexpr (C::kStateTmem) {
         tmem_st_pairs(t_state + t_quad + ((uint32_t)(16 * rh) << 16) + half * (C::kCols / 2), v);
       } else {  // rows of Da: 64-column boxes of DC 128-byte rows
 #pragma unroll
         for (int i = 0; i < C::kCols / 4; ++i) {
-          const int x = half * C::kCols + 8 * (i >> 1), y = erow + 8 * (i & 1);
+          const int x = half * C::kCols + 8 * (i >> 1), y = state.row + 8 * (i & 1);
           *reinterpret_cast<uint32_t*>(sE + (x >> 6) * (DC * 128) + y * 128 +
                                        ((((x & 63) >> 3) ^ (y & 7)) << 4) + (lane & 3) * 4) = v[i];
         }
@@ -497,7 +735,7 @@ __global__ void __launch_bounds__(Cfg<DA, DC>::kThreads, Cfg<DA, DC>::kBlocksPer
     if constexpr (C::kStateTmem) tmem_wait_st();
   };
   __syncwarp();
-  if (!states_only && n_chunks > 0) {
+  if (n_chunks > 0) {
     put_state(0);
     gemm::fence_async_smem();
     gemm::tc_fence_before();
@@ -506,18 +744,19 @@ __global__ void __launch_bounds__(Cfg<DA, DC>::kThreads, Cfg<DA, DC>::kBlocksPer
 
   const int y0 = 16 * quad + (lane >> 2);            // this lane's score rows: y0, y0 + 8
   const int tok = half * C::kToks + 2 * (lane & 3);  // its output tokens: tok + 8k (+1)
-  const bool third = !kHalf && r.s_out;
+  // the third part: only the last segment's state is an output
+  const bool third = !kHalf && ends;
   uint32_t u_phase = 0;
   int fail = 0, it = 0;
   for (; it < n_chunks; ++it) {
     const uint32_t par = it & 1;
-    const int t0 = chunk_start(it);
-    const int n = min(kChunk, len - t0);
+    const int t0 = at.start(it, rev);
+    const int n = min(kChunk, at.len - t0);
     const bool last = ends && !rev && it == n_chunks - 1;  // leave S, not beta S
     const int ex = n - (last ? 1 : 0);
     const bool more = it + 1 < n_chunks;
 
-    if (!states_only && warp == 0) {
+    if (warp == 0) {
       if (kHalf && lane == 0) top[(it + 1) & 1] = 0u;
       fail |= wait_all(bar_a, par);
       fail |= wait_all(bar_b, par);
@@ -549,32 +788,35 @@ __global__ void __launch_bounds__(Cfg<DA, DC>::kThreads, Cfg<DA, DC>::kBlocksPer
 
     // decayed values in two parts
     fail |= wait_all(bar_c, par);
-    if (states_only) fail |= wait_all(bar_b, par);
     constexpr int kPieces = C::kCBytes / 16 / NT;
     uint4 low[kPieces];
 #pragma unroll
     for (int i = 0; i < kPieces; ++i) {
       const int piece = i * NT + tid, y = (piece >> 3) & 63;
-      uint4 v = reinterpret_cast<const uint4*>(sC)[piece], hi;
-      if (n < kChunk && y >= n) v = make_uint4(0, 0, 0, 0);
-      const int at = max(0, rev ? y + 1 : ex - y);
-      const T2 w = wt[at], w1 = T2(w.x, w.x), w2 = T2(w.y, w.y);
-      const T2* vp = reinterpret_cast<const T2*>(&v);
-      T2 *hp = reinterpret_cast<T2*>(&hi), *lp = reinterpret_cast<T2*>(&low[i]);
-#pragma unroll
-      for (int e = 0; e < 4; ++e) split_product(vp[e], w1, w2, hp[e], lp[e]);
-      reinterpret_cast<uint4*>(sW)[piece] = hi;
+      uint4 high;
+      split_piece<T>(sC, piece, y < n, decays.parts[max(0, rev ? y + 1 : ex - y)], high, low[i]);
+      reinterpret_cast<uint4*>(sW)[piece] = high;
       if (!C::kLowInA) reinterpret_cast<uint4*>(sL)[piece] = low[i];
     }
+    auto put_third = [&](unsigned char* to) {
+#pragma unroll
+      for (int i = 0; i < kPieces; ++i) {
+        const int piece = i * NT + tid, y = (piece >> 3) & 63;
+        reinterpret_cast<uint4*>(to)[piece] =
+            third_part<T>(sC, piece, y < n, decays.of(max(0, rev ? y + 1 : ex - y), rev),
+                          reinterpret_cast<const uint4*>(sW)[piece],
+                          reinterpret_cast<const uint4*>(sL)[piece]);
+      }
+    };
 
-    if (!states_only) {
+    {
       // decayed scores
       fail |= wait_all(bar_s, par);
       gemm::tc_fence_after();
       float s[C::kToks / 2];
       tmem_ld_rows(t_upd + t_quad + half * C::kToks, s);
       const int x0 = half * C::kToks;
-      const float* w = lag + 64 + y0 - x0 - 2 * (lane & 3);
+      const float* w = decays.lag + 64 + y0 - x0 - 2 * (lane & 3);
 #pragma unroll
       for (int i = 0; i < C::kToks / 2; ++i) s[i] = s[i] * scale * w[8 * ((i >> 1) & 1) - 8 * (i >> 2) - (i & 1)];
       if (n < kChunk) {  // places past the sequence hold anything
@@ -591,14 +833,14 @@ __global__ void __launch_bounds__(Cfg<DA, DC>::kThreads, Cfg<DA, DC>::kBlocksPer
       }
       if (!C::kSharedOut) fail |= wait_all(bar_x, par);
       gemm::tc_fence_after();
-      if (!C::kLowInA && tid == 32 && more) load_a(it + 1);
+      if (!C::kLowInA && tid == 32 && more && !third) load_a(it + 1);
       __syncwarp();
       // the inter product, decayed, is what the intra product adds to
       float f[C::kToks / 4];
 #pragma unroll
       for (int i = 0; i < C::kToks / 4; ++i) {
         const int y = tok + 8 * (i >> 1) + (i & 1);
-        f[i] = e_back * scale * lag[64 + (rev ? y + 1 - n : y)];
+        f[i] = e_back * scale * decays.lag[64 + (rev ? y + 1 - n : y)];
       }
 #pragma unroll
       for (int rh = 0; rh < C::kRowHalves; ++rh) {
@@ -614,12 +856,10 @@ __global__ void __launch_bounds__(Cfg<DA, DC>::kThreads, Cfg<DA, DC>::kBlocksPer
 #pragma unroll
       for (int i = 0; i < kPieces; ++i) reinterpret_cast<uint4*>(sL)[i * NT + tid] = low[i];
     }
-    if (n < kChunk) {  // clear the places past the sequence
-      const uint4 z = make_uint4(0, 0, 0, 0);
-      for (int i = tid; i < C::kABytes / 16; i += NT)
-        if (((i >> 3) & 63) >= n) reinterpret_cast<uint4*>(sB)[i] = z;
-      for (int i = tid; i < C::kCBytes / 16; i += NT)
-        if (((i >> 3) & 63) >= n) reinterpret_cast<uint4*>(sC)[i] = z;
+    if (!C::kLowInA && third) put_third(sA);  // the scores and the inter product have read a
+    if (n < kChunk) {
+      clear_rows(sB, C::kABytes, n, tid, NT);
+      clear_rows(sC, C::kCBytes, n, tid, NT);
     }
     if (!C::kSharedOut && tid == kStorer) bulk_wait_read_all();  // the last output has left sO
     gemm::fence_async_smem();
@@ -636,22 +876,21 @@ __global__ void __launch_bounds__(Cfg<DA, DC>::kThreads, Cfg<DA, DC>::kBlocksPer
     if (warp == 0) {
       gemm::tc_fence_after();
       const uint32_t e = elect_one();
-      if (!states_only) {
-        constexpr uint32_t id = idesc<T>(DC, kChunk, true, false);
+      constexpr uint32_t id = idesc<T>(DC, kChunk, true, false);
 #pragma unroll
-        for (int kk = 0; kk < kChunk / 16; ++kk)
-          mma_ss(e, t_out, sdesc_mn(sC + kk * 2048, kBoxBytes), gemm::sdesc_sw128(sP + kk * 32), id, 1);
-        mma_commit(e, bar_o);
-      }
+      for (int kk = 0; kk < kChunk / 16; ++kk)
+        mma_ss(e, t_out, sdesc_mn(sC + kk * 2048, kBoxBytes), gemm::sdesc_sw128(sP + kk * 32), id, 1);
+      mma_commit(e, bar_o);
       update(e, sW, 0);
       update(e, sL, 1);
+      if (!C::kLowInA && third) update(e, sA, 1);
       mma_commit(e, bar_u);
     }
 
-    if (!states_only) {
+    {
       fail |= wait_all(bar_o, par);
       gemm::tc_fence_after();
-      if (tid == 96 && more && !third) load_c(it + 1);
+      if (tid == 96 && more && !(C::kLowInA && third)) load_c(it + 1);
       __syncwarp();
 #pragma unroll
       for (int rh = 0; rh < C::kRowHalves; ++rh) {
@@ -663,7 +902,7 @@ __global__ void __launch_bounds__(Cfg<DA, DC>::kThreads, Cfg<DA, DC>::kBlocksPer
             if (tok + 8 * (i >> 2) + (i & 1) >= n) o[i] = 0.0f;
         }
         if (out_f32) {
-          const int y = erow + 16 * rh;
+          const int y = state.row + 16 * rh;
           float* d = static_cast<float*>(r.out.data) + b * r.out.sb + h * r.out.sh + y;
 #pragma unroll
           for (int i = 0; i < C::kToks / 2; ++i) {
@@ -672,7 +911,7 @@ __global__ void __launch_bounds__(Cfg<DA, DC>::kThreads, Cfg<DA, DC>::kBlocksPer
           }
         } else {
           // tokens as rows again: blocks (channels, +8) x (tokens 16j, 16j + 8)
-          const int x = (erow - (lane >> 2)) + 16 * rh;  // the warp's first channel
+          const int x = (state.row - (lane >> 2)) + 16 * rh;  // the warp's first channel
           unsigned char* tile = sO + (x >> 6) * kBoxBytes;
 #pragma unroll
           for (int j = 0; j < C::kToks / 16; ++j) {
@@ -688,19 +927,8 @@ __global__ void __launch_bounds__(Cfg<DA, DC>::kThreads, Cfg<DA, DC>::kBlocksPer
 
     fail |= wait_all(bar_u, u_phase);
     u_phase ^= 1;
-    if (third) {  // what the two parts left of the decayed values
-#pragma unroll
-      for (int i = 0; i < kPieces; ++i) {
-        const int piece = i * NT + tid, y = (piece >> 3) & 63;
-        float v[8], hi[8], lo[8];
-        Elem<T>::load8(reinterpret_cast<const T*>(sC) + piece * 8, v);
-        Elem<T>::load8(reinterpret_cast<const T*>(sW) + piece * 8, hi);
-        Elem<T>::load8(reinterpret_cast<const T*>(sL) + piece * 8, lo);
-        const float w = decay_of(max(0, rev ? y + 1 : ex - y));
-#pragma unroll
-        for (int e = 0; e < 8; ++e) v[e] = fmaf(v[e], w, -hi[e]) - lo[e];
-        Elem<T>::store8(reinterpret_cast<T*>(sW) + piece * 8, v);
-      }
+    if (C::kLowInA && third) {  // no buffer is free before the first parts are used
+      put_third(sW);
       gemm::fence_async_smem();
       if (__syncthreads_or(fail)) break;
       if (warp == 0) {
@@ -712,25 +940,16 @@ __global__ void __launch_bounds__(Cfg<DA, DC>::kThreads, Cfg<DA, DC>::kBlocksPer
       u_phase ^= 1;
     }
     gemm::tc_fence_after();
-    if (C::kLowInA && tid == 32 && more) load_a(it + 1);
+    if (tid == 32 && more && (C::kLowInA || third)) load_a(it + 1);
     if (tid == 64 && more) load_b(it + 1);
-    if (tid == 96 && more && third && !states_only) load_c(it + 1);
+    if (tid == 96 && more && C::kLowInA && third) load_c(it + 1);
     __syncwarp();
-    const float decay = decay_of(ex);
-#pragma unroll
-    for (int rh = 0; rh < C::kRowHalves; ++rh) {
-      float u[C::kCols / 2];
-      tmem_ld_rows(t_upd + t_quad + ((uint32_t)(16 * rh) << 16) + half * C::kCols, u);
-#pragma unroll
-      for (int i = 0; i < C::kCols / 2; ++i) E[rh][i] = fmaf(decay, E[rh][i], u[i]);
-    }
-    if (!states_only && more) put_state((it + 1) & 1);
+    state.add_update(t_upd + t_quad + half * C::kCols, decays.of(ex, rev));
+    if (more) put_state((it + 1) & 1);
     gemm::fence_async_smem();
     gemm::tc_fence_before();
     if (__syncthreads_or(fail)) break;
-    if (states_only) {
-      if (tid == 96 && more) load_c(it + 1);
-    } else if (tid == kStorer && !out_f32) {
+    if (tid == kStorer && !out_f32) {
 #pragma unroll
       for (int x = 0; x < DC / 64; ++x)
         tma_store_4d(&maps.out, sO + x * kBoxBytes, 64 * x, t0, ho, b);
@@ -743,27 +962,22 @@ __global__ void __launch_bounds__(Cfg<DA, DC>::kThreads, Cfg<DA, DC>::kBlocksPer
     // it + 1's where they were started
     if (tid == 0) {
       for (int j = 0; j < 2; ++j) {
-        if (!states_only) mbar_wait_bounded(bar_a, (it + j) & 1, gemm::kDrainWaitNs / 4);
+        mbar_wait_bounded(bar_a, (it + j) & 1, gemm::kDrainWaitNs / 4);
         mbar_wait_bounded(bar_b, (it + j) & 1, gemm::kDrainWaitNs / 4);
         mbar_wait_bounded(bar_c, (it + j) & 1, gemm::kDrainWaitNs / 4);
       }
     }
-  } else if (states_only) {
-    if (active && order < last_seg) store_segment(order + 1);
-  } else if (ends && so >= 0) {
-    const float f = rev ? scale : 1.0f;
-    float* s_out = r.s_out + so;
-    each_state([&](float& e, int y, int x) {
-      if (y < Dc && x < Da) s_out[y * s_row + x * s_col] = f * e;
-    });
+  } else if (ends) {
+    state.store(g, r, b, h, rev ? scale : 1.0f);
   }
-  if (!states_only) {
+  {
     // whole chunks past the sequence's end
-    const int from = t_begin + (n_tok + kChunk - 1) / kChunk * kChunk;
+    const int from = at.begin + at.chunks * kChunk;
+    const int to = min(T_all, at.begin + p.seg_tokens);
     const int per = out_f32 ? 4 : 8, pieces = Dc / per;
     const size_t es = out_f32 ? 4 : 2;
     unsigned char* o = static_cast<unsigned char*>(r.out.data) + (b * r.out.sb + ho * r.out.sh) * es;
-    for (int i = tid; i < (t_end - from) * pieces; i += NT)
+    for (int i = tid; i < (to - from) * pieces; i += NT)
       *reinterpret_cast<uint4*>(o + ((from + i / pieces) * r.out.st + (i % pieces) * per) * es) =
           make_uint4(0, 0, 0, 0);
   }
