@@ -120,6 +120,11 @@ cudaError_t launch_tile(const ChunkArgs& p, cudaStream_t st) {
     cudaError_t es = ensure_smem((const void*)attn_segments<T, DA, DC>, smem);
     if (es == cudaSuccess)
       es = launch_pdl(attn_segments<T, DA, DC>, dim3((unsigned)blocks), dim3(C::kThreads), smem, st, p);
+    if (es == cudaSuccess && p.nseg > 2) {
+      const int64_t heads = (int64_t)p.g.B * p.g.H * p.g.nroles;
+      es = launch_pdl(attn_segment_scan, dim3((unsigned)(heads * (DA * DC / (4 * kScanThreads)))),
+                      dim3(kScanThreads), 0, st, p, DA * DC);
+    }
     if (es != cudaSuccess) return es;
   }
   return launch_pdl(attn_chunks<T, DA, DC>, dim3((unsigned)blocks), dim3(C::kThreads), C::kSmem, st, p);

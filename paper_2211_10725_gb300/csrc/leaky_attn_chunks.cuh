@@ -30,8 +30,7 @@
 //
 // Few heads and many tokens: the tokens are cut into segments, a first kernel
 // (attn_segments: update products only) finds each segment's own contribution
-// to the state, and each segment then starts from the decayed sum of those
-// before it.
+// to the state, a second (attn_segment_scan) the state each one starts from.
 #pragma once
 
 #include <cuda.h>
@@ -79,15 +78,15 @@ struct Cfg {
   // cost the fourth block of an SM) the place of a once it has been used
   static constexpr bool kLowInA = DA == 64 && DC == 64;
   static constexpr int kLowBytes = kLowInA ? 0 : kCBytes;
-  // the decayed scores' buffer is the output's as well where smem is short
-  static constexpr bool kSharedOut = kLowInA;
-  static constexpr int kScoreBytes = kSharedOut ? 0 : kBoxBytes;
-  static constexpr int kOutBytes = kCBytes;
+  static constexpr int kOutBytes = kCBytes;        // decayed scores (8 KB), then the output
   static constexpr int kTail = 1024;               // barriers, tables
+  // b has two stages, as its last use in a chunk is the latest (one in a
+  // 64 x 64 head, where the second would cost the fourth block of an SM)
+  static constexpr int kBStages = kLowInA ? 1 : 2;
   // a's place, big enough to take a third part of the values after a's last use
   static constexpr int kQBytes = kLowInA || kABytes > kCBytes ? kABytes : kCBytes;
   static constexpr size_t kSmem =
-      kQBytes + kABytes + 2 * kCBytes + kLowBytes + kEBytes + kScoreBytes + kOutBytes + kTail;
+      kQBytes + kBStages * kABytes + 2 * kCBytes + kLowBytes + kEBytes + kOutBytes + kTail;
   // attn_segments: two stages of b and c, the parts of the decayed values
   static constexpr size_t kSegSmem = 2 * (kABytes + kCBytes) + 2 * kCBytes + kTail;
   static constexpr uint32_t kSegTmemCols = 2 * DA;
@@ -112,6 +111,14 @@ __device__ __forceinline__ void tma_store_4d(const CUtensorMap* map, const void*
           reinterpret_cast<uint64_t>(map)),
       "r"(smem_u32(src)), "r"(x), "r"(y), "r"(z), "r"(w)
       : "memory");
+}
+
+// Bring a box into L2, ahead of the load that will want it.
+__device__ __forceinline__ void tma_prefetch_4d(const CUtensorMap* map, int x, int y, int z, int w) {
+  asm volatile("cp.async.bulk.prefetch.tensor.4d.L2.global.tile [%0, {%1, %2, %3, %4}];" ::"l"(
+                   reinterpret_cast<uint64_t>(map)),
+               "r"(x), "r"(y), "r"(z), "r"(w)
+               : "memory");
 }
 
 __device__ __forceinline__ void bulk_wait_read_all() {
@@ -307,15 +314,10 @@ template <typename T>
 struct Decays {
   float lag[2 * kChunk + 1];
   typename Pair<T>::type parts[kChunk + 1];
-  float segment;  // beta^tokens of a segment
 
-  __device__ __forceinline__ void fill(float beta, bool rev, int seg_tokens, int tid) {
-    if (tid > kChunk + 1) return;
-    const float w = power(beta, tid <= kChunk ? tid : seg_tokens);
-    if (tid > kChunk) {
-      segment = w;
-      return;
-    }
+  __device__ __forceinline__ void fill(float beta, bool rev, int tid) {
+    if (tid > kChunk) return;
+    const float w = power(beta, tid);
     const T hi = T(w);
     parts[tid] = typename Pair<T>::type(hi, T(w - (float)hi));
     if (tid > 0) lag[rev ? kChunk + tid : kChunk - tid] = 0.0f;
@@ -402,17 +404,17 @@ struct State {
         reinterpret_cast<float4*>(at)[(rh * (C::kCols / 8) + i / 4) * C::kThreads + tid] =
             make_float4(e[rh][i], e[rh][i + 1], e[rh][i + 2], e[rh][i + 3]);
   }
-  __device__ __forceinline__ void add_segment(const float* at, int tid, float decay) {  // e = decay e + it
+  __device__ __forceinline__ void get_segment(const float* at, int tid) {
 #pragma unroll
     for (int rh = 0; rh < C::kRowHalves; ++rh)
 #pragma unroll
       for (int i = 0; i < C::kCols / 2; i += 4) {
         const float4 v =
             reinterpret_cast<const float4*>(at)[(rh * (C::kCols / 8) + i / 4) * C::kThreads + tid];
-        e[rh][i] = fmaf(e[rh][i], decay, v.x);
-        e[rh][i + 1] = fmaf(e[rh][i + 1], decay, v.y);
-        e[rh][i + 2] = fmaf(e[rh][i + 2], decay, v.z);
-        e[rh][i + 3] = fmaf(e[rh][i + 3], decay, v.w);
+        e[rh][i] = v.x;
+        e[rh][i + 1] = v.y;
+        e[rh][i + 2] = v.z;
+        e[rh][i + 3] = v.w;
       }
   }
   // e = decay e + the update product in tensor memory
@@ -524,7 +526,7 @@ __global__ void __launch_bounds__(Cfg<DA, DC>::kThreads, Cfg<DA, DC>::kBlocksPer
     if (n_chunks > 0) load(0);
     if (n_chunks > 1) load(1);
   }
-  decays.fill(beta, rev, p.seg_tokens, tid);
+  decays.fill(beta, rev, tid);
   State<DA, DC> state(quad, half, lane);
   float* const seg0 = p.seg_state + ((size_t)at.role * g.B * g.H + at.row) * p.nseg * (size_t)(DA * DC);
   if (at.order == 0) {
@@ -603,29 +605,66 @@ __global__ void __launch_bounds__(Cfg<DA, DC>::kThreads, Cfg<DA, DC>::kBlocksPer
   }
 }
 
+// The second kernel of a segmented run: in place, the state that the segment at
+// each place in time starts from.  At 0 is the first one's; from 1 on, what the
+// segment before it added (1: with the first one's start), so
+//   E_1 = s_1,  E_m = beta^tokens E_{m-1} + s_m.
+// Every thread takes four neighbouring floats through all places, eight loads
+// in flight.
+constexpr int kScanThreads = 256;
+__global__ void __launch_bounds__(kScanThreads) attn_segment_scan(const __grid_constant__ ChunkArgs p,
+                                                                  int floats) {
+  grid_dep_wait();
+  const int per = floats / (4 * kScanThreads);  // blocks of a head
+  const int head = blockIdx.x / per;            // role * B * H + row
+  const int row = head % (p.g.B * p.g.H);
+  const int len = seq_len(p.g, row / p.g.H);
+  const int last_seg = len > 0 ? (len - 1) / p.seg_tokens : 0;
+  if (last_seg < 2) return;
+  const float decay = power(p.g.beta[row % p.g.H], p.seg_tokens);
+  const size_t step = (size_t)floats / 4;
+  float4* s = reinterpret_cast<float4*>(p.seg_state + (size_t)head * p.nseg * floats) +
+              (blockIdx.x % per) * kScanThreads + threadIdx.x;
+  float4 e = s[step];
+  for (int m = 2; m <= last_seg; m += 8) {
+    float4 v[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+      if (m + i <= last_seg) v[i] = s[(m + i) * step];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      if (m + i > last_seg) break;
+      e.x = fmaf(e.x, decay, v[i].x);
+      e.y = fmaf(e.y, decay, v[i].y);
+      e.z = fmaf(e.z, decay, v[i].z);
+      e.w = fmaf(e.w, decay, v[i].w);
+      s[(m + i) * step] = e;
+    }
+  }
+}
+
 template <typename T, int DA, int DC>
 __global__ void __launch_bounds__(Cfg<DA, DC>::kThreads, Cfg<DA, DC>::kBlocksPerSm)
     attn_chunks(const __grid_constant__ ChunkArgs p) {
   using C = Cfg<DA, DC>;
   using T2 = typename Pair<T>::type;
   constexpr int NT = C::kThreads;
-  constexpr int kStorer = C::kSharedOut ? 0 : NT - 32;  // thread that issues and awaits the output's copies
+  constexpr int kStorer = NT - 32;  // thread that issues and awaits the output's copies
   constexpr bool kHalf = std::is_same<T, __half>::value;
   extern __shared__ __align__(1024) unsigned char smem[];
   unsigned char* sA = smem;
-  unsigned char* sB = sA + C::kQBytes;
-  unsigned char* sC = sB + C::kABytes;
+  unsigned char* sB2 = sA + C::kQBytes;                   // the stages of b
+  unsigned char* sC = sB2 + C::kBStages * C::kABytes;
   unsigned char* sW = sC + C::kCBytes;                    // decayed values, high parts
   unsigned char* sL = C::kLowInA ? sA : sW + C::kCBytes;  // low parts
   unsigned char* sE = sW + C::kCBytes + C::kLowBytes;     // the state's copy (64-wide heads)
-  unsigned char* sP = sE + C::kEBytes;                    // decayed scores
-  unsigned char* sO = sP + C::kScoreBytes;                // the output
-  uint64_t* bar = reinterpret_cast<uint64_t*>(sO + C::kOutBytes);
-  uint64_t *bar_a = bar, *bar_b = bar + 1, *bar_c = bar + 2, *bar_s = bar + 3, *bar_u = bar + 4,
-           *bar_o = bar + 5, *bar_x = bar + 6;
-  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bar + 7);
-  unsigned* top = reinterpret_cast<unsigned*>(bar + 8);  // [2] bits of the state's largest element
-  Decays<T>& decays = *reinterpret_cast<Decays<T>*>(bar + 9);
+  unsigned char* sP = sE + C::kEBytes;                    // decayed scores, then the output
+  uint64_t* bar = reinterpret_cast<uint64_t*>(sP + C::kOutBytes);
+  uint64_t *bar_a = bar, *bar_b = bar + 1, *bar_c = bar + 3, *bar_s = bar + 4, *bar_u = bar + 5,
+           *bar_o = bar + 6, *bar_x = bar + 7, *bar_p = bar + 8;  // bar_b: one for each stage
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bar + 9);
+  unsigned* top = reinterpret_cast<unsigned*>(bar + 10);  // [2] bits of the state's largest element
+  Decays<T>& decays = *reinterpret_cast<Decays<T>*>(bar + 11);
 
   const int tid = threadIdx.x, warp = __shfl_sync(0xffffffffu, tid >> 5, 0), lane = tid & 31;
   const int quad = warp & 3, half = warp >> 2;
@@ -640,7 +679,7 @@ __global__ void __launch_bounds__(Cfg<DA, DC>::kThreads, Cfg<DA, DC>::kBlocksPer
   const float scale = g.scale;
 
   if (tid == 0) {
-    for (int i = 0; i < 7; ++i) mbar_init(&bar[i], 1);
+    for (int i = 0; i < 9; ++i) mbar_init(&bar[i], 1);
     top[0] = top[1] = 0u;
     fence_barrier_init();
   }
@@ -664,10 +703,12 @@ __global__ void __launch_bounds__(Cfg<DA, DC>::kThreads, Cfg<DA, DC>::kBlocksPer
       tma_load_4d(sA + x * kBoxBytes, &maps.a, 64 * x, at.start(it, rev), ha, b, bar_a);
   };
   auto load_b = [&](int it) {
-    mbar_arrive_expect_tx(bar_b, C::kABytes);
+    const int stage = it % C::kBStages;
+    unsigned char* to = sB2 + stage * C::kABytes;
+    mbar_arrive_expect_tx(bar_b + stage, C::kABytes);
 #pragma unroll
     for (int x = 0; x < DA / 64; ++x)
-      tma_load_4d(sB + x * kBoxBytes, &maps.b, 64 * x, at.start(it, rev), hb, b, bar_b);
+      tma_load_4d(to + x * kBoxBytes, &maps.b, 64 * x, at.start(it, rev), hb, b, bar_b + stage);
   };
   auto load_c = [&](int it) {
     mbar_arrive_expect_tx(bar_c, C::kCBytes);
@@ -675,13 +716,24 @@ __global__ void __launch_bounds__(Cfg<DA, DC>::kThreads, Cfg<DA, DC>::kBlocksPer
     for (int x = 0; x < DC / 64; ++x)
       tma_load_4d(sC + x * kBoxBytes, &maps.c, 64 * x, at.start(it, rev), hc, b, bar_c);
   };
+  // a and c of chunk it into L2: their buffers free up only shortly before
+  // they are wanted, so the loads themselves should not have to go to HBM
+  auto prefetch = [&](int it) {
+    if (it >= n_chunks) return;
+    const int t0 = at.start(it, rev);
+#pragma unroll
+    for (int x = 0; x < DC / 64; ++x) tma_prefetch_4d(&maps.c, 64 * x, t0, hc, b);
+#pragma unroll
+    for (int x = 0; x < DA / 64; ++x) tma_prefetch_4d(&maps.a, 64 * x, t0, ha, b);
+  };
   if (tid == 0 && n_chunks > 0) {
     load_a(0);
     load_b(0);
     load_c(0);
+    prefetch(1);
   }
 
-  decays.fill(beta, rev, p.seg_tokens, tid);
+  decays.fill(beta, rev, tid);
   __syncthreads();
   State<DA, DC> state(quad, half, lane);
   const float* const seg0 =
@@ -689,8 +741,7 @@ __global__ void __launch_bounds__(Cfg<DA, DC>::kThreads, Cfg<DA, DC>::kBlocksPer
   if (p.nseg == 1) {
     state.load(g, r, b, h, rev ? 1.0f / scale : (at.len > 0 ? beta : 1.0f));
   } else if (at.seg <= at.last_seg) {
-    for (int m = at.order == 0 ? 0 : 1; m <= at.order; ++m)
-      state.add_segment(seg0 + (size_t)m * (DA * DC), tid, decays.segment);
+    state.get_segment(seg0 + (size_t)at.order * (DA * DC), tid);
   }
 
   const uint32_t t_quad = (uint32_t)(quad * 32) << 16;
@@ -755,11 +806,14 @@ __global__ void __launch_bounds__(Cfg<DA, DC>::kThreads, Cfg<DA, DC>::kBlocksPer
     const bool last = ends && !rev && it == n_chunks - 1;  // leave S, not beta S
     const int ex = n - (last ? 1 : 0);
     const bool more = it + 1 < n_chunks;
+    unsigned char* sB = sB2 + (it % C::kBStages) * C::kABytes;
+    if (C::kBStages == 2 && tid == 64 && more) load_b(it + 1);  // chunk it - 1 is done with its stage
+    if (tid == 96) prefetch(it + 2);
 
     if (warp == 0) {
       if (kHalf && lane == 0) top[(it + 1) & 1] = 0u;
       fail |= wait_all(bar_a, par);
-      fail |= wait_all(bar_b, par);
+      fail |= wait_all(bar_b + it % C::kBStages, (it / C::kBStages) & 1);
       gemm::tc_fence_after();
       const uint32_t e = elect_one();
       constexpr uint32_t id_s = idesc<T>(kChunk, kChunk, false, false);
@@ -778,15 +832,10 @@ __global__ void __launch_bounds__(Cfg<DA, DC>::kThreads, Cfg<DA, DC>::kBlocksPer
         else
           mma_ss(e, t_out, gemm::sdesc_sw128(sE + (kk / 4) * (DC * 128) + (kk % 4) * 32), q, id_x, kk != 0);
       }
-      if (C::kSharedOut) {
-        if (lane == 0) bulk_wait_read_all();  // the last output has left the scores' buffer
-        __syncwarp();
-        asm volatile("" ::: "memory");
-      }
       mma_commit(e, bar_x);
     }
 
-    // decayed values in two parts
+    // decayed values in two parts, while the scores are under way
     fail |= wait_all(bar_c, par);
     constexpr int kPieces = C::kCBytes / 16 / NT;
     uint4 low[kPieces];
@@ -824,14 +873,14 @@ __global__ void __launch_bounds__(Cfg<DA, DC>::kThreads, Cfg<DA, DC>::kBlocksPer
         for (int i = 0; i < C::kToks / 2; ++i)
           if (max(y0 + 8 * ((i >> 1) & 1), x0 + 2 * (lane & 3) + 8 * (i >> 2) + (i & 1)) >= n) s[i] = 0.0f;
       }
-      if (C::kSharedOut) fail |= wait_all(bar_x, par);
+      if (it > 0) fail |= wait_all(bar_p, (it - 1) & 1);  // the last output has left sP
 #pragma unroll
       for (int k = 0; k < C::kToks / 8; ++k) {
         unsigned char* to = sP + y0 * 128 + ((((x0 >> 3) + k) ^ (y0 & 7)) << 4) + (lane & 3) * 4;
         *reinterpret_cast<uint32_t*>(to) = Elem<T>::from2(s[4 * k], s[4 * k + 1]);
         *reinterpret_cast<uint32_t*>(to + 1024) = Elem<T>::from2(s[4 * k + 2], s[4 * k + 3]);
       }
-      if (!C::kSharedOut) fail |= wait_all(bar_x, par);
+      fail |= wait_all(bar_x, par);
       gemm::tc_fence_after();
       if (!C::kLowInA && tid == 32 && more && !third) load_a(it + 1);
       __syncwarp();
@@ -861,7 +910,6 @@ __global__ void __launch_bounds__(Cfg<DA, DC>::kThreads, Cfg<DA, DC>::kBlocksPer
       clear_rows(sB, C::kABytes, n, tid, NT);
       clear_rows(sC, C::kCBytes, n, tid, NT);
     }
-    if (!C::kSharedOut && tid == kStorer) bulk_wait_read_all();  // the last output has left sO
     gemm::fence_async_smem();
     gemm::tc_fence_before();
     if (__syncthreads_or(fail)) break;
@@ -912,7 +960,7 @@ __global__ void __launch_bounds__(Cfg<DA, DC>::kThreads, Cfg<DA, DC>::kBlocksPer
         } else {
           // tokens as rows again: blocks (channels, +8) x (tokens 16j, 16j + 8)
           const int x = (state.row - (lane >> 2)) + 16 * rh;  // the warp's first channel
-          unsigned char* tile = sO + (x >> 6) * kBoxBytes;
+          unsigned char* tile = sP + (x >> 6) * kBoxBytes;
 #pragma unroll
           for (int j = 0; j < C::kToks / 16; ++j) {
             const int y = half * C::kToks + 16 * j + 8 * (lane >> 4) + (lane & 7);
@@ -941,7 +989,7 @@ __global__ void __launch_bounds__(Cfg<DA, DC>::kThreads, Cfg<DA, DC>::kBlocksPer
     }
     gemm::tc_fence_after();
     if (tid == 32 && more && (C::kLowInA || third)) load_a(it + 1);
-    if (tid == 64 && more) load_b(it + 1);
+    if (C::kBStages == 1 && tid == 64 && more) load_b(it + 1);
     if (tid == 96 && more && C::kLowInA && third) load_c(it + 1);
     __syncwarp();
     state.add_update(t_upd + t_quad + half * C::kCols, decays.of(ex, rev));
@@ -949,11 +997,15 @@ __global__ void __launch_bounds__(Cfg<DA, DC>::kThreads, Cfg<DA, DC>::kBlocksPer
     gemm::fence_async_smem();
     gemm::tc_fence_before();
     if (__syncthreads_or(fail)) break;
-    if (tid == kStorer && !out_f32) {
+    if (tid == kStorer) {
+      if (!out_f32) {
 #pragma unroll
-      for (int x = 0; x < DC / 64; ++x)
-        tma_store_4d(&maps.out, sO + x * kBoxBytes, 64 * x, t0, ho, b);
-      gemm::bulk_commit();
+        for (int x = 0; x < DC / 64; ++x)
+          tma_store_4d(&maps.out, sP + x * kBoxBytes, 64 * x, t0, ho, b);
+        gemm::bulk_commit();
+        bulk_wait_read_all();
+      }
+      mbar_arrive(bar_p);
     }
   }
   if (it < n_chunks) {  // a wait gave up
@@ -961,10 +1013,10 @@ __global__ void __launch_bounds__(Cfg<DA, DC>::kThreads, Cfg<DA, DC>::kBlocksPer
     // loads in flight land before the block may exit: chunk it's, and chunk
     // it + 1's where they were started
     if (tid == 0) {
-      for (int j = 0; j < 2; ++j) {
-        mbar_wait_bounded(bar_a, (it + j) & 1, gemm::kDrainWaitNs / 4);
-        mbar_wait_bounded(bar_b, (it + j) & 1, gemm::kDrainWaitNs / 4);
-        mbar_wait_bounded(bar_c, (it + j) & 1, gemm::kDrainWaitNs / 4);
+      for (int j = it; j < it + 2; ++j) {
+        mbar_wait_bounded(bar_a, j & 1, gemm::kDrainWaitNs / 4);
+        mbar_wait_bounded(bar_b + j % C::kBStages, (j / C::kBStages) & 1, gemm::kDrainWaitNs / 4);
+        mbar_wait_bounded(bar_c, j & 1, gemm::kDrainWaitNs / 4);
       }
     }
   } else if (ends) {
