@@ -18,63 +18,83 @@
 namespace snn {
 namespace attn {
 
-// out[b, t, hk, :] = sum over the group's query heads, in head order, of the
-// fp32 shares part[b, t, h, :], rounded once.
+// A shared head's gradients: out[b, t, hk, :] = sum over the group's query
+// heads, in head order, of their fp32 shares part[b, t, h, :], rounded once.
+// blockIdx.y picks the gradient (of k or of v).
+struct SumArgs {
+  const float* part[2];
+  Tensor out[2];
+  int D[2];
+  int Hk, G;
+  int64_t T, rows;  // rows: (b, t, hk)
+};
+
 template <typename T>
-__global__ void __launch_bounds__(256) sum_group(const float* __restrict__ part, Tensor out, int Hk,
-                                                 int G, int D, int64_t nt, int64_t n8) {
+__global__ void __launch_bounds__(256) sum_group(const SumArgs g) {
   grid_dep_wait();
+  const int which = blockIdx.y, D = g.D[which], d8 = D / 8;
   const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
-  if (i >= n8) return;
-  const int d8 = D / 8;
+  if (i >= g.rows * d8) return;
   const int d = (int)(i % d8) * 8;
-  const int64_t row = i / d8;  // (b, t, hk)
-  const int hk = (int)(row % Hk);
-  const int64_t bt = row / Hk;
-  const float* p = part + (bt * Hk + hk) * (int64_t)G * D + d;
+  const int64_t row = i / d8, bt = row / g.Hk;
+  const int hk = (int)(row % g.Hk);
+  const float* p = g.part[which] + row * g.G * D + d;
   float s[8];
   Elem<float>::load8(p, s);
-  for (int j = 1; j < G; ++j) {
+  for (int j = 1; j < g.G; ++j) {
     float v[8];
     Elem<float>::load8(p + (int64_t)j * D, v);
 #pragma unroll
     for (int e = 0; e < 8; ++e) s[e] += v[e];
   }
-  T* o = static_cast<T*>(out.data) + (bt / nt) * out.sb + (bt % nt) * out.st + hk * out.sh + d;
-  Elem<T>::store8(o, s);
+  const Tensor& o = g.out[which];
+  Elem<T>::store8(static_cast<T*>(o.data) + (bt / g.T) * o.sb + (bt % g.T) * o.st + hk * o.sh + d, s);
 }
 
 // ---------------------------------------------------------------------------
 // Host side
 // ---------------------------------------------------------------------------
 
-// How a run of `nroles` roles over B*H heads cuts T tokens into segments.
-// Every block costs its chunks and about kStart chunks of set-up; a segmented
-// run adds a launch over the segments (update products only, about half of a
-// chunk's time) and a sum of the earlier segments' states in each block.  The
-// count that ends soonest is taken, with full waves of kSlots resident blocks.
+// How a run of `nroles` roles over B*H heads cuts T tokens into segments: the
+// count that should end soonest, from the times (us) of a chunk in a block
+// alone on its SM and in one of a full SM, and of a block's start:
+//   128-wide heads, two blocks on an SM: attn_chunks 2.35 alone, 3.0 beside
+//   another (16384 tokens of 16 heads, 1 to 19 segments: 602 to 88);
+//   attn_segments 1.05 and 1.8.
+// Two segments of 777 tokens in 36 heads' three roles take 44 where one takes
+// 35; four of 1024 tokens in 32 heads take 26 where one takes 42.
 // A function of the shapes alone, so that a shape always sums in the same
 // order.
 struct Plan {
   int nseg = 1, seg_tokens = kChunk;
 };
 constexpr int kMaxSeg = 64;
+constexpr int kSms = 152;
 inline int tile(int64_t D) { return D <= 64 ? 64 : 128; }
+
+// Time of `blocks` blocks of `per` chunks, at most per_sm on an SM.
+double wave_time(int64_t blocks, int64_t per, int per_sm, double alone, double full) {
+  constexpr double kStart = 5.0;
+  const int64_t slots = (int64_t)kSms * per_sm, rest = blocks % slots;
+  const double on_sm = (double)ceil_div(rest, kSms);
+  const double chunk = alone + (full - alone) * (on_sm - 1.0) / (per_sm - 1);
+  return (double)(blocks / slots) * (kStart + full * per) + (rest ? kStart + chunk * per : 0.0);
+}
 
 Plan plan(const snn_attn_desc* d, int nroles) {
   const int64_t chunks = ceil_div(d->T, kChunk), heads = d->B * d->H * nroles;
-  const int64_t slots = tile(d->Dk) + tile(d->Dv) == 128 ? 152 * 4 : 152 * 2;
-  constexpr double kStart = 2.0, kHalf = 0.5, kSum = 0.1;
+  const int per_sm = tile(d->Dk) + tile(d->Dv) == 128 ? 4 : 2;
+  constexpr double kLaunch = 3.0, kScan = 2.0;
   Plan best;
-  double best_cost = 0.0;
-  for (int64_t s = 1; s <= kMaxSeg && s <= (chunks > 1 ? chunks : 1); ++s) {
-    const int64_t per = chunks > 0 ? ceil_div(chunks, s) : 1;
-    const int64_t n = chunks > 0 ? ceil_div(chunks, per) : 1;
-    const double waves = (double)ceil_div(heads * n, slots);
-    double cost = waves * (kStart + per);
-    if (n > 1) cost += waves * (kStart + kHalf * per) + kSum * n;
-    if (s == 1 || cost < best_cost) {
-      best_cost = cost;
+  if (chunks == 0) return best;
+  double best_time = 0.0;
+  for (int64_t s = 1; s <= kMaxSeg && s <= chunks; ++s) {
+    const int64_t per = ceil_div(chunks, s), n = ceil_div(chunks, per);
+    double t = wave_time(heads * n, per, per_sm, 2.35, 3.0);
+    if (n > 1) t += kLaunch + wave_time(heads * (n - 1), per, per_sm, 1.05, 1.8);
+    if (n > 2) t += kScan + 0.1 * n;
+    if (s == 1 || t < best_time) {
+      best_time = t;
       best.nseg = (int)n;
       best.seg_tokens = (int)(per * kChunk);
     }
@@ -157,10 +177,9 @@ cudaError_t launch(const snn_attn_desc* d, const Args& g, const Plan& pl, float*
 }
 
 template <typename T>
-cudaError_t launch_sum(const snn_attn_desc* d, const float* part, const snn_bthd* out, int D, cudaStream_t st) {
-  const int64_t n8 = d->B * d->T * d->Hk * (D / 8);
-  return launch_pdl(sum_group<T>, dim3((unsigned)((n8 + 255) / 256)), dim3(256), 0, st, part,
-                    tensor(out, 1), (int)d->Hk, (int)(d->H / d->Hk), D, d->T, n8);
+cudaError_t launch_sum(const SumArgs& g, cudaStream_t st) {
+  const int64_t n8 = g.rows * ((g.D[0] > g.D[1] ? g.D[0] : g.D[1]) / 8);
+  return launch_pdl(sum_group<T>, dim3((unsigned)((n8 + 255) / 256), 2), dim3(256), 0, st, g);
 }
 
 size_t share_bytes(const snn_attn_desc* d, int64_t D) {
@@ -303,7 +322,6 @@ snn_status_t snn_leaky_attn_bwd(const snn_attn_desc* desc, const snn_bthd* q, co
   rv.s_out = grad_state_in;
   rv.out_f32 = rk.out_f32 = G > 1;
   cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
-  const bool bf = desc->dtype == SNN_BF16;
   const Plan pl = plan(desc, 3);
   cudaError_t e;
   if (tile(desc->Dk) == tile(desc->Dv)) {
@@ -318,11 +336,10 @@ snn_status_t snn_leaky_attn_bwd(const snn_attn_desc* desc, const snn_bthd* q, co
       e = launch(desc, gv, pl, seg_state + (size_t)(desc->B * desc->H * 2) * pl.nseg * 64 * 128, st);
   }
   if (e == cudaSuccess && G > 1 && desc->T > 0) {
-    e = bf ? launch_sum<__nv_bfloat16>(desc, share_k, grad_k, g.Dk, st)
-           : launch_sum<__half>(desc, share_k, grad_k, g.Dk, st);
-    if (e == cudaSuccess)
-      e = bf ? launch_sum<__nv_bfloat16>(desc, share_v, grad_v, g.Dv, st)
-             : launch_sum<__half>(desc, share_v, grad_v, g.Dv, st);
+    const SumArgs sum{{share_k, share_v},  {tensor(grad_k, 1), tensor(grad_v, 1)}, {g.Dk, g.Dv},
+                      (int)desc->Hk,       G,
+                      desc->T,             desc->B * desc->T * desc->Hk};
+    e = desc->dtype == SNN_BF16 ? launch_sum<__nv_bfloat16>(sum, st) : launch_sum<__half>(sum, st);
   }
   return e == cudaSuccess ? SNN_OK : SNN_ERR_CUDA;
 }

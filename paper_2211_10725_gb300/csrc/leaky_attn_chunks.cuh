@@ -104,6 +104,10 @@ __device__ __forceinline__ void tma_load_4d(void* dst, const CUtensorMap* map, i
       : "memory");
 }
 
+__device__ __forceinline__ void prefetch_map(const CUtensorMap* map) {
+  asm volatile("prefetch.tensormap [%0];" ::"l"(reinterpret_cast<uint64_t>(map)) : "memory");
+}
+
 __device__ __forceinline__ void tma_store_4d(const CUtensorMap* map, const void* src, int x, int y,
                                              int z, int w) {
   asm volatile(
@@ -267,25 +271,9 @@ struct Pair<__half> {
   using type = __half2;
 };
 
-// x^n for n >= 0 as an unevaluated sum of two floats (about 46 bits), by
-// squaring: the tables' powers come out correctly rounded or next to it.
-struct Two {
-  float hi, lo;
-};
-__device__ __forceinline__ Two mul(Two a, Two b) {
-  const float p = a.hi * b.hi;
-  const float e = fmaf(a.hi, b.lo, fmaf(a.lo, b.hi, fmaf(a.hi, b.hi, -p)));
-  const float s = p + e;
-  return Two{s, e - (s - p)};
-}
-__device__ __forceinline__ float power(float x, int n) {
-  Two v{1.0f, 0.0f}, s{x, 0.0f};
-  for (; n > 0; n >>= 1) {
-    if (n & 1) v = mul(v, s);
-    s = mul(s, s);
-  }
-  return v.hi;
-}
+// x^n for 0 <= x <= 1, n >= 0.  The error is n |log2 x| 2^-24, i.e. |log2 of the
+// result| units: a weight that counts is as good as an fp32 product.
+__device__ __forceinline__ float power(float x, int n) { return n == 0 ? 1.0f : exp2f((float)n * log2f(x)); }
 
 // MN-major descriptor whose next 64 elements along MN are box_bytes on.
 __device__ __forceinline__ uint64_t sdesc_mn(const void* tile, uint32_t box_bytes) {
@@ -495,6 +483,10 @@ __global__ void __launch_bounds__(Cfg<DA, DC>::kThreads, Cfg<DA, DC>::kBlocksPer
   const bool rev = r.rev != 0;
   const int hb = at.h / r.b.group, hc = at.h / r.c.group;
 
+  if (tid == 32) {
+    prefetch_map(&maps.b);
+    prefetch_map(&maps.c);
+  }
   if (tid == 0) {
     for (int i = 0; i < 3; ++i) mbar_init(&bar[i], 1);
     fence_barrier_init();
@@ -678,6 +670,11 @@ __global__ void __launch_bounds__(Cfg<DA, DC>::kThreads, Cfg<DA, DC>::kBlocksPer
   const int Dc = r.Dc, T_all = g.T;
   const float scale = g.scale;
 
+  if (tid == 32) {
+    prefetch_map(&maps.a);
+    prefetch_map(&maps.b);
+    prefetch_map(&maps.c);
+  }
   if (tid == 0) {
     for (int i = 0; i < 9; ++i) mbar_init(&bar[i], 1);
     top[0] = top[1] = 0u;

@@ -497,41 +497,38 @@ def _attn_desc(where, B, T, H, Hk, Dk, Dv, dtype, scale) -> AttnDesc:
     return AttnDesc(B, T, H, Hk, Dk, Dv, code, scale)
 
 
-class _Strided:
-    """The snn_bthd or snn_rows structures of one call, as one array of 64-bit
-    words (both structures are a pointer and 64-bit strides)."""
-    __slots__ = ("where", "dtype", "words", "array")
+def _bthd(where, name, t, shape, dtype):
+    """The words of snn_bthd for a [B, T, heads, D] tensor (a [B, heads, D] one
+    for a single token) with contiguous D."""
+    if t.shape != shape or t.dtype != dtype or not t.is_cuda:
+        raise ValueError(f"{where}: {name} must be a CUDA {dtype} tensor of shape {shape}")
+    st = t.stride()
+    if st[-1] != 1 and shape[-1] > 1:
+        raise ValueError(f"{where}: {name} must have a contiguous last dimension")
+    return t.data_ptr(), st[0], st[1], st[-2]
 
-    def __init__(self, where):
-        self.where, self.words = where, []
 
-    def bthd(self, name, t, shape, dtype):
-        """Place of a [B, T, heads, D] tensor (a [B, heads, D] one for a single
-        token) with contiguous D."""
-        if t.shape != shape or t.dtype != dtype or not t.is_cuda:
-            raise ValueError(f"{self.where}: {name} must be a CUDA {dtype} tensor of shape {shape}")
-        st = t.stride()
-        if st[-1] != 1 and shape[-1] > 1:
-            raise ValueError(f"{self.where}: {name} must have a contiguous last dimension")
-        self.words += (t.data_ptr(), st[0], st[1], st[-2])
+def _rows(where, name, t, shape, dtype):
+    """The words of snn_rows for an [M, N] matrix with contiguous rows, or for None."""
+    if t is None:
+        return 0, 0
+    if t.shape != shape or t.dtype != dtype or not t.is_cuda:
+        raise ValueError(f"{where}: {name} must be a CUDA {dtype} tensor of shape {shape}")
+    ld, inner = t.stride()
+    if inner != 1 and shape[1] > 1:
+        raise ValueError(f"{where}: {name} must have contiguous rows")
+    return t.data_ptr(), ld
 
-    def rows(self, name, t, shape, dtype):
-        """Place of an [M, N] matrix with contiguous rows, or of None."""
-        if t is None:
-            self.words += (0, 0)
-            return
-        if t.shape != shape or t.dtype != dtype or not t.is_cuda:
-            raise ValueError(f"{self.where}: {name} must be a CUDA {dtype} tensor of shape {shape}")
-        ld, inner = t.stride()
-        if inner != 1 and shape[1] > 1:
-            raise ValueError(f"{self.where}: {name} must have contiguous rows")
-        self.words += (t.data_ptr(), ld)
 
-    def pointers(self, words):
-        """Addresses of the structures, of `words` words each."""
-        self.array = (ctypes.c_int64 * len(self.words))(*self.words)
-        at = ctypes.addressof(self.array)
-        return range(at, at + 8 * len(self.words), 8 * words)
+# a call's snn_bthd or snn_rows structures (a pointer and 64-bit strides) lie
+# in one array; its address and those of the structures in it
+_WORDS = {n: ctypes.c_int64 * n for n in (10, 16, 28)}
+
+
+def _places(words, each):
+    array = _WORDS[len(words)](*words)
+    at = ctypes.addressof(array)
+    return array, range(at, at + 8 * len(words), 8 * each)
 
 
 def _flat(where, name, t, shape, dtype):
@@ -574,12 +571,9 @@ def snn_leaky_attn_fwd(q, k, v, beta, o, ws, scale=1.0, seq_lens=None, state_in=
     if state_in is not None and state_out is not None and len(state_in) != len(state_out):
         raise ValueError(f"{w}: state_in and state_out differ in places")
     ps, n = _state_places(w, slots, B, (state_in, state_out))
-    x = _Strided(w)
-    x.bthd("q", q, (B, T, H, Dk), dt)
-    x.bthd("k", k, (B, T, Hk, Dk), dt)
-    x.bthd("v", v, (B, T, Hk, Dv), dt)
-    x.bthd("o", o, (B, T, H, Dv), dt)
-    pq, pk, pv, po = x.pointers(4)
+    array, (pq, pk, pv, po) = _places(
+        _bthd(w, "q", q, (B, T, H, Dk), dt) + _bthd(w, "k", k, (B, T, Hk, Dk), dt)
+        + _bthd(w, "v", v, (B, T, Hk, Dv), dt) + _bthd(w, "o", o, (B, T, H, Dv), dt), 4)
     _check(load_library().snn_leaky_attn_fwd(
         ctypes.byref(d), pq, pk, pv, _flat(w, "beta", beta, (H,), torch.float32),
         _flat(w, "seq_lens", seq_lens, (B,), torch.int32),
@@ -597,11 +591,10 @@ def snn_leaky_attn_bwd(q, k, v, beta, grad_o, grad_q, grad_k, grad_v, ws, scale=
     (B, T, H, Dk), Hk, Dv, dt = q.shape, k.shape[2], v.shape[-1], q.dtype
     d = _attn_desc(w, B, T, H, Hk, Dk, Dv, dt, scale)
     qs, ks, vs, os = (B, T, H, Dk), (B, T, Hk, Dk), (B, T, Hk, Dv), (B, T, H, Dv)
-    x = _Strided(w)
-    for name, t, shape in (("q", q, qs), ("k", k, ks), ("v", v, vs), ("grad_o", grad_o, os),
-                           ("grad_q", grad_q, qs), ("grad_k", grad_k, ks), ("grad_v", grad_v, vs)):
-        x.bthd(name, t, shape, dt)
-    pq, pk, pv, po, gq, gk, gv = x.pointers(4)
+    array, (pq, pk, pv, po, gq, gk, gv) = _places(
+        _bthd(w, "q", q, qs, dt) + _bthd(w, "k", k, ks, dt) + _bthd(w, "v", v, vs, dt)
+        + _bthd(w, "grad_o", grad_o, os, dt) + _bthd(w, "grad_q", grad_q, qs, dt)
+        + _bthd(w, "grad_k", grad_k, ks, dt) + _bthd(w, "grad_v", grad_v, vs, dt), 4)
     state = lambda name, t: _flat(w, name, t, (B, H, Dk, Dv), torch.float32)
     _check(load_library().snn_leaky_attn_bwd(
         ctypes.byref(d), pq, pk, pv, _flat(w, "beta", beta, (H,), torch.float32),
@@ -619,12 +612,9 @@ def snn_leaky_attn_step(q, k, v, beta, state, o, scale=1.0, slots=None, stream=N
     (B, H, Dk), Hk, Dv, dt = q.shape, k.shape[1], v.shape[-1], q.dtype
     d = _attn_desc(w, B, 1, H, Hk, Dk, Dv, dt, scale)
     n = state.shape[0]
-    x = _Strided(w)
-    x.bthd("q", q, (B, H, Dk), dt)
-    x.bthd("k", k, (B, Hk, Dk), dt)
-    x.bthd("v", v, (B, Hk, Dv), dt)
-    x.bthd("o", o, (B, H, Dv), dt)
-    pq, pk, pv, po = x.pointers(4)
+    array, (pq, pk, pv, po) = _places(
+        _bthd(w, "q", q, (B, H, Dk), dt) + _bthd(w, "k", k, (B, Hk, Dk), dt)
+        + _bthd(w, "v", v, (B, Hk, Dv), dt) + _bthd(w, "o", o, (B, H, Dv), dt), 4)
     _check(load_library().snn_leaky_attn_step(
         ctypes.byref(d), pq, pk, pv, _flat(w, "beta", beta, (H,), torch.float32),
         _flat(w, "state", state, (n, H, Dk, Dv), torch.float32),
@@ -657,13 +647,9 @@ def snn_block_norm_fwd(r, a, z, w_post, res_scale, w_pre, r_out, y, eps=1e-6, gr
     shape, res = r.shape, r.dtype
     io = a.dtype if a is not None else y.dtype if y is not None else res
     d = _norm_desc(w, *shape, group, io, res, gate, eps)
-    x = _Strided(w)
-    x.rows("r", r, shape, res)
-    x.rows("a", a, shape, io)
-    x.rows("z", z, shape, io)
-    x.rows("r_out", r_out, shape, res)
-    x.rows("y", y, shape, io)
-    pr, pa, pz, po, py = x.pointers(2)
+    array, (pr, pa, pz, po, py) = _places(
+        _rows(w, "r", r, shape, res) + _rows(w, "a", a, shape, io) + _rows(w, "z", z, shape, io)
+        + _rows(w, "r_out", r_out, shape, res) + _rows(w, "y", y, shape, io), 2)
     n = shape[1:]
     _check(load_library().snn_block_norm_fwd(
         ctypes.byref(d), pr, pa, pz, _flat(w, "w_post", w_post, n, torch.float32),
@@ -682,12 +668,11 @@ def snn_block_norm_bwd(r_out, a, z, w_post, res_scale, w_pre, grad_r_out, grad_y
     shape, res = of.shape, of.dtype
     io = a.dtype if a is not None else grad_y.dtype if grad_y is not None else res
     d = _norm_desc(w, *shape, group, io, res, gate, eps)
-    x = _Strided(w)
-    for name, t, dt in (("r_out", r_out, res), ("a", a, io), ("z", z, io),
-                        ("grad_r_out", grad_r_out, res), ("grad_y", grad_y, io),
-                        ("grad_r", grad_r, res), ("grad_a", grad_a, io), ("grad_z", grad_z, io)):
-        x.rows(name, t, shape, dt)
-    pr, pa, pz, gro, gy, gr, ga, gz = x.pointers(2)
+    array, (pr, pa, pz, gro, gy, gr, ga, gz) = _places(
+        _rows(w, "r_out", r_out, shape, res) + _rows(w, "a", a, shape, io)
+        + _rows(w, "z", z, shape, io) + _rows(w, "grad_r_out", grad_r_out, shape, res)
+        + _rows(w, "grad_y", grad_y, shape, io) + _rows(w, "grad_r", grad_r, shape, res)
+        + _rows(w, "grad_a", grad_a, shape, io) + _rows(w, "grad_z", grad_z, shape, io), 2)
     n = shape[1:]
     par = lambda name, t: _flat(w, name, t, n, torch.float32)
     _check(load_library().snn_block_norm_bwd(
