@@ -108,20 +108,21 @@ size_t segment_bytes(const snn_attn_desc* d, int nroles) {
   return round256((size_t)(d->B * d->H * nroles) * pl.nseg * tile(d->Dk) * tile(d->Dv) * sizeof(float));
 }
 
-// Map of a [B, T, heads, D] tensor read or written as boxes of 64 tokens x 64
-// elements of one head; tokens past T and elements past D read as zero and
-// are not written.
-bool make_map_bthd(CUtensorMap* map, const Tensor& x, const Args& g, int heads, int D, bool bf16) {
+// Map of a [B, T, heads, D] tensor read or written as boxes of 64 tokens x 128
+// bytes (64 16-bit elements, or 32 fp32 ones) of one head; tokens past T and
+// elements past D read as zero and are not written.
+bool make_map_bthd(CUtensorMap* map, const Tensor& x, const Args& g, int heads, int D,
+                   CUtensorMapDataType type) {
   auto fn = gemm::encode_fn();
   if (!fn) return false;
   const cuuint64_t dims[4] = {(cuuint64_t)D, (cuuint64_t)g.T, (cuuint64_t)heads, (cuuint64_t)g.B};
   // the stride of an extent of 1 is never stepped over: any valid value
-  auto bytes = [&](int64_t extent, int64_t stride) { return (cuuint64_t)(extent == 1 ? 16 : 2 * stride); };
+  const int size = type == CU_TENSOR_MAP_DATA_TYPE_FLOAT32 ? 4 : 2;
+  auto bytes = [&](int64_t extent, int64_t stride) { return (cuuint64_t)(extent == 1 ? 16 : size * stride); };
   const cuuint64_t strides[3] = {bytes(g.T, x.st), bytes(heads, x.sh), bytes(g.B, x.sb)};
-  const cuuint32_t box[4] = {64u, (cuuint32_t)kChunk, 1u, 1u};
+  const cuuint32_t box[4] = {128u / size, (cuuint32_t)kChunk, 1u, 1u};
   const cuuint32_t estr[4] = {1, 1, 1, 1};
-  return fn(map, bf16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 4, x.data,
-            dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
+  return fn(map, type, 4, x.data, dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
             CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
@@ -157,13 +158,16 @@ cudaError_t launch(const Args& g, const Plan& pl, float* seg_state, cudaStream_t
   p.nseg = pl.nseg;
   p.seg_tokens = pl.seg_tokens;
   p.seg_state = seg_state;
-  constexpr bool bf = std::is_same<T, __nv_bfloat16>::value;
+  constexpr CUtensorMapDataType kType = std::is_same<T, __nv_bfloat16>::value
+                                            ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16
+                                            : CU_TENSOR_MAP_DATA_TYPE_FLOAT16;
   for (int i = 0; i < g.nroles && g.T > 0; ++i) {
     const Role& r = g.role[i];
-    if (!make_map_bthd(&p.map[i].a, r.a, g, g.H / r.a.group, r.Da, bf) ||
-        !make_map_bthd(&p.map[i].b, r.b, g, g.H / r.b.group, r.Da, bf) ||
-        !make_map_bthd(&p.map[i].c, r.c, g, g.H / r.c.group, r.Dc, bf) ||
-        (!r.out_f32 && !make_map_bthd(&p.map[i].out, r.out, g, g.H / r.out.group, r.Dc, bf)))
+    if (!make_map_bthd(&p.map[i].a, r.a, g, g.H / r.a.group, r.Da, kType) ||
+        !make_map_bthd(&p.map[i].b, r.b, g, g.H / r.b.group, r.Da, kType) ||
+        !make_map_bthd(&p.map[i].c, r.c, g, g.H / r.c.group, r.Dc, kType) ||
+        !make_map_bthd(&p.map[i].out, r.out, g, g.H / r.out.group, r.Dc,
+                       r.out_f32 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT32 : kType))
       return cudaErrorInvalidValue;
   }
   const int da = tile(g.role[0].Da), dc = tile(g.role[0].Dc);

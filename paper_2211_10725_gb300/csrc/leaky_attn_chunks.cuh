@@ -649,9 +649,11 @@ __global__ void __launch_bounds__(Cfg<DA, DC>::kThreads, Cfg<DA, DC>::kBlocksPer
   unsigned char* sC = sB2 + C::kBStages * C::kABytes;
   unsigned char* sW = sC + C::kCBytes;                    // decayed values, high parts
   unsigned char* sL = C::kLowInA ? sA : sW + C::kCBytes;  // low parts
-  unsigned char* sE = sW + C::kCBytes + C::kLowBytes;     // the state's copy (64-wide heads)
-  unsigned char* sP = sE + C::kEBytes;                    // decayed scores, then the output
-  uint64_t* bar = reinterpret_cast<uint64_t*>(sP + C::kOutBytes);
+  unsigned char* sP = sW + C::kCBytes + C::kLowBytes;     // decayed scores, then the output
+  unsigned char* sE = sP + C::kOutBytes;                  // the state's copy (64-wide heads)
+  // an fp32 output is twice as long: it goes where the decayed values were
+  unsigned char* sO32 = sW;
+  uint64_t* bar = reinterpret_cast<uint64_t*>(sE + C::kEBytes);
   uint64_t *bar_a = bar, *bar_b = bar + 1, *bar_c = bar + 3, *bar_s = bar + 4, *bar_u = bar + 5,
            *bar_o = bar + 6, *bar_x = bar + 7, *bar_p = bar + 8;  // bar_b: one for each stage
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bar + 9);
@@ -834,6 +836,7 @@ __global__ void __launch_bounds__(Cfg<DA, DC>::kThreads, Cfg<DA, DC>::kBlocksPer
 
     // decayed values in two parts, while the scores are under way
     fail |= wait_all(bar_c, par);
+    if (out_f32 && it > 0) fail |= wait_all(bar_p, (it - 1) & 1);  // the last output has left sO32
     constexpr int kPieces = C::kCBytes / 16 / NT;
     uint4 low[kPieces];
 #pragma unroll
@@ -932,11 +935,11 @@ __global__ void __launch_bounds__(Cfg<DA, DC>::kThreads, Cfg<DA, DC>::kBlocksPer
       mma_commit(e, bar_u);
     }
 
-    {
-      fail |= wait_all(bar_o, par);
-      gemm::tc_fence_after();
-      if (tid == 96 && more && !(C::kLowInA && third)) load_c(it + 1);
-      __syncwarp();
+    fail |= wait_all(bar_o, par);
+    gemm::tc_fence_after();
+    if (tid == 96 && more && !(C::kLowInA && third)) load_c(it + 1);
+    __syncwarp();
+    auto output = [&](auto put) {  // put(16-lane half, its registers)
 #pragma unroll
       for (int rh = 0; rh < C::kRowHalves; ++rh) {
         float o[C::kToks / 2];
@@ -946,28 +949,23 @@ __global__ void __launch_bounds__(Cfg<DA, DC>::kThreads, Cfg<DA, DC>::kBlocksPer
           for (int i = 0; i < C::kToks / 2; ++i)
             if (tok + 8 * (i >> 2) + (i & 1) >= n) o[i] = 0.0f;
         }
-        if (out_f32) {
-          const int y = state.row + 16 * rh;
-          float* d = static_cast<float*>(r.out.data) + b * r.out.sb + h * r.out.sh + y;
-#pragma unroll
-          for (int i = 0; i < C::kToks / 2; ++i) {
-            const int t = t0 + tok + 8 * (i >> 2) + (i & 1), c = 8 * ((i >> 1) & 1);
-            if (t < T_all && y + c < Dc) d[t * r.out.st + c] = o[i];
-          }
-        } else {
-          // tokens as rows again: blocks (channels, +8) x (tokens 16j, 16j + 8)
-          const int x = (state.row - (lane >> 2)) + 16 * rh;  // the warp's first channel
-          unsigned char* tile = sP + (x >> 6) * kBoxBytes;
-#pragma unroll
-          for (int j = 0; j < C::kToks / 16; ++j) {
-            const int y = half * C::kToks + 16 * j + 8 * (lane >> 4) + (lane & 7);
-            const int piece = ((x & 63) >> 3) + ((lane >> 3) & 1);
-            stmatrix_t(tile + y * 128 + ((piece ^ (y & 7)) << 4),
-                       Elem<T>::from2(o[8 * j], o[8 * j + 1]), Elem<T>::from2(o[8 * j + 2], o[8 * j + 3]),
-                       Elem<T>::from2(o[8 * j + 4], o[8 * j + 5]), Elem<T>::from2(o[8 * j + 6], o[8 * j + 7]));
-          }
-        }
+        put(rh, o);
       }
+    };
+    if (!out_f32) {
+      output([&](int rh, const float (&o)[C::kToks / 2]) {
+        // tokens as rows again: blocks (channels, +8) x (tokens 16j, 16j + 8)
+        const int x = (state.row - (lane >> 2)) + 16 * rh;  // the warp's first channel
+        unsigned char* tile = sP + (x >> 6) * kBoxBytes;
+#pragma unroll
+        for (int j = 0; j < C::kToks / 16; ++j) {
+          const int y = half * C::kToks + 16 * j + 8 * (lane >> 4) + (lane & 7);
+          const int piece = ((x & 63) >> 3) + ((lane >> 3) & 1);
+          stmatrix_t(tile + y * 128 + ((piece ^ (y & 7)) << 4),
+                     Elem<T>::from2(o[8 * j], o[8 * j + 1]), Elem<T>::from2(o[8 * j + 2], o[8 * j + 3]),
+                     Elem<T>::from2(o[8 * j + 4], o[8 * j + 5]), Elem<T>::from2(o[8 * j + 6], o[8 * j + 7]));
+        }
+      });
     }
 
     fail |= wait_all(bar_u, u_phase);
@@ -985,6 +983,16 @@ __global__ void __launch_bounds__(Cfg<DA, DC>::kThreads, Cfg<DA, DC>::kBlocksPer
       u_phase ^= 1;
     }
     gemm::tc_fence_after();
+    if (out_f32) {
+      output([&](int rh, const float (&o)[C::kToks / 2]) {  // boxes of 32 channels (128 bytes) x 64 tokens
+#pragma unroll
+        for (int i = 0; i < C::kToks / 2; ++i) {
+          const int x = state.row + 16 * rh + 8 * ((i >> 1) & 1), y = tok + 8 * (i >> 2) + (i & 1);
+          *reinterpret_cast<float*>(sO32 + (x >> 5) * kBoxBytes + y * 128 + ((((x & 31) >> 2) ^ (y & 7)) << 4) +
+                                    (x & 3) * 4) = o[i];
+        }
+      });
+    }
     if (tid == 32 && more && (C::kLowInA || third)) load_a(it + 1);
     if (C::kBStages == 1 && tid == 64 && more) load_b(it + 1);
     if (tid == 96 && more && C::kLowInA && third) load_c(it + 1);
@@ -995,13 +1003,16 @@ __global__ void __launch_bounds__(Cfg<DA, DC>::kThreads, Cfg<DA, DC>::kBlocksPer
     gemm::tc_fence_before();
     if (__syncthreads_or(fail)) break;
     if (tid == kStorer) {
-      if (!out_f32) {
+      if (out_f32) {
+#pragma unroll 1
+        for (int x = 0; x < Dc; x += 32) tma_store_4d(&maps.out, sO32 + (x >> 5) * kBoxBytes, x, t0, ho, b);
+      } else {
 #pragma unroll
         for (int x = 0; x < DC / 64; ++x)
           tma_store_4d(&maps.out, sP + x * kBoxBytes, 64 * x, t0, ho, b);
-        gemm::bulk_commit();
-        bulk_wait_read_all();
       }
+      gemm::bulk_commit();
+      bulk_wait_read_all();
       mbar_arrive(bar_p);
     }
   }
