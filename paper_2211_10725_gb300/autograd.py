@@ -7,6 +7,9 @@ running in libsnn's kernels.
 (reduced to their layouts).  The Synaptic and recurrent neurons take alpha
 or v as a fourth tensor and return its gradient as well.  Only the spike
 output is differentiable; the membrane trace is not returned.
+
+``leaky_attention`` and ``block_norm`` wrap the two operators of a residual
+block of a sequence network in the same way.
 """
 from __future__ import annotations
 
@@ -52,3 +55,87 @@ def scan(I, beta, thr, w: W.ScanWorkload, third=None):
     if (w.T, w.B, w.N) != tuple(I.shape):
         raise ValueError("scan: I does not have the workload's [T, B, N] shape")
     return _ScanFunction.apply(I, beta, thr, third, w)
+
+
+class _AttentionFunction(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, q, k, v, beta, state, scale, seq_lens):
+        B, T, H, Dk = q.shape
+        Hk, Dv = k.shape[2], v.shape[-1]
+        o = torch.empty((B, T, H, Dv), dtype=q.dtype, device=q.device)
+        end = torch.empty((B, H, Dk, Dv), dtype=torch.float32, device=q.device)
+        ws = torch.zeros(snn.snn_leaky_attn_workspace_bytes(B, T, H, Hk, Dk, Dv),
+                         dtype=torch.uint8, device=q.device)
+        snn.snn_leaky_attn_fwd(q, k, v, beta, o, ws, scale=scale, seq_lens=seq_lens,
+                               state_in=state, state_out=end)
+        ctx.save_for_backward(q, k, v, beta, state, seq_lens)
+        ctx.scale = scale
+        return o, end
+
+    @staticmethod
+    def backward(ctx, grad_o, grad_end):
+        q, k, v, beta, state, seq_lens = ctx.saved_tensors
+        B, T, H, Dk = q.shape
+        Hk, Dv = k.shape[2], v.shape[-1]
+        gq, gk, gv = (torch.empty(x.shape, dtype=q.dtype, device=q.device) for x in (q, k, v))
+        gs = torch.empty((B, H, Dk, Dv), dtype=torch.float32, device=q.device) \
+            if state is not None and ctx.needs_input_grad[4] else None
+        ws = torch.zeros(snn.snn_leaky_attn_workspace_bytes(B, T, H, Hk, Dk, Dv, backward=True),
+                         dtype=torch.uint8, device=q.device)
+        grad_o = torch.zeros((B, T, H, Dv), dtype=q.dtype, device=q.device) if grad_o is None \
+            else grad_o.to(q.dtype).contiguous()
+        snn.snn_leaky_attn_bwd(q, k, v, beta, grad_o, gq, gk, gv, ws, scale=ctx.scale,
+                               seq_lens=seq_lens, state_in=state,
+                               grad_state_out=None if grad_end is None else grad_end.contiguous(),
+                               grad_state_in=gs)
+        return gq, gk, gv, None, gs, None, None
+
+
+def leaky_attention(q, k, v, beta, state=None, scale=1.0, seq_lens=None):
+    """(o, state after the last token) of leaky attention, S_t = beta_h S_{t-1}
+    + k_t v_t^T and o_t = scale S_t^T q_t: q [B, T, H, Dk], k [B, T, Hk, Dk], v
+    [B, T, Hk, Dv] (bf16 or fp16), state fp32 [B, H, Dk, Dv] or None.
+    Differentiable in q, k, v and state; beta (fp32 [H]) is a fixed schedule
+    over the heads."""
+    return _AttentionFunction.apply(q, k, v, beta, state, float(scale), seq_lens)
+
+
+class _BlockNormFunction(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, r, a, z, w_post, res_scale, w_pre, eps, group, gate):
+        shape = r.shape
+        flat = lambda t: None if t is None else t.reshape(-1, shape[-1])
+        r2, a2, z2 = flat(r), flat(a), flat(z)
+        r_out = torch.empty_like(r2)
+        y = torch.empty(r2.shape, dtype=a.dtype, device=a.device) if w_pre is not None else None
+        snn.snn_block_norm_fwd(r2, a2, z2, w_post, res_scale, w_pre, r_out, y, eps=eps, group=group,
+                               gate=gate)
+        ctx.save_for_backward(r_out, a2, z2, w_post, res_scale, w_pre)
+        ctx.opts, ctx.shape = dict(eps=eps, group=group, gate=gate), shape
+        return r_out.view(shape), None if y is None else y.view(shape)
+
+    @staticmethod
+    def backward(ctx, grad_r, grad_y):
+        r_out, a, z, w_post, res_scale, w_pre = ctx.saved_tensors
+        M, N = r_out.shape
+        flat = lambda t, like: None if t is None else t.to(like).reshape(M, N).contiguous()
+        grad_r, grad_y = flat(grad_r, r_out.dtype), flat(grad_y, a.dtype)
+        if grad_r is None and grad_y is None:
+            return (None,) * 9
+        like = lambda t: None if t is None else torch.empty(t.shape, dtype=t.dtype, device=t.device)
+        gr, ga, gz = like(r_out), like(a), like(z)
+        gp, gs = like(w_post), like(res_scale)
+        gw = like(w_pre)
+        ws = torch.empty(snn.snn_block_norm_workspace_bytes(M, N), dtype=torch.uint8, device=a.device)
+        snn.snn_block_norm_bwd(r_out, a, z, w_post, res_scale, w_pre, grad_r, grad_y, gr, ga, gz, gp,
+                               gs, gw, ws, **ctx.opts)
+        shaped = lambda t: None if t is None else t.view(ctx.shape)
+        return shaped(gr), shaped(ga), shaped(gz), gp, gs, gw, None, None, None
+
+
+def block_norm(r, a, z=None, w_post=None, res_scale=None, w_pre=None, eps=1e-6, group=0,
+               gate="none"):
+    """(r', y): r' = r + res_scale * norm(a) w_post * act(z) and y = norm(r')
+    w_pre (None without w_pre) over the last dimension, the norm of a per
+    `group` channels.  Differentiable in all the tensors."""
+    return _BlockNormFunction.apply(r, a, z, w_post, res_scale, w_pre, eps, group, gate)

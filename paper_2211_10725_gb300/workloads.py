@@ -279,3 +279,62 @@ def make_conv_inputs(w: ConvWorkload, seed: Optional[int] = None) -> dict:
     Wfc = (2.0 * torch.rand((w.n_classes, n_flat), generator=g, dtype=torch.float32) - 1.0) * bound
     labels = torch.randint(0, w.n_classes, (w.B,), generator=g, dtype=torch.int64).to(torch.int32)
     return {"X": X, "convs": convs, "Wfc": Wfc.to(torch.bfloat16), "labels": labels}
+
+
+# ---------------------------------------------------------------------------
+# Sequence network: leaky-attention blocks on spikes (784 inputs a step,
+# two blocks of width 256, four query heads on two shared key/value heads)
+# ---------------------------------------------------------------------------
+
+@dataclasses.dataclass(frozen=True)
+class AttnWorkload:
+    name: str = "asnn_784_256_h4_10_T100_B32"
+    T: int = 100
+    B: int = 32
+    n_in: int = 784
+    heads: int = 4
+    kv_heads: int = 2
+    head_dim: int = 64          # width = heads * head_dim
+    blocks: int = 2
+    n_classes: int = 10
+    rate_max: float = 0.3
+    beta: float = 0.9           # the neurons' decay
+    thr: float = 0.5
+    sg_param: float = 25.0      # fast-sigmoid slope
+    seed_index: int = 10
+
+    def scaled(self, **kw) -> "AttnWorkload":
+        return dataclasses.replace(self, **kw)
+
+    @property
+    def width(self) -> int:
+        return self.heads * self.head_dim
+
+    @property
+    def spikes(self) -> int:
+        """Neurons of a block whose spikes are queries, keys and values."""
+        return (self.heads + 2 * self.kv_heads) * self.head_dim
+
+
+ASNN = AttnWorkload()
+
+
+def make_attn_inputs(w: AttnWorkload, seed: Optional[int] = None) -> dict:
+    """Bernoulli input spikes as for the dense network; He-uniform bf16
+    weights without bias: input [width, n_in], per block [spikes + width,
+    width] (queries, keys, values, gate), readout [n_classes, width]; uniform
+    labels."""
+    seed = SEED_BASE + w.seed_index if seed is None else seed
+    g = _gen(seed)
+    rate = w.rate_max * torch.rand((w.B, w.n_in), generator=g, dtype=torch.float32)
+    u = torch.rand((w.T, w.B, w.n_in), generator=g, dtype=torch.float32)
+    X = (u < rate.unsqueeze(0)).to(torch.bfloat16)
+
+    def he(n_out, k_in):
+        r = 2.0 * torch.rand((n_out, k_in), generator=g, dtype=torch.float32) - 1.0
+        return (r * (6.0 / k_in) ** 0.5).to(torch.bfloat16)
+    weights = [he(w.width, w.n_in)]
+    weights += [he(w.spikes + w.width, w.width) for _ in range(w.blocks)]
+    weights.append(he(w.n_classes, w.width))
+    labels = torch.randint(0, w.n_classes, (w.B,), generator=g, dtype=torch.int64).to(torch.int32)
+    return {"X": X, "W": weights, "labels": labels}
