@@ -8,14 +8,17 @@
 //   grad_r = d;  grad_z = d s n act'(z)
 //   grad_a = rstd_a (m - h mean_group(m h)),  h = a rstd_a,  m = d s act(z) w_post
 //   grad_w_post = s G,  grad_s = w_post G  with  G = sum d act(z) h;  grad_w_pre = sum grad_y e
-// Every tensor is read and written once: the bound is HBM.  A row stays in
-// the registers of one warp (short rows) or one block, eight channels to a
-// thread; blocks stay on the GPU and take rows in turn, with the next row's
-// loads in flight while the sums of the present one meet.  The parameters'
-// gradients gather in the registers (long rows: in shared memory) of the
-// thread that owns the channels over all the rows of its block, so the sums
-// over rows need one [blocks, 2, N] array of partials and a second kernel
-// that adds them in block order (no atomics: the same bits on every call).
+// Every tensor is read and written once: the bound is HBM.  One warp (short
+// rows) or one block takes a row, eight channels to a thread; blocks stay on the
+// GPU and take rows in turn, with the next row or two on their way to shared
+// memory (16-byte asynchronous copies) while the present one is worked on.  Rows of
+// whole 16-byte vectors are copied and read by the thread that owns the
+// channels; rows of any other length or stride are copied as the aligned
+// vectors that cover them and read element by element.  The parameters' gradients gather in the registers (long
+// rows: in shared memory) of the thread that owns the channels over all the
+// rows of its block, so the sums over rows need one [blocks, 2, N] array of
+// partials and a second kernel that adds them in block order (no atomics: the
+// same bits on every call).
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 #include <cuda_runtime.h>
@@ -34,6 +37,7 @@ namespace norm {
 constexpr int64_t kMaxN = 8192;
 constexpr int kSms = 152;
 constexpr int E = 8;  // channels of a thread
+constexpr int kBwdThreads = 512;  // of the backward's blocks on an SM
 
 struct Rows {
   void* data;
@@ -47,6 +51,7 @@ struct Args {
   Rows r, a, z, ro, y;        // forward
   Rows gro, gy, gr, ga, gz;   // backward (reads ro, a, z)
   const float *w_post, *scale, *w_pre;
+  int stages;                 // rows a team has in shared memory at once, 1 to 3
   float* part;                // [blocks][2][N]
 };
 
@@ -54,6 +59,85 @@ __device__ __forceinline__ float sigmoidf_(float z) { return __fdividef(1.0f, 1.
 
 // Eight floats as one 32-byte access (p 32-byte aligned): two 16-byte ones
 // would each touch half of every 32-byte sector.
+__device__ __forceinline__ void store32(float* p, const float v[8]) {
+  asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(p), "f"(v[0]),
+               "f"(v[1]), "f"(v[2]), "f"(v[3]), "f"(v[4]), "f"(v[5]), "f"(v[6]), "f"(v[7])
+               : "memory");
+}
+
+// 16 bytes from global to shared memory, both aligned.
+__device__ __forceinline__ void copy16(unsigned char* dst, const unsigned char* src) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(smem_u32(dst)), "l"(src) : "memory");
+}
+// (by the whole warp at once: its copies are counted together)
+__device__ __forceinline__ void copies_commit() {
+  __syncwarp();
+  asm volatile("cp.async.commit_group;" ::: "memory");
+}
+__device__ __forceinline__ void copies_wait(int left) {  // all groups of this thread but the newest
+  if (left == 0) asm volatile("cp.async.wait_group 0;" ::: "memory");
+  else if (left == 1) asm volatile("cp.async.wait_group 1;" ::: "memory");
+  else asm volatile("cp.async.wait_group 2;" ::: "memory");
+}
+
+// Bytes a row of a tensor takes in shared memory (16 more for a row that does
+// not start on a 16-byte boundary).
+__host__ __device__ constexpr int slot_bytes(int N, int size) { return (N * size + 15) / 16 * 16 + 16; }
+
+// One tensor's row in shared memory; a thread's share is eight consecutive
+// channels (VEC), else every TPR-th.
+template <typename T, bool VEC, int TPR>
+struct Slot {
+  unsigned char* smem;
+
+  __device__ __forceinline__ static const unsigned char* row_of(const Rows& m, int64_t row) {
+    return reinterpret_cast<const unsigned char*>(static_cast<const T*>(m.data) + row * m.ld);
+  }
+  __device__ __forceinline__ void fetch(const Rows& m, int64_t row, int64_t M, int N, int t) const {
+    const unsigned char* src = row_of(m, row);
+    if constexpr (VEC) {
+      if (t * E >= N) return;
+#pragma unroll
+      for (int i = 0; i < E * (int)sizeof(T) / 16; ++i) {
+        const int o = t * E * (int)sizeof(T) + 16 * i;
+        copy16(smem + o, src + o);
+      }
+    } else {
+      const int skew = (int)(reinterpret_cast<uintptr_t>(src) & 15u), end = skew + N * (int)sizeof(T);
+      // whole vectors as far as the matrix goes: past the row's end lies the next row
+      const int64_t rest = skew + ((M - 1 - row) * m.ld + N) * (int64_t)sizeof(T);
+#pragma unroll
+      for (int k = 0; k <= E * (int)sizeof(T) / 16; ++k) {
+        const int o = 16 * (k * TPR + t);
+        if (o + 16 <= rest && o < end) {
+          copy16(smem + o, src - skew + o);
+        } else if (o < end) {  // the matrix's last elements
+          for (int i = o; i < end; i += (int)sizeof(T))
+            if (i >= skew) *reinterpret_cast<T*>(smem + i) = *reinterpret_cast<const T*>(src - skew + i);
+        }
+      }
+    }
+  }
+  // in 32 bits, zero past N
+  __device__ __forceinline__ void get(const Rows& m, int64_t row, int N, int t, float v[E]) const {
+    if constexpr (VEC) {
+      if (t * E < N) {
+        Elem<T>::load8(reinterpret_cast<const T*>(smem) + t * E, v);
+      } else {
+#pragma unroll
+        for (int e = 0; e < E; ++e) v[e] = 0.0f;
+      }
+    } else {
+      const int skew = (int)(reinterpret_cast<uintptr_t>(row_of(m, row)) & 15u);
+      const T* x = reinterpret_cast<const T*>(smem + skew);
+#pragma unroll
+      for (int e = 0; e < E; ++e) v[e] = e * TPR + t < N ? (float)x[e * TPR + t] : 0.0f;
+    }
+  }
+};
+
+// A thread's eight consecutive channels of a row, as they lie in memory, in
+// registers.
 __device__ __forceinline__ void load32(const float* p, uint4 w[2]) {
   asm volatile("ld.global.v8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
                : "=r"(w[0].x), "=r"(w[0].y), "=r"(w[0].z), "=r"(w[0].w), "=r"(w[1].x), "=r"(w[1].y),
@@ -61,47 +145,21 @@ __device__ __forceinline__ void load32(const float* p, uint4 w[2]) {
                : "l"(p)
                : "memory");
 }
-__device__ __forceinline__ void store32(float* p, const float v[8]) {
-  asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(p), "f"(v[0]),
-               "f"(v[1]), "f"(v[2]), "f"(v[3]), "f"(v[4]), "f"(v[5]), "f"(v[6]), "f"(v[7])
-               : "memory");
-}
-
-// A thread's share of a row as it lies in memory: eight consecutive channels
-// (VEC), else every TPR-th.
-template <typename T, bool VEC, int TPR>
-struct Share {
-  static constexpr int kWords = E * sizeof(T) / 16;
-  uint4 w[VEC ? kWords : 1];
-  T x[VEC ? 1 : E];
-
-  __device__ __forceinline__ void load(const Rows& m, int64_t row, int N, int t) {
-    const T* p = static_cast<const T*>(m.data) + row * m.ld;
-    if constexpr (VEC) {
-      if (t * E < N) {
-        if constexpr (sizeof(T) == 4) load32(reinterpret_cast<const float*>(p + t * E), w);
-        else
-#pragma unroll
-        for (int i = 0; i < kWords; ++i) w[i] = reinterpret_cast<const uint4*>(p + t * E)[i];
-      }
-    } else {
-#pragma unroll
-      for (int e = 0; e < E; ++e)
-        if (e * TPR + t < N) x[e] = p[e * TPR + t];
-    }
+template <typename T>
+struct Held {
+  uint4 w[E * sizeof(T) / 16];
+  __device__ __forceinline__ void fetch(const Rows& m, int64_t row, int N, int t) {
+    const T* p = static_cast<const T*>(m.data) + row * m.ld + t * E;
+    if (t * E >= N) return;
+    if constexpr (sizeof(T) == 4) load32(p, w);
+    else w[0] = *reinterpret_cast<const uint4*>(p);
   }
-  // in 32 bits, zero past N
   __device__ __forceinline__ void get(int N, int t, float v[E]) const {
-    if constexpr (VEC) {
-      if (t * E < N) {
-        Elem<T>::load8(reinterpret_cast<const T*>(w), v);
-      } else {
-#pragma unroll
-        for (int e = 0; e < E; ++e) v[e] = 0.0f;
-      }
+    if (t * E < N) {
+      Elem<T>::load8(reinterpret_cast<const T*>(w), v);
     } else {
 #pragma unroll
-      for (int e = 0; e < E; ++e) v[e] = e * TPR + t < N ? (float)x[e] : 0.0f;
+      for (int e = 0; e < E; ++e) v[e] = 0.0f;
     }
   }
 };
@@ -159,8 +217,9 @@ struct RowSum {
 #pragma unroll
       for (int k = 0; k < K; ++k) {
         float a = 0.0f;
+        if constexpr (W == 2) a = s[k][0] + s[k][1];
 #pragma unroll
-        for (int w = 0; w < W; w += 4) {
+        for (int w = 0; w + 4 <= W; w += 4) {
           const float4 x = *reinterpret_cast<const float4*>(&s[k][w]);
           a += (x.x + x.y) + (x.z + x.w);
         }
@@ -178,17 +237,33 @@ __device__ __forceinline__ float group_sum(float v, int lanes) {
 
 template <int TPR>
 constexpr int kBlockThreads = TPR == 32 ? 256 : TPR;  // short rows: eight warps, a row each
+template <int TPR>
+constexpr int kTeams = kBlockThreads<TPR> / TPR;
 
-// Registers: two blocks of 512 threads (or as many smaller ones) on an SM,
-// one of 1024.
+// Before a team reads what its other threads copied.
+template <int TPR>
+__device__ __forceinline__ void team_sync() {
+  if constexpr (TPR == 32) __syncwarp();
+  else __syncthreads();
+}
+
+// Shared memory of a stage: the rows a team reads.
+__host__ __device__ constexpr int fwd_stage(int N, int t_size, int r_size) {
+  return slot_bytes(N, r_size) + 2 * slot_bytes(N, t_size);
+}
+__host__ __device__ constexpr int bwd_stage(int N, int t_size, int r_size) {
+  return 2 * slot_bytes(N, r_size) + 3 * slot_bytes(N, t_size);
+}
+
+extern __shared__ __align__(16) unsigned char norm_smem[];
+
 template <typename T, typename R, bool VEC, int TPR>
 __global__ void __launch_bounds__(kBlockThreads<TPR>, 1024 / kBlockThreads<TPR>) norm_fwd(const Args g) {
   __shared__ __align__(16) float scratch[2][3][32];
   grid_dep_wait();
-  constexpr int kTeams = kBlockThreads<TPR> / TPR;
-  const int t = threadIdx.x % TPR, N = g.N;
-  const int64_t step = (int64_t)gridDim.x * kTeams;
-  int64_t row = (int64_t)blockIdx.x * kTeams + threadIdx.x / TPR;
+  const int t = threadIdx.x % TPR, team = threadIdx.x / TPR, N = g.N;
+  const int64_t step = (int64_t)gridDim.x * kTeams<TPR>;
+  int64_t row = (int64_t)blockIdx.x * kTeams<TPR> + team;
   const bool whole = g.group == N, block = g.a.data != nullptr, gated = g.z.data != nullptr;
   const float inv_n = 1.0f / (float)N, inv_g = 1.0f / (float)g.group;
   RowSum<TPR> row_sum{scratch};
@@ -201,75 +276,93 @@ __global__ void __launch_bounds__(kBlockThreads<TPR>, 1024 / kBlockThreads<TPR>)
 #pragma unroll
     for (int e = 0; e < E; ++e) w_post[e] *= sc[e];
   }
-  Share<R, VEC, TPR> r;
-  Share<T, VEC, TPR> a, z;
-  auto fetch = [&](int64_t i) {
-    r.load(g.r, i, N, t);
-    if (block) a.load(g.a, i, N, t);
-    if (gated) z.load(g.z, i, N, t);
+  const int stage = fwd_stage(N, sizeof(T), sizeof(R));
+  unsigned char* const base = norm_smem + team * g.stages * stage;
+  auto r_slot = [&](int k) { return Slot<R, VEC, TPR>{base + k * stage}; };
+  auto a_slot = [&](int k) { return Slot<T, VEC, TPR>{base + k * stage + slot_bytes(N, sizeof(R))}; };
+  auto z_slot = [&](int k) {
+    return Slot<T, VEC, TPR>{base + k * stage + slot_bytes(N, sizeof(R)) + slot_bytes(N, sizeof(T))};
   };
-  if (row < g.M) fetch(row);
-  for (; row < g.M; row += step) {
-    float x[E], u[E], sg[E];
-    r.get(N, t, x);
-    if (block) a.get(N, t, u);
-    if (gated) z.get(N, t, sg);
-    if (row + step < g.M) fetch(row + step);
+  auto fetch = [&](int64_t i, int k) {
+    if (i < g.M) {
+      r_slot(k).fetch(g.r, i, g.M, N, t);
+      if (block) a_slot(k).fetch(g.a, i, g.M, N, t);
+      if (gated) z_slot(k).fetch(g.z, i, g.M, N, t);
+    }
+    copies_commit();
+  };
+  const int ahead = g.stages - 1;  // at least one
+  for (int i = 0; i < ahead; ++i) fetch(row + i * step, i);
+  for (int k = 0, next = ahead; row < g.M; row += step) {
+    fetch(row + ahead * step, next);  // that stage was read before the last row's sums
+    copies_wait(ahead);
+    if (!VEC) team_sync<TPR>();
+    float x[E], u[E];
+    r_slot(k).get(g.r, row, N, t, x);
     if (block) {
+      a_slot(k).get(g.a, row, N, t, u);
       float ss[1] = {0.0f};
 #pragma unroll
       for (int e = 0; e < E; ++e) ss[0] = fmaf(u[e], u[e], ss[0]);
       if (whole) row_sum(ss);
       else ss[0] = group_sum(ss[0], g.group >> 3);
       const float rstd = rsqrtf(fmaf(ss[0], whole ? inv_n : inv_g, g.eps));
+      float z[E];
+      if (gated) z_slot(k).get(g.z, row, N, t, z);
 #pragma unroll
       for (int e = 0; e < E; ++e) {
         u[e] = u[e] * rstd * w_post[e];
         if (gated) {
-          const float s = sigmoidf_(sg[e]);
-          u[e] *= g.gate == SNN_GATE_SILU ? sg[e] * s : s;
+          const float s = sigmoidf_(z[e]);
+          u[e] *= g.gate == SNN_GATE_SILU ? z[e] * s : s;
         }
         x[e] += u[e];
       }
       store_row<R, VEC, TPR>(g.ro, row, N, t, x);
     }
-    if (g.y.data) {
-      float ss[1] = {0.0f};
+    float ss[1] = {0.0f};
 #pragma unroll
-      for (int e = 0; e < E; ++e) ss[0] = fmaf(x[e], x[e], ss[0]);
-      row_sum(ss);
+    for (int e = 0; e < E; ++e) ss[0] = fmaf(x[e], x[e], ss[0]);
+    row_sum(ss);  // also where there is no y: it is what frees the stage
+    if (TPR == 32) team_sync<TPR>();
+    if (g.y.data) {
       const float rstd = rsqrtf(fmaf(ss[0], inv_n, g.eps));
 #pragma unroll
       for (int e = 0; e < E; ++e) x[e] = x[e] * rstd * w_pre[e];
       store_row<T, VEC, TPR>(g.y, row, N, t, x);
     }
+    k = k + 1 == g.stages ? 0 : k + 1;
+    next = next + 1 == g.stages ? 0 : next + 1;
   }
+  copies_wait(0);
 }
 
-// Two vectors of a thread's channels that live as long as its block: in
-// registers, or (long rows, whose threads have none to spare) in shared
-// memory, [4][E / 4][threads] float4 with the pair at FIRST.
-template <bool SMEM, int THREADS, int FIRST>
-struct Kept {
+// Two vectors of a thread's channels: parameters, or sums over rows.  In
+// registers; for long rows, whose threads have none to spare, the sums lie in
+// shared memory ([2][E / 4][threads] float4) and the parameters are read again.
+template <bool SMEM>
+struct Sums {
   float v[SMEM ? 1 : 2][E];
-  __device__ __forceinline__ float4& at(int k, int i) {
-    extern __shared__ float4 kept_smem[];
-    return kept_smem[((FIRST + k) * (E / 4) + i) * THREADS + threadIdx.x];
-  }
-  __device__ __forceinline__ void set(int k, const float (&a)[E]) {
-    if constexpr (SMEM) {
+  float4* at;
+  int threads;
+  __device__ __forceinline__ float4& word(int k, int i) { return at[(k * (E / 4) + i) * threads + threadIdx.x]; }
+  __device__ __forceinline__ void clear() {
 #pragma unroll
-      for (int i = 0; i < E / 4; ++i) at(k, i) = make_float4(a[4 * i], a[4 * i + 1], a[4 * i + 2], a[4 * i + 3]);
-    } else {
+    for (int k = 0; k < 2; ++k) {
+      if constexpr (SMEM) {
 #pragma unroll
-      for (int e = 0; e < E; ++e) v[k][e] = a[e];
+        for (int i = 0; i < E / 4; ++i) word(k, i) = make_float4(0.f, 0.f, 0.f, 0.f);
+      } else {
+#pragma unroll
+        for (int e = 0; e < E; ++e) v[k][e] = 0.0f;
+      }
     }
   }
   __device__ __forceinline__ void get(int k, float (&a)[E]) {
     if constexpr (SMEM) {
 #pragma unroll
       for (int i = 0; i < E / 4; ++i) {
-        const float4 s = at(k, i);
+        const float4 s = word(k, i);
         a[4 * i] = s.x;
         a[4 * i + 1] = s.y;
         a[4 * i + 2] = s.z;
@@ -281,79 +374,110 @@ struct Kept {
     }
   }
   __device__ __forceinline__ void add(int k, const float (&a)[E], const float (&b)[E]) {  // += a b
-    float s[E];
-    get(k, s);
+    if constexpr (SMEM) {
 #pragma unroll
-    for (int e = 0; e < E; ++e) s[e] = fmaf(a[e], b[e], s[e]);
-    set(k, s);
+      for (int i = 0; i < E / 4; ++i) {
+        float4 s = word(k, i);
+        s.x = fmaf(a[4 * i], b[4 * i], s.x);
+        s.y = fmaf(a[4 * i + 1], b[4 * i + 1], s.y);
+        s.z = fmaf(a[4 * i + 2], b[4 * i + 2], s.z);
+        s.w = fmaf(a[4 * i + 3], b[4 * i + 3], s.w);
+        word(k, i) = s;
+      }
+    } else {
+#pragma unroll
+      for (int e = 0; e < E; ++e) v[k][e] = fmaf(a[e], b[e], v[k][e]);
+    }
   }
 };
 
 template <typename T, typename R, bool VEC, int TPR>
-__global__ void __launch_bounds__(kBlockThreads<TPR>, TPR == 1024 ? 1 : 512 / kBlockThreads<TPR>)
+__global__ void __launch_bounds__(kBlockThreads<TPR>, TPR == 1024 ? 1 : kBwdThreads / kBlockThreads<TPR>)
     norm_bwd(const Args g) {
   __shared__ __align__(16) float scratch[2][3][32];
   grid_dep_wait();
-  constexpr int kTeams = kBlockThreads<TPR> / TPR;
+  // Five tensors' next row in registers rather than in shared memory, where the
+  // threads have them: whole vectors of rows up to 4096 channels (8192 rows of
+  // 4096, 16-bit on a 32-bit stream: 129 us, 151 through shared memory).
+  constexpr bool kLong = TPR == 1024, kHeld = VEC && !kLong;
   const int t = threadIdx.x % TPR, team = threadIdx.x / TPR, N = g.N;
-  const int64_t step = (int64_t)gridDim.x * kTeams;
-  int64_t row = (int64_t)blockIdx.x * kTeams + team;
+  const int64_t step = (int64_t)gridDim.x * kTeams<TPR>;
+  int64_t row = (int64_t)blockIdx.x * kTeams<TPR> + team;
   const bool whole = g.group == N, block = g.a.data != nullptr, gated = g.z.data != nullptr;
   const bool pre = g.gy.data != nullptr, through = g.gro.data != nullptr;
   const float inv_n = 1.0f / (float)N, inv_g = 1.0f / (float)g.group;
   RowSum<TPR> row_sum{scratch};
-  // 0: of d act(z) h, 1: of grad_y y';  0: w_pre, 1: s w_post
-  Kept<TPR == 1024, TPR, 0> sums;
-  Kept<TPR == 1024, TPR, 2> params;
-  {
-    float w[E], sc[E];
-    load_param<VEC, TPR>(g.w_pre, N, t, w);
-    params.set(0, w);
-    load_param<VEC, TPR>(g.w_post, N, t, w);
+  const int stage = bwd_stage(N, sizeof(T), sizeof(R));
+  unsigned char* const base = norm_smem + team * g.stages * stage;
+  const int r_bytes = slot_bytes(N, sizeof(R)), t_bytes = slot_bytes(N, sizeof(T));
+  auto ro_slot = [&](int k) { return Slot<R, VEC, TPR>{base + k * stage}; };
+  auto gro_slot = [&](int k) { return Slot<R, VEC, TPR>{base + k * stage + r_bytes}; };
+  auto t_slot = [&](int k, int i) { return Slot<T, VEC, TPR>{base + k * stage + 2 * r_bytes + i * t_bytes}; };
+  auto fetch = [&](int64_t i, int k) {
+    if (i < g.M) {
+      if (pre) ro_slot(k).fetch(g.ro, i, g.M, N, t);
+      if (pre) t_slot(k, 0).fetch(g.gy, i, g.M, N, t);
+      if (through) gro_slot(k).fetch(g.gro, i, g.M, N, t);
+      if (block) t_slot(k, 1).fetch(g.a, i, g.M, N, t);
+      if (gated) t_slot(k, 2).fetch(g.z, i, g.M, N, t);
+    }
+    copies_commit();
+  };
+  const int ahead = g.stages - 1;
+  Held<R> held_ro, held_gro;
+  Held<T> held_gy, held_a, held_z;
+  auto hold = [&](int64_t i) {
+    if (i >= g.M) return;
+    if (pre) held_ro.fetch(g.ro, i, N, t);
+    if (pre) held_gy.fetch(g.gy, i, N, t);
+    if (through) held_gro.fetch(g.gro, i, N, t);
+    if (block) held_a.fetch(g.a, i, N, t);
+    if (gated) held_z.fetch(g.z, i, N, t);
+  };
+  if constexpr (kHeld) {
+    hold(row);
+  } else {
+    for (int i = 0; i < (ahead ? ahead : 1); ++i) fetch(row + i * step, i);
+  }
+  Sums<kLong> sums;  // 0: of d act(z) h, 1: of grad_y y'
+  sums.at = reinterpret_cast<float4*>(norm_smem + g.stages * stage);
+  sums.threads = TPR;
+  sums.clear();
+  float w_pre[E], c[E];  // c: the factors s w_post of a channel as one
+  auto params = [&]() {
+    float sc[E];
+    load_param<VEC, TPR>(g.w_pre, N, t, w_pre);
+    load_param<VEC, TPR>(g.w_post, N, t, c);
     load_param<VEC, TPR>(g.scale, N, t, sc);
 #pragma unroll
-    for (int e = 0; e < E; ++e) {
-      w[e] *= sc[e];
-      sc[e] = 0.0f;
-    }
-    params.set(1, w);
-    sums.set(0, sc);
-    sums.set(1, sc);
-  }
-  Share<R, VEC, TPR> ro, gro;
-  Share<T, VEC, TPR> gy, a, z;
-  auto fetch = [&](int64_t i) {
-    if (pre) ro.load(g.ro, i, N, t);
-    if (pre) gy.load(g.gy, i, N, t);
-    if (through) gro.load(g.gro, i, N, t);
-    if (block) a.load(g.a, i, N, t);
-    if (gated) z.load(g.z, i, N, t);
+    for (int e = 0; e < E; ++e) c[e] *= sc[e];
   };
-  // long rows have not the registers to hold a row ahead
-  constexpr bool kAhead = TPR < 1024;
-  if (kAhead && row < g.M) fetch(row);
-  for (; row < g.M; row += step) {
-    if (!kAhead) fetch(row);
-    float d[E], x[E], gw[E], h[E], zz[E];
-    if (pre) ro.get(N, t, x);
-    if (pre) gy.get(N, t, gw);
-    if (block) a.get(N, t, h);
-    if (gated) z.get(N, t, zz);
-    if (through) {
-      gro.get(N, t, d);
+  if (!kLong) params();
+  for (int k = 0, next = ahead; row < g.M; row += step) {
+    float d[E], x[E], gw[E], h[E], z_held[kHeld ? E : 1];
+    float* const z = kHeld ? z_held : gw;  // read late into grad_y's place, or held
+    if constexpr (kHeld) {
+      if (pre) held_ro.get(N, t, x);
+      if (pre) held_gy.get(N, t, gw);
+      if (through) held_gro.get(N, t, d);
+      if (block) held_a.get(N, t, h);
+      if (gated) held_z.get(N, t, z);
+      hold(row + step);
     } else {
-#pragma unroll
-      for (int e = 0; e < E; ++e) d[e] = 0.0f;
+      if (ahead) fetch(row + ahead * step, next);  // that stage was read before the last row's sums
+      copies_wait(ahead);
+      if (!VEC) team_sync<TPR>();
+      if (pre) ro_slot(k).get(g.ro, row, N, t, x);
+      if (pre) t_slot(k, 0).get(g.gy, row, N, t, gw);
+      if (block) t_slot(k, 1).get(g.a, row, N, t, h);
     }
-    if (kAhead && row + step < g.M) fetch(row + step);
+    if (kLong) load_param<VEC, TPR>(g.w_pre, N, t, w_pre);
     float ss[3] = {0.0f, 0.0f, 0.0f};  // of r'^2, grad_y w_pre r', a^2
-    float w[E];
-    params.get(0, w);
     if (pre) {
 #pragma unroll
       for (int e = 0; e < E; ++e) {
         ss[0] = fmaf(x[e], x[e], ss[0]);
-        ss[1] = fmaf(gw[e] * w[e], x[e], ss[1]);
+        ss[1] = fmaf(gw[e] * w_pre[e], x[e], ss[1]);
       }
     }
     if (block) {
@@ -363,6 +487,12 @@ __global__ void __launch_bounds__(kBlockThreads<TPR>, TPR == 1024 ? 1 : 512 / kB
     float in_group = 0.0f;
     if (block && !whole) in_group = group_sum(ss[2], g.group >> 3);
     row_sum(ss);
+    if (!through) {
+#pragma unroll
+      for (int e = 0; e < E; ++e) d[e] = 0.0f;
+    } else if (!kHeld) {
+      gro_slot(k).get(g.gro, row, N, t, d);
+    }
     if (pre) {
       const float rstd = rsqrtf(fmaf(ss[0], inv_n, g.eps));
       const float mean = ss[1] * rstd * inv_n;  // mean of (grad_y w_pre) y'
@@ -370,55 +500,66 @@ __global__ void __launch_bounds__(kBlockThreads<TPR>, TPR == 1024 ? 1 : 512 / kB
       for (int e = 0; e < E; ++e) x[e] *= rstd;  // y'
       sums.add(1, gw, x);
 #pragma unroll
-      for (int e = 0; e < E; ++e) d[e] = fmaf(rstd, fmaf(-x[e], mean, gw[e] * w[e]), d[e]);
+      for (int e = 0; e < E; ++e) d[e] = fmaf(rstd, fmaf(-x[e], mean, gw[e] * w_pre[e]), d[e]);
     }
     if (g.gr.data) store_row<R, VEC, TPR>(g.gr, row, N, t, d);
-    if (!block) continue;
-    const float rstd_a = rsqrtf(whole ? fmaf(ss[2], inv_n, g.eps) : fmaf(in_group, inv_g, g.eps));
     float q[1] = {0.0f};
-    params.get(1, w);
+    const float rstd_a = rsqrtf(whole ? fmaf(ss[2], inv_n, g.eps) : fmaf(in_group, inv_g, g.eps));
+    if (block) {
+      if (kLong) params();
+      if (!kHeld && gated) t_slot(k, 2).get(g.z, row, N, t, z);
 #pragma unroll
-    for (int e = 0; e < E; ++e) {
-      h[e] *= rstd_a;
-      x[e] = d[e];
-      d[e] *= w[e];
-      if (gated) {
-        const float s = sigmoidf_(zz[e]);
-        const float act = g.gate == SNN_GATE_SILU ? zz[e] * s : s;
-        const float slope = g.gate == SNN_GATE_SILU ? s * fmaf(zz[e], 1.0f - s, 1.0f) : s * (1.0f - s);
-        zz[e] = d[e] * h[e] * slope;  // grad_z
-        x[e] *= act;
-        d[e] *= act;                  // m
+      for (int e = 0; e < E; ++e) {
+        h[e] *= rstd_a;
+        x[e] = d[e];
+        d[e] *= c[e];
+        if (gated) {
+          const float s = sigmoidf_(z[e]);
+          const float act = g.gate == SNN_GATE_SILU ? z[e] * s : s;
+          const float slope = g.gate == SNN_GATE_SILU ? s * fmaf(z[e], 1.0f - s, 1.0f) : s * (1.0f - s);
+          z[e] = d[e] * h[e] * slope;  // grad_z
+          x[e] *= act;
+          d[e] *= act;                  // m
+        }
+        q[0] = fmaf(d[e], h[e], q[0]);
       }
-      q[0] = fmaf(d[e], h[e], q[0]);
+      sums.add(0, x, h);
+      if (g.gz.data) store_row<T, VEC, TPR>(g.gz, row, N, t, z);
     }
-    sums.add(0, x, h);
-    if (g.gz.data) store_row<T, VEC, TPR>(g.gz, row, N, t, zz);
-    if (!g.ga.data) continue;
+    // the row is read (VEC: by the threads that copied it): its stage is free
     if (whole) row_sum(q);
-    else q[0] = group_sum(q[0], g.group >> 3);
-    const float mean = q[0] * (whole ? inv_n : inv_g);
+    else if (block) q[0] = group_sum(q[0], g.group >> 3);
+    if (!VEC && (!whole || TPR == 32)) team_sync<TPR>();
+    if (!kHeld && !ahead) fetch(row + step, 0);
+    if (g.ga.data) {
+      const float mean = q[0] * (whole ? inv_n : inv_g);
 #pragma unroll
-    for (int e = 0; e < E; ++e) d[e] = rstd_a * fmaf(-h[e], mean, d[e]);
-    store_row<T, VEC, TPR>(g.ga, row, N, t, d);
+      for (int e = 0; e < E; ++e) d[e] = rstd_a * fmaf(-h[e], mean, d[e]);
+      store_row<T, VEC, TPR>(g.ga, row, N, t, d);
+    }
+    k = k + 1 == g.stages ? 0 : k + 1;
+    next = next + 1 == g.stages ? 0 : next + 1;
   }
+  copies_wait(0);
   if (!g.part) return;
   float* p = g.part + (int64_t)blockIdx.x * 2 * N;
-  if constexpr (kTeams > 1) {  // the block's teams, in order
-    __shared__ float all[kTeams][2][TPR * E];
+  if constexpr (kTeams<TPR> > 1) {  // the block's teams, in order
+    constexpr int kWidth = TPR * E;
+    float* all = reinterpret_cast<float*>(norm_smem);  // [teams][2][kWidth], over the rows
+    __syncthreads();
 #pragma unroll
     for (int k = 0; k < 2; ++k) {
       float v[E];
       sums.get(k, v);
 #pragma unroll
-      for (int e = 0; e < E; ++e) all[team][k][VEC ? t * E + e : e * TPR + t] = v[e];
+      for (int e = 0; e < E; ++e) all[(team * 2 + k) * kWidth + (VEC ? t * E + e : e * TPR + t)] = v[e];
     }
     __syncthreads();
     for (int i = threadIdx.x; i < 2 * N; i += kBlockThreads<TPR>) {
-      const int k = i / N, at = i - k * N;
-      float v = all[0][k][at];
+      const int k = i / N, at = k * kWidth + i - k * N;
+      float v = all[at];
 #pragma unroll
-      for (int j = 1; j < kTeams; ++j) v += all[j][k][at];
+      for (int j = 1; j < kTeams<TPR>; ++j) v += all[j * 2 * kWidth + at];
       p[i] = v;
     }
   } else {
@@ -470,7 +611,7 @@ int64_t least(int64_t a, int64_t b) { return a < b ? a : b; }
 
 // Threads of a row, eight channels each.
 int row_threads(int64_t N) {
-  return N <= 256 ? 32 : N <= 1024 ? 128 : N <= 2048 ? 256 : N <= 4096 ? 512 : 1024;
+  return N <= 256 ? 32 : N <= 512 ? 64 : N <= 1024 ? 128 : N <= 2048 ? 256 : N <= 4096 ? 512 : 1024;
 }
 
 // Blocks for M rows with `threads` of them on an SM; from the shape alone, so
@@ -480,7 +621,7 @@ int64_t blocks_for(int64_t M, int64_t N, int threads) {
   const int64_t resident = (int64_t)kSms * (threads > block ? threads / block : 1);
   return least(resident, tpr == 32 ? (M + 7) / 8 : M);
 }
-int64_t bwd_blocks(int64_t M, int64_t N) { return blocks_for(M, N, 512); }
+int64_t bwd_blocks(int64_t M, int64_t N) { return blocks_for(M, N, kBwdThreads); }
 
 snn_status_t check_desc(const snn_norm_desc* d) {
   if (!d || d->reserved[0] || d->reserved[1]) return SNN_ERR_INVALID_ARG;
@@ -520,20 +661,43 @@ struct Launch {
   cudaStream_t st;
 };
 
+// Rows in shared memory: up to three, as many as fit beside the other blocks
+// of an SM (and the sums of long rows).
+template <typename K>
+cudaError_t launch_staged(K* kernel, const Launch& l, int threads, int teams, int stage, size_t fixed,
+                          int resident, int least_stages) {
+  constexpr size_t kPerSm = 224 * 1024;
+  Args g = l.g;
+  g.stages = 3;
+  while (g.stages > least_stages && g.stages * (size_t)teams * stage + fixed + 1024 > kPerSm / resident) --g.stages;
+  size_t smem = g.stages * (size_t)teams * stage + fixed;
+  // the teams' sums of short rows
+  const size_t all = teams > 1 ? (size_t)teams * 2 * 32 * E * sizeof(float) : 0;
+  if (smem < all) smem = all;
+  // with the kernel's static shared memory, past the limit that needs no asking
+  const size_t ask = smem + 1024 > 48 * 1024 && smem <= 48 * 1024 ? 48 * 1024 + 16 : smem;
+  const cudaError_t e = ensure_smem((const void*)kernel, ask);
+  if (e != cudaSuccess) return e;
+  return launch_pdl(kernel, dim3((unsigned)l.blocks), dim3(threads), smem, l.st, g);
+}
+
 template <typename T, typename R, bool VEC, int TPR>
 cudaError_t launch_tpr(const Launch& l) {
-  const dim3 grid((unsigned)l.blocks), block(kBlockThreads<TPR>);
-  if (!l.bwd) return launch_pdl(norm_fwd<T, R, VEC, TPR>, grid, block, 0, l.st, l.g);
-  const size_t smem = TPR == 1024 ? 4 * E * sizeof(float) * TPR : 0;
-  const cudaError_t e = ensure_smem((const void*)norm_bwd<T, R, VEC, TPR>, smem);
-  if (e != cudaSuccess) return e;
-  return launch_pdl(norm_bwd<T, R, VEC, TPR>, grid, block, smem, l.st, l.g);
+  constexpr int kThreads = kBlockThreads<TPR>;
+  if (!l.bwd)
+    return launch_staged(norm_fwd<T, R, VEC, TPR>, l, kThreads, kTeams<TPR>,
+                         fwd_stage(l.g.N, sizeof(T), sizeof(R)), 0, 1024 / kThreads, 2);
+  return launch_staged(norm_bwd<T, R, VEC, TPR>, l, kThreads, kTeams<TPR>,
+                       VEC && TPR < 1024 ? 0 : bwd_stage(l.g.N, sizeof(T), sizeof(R)),
+                       TPR == 1024 ? 2 * E * sizeof(float) * TPR : 0,
+                       TPR == 1024 ? 1 : kBwdThreads / kThreads, 1);
 }
 
 template <typename T, typename R, bool VEC>
 cudaError_t launch_vec(const Launch& l) {
   switch (row_threads(l.g.N)) {
     case 32: return launch_tpr<T, R, VEC, 32>(l);
+    case 64: return launch_tpr<T, R, VEC, 64>(l);
     case 128: return launch_tpr<T, R, VEC, 128>(l);
     case 256: return launch_tpr<T, R, VEC, 256>(l);
     case 512: return launch_tpr<T, R, VEC, 512>(l);
