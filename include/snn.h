@@ -562,10 +562,11 @@ size_t snn_leaky_attn_workspace_bytes(const snn_attn_desc* desc, int backward);
  *              must differ where state_out is given.
  *   ws         snn_leaky_attn_workspace_bytes(desc, 0) bytes, 16-byte aligned
  *              (its first 256 bytes are the status word of snn_workspace_status)
- * Products run on the tensor cores with fp32 accumulation; the state is kept
- * in fp32 between chunks.  Valid tokens must be finite: an infinity or NaN
- * there reaches every token of its sequence and head, earlier ones of its
- * chunk included.
+ * o must not overlap q, k or v.  Products run on the tensor cores with fp32
+ * accumulation; the state is kept in fp32 between chunks.  Valid tokens must
+ * be finite: an infinity or NaN there reaches every token of its sequence and
+ * head, earlier ones of its chunk included; in fp16 a decayed score scale *
+ * beta^(i-j) q_i.k_j past 65504 is infinite.
  */
 snn_status_t snn_leaky_attn_fwd(const snn_attn_desc* desc, const snn_bthd* q, const snn_bthd* k,
                                 const snn_bthd* v, const float* beta, const int32_t* seq_lens,
@@ -580,7 +581,8 @@ snn_status_t snn_leaky_attn_fwd(const snn_attn_desc* desc, const snn_bthd* q, co
  *   grad_state_out   fp32 [B, H, Dk, Dv] or NULL (zeros)
  *   grad_q [B, T, H, Dk], grad_k [B, T, Hk, Dk], grad_v [B, T, Hk, Dv] (out);
  *              zero in places at and past seq_lens[b]
- *   grad_state_in    fp32 [B, H, Dk, Dv] (out) or NULL.  Must not be grad_state_out.
+ *   grad_state_in    fp32 [B, H, Dk, Dv] (out) or NULL; neither grad_state_out nor
+ *              state_in
  *   state_in   fp32 [B, H, Dk, Dv] or NULL, as in the forward (place b for sequence b)
  *   ws         snn_leaky_attn_workspace_bytes(desc, 1) bytes
  * The three gradients are the forward's recurrence with the tensors' roles
@@ -654,9 +656,10 @@ size_t snn_block_norm_workspace_bytes(int64_t M, int64_t N);
  * Forward.  w_post, res_scale (NULL: ones) and w_pre are fp32 [N].
  *   r_out  (out) r'; NULL when a is NULL.  May be r itself.
  *   y      (out); NULL when w_pre is NULL
- * z is given exactly when gate is not SNN_GATE_NONE.  Rows whose N and ld are
- * whole 16-byte vectors move in vectors; others element by element, where a
- * group must be the whole row (SNN_ERR_UNSUPPORTED otherwise).
+ * z is given exactly when gate is not SNN_GATE_NONE.  Where N and every ld are
+ * multiples of 8 a thread moves whole vectors; any other rows are staged as
+ * the aligned vectors that cover them, and there a group must be the whole row
+ * (SNN_ERR_UNSUPPORTED otherwise).
  */
 snn_status_t snn_block_norm_fwd(const snn_norm_desc* desc, const snn_rows* r, const snn_rows* a,
                                 const snn_rows* z, const float* w_post, const float* res_scale,

@@ -57,8 +57,10 @@ struct Args {
 
 __device__ __forceinline__ float sigmoidf_(float z) { return __fdividef(1.0f, 1.0f + __expf(-z)); }
 
-// Eight floats as one 32-byte access (p 32-byte aligned): two 16-byte ones
-// would each touch half of every 32-byte sector.
+// Eight floats as one 32-byte access: two 16-byte ones would each touch half of
+// every 32-byte sector (norms of 16384x4096 on a 32-bit stream: 168 us, 210 with
+// halves).  A matrix that starts between 32-byte boundaries takes the halves.
+__device__ __forceinline__ bool wide(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 31u) == 0; }
 __device__ __forceinline__ void store32(float* p, const float v[8]) {
   asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(p), "f"(v[0]),
                "f"(v[1]), "f"(v[2]), "f"(v[3]), "f"(v[4]), "f"(v[5]), "f"(v[6]), "f"(v[7])
@@ -151,8 +153,12 @@ struct Held {
   __device__ __forceinline__ void fetch(const Rows& m, int64_t row, int N, int t) {
     const T* p = static_cast<const T*>(m.data) + row * m.ld + t * E;
     if (t * E >= N) return;
-    if constexpr (sizeof(T) == 4) load32(p, w);
-    else w[0] = *reinterpret_cast<const uint4*>(p);
+    if (sizeof(T) == 4 && wide(p)) {
+      load32(reinterpret_cast<const float*>(p), w);
+    } else {
+#pragma unroll
+      for (int i = 0; i < (int)(E * sizeof(T) / 16); ++i) w[i] = reinterpret_cast<const uint4*>(p)[i];
+    }
   }
   __device__ __forceinline__ void get(int N, int t, float v[E]) const {
     if (t * E < N) {
@@ -169,8 +175,12 @@ __device__ __forceinline__ void store_row(const Rows& m, int64_t row, int N, int
   T* p = static_cast<T*>(m.data) + row * m.ld;
   if constexpr (VEC) {
     if (t * E < N) {
-      if constexpr (sizeof(T) == 4) store32(p + t * E, v);
-      else Elem<T>::store8(p + t * E, v);
+      if constexpr (sizeof(T) == 4) {
+        if (wide(p)) store32(p + t * E, v);
+        else Elem<T>::store8(p + t * E, v);
+      } else {
+        Elem<T>::store8(p + t * E, v);
+      }
     }
   } else {
 #pragma unroll
@@ -649,7 +659,6 @@ snn_status_t take(const snn_norm_desc* d, const snn_rows* x, int dtype, Rows* ou
   if (!aligned16(x->data)) return SNN_ERR_ALIGNMENT;
   if (d->M > 1 && (x->ld < d->N || x->ld > (int64_t(1) << 40))) return SNN_ERR_INVALID_ARG;
   if (d->M > 1 && x->ld % 8) *vec = false;
-  if (dtype == SNN_F32 && (reinterpret_cast<uintptr_t>(x->data) & 31u)) *vec = false;
   *out = Rows{x->data, x->ld};
   return SNN_OK;
 }

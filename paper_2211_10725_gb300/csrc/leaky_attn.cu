@@ -272,7 +272,10 @@ snn_status_t snn_leaky_attn_bwd(const snn_attn_desc* desc, const snn_bthd* q, co
   const int64_t heads[7] = {desc->H, desc->Hk, desc->Hk, desc->H, desc->H, desc->Hk, desc->Hk};
   for (int i = 0; i < 7; ++i)
     if ((s = check_tensor(desc, x[i], heads[i])) != SNN_OK) return s;
-  if (!beta || (grad_state_in && grad_state_in == grad_state_out)) return SNN_ERR_INVALID_ARG;
+  if (!beta) return SNN_ERR_INVALID_ARG;
+  // one role writes the one while the others read the other two
+  if (grad_state_in && (grad_state_in == grad_state_out || grad_state_in == state_in))
+    return SNN_ERR_INVALID_ARG;
   const void* ptrs[6] = {beta, seq_lens, state_in, grad_state_out, grad_state_in, ws};
   for (const void* p : ptrs)
     if (!aligned16(p)) return SNN_ERR_ALIGNMENT;

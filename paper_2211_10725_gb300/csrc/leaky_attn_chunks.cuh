@@ -483,7 +483,7 @@ __global__ void __launch_bounds__(Cfg<DA, DC>::kThreads, Cfg<DA, DC>::kBlocksPer
   const bool rev = r.rev != 0;
   const int hb = at.h / r.b.group, hc = at.h / r.c.group;
 
-  if (tid == 32) {
+  if (tid == 32 && g.T > 0) {
     prefetch_map(&maps.b);
     prefetch_map(&maps.c);
   }
@@ -672,7 +672,7 @@ __global__ void __launch_bounds__(Cfg<DA, DC>::kThreads, Cfg<DA, DC>::kBlocksPer
   const int Dc = r.Dc, T_all = g.T;
   const float scale = g.scale;
 
-  if (tid == 32) {
+  if (tid == 32 && g.T > 0) {
     prefetch_map(&maps.a);
     prefetch_map(&maps.b);
     prefetch_map(&maps.c);

@@ -255,3 +255,12 @@ def test_norm_backward_refusals(lib):
     assert bwd(d, nws=64) == WORKSPACE
     assert bwd(_norm(res_dtype=2)) == UNSUPPORTED
     assert lib.snn_block_norm_workspace_bytes(4, 8200) == 0
+
+
+def test_attention_backward_refuses_a_state_written_while_it_is_read(lib):
+    d = _attn()
+    call = lambda s_in, gs_out, gs_in: lib.snn_leaky_attn_bwd(
+        ctypes.byref(d), _t(), _t(), _t(), 16, None, s_in, _t(), gs_out, _t(), _t(), _t(), gs_in, 256,
+        BIG, None)
+    assert call(64, None, 64) == INVALID
+    assert call(None, 64, 64) == INVALID
