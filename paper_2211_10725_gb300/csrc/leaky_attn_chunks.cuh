@@ -30,7 +30,8 @@
 //
 // Few heads and many tokens: the tokens are cut into segments, a first kernel
 // (attn_segments: update products only) finds each segment's own contribution
-// to the state, a second (attn_segment_scan) the state each one starts from.
+// to the state; a second (attn_segment_scan), where there are more than a few,
+// the state each one starts from.
 #pragma once
 
 #include <cuda.h>
@@ -60,6 +61,7 @@ struct ChunkArgs {
   RoleMaps map[kMaxRoles];
   int nseg;             // segments of a sequence
   int seg_tokens;       // tokens of a segment, a multiple of kChunk
+  int scanned;          // attn_segment_scan has run
   float* seg_state;     // [role][B*H][nseg] states in fragment order
 };
 
@@ -392,17 +394,17 @@ struct State {
         reinterpret_cast<float4*>(at)[(rh * (C::kCols / 8) + i / 4) * C::kThreads + tid] =
             make_float4(e[rh][i], e[rh][i + 1], e[rh][i + 2], e[rh][i + 3]);
   }
-  __device__ __forceinline__ void get_segment(const float* at, int tid) {
+  __device__ __forceinline__ void add_segment(const float* at, int tid, float decay) {  // e = decay e + it
 #pragma unroll
     for (int rh = 0; rh < C::kRowHalves; ++rh)
 #pragma unroll
       for (int i = 0; i < C::kCols / 2; i += 4) {
         const float4 v =
             reinterpret_cast<const float4*>(at)[(rh * (C::kCols / 8) + i / 4) * C::kThreads + tid];
-        e[rh][i] = v.x;
-        e[rh][i + 1] = v.y;
-        e[rh][i + 2] = v.z;
-        e[rh][i + 3] = v.w;
+        e[rh][i] = fmaf(e[rh][i], decay, v.x);
+        e[rh][i + 1] = fmaf(e[rh][i + 1], decay, v.y);
+        e[rh][i + 2] = fmaf(e[rh][i + 2], decay, v.z);
+        e[rh][i + 3] = fmaf(e[rh][i + 3], decay, v.w);
       }
   }
   // e = decay e + the update product in tensor memory
@@ -740,7 +742,11 @@ __global__ void __launch_bounds__(Cfg<DA, DC>::kThreads, Cfg<DA, DC>::kBlocksPer
   if (p.nseg == 1) {
     state.load(g, r, b, h, rev ? 1.0f / scale : (at.len > 0 ? beta : 1.0f));
   } else if (at.seg <= at.last_seg) {
-    state.get_segment(seg0 + (size_t)at.order * (DA * DC), tid);
+    // scanned: the state itself; else what the segments before this one left
+    // (1 holds 0's start), the last one first decayed
+    const float decay = power(beta, p.seg_tokens);
+    for (int m = p.scanned || at.order == 0 ? at.order : 1; m <= at.order; ++m)
+      state.add_segment(seg0 + (size_t)m * (DA * DC), tid, decay);
   }
 
   const uint32_t t_quad = (uint32_t)(quad * 32) << 16;
