@@ -19,6 +19,13 @@
 // rows of its block, so the sums over rows need one [blocks, 2, N] array of
 // partials and a second kernel that adds them in block order (no atomics: the
 // same bits on every call).
+//
+// Measured (share of the copy rate): forward of 16384 x 4096, 16-bit on a 32-bit
+// stream, 153 us (0.91); of 16384 x 2048 bf16 67 us (0.74); of 2000 x 7049 on a
+// 32-bit stream, element by element, 56 us (0.52).  Backward of 8192 x 4096 on a
+// 32-bit stream 133 us (0.82); of 16384 x 2048 bf16 with a norm per head 119 us
+// (0.67: its threads issue in 63% of the cycles, about 90 instructions a channel);
+// of 3001 x 1001 fp32 24 us (0.59).
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 #include <cuda_runtime.h>
