@@ -48,7 +48,8 @@ def test_parameters_share_one_buffer_each():
     w, net = _net()
     assert len(net.weights.parts) == w.blocks + 2 and len(net.norms.parts) == 3 * w.blocks + 1
     for f in (net.weights, net.norms):
-        assert all(p.data_ptr() % 128 == 0 for p in f.grads)
+        # 64-element boundaries of the buffer (whose own address is the allocator's)
+        assert all((p.data_ptr() - f.grad.data_ptr()) % 256 == 0 for p in f.grads)
     assert torch.equal(net.weights.parts[0], W.make_attn_inputs(w)["W"][0])
     assert net.weights.parts[-1].shape == (16, w.width)
     assert torch.count_nonzero(net.weights.parts[-1][w.n_classes:]) == 0
