@@ -62,7 +62,10 @@ __global__ void __launch_bounds__(256) sum_group(const SumArgs g) {
 // alone on its SM and in one of a full SM, and of a block's start:
 //   128-wide heads, two blocks on an SM: attn_chunks 2.35 alone, 3.0 beside
 //   another (16384 tokens of 16 heads, 1 to 19 segments: 602 to 88);
-//   attn_segments 1.05 and 1.8.
+//   attn_segments 1.05 and 1.8;
+//   64-wide heads, four blocks on an SM: attn_chunks 2.2 and 3.55 (64 chunks in
+//   one, two, three and four blocks on every SM: 155, 177, 204 and 233),
+//   attn_segments 0.65 and 1.6.
 // Two segments of 777 tokens in 36 heads' three roles take 44 where one takes
 // 35; four of 1024 tokens in 32 heads take 26 where one takes 42.
 // A function of the shapes alone, so that a shape always sums in the same
@@ -86,15 +89,18 @@ double wave_time(int64_t blocks, int64_t per, int per_sm, double alone, double f
 
 Plan plan(const snn_attn_desc* d, int nroles) {
   const int64_t chunks = ceil_div(d->T, kChunk), heads = d->B * d->H * nroles;
-  const int per_sm = tile(d->Dk) + tile(d->Dv) == 128 ? 4 : 2;
+  const bool narrow = tile(d->Dk) + tile(d->Dv) == 128;
+  const int per_sm = narrow ? 4 : 2;
+  const double alone = narrow ? 2.2 : 2.35, full = narrow ? 3.55 : 3.0;
+  const double seg_alone = narrow ? 0.65 : 1.05, seg_full = narrow ? 1.6 : 1.8;
   constexpr double kLaunch = 3.0, kScan = 2.0;
   Plan best;
   if (chunks == 0) return best;
   double best_time = 0.0;
   for (int64_t s = 1; s <= kMaxSeg && s <= chunks; ++s) {
     const int64_t per = ceil_div(chunks, s), n = ceil_div(chunks, per);
-    double t = wave_time(heads * n, per, per_sm, 2.35, 3.0);
-    if (n > 1) t += kLaunch + wave_time(heads * (n - 1), per, per_sm, 1.05, 1.8);
+    double t = wave_time(heads * n, per, per_sm, alone, full);
+    if (n > 1) t += kLaunch + wave_time(heads * (n - 1), per, per_sm, seg_alone, seg_full);
     if (n > 1) t += n > kSummed ? kScan + 0.1 * n : 0.8 * n;
     if (s == 1 || t < best_time) {
       best_time = t;

@@ -25,8 +25,9 @@
 // The decayed values are two 16-bit parts each (v w = hi + lo with products
 // and residuals exact in packed 16-bit arithmetic), multiplied in turn, so a
 // state keeps 16 bits or more of each term; where a bf16 state is an output, a
-// third part makes them 24.  fp16 has not the range of a sum of products: its
-// state copy is scaled by a power of two.
+// third part makes them 24 (fp16: two make 22, and parts below 6e-8 vanish).
+// fp16 has not the range of a sum of products: its state copy is scaled by a
+// power of two.
 //
 // Few heads and many tokens: the tokens are cut into segments, a first kernel
 // (attn_segments: update products only) finds each segment's own contribution
@@ -651,7 +652,6 @@ template <typename T, int DA, int DC>
 __global__ void __launch_bounds__(Cfg<DA, DC>::kThreads, Cfg<DA, DC>::kBlocksPerSm)
     attn_chunks(const __grid_constant__ ChunkArgs p) {
   using C = Cfg<DA, DC>;
-  using T2 = typename Pair<T>::type;
   constexpr int NT = C::kThreads;
   constexpr int kStorer = NT - 32;  // thread that issues and awaits the output's copies
   constexpr bool kHalf = std::is_same<T, __half>::value;
