@@ -57,21 +57,28 @@ __global__ void __launch_bounds__(256) sum_group(const SumArgs g) {
 // Host side
 // ---------------------------------------------------------------------------
 
-// How a run of `nroles` roles over B*H heads cuts T tokens into segments: the
-// count that should end soonest, from the times (us) of a chunk in a block
+// How a run over `heads` heads (of all its roles) cuts T tokens into segments:
+// the count that should end soonest, from the times (us) of a chunk in a block
 // alone on its SM and in one of a full SM, and of a block's start:
-//   128-wide heads, two blocks on an SM: attn_chunks 2.35 alone, 3.0 beside
+//   128 x 128 tiles, two blocks on an SM: attn_chunks 2.35 alone, 3.0 beside
 //   another (16384 tokens of 16 heads, 1 to 19 segments: 602 to 88);
 //   attn_segments 1.05 and 1.8;
-//   64-wide heads, four blocks on an SM: attn_chunks 2.2 and 3.55 (64 chunks in
+//   64 x 64 tiles, four blocks on an SM: attn_chunks 2.2 and 3.55 (64 chunks in
 //   one, two, three and four blocks on every SM: 155, 177, 204 and 233),
-//   attn_segments 0.65 and 1.6.
+//   attn_segments 0.65 and 1.6;
+//   tiles of both widths, two blocks on an SM: between these.
 // Two segments of 777 tokens in 36 heads' three roles take 44 where one takes
 // 35; four of 1024 tokens in 32 heads take 26 where one takes 42.
 // A function of the shapes alone, so that a shape always sums in the same
 // order.
 struct Plan {
+  int da = 64, dc = 64;  // the tile: widths of a/b and of c/out, 64 or 128
   int nseg = 1, seg_tokens = kChunk;
+  int64_t heads = 0;
+  double time = 0.0;
+  size_t bytes() const {  // of the segments' states
+    return nseg == 1 ? 0 : (size_t)heads * nseg * da * dc * sizeof(float);
+  }
 };
 constexpr int kMaxSeg = 64;
 constexpr int kSummed = 4;  // segments whose states the blocks sum themselves
@@ -87,23 +94,24 @@ double wave_time(int64_t blocks, int64_t per, int per_sm, double alone, double f
   return (double)(blocks / slots) * (kStart + full * per) + (rest ? kStart + chunk * per : 0.0);
 }
 
-Plan plan(const snn_attn_desc* d, int nroles) {
-  const int64_t chunks = ceil_div(d->T, kChunk), heads = d->B * d->H * nroles;
-  const bool narrow = tile(d->Dk) + tile(d->Dv) == 128;
-  const int per_sm = narrow ? 4 : 2;
-  const double alone = narrow ? 2.2 : 2.35, full = narrow ? 3.55 : 3.0;
-  const double seg_alone = narrow ? 0.65 : 1.05, seg_full = narrow ? 1.6 : 1.8;
-  constexpr double kLaunch = 3.0, kScan = 2.0;
+Plan plan(int64_t T, int64_t heads, int da, int dc) {
   Plan best;
-  if (chunks == 0) return best;
-  double best_time = 0.0;
+  best.da = da;
+  best.dc = dc;
+  best.heads = heads;
+  const int64_t chunks = ceil_div(T, kChunk);
+  const int kind = (da + dc) / 64 - 2;  // 0: 64 x 64, 1: both, 2: 128 x 128
+  const int per_sm = kind == 0 ? 4 : 2;
+  constexpr double kAlone[3] = {2.2, 2.2, 2.35}, kFull[3] = {3.55, 2.7, 3.0};
+  constexpr double kSegAlone[3] = {0.65, 0.85, 1.05}, kSegFull[3] = {1.6, 1.6, 1.8};
+  constexpr double kLaunch = 3.0, kScan = 2.0;
   for (int64_t s = 1; s <= kMaxSeg && s <= chunks; ++s) {
     const int64_t per = ceil_div(chunks, s), n = ceil_div(chunks, per);
-    double t = wave_time(heads * n, per, per_sm, alone, full);
-    if (n > 1) t += kLaunch + wave_time(heads * (n - 1), per, per_sm, seg_alone, seg_full);
+    double t = wave_time(heads * n, per, per_sm, kAlone[kind], kFull[kind]);
+    if (n > 1) t += kLaunch + wave_time(heads * (n - 1), per, per_sm, kSegAlone[kind], kSegFull[kind]);
     if (n > 1) t += n > kSummed ? kScan + 0.1 * n : 0.8 * n;
-    if (s == 1 || t < best_time) {
-      best_time = t;
+    if (s == 1 || t < best.time) {
+      best.time = t;
       best.nseg = (int)n;
       best.seg_tokens = (int)(per * kChunk);
     }
@@ -111,10 +119,33 @@ Plan plan(const snn_attn_desc* d, int nroles) {
   return best;
 }
 
-size_t segment_bytes(const snn_attn_desc* d, int nroles) {
-  const Plan pl = plan(d, nroles);
-  if (pl.nseg == 1) return 0;
-  return round256((size_t)(d->B * d->H * nroles) * pl.nseg * tile(d->Dk) * tile(d->Dv) * sizeof(float));
+Plan plan_fwd(const snn_attn_desc* d) { return plan(d->T, d->B * d->H, tile(d->Dk), tile(d->Dv)); }
+
+// The backward's three roles: in one launch where their tiles are the same.
+// Where Dk and Dv differ in tile, grad_q and grad_k have the widths the other way
+// round from grad_v: in two launches, or, where that ends sooner, in one with
+// 128 x 128 tiles, whose blocks are longer but fill the SMs at once. 64 x 128,
+// one launch against two: 78 us and 110 (6 x 1500 tokens, 16 heads), 16 and 25
+// (300 tokens, 8 heads); 290 and 240 (8 x 2048, 32 heads), 274 and 238
+// (32 x 512, 32 heads).
+struct BwdPlan {
+  bool one = true;
+  Plan first, last;  // first: all three, or grad_q and grad_k; last: grad_v
+  size_t bytes() const { return first.bytes() + (one ? 0 : last.bytes()); }
+};
+BwdPlan plan_bwd(const snn_attn_desc* d) {
+  const int64_t heads = d->B * d->H;
+  const int tk = tile(d->Dk), tv = tile(d->Dv);
+  BwdPlan p;
+  p.first = plan(d->T, 3 * heads, tk > tv ? tk : tv, tk > tv ? tk : tv);
+  if (tk == tv) return p;
+  const Plan two = plan(d->T, 2 * heads, tv, tk);
+  p.last = plan(d->T, heads, tk, tv);
+  if (two.time + p.last.time < p.first.time) {
+    p.one = false;
+    p.first = two;
+  }
+  return p;
 }
 
 // Map of a [B, T, heads, D] tensor read or written as boxes of 64 tokens x 128
@@ -182,9 +213,8 @@ cudaError_t launch(const Args& g, const Plan& pl, float* seg_state, cudaStream_t
                        r.out_f32 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT32 : kType))
       return cudaErrorInvalidValue;
   }
-  const int da = tile(g.role[0].Da), dc = tile(g.role[0].Dc);
-  if (da == 64) return dc == 64 ? launch_tile<T, 64, 64>(p, st) : launch_tile<T, 64, 128>(p, st);
-  return dc == 64 ? launch_tile<T, 128, 64>(p, st) : launch_tile<T, 128, 128>(p, st);
+  if (pl.da == 64) return pl.dc == 64 ? launch_tile<T, 64, 64>(p, st) : launch_tile<T, 64, 128>(p, st);
+  return pl.dc == 64 ? launch_tile<T, 128, 64>(p, st) : launch_tile<T, 128, 128>(p, st);
 }
 
 cudaError_t launch(const snn_attn_desc* d, const Args& g, const Plan& pl, float* seg_state, cudaStream_t st) {
@@ -227,10 +257,10 @@ size_t snn_attn_desc_size(void) { return sizeof(snn_attn_desc); }
 
 size_t snn_leaky_attn_workspace_bytes(const snn_attn_desc* desc, int backward) {
   if (check_desc(desc) != SNN_OK) return 0;
-  const size_t fwd = segment_bytes(desc, 1);
+  const size_t fwd = plan_fwd(desc).bytes();
   if (!backward) return 256 + fwd;
   const size_t bwd =
-      segment_bytes(desc, 3) + share_bytes(desc, desc->Dk) + share_bytes(desc, desc->Dv);
+      plan_bwd(desc).bytes() + share_bytes(desc, desc->Dk) + share_bytes(desc, desc->Dv);
   return 256 + (fwd > bwd ? fwd : bwd);
 }
 
@@ -266,7 +296,8 @@ snn_status_t snn_leaky_attn_fwd(const snn_attn_desc* desc, const snn_bthd* q, co
   r.s_in = state_in;
   r.s_out = state_out;
   cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
-  const cudaError_t e = launch(desc, g, plan(desc, 1), reinterpret_cast<float*>(static_cast<unsigned char*>(ws) + 256), st);
+  float* seg_state = reinterpret_cast<float*>(static_cast<unsigned char*>(ws) + 256);
+  const cudaError_t e = launch(desc, g, plan_fwd(desc), seg_state, st);
   return e == cudaSuccess ? SNN_OK : SNN_ERR_CUDA;
 }
 
@@ -299,7 +330,8 @@ snn_status_t snn_leaky_attn_bwd(const snn_attn_desc* desc, const snn_bthd* q, co
   g.nroles = 3;
   unsigned char* at = static_cast<unsigned char*>(ws) + 256;
   float* seg_state = reinterpret_cast<float*>(at);
-  at += segment_bytes(desc, 3);
+  const BwdPlan pl = plan_bwd(desc);
+  at += pl.bytes();
   float* share_k = reinterpret_cast<float*>(at);
   float* share_v = reinterpret_cast<float*>(at + share_bytes(desc, desc->Dk));
   auto share = [&](float* p, int64_t D) {
@@ -341,18 +373,17 @@ snn_status_t snn_leaky_attn_bwd(const snn_attn_desc* desc, const snn_bthd* q, co
   rv.s_out = grad_state_in;
   rv.out_f32 = rk.out_f32 = G > 1;
   cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
-  const Plan pl = plan(desc, 3);
   cudaError_t e;
-  if (tile(desc->Dk) == tile(desc->Dv)) {
-    e = launch(desc, g, pl, seg_state, st);
-  } else {  // the first two roles have the widths the other way round
+  if (pl.one) {
+    e = launch(desc, g, pl.first, seg_state, st);
+  } else {
     Args gv = g;
     gv.role[0] = rv;
     gv.nroles = 1;
     g.nroles = 2;
-    e = launch(desc, g, pl, seg_state, st);
+    e = launch(desc, g, pl.first, seg_state, st);
     if (e == cudaSuccess)
-      e = launch(desc, gv, pl, seg_state + (size_t)(desc->B * desc->H * 2) * pl.nseg * 64 * 128, st);
+      e = launch(desc, gv, pl.last, seg_state + pl.first.bytes() / sizeof(float), st);
   }
   if (e == cudaSuccess && G > 1 && desc->T > 0) {
     const SumArgs sum{{share_k, share_v},  {tensor(grad_k, 1), tensor(grad_v, 1)}, {g.Dk, g.Dv},

@@ -1025,7 +1025,7 @@ __global__ void __launch_bounds__(Cfg<DA, DC>::kThreads, Cfg<DA, DC>::kBlocksPer
       } else {
 #pragma unroll
         for (int x = 0; x < DC / 64; ++x)
-          tma_store_4d(&maps.out, sP + x * kBoxBytes, 64 * x, t0, ho, b);
+          if (64 * x < Dc) tma_store_4d(&maps.out, sP + x * kBoxBytes, 64 * x, t0, ho, b);
       }
       gemm::bulk_commit();
       bulk_wait_read_all();

@@ -147,6 +147,17 @@ def test_widths(Dk, Dv, dtype, cuda_device):
     check_backward(c)
 
 
+# one width up to 64, the other above, and heads enough that the backward takes two launches; in the
+# longer case the second launch cuts its tokens into segments and the first does not
+@pytest.mark.parametrize("B,T,H,Hk,Dk,Dv,lens", [(4, 200, 38, 38, 64, 128, None),
+                                                 (4, 200, 38, 19, 104, 24, [200, 0, 77, 128]),
+                                                 (5, 1500, 22, 22, 16, 72, [1500, 767, 1, 1499, 769])])
+def test_mixed_widths_of_many_heads(B, T, H, Hk, Dk, Dv, lens, cuda_device):
+    c = Case(cuda_device, B, T, H, Hk, Dk, Dv, lens=lens)
+    check_forward(c)
+    check_backward(c)
+
+
 @pytest.mark.parametrize("H,Hk", [(6, 1), (6, 2), (6, 3)])
 @pytest.mark.parametrize("dtype", [BF, HF])
 def test_shared_heads(H, Hk, dtype, cuda_device):
