@@ -62,7 +62,51 @@ struct Args {
   float* part;                // [blocks][2][N]
 };
 
-__device__ __forceinline__ float sigmoidf_(float z) { return __fdividef(1.0f, 1.0f + __expf(-z)); }
+// Two channels an instruction: fma, mul and add of a pair of floats, each half
+// rounded as by itself.
+__device__ __forceinline__ uint64_t bits(float2 a) {
+  uint64_t w;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(w) : "f"(a.x), "f"(a.y));
+  return w;
+}
+__device__ __forceinline__ float2 halves(uint64_t w) {
+  float2 a;
+  asm("mov.b64 {%0, %1}, %2;" : "=f"(a.x), "=f"(a.y) : "l"(w));
+  return a;
+}
+__device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c) {
+  uint64_t w;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(w) : "l"(bits(a)), "l"(bits(b)), "l"(bits(c)));
+  return halves(w);
+}
+__device__ __forceinline__ float2 mul2(float2 a, float2 b) {
+  uint64_t w;
+  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(w) : "l"(bits(a)), "l"(bits(b)));
+  return halves(w);
+}
+__device__ __forceinline__ float2 add2(float2 a, float2 b) {
+  uint64_t w;
+  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(w) : "l"(bits(a)), "l"(bits(b)));
+  return halves(w);
+}
+__device__ __forceinline__ float2 both(float a) { return make_float2(a, a); }
+__device__ __forceinline__ float2 two(const float* v, int e) { return make_float2(v[e], v[e + 1]); }
+__device__ __forceinline__ void put2(float* v, int e, float2 a) {
+  v[e] = a.x;
+  v[e + 1] = a.y;
+}
+
+// 1 / (1 + 2^(-z log2 e)) of two channels.
+__device__ __forceinline__ float2 sigmoid2(float2 z) {
+  constexpr float kLog2E = 1.44269504088896340736f;
+  float2 p = mul2(z, both(-kLog2E));
+  asm("ex2.approx.ftz.f32 %0, %0;" : "+f"(p.x));
+  asm("ex2.approx.ftz.f32 %0, %0;" : "+f"(p.y));
+  p = add2(p, both(1.0f));
+  asm("rcp.approx.ftz.f32 %0, %0;" : "+f"(p.x));
+  asm("rcp.approx.ftz.f32 %0, %0;" : "+f"(p.y));
+  return p;
+}
 
 // Eight floats as one 32-byte access: two 16-byte ones would each touch half of
 // every 32-byte sector (norms of 16384x4096 on a 32-bit stream: 168 us, 210 with
@@ -246,6 +290,15 @@ struct RowSum {
   }
 };
 
+// Sum of a b over a thread's channels, and of a^2.
+__device__ __forceinline__ float dot(const float a[E], const float b[E]) {
+  float2 s = mul2(two(a, 0), two(b, 0));
+#pragma unroll
+  for (int e = 2; e < E; e += 2) s = fma2(two(a, e), two(b, e), s);
+  return s.x + s.y;
+}
+__device__ __forceinline__ float square_sum(const float a[E]) { return dot(a, a); }
+
 // Sum over the group of `lanes` neighbouring threads that a vector lies in.
 __device__ __forceinline__ float group_sum(float v, int lanes) {
   for (int o = 1; o < lanes; o <<= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
@@ -282,6 +335,7 @@ __global__ void __launch_bounds__(kBlockThreads<TPR>, 1024 / kBlockThreads<TPR>)
   const int64_t step = (int64_t)gridDim.x * kTeams<TPR>;
   int64_t row = (int64_t)blockIdx.x * kTeams<TPR> + team;
   const bool whole = g.group == N, block = g.a.data != nullptr, gated = g.z.data != nullptr;
+  const bool silu = g.gate == SNN_GATE_SILU;
   const float inv_n = 1.0f / (float)N, inv_g = 1.0f / (float)g.group;
   RowSum<TPR> row_sum{scratch};
   float w_post[E], w_pre[E];
@@ -318,34 +372,31 @@ __global__ void __launch_bounds__(kBlockThreads<TPR>, 1024 / kBlockThreads<TPR>)
     r_slot(k).get(g.r, row, N, t, x);
     if (block) {
       a_slot(k).get(g.a, row, N, t, u);
-      float ss[1] = {0.0f};
-#pragma unroll
-      for (int e = 0; e < E; ++e) ss[0] = fmaf(u[e], u[e], ss[0]);
+      float ss[1] = {square_sum(u)};
       if (whole) row_sum(ss);
       else ss[0] = group_sum(ss[0], g.group >> 3);
       const float rstd = rsqrtf(fmaf(ss[0], whole ? inv_n : inv_g, g.eps));
       float z[E];
       if (gated) z_slot(k).get(g.z, row, N, t, z);
 #pragma unroll
-      for (int e = 0; e < E; ++e) {
-        u[e] = u[e] * rstd * w_post[e];
+      for (int e = 0; e < E; e += 2) {
+        const float2 n = mul2(mul2(two(u, e), both(rstd)), two(w_post, e));
+        float2 act = both(1.0f);
         if (gated) {
-          const float s = sigmoidf_(z[e]);
-          u[e] *= g.gate == SNN_GATE_SILU ? z[e] * s : s;
+          act = sigmoid2(two(z, e));
+          if (silu) act = mul2(act, two(z, e));
         }
-        x[e] += u[e];
+        put2(x, e, fma2(n, act, two(x, e)));
       }
       store_row<R, VEC, TPR>(g.ro, row, N, t, x);
     }
-    float ss[1] = {0.0f};
-#pragma unroll
-    for (int e = 0; e < E; ++e) ss[0] = fmaf(x[e], x[e], ss[0]);
+    float ss[1] = {square_sum(x)};
     row_sum(ss);  // also where there is no y: it is what frees the stage
     if (TPR == 32) team_sync<TPR>();
     if (g.y.data) {
       const float rstd = rsqrtf(fmaf(ss[0], inv_n, g.eps));
 #pragma unroll
-      for (int e = 0; e < E; ++e) x[e] = x[e] * rstd * w_pre[e];
+      for (int e = 0; e < E; e += 2) put2(x, e, mul2(mul2(two(x, e), both(rstd)), two(w_pre, e)));
       store_row<T, VEC, TPR>(g.y, row, N, t, x);
     }
     k = k + 1 == g.stages ? 0 : k + 1;
@@ -403,7 +454,7 @@ struct Sums {
       }
     } else {
 #pragma unroll
-      for (int e = 0; e < E; ++e) v[k][e] = fmaf(a[e], b[e], v[k][e]);
+      for (int e = 0; e < E; e += 2) put2(v[k], e, fma2(two(a, e), two(b, e), two(v[k], e)));
     }
   }
 };
@@ -421,6 +472,7 @@ __global__ void __launch_bounds__(kBlockThreads<TPR>, TPR == 1024 ? 1 : kBwdThre
   const int64_t step = (int64_t)gridDim.x * kTeams<TPR>;
   int64_t row = (int64_t)blockIdx.x * kTeams<TPR> + team;
   const bool whole = g.group == N, block = g.a.data != nullptr, gated = g.z.data != nullptr;
+  const bool silu = g.gate == SNN_GATE_SILU;
   const bool pre = g.gy.data != nullptr, through = g.gro.data != nullptr;
   const float inv_n = 1.0f / (float)N, inv_g = 1.0f / (float)g.group;
   RowSum<TPR> row_sum{scratch};
@@ -491,16 +543,13 @@ __global__ void __launch_bounds__(kBlockThreads<TPR>, TPR == 1024 ? 1 : kBwdThre
     if (kLong) load_param<VEC, TPR>(g.w_pre, N, t, w_pre);
     float ss[3] = {0.0f, 0.0f, 0.0f};  // of r'^2, grad_y w_pre r', a^2
     if (pre) {
+      float v[E];
 #pragma unroll
-      for (int e = 0; e < E; ++e) {
-        ss[0] = fmaf(x[e], x[e], ss[0]);
-        ss[1] = fmaf(gw[e] * w_pre[e], x[e], ss[1]);
-      }
+      for (int e = 0; e < E; e += 2) put2(v, e, mul2(two(gw, e), two(w_pre, e)));
+      ss[0] = square_sum(x);
+      ss[1] = dot(v, x);
     }
-    if (block) {
-#pragma unroll
-      for (int e = 0; e < E; ++e) ss[2] = fmaf(h[e], h[e], ss[2]);
-    }
+    if (block) ss[2] = square_sum(h);
     float in_group = 0.0f;
     if (block && !whole) in_group = group_sum(ss[2], g.group >> 3);
     row_sum(ss);
@@ -514,10 +563,13 @@ __global__ void __launch_bounds__(kBlockThreads<TPR>, TPR == 1024 ? 1 : kBwdThre
       const float rstd = rsqrtf(fmaf(ss[0], inv_n, g.eps));
       const float mean = ss[1] * rstd * inv_n;  // mean of (grad_y w_pre) y'
 #pragma unroll
-      for (int e = 0; e < E; ++e) x[e] *= rstd;  // y'
+      for (int e = 0; e < E; e += 2) put2(x, e, mul2(two(x, e), both(rstd)));  // y'
       sums.add(1, gw, x);
 #pragma unroll
-      for (int e = 0; e < E; ++e) d[e] = fmaf(rstd, fmaf(-x[e], mean, gw[e] * w_pre[e]), d[e]);
+      for (int e = 0; e < E; e += 2) {
+        const float2 v = fma2(two(x, e), both(-mean), mul2(two(gw, e), two(w_pre, e)));
+        put2(d, e, fma2(both(rstd), v, two(d, e)));
+      }
     }
     if (g.gr.data) store_row<R, VEC, TPR>(g.gr, row, N, t, d);
     float q[1] = {0.0f};
@@ -526,20 +578,25 @@ __global__ void __launch_bounds__(kBlockThreads<TPR>, TPR == 1024 ? 1 : kBwdThre
       if (kLong) params();
       if (!kHeld && gated) t_slot(k, 2).get(g.z, row, N, t, z);
 #pragma unroll
-      for (int e = 0; e < E; ++e) {
-        h[e] *= rstd_a;
-        x[e] = d[e];
-        d[e] *= c[e];
+      for (int e = 0; e < E; e += 2) {
+        const float2 hn = mul2(two(h, e), both(rstd_a)), dr = two(d, e);
+        float2 m = mul2(dr, two(c, e));
+        put2(h, e, hn);
+        put2(x, e, dr);
         if (gated) {
-          const float s = sigmoidf_(z[e]);
-          const float act = g.gate == SNN_GATE_SILU ? z[e] * s : s;
-          const float slope = g.gate == SNN_GATE_SILU ? s * fmaf(z[e], 1.0f - s, 1.0f) : s * (1.0f - s);
-          z[e] = d[e] * h[e] * slope;  // grad_z
-          x[e] *= act;
-          d[e] *= act;                  // m
+          const float2 s = sigmoid2(two(z, e)), rest = fma2(s, both(-1.0f), both(1.0f));
+          float2 act = s, slope = mul2(s, rest);
+          if (silu) {
+            act = mul2(two(z, e), s);
+            slope = fma2(act, rest, s);
+          }
+          put2(z, e, mul2(mul2(m, hn), slope));  // grad_z
+          put2(x, e, mul2(dr, act));
+          m = mul2(m, act);
         }
-        q[0] = fmaf(d[e], h[e], q[0]);
+        put2(d, e, m);
       }
+      q[0] = dot(d, h);
       sums.add(0, x, h);
       if (g.gz.data) store_row<T, VEC, TPR>(g.gz, row, N, t, z);
     }
@@ -551,7 +608,8 @@ __global__ void __launch_bounds__(kBlockThreads<TPR>, TPR == 1024 ? 1 : kBwdThre
     if (g.ga.data) {
       const float mean = q[0] * (whole ? inv_n : inv_g);
 #pragma unroll
-      for (int e = 0; e < E; ++e) d[e] = rstd_a * fmaf(-h[e], mean, d[e]);
+      for (int e = 0; e < E; e += 2)
+        put2(d, e, mul2(both(rstd_a), fma2(two(h, e), both(-mean), two(d, e))));
       store_row<T, VEC, TPR>(g.ga, row, N, t, d);
     }
     k = k + 1 == g.stages ? 0 : k + 1;
