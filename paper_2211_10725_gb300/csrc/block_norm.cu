@@ -261,12 +261,16 @@ template <int TPR>
 struct RowSum {
   float (*scratch)[3][32];  // [2][value][warp]
   int turn = 0;
+  // in_group: the last value's sum over a group's `lanes` neighbouring threads
   template <int K>
-  __device__ __forceinline__ void operator()(float (&v)[K]) {
+  __device__ __forceinline__ void operator()(float (&v)[K], int lanes = 32, float* in_group = nullptr) {
 #pragma unroll
-    for (int o = 16; o > 0; o >>= 1)
+    for (int o = 1; o < 32; o <<= 1) {
+      if (in_group && o == lanes) *in_group = v[K - 1];
 #pragma unroll
       for (int k = 0; k < K; ++k) v[k] += __shfl_xor_sync(0xffffffffu, v[k], o);
+    }
+    if (in_group && lanes >= 32) *in_group = v[K - 1];
     if constexpr (TPR > 32) {
       constexpr int W = TPR / 32;
       float (*s)[32] = scratch[turn];
@@ -471,7 +475,7 @@ __global__ void __launch_bounds__(kBlockThreads<TPR>, TPR == 1024 ? 1 : kBwdThre
   const int t = threadIdx.x % TPR, team = threadIdx.x / TPR, N = g.N;
   const int64_t step = (int64_t)gridDim.x * kTeams<TPR>;
   int64_t row = (int64_t)blockIdx.x * kTeams<TPR> + team;
-  const bool whole = g.group == N, block = g.a.data != nullptr, gated = g.z.data != nullptr;
+  const bool whole = !VEC || g.group == N, block = g.a.data != nullptr, gated = g.z.data != nullptr;
   const bool silu = g.gate == SNN_GATE_SILU;
   const bool pre = g.gy.data != nullptr, through = g.gro.data != nullptr;
   const float inv_n = 1.0f / (float)N, inv_g = 1.0f / (float)g.group;
@@ -551,8 +555,12 @@ __global__ void __launch_bounds__(kBlockThreads<TPR>, TPR == 1024 ? 1 : kBwdThre
     }
     if (block) ss[2] = square_sum(h);
     float in_group = 0.0f;
-    if (block && !whole) in_group = group_sum(ss[2], g.group >> 3);
-    row_sum(ss);
+    if (kHeld && !whole) {
+      row_sum(ss, g.group >> 3, &in_group);
+    } else {
+      if (kLong && block && !whole) in_group = group_sum(ss[2], g.group >> 3);
+      row_sum(ss);
+    }
     if (!through) {
 #pragma unroll
       for (int e = 0; e < E; ++e) d[e] = 0.0f;
@@ -603,7 +611,7 @@ __global__ void __launch_bounds__(kBlockThreads<TPR>, TPR == 1024 ? 1 : kBwdThre
     // the row is read (VEC: by the threads that copied it): its stage is free
     if (whole) row_sum(q);
     else if (block) q[0] = group_sum(q[0], g.group >> 3);
-    if (!VEC && (!whole || TPR == 32)) team_sync<TPR>();
+    if (!VEC && TPR == 32) team_sync<TPR>();
     if (!kHeld && !ahead) fetch(row + step, 0);
     if (g.ga.data) {
       const float mean = q[0] * (whole ? inv_n : inv_g);
