@@ -281,14 +281,14 @@ struct RowSum {
       __syncthreads();
 #pragma unroll
       for (int k = 0; k < K; ++k) {
-        float a = 0.0f;
-        if constexpr (W == 2) a = s[k][0] + s[k][1];
+        float2 a = make_float2(s[k][0], s[k][1]);
 #pragma unroll
         for (int w = 0; w + 4 <= W; w += 4) {
           const float4 x = *reinterpret_cast<const float4*>(&s[k][w]);
-          a += (x.x + x.y) + (x.z + x.w);
+          const float2 lo = make_float2(x.x, x.y), hi = make_float2(x.z, x.w);
+          a = w ? add2(a, add2(lo, hi)) : add2(lo, hi);
         }
-        v[k] = a;
+        v[k] = a.x + a.y;
       }
     }
   }
