@@ -21,7 +21,10 @@
 // Two blocks (128-wide heads) or four (64-wide) share an SM and fill each
 // other's waits; 64-token chunks are what lets two working sets fit.
 //
-// Roundings to 16 bits: the decayed scores, the state's copy and the output.
+// Roundings to 16 bits: the state's copy and the output.  The decayed scores
+// are two 16-bit parts each, multiplied in turn: an output of few tokens would
+// show a single one's rounding in full (one token, bf16: up to 2^-8 beside the
+// output's own).
 // The decayed values are two 16-bit parts each (v w = hi + lo with products
 // and residuals exact in packed 16-bit arithmetic), multiplied in turn, so a
 // state keeps 16 bits or more of each term; where a bf16 state is an output, a
@@ -88,7 +91,7 @@ struct Cfg {
   // cost the fourth block of an SM) the place of a once it has been used
   static constexpr bool kLowInA = DA == 64 && DC == 64;
   static constexpr int kLowBytes = kLowInA ? 0 : kCBytes;
-  static constexpr int kOutBytes = kCBytes;        // decayed scores (8 KB), then the output
+  static constexpr int kOutBytes = kCBytes;        // decayed scores (8 KB a part), then the output
   static constexpr int kTail = 1024;               // barriers, tables
   // b has two stages, as its last use in a chunk is the latest (one in a
   // 64 x 64 head, where the second would cost the fourth block of an SM)
@@ -663,6 +666,9 @@ __global__ void __launch_bounds__(Cfg<DA, DC>::kThreads, Cfg<DA, DC>::kBlocksPer
   unsigned char* sL = C::kLowInA ? sA : sW + C::kCBytes;  // low parts
   unsigned char* sP = sW + C::kCBytes + C::kLowBytes;     // decayed scores, then the output
   unsigned char* sE = sP + C::kOutBytes;                  // the state's copy (64-wide heads)
+  // second parts of the decayed scores: beside the first ones, or where the
+  // state's copy was (the inter product has read it)
+  unsigned char* sQ = C::kStateTmem ? sP + kBoxBytes : sE;
   // an fp32 output is twice as long: it goes where the decayed values were
   unsigned char* sO32 = sW;
   uint64_t* bar = reinterpret_cast<uint64_t*>(sE + C::kEBytes);
@@ -890,14 +896,21 @@ __global__ void __launch_bounds__(Cfg<DA, DC>::kThreads, Cfg<DA, DC>::kBlocksPer
           if (max(y0 + 8 * ((i >> 1) & 1), x0 + 2 * (lane & 3) + 8 * (i >> 2) + (i & 1)) >= n) s[i] = 0.0f;
       }
       if (it > 0) fail |= wait_all(bar_p, (it - 1) & 1);  // the last output has left sP
+      auto at_score = [&](unsigned char* tile, int k) {  // and 1024 bytes on: row y0 + 8
+        return reinterpret_cast<uint32_t*>(tile + y0 * 128 + ((((x0 >> 3) + k) ^ (y0 & 7)) << 4) + (lane & 3) * 4);
+      };
+      uint32_t rest[C::kToks / 4];  // what the first 16 bits leave, to 16 more
 #pragma unroll
-      for (int k = 0; k < C::kToks / 8; ++k) {
-        unsigned char* to = sP + y0 * 128 + ((((x0 >> 3) + k) ^ (y0 & 7)) << 4) + (lane & 3) * 4;
-        *reinterpret_cast<uint32_t*>(to) = Elem<T>::from2(s[4 * k], s[4 * k + 1]);
-        *reinterpret_cast<uint32_t*>(to + 1024) = Elem<T>::from2(s[4 * k + 2], s[4 * k + 3]);
+      for (int i = 0; i < C::kToks / 4; ++i) {
+        const uint32_t first = Elem<T>::from2(s[2 * i], s[2 * i + 1]);
+        at_score(sP, i >> 1)[(i & 1) * 256] = first;
+        const T* f = reinterpret_cast<const T*>(&first);
+        rest[i] = Elem<T>::from2(s[2 * i] - (float)f[0], s[2 * i + 1] - (float)f[1]);
       }
       fail |= wait_all(bar_x, par);
       gemm::tc_fence_after();
+#pragma unroll
+      for (int i = 0; i < C::kToks / 4; ++i) at_score(sQ, i >> 1)[(i & 1) * 256] = rest[i];
       if (!C::kLowInA && tid == 32 && more && !third) load_a(it + 1);
       __syncwarp();
       // the inter product, decayed, is what the intra product adds to
@@ -942,8 +955,9 @@ __global__ void __launch_bounds__(Cfg<DA, DC>::kThreads, Cfg<DA, DC>::kBlocksPer
       const uint32_t e = elect_one();
       constexpr uint32_t id = idesc<T>(DC, kChunk, true, false);
 #pragma unroll
-      for (int kk = 0; kk < kChunk / 16; ++kk)
-        mma_ss(e, t_out, sdesc_mn(sC + kk * 2048, kBoxBytes), gemm::sdesc_sw128(sP + kk * 32), id, 1);
+      for (int kk = 0; kk < kChunk / 8; ++kk)
+        mma_ss(e, t_out, sdesc_mn(sC + (kk & 3) * 2048, kBoxBytes),
+               gemm::sdesc_sw128((kk < 4 ? sP : sQ) + (kk & 3) * 32), id, 1);
       mma_commit(e, bar_o);
       update(e, sW, 0);
       update(e, sL, 1);
