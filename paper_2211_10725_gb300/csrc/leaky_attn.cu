@@ -60,15 +60,14 @@ __global__ void __launch_bounds__(256) sum_group(const SumArgs g) {
 // How a run over `heads` heads (of all its roles) cuts T tokens into segments:
 // the count that should end soonest, from the times (us) of a chunk in a block
 // alone on its SM and in one of a full SM, and of a block's start:
-//   128 x 128 tiles, two blocks on an SM: attn_chunks 2.35 alone, 3.0 beside
-//   another (16384 tokens of 16 heads, 1 to 19 segments: 602 to 88);
+//   128 x 128 tiles, two blocks on an SM: attn_chunks 2.6 alone, 3.65 beside
+//   another (64 chunks in one and two blocks on every SM: 172 and 240);
 //   attn_segments 1.05 and 1.8;
-//   64 x 64 tiles, four blocks on an SM: attn_chunks 2.2 and 3.55 (64 chunks in
-//   one, two, three and four blocks on every SM: 155, 177, 204 and 233),
-//   attn_segments 0.65 and 1.6;
-//   tiles of both widths, two blocks on an SM: between these.
-// Two segments of 777 tokens in 36 heads' three roles take 44 where one takes
-// 35; four of 1024 tokens in 32 heads take 26 where one takes 42.
+//   64 x 64 tiles: attn_chunks, three blocks on an SM, 2.0 and 3.0 (64 chunks
+//   in one, two and three blocks on every SM: 131, 171 and 197);
+//   attn_segments, four blocks, 0.65 and 1.6;
+//   tiles of both widths, two blocks on an SM: between these (64 x 128: 136 and
+//   189; 128 x 64: 146 and 205).
 // A function of the shapes alone, so that a shape always sums in the same
 // order.
 struct Plan {
@@ -101,14 +100,15 @@ Plan plan(int64_t T, int64_t heads, int da, int dc) {
   best.heads = heads;
   const int64_t chunks = ceil_div(T, kChunk);
   const int kind = (da + dc) / 64 - 2;  // 0: 64 x 64, 1: both, 2: 128 x 128
-  const int per_sm = kind == 0 ? 4 : 2;
-  constexpr double kAlone[3] = {2.2, 2.2, 2.35}, kFull[3] = {3.55, 2.7, 3.0};
+  const int per_sm = kind == 0 ? 3 : 2, seg_per_sm = kind == 0 ? 4 : 2;
+  constexpr double kAlone[3] = {2.0, 2.1, 2.6}, kFull[3] = {3.0, 3.0, 3.65};
   constexpr double kSegAlone[3] = {0.65, 0.85, 1.05}, kSegFull[3] = {1.6, 1.6, 1.8};
   constexpr double kLaunch = 3.0, kScan = 2.0;
   for (int64_t s = 1; s <= kMaxSeg && s <= chunks; ++s) {
     const int64_t per = ceil_div(chunks, s), n = ceil_div(chunks, per);
     double t = wave_time(heads * n, per, per_sm, kAlone[kind], kFull[kind]);
-    if (n > 1) t += kLaunch + wave_time(heads * (n - 1), per, per_sm, kSegAlone[kind], kSegFull[kind]);
+    if (n > 1)
+      t += kLaunch + wave_time(heads * (n - 1), per, seg_per_sm, kSegAlone[kind], kSegFull[kind]);
     if (n > 1) t += n > kSummed ? kScan + 0.1 * n : 0.8 * n;
     if (s == 1 || t < best.time) {
       best.time = t;

@@ -11,38 +11,38 @@
 // every token is read once and the state never leaves the SM.  The last three
 // products are taken transposed, with the Dc channels as the rows: a 128-wide
 // head then fills the tensor core's 128 rows although a chunk has 64 tokens,
-// and the state's 16-bit copy is an operand in tensor memory (in shared
+// and the state's 16-bit parts are an operand in tensor memory (in shared
 // memory for a 64-wide head).  Operands land by TMA as 64-token, 64-element
 // boxes (128-byte swizzle); the same box of b is the K-major operand of the
 // scores and the MN-major one of the update.  Per chunk one thread issues the
 // MMAs in two groups, with the block's work between: the decayed scores and
 // values go back to shared memory as 16-bit operands, the inter product is
 // decayed in place; then the output leaves by TMA and the state is updated.
-// Two blocks (128-wide heads) or four (64-wide) share an SM and fill each
+// Two blocks (128-wide heads) or three (64-wide) share an SM and fill each
 // other's waits; 64-token chunks are what lets two working sets fit.
 //
-// Roundings to 16 bits: the state's copy and the output.  The decayed scores
-// are two 16-bit parts each, multiplied in turn: an output of few tokens would
-// show a single one's rounding in full (one token, bf16: up to 2^-8 beside the
-// output's own).
+// The output is rounded to 16 bits.  The decayed scores and the state are two
+// 16-bit parts each in their products, multiplied in turn: rounded to one, each
+// would add as much error as the output's own rounding (2-norm, bf16: 0.0023
+// instead of 0.0017; an output of few tokens shows a single score's in full).
 // The decayed values are two 16-bit parts each (v w = hi + lo with products
 // and residuals exact in packed 16-bit arithmetic), multiplied in turn, so a
 // state keeps 16 bits or more of each term; where a bf16 state is an output, a
 // third part makes them 24 (fp16: two make 22, and parts below 6e-8 vanish).
-// fp16 has not the range of a sum of products: its state copy is scaled by a
-// power of two.
+// fp16 has not the range of a sum of products: its state's parts are scaled by
+// a power of two.
 //
 // Few heads and many tokens: the tokens are cut into segments, a first kernel
 // (attn_segments: update products only) finds each segment's own contribution
 // to the state; a second (attn_segment_scan), where there are more than a few,
 // the state each one starts from.
 //
-// What bounds it, measured (bf16, 128 x 128): with two blocks on every SM (8 x
-// 4096 tokens, 38 heads) 194 us, the tensors' bytes at 6.6 TB/s, 0.97 of the
-// measured copy rate.  There a chunk takes an SM 1.5 us, of which its MMAs' operand
-// reads from shared memory are about 1.1 (1088 cycles: scores 256, inter 128, intra
-// 192, update 512).  A block alone on its SM takes 2.35 us a chunk, the chain of
-// its products and barriers.
+// What bounds it, measured (bf16, 128 x 128): the instructions of the state's and
+// the scores' parts and the chain of a chunk's products and barriers.  With two
+// blocks on every SM (8 x 4096 tokens, 38 heads) 240 us, the tensors' bytes at
+// 5.3 TB/s, 0.78 of the measured copy rate; 201 with one part each of the scores
+// and the state, 219 with two of the scores alone.  A block alone on its SM takes
+// 2.6 us a chunk, one of two 3.7.
 #pragma once
 
 #include <cuda.h>
@@ -81,31 +81,31 @@ struct Cfg {
   static constexpr int kThreads = (DA == 128 || DC == 128) ? 256 : 128;
   static constexpr int kHalves = kThreads / 128;   // column halves of an accumulator
   static constexpr int kRowHalves = DC / 64;       // 16-lane halves of a warp's channels
-  static constexpr int kCols = DA / kHalves;       // state columns of a warp
+  static constexpr int kCols = DA / kHalves;       // state columns of a warp: neighbours,
+  // or, of 128 in two halves, 32 in each 64, so that every warp has read the
+  // upper 64 columns of its update where it puts the state's second parts
+  static constexpr bool kSplit = DA == 128 && kHalves == 2;
+  static constexpr int kStep = kSplit ? 32 : kCols;  // from one half's first column to the other's
   static constexpr int kToks = kChunk / kHalves;   // tokens (score columns) of a warp
   static constexpr int kABytes = kChunk * DA * 2;
   static constexpr int kCBytes = kChunk * DC * 2;
-  static constexpr bool kStateTmem = DC == 128;    // where the state's 16-bit copy is
-  static constexpr int kEBytes = kStateTmem ? 0 : DA * DC * 2;
-  // the values' low parts: a buffer of their own, or (64 x 64, where it would
-  // cost the fourth block of an SM) the place of a once it has been used
-  static constexpr bool kLowInA = DA == 64 && DC == 64;
-  static constexpr int kLowBytes = kLowInA ? 0 : kCBytes;
+  static constexpr bool kStateTmem = DC == 128;    // where the state's 16-bit parts are
+  static constexpr int kEBytes = kStateTmem ? 0 : 2 * DA * DC * 2;
   static constexpr int kOutBytes = kCBytes;        // decayed scores (8 KB a part), then the output
   static constexpr int kTail = 1024;               // barriers, tables
-  // b has two stages, as its last use in a chunk is the latest (one in a
-  // 64 x 64 head, where the second would cost the fourth block of an SM)
-  static constexpr int kBStages = kLowInA ? 1 : 2;
+  // b has two stages, as its last use in a chunk is the latest
+  static constexpr int kBStages = 2;
   // a's place, big enough to take a third part of the values after a's last use
-  static constexpr int kQBytes = kLowInA || kABytes > kCBytes ? kABytes : kCBytes;
-  static constexpr size_t kSmem =
-      kQBytes + kBStages * kABytes + 2 * kCBytes + kLowBytes + kEBytes + kOutBytes + kTail;
+  static constexpr int kQBytes = kABytes > kCBytes ? kABytes : kCBytes;
+  static constexpr size_t kSmem = kQBytes + kBStages * kABytes + 3 * kCBytes + kEBytes + kOutBytes + kTail;
   // attn_segments: two stages of b and c, the parts of the decayed values
   static constexpr size_t kSegSmem = 2 * (kABytes + kCBytes) + 2 * kCBytes + kTail;
   static constexpr uint32_t kSegTmemCols = 2 * DA;
-  // tensor memory: output, update (scores in its first 64 columns), state
+  // tensor memory: output, update (scores in its first 64 columns), first
+  // parts of the state; the second ones behind, or in the update's upper half
   static constexpr uint32_t kTmemCols = kStateTmem ? 256 : (DA == 64 ? 128 : 256);
-  static constexpr int kBlocksPerSm = kThreads == 128 ? 4 : 2;
+  static constexpr int kBlocksPerSm = kThreads == 128 ? 3 : 2;
+  static constexpr int kSegBlocksPerSm = kThreads == 128 ? 4 : 2;
 };
 
 __device__ __forceinline__ void tma_load_4d(void* dst, const CUtensorMap* map, int x, int y, int z,
@@ -273,6 +273,30 @@ __device__ __forceinline__ void split_product(__half2 v, __half2 w1, __half2 w2,
   lo = __hfma2(v, w2, __hfma2(v, w1, __hneg2(hi)));
 }
 
+// x and y as two 16-bit parts each.
+__device__ __forceinline__ float2 minus2(float x, float y, float a, float b) {
+  uint64_t w, v;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(w) : "f"(x), "f"(y));
+  asm("mov.b64 %0, {%1, %2};" : "=l"(v) : "f"(-a), "f"(-b));
+  asm("add.rn.f32x2 %0, %0, %1;" : "+l"(w) : "l"(v));
+  float2 d;
+  asm("mov.b64 {%0, %1}, %2;" : "=f"(d.x), "=f"(d.y) : "l"(w));
+  return d;
+}
+template <typename T>
+__device__ __forceinline__ uint32_t two_parts(float x, float y, uint32_t& rest) {
+  const uint32_t first = Elem<T>::from2(x, y);
+  float2 d;
+  if constexpr (std::is_same<T, __half>::value) {
+    const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&first));
+    d = minus2(x, y, f.x, f.y);
+  } else {
+    d = minus2(x, y, __uint_as_float(first << 16), __uint_as_float(first & 0xffff0000u));
+  }
+  rest = Elem<T>::from2(d.x, d.y);
+  return first;
+}
+
 template <typename T>
 struct Pair;
 template <>
@@ -358,7 +382,7 @@ struct Place {
 };
 
 // A thread's part of a head's transposed state: channels row + 16*rh (+8) of c,
-// columns col + 8k (+1) of a and b.
+// columns col + 8k (+1) of a and b (split columns: from k = 4 on 32 further).
 template <int DA, int DC>
 struct State {
   using C = Cfg<DA, DC>;
@@ -366,7 +390,7 @@ struct State {
   int row, col;
 
   __device__ __forceinline__ State(int quad, int half, int lane)
-      : row((C::kRowHalves == 2 ? 32 : 16) * quad + (lane >> 2)), col(half * C::kCols + 2 * (lane & 3)) {
+      : row((C::kRowHalves == 2 ? 32 : 16) * quad + (lane >> 2)), col(half * C::kStep + 2 * (lane & 3)) {
     each([](float& x, int, int) { x = 0.0f; });
   }
   template <typename F>
@@ -375,7 +399,8 @@ struct State {
     for (int rh = 0; rh < C::kRowHalves; ++rh)
 #pragma unroll
       for (int i = 0; i < C::kCols / 2; ++i)
-        f(e[rh][i], row + 16 * rh + 8 * ((i >> 1) & 1), col + 8 * (i >> 2) + (i & 1));
+        f(e[rh][i], row + 16 * rh + 8 * ((i >> 1) & 1),
+          col + 8 * (i >> 2) + (C::kSplit && i >= 16 ? 32 : 0) + (i & 1));
   }
   // e = f * the caller's state (zeros where there is none)
   __device__ __forceinline__ void load(const Args& g, const Role& r, int b, int h, float f) {
@@ -418,15 +443,18 @@ struct State {
         e[rh][i + 3] = fmaf(e[rh][i + 3], decay, v.w);
       }
   }
-  // e = decay e + the update product in tensor memory
+  // e = decay e + the update product in tensor memory (at: the thread's half)
   __device__ __forceinline__ void add_update(uint32_t at, float decay) {
+    constexpr int kRun = C::kSplit ? 16 : C::kCols / 2;  // registers of neighbouring columns
 #pragma unroll
-    for (int rh = 0; rh < C::kRowHalves; ++rh) {
-      float u[C::kCols / 2];
-      tmem_ld_rows(at + ((uint32_t)(16 * rh) << 16), u);
+    for (int rh = 0; rh < C::kRowHalves; ++rh)
 #pragma unroll
-      for (int i = 0; i < C::kCols / 2; ++i) e[rh][i] = fmaf(decay, e[rh][i], u[i]);
-    }
+      for (int j = 0; j < C::kCols / 2; j += kRun) {
+        float u[kRun];
+        tmem_ld_rows(at + ((uint32_t)(16 * rh) << 16) + (j ? 64 : 0), u);
+#pragma unroll
+        for (int i = 0; i < kRun; ++i) e[rh][j + i] = fmaf(decay, e[rh][j + i], u[i]);
+      }
   }
 };
 
@@ -475,7 +503,7 @@ __device__ __forceinline__ void clear_rows(unsigned char* tile, int bytes, int n
 // values through their products; the reads alone would be 1.45.  One block on an
 // SM with the split pipelined as well (twice the shared memory) took 1.1.
 template <typename T, int DA, int DC>
-__global__ void __launch_bounds__(Cfg<DA, DC>::kThreads, Cfg<DA, DC>::kBlocksPerSm)
+__global__ void __launch_bounds__(Cfg<DA, DC>::kThreads, Cfg<DA, DC>::kSegBlocksPerSm)
     attn_segments(const __grid_constant__ ChunkArgs p) {
   using C = Cfg<DA, DC>;
   constexpr int NT = C::kThreads;
@@ -543,7 +571,7 @@ __global__ void __launch_bounds__(Cfg<DA, DC>::kThreads, Cfg<DA, DC>::kBlocksPer
   }
   __syncthreads();
 
-  const uint32_t t_upd = tmem + ((uint32_t)(quad * 32) << 16) + half * C::kCols;
+  const uint32_t t_upd = tmem + ((uint32_t)(quad * 32) << 16) + half * C::kStep;
   const bool third = !kHalf && r.s_out;
   int fail = 0, it = 0, n_last = 0;
   for (; it < n_chunks; ++it) {
@@ -663,11 +691,11 @@ __global__ void __launch_bounds__(Cfg<DA, DC>::kThreads, Cfg<DA, DC>::kBlocksPer
   unsigned char* sB2 = sA + C::kQBytes;                   // the stages of b
   unsigned char* sC = sB2 + C::kBStages * C::kABytes;
   unsigned char* sW = sC + C::kCBytes;                    // decayed values, high parts
-  unsigned char* sL = C::kLowInA ? sA : sW + C::kCBytes;  // low parts
-  unsigned char* sP = sW + C::kCBytes + C::kLowBytes;     // decayed scores, then the output
-  unsigned char* sE = sP + C::kOutBytes;                  // the state's copy (64-wide heads)
+  unsigned char* sL = sW + C::kCBytes;                    // low parts
+  unsigned char* sP = sL + C::kCBytes;                    // decayed scores, then the output
+  unsigned char* sE = sP + C::kOutBytes;                  // the state's parts (64-wide heads)
   // second parts of the decayed scores: beside the first ones, or where the
-  // state's copy was (the inter product has read it)
+  // state's were (the inter product has read them)
   unsigned char* sQ = C::kStateTmem ? sP + kBoxBytes : sE;
   // an fp32 output is twice as long: it goes where the decayed values were
   unsigned char* sO32 = sW;
@@ -767,7 +795,8 @@ __global__ void __launch_bounds__(Cfg<DA, DC>::kThreads, Cfg<DA, DC>::kBlocksPer
 
   const uint32_t t_quad = (uint32_t)(quad * 32) << 16;
   const uint32_t t_out = tmem, t_upd = tmem + kChunk, t_state = tmem + kChunk + DA;
-  // The state's 16-bit copy.  fp16 has not the range of a sum of products: its
+  const uint32_t t_low = C::kSplit ? t_upd + 64 : t_state + DA / 2;
+  // The state as two 16-bit parts.  fp16 has not the range of a sum of products: its
   // copy is scaled by the power of two that brings the largest element to
   // 2^10 .. 2^11, and e_back undoes it.
   float e_back = 1.0f;
@@ -786,24 +815,32 @@ __global__ void __launch_bounds__(Cfg<DA, DC>::kThreads, Cfg<DA, DC>::kBlocksPer
       f = __uint_as_float((unsigned)(127 - e) << 23);
       e_back = __uint_as_float((unsigned)(127 + e) << 23);
     }
+    constexpr int kRun = C::kSplit ? 8 : C::kCols / 4;  // pairs of neighbouring columns
 #pragma unroll
-    for (int rh = 0; rh < C::kRowHalves; ++rh) {
-      uint32_t v[C::kCols / 4];
+    for (int rh = 0; rh < C::kRowHalves; ++rh)
 #pragma unroll
-      for (int i = 0; i < C::kCols / 4; ++i)
-        v[i] = kHalf ? Elem<T>::from2(f * state.e[rh][2 * i], f * state.e[rh][2 * i + 1])
-                     : Elem<T>::from2(state.e[rh][2 * i], state.e[rh][2 * i + 1]);
-      if constexpr (C::kStateTmem) {
-        tmem_st_pairs(t_state + t_quad + ((uint32_t)(16 * rh) << 16) + half * (C::kCols / 2), v);
-      } else {  // rows of Da: 64-column boxes of DC 128-byte rows
+      for (int j = 0; j < C::kCols / 4; j += kRun) {
+        uint32_t v[kRun], rest[kRun];  // a pair's first 16 bits, and what they leave to 16 more
 #pragma unroll
-        for (int i = 0; i < C::kCols / 4; ++i) {
-          const int x = half * C::kCols + 8 * (i >> 1), y = state.row + 8 * (i & 1);
-          *reinterpret_cast<uint32_t*>(sE + (x >> 6) * (DC * 128) + y * 128 +
-                                       ((((x & 63) >> 3) ^ (y & 7)) << 4) + (lane & 3) * 4) = v[i];
+        for (int i = 0; i < kRun; ++i) {
+          v[i] = two_parts<T>(f * state.e[rh][2 * (j + i)], f * state.e[rh][2 * (j + i) + 1], rest[i]);
+        }
+        if constexpr (C::kStateTmem) {
+          const uint32_t at = t_quad + ((uint32_t)(16 * rh) << 16) + half * (C::kStep / 2);
+          tmem_st_pairs(t_state + at + (j ? 32 : 0), v);
+          // split columns: a half's 64 side by side, in the columns it has read
+          tmem_st_pairs(t_low + at + (C::kSplit ? half * (C::kStep / 2) + 2 * j : 0), rest);
+        } else {  // rows of Da: 64-column boxes of DC 128-byte rows
+#pragma unroll
+          for (int i = 0; i < kRun; ++i) {
+            const int x = half * C::kStep + 8 * (i >> 1) + (j ? 64 : 0), y = state.row + 8 * (i & 1);
+            uint32_t* to = reinterpret_cast<uint32_t*>(sE + (x >> 6) * (DC * 128) + y * 128 +
+                                                       ((((x & 63) >> 3) ^ (y & 7)) << 4) + (lane & 3) * 4);
+            to[0] = v[i];
+            to[DA * DC / 2] = rest[i];
+          }
         }
       }
-    }
     if constexpr (C::kStateTmem) tmem_wait_st();
   };
   __syncwarp();
@@ -818,7 +855,6 @@ __global__ void __launch_bounds__(Cfg<DA, DC>::kThreads, Cfg<DA, DC>::kBlocksPer
   const int tok = half * C::kToks + 2 * (lane & 3);  // its output tokens: tok + 8k (+1)
   // the third part: only the last segment's state is an output
   const bool third = !kHalf && ends;
-  uint32_t u_phase = 0;
   int fail = 0, it = 0;
   for (; it < n_chunks; ++it) {
     const uint32_t par = it & 1;
@@ -828,7 +864,7 @@ __global__ void __launch_bounds__(Cfg<DA, DC>::kThreads, Cfg<DA, DC>::kBlocksPer
     const int ex = n - (last ? 1 : 0);
     const bool more = it + 1 < n_chunks;
     unsigned char* sB = sB2 + (it % C::kBStages) * C::kABytes;
-    if (C::kBStages == 2 && tid == 64 && more) load_b(it + 1);  // chunk it - 1 is done with its stage
+    if (tid == 64 && more) load_b(it + 1);  // chunk it - 1 is done with its stage
     if (tid == 96) prefetch(it + 2);
 
     if (warp == 0) {
@@ -846,13 +882,18 @@ __global__ void __launch_bounds__(Cfg<DA, DC>::kThreads, Cfg<DA, DC>::kBlocksPer
       }
       mma_commit(e, bar_s);
 #pragma unroll
-      for (int kk = 0; kk < DA / 16; ++kk) {
-        const uint64_t q = gemm::sdesc_sw128(sA + (kk / 4) * kBoxBytes + (kk % 4) * 32);
-        if constexpr (C::kStateTmem)
-          mma_ts(e, t_out, t_state + 8 * kk, q, id_x, kk != 0);
-        else
-          mma_ss(e, t_out, gemm::sdesc_sw128(sE + (kk / 4) * (DC * 128) + (kk % 4) * 32), q, id_x, kk != 0);
-      }
+      for (int part = 0; part < 2; ++part)
+#pragma unroll
+        for (int kk = 0; kk < DA / 16; ++kk) {
+          const uint64_t q = gemm::sdesc_sw128(sA + (kk / 4) * kBoxBytes + (kk % 4) * 32);
+          if constexpr (C::kStateTmem) {
+            const uint32_t low = C::kSplit ? 32 * ((kk >> 1) & 1) + 16 * (kk >> 2) + 8 * (kk & 1) : 8 * kk;
+            mma_ts(e, t_out, part ? t_low + low : t_state + 8 * kk, q, id_x, part | kk);
+          } else {
+            mma_ss(e, t_out, gemm::sdesc_sw128(sE + part * (DA * DC * 2) + (kk / 4) * (DC * 128) + (kk % 4) * 32), q,
+                   id_x, part | kk);
+          }
+        }
       mma_commit(e, bar_x);
     }
 
@@ -860,25 +901,14 @@ __global__ void __launch_bounds__(Cfg<DA, DC>::kThreads, Cfg<DA, DC>::kBlocksPer
     fail |= wait_all(bar_c, par);
     if (out_f32 && it > 0) fail |= wait_all(bar_p, (it - 1) & 1);  // the last output has left sO32
     constexpr int kPieces = C::kCBytes / 16 / NT;
-    uint4 low[kPieces];
 #pragma unroll
     for (int i = 0; i < kPieces; ++i) {
       const int piece = i * NT + tid, y = (piece >> 3) & 63;
-      uint4 high;
-      split_piece<T>(sC, piece, y < n, decays.parts[max(0, rev ? y + 1 : ex - y)], high, low[i]);
+      uint4 high, low;
+      split_piece<T>(sC, piece, y < n, decays.parts[max(0, rev ? y + 1 : ex - y)], high, low);
       reinterpret_cast<uint4*>(sW)[piece] = high;
-      if (!C::kLowInA) reinterpret_cast<uint4*>(sL)[piece] = low[i];
+      reinterpret_cast<uint4*>(sL)[piece] = low;
     }
-    auto put_third = [&](unsigned char* to) {
-#pragma unroll
-      for (int i = 0; i < kPieces; ++i) {
-        const int piece = i * NT + tid, y = (piece >> 3) & 63;
-        reinterpret_cast<uint4*>(to)[piece] =
-            third_part<T>(sC, piece, y < n, decays.of(max(0, rev ? y + 1 : ex - y), rev),
-                          reinterpret_cast<const uint4*>(sW)[piece],
-                          reinterpret_cast<const uint4*>(sL)[piece]);
-      }
-    };
 
     {
       // decayed scores
@@ -901,17 +931,13 @@ __global__ void __launch_bounds__(Cfg<DA, DC>::kThreads, Cfg<DA, DC>::kBlocksPer
       };
       uint32_t rest[C::kToks / 4];  // what the first 16 bits leave, to 16 more
 #pragma unroll
-      for (int i = 0; i < C::kToks / 4; ++i) {
-        const uint32_t first = Elem<T>::from2(s[2 * i], s[2 * i + 1]);
-        at_score(sP, i >> 1)[(i & 1) * 256] = first;
-        const T* f = reinterpret_cast<const T*>(&first);
-        rest[i] = Elem<T>::from2(s[2 * i] - (float)f[0], s[2 * i + 1] - (float)f[1]);
-      }
+      for (int i = 0; i < C::kToks / 4; ++i)
+        at_score(sP, i >> 1)[(i & 1) * 256] = two_parts<T>(s[2 * i], s[2 * i + 1], rest[i]);
       fail |= wait_all(bar_x, par);
       gemm::tc_fence_after();
 #pragma unroll
       for (int i = 0; i < C::kToks / 4; ++i) at_score(sQ, i >> 1)[(i & 1) * 256] = rest[i];
-      if (!C::kLowInA && tid == 32 && more && !third) load_a(it + 1);
+      if (tid == 32 && more && !third) load_a(it + 1);
       __syncwarp();
       // the inter product, decayed, is what the intra product adds to
       float f[C::kToks / 4];
@@ -930,11 +956,16 @@ __global__ void __launch_bounds__(Cfg<DA, DC>::kThreads, Cfg<DA, DC>::kBlocksPer
         tmem_st_rows(at, x);
       }
     }
-    if (C::kLowInA) {
+    if (third) {  // where a was: the scores and the inter product have read it
 #pragma unroll
-      for (int i = 0; i < kPieces; ++i) reinterpret_cast<uint4*>(sL)[i * NT + tid] = low[i];
+      for (int i = 0; i < kPieces; ++i) {
+        const int piece = i * NT + tid, y = (piece >> 3) & 63;
+        reinterpret_cast<uint4*>(sA)[piece] =
+            third_part<T>(sC, piece, y < n, decays.of(max(0, rev ? y + 1 : ex - y), rev),
+                          reinterpret_cast<const uint4*>(sW)[piece],
+                          reinterpret_cast<const uint4*>(sL)[piece]);
+      }
     }
-    if (!C::kLowInA && third) put_third(sA);  // the scores and the inter product have read a
     if (n < kChunk) {
       clear_rows(sB, C::kABytes, n, tid, NT);
       clear_rows(sC, C::kCBytes, n, tid, NT);
@@ -961,13 +992,13 @@ __global__ void __launch_bounds__(Cfg<DA, DC>::kThreads, Cfg<DA, DC>::kBlocksPer
       mma_commit(e, bar_o);
       update(e, sW, 0);
       update(e, sL, 1);
-      if (!C::kLowInA && third) update(e, sA, 1);
+      if (third) update(e, sA, 1);
       mma_commit(e, bar_u);
     }
 
     fail |= wait_all(bar_o, par);
     gemm::tc_fence_after();
-    if (tid == 96 && more && !(C::kLowInA && third)) load_c(it + 1);
+    if (tid == 96 && more) load_c(it + 1);
     __syncwarp();
     auto output = [&](auto put) {  // put(16-lane half, its registers)
 #pragma unroll
@@ -998,20 +1029,7 @@ __global__ void __launch_bounds__(Cfg<DA, DC>::kThreads, Cfg<DA, DC>::kBlocksPer
       });
     }
 
-    fail |= wait_all(bar_u, u_phase);
-    u_phase ^= 1;
-    if (C::kLowInA && third) {  // no buffer is free before the first parts are used
-      put_third(sW);
-      gemm::fence_async_smem();
-      if (__syncthreads_or(fail)) break;
-      if (warp == 0) {
-        const uint32_t e = elect_one();
-        update(e, sW, 1);
-        mma_commit(e, bar_u);
-      }
-      fail |= wait_all(bar_u, u_phase);
-      u_phase ^= 1;
-    }
+    fail |= wait_all(bar_u, par);
     gemm::tc_fence_after();
     if (out_f32) {
       output([&](int rh, const float (&o)[C::kToks / 2]) {  // boxes of 32 channels (128 bytes) x 64 tokens
@@ -1023,11 +1041,9 @@ __global__ void __launch_bounds__(Cfg<DA, DC>::kThreads, Cfg<DA, DC>::kBlocksPer
         }
       });
     }
-    if (tid == 32 && more && (C::kLowInA || third)) load_a(it + 1);
-    if (C::kBStages == 1 && tid == 64 && more) load_b(it + 1);
-    if (tid == 96 && more && C::kLowInA && third) load_c(it + 1);
+    if (tid == 32 && more && third) load_a(it + 1);
     __syncwarp();
-    state.add_update(t_upd + t_quad + half * C::kCols, decays.of(ex, rev));
+    state.add_update(t_upd + t_quad + half * C::kStep, decays.of(ex, rev));
     if (more) put_state((it + 1) & 1);
     gemm::fence_async_smem();
     gemm::tc_fence_before();

@@ -69,3 +69,16 @@ def check(c, with_state):
 @pytest.mark.parametrize("dtype", [BF, HF])
 def test_one_chunk(T, H, Hk, Dk, Dv, dtype, cuda_device):
     check(Case(cuda_device, 5, T, H, Hk, Dk, Dv, dtype), False)
+
+
+# from a state and over several chunks: what the state adds is rounded once as well
+@pytest.mark.parametrize("T", [1, 65, 200, 700])
+@pytest.mark.parametrize("H,Hk,Dk,Dv", [(6, 6, 128, 128), (4, 2, 64, 64), (6, 3, 40, 72), (3, 1, 128, 48)])
+@pytest.mark.parametrize("dtype", [BF, HF])
+def test_states(T, H, Hk, Dk, Dv, dtype, cuda_device):
+    check(Case(cuda_device, 2, T, H, Hk, Dk, Dv, dtype), True)
+
+
+@pytest.mark.parametrize("dtype", [BF, HF])
+def test_ragged(dtype, cuda_device):
+    check(Case(cuda_device, 4, 300, 6, 2, 96, 120, dtype, lens=[300, 0, 1, 131]), True)
