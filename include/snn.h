@@ -565,8 +565,7 @@ size_t snn_leaky_attn_workspace_bytes(const snn_attn_desc* desc, int backward);
  * o must not overlap q, k or v.  Products run on the tensor cores with fp32
  * accumulation; the state is kept in fp32 between chunks.  Valid tokens must
  * be finite: an infinity or NaN there reaches every token of its sequence and
- * head, earlier ones of its chunk included; in fp16 a decayed score scale *
- * beta^(i-j) q_i.k_j past 65504 is infinite.
+ * head, earlier ones of its chunk included.
  */
 snn_status_t snn_leaky_attn_fwd(const snn_attn_desc* desc, const snn_bthd* q, const snn_bthd* k,
                                 const snn_bthd* v, const float* beta, const int32_t* seq_lens,

@@ -29,8 +29,8 @@
 // and residuals exact in packed 16-bit arithmetic), multiplied in turn, so a
 // state keeps 16 bits or more of each term; where a bf16 state is an output, a
 // third part makes them 24 (fp16: two make 22, and parts below 6e-8 vanish).
-// fp16 has not the range of a sum of products: its state's parts are scaled by
-// a power of two.
+// fp16 has not the range of a sum of products: its state's and its scores'
+// parts are scaled by a power of two each chunk.
 //
 // Few heads and many tokens: the tokens are cut into segments, a first kernel
 // (attn_segments: update products only) finds each segment's own contribution
@@ -488,6 +488,18 @@ __device__ __forceinline__ uint4 third_part(const unsigned char* values, int pie
   return out;
 }
 
+__device__ __forceinline__ float power_of_2(int e) { return __uint_as_float((unsigned)(127 + e) << 23); }
+
+// e for which the block's largest m lies in 2^(e+to) .. 2^(e+to+1) (0 where it is
+// zero or not finite).  Every thread of the block calls; *slot is 0 before.
+__device__ __forceinline__ int exponent_of_all(unsigned* slot, float m, int lane, int to) {
+  const unsigned bits = __reduce_max_sync(0xffffffffu, __float_as_uint(m));
+  if (lane == 0) atomicMax(slot, bits);
+  __syncthreads();
+  const unsigned all = *reinterpret_cast<volatile unsigned*>(slot);
+  return all == 0u || all >= 0x7f800000u ? 0 : (int)(all >> 23) - 127 - to;
+}
+
 // Zero the places past the sequence's end in a tile of 128-byte rows.
 __device__ __forceinline__ void clear_rows(unsigned char* tile, int bytes, int n, int tid, int threads) {
   for (int i = tid; i < bytes / 16; i += threads)
@@ -703,8 +715,9 @@ __global__ void __launch_bounds__(Cfg<DA, DC>::kThreads, Cfg<DA, DC>::kBlocksPer
   uint64_t *bar_a = bar, *bar_b = bar + 1, *bar_c = bar + 3, *bar_s = bar + 4, *bar_u = bar + 5,
            *bar_o = bar + 6, *bar_x = bar + 7, *bar_p = bar + 8;  // bar_b: one for each stage
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bar + 9);
-  unsigned* top = reinterpret_cast<unsigned*>(bar + 10);  // [2] bits of the state's largest element
-  Decays<T>& decays = *reinterpret_cast<Decays<T>*>(bar + 11);
+  unsigned* top = reinterpret_cast<unsigned*>(bar + 10);   // [2] bits of the state's largest element
+  unsigned* peak = reinterpret_cast<unsigned*>(bar + 11);  // [2] and of the scores'
+  Decays<T>& decays = *reinterpret_cast<Decays<T>*>(bar + 12);
 
   const int tid = threadIdx.x, warp = __shfl_sync(0xffffffffu, tid >> 5, 0), lane = tid & 31;
   const int quad = warp & 3, half = warp >> 2;
@@ -725,7 +738,7 @@ __global__ void __launch_bounds__(Cfg<DA, DC>::kThreads, Cfg<DA, DC>::kBlocksPer
   }
   if (tid == 0) {
     for (int i = 0; i < 9; ++i) mbar_init(&bar[i], 1);
-    top[0] = top[1] = 0u;
+    top[0] = top[1] = peak[0] = peak[1] = 0u;
     fence_barrier_init();
   }
   __syncwarp();
@@ -796,8 +809,8 @@ __global__ void __launch_bounds__(Cfg<DA, DC>::kThreads, Cfg<DA, DC>::kBlocksPer
   const uint32_t t_quad = (uint32_t)(quad * 32) << 16;
   const uint32_t t_out = tmem, t_upd = tmem + kChunk, t_state = tmem + kChunk + DA;
   const uint32_t t_low = C::kSplit ? t_upd + 64 : t_state + DA / 2;
-  // The state as two 16-bit parts.  fp16 has not the range of a sum of products: its
-  // copy is scaled by the power of two that brings the largest element to
+  // The state as two 16-bit parts.  fp16 has not the range of a sum of products: they
+  // are scaled by the power of two that brings the largest element to
   // 2^10 .. 2^11, and e_back undoes it.
   float e_back = 1.0f;
   auto put_state = [&](int slot) {
@@ -805,15 +818,9 @@ __global__ void __launch_bounds__(Cfg<DA, DC>::kThreads, Cfg<DA, DC>::kBlocksPer
     if constexpr (kHalf) {
       float m = 0.0f;
       state.each([&](float& e, int, int) { m = fmaxf(m, fabsf(e)); });
-      const unsigned bits = __reduce_max_sync(0xffffffffu, __float_as_uint(m));
-      if (lane == 0) atomicMax(&top[slot], bits);
-      __syncthreads();
-      const unsigned all = *reinterpret_cast<volatile unsigned*>(&top[slot]);
-      int e = (int)(all >> 23) - 127 - 10;
-      if (all == 0u || all >= 0x7f800000u) e = 0;
-      e = max(e, -116);  // keeps 2^-e and 2^e normal
-      f = __uint_as_float((unsigned)(127 - e) << 23);
-      e_back = __uint_as_float((unsigned)(127 + e) << 23);
+      const int e = max(exponent_of_all(&top[slot], m, lane, 10), -116);  // keeps 2^-e and 2^e normal
+      f = power_of_2(-e);
+      e_back = power_of_2(e);
     }
     constexpr int kRun = C::kSplit ? 8 : C::kCols / 4;  // pairs of neighbouring columns
 #pragma unroll
@@ -868,7 +875,7 @@ __global__ void __launch_bounds__(Cfg<DA, DC>::kThreads, Cfg<DA, DC>::kBlocksPer
     if (tid == 96) prefetch(it + 2);
 
     if (warp == 0) {
-      if (kHalf && lane == 0) top[(it + 1) & 1] = 0u;
+      if (kHalf && lane == 0) top[(it + 1) & 1] = peak[(it + 1) & 1] = 0u;
       fail |= wait_all(bar_a, par);
       fail |= wait_all(bar_b + it % C::kBStages, (it / C::kBStages) & 1);
       gemm::tc_fence_after();
@@ -910,6 +917,11 @@ __global__ void __launch_bounds__(Cfg<DA, DC>::kThreads, Cfg<DA, DC>::kBlocksPer
       reinterpret_cast<uint4*>(sL)[piece] = low;
     }
 
+    // A sum of 16-bit products may pass fp16's range where the output does not:
+    // the scores are scaled by the power of two that brings the largest to
+    // 2^14 .. 2^15, the inter product with them, and s_back undoes it in the
+    // output.  No further up than 2^24, which leaves fp32 room for the state's part.
+    float s_back = 1.0f;
     {
       // decayed scores
       fail |= wait_all(bar_s, par);
@@ -924,6 +936,17 @@ __global__ void __launch_bounds__(Cfg<DA, DC>::kThreads, Cfg<DA, DC>::kBlocksPer
 #pragma unroll
         for (int i = 0; i < C::kToks / 2; ++i)
           if (max(y0 + 8 * ((i >> 1) & 1), x0 + 2 * (lane & 3) + 8 * (i >> 2) + (i & 1)) >= n) s[i] = 0.0f;
+      }
+      float s_scale = 1.0f;
+      if constexpr (kHalf) {
+        float m = 0.0f;
+#pragma unroll
+        for (int i = 0; i < C::kToks / 2; ++i) m = fmaxf(m, fabsf(s[i]));
+        const int e = max(exponent_of_all(&peak[par], m, lane, 14), -24);
+        s_scale = power_of_2(-e);
+        s_back = power_of_2(e);
+#pragma unroll
+        for (int i = 0; i < C::kToks / 2; ++i) s[i] *= s_scale;
       }
       if (it > 0) fail |= wait_all(bar_p, (it - 1) & 1);  // the last output has left sP
       auto at_score = [&](unsigned char* tile, int k) {  // and 1024 bytes on: row y0 + 8
@@ -944,7 +967,7 @@ __global__ void __launch_bounds__(Cfg<DA, DC>::kThreads, Cfg<DA, DC>::kBlocksPer
 #pragma unroll
       for (int i = 0; i < C::kToks / 4; ++i) {
         const int y = tok + 8 * (i >> 1) + (i & 1);
-        f[i] = e_back * scale * decays.lag[64 + (rev ? y + 1 - n : y)];
+        f[i] = s_scale * e_back * scale * decays.lag[64 + (rev ? y + 1 - n : y)];
       }
 #pragma unroll
       for (int rh = 0; rh < C::kRowHalves; ++rh) {
@@ -1005,6 +1028,10 @@ __global__ void __launch_bounds__(Cfg<DA, DC>::kThreads, Cfg<DA, DC>::kBlocksPer
       for (int rh = 0; rh < C::kRowHalves; ++rh) {
         float o[C::kToks / 2];
         tmem_ld_rows(t_out + t_quad + ((uint32_t)(16 * rh) << 16) + half * C::kToks, o);
+        if constexpr (kHalf) {
+#pragma unroll
+          for (int i = 0; i < C::kToks / 2; ++i) o[i] *= s_back;
+        }
         if (n < kChunk) {
 #pragma unroll
           for (int i = 0; i < C::kToks / 2; ++i)
