@@ -28,9 +28,9 @@
 // The decayed values are two 16-bit parts each (v w = hi + lo with products
 // and residuals exact in packed 16-bit arithmetic), multiplied in turn, so a
 // state keeps 16 bits or more of each term; where a bf16 state is an output, a
-// third part makes them 24 (fp16: two make 22, and parts below 6e-8 vanish).
-// fp16 has not the range of a sum of products: its state's and its scores'
-// parts are scaled by a power of two each chunk.
+// third part makes them 24 (fp16: two make 22).  fp16 has not the range of a sum
+// of products: its values, scores and state are scaled by a power of two each
+// chunk.
 //
 // Few heads and many tokens: the tokens are cut into segments, a first kernel
 // (attn_segments: update products only) finds each segment's own contribution
@@ -443,8 +443,8 @@ struct State {
         e[rh][i + 3] = fmaf(e[rh][i + 3], decay, v.w);
       }
   }
-  // e = decay e + the update product in tensor memory (at: the thread's half)
-  __device__ __forceinline__ void add_update(uint32_t at, float decay) {
+  // e = decay e + f * the update product in tensor memory (at: the thread's half)
+  __device__ __forceinline__ void add_update(uint32_t at, float decay, float f) {
     constexpr int kRun = C::kSplit ? 16 : C::kCols / 2;  // registers of neighbouring columns
 #pragma unroll
     for (int rh = 0; rh < C::kRowHalves; ++rh)
@@ -453,20 +453,25 @@ struct State {
         float u[kRun];
         tmem_ld_rows(at + ((uint32_t)(16 * rh) << 16) + (j ? 64 : 0), u);
 #pragma unroll
-        for (int i = 0; i < kRun; ++i) e[rh][j + i] = fmaf(decay, e[rh][j + i], u[i]);
+        for (int i = 0; i < kRun; ++i) e[rh][j + i] = fmaf(decay, e[rh][j + i], f * u[i]);
       }
   }
 };
 
-// The decayed values of a chunk: piece i of this thread, hi and lo parts.
-// `at` is the power of the decay (0 for a place past the sequence, whose
-// values count as zero).
+// The decayed values of a chunk, hi and lo parts: a piece of 8 with its weight
+// in two parts (a place past the sequence counts as zeros), scaled up by f.
 template <typename T>
 __device__ __forceinline__ void split_piece(const unsigned char* values, int piece, bool live,
-                                            typename Pair<T>::type w, uint4& hi, uint4& lo) {
+                                            typename Pair<T>::type w, float f, uint4& hi, uint4& lo) {
   using T2 = typename Pair<T>::type;
   uint4 v = reinterpret_cast<const uint4*>(values)[piece];
   if (!live) v = make_uint4(0, 0, 0, 0);
+  if constexpr (std::is_same<T, __half>::value) {
+    const __half2 up = __float2half2_rn(f);
+    __half2* p = reinterpret_cast<__half2*>(&v);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) p[e] = __hmul2(p[e], up);
+  }
   const T2 w1 = T2(w.x, w.x), w2 = T2(w.y, w.y);
   const T2* vp = reinterpret_cast<const T2*>(&v);
   T2 *hp = reinterpret_cast<T2*>(&hi), *lp = reinterpret_cast<T2*>(&lo);
@@ -500,6 +505,26 @@ __device__ __forceinline__ int exponent_of_all(unsigned* slot, float m, int lane
   return all == 0u || all >= 0x7f800000u ? 0 : (int)(all >> 23) - 127 - to;
 }
 
+// fp16 keeps parts of a decayed value to 2^-25.  e for which 2^-e brings a
+// chunk's largest value to 2^14 .. 2^15 (no further up than 2^15, fp16's largest
+// power), so that they go by that value; the update product is 2^-e too large.
+template <int PIECES>
+__device__ __forceinline__ int values_exponent(unsigned* slot, const unsigned char* values, int n, int tid,
+                                               int threads) {
+  __half2 m = __float2half2_rn(0.0f);
+#pragma unroll
+  for (int i = 0; i < PIECES; ++i) {
+    const int piece = i * threads + tid;
+    uint4 v = reinterpret_cast<const uint4*>(values)[piece];
+    if (((piece >> 3) & 63) >= n) v = make_uint4(0, 0, 0, 0);
+    const __half2* p = reinterpret_cast<const __half2*>(&v);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) m = __hmax2(m, __habs2(p[e]));
+  }
+  const float most = fmaxf(__low2float(m), __high2float(m));
+  return min(max(exponent_of_all(slot, most, tid & 31, 14), -15), 0);
+}
+
 // Zero the places past the sequence's end in a tile of 128-byte rows.
 __device__ __forceinline__ void clear_rows(unsigned char* tile, int bytes, int n, int tid, int threads) {
   for (int i = tid; i < bytes / 16; i += threads)
@@ -527,7 +552,8 @@ __global__ void __launch_bounds__(Cfg<DA, DC>::kThreads, Cfg<DA, DC>::kSegBlocks
   uint64_t* bar = reinterpret_cast<uint64_t*>(sL + C::kCBytes);  // [2] loads, [1] update
   uint64_t* bar_u = bar + 2;
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bar + 3);
-  Decays<T>& decays = *reinterpret_cast<Decays<T>*>(bar + 4);
+  unsigned* top = reinterpret_cast<unsigned*>(bar + 4);  // [2] bits of the largest value (fp16)
+  Decays<T>& decays = *reinterpret_cast<Decays<T>*>(bar + 5);
   unsigned char* sT = sL + C::kCBytes + C::kTail;  // third parts, where there are any
 
   const int tid = threadIdx.x, warp = __shfl_sync(0xffffffffu, tid >> 5, 0), lane = tid & 31;
@@ -545,6 +571,7 @@ __global__ void __launch_bounds__(Cfg<DA, DC>::kThreads, Cfg<DA, DC>::kSegBlocks
   }
   if (tid == 0) {
     for (int i = 0; i < 3; ++i) mbar_init(&bar[i], 1);
+    top[0] = top[1] = 0u;
     fence_barrier_init();
   }
   __syncwarp();
@@ -585,6 +612,7 @@ __global__ void __launch_bounds__(Cfg<DA, DC>::kThreads, Cfg<DA, DC>::kSegBlocks
 
   const uint32_t t_upd = tmem + ((uint32_t)(quad * 32) << 16) + half * C::kStep;
   const bool third = !kHalf && r.s_out;
+  float back_last = 1.0f;
   int fail = 0, it = 0, n_last = 0;
   for (; it < n_chunks; ++it) {
     const int n = min(kChunk, at.len - at.start(it, rev));
@@ -596,12 +624,19 @@ __global__ void __launch_bounds__(Cfg<DA, DC>::kThreads, Cfg<DA, DC>::kSegBlocks
       __syncwarp();
     }
     fail |= wait_all(&bar[it & 1], (it >> 1) & 1);
+    float up = 1.0f, back = 1.0f;
+    if constexpr (kHalf) {
+      if (tid == 0) top[(it + 1) & 1] = 0u;
+      const int e = values_exponent<C::kCBytes / 16 / NT>(&top[it & 1], sC, n, tid, NT);
+      up = power_of_2(-e);
+      back = power_of_2(e);
+    }
 #pragma unroll
     for (int i = 0; i < C::kCBytes / 16 / NT; ++i) {
       const int piece = i * NT + tid, y = (piece >> 3) & 63;
       const int lag = max(0, rev ? y + 1 : n - y);
       uint4 hi, lo;
-      split_piece<T>(sC, piece, y < n, decays.parts[lag], hi, lo);
+      split_piece<T>(sC, piece, y < n, decays.parts[lag], up, hi, lo);
       reinterpret_cast<uint4*>(sW)[piece] = hi;
       reinterpret_cast<uint4*>(sL)[piece] = lo;
       if (third)
@@ -628,9 +663,10 @@ __global__ void __launch_bounds__(Cfg<DA, DC>::kThreads, Cfg<DA, DC>::kSegBlocks
     }
     if (it > 0) {
       gemm::tc_fence_after();
-      state.add_update(t_upd + ((it - 1) & 1) * DA, decays.of(n_last, rev));
+      state.add_update(t_upd + ((it - 1) & 1) * DA, decays.of(n_last, rev), back_last);
     }
     n_last = n;
+    back_last = back;
   }
   if (it < n_chunks) {  // a wait gave up: loads in flight land before the block may exit
     if (fail) record_status(g.status, kStatusTimeout);
@@ -641,7 +677,7 @@ __global__ void __launch_bounds__(Cfg<DA, DC>::kThreads, Cfg<DA, DC>::kSegBlocks
     if (n_chunks > 0) {
       if (wait_all(bar_u, (n_chunks - 1) & 1)) record_status(g.status, kStatusTimeout);
       gemm::tc_fence_after();
-      state.add_update(t_upd + ((n_chunks - 1) & 1) * DA, decays.of(n_last, rev));
+      state.add_update(t_upd + ((n_chunks - 1) & 1) * DA, decays.of(n_last, rev), back_last);
     }
     state.put_segment(seg0 + (size_t)(at.order + 1) * (DA * DC), tid);
   }
@@ -716,8 +752,9 @@ __global__ void __launch_bounds__(Cfg<DA, DC>::kThreads, Cfg<DA, DC>::kBlocksPer
            *bar_o = bar + 6, *bar_x = bar + 7, *bar_p = bar + 8;  // bar_b: one for each stage
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bar + 9);
   unsigned* top = reinterpret_cast<unsigned*>(bar + 10);   // [2] bits of the state's largest element
-  unsigned* peak = reinterpret_cast<unsigned*>(bar + 11);  // [2] and of the scores'
-  Decays<T>& decays = *reinterpret_cast<Decays<T>*>(bar + 12);
+  unsigned* peak = reinterpret_cast<unsigned*>(bar + 11);  // [2] of the scores'
+  unsigned* most = reinterpret_cast<unsigned*>(bar + 12);  // [2] and of the values'
+  Decays<T>& decays = *reinterpret_cast<Decays<T>*>(bar + 13);
 
   const int tid = threadIdx.x, warp = __shfl_sync(0xffffffffu, tid >> 5, 0), lane = tid & 31;
   const int quad = warp & 3, half = warp >> 2;
@@ -738,7 +775,7 @@ __global__ void __launch_bounds__(Cfg<DA, DC>::kThreads, Cfg<DA, DC>::kBlocksPer
   }
   if (tid == 0) {
     for (int i = 0; i < 9; ++i) mbar_init(&bar[i], 1);
-    top[0] = top[1] = peak[0] = peak[1] = 0u;
+    top[0] = top[1] = peak[0] = peak[1] = most[0] = most[1] = 0u;
     fence_barrier_init();
   }
   __syncwarp();
@@ -875,7 +912,7 @@ __global__ void __launch_bounds__(Cfg<DA, DC>::kThreads, Cfg<DA, DC>::kBlocksPer
     if (tid == 96) prefetch(it + 2);
 
     if (warp == 0) {
-      if (kHalf && lane == 0) top[(it + 1) & 1] = peak[(it + 1) & 1] = 0u;
+      if (kHalf && lane == 0) top[(it + 1) & 1] = peak[(it + 1) & 1] = most[(it + 1) & 1] = 0u;
       fail |= wait_all(bar_a, par);
       fail |= wait_all(bar_b + it % C::kBStages, (it / C::kBStages) & 1);
       gemm::tc_fence_after();
@@ -908,11 +945,17 @@ __global__ void __launch_bounds__(Cfg<DA, DC>::kThreads, Cfg<DA, DC>::kBlocksPer
     fail |= wait_all(bar_c, par);
     if (out_f32 && it > 0) fail |= wait_all(bar_p, (it - 1) & 1);  // the last output has left sO32
     constexpr int kPieces = C::kCBytes / 16 / NT;
+    float v_up = 1.0f, v_back = 1.0f;
+    if constexpr (kHalf) {
+      const int e = values_exponent<kPieces>(&most[par], sC, n, tid, NT);
+      v_up = power_of_2(-e);
+      v_back = power_of_2(e);
+    }
 #pragma unroll
     for (int i = 0; i < kPieces; ++i) {
       const int piece = i * NT + tid, y = (piece >> 3) & 63;
       uint4 high, low;
-      split_piece<T>(sC, piece, y < n, decays.parts[max(0, rev ? y + 1 : ex - y)], high, low);
+      split_piece<T>(sC, piece, y < n, decays.parts[max(0, rev ? y + 1 : ex - y)], v_up, high, low);
       reinterpret_cast<uint4*>(sW)[piece] = high;
       reinterpret_cast<uint4*>(sL)[piece] = low;
     }
@@ -1070,7 +1113,7 @@ __global__ void __launch_bounds__(Cfg<DA, DC>::kThreads, Cfg<DA, DC>::kBlocksPer
     }
     if (tid == 32 && more && third) load_a(it + 1);
     __syncwarp();
-    state.add_update(t_upd + t_quad + half * C::kStep, decays.of(ex, rev));
+    state.add_update(t_upd + t_quad + half * C::kStep, decays.of(ex, rev), v_back);
     if (more) put_state((it + 1) & 1);
     gemm::fence_async_smem();
     gemm::tc_fence_before();

@@ -107,3 +107,16 @@ def test_fp16_scores_far_below_the_state(small, cuda_device):
     c.k.mul_(small)
     c.state.mul_(2.0 ** 8)
     check(c, True)
+
+
+# Values and gradients near fp16's smallest, as those of a mean over many tokens are: what a decayed
+# value keeps in the state goes by the chunk's largest, not by fp16's last bit.
+@pytest.mark.parametrize("T", [150, 1300])
+@pytest.mark.parametrize("H,Hk,Dk,Dv", [(2, 2, 128, 128), (2, 1, 64, 64), (2, 2, 48, 120), (2, 2, 104, 64)])
+def test_fp16_small_values(T, H, Hk, Dk, Dv, cuda_device):
+    c = Case(cuda_device, 2, T, H, Hk, Dk, Dv, HF)
+    for x in (c.q, c.k):
+        x.mul_(16.0)
+    for x in (c.v, c.do):
+        x.mul_(2.0 ** -16)
+    check(c, False)
