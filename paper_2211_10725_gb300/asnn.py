@@ -105,7 +105,12 @@ class AttnSNN:
         self.ws_dense = [u8(snn.snn_dense_workspace_bytes(self.M, p.shape[1], p.shape[0]))
                          for p in self.weights.parts]
         self.ws_loss = u8(snn.snn_rate_ce_workspace_bytes(B))
-        self._token = None
+        # single steps after a prompt: layers of one step, and the membrane
+        # potentials that they go on from (here, so that prompt and token
+        # allocate and initialise nothing and run on any stream)
+        self._token = {"scans": [self._scan(1, B, S + N, "asnn_token") for _ in range(w.blocks)],
+                       "readout": self._scan(1, B, self.n_out, "asnn_token_out")}
+        self.mem = [torch.zeros_like(sc.mem_final) for sc in [*self.scans, self.readout]]
 
     def _scan(self, T, B, n, name):
         w = self.w
@@ -240,14 +245,12 @@ class AttnSNN:
         returns the readout's spikes [T, B, n_classes]."""
         for _, call in self._forward_ops(X, stream, True):
             call()
-        if self._token is None:
-            one = self.w.scaled(T=1)
-            self._token = {"scans": [self._scan(1, one.B, one.spikes + one.width, "asnn_token")
-                                     for _ in range(one.blocks)],
-                           "readout": self._scan(1, one.B, self.n_out, "asnn_token_out")}
-        layers = [*self.scans, self.readout]
-        self.mem = [sc.mem_final.clone() for sc in layers]
+        self._on(stream, self._keep_mem)
         return self.readout.spk[..., :self.w.n_classes]
+
+    def _keep_mem(self):
+        for mem, sc in zip(self.mem, [*self.scans, self.readout]):
+            mem.copy_(sc.mem_final)
 
     def token(self, x, stream=None):
         """One more step x [B, n_in] of every sequence after `prompt`: the

@@ -53,3 +53,34 @@ def test_parameters_share_one_buffer_each():
     assert torch.equal(net.weights.parts[0], W.make_attn_inputs(w)["W"][0])
     assert net.weights.parts[-1].shape == (16, w.width)
     assert torch.count_nonzero(net.weights.parts[-1][w.n_classes:]) == 0
+
+
+class _Queue:
+    """A stream whose work waits until something torch does is ordered behind it."""
+
+    def __init__(self):
+        self.work = []
+
+    def __enter__(self):      # torch.cuda.stream(queue): torch's calls come after what is queued
+        for call in self.work:
+            call()
+        self.work = []
+
+    def __exit__(self, *exc):
+        pass
+
+
+def test_a_prompt_on_a_stream_keeps_what_that_stream_computes(monkeypatch):
+    w, net = _net()
+    for name in ("snn_dense_layer_fwd", "snn_block_norm_fwd", "snn_leaky_attn_fwd"):
+        monkeypatch.setattr(snn, name, lambda *a, **k: None)
+    monkeypatch.setattr(snn.ScanLayer, "forward", lambda self, *a, stream=None, **k: stream.work.append(
+        lambda: self.mem_final.fill_(7.0)))
+    monkeypatch.setattr(torch.cuda, "stream", lambda s: s)
+    allocated = []
+    monkeypatch.setattr(snn, "snn_workspace_init", lambda *a, **k: allocated.append(a))
+    net.prompt(torch.zeros(w.T * w.B, w.n_in, dtype=torch.bfloat16), stream=_Queue())
+    assert len(net.mem) == w.blocks + 1
+    for mem in net.mem:
+        assert torch.all(mem == 7.0)
+    assert not allocated       # nothing is set up on a stream that is not the caller's

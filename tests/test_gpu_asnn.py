@@ -160,3 +160,27 @@ def test_training_lowers_the_loss_and_graph_replays(cuda_device):
 def test_head_decays_are_a_schedule():
     d = head_decays(4)
     assert torch.equal(d, torch.tensor([1 - 1 / 8, 1 - 1 / 16, 1 - 1 / 32, 1 - 1 / 64]))
+
+
+def test_prompt_and_tokens_on_a_side_stream(cuda_device):
+    """On a stream that is kept busy first, with nothing else waiting for it."""
+    w = SMALL
+    n = w.T - 2
+    inp = W.make_attn_inputs(w)
+    x = inp["X"].to(cuda_device)
+    outs = []
+    for side in (None, torch.cuda.Stream()):
+        net = AttnSNN(w.scaled(T=n), inp["W"], device=cuda_device)
+        big = torch.randn(8192, 8192, device=cuda_device)
+        torch.cuda.synchronize()
+        if side is not None:
+            with torch.cuda.stream(side):
+                for _ in range(8):
+                    big = big @ big
+        net.prompt(x[:n].reshape(-1, w.n_in).contiguous(), stream=side)
+        for t in range(n, w.T):
+            net.token(x[t], stream=side)
+        torch.cuda.synchronize()
+        outs.append([*(t.clone() for t in net.mem), *(t.clone() for t in net.state),
+                     *(t.clone() for t in net.token_o)])
+    assert all(torch.equal(a, b) for a, b in zip(*outs))
