@@ -570,7 +570,7 @@ def snn_leaky_attn_fwd(q, k, v, beta, o, ws, scale=1.0, seq_lens=None, state_in=
     range: no state).  ws: snn_leaky_attn_workspace_bytes of the shape."""
     w = "snn_leaky_attn_fwd"
     (B, T, H, Dk), Hk, Dv, dt = q.shape, k.shape[2], v.shape[-1], q.dtype
-    d = _attn_desc(w, B, T, H, Hk, Dk, Dv, dt, scale)
+    d = _attn_desc(w, B, T, H, Hk, Dk, Dv, dt, float(scale))
     if state_in is not None and state_out is not None and len(state_in) != len(state_out):
         raise ValueError(f"{w}: state_in and state_out differ in places")
     ps, n = _state_places(w, slots, B, (state_in, state_out))
@@ -592,7 +592,7 @@ def snn_leaky_attn_bwd(q, k, v, beta, grad_o, grad_q, grad_k, grad_v, ws, scale=
     order); ws: snn_leaky_attn_workspace_bytes(..., backward=True)."""
     w = "snn_leaky_attn_bwd"
     (B, T, H, Dk), Hk, Dv, dt = q.shape, k.shape[2], v.shape[-1], q.dtype
-    d = _attn_desc(w, B, T, H, Hk, Dk, Dv, dt, scale)
+    d = _attn_desc(w, B, T, H, Hk, Dk, Dv, dt, float(scale))
     qs, ks, vs, os = (B, T, H, Dk), (B, T, Hk, Dk), (B, T, Hk, Dv), (B, T, H, Dv)
     array, (pq, pk, pv, po, gq, gk, gv) = _places(
         _bthd(w, "q", q, qs, dt) + _bthd(w, "k", k, ks, dt) + _bthd(w, "v", v, vs, dt)
@@ -613,7 +613,7 @@ def snn_leaky_attn_step(q, k, v, beta, state, o, scale=1.0, slots=None, stream=N
     the batch, whose o is zero)."""
     w = "snn_leaky_attn_step"
     (B, H, Dk), Hk, Dv, dt = q.shape, k.shape[1], v.shape[-1], q.dtype
-    d = _attn_desc(w, B, 1, H, Hk, Dk, Dv, dt, scale)
+    d = _attn_desc(w, B, 1, H, Hk, Dk, Dv, dt, float(scale))
     n = state.shape[0]
     array, (pq, pk, pv, po) = _places(
         _bthd(w, "q", q, (B, H, Dk), dt) + _bthd(w, "k", k, (B, Hk, Dk), dt)
@@ -649,7 +649,7 @@ def snn_block_norm_fwd(r, a, z, w_post, res_scale, w_pre, r_out, y, eps=1e-6, gr
     w = "snn_block_norm_fwd"
     shape, res = r.shape, r.dtype
     io = a.dtype if a is not None else y.dtype if y is not None else res
-    d = _norm_desc(w, *shape, group, io, res, gate, eps)
+    d = _norm_desc(w, *shape, int(group), io, res, gate, float(eps))
     array, (pr, pa, pz, po, py) = _places(
         _rows(w, "r", r, shape, res) + _rows(w, "a", a, shape, io) + _rows(w, "z", z, shape, io)
         + _rows(w, "r_out", r_out, shape, res) + _rows(w, "y", y, shape, io), 2)
@@ -670,7 +670,7 @@ def snn_block_norm_bwd(r_out, a, z, w_post, res_scale, w_pre, grad_r_out, grad_y
     of = r_out if r_out is not None else grad_r_out
     shape, res = of.shape, of.dtype
     io = a.dtype if a is not None else grad_y.dtype if grad_y is not None else res
-    d = _norm_desc(w, *shape, group, io, res, gate, eps)
+    d = _norm_desc(w, *shape, int(group), io, res, gate, float(eps))
     array, (pr, pa, pz, gro, gy, gr, ga, gz) = _places(
         _rows(w, "r_out", r_out, shape, res) + _rows(w, "a", a, shape, io)
         + _rows(w, "z", z, shape, io) + _rows(w, "grad_r_out", grad_r_out, shape, res)

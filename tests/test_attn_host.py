@@ -264,3 +264,41 @@ def test_attention_backward_refuses_a_state_written_while_it_is_read(lib):
         BIG, None)
     assert call(64, None, 64) == INVALID
     assert call(None, 64, 64) == INVALID
+
+
+class _Library:
+    """Keeps what the binding hands to a call."""
+
+    def __init__(self):
+        self.seen = []
+
+    def __getattr__(self, name):
+        def call(desc, *args):
+            d = desc._obj
+            self.seen.append(d.scale if isinstance(d, snn.AttnDesc) else d.eps)
+            return 0
+        return call
+
+
+def test_a_scale_or_eps_that_is_a_tensor_is_read_at_each_call(monkeypatch):
+    """A learned or scheduled scalar, changed in place between calls."""
+    import torch
+    lib = _Library()
+    monkeypatch.setattr(snn, "load_library", lambda: lib)
+    monkeypatch.setattr(snn, "_bthd", lambda *a: (16, 8, 8, 8))
+    monkeypatch.setattr(snn, "_rows", lambda *a: (16, 8))
+    monkeypatch.setattr(snn, "_flat", lambda *a: 16)
+    monkeypatch.setattr(snn, "_stream", lambda s: None)
+    x, ws = torch.zeros(1, 1, 1, 8, dtype=torch.bfloat16), torch.zeros(256, dtype=torch.uint8)
+    row, value = torch.zeros(1, 8), torch.tensor(0.5)
+    calls = [lambda: snn.snn_leaky_attn_fwd(x, x, x, None, x, ws, scale=value),
+             lambda: snn.snn_leaky_attn_bwd(x, x, x, None, x, x, x, x, ws, scale=value),
+             lambda: snn.snn_leaky_attn_step(x[0], x[0], x[0], None, x, x[0], scale=value),
+             lambda: snn.snn_block_norm_fwd(row, None, None, None, None, None, None, row, eps=value),
+             lambda: snn.snn_block_norm_bwd(row, None, None, None, None, None, row, None, row, None, None, None,
+                                            None, None, ws, eps=value)]
+    for call in calls:
+        for want in (0.5, 0.25):
+            value.fill_(want)
+            call()
+            assert lib.seen[-1] == want
