@@ -96,7 +96,9 @@ def leaky_attention(q, k, v, beta, state=None, scale=1.0, seq_lens=None):
     + k_t v_t^T and o_t = scale S_t^T q_t: q [B, T, H, Dk], k [B, T, Hk, Dk], v
     [B, T, Hk, Dv] (bf16 or fp16), state fp32 [B, H, Dk, Dv] or None.
     Differentiable in q, k, v and state; beta (fp32 [H]) is a fixed schedule
-    over the heads."""
+    over the heads, and one that wants a gradient is refused."""
+    if beta.requires_grad and torch.is_grad_enabled():
+        raise ValueError("leaky_attention: beta is a fixed schedule and has no gradient")
     return _AttentionFunction.apply(q, k, v, beta, state, float(scale), seq_lens)
 
 
