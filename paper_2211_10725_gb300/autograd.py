@@ -9,11 +9,13 @@ or v as a fourth tensor and return its gradient as well.  Only the spike
 output is differentiable; the membrane trace is not returned.
 
 ``leaky_attention`` and ``block_norm`` wrap the two operators of a residual
-block of a sequence network in the same way.
+block of a sequence network in the same way; their gradients have none of
+their own (asked for, they raise).
 """
 from __future__ import annotations
 
 import torch
+from torch.autograd.function import once_differentiable
 
 from . import snn
 from . import workloads as W
@@ -73,6 +75,7 @@ class _AttentionFunction(torch.autograd.Function):
         return o, end
 
     @staticmethod
+    @once_differentiable
     def backward(ctx, grad_o, grad_end):
         q, k, v, beta, state, seq_lens = ctx.saved_tensors
         B, T, H, Dk = q.shape
@@ -117,6 +120,7 @@ class _BlockNormFunction(torch.autograd.Function):
         return r_out.view(shape), None if y is None else y.view(shape)
 
     @staticmethod
+    @once_differentiable
     def backward(ctx, grad_r, grad_y):
         r_out, a, z, w_post, res_scale, w_pre = ctx.saved_tensors
         M, N = r_out.shape

@@ -49,3 +49,18 @@ def test_a_decay_that_wants_a_gradient_is_refused(calls):
         autograd.leaky_attention(*_qkv(), beta)
     autograd.leaky_attention(*_qkv(), beta.detach())
     assert len(calls.seen) == 2
+
+
+def _rows(M=3, N=24, dtype=torch.float32):
+    return torch.randn(M, N).to(dtype).requires_grad_()
+
+
+def test_second_derivatives_are_refused(calls):
+    """Not given as zero: a gradient penalty would go unnoticed."""
+    q, k, v = _qkv()
+    r = _rows()
+    for out, x in ((autograd.leaky_attention(q, k, v, torch.full((4,), 0.9))[0], q),
+                   (autograd.block_norm(r, _rows(), w_pre=torch.ones(24))[1], r)):
+        g, = torch.autograd.grad(out.float().square().sum(), x, create_graph=True)
+        with pytest.raises(RuntimeError, match="twice"):
+            g.float().square().sum().backward()
