@@ -59,9 +59,47 @@ def scan(I, beta, thr, w: W.ScanWorkload, third=None):
     return _ScanFunction.apply(I, beta, thr, third, w)
 
 
+def _starts(t):
+    """Whether t starts on the 16-byte boundary that the library wants."""
+    return t.data_ptr() % 16 == 0
+
+
+def _copied(t):
+    """A contiguous copy, on a boundary of its own."""
+    return torch.empty(t.shape, dtype=t.dtype, device=t.device).copy_(t)
+
+
+def _whole(t):
+    """t contiguous and on a boundary (or None)."""
+    return t if t is None or (t.is_contiguous() and _starts(t)) else _copied(t)
+
+
+def _tokens(t):
+    """A [B, T, heads, D] tensor as the library reads it in place, or a copy: D
+    contiguous, the other steps positive multiples of 8."""
+    n, st = t.shape, t.stride()
+    ok = _starts(t) and (n[3] == 1 or st[3] == 1) and all(
+        n[i] <= 1 or (st[i] > 0 and st[i] % 8 == 0) for i in range(3))
+    return t if ok else _copied(t)
+
+
+def _matrix(t, N, group, dtype=None):
+    """t as rows of N, as the library reads them in place, or a copy (or None);
+    with groups the rows have to be whole vectors apart."""
+    if t is None:
+        return None
+    t = (t if dtype is None else t.to(dtype)).reshape(-1, N)
+    step = t.stride(0)
+    ok = _starts(t) and (N == 1 or t.stride(1) == 1) and (
+        t.shape[0] <= 1 or (step >= N and (step % 8 == 0 or group in (0, N))))
+    return t if ok else _copied(t)
+
+
 class _AttentionFunction(torch.autograd.Function):
     @staticmethod
     def forward(ctx, q, k, v, beta, state, scale, seq_lens):
+        q, k, v = _tokens(q), _tokens(k), _tokens(v)
+        beta, state, seq_lens = _whole(beta), _whole(state), _whole(seq_lens)
         B, T, H, Dk = q.shape
         Hk, Dv = k.shape[2], v.shape[-1]
         o = torch.empty((B, T, H, Dv), dtype=q.dtype, device=q.device)
@@ -86,10 +124,10 @@ class _AttentionFunction(torch.autograd.Function):
         ws = torch.zeros(snn.snn_leaky_attn_workspace_bytes(B, T, H, Hk, Dk, Dv, backward=True),
                          dtype=torch.uint8, device=q.device)
         grad_o = torch.zeros((B, T, H, Dv), dtype=q.dtype, device=q.device) if grad_o is None \
-            else grad_o.to(q.dtype).contiguous()
+            else _tokens(grad_o.to(q.dtype))
         snn.snn_leaky_attn_bwd(q, k, v, beta, grad_o, gq, gk, gv, ws, scale=ctx.scale,
                                seq_lens=seq_lens, state_in=state,
-                               grad_state_out=None if grad_end is None else grad_end.contiguous(),
+                               grad_state_out=_whole(grad_end),
                                grad_state_in=gs)
         return gq, gk, gv, None, gs, None, None
 
@@ -109,9 +147,9 @@ class _BlockNormFunction(torch.autograd.Function):
     @staticmethod
     def forward(ctx, r, a, z, w_post, res_scale, w_pre, eps, group, gate):
         shape = r.shape
-        flat = lambda t: None if t is None else t.reshape(-1, shape[-1])
-        r2, a2, z2 = flat(r), flat(a), flat(z)
-        r_out = torch.empty_like(r2)
+        r2, a2, z2 = (_matrix(t, shape[-1], group) for t in (r, a, z))
+        w_post, res_scale, w_pre = _whole(w_post), _whole(res_scale), _whole(w_pre)
+        r_out = torch.empty(r2.shape, dtype=r.dtype, device=r.device)
         y = torch.empty(r2.shape, dtype=a.dtype, device=a.device) if w_pre is not None else None
         snn.snn_block_norm_fwd(r2, a2, z2, w_post, res_scale, w_pre, r_out, y, eps=eps, group=group,
                                gate=gate)
@@ -124,8 +162,8 @@ class _BlockNormFunction(torch.autograd.Function):
     def backward(ctx, grad_r, grad_y):
         r_out, a, z, w_post, res_scale, w_pre = ctx.saved_tensors
         M, N = r_out.shape
-        flat = lambda t, like: None if t is None else t.to(like).reshape(M, N).contiguous()
-        grad_r, grad_y = flat(grad_r, r_out.dtype), flat(grad_y, a.dtype)
+        group = ctx.opts["group"]
+        grad_r, grad_y = _matrix(grad_r, N, group, r_out.dtype), _matrix(grad_y, N, group, a.dtype)
         if grad_r is None and grad_y is None:
             return (None,) * 9
         like = lambda t: None if t is None else torch.empty(t.shape, dtype=t.dtype, device=t.device)

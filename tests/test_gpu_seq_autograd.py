@@ -52,3 +52,32 @@ def test_block_norm_gradients_are_the_abi_s(cuda_device):
                            flat(gy), *out, ws, eps=1e-6, group=32, gate="silu")
     for t, want in zip((r, a, z, wp, sc, pre), out):
         assert torch.equal(t.grad.reshape(want.shape), want)
+
+
+def test_other_layouts_give_the_same_bits(cuda_device):
+    """Odd fp32 rows whose gradient is a part of torch.cat's, and attention on broadcast keys and
+    shifted values: as with contiguous tensors."""
+    g = torch.Generator().manual_seed(4)
+    rnd = lambda *s: torch.randn(s, generator=g).to(cuda_device)
+    r, a, w, up = rnd(3, 1001), rnd(3, 1001), rnd(1001), rnd(4, 1001)
+    grads = []
+    for first in (0, 1):
+        x = [t.clone().requires_grad_() for t in (r, a, w)]
+        out, y = block_norm(x[0], x[1], w_pre=x[2])
+        y = torch.cat([torch.zeros(first, 1001, device=cuda_device, requires_grad=True), y])
+        torch.autograd.backward([out, y], [up[1:], up[1 - first:]])
+        grads.append([t.grad for t in x])
+    assert all(torch.equal(s, t) for s, t in zip(*grads))
+    B, T, H, D = 2, 70, 2, 64
+    q, k1, v1 = (rnd(*s).to(torch.bfloat16) for s in ((B, T, H, D), (1, T, H, D), (B * T * H * D + 3,)))
+    beta, do = torch.tensor([0.9, 1.0], device=cuda_device), rnd(B, T, H, D).to(torch.bfloat16)
+    results = []
+    for copied in (False, True):
+        k, v = k1.expand(B, T, H, D), v1[3:].view(B, T, H, D)
+        if copied:
+            k, v = k.contiguous(), v.clone()
+        x = [t.detach().requires_grad_() for t in (q, k, v)]
+        o, end = leaky_attention(*x, beta)
+        o.backward(do)
+        results.append([o.detach(), end.detach(), *(t.grad for t in x)])
+    assert all(torch.equal(s, t) for s, t in zip(*results))

@@ -64,3 +64,59 @@ def test_second_derivatives_are_refused(calls):
         g, = torch.autograd.grad(out.float().square().sum(), x, create_graph=True)
         with pytest.raises(RuntimeError, match="twice"):
             g.float().square().sum().backward()
+
+
+def _library_takes(name, t):
+    """The C ABI's rules on one tensor: 16-byte start; strides of [B, T, heads, D] positive multiples
+    of 8, of rows at least their length; the rest contiguous."""
+    if t.numel() == 0:
+        return True
+    if t.data_ptr() % 16:
+        return False
+    steps = [s for n, s in zip(t.shape, t.stride()) if n > 1]
+    if t.dim() == 4 and t.dtype != torch.float32:
+        return t.stride(-1) == 1 and all(s > 0 and s % 8 == 0 for s in steps[:-1])
+    if t.dim() == 2:
+        return (t.shape[1] == 1 or t.stride(1) == 1) and (t.shape[0] == 1 or t.stride(0) >= t.shape[1])
+    return t.is_contiguous()
+
+
+def test_attention_inputs_of_any_layout(calls):
+    """Broadcast sequences, another order of dimensions, parts that start or step off 16 bytes."""
+    B, T, H, D = 2, 6, 4, 16
+    bf = lambda *s: torch.randn(*s).to(torch.bfloat16)
+    layouts = [bf(B, T, H, D), bf(1, T, H, D).expand(B, T, H, D), bf(B, T, 1, D).expand(B, T, H, D),
+               bf(B, T, D, H).transpose(2, 3), bf(B * T * H * D + 3)[3:].view(B, T, H, D),
+               bf(B, T, H * D + 4)[..., 4:].unflatten(-1, (H, D)), bf(B, T, H, 2 * D)[..., ::2]]
+    beta, lens = torch.rand(H + 1)[1:], torch.tensor([9, 6, 3], dtype=torch.int32)[1:]
+    state = torch.randn(B, H, D, D).transpose(2, 3)
+    for x in layouts:
+        q, k, v, s = (t.detach().requires_grad_() for t in (x, x, x, state))
+        o, end = autograd.leaky_attention(q, k, v, beta, s, seq_lens=lens)
+        torch.autograd.backward([o, end], [bf(B * T * H * D + 1)[1:].view(B, T, H, D),
+                                           torch.randn(B, H, D, D).transpose(2, 3)])
+    assert len(calls.seen) == 2 * len(layouts)
+    for name, t in calls.tensors():
+        assert _library_takes(name, t), (name, t.shape, t.stride(), t.data_ptr() % 16)
+
+
+@pytest.mark.parametrize("group", [0, 8])
+def test_norm_inputs_and_gradients_of_any_layout(group, calls):
+    """Odd rows whose gradient is a part of another tensor (as torch.cat hands back), broadcast and
+    transposed rows, parameters inside a longer vector."""
+    M, N = 3, 24 if group else 9
+    f = torch.randn
+    layouts = [f(M, N), f(1, N).expand(M, N), f(N, M).t(), f(M * N + 1)[1:].view(M, N), f(M, 2 * N)[:, ::2],
+               f(M, N + 3)[:, :N]]
+    for x in layouts:
+        par = [f(N + 1)[1:].requires_grad_() for _ in range(3)]
+        r, a, z = (x.detach().requires_grad_() for _ in range(3))
+        out = autograd.block_norm(r, a, z, *par, group=group, gate="silu")
+        other = torch.randn(1, N, requires_grad=True)
+        joined = [torch.cat([other, t]) for t in out]
+        torch.autograd.backward(joined, [f(M + 1, N) for _ in joined])
+    assert len(calls.seen) == 2 * len(layouts)
+    for name, t in calls.tensors():
+        assert _library_takes(name, t), (name, t.shape, t.stride(), t.data_ptr() % 16)
+        if group and t.dim() == 2:     # groups are for rows of whole vectors
+            assert t.stride(0) % 8 == 0
