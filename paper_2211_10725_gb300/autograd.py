@@ -140,6 +140,8 @@ def leaky_attention(q, k, v, beta, state=None, scale=1.0, seq_lens=None):
     over the heads, and one that wants a gradient is refused."""
     if beta.requires_grad and torch.is_grad_enabled():
         raise ValueError("leaky_attention: beta is a fixed schedule and has no gradient")
+    if any(t.dim() != 4 for t in (q, k, v)):
+        raise ValueError("leaky_attention: q, k and v must be of shape [B, T, heads, D]")
     return _AttentionFunction.apply(q, k, v, beta, state, float(scale), seq_lens)
 
 
@@ -181,5 +183,11 @@ def block_norm(r, a, z=None, w_post=None, res_scale=None, w_pre=None, eps=1e-6, 
                gate="none"):
     """(r', y): r' = r + res_scale * norm(a) w_post * act(z) and y = norm(r')
     w_pre (None without w_pre) over the last dimension, the norm of a per
-    `group` channels.  Differentiable in all the tensors."""
+    `group` channels.  r, a and z have one shape.  Differentiable in all the
+    tensors.  (The norm of r alone, without a block before it:
+    snn.snn_block_norm_fwd and snn_block_norm_bwd.)"""
+    if a is None:
+        raise ValueError("block_norm: needs a; snn.snn_block_norm_fwd takes the norm of r alone")
+    if a.shape != r.shape or (z is not None and z.shape != r.shape):
+        raise ValueError("block_norm: r, a and z must have one shape")
     return _BlockNormFunction.apply(r, a, z, w_post, res_scale, w_pre, eps, group, gate)

@@ -120,3 +120,18 @@ def test_norm_inputs_and_gradients_of_any_layout(group, calls):
         assert _library_takes(name, t), (name, t.shape, t.stride(), t.data_ptr() % 16)
         if group and t.dim() == 2:     # groups are for rows of whole vectors
             assert t.stride(0) % 8 == 0
+
+
+def test_shapes_that_do_not_match_are_refused(calls):
+    """As many elements in another order are not the same rows."""
+    r = torch.randn(2, 5, 16)
+    for a, z in ((torch.randn(5, 2, 16), None), (torch.randn(2, 10, 8), None), (torch.randn(10, 16), None),
+                 (torch.randn(2, 5, 16), torch.randn(5, 2, 16))):
+        with pytest.raises(ValueError, match="shape"):
+            autograd.block_norm(r, a, z, w_pre=torch.ones(16), gate="none" if z is None else "silu")
+    q, k, v = _qkv()
+    with pytest.raises(ValueError, match="shape"):
+        autograd.leaky_attention(q[0], k[0], v[0], torch.full((4,), 0.9))
+    with pytest.raises(ValueError, match="needs a"):
+        autograd.block_norm(r, None, w_pre=torch.ones(16))
+    assert not calls.seen
