@@ -95,6 +95,15 @@ def _matrix(t, N, group, dtype=None):
     return t if ok else _copied(t)
 
 
+def _attention_workspace(q, *shape, backward=False):
+    """A call's workspace: zero where its status word is, the rest is written
+    before it is read."""
+    ws = torch.empty(snn.snn_leaky_attn_workspace_bytes(*shape, backward=backward), dtype=torch.uint8,
+                     device=q.device)
+    ws[:256].zero_()
+    return ws
+
+
 class _AttentionFunction(torch.autograd.Function):
     @staticmethod
     def forward(ctx, q, k, v, beta, state, scale, seq_lens):
@@ -104,8 +113,7 @@ class _AttentionFunction(torch.autograd.Function):
         Hk, Dv = k.shape[2], v.shape[-1]
         o = torch.empty((B, T, H, Dv), dtype=q.dtype, device=q.device)
         end = torch.empty((B, H, Dk, Dv), dtype=torch.float32, device=q.device)
-        ws = torch.zeros(snn.snn_leaky_attn_workspace_bytes(B, T, H, Hk, Dk, Dv),
-                         dtype=torch.uint8, device=q.device)
+        ws = _attention_workspace(q, B, T, H, Hk, Dk, Dv)
         snn.snn_leaky_attn_fwd(q, k, v, beta, o, ws, scale=scale, seq_lens=seq_lens,
                                state_in=state, state_out=end)
         ctx.save_for_backward(q, k, v, beta, state, seq_lens)
@@ -121,8 +129,7 @@ class _AttentionFunction(torch.autograd.Function):
         gq, gk, gv = (torch.empty(x.shape, dtype=q.dtype, device=q.device) for x in (q, k, v))
         gs = torch.empty((B, H, Dk, Dv), dtype=torch.float32, device=q.device) \
             if state is not None and ctx.needs_input_grad[4] else None
-        ws = torch.zeros(snn.snn_leaky_attn_workspace_bytes(B, T, H, Hk, Dk, Dv, backward=True),
-                         dtype=torch.uint8, device=q.device)
+        ws = _attention_workspace(q, B, T, H, Hk, Dk, Dv, backward=True)
         grad_o = torch.zeros((B, T, H, Dv), dtype=q.dtype, device=q.device) if grad_o is None \
             else _tokens(grad_o.to(q.dtype))
         snn.snn_leaky_attn_bwd(q, k, v, beta, grad_o, gq, gk, gv, ws, scale=ctx.scale,

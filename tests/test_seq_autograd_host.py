@@ -135,3 +135,21 @@ def test_shapes_that_do_not_match_are_refused(calls):
     with pytest.raises(ValueError, match="needs a"):
         autograd.block_norm(r, None, w_pre=torch.ones(16))
     assert not calls.seen
+
+
+def test_attention_zeroes_the_status_word_alone(calls, monkeypatch):
+    """Workspaces hold segment states and shared heads' sums, which kernels write before they read."""
+    empty = torch.empty
+
+    def dirty(*a, **k):
+        t = empty(*a, **k)
+        return t.fill_(0xA5) if t.dtype == torch.uint8 else t
+    monkeypatch.setattr(torch, "empty", dirty)
+    q, k, v = _qkv(T=200)
+    o, _ = autograd.leaky_attention(q, k, v, torch.full((4,), 0.9))
+    o.sum().backward()
+    for name, args, kw in calls.seen:
+        ws = next(t for t in args if isinstance(t, torch.Tensor) and t.dtype == torch.uint8)
+        assert torch.count_nonzero(ws[:256]) == 0
+        assert ws.numel() == 256 or (ws[256:] == 0xA5).all()
+    assert any(next(t for t in args if t.dtype == torch.uint8).numel() > 256 for _, args, _ in calls.seen)
