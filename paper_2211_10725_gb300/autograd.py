@@ -118,6 +118,7 @@ class _AttentionFunction(torch.autograd.Function):
                                state_in=state, state_out=end)
         ctx.save_for_backward(q, k, v, beta, state, seq_lens)
         ctx.scale = scale
+        ctx.set_materialize_grads(False)
         return o, end
 
     @staticmethod
@@ -164,6 +165,7 @@ class _BlockNormFunction(torch.autograd.Function):
                                gate=gate)
         ctx.save_for_backward(r_out, a2, z2, w_post, res_scale, w_pre)
         ctx.opts, ctx.shape = dict(eps=eps, group=group, gate=gate), shape
+        ctx.set_materialize_grads(False)
         return r_out.view(shape), None if y is None else y.view(shape)
 
     @staticmethod

@@ -153,3 +153,13 @@ def test_attention_zeroes_the_status_word_alone(calls, monkeypatch):
         assert torch.count_nonzero(ws[:256]) == 0
         assert ws.numel() == 256 or (ws[256:] == 0xA5).all()
     assert any(next(t for t in args if t.dtype == torch.uint8).numel() > 256 for _, args, _ in calls.seen)
+
+
+def test_outputs_that_nothing_uses_bring_no_gradients(calls):
+    q, k, v = _qkv()
+    o, end = autograd.leaky_attention(q, k, v, torch.full((4,), 0.9))
+    o.sum().backward()
+    assert calls.seen[-1][2]["grad_state_out"] is None
+    r = _rows()
+    autograd.block_norm(r, _rows(), w_pre=torch.ones(24))[1].sum().backward()
+    assert calls.seen[-1][1][6] is None and calls.seen[-1][1][7] is not None   # grad_r_out, grad_y
