@@ -104,9 +104,15 @@ def _attention_workspace(q, *shape, backward=False):
     return ws
 
 
+def _keep_status(status, ws):
+    """What a call left in its workspace's status word, into the caller's."""
+    if status is not None:
+        torch.maximum(status, ws[:4].view(torch.int32), out=status)
+
+
 class _AttentionFunction(torch.autograd.Function):
     @staticmethod
-    def forward(ctx, q, k, v, beta, state, scale, seq_lens):
+    def forward(ctx, q, k, v, beta, state, scale, seq_lens, status):
         q, k, v = _tokens(q), _tokens(k), _tokens(v)
         beta, state, seq_lens = _whole(beta), _whole(state), _whole(seq_lens)
         B, T, H, Dk = q.shape
@@ -117,7 +123,8 @@ class _AttentionFunction(torch.autograd.Function):
         snn.snn_leaky_attn_fwd(q, k, v, beta, o, ws, scale=scale, seq_lens=seq_lens,
                                state_in=state, state_out=end)
         ctx.save_for_backward(q, k, v, beta, state, seq_lens)
-        ctx.scale = scale
+        _keep_status(status, ws)
+        ctx.scale, ctx.status = scale, status
         ctx.set_materialize_grads(False)
         return o, end
 
@@ -137,20 +144,26 @@ class _AttentionFunction(torch.autograd.Function):
                                seq_lens=seq_lens, state_in=state,
                                grad_state_out=_whole(grad_end),
                                grad_state_in=gs)
-        return gq, gk, gv, None, gs, None, None
+        _keep_status(ctx.status, ws)
+        return gq, gk, gv, None, gs, None, None, None
 
 
-def leaky_attention(q, k, v, beta, state=None, scale=1.0, seq_lens=None):
+def leaky_attention(q, k, v, beta, state=None, scale=1.0, seq_lens=None, status=None):
     """(o, state after the last token) of leaky attention, S_t = beta_h S_{t-1}
     + k_t v_t^T and o_t = scale S_t^T q_t: q [B, T, H, Dk], k [B, T, Hk, Dk], v
     [B, T, Hk, Dv] (bf16 or fp16), state fp32 [B, H, Dk, Dv] or None.
     Differentiable in q, k, v and state; beta (fp32 [H]) is a fixed schedule
-    over the heads, and one that wants a gradient is refused."""
+    over the heads, and one that wants a gradient is refused.
+    status: an int32 tensor [1] on the same device, 0 before.  A kernel of the
+    call or of its backward that gave up on a wait (its results are undefined
+    then) leaves SNN_ERR_TIMEOUT there until the caller clears it."""
     if beta.requires_grad and torch.is_grad_enabled():
         raise ValueError("leaky_attention: beta is a fixed schedule and has no gradient")
     if any(t.dim() != 4 for t in (q, k, v)):
         raise ValueError("leaky_attention: q, k and v must be of shape [B, T, heads, D]")
-    return _AttentionFunction.apply(q, k, v, beta, state, float(scale), seq_lens)
+    if status is not None and (status.shape != (1,) or status.dtype != torch.int32):
+        raise ValueError("leaky_attention: status must be an int32 tensor of shape [1]")
+    return _AttentionFunction.apply(q, k, v, beta, state, float(scale), seq_lens, status)
 
 
 class _BlockNormFunction(torch.autograd.Function):

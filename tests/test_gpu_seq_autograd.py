@@ -81,3 +81,14 @@ def test_other_layouts_give_the_same_bits(cuda_device):
         o.backward(do)
         results.append([o.detach(), end.detach(), *(t.grad for t in x)])
     assert all(torch.equal(s, t) for s, t in zip(*results))
+
+
+def test_status_of_calls_that_finish(cuda_device):
+    status = torch.zeros(1, dtype=torch.int32, device=cuda_device)
+    x = [torch.randn(2, 700, 2, 64, device=cuda_device).to(torch.bfloat16).requires_grad_() for _ in range(3)]
+    o, _ = leaky_attention(*x, torch.tensor([0.9, 1.0], device=cuda_device), status=status)
+    o.sum().backward()
+    assert status.item() == 0
+    status.fill_(6)            # SNN_ERR_TIMEOUT
+    leaky_attention(*x, torch.tensor([0.9, 1.0], device=cuda_device), status=status)
+    assert status.item() == 6

@@ -163,3 +163,30 @@ def test_outputs_that_nothing_uses_bring_no_gradients(calls):
     r = _rows()
     autograd.block_norm(r, _rows(), w_pre=torch.ones(24))[1].sum().backward()
     assert calls.seen[-1][1][6] is None and calls.seen[-1][1][7] is not None   # grad_r_out, grad_y
+
+
+def test_a_call_that_gave_up_shows_in_the_status(calls, monkeypatch):
+    """A kernel's bounded wait that runs out leaves its code in the workspace."""
+    give_up = {"snn_leaky_attn_fwd": 0, "snn_leaky_attn_bwd": 0}
+    for name in give_up:
+        real = getattr(snn, name)
+
+        def call(*a, real=real, name=name, **kw):
+            real(*a, **kw)
+            next(t for t in a if t.dtype == torch.uint8)[:4].view(torch.int32).fill_(give_up[name])
+        monkeypatch.setattr(snn, name, call)
+    beta = torch.full((4,), 0.9)
+    for fwd, bwd in ((0, 0), (6, 0), (0, 6)):
+        give_up.update(snn_leaky_attn_fwd=fwd, snn_leaky_attn_bwd=bwd)
+        status = torch.zeros(1, dtype=torch.int32)
+        o, _ = autograd.leaky_attention(*_qkv(), beta, status=status)
+        assert status.item() == fwd
+        o.sum().backward()
+        assert status.item() == max(fwd, bwd)
+    give_up.update(snn_leaky_attn_fwd=0, snn_leaky_attn_bwd=0)
+    status.fill_(6)                     # it stays until the caller clears it
+    autograd.leaky_attention(*_qkv(), beta, status=status)
+    assert status.item() == 6
+    for bad in (torch.zeros(2, dtype=torch.int32), torch.zeros(1)):
+        with pytest.raises(ValueError, match="status"):
+            autograd.leaky_attention(*_qkv(), beta, status=bad)
