@@ -524,7 +524,7 @@ typedef struct snn_attn_desc {
   int64_t B, T, H, Hk;  /* sequences, tokens, query heads, key/value heads     */
   int64_t Dk, Dv;       /* widths of q/k and of v/o: multiples of 8, 8 .. 128  */
   int32_t dtype;        /* of q, k, v, o and their gradients: SNN_BF16/SNN_F16 */
-  float scale;          /* finite; not 0 for the backward                      */
+  float scale;          /* finite; for the backward 2^-126 <= |scale| <= 2^126  */
   uint32_t reserved[2]; /* must be 0                                           */
 } snn_attn_desc;
 

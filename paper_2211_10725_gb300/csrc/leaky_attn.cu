@@ -310,7 +310,8 @@ snn_status_t snn_leaky_attn_bwd(const snn_attn_desc* desc, const snn_bthd* q, co
                                 snn_stream_t stream) {
   snn_status_t s = check_desc(desc);
   if (s != SNN_OK) return s;
-  if (desc->scale == 0.0f) return SNN_ERR_INVALID_ARG;
+  // the gradient of the end state is divided by it
+  if (!std::isnormal(desc->scale) || !std::isnormal(1.0f / desc->scale)) return SNN_ERR_INVALID_ARG;
   const snn_bthd* x[7] = {q, k, v, grad_o, grad_q, grad_k, grad_v};
   const int64_t heads[7] = {desc->H, desc->Hk, desc->Hk, desc->H, desc->H, desc->Hk, desc->Hk};
   for (int i = 0; i < 7; ++i)

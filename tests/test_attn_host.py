@@ -302,3 +302,13 @@ def test_a_scale_or_eps_that_is_a_tensor_is_read_at_each_call(monkeypatch):
             value.fill_(want)
             call()
             assert lib.seen[-1] == want
+
+
+@pytest.mark.parametrize("scale", [1e-40, -1e-40, 2.0 ** -127, 2.0 ** 127, -2.0 ** 127])
+def test_attention_backward_refuses_a_scale_without_a_reciprocal(lib, scale):
+    """The gradient of the end state is divided by it: infinite below 2^-126, short of bits above
+    2^126."""
+    d = _attn(scale=scale)
+    assert lib.snn_leaky_attn_bwd(ctypes.byref(d), _t(), _t(), _t(), 16, None, None, _t(), 64, _t(), _t(), _t(),
+                                  None, 256, BIG, None) == INVALID
+    assert _fwd(lib, d, ws=None) == WORKSPACE      # the forward takes it
