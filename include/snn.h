@@ -560,10 +560,14 @@ size_t snn_leaky_attn_workspace_bytes(const snn_attn_desc* desc, int backward);
  *              state_out (NULL: b).  A place outside 0 .. num_slots-1 means
  *              no state: zeros in, nothing written.  Places of one call
  *              must differ where state_out is given.
- *   ws         snn_leaky_attn_workspace_bytes(desc, 0) bytes, 16-byte aligned
- *              (its first 256 bytes are the status word of snn_workspace_status)
+ *   ws         snn_leaky_attn_workspace_bytes(desc, 0) bytes, 16-byte aligned.
+ *              Its first 256 bytes are the status word of snn_workspace_status and
+ *              have to be zero before the first call (snn_workspace_init): a
+ *              word that is not reads as an error and hides one.  The rest
+ *              may hold anything.
  * o must not overlap q, k or v.  Products run on the tensor cores with fp32
- * accumulation; the state is kept in fp32 between chunks.  Valid tokens must
+ * accumulation, on operands of 16 bits or more in two parts; the state is kept in
+ * fp32 between chunks, and the output is rounded to 16 bits once.  Valid tokens must
  * be finite: an infinity or NaN there reaches every token of its sequence and
  * head, earlier ones of its chunk included.
  */
@@ -583,7 +587,7 @@ snn_status_t snn_leaky_attn_fwd(const snn_attn_desc* desc, const snn_bthd* q, co
  *   grad_state_in    fp32 [B, H, Dk, Dv] (out) or NULL; neither grad_state_out nor
  *              state_in
  *   state_in   fp32 [B, H, Dk, Dv] or NULL, as in the forward (place b for sequence b)
- *   ws         snn_leaky_attn_workspace_bytes(desc, 1) bytes
+ *   ws         snn_leaky_attn_workspace_bytes(desc, 1) bytes, as in the forward
  * The three gradients are the forward's recurrence with the tensors' roles
  * changed, two of them backwards in time:
  *   grad_q = fwd(grad_o, v, k);  grad_v = rev(k, q, grad_o);  grad_k = rev(v, grad_o, q).

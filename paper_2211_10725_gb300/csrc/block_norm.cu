@@ -27,9 +27,9 @@
 // Measured (share of the copy rate): forward of 16384 x 4096, 16-bit on a 32-bit
 // stream, 151 us (0.92); of 16384 x 2048 bf16 58 us (0.85); of 8192 x 8192 bf16
 // 137 us (0.72); of 2000 x 7049 on a 32-bit stream, element by element, 52 us
-// (0.56).  Backward of 8192 x 4096 on a 32-bit stream 127 us (0.85); of 16384 x
-// 2048 bf16 with a norm per head 103 us (0.77); of 3001 x 1001 fp32 23 us (0.61);
-// of 4096 x 8192 bf16 182 us (0.44: one block of 1024 threads on an SM, nothing
+// (0.56).  Backward of 8192 x 4096 on a 32-bit stream 128 us (0.85); of 16384 x
+// 2048 bf16 with a norm per head 104 us (0.76); of 3001 x 1001 fp32 25 us (0.57);
+// of 4096 x 8192 bf16 189 us (0.42: one block of 1024 threads on an SM, nothing
 // beside its barriers, sums and parameters outside its registers).
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>

@@ -21,8 +21,8 @@ namespace attn {
 // A shared head's gradients: out[b, t, hk, :] = sum over the group's query
 // heads, in head order, of their fp32 shares part[b, t, h, :], rounded once.
 // blockIdx.y picks the gradient (of k or of v).  The shares stay fp32 so that a
-// shared head's gradient is rounded once (3 x 777 tokens, 12 heads on 4: 5 us of
-// 50).
+// shared head's gradient is rounded once (3 x 777 tokens, 12 heads on 4: 8 us from a
+// cold cache, 62 for the whole backward).
 struct SumArgs {
   const float* part[2];
   Tensor out[2];
@@ -125,8 +125,8 @@ Plan plan_fwd(const snn_attn_desc* d) { return plan(d->T, d->B * d->H, tile(d->D
 // Where Dk and Dv differ in tile, grad_q and grad_k have the widths the other way
 // round from grad_v: in two launches, or, where that ends sooner, in one with
 // 128 x 128 tiles, whose blocks are longer but fill the SMs at once. 64 x 128,
-// one launch against two: 78 us and 110 (6 x 1500 tokens, 16 heads), 16 and 25
-// (300 tokens, 8 heads); 290 and 240 (8 x 2048, 32 heads), 274 and 238
+// one launch against two: 92 us and 123 (6 x 1500 tokens, 16 heads), 17 and 28
+// (300 tokens, 8 heads); 350 and 296 (8 x 2048, 32 heads), 323 and 287
 // (32 x 512, 32 heads).
 struct BwdPlan {
   bool one = true;
@@ -178,8 +178,8 @@ cudaError_t launch_tile(ChunkArgs& p, cudaStream_t st) {
     for (int i = 0; i < p.g.nroles; ++i)
       third = third || (p.g.role[i].s_out && std::is_same<T, __nv_bfloat16>::value);
     const size_t smem = C::kSegSmem + (third ? C::kCBytes : 0);
-    // up to four states are summed as quickly by the segments themselves (2x4096
-    // tokens of 32 heads, four segments: 87 us, 89 with the scan)
+    // up to four states are summed sooner by the segments themselves (2x4096
+    // tokens of 32 heads, four segments: 97 us, 102 with the scan)
     p.scanned = p.nseg > kSummed;
     cudaError_t es = ensure_smem((const void*)attn_segments<T, DA, DC>, smem);
     if (es == cudaSuccess)

@@ -37,12 +37,14 @@
 // to the state; a second (attn_segment_scan), where there are more than a few,
 // the state each one starts from.
 //
-// What bounds it, measured (bf16, 128 x 128): the instructions of the state's and
-// the scores' parts and the chain of a chunk's products and barriers.  With two
-// blocks on every SM (8 x 4096 tokens, 38 heads) 240 us, the tensors' bytes at
-// 5.3 TB/s, 0.78 of the measured copy rate; 201 with one part each of the scores
-// and the state, 219 with two of the scores alone.  A block alone on its SM takes
-// 2.6 us a chunk, one of two 3.7.
+// What bounds it, measured (128 x 128): with two blocks on every SM issue slots and
+// the tensor core's operand reads are each busy half of the time, and the rest is
+// the chain of a chunk's products and barriers.  8 x 4096 tokens of 38 heads, which
+// are two blocks for each of 152 SMs: bf16 239 us, the tensors' bytes at 5.3 TB/s,
+// 0.79 of the measured copy rate (201 with one part each of the scores and the
+// state, 219 with two of the scores alone); fp16 314 (its three scalings a chunk
+// cost a barrier each).  2 x 4096 tokens of 32 heads, bf16: 97.  A block alone on its
+// SM takes 2.6 us a chunk, one of two 3.7.
 #pragma once
 
 #include <cuda.h>
@@ -535,10 +537,10 @@ __device__ __forceinline__ void clear_rows(unsigned char* tile, int bytes, int n
 // tokens (the first one's from the caller's state, kept too, because that may
 // be overwritten in place).  The tiles of b and c have two stages, and the
 // state is updated from one accumulator while the next chunk's products fill
-// the other.  Two blocks of an SM take 1.9 us a chunk each (2 x 4096 tokens, 32
-// heads in four segments: 31 us), bound by the chain from the split of the
-// values through their products; the reads alone would be 1.45.  One block on an
-// SM with the split pipelined as well (twice the shared memory) took 1.1.
+// the other.  2 x 4096 tokens of 32 heads in four segments take 31 us, 3.2 TB/s: two
+// blocks of an SM take 1.9 us a chunk each, bound by the chain from the split of
+// the values through their products.  One block on an SM with the split
+// pipelined as well (twice the shared memory) took 1.1.
 template <typename T, int DA, int DC>
 __global__ void __launch_bounds__(Cfg<DA, DC>::kThreads, Cfg<DA, DC>::kSegBlocksPerSm)
     attn_segments(const __grid_constant__ ChunkArgs p) {
@@ -694,7 +696,7 @@ __global__ void __launch_bounds__(Cfg<DA, DC>::kThreads, Cfg<DA, DC>::kSegBlocks
 // segment before it added (1: with the first one's start), so
 //   E_1 = s_1,  E_m = beta^tokens E_{m-1} + s_m.
 // Every thread takes four neighbouring floats through all places, eight loads
-// in flight (19 places of 16 heads: 20 MB, about 5 us).
+// in flight (19 places of 16 heads: 19 MB read from a cold cache in 8 us).
 constexpr int kScanThreads = 256;
 __global__ void __launch_bounds__(kScanThreads) attn_segment_scan(const __grid_constant__ ChunkArgs p,
                                                                   int floats) {
