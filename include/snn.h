@@ -689,6 +689,223 @@ snn_status_t snn_block_norm_bwd(const snn_norm_desc* desc, const snn_rows* r_out
                                 float* grad_w_pre, void* ws, size_t ws_bytes, snn_stream_t stream);
 
 /*
+ * Selective scan: a leaky scan in time whose leak follows its input, the
+ * membrane of Eq. (2) with N diagonal states for every channel.  For channel d of
+ * group g = d / (D / G) and its states n:
+ *   s_t    = softplus(delta_t + delta_bias)       (or delta_t + delta_bias itself)
+ *   h_t[n] = exp(s_t A[d, n]) h_{t-1}[n] + s_t u_t B_t[g, n]
+ *   y_t    = (sum_n C_t[g, n] h_t[n] + D_d u_t) silu(z_t)
+ * over u, delta, z, y [B, T, D] and B, C [B, T, G, N].  The states and all
+ * arithmetic are fp32; outputs are rounded to their type once.
+ */
+typedef struct snn_sscan_desc {
+  int64_t B, T;         /* sequences, tokens                                   */
+  int64_t D, N, G;      /* channels, states of a channel (1 .. 64), groups that
+                           share B and C (G divides D)                         */
+  int32_t dtype;        /* snn_dtype_t of u, delta, z, B, C, y, their gradients */
+  int32_t softplus;     /* 1: s = softplus(delta + bias); 0: delta + bias      */
+  uint32_t reserved[2]; /* must be 0                                           */
+} snn_sscan_desc;
+
+/* A [B, T, C] tensor on the device with contiguous channels: element (b, t, c)
+ * at data[b*stride_b + t*stride_t + c].  data 16-byte aligned; strides positive (that
+ * of an extent of 1 is not looked at).  Strides of whole vectors (multiples of 8)
+ * and of channels (D, or C, likewise) are the quick ones. */
+typedef struct snn_btc {
+  void* data;
+  int64_t stride_b, stride_t;
+} snn_btc;
+
+/* sizeof(snn_sscan_desc) as compiled into the library (ABI check). */
+size_t snn_sscan_desc_size(void);
+
+/* Bytes of device workspace of snn_selective_scan_fwd (backward = 0) or _bwd (backward
+ * != 0; enough for the forward too); it need not be initialised.  0 for an invalid
+ * desc.  dtype and softplus are not looked at. */
+size_t snn_selective_scan_workspace_bytes(const snn_sscan_desc* desc, int backward);
+
+/* Floats of the checkpoints that a forward leaves for its backward: the states
+ * before every eighth token.  0 for an invalid desc. */
+int64_t snn_selective_scan_ckpt_elems(const snn_sscan_desc* desc);
+
+/*
+ * Forward over whole sequences (prompts, training).
+ *   A          fp32 [D, N]; finite.  Decays are those of negative values.
+ *   Bm, Cm     [B, T, G, N], states contiguous; strides positive, of any
+ *              number of elements (stride_h of snn_bthd is the groups')
+ *   D          fp32 [D] or NULL (zeros)
+ *   z          [B, T, D] or NULL (no gate)
+ *   delta_bias fp32 [D] or NULL (zeros)
+ *   seq_lens   int32 [B] or NULL: sequence b has its first seq_lens[b] tokens
+ *              (clamped to 0 .. T; NULL: all T).  Later places are not read into any
+ *              result, whatever they hold (NaN included); their outputs are zero.
+ *   state_in   fp32 [num_slots, D, N] or NULL (zeros): h before the first token
+ *   state_out  the same or NULL: h after the last one (equal to state_in's for an
+ *              empty sequence).  May be state_in itself.
+ *   slots      int32 [B] or NULL: the place of sequence b's state (NULL: b).  A
+ *              place outside 0 .. num_slots-1 means no state: zeros in, nothing
+ *              written.  Places of one call must differ where state_out is given.
+ *   ckpt       fp32 [snn_selective_scan_ckpt_elems] (out) or NULL: what the backward reads
+ *   y          (out); must not overlap an input
+ *   ws         snn_selective_scan_workspace_bytes(desc, 0) bytes, 16-byte aligned
+ * A long axis is cut into spans where there are few channels: a first kernel
+ * finds what each span adds to the state, a second goes through the spans
+ * side by side.  Results do not depend on the order in which blocks run.
+ */
+snn_status_t snn_selective_scan_fwd(const snn_sscan_desc* desc, const snn_btc* u,
+                                    const snn_btc* delta, const float* A, const snn_bthd* Bm,
+                                    const snn_bthd* Cm, const float* D, const snn_btc* z,
+                                    const float* delta_bias, const int32_t* seq_lens,
+                                    const float* state_in, float* state_out,
+                                    const int32_t* slots, int64_t num_slots, float* ckpt,
+                                    const snn_btc* y, void* ws, size_t ws_bytes,
+                                    snn_stream_t stream);
+
+/*
+ * Backward of snn_selective_scan_fwd from the same inputs and the checkpoints that it left
+ * (which hold state_in).
+ *   grad_y          [B, T, D]
+ *   grad_state_out  fp32 [B, D, N] or NULL (zeros)
+ *   grad_u, grad_delta [B, T, D], grad_B, grad_C [B, T, G, N] (out); zero in
+ *                   places at and past seq_lens[b]
+ *   grad_A          fp32 [D, N] (out)
+ *   grad_D, grad_delta_bias  fp32 [D] (out) or NULL
+ *   grad_z          [B, T, D] (out), given exactly when z is
+ *   grad_state_in   fp32 [B, D, N] (out) or NULL; not grad_state_out
+ *   ws              snn_selective_scan_workspace_bytes(desc, 1) bytes, 16-byte aligned
+ * Sums over channels, sequences and spans are taken in a fixed order (no
+ * atomics: the same bits on every call).  No output may overlap an input.
+ */
+snn_status_t snn_selective_scan_bwd(const snn_sscan_desc* desc, const snn_btc* u,
+                                    const snn_btc* delta, const float* A, const snn_bthd* Bm,
+                                    const snn_bthd* Cm, const float* D, const snn_btc* z,
+                                    const float* delta_bias, const int32_t* seq_lens,
+                                    const float* ckpt, const snn_btc* grad_y,
+                                    const float* grad_state_out, const snn_btc* grad_u,
+                                    const snn_btc* grad_delta, float* grad_A,
+                                    const snn_bthd* grad_B, const snn_bthd* grad_C, float* grad_D,
+                                    const snn_btc* grad_z, float* grad_delta_bias,
+                                    float* grad_state_in, void* ws, size_t ws_bytes,
+                                    snn_stream_t stream);
+
+/*
+ * One token for each of B sequences (decoding): the states are updated in place.
+ *   desc    T = 1 (stride_t is not looked at)
+ *   state   fp32 [num_slots, D, N] (in/out)
+ *   slots   int32 [B] or NULL (sequence b at place b; num_slots >= B then).  A place
+ *           outside 0 .. num_slots-1 is an empty place of the batch: its y is
+ *           zero and no state changes.  Places of one call must differ.
+ */
+snn_status_t snn_selective_scan_step(const snn_sscan_desc* desc, const snn_btc* u,
+                                     const snn_btc* delta, const float* A, const snn_bthd* Bm,
+                                     const snn_bthd* Cm, const float* D, const snn_btc* z,
+                                     const float* delta_bias, float* state, const int32_t* slots,
+                                     int64_t num_slots, const snn_btc* y, snn_stream_t stream);
+
+/*
+ * Causal convolution of each channel over W tokens (depthwise), the short one
+ * before a selective scan:
+ *   p_t = bias + sum_j w[j] x_{t-W+1+j},   y_t = act(p_t)
+ * with act the identity (SNN_GATE_NONE) or p * sigmoid(p) (SNN_GATE_SILU), over x and y
+ * [B, T, C].  The inputs before the sequence come from a state of W - 1 of
+ * them, oldest first, or are zero.
+ */
+typedef struct snn_conv_desc {
+  int64_t B, T, C, W;   /* sequences, tokens, channels, taps (2, 3 or 4)       */
+  int32_t dtype;        /* snn_dtype_t of x, y, the states and gradients       */
+  int32_t act;          /* snn_gate_t: SNN_GATE_NONE or SNN_GATE_SILU          */
+  uint32_t reserved[2]; /* must be 0                                           */
+} snn_conv_desc;
+
+/* sizeof(snn_conv_desc) as compiled into the library (ABI check). */
+size_t snn_conv_desc_size(void);
+
+/* Bytes of device workspace of snn_causal_conv_bwd (partial sums of the
+ * parameters' gradients; need not be initialised); 0 for an invalid desc. */
+size_t snn_causal_conv_workspace_bytes(const snn_conv_desc* desc);
+
+/*
+ * Forward.
+ *   w          fp32 [C, W];  bias fp32 [C] or NULL (zeros)
+ *   seq_lens, slots  as in snn_selective_scan_fwd
+ *   state_in   [num_slots, W-1, C] of dtype or NULL (zeros)
+ *   state_out  the same or NULL: the last W - 1 inputs of the state and the
+ *              sequence's tokens.  May be state_in itself.
+ *   y          (out); must not overlap x
+ */
+snn_status_t snn_causal_conv_fwd(const snn_conv_desc* desc, const snn_btc* x, const float* w,
+                                 const float* bias, const int32_t* seq_lens, const void* state_in,
+                                 void* state_out, const int32_t* slots, int64_t num_slots,
+                                 const snn_btc* y, snn_stream_t stream);
+
+/*
+ * Backward (the pre-activations are computed again).  State tensors [B, W-1, C].
+ *   grad_x (out), grad_w fp32 [C, W], grad_bias fp32 [C], grad_state_in (out): each or NULL
+ *   grad_state_out  of dtype or NULL (zeros)
+ *   grad_state_in   neither state_in nor grad_state_out; grad_x must not overlap x or grad_y
+ *   ws         snn_causal_conv_workspace_bytes(desc) bytes, 16-byte aligned (may be NULL
+ *              without grad_w and grad_bias)
+ * The parameters' gradients are summed in a fixed order.
+ */
+snn_status_t snn_causal_conv_bwd(const snn_conv_desc* desc, const snn_btc* x, const float* w,
+                                 const float* bias, const int32_t* seq_lens, const void* state_in,
+                                 const snn_btc* grad_y, const void* grad_state_out,
+                                 const snn_btc* grad_x, float* grad_w, float* grad_bias,
+                                 void* grad_state_in, void* ws, size_t ws_bytes,
+                                 snn_stream_t stream);
+
+/* One token for each of B sequences (decoding, desc->T = 1): state [num_slots, W-1, C] of
+ * dtype loses its oldest input and takes x; slots as in snn_selective_scan_step. */
+snn_status_t snn_causal_conv_step(const snn_conv_desc* desc, const snn_btc* x, const float* w,
+                                  const float* bias, void* state, const int32_t* slots,
+                                  int64_t num_slots, const snn_btc* y, snn_stream_t stream);
+
+/*
+ * Layer norm of the rows of an [M, N] matrix:
+ *   y = (x - mean) * rsqrt(mean of (x - mean)^2 + eps) * w + b
+ * in fp32, rounded to y's type once.
+ */
+typedef struct snn_layer_norm_desc {
+  int64_t M, N;         /* rows, channels (N <= 8192)                          */
+  int32_t dtype;        /* snn_dtype_t of y and its gradient                   */
+  int32_t res_dtype;    /* of x and its gradient: dtype or SNN_F32             */
+  float eps;            /* > 0                                                 */
+  uint32_t reserved;    /* must be 0                                           */
+} snn_layer_norm_desc;
+
+/* sizeof(snn_layer_norm_desc) as compiled into the library (ABI check). */
+size_t snn_layer_norm_desc_size(void);
+
+/* Bytes of device workspace of snn_layer_norm_bwd (partial sums of the
+ * parameters' gradients; need not be initialised); 0 for a bad shape. */
+size_t snn_layer_norm_workspace_bytes(int64_t M, int64_t N);
+
+/*
+ * Forward.  w (NULL: ones) and b (NULL: zeros) are fp32 [N].
+ *   y      (out); may be x itself where the types are equal
+ *   stats  fp32 [2, M] (out) or NULL: means and reciprocal deviations, for the backward
+ * Where N and every ld are multiples of 8 a thread moves whole vectors; any
+ * other rows are staged as the aligned vectors that cover them.
+ */
+snn_status_t snn_layer_norm_fwd(const snn_layer_norm_desc* desc, const snn_rows* x,
+                                const float* w, const float* b, const snn_rows* y, float* stats,
+                                snn_stream_t stream);
+
+/*
+ * Backward from x and the forward's stats (g = grad_y w, e the normalised x; eps is
+ * not looked at):
+ *   grad_x = rstd (g - mean(g) - e mean(g e)) or NULL; may be grad_y where the types are equal
+ *   grad_w = sum of grad_y e, grad_b = sum of grad_y: fp32 [N] or NULL, summed over the
+ *          rows in a fixed order
+ *   ws     snn_layer_norm_workspace_bytes(M, N) bytes, 16-byte aligned (may be NULL without
+ *          grad_w and grad_b)
+ */
+snn_status_t snn_layer_norm_bwd(const snn_layer_norm_desc* desc, const snn_rows* x,
+                                const float* w, const float* stats, const snn_rows* grad_y,
+                                const snn_rows* grad_x, float* grad_w, float* grad_b, void* ws,
+                                size_t ws_bytes, snn_stream_t stream);
+
+/*
  * Leaky BPTT that allocates nothing (no counterpart in the paper; it exists
  * for callers of this library that cannot allocate device memory: hosts
  * whose device memory is budgeted by another runtime, real-time loops that

@@ -9,8 +9,9 @@ or v as a fourth tensor and return its gradient as well.  Only the spike
 output is differentiable; the membrane trace is not returned.
 
 ``leaky_attention`` and ``block_norm`` wrap the two operators of a residual
-block of a sequence network in the same way; their gradients have none of
-their own (asked for, they raise).
+block of a sequence network in the same way, ``selective_scan``,
+``causal_conv`` and ``layer_norm`` those of a block whose leak follows its
+input; their gradients have none of their own (asked for, they raise).
 """
 from __future__ import annotations
 
@@ -213,3 +214,154 @@ def block_norm(r, a, z=None, w_post=None, res_scale=None, w_pre=None, eps=1e-6, 
     if a.shape != r.shape or (z is not None and z.shape != r.shape):
         raise ValueError("block_norm: r, a and z must have one shape")
     return _BlockNormFunction.apply(r, a, z, w_post, res_scale, w_pre, eps, group, gate)
+
+
+def _channels(t, dtype):
+    """A [B, T, C] tensor as the library reads it in place, or a copy (or None):
+    C contiguous, the other steps positive."""
+    if t is None:
+        return None
+    t = t.to(dtype)
+    n, st = t.shape, t.stride()
+    ok = _starts(t) and (n[2] <= 1 or st[2] == 1) and all(n[i] <= 1 or st[i] > 0 for i in range(2))
+    return t if ok else _copied(t)
+
+
+def _grouped(t):
+    """A [B, T, G, N] tensor as the library reads it in place, or a copy."""
+    n, st = t.shape, t.stride()
+    ok = _starts(t) and (n[3] <= 1 or st[3] == 1) and all(n[i] <= 1 or st[i] > 0 for i in range(3))
+    return t if ok else _copied(t)
+
+
+def _like(t):
+    return None if t is None else torch.empty(t.shape, dtype=t.dtype, device=t.device)
+
+
+def _scratch(n, like):
+    return torch.empty(n, dtype=torch.uint8, device=like.device)
+
+
+class _SelectiveScanFunction(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, u, delta, A, B, C, D, z, delta_bias, state, softplus, seq_lens):
+        u, delta, z = (_channels(t, u.dtype) for t in (u, delta, z))
+        B, C = _grouped(B), _grouped(C)
+        A, D, delta_bias, state, seq_lens = map(_whole, (A, D, delta_bias, state, seq_lens))
+        shape = (*u.shape, A.shape[1], B.shape[2])
+        y = torch.empty(u.shape, dtype=u.dtype, device=u.device)
+        end = torch.empty((u.shape[0], *A.shape), dtype=torch.float32, device=u.device)
+        ckpt = None
+        if any(ctx.needs_input_grad):
+            ckpt = torch.empty(snn.snn_selective_scan_ckpt_elems(*shape), dtype=torch.float32, device=u.device)
+        snn.snn_selective_scan_fwd(u, delta, A, B, C, y,
+                                   _scratch(snn.snn_selective_scan_workspace_bytes(*shape), u), D=D, z=z,
+                                   delta_bias=delta_bias, softplus=softplus, seq_lens=seq_lens,
+                                   state_in=state, state_out=end, ckpt=ckpt)
+        ctx.save_for_backward(u, delta, A, B, C, D, z, delta_bias, state, seq_lens, ckpt)
+        ctx.softplus = softplus
+        ctx.set_materialize_grads(False)
+        return y, end
+
+    @staticmethod
+    @once_differentiable
+    def backward(ctx, grad_y, grad_end):
+        u, delta, A, B, C, D, z, delta_bias, state, seq_lens, ckpt = ctx.saved_tensors
+        if grad_y is None and grad_end is None:
+            return (None,) * 11
+        shape = (*u.shape, A.shape[1], B.shape[2])
+        grad_y = torch.zeros(u.shape, dtype=u.dtype, device=u.device) if grad_y is None \
+            else _channels(grad_y, u.dtype)
+        gu, gd, gA, gB, gC, gD, gz, gb = map(_like, (u, delta, A, B, C, D, z, delta_bias))
+        gs = _like(state) if state is not None and ctx.needs_input_grad[8] else None
+        snn.snn_selective_scan_bwd(u, delta, A, B, C, grad_y, ckpt, gu, gd, gA, gB, gC,
+                                   _scratch(snn.snn_selective_scan_workspace_bytes(*shape, backward=True), u),
+                                   D=D, z=z, delta_bias=delta_bias, softplus=ctx.softplus, seq_lens=seq_lens,
+                                   grad_state_out=_whole(grad_end), grad_D=gD, grad_z=gz,
+                                   grad_delta_bias=gb, grad_state_in=gs)
+        return gu, gd, gA, gB, gC, gD, gz, gb, gs, None, None
+
+
+def selective_scan(u, delta, A, B, C, D=None, z=None, delta_bias=None, softplus=True, state=None,
+                   seq_lens=None):
+    """(y, state after the last token) of the selective scan, s = softplus(delta +
+    delta_bias), h_t = exp(s A) h_{t-1} + s u B and y = (C h + D u) silu(z): u, delta, z
+    [B, T, D] and B, C [B, T, G, N] of one type (fp32, bf16 or fp16), G dividing D; A [D, N],
+    D and delta_bias [D] fp32; state fp32 [B, D, N] or None.  Differentiable in all the tensors."""
+    if u.dim() != 3 or B.dim() != 4 or C.dim() != 4 or A.dim() != 2:
+        raise ValueError("selective_scan: u must be [B, T, D], B and C [B, T, G, N], A [D, N]")
+    if any(t is not None and t.dtype != u.dtype for t in (delta, z, B, C)):
+        raise ValueError("selective_scan: u, delta, z, B and C must have one type")
+    return _SelectiveScanFunction.apply(u, delta, A, B, C, D, z, delta_bias, state, bool(softplus), seq_lens)
+
+
+class _CausalConvFunction(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, x, w, bias, state, act, seq_lens):
+        x = _channels(x, x.dtype)
+        w, bias, state, seq_lens = map(_whole, (w, bias, state, seq_lens))
+        y = torch.empty(x.shape, dtype=x.dtype, device=x.device)
+        end = torch.empty((x.shape[0], w.shape[1] - 1, x.shape[2]), dtype=x.dtype, device=x.device)
+        snn.snn_causal_conv_fwd(x, w, bias, y, act=act, seq_lens=seq_lens, state_in=state, state_out=end)
+        ctx.save_for_backward(x, w, bias, state, seq_lens)
+        ctx.act = act
+        ctx.set_materialize_grads(False)
+        return y, end
+
+    @staticmethod
+    @once_differentiable
+    def backward(ctx, grad_y, grad_end):
+        x, w, bias, state, seq_lens = ctx.saved_tensors
+        if grad_y is None and grad_end is None:
+            return (None,) * 6
+        grad_y = torch.zeros(x.shape, dtype=x.dtype, device=x.device) if grad_y is None \
+            else _channels(grad_y, x.dtype)
+        gx, gw, gb = map(_like, (x, w, bias))
+        gs = _like(state) if state is not None and ctx.needs_input_grad[3] else None
+        snn.snn_causal_conv_bwd(x, w, bias, grad_y, gx, gw, gb,
+                                _scratch(snn.snn_causal_conv_workspace_bytes(*x.shape, w.shape[1]), x),
+                                act=ctx.act, seq_lens=seq_lens, state_in=state,
+                                grad_state_out=_whole(grad_end), grad_state_in=gs)
+        return gx, gw, gb, gs, None, None
+
+
+def causal_conv(x, w, bias=None, act="silu", state=None, seq_lens=None):
+    """(y, the last W - 1 inputs) of the causal convolution of each channel, y_t =
+    act(bias + sum_j w[j] x_{t-W+1+j}): x [B, T, C] (fp32, bf16 or fp16), w [C, W] and bias
+    [C] fp32, state [B, W-1, C] of x's type or None.  Differentiable in all the tensors."""
+    if x.dim() != 3 or w.dim() != 2:
+        raise ValueError("causal_conv: x must be [B, T, C] and w [C, W]")
+    if state is not None and state.dtype != x.dtype:
+        raise ValueError("causal_conv: the state must have x's type")
+    return _CausalConvFunction.apply(x, w, bias, state, act, seq_lens)
+
+
+class _LayerNormFunction(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, x, w, b, eps, dtype):
+        shape, N = x.shape, x.shape[-1]
+        x2 = _matrix(x, N, 0)
+        w, b = _whole(w), _whole(b)
+        y = torch.empty(x2.shape, dtype=dtype, device=x.device)
+        stats = torch.empty((2, x2.shape[0]), dtype=torch.float32, device=x.device) \
+            if any(ctx.needs_input_grad) else None
+        snn.snn_layer_norm_fwd(x2, w, b, y, stats=stats, eps=eps)
+        ctx.save_for_backward(x2, w, b, stats)
+        ctx.shape, ctx.dtype = shape, dtype
+        return y.view(shape)
+
+    @staticmethod
+    @once_differentiable
+    def backward(ctx, grad_y):
+        x, w, b, stats = ctx.saved_tensors
+        M, N = x.shape
+        gx, gw, gb = map(_like, (x, w, b))
+        snn.snn_layer_norm_bwd(x, w, stats, _matrix(grad_y, N, 0, ctx.dtype), gx, gw, gb,
+                               _scratch(snn.snn_layer_norm_workspace_bytes(M, N), x))
+        return gx.view(ctx.shape), gw, gb, None, None
+
+
+def layer_norm(x, w=None, b=None, eps=1e-5, dtype=None):
+    """(x - mean) rsqrt(var + eps) w + b over the last dimension, as `dtype` (x's own, or a
+    16-bit type of an fp32 x).  w and b: fp32 or None.  Differentiable in x, w and b."""
+    return _LayerNormFunction.apply(x, w, b, float(eps), dtype or x.dtype)

@@ -24,7 +24,8 @@ SOURCES = ["snn_api.cu", "scan_fwd.cu", "scan_bwd_leaky.cu", "scan_bwd_leaky_rec
            "scan_bwd_leaky_seg12.cu",
            "scan_bwd_synaptic.cu", "scan_bwd_synaptic_recompute.cu", "reduce.cu", "snn_noalloc.cu",
            "gemm_tcgen05.cu", "gemm_scan.cu", "ce_loss.cu", "adamw.cu", "conv_pool.cu", "conv_small.cu",
-           "leaky_attn.cu", "leaky_attn_step.cu", "block_norm.cu"]
+           "leaky_attn.cu", "leaky_attn_step.cu", "block_norm.cu", "layer_norm.cu", "causal_conv.cu",
+           "sel_scan_step.cu", "sel_scan_fwd.cu", "sel_scan_bwd.cu"]
 ARCH = ["-gencode", "arch=compute_103a,code=sm_103a"]
 NVCC_FLAGS = ARCH + ["-O3", "-lineinfo", "-std=c++17", "-Xcompiler", "-fPIC",
                      "-Xcompiler", "-fvisibility=hidden", "--expt-relaxed-constexpr",

@@ -1,0 +1,272 @@
+// Shared by the selective-scan kernels and their entry points.
+//
+//   s = softplus(delta + bias),  x = s u,  a_t = exp(s A)
+//   h_t = a_t h_{t-1} + x_t B_t,   y_t = (sum_n C_t h_t + D u_t) silu(z_t)
+//
+// A thread holds four states of two neighbouring channels of a group (a pair), in
+// pairs of floats: one instruction serves both channels.  P = ceil(N / 4) threads
+// side by side hold a pair's states.  The decay of a span of tokens is
+// exp(A sum s), so a cut axis hands on one sum a channel beside the states.
+#pragma once
+
+#include <cuda_bf16.h>
+#include <cuda_fp16.h>
+#include <cuda_runtime.h>
+
+#include <cmath>
+#include <cstdint>
+
+#include "launch.cuh"
+#include "scan_host.cuh"
+#include "snn.h"
+#include "snn_device.cuh"
+
+namespace snn {
+namespace sscan {
+
+constexpr int kStates = 4;        // of a channel in a thread
+constexpr int kMaxN = 64;
+constexpr int kCkpt = 8;          // tokens between checkpoints
+constexpr float kLog2E = 1.44269504088896340736f;
+
+struct Seq {  // [B, T, channels]
+  void* data = nullptr;
+  int64_t sb = 0, st = 0;
+};
+struct Mat {  // [B, T, G, N]
+  void* data = nullptr;
+  int64_t sb = 0, st = 0, sg = 0;
+};
+
+struct Args {
+  int B, T, D, N, G, Dg;   // Dg channels of a group
+  int softplus;
+  int pair_ok;             // channel pairs lie on their own boundaries in every tensor
+  int P;                   // threads of a pair
+  int pairs;               // of a group
+  int spans, span;         // cuts of the axis, tokens of each
+  Seq u, delta, z, y, gy, gu, gdelta, gz;
+  Mat Bm, Cm;
+  const float *A, *D_skip, *bias;
+  const int32_t *seq_lens, *slots;
+  const float* state_in;
+  float* state_out;
+  int64_t num_slots;
+  float* ckpt;             // [B][ceil(T / 8)][G pairs][P][2 kStates]
+  float* ends;             // [spans][B][G pairs][P][2 kStates]: what a span adds to the state
+  float2* sums;            // [spans][B][G pairs]: of s over a span
+  // backward
+  const float* grad_state_out;
+  float* grad_state_in;
+  int per_block;           // turns of a block over its pairs
+  float *part_B, *part_C;  // [blocks of a group][B][T][G][N]
+  float* part_A;           // [spans][B][D][N]
+  float *part_D, *part_bias;  // [spans][B][D]
+};
+
+__device__ __forceinline__ int seq_len(const Args& g, int b) {
+  if (!g.seq_lens) return g.T;
+  const int n = g.seq_lens[b];
+  return n < 0 ? 0 : (n > g.T ? g.T : n);
+}
+
+__device__ __forceinline__ float ex2(float x) {
+  asm("ex2.approx.ftz.f32 %0, %0;" : "+f"(x));
+  return x;
+}
+__device__ __forceinline__ float2 ex2(float2 x) { return make_float2(ex2(x.x), ex2(x.y)); }
+__device__ __forceinline__ float rcp(float x) {
+  asm("rcp.approx.ftz.f32 %0, %0;" : "+f"(x));
+  return x;
+}
+
+// log(1 + e^x) = max(x, 0) + log(1 + e), e = e^-|x|, with the area tangent's
+// series: log(1 + e) = 2 atanh(r), r = e / (2 + e) <= 1/3, whose terms past r^13
+// are below 2^-25 of it.
+__device__ __forceinline__ float softplus(float x) {
+  const float e = expf(-fabsf(x));
+  const float r = e * rcp(2.0f + e), q = r * r;
+  float p = 1.0f / 15.0f;
+  p = fmaf(p, q, 1.0f / 13.0f);
+  p = fmaf(p, q, 1.0f / 11.0f);
+  p = fmaf(p, q, 1.0f / 9.0f);
+  p = fmaf(p, q, 1.0f / 7.0f);
+  p = fmaf(p, q, 1.0f / 5.0f);
+  p = fmaf(p, q, 1.0f / 3.0f);
+  p = fmaf(p * q, r, r);
+  return fmaf(2.0f, p, fmaxf(x, 0.0f));
+}
+
+// 1 / (1 + e^-x).  Results rounded to 16 bits take the approximate power of
+// two and reciprocal: the rounding of x log2(e) costs |x| 2^-24 of the result.
+template <typename T>
+__device__ __forceinline__ float sigmoid(float x) {
+  if constexpr (sizeof(T) == 4) return __frcp_rn(1.0f + expf(-x));
+  else return rcp(1.0f + ex2(-kLog2E * x));
+}
+template <typename T>
+__device__ __forceinline__ float2 sigmoid(float2 x) {
+  return make_float2(sigmoid<T>(x.x), sigmoid<T>(x.y));
+}
+
+// The channels c and c + 1 of a token as they lie in memory.
+template <typename T>
+struct Raw {
+  uint32_t w[sizeof(T) / 2];
+  __device__ __forceinline__ void clear() {
+#pragma unroll
+    for (int i = 0; i < (int)sizeof(T) / 2; ++i) w[i] = 0;
+  }
+  __device__ __forceinline__ void load(const T* p, bool pair, bool second) {
+    if (pair) {
+      if constexpr (sizeof(T) == 2) {
+        w[0] = *reinterpret_cast<const uint32_t*>(p);
+      } else {
+        const uint2 a = *reinterpret_cast<const uint2*>(p);
+        w[0] = a.x;
+        w[1] = a.y;
+      }
+    } else if constexpr (sizeof(T) == 2) {
+      const uint16_t* h = reinterpret_cast<const uint16_t*>(p);
+      w[0] = h[0] | (second ? (uint32_t)h[1] << 16 : 0u);
+    } else {
+      const uint32_t* h = reinterpret_cast<const uint32_t*>(p);
+      w[0] = h[0];
+      w[1] = second ? h[1] : 0u;
+    }
+  }
+  __device__ __forceinline__ float2 get() const {
+    if constexpr (sizeof(T) == 2) return Elem<T>::to2(w[0]);
+    else return make_float2(__uint_as_float(w[0]), __uint_as_float(w[1]));
+  }
+};
+
+template <typename T>
+__device__ __forceinline__ void put_pair(T* p, float2 v, bool pair, bool second) {
+  if (pair) {
+    if constexpr (sizeof(T) == 2) *reinterpret_cast<uint32_t*>(p) = Elem<T>::from2(v.x, v.y);
+    else *reinterpret_cast<float2*>(p) = v;
+  } else {
+    Elem<T>::store1(p, v.x);
+    if (second) Elem<T>::store1(p + 1, v.y);
+  }
+}
+
+// s of the two channels of a raw delta.
+__device__ __forceinline__ float2 step_of(float2 raw, float2 bias, bool soft) {
+  raw = add2(raw, bias);
+  return soft ? make_float2(softplus(raw.x), softplus(raw.y)) : raw;
+}
+
+// A thread's states of its pair in an fp32 [.., D, N] array (element (c, n) at
+// base + c N + n): `at` is (channel 0's row) + 4 pl; absent states are zero.
+__device__ __forceinline__ void load_states(const float* p, int N, int n0, bool second, float2 v[kStates]) {
+#pragma unroll
+  for (int q = 0; q < kStates; ++q) {
+    const bool in = n0 + q < N;
+    v[q].x = in ? p[n0 + q] : 0.0f;
+    v[q].y = in && second ? p[N + n0 + q] : 0.0f;
+  }
+}
+__device__ __forceinline__ void store_states(float* p, int N, int n0, bool second, const float2 v[kStates]) {
+#pragma unroll
+  for (int q = 0; q < kStates; ++q) {
+    if (n0 + q < N) {
+      p[n0 + q] = v[q].x;
+      if (second) p[N + n0 + q] = v[q].y;
+    }
+  }
+}
+
+// A thread's eight floats in an array of its own layout.
+__device__ __forceinline__ void load_own(const float* p, float2 v[kStates]) {
+  const float4 a = reinterpret_cast<const float4*>(p)[0], b = reinterpret_cast<const float4*>(p)[1];
+  v[0] = make_float2(a.x, a.y);
+  v[1] = make_float2(a.z, a.w);
+  v[2] = make_float2(b.x, b.y);
+  v[3] = make_float2(b.z, b.w);
+}
+__device__ __forceinline__ void store_own(float* p, const float2 v[kStates]) {
+  reinterpret_cast<float4*>(p)[0] = make_float4(v[0].x, v[0].y, v[1].x, v[1].y);
+  reinterpret_cast<float4*>(p)[1] = make_float4(v[2].x, v[2].y, v[3].x, v[3].y);
+}
+
+// ---------------------------------------------------------------------------
+// Host side
+// ---------------------------------------------------------------------------
+
+constexpr int64_t kMost = int64_t(1) << 28;
+
+inline bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
+inline size_t round256(size_t n) { return (n + 255) & ~size_t(255); }
+
+inline snn_status_t check_desc(const snn_sscan_desc* d) {
+  if (!d || d->reserved[0] || d->reserved[1]) return SNN_ERR_INVALID_ARG;
+  if (d->B < 0 || d->T < 0 || d->D < 1 || d->N < 1 || d->G < 1 || d->D % d->G) return SNN_ERR_INVALID_ARG;
+  if (d->dtype < SNN_F32 || d->dtype > SNN_F16) return SNN_ERR_INVALID_ARG;
+  if (d->softplus != 0 && d->softplus != 1) return SNN_ERR_INVALID_ARG;
+  if (d->N > kMaxN) return SNN_ERR_UNSUPPORTED;
+  // token, channel and block indexes are 32-bit
+  if (d->T > kMost || d->B > kMost || d->D > (kMost >> 6) || (d->T > 0 && d->B * d->T > kMost) ||
+      d->B * d->D > kMost)
+    return SNN_ERR_UNSUPPORTED;
+  return SNN_OK;
+}
+
+// A [B, T, D] tensor; *pair is cleared where channel pairs may lie between
+// boundaries.
+inline snn_status_t take(const snn_sscan_desc* d, const snn_btc* x, Seq* out, bool* pair) {
+  if (!x || !x->data) return SNN_ERR_INVALID_ARG;
+  if (!aligned16(x->data)) return SNN_ERR_ALIGNMENT;
+  const int64_t ext[2] = {d->B, d->T}, str[2] = {x->stride_b, x->stride_t};
+  for (int i = 0; i < 2; ++i) {
+    if (ext[i] <= 1) continue;
+    if (str[i] <= 0 || str[i] >= (int64_t(1) << 38)) return SNN_ERR_INVALID_ARG;
+    if (str[i] % 2) *pair = false;
+  }
+  out->data = x->data;
+  out->sb = d->B > 1 ? x->stride_b : 0;
+  out->st = d->T > 1 ? x->stride_t : 0;
+  return SNN_OK;
+}
+inline snn_status_t take(const snn_sscan_desc* d, const snn_bthd* x, Mat* out) {
+  if (!x || !x->data) return SNN_ERR_INVALID_ARG;
+  if (!aligned16(x->data)) return SNN_ERR_ALIGNMENT;
+  const int64_t ext[3] = {d->B, d->T, d->G}, str[3] = {x->stride_b, x->stride_t, x->stride_h};
+  for (int i = 0; i < 3; ++i)
+    if (ext[i] > 1 && (str[i] <= 0 || str[i] >= (int64_t(1) << 38))) return SNN_ERR_INVALID_ARG;
+  out->data = x->data;
+  out->sb = d->B > 1 ? x->stride_b : 0;
+  out->st = d->T > 1 ? x->stride_t : 0;
+  out->sg = d->G > 1 ? x->stride_h : 0;
+  return SNN_OK;
+}
+
+inline Args base_args(const snn_sscan_desc* d) {
+  Args g = {};
+  g.B = (int)d->B;
+  g.T = (int)d->T;
+  g.D = (int)d->D;
+  g.N = (int)d->N;
+  g.G = (int)d->G;
+  g.Dg = (int)(d->D / d->G);
+  g.softplus = d->softplus;
+  g.P = (g.N + kStates - 1) / kStates;
+  g.pairs = (g.Dg + 1) / 2;
+  return g;
+}
+
+// How the axis is cut, from the shape alone.
+struct Plan {
+  int spans, span;
+};
+// What the kernels of a call need beside its tensors.
+inline size_t ends_bytes(const Args& g, int spans) {
+  return round256((size_t)spans * g.B * g.G * g.pairs * g.P * 2 * kStates * sizeof(float));
+}
+inline size_t sums_bytes(const Args& g, int spans) {
+  return round256((size_t)spans * g.B * g.G * g.pairs * sizeof(float2));
+}
+
+}  // namespace sscan
+}  // namespace snn

@@ -90,6 +90,36 @@ class Rows(ctypes.Structure):
     _fields_ = [("data", ctypes.c_void_p), ("ld", ctypes.c_int64)]
 
 
+class SscanDesc(ctypes.Structure):
+    """Mirror of snn_sscan_desc."""
+    _fields_ = [
+        ("B", ctypes.c_int64), ("T", ctypes.c_int64), ("D", ctypes.c_int64),
+        ("N", ctypes.c_int64), ("G", ctypes.c_int64),
+        ("dtype", ctypes.c_int32), ("softplus", ctypes.c_int32), ("reserved", ctypes.c_uint32 * 2),
+    ]
+
+
+class ConvDesc(ctypes.Structure):
+    """Mirror of snn_conv_desc."""
+    _fields_ = [
+        ("B", ctypes.c_int64), ("T", ctypes.c_int64), ("C", ctypes.c_int64), ("W", ctypes.c_int64),
+        ("dtype", ctypes.c_int32), ("act", ctypes.c_int32), ("reserved", ctypes.c_uint32 * 2),
+    ]
+
+
+class LayerNormDesc(ctypes.Structure):
+    """Mirror of snn_layer_norm_desc."""
+    _fields_ = [
+        ("M", ctypes.c_int64), ("N", ctypes.c_int64), ("dtype", ctypes.c_int32),
+        ("res_dtype", ctypes.c_int32), ("eps", ctypes.c_float), ("reserved", ctypes.c_uint32),
+    ]
+
+
+class Btc(ctypes.Structure):
+    """Mirror of snn_btc."""
+    _fields_ = [("data", ctypes.c_void_p), ("stride_b", ctypes.c_int64), ("stride_t", ctypes.c_int64)]
+
+
 _P = ctypes.c_void_p
 _SIGS = {
     "snn_status_string": ([ctypes.c_int], ctypes.c_char_p),
@@ -137,6 +167,22 @@ _SIGS = {
     "snn_block_norm_workspace_bytes": ([ctypes.c_int64] * 2, ctypes.c_size_t),
     "snn_block_norm_fwd": ([_P] * 10, ctypes.c_int),
     "snn_block_norm_bwd": ([_P] * 16 + [ctypes.c_size_t, _P], ctypes.c_int),
+    "snn_sscan_desc_size": ([], ctypes.c_size_t),
+    "snn_selective_scan_workspace_bytes": ([_P, ctypes.c_int], ctypes.c_size_t),
+    "snn_selective_scan_ckpt_elems": ([_P], ctypes.c_int64),
+    "snn_selective_scan_fwd": ([_P] * 13 + [ctypes.c_int64] + [_P] * 3 + [ctypes.c_size_t, _P],
+                               ctypes.c_int),
+    "snn_selective_scan_bwd": ([_P] * 23 + [ctypes.c_size_t, _P], ctypes.c_int),
+    "snn_selective_scan_step": ([_P] * 11 + [ctypes.c_int64] + [_P] * 2, ctypes.c_int),
+    "snn_conv_desc_size": ([], ctypes.c_size_t),
+    "snn_causal_conv_workspace_bytes": ([_P], ctypes.c_size_t),
+    "snn_causal_conv_fwd": ([_P] * 8 + [ctypes.c_int64] + [_P] * 2, ctypes.c_int),
+    "snn_causal_conv_bwd": ([_P] * 13 + [ctypes.c_size_t, _P], ctypes.c_int),
+    "snn_causal_conv_step": ([_P] * 6 + [ctypes.c_int64] + [_P] * 2, ctypes.c_int),
+    "snn_layer_norm_desc_size": ([], ctypes.c_size_t),
+    "snn_layer_norm_workspace_bytes": ([ctypes.c_int64] * 2, ctypes.c_size_t),
+    "snn_layer_norm_fwd": ([_P] * 7, ctypes.c_int),
+    "snn_layer_norm_bwd": ([_P] * 9 + [ctypes.c_size_t, _P], ctypes.c_int),
     "snn_adamw_step": ([ctypes.c_int64] + [_P] * 5 + [ctypes.c_float] * 5 + [ctypes.c_int64] +
                        [_P, _P], ctypes.c_int),
 }
@@ -683,6 +729,319 @@ def snn_block_norm_bwd(r_out, a, z, w_post, res_scale, w_pre, grad_r_out, grad_y
         par("w_pre", w_pre), gro, gy, gr, ga, gz, par("grad_w_post", grad_w_post),
         par("grad_scale", grad_scale), par("grad_w_pre", grad_w_pre), _ptr(ws),
         ws.numel() * ws.element_size() if ws is not None else 0, _stream(stream)), w)
+
+
+# Tensors of the selective scan, the causal convolution and the layer norm: all on one
+# device, which has to be the current one (its stream takes the launches).
+
+def _device(where, t):
+    if not t.is_cuda or t.device.index != torch.cuda.current_device():
+        raise ValueError(f"{where}: tensors must be on the current CUDA device, not {t.device}")
+    return t.device
+
+
+def _on(where, name, t, shape, dtype, device):
+    if t.shape != shape or t.dtype != dtype or t.device != device:
+        raise ValueError(f"{where}: {name} must be a {dtype} tensor of shape {shape} on {device}")
+
+
+def _btc(where, name, t, shape, dtype, device):
+    """The words of snn_btc for a [B, T, C] tensor (a [B, C] one for a single
+    token) with contiguous C, or for None."""
+    if t is None:
+        return 0, 0, 0
+    _on(where, name, t, shape, dtype, device)
+    st = t.stride()
+    if st[-1] != 1 and shape[-1] > 1:
+        raise ValueError(f"{where}: {name} must have a contiguous last dimension")
+    return t.data_ptr(), st[0], st[-2]
+
+
+def _btgn(where, name, t, shape, dtype, device):
+    """The words of snn_bthd for a [B, T, G, N] tensor (a [B, G, N] one for a single
+    token) with contiguous N."""
+    _on(where, name, t, shape, dtype, device)
+    st = t.stride()
+    if st[-1] != 1 and shape[-1] > 1:
+        raise ValueError(f"{where}: {name} must have a contiguous last dimension")
+    return t.data_ptr(), st[0], st[1], st[-2]
+
+
+def _whole(where, name, t, shape, dtype, device):
+    """Pointer of a contiguous tensor, or None."""
+    if t is None:
+        return None
+    _on(where, name, t, shape, dtype, device)
+    if not t.is_contiguous():
+        raise ValueError(f"{where}: {name} must be contiguous")
+    return t.data_ptr()
+
+
+@functools.lru_cache(maxsize=64)
+def _layout(sizes):
+    """(pack, array type, offsets) of structures of these many 64-bit words."""
+    n, at = sum(sizes), [0]
+    for k in sizes[:-1]:
+        at.append(at[-1] + 8 * k)
+    return struct.Struct(f"{n}q").pack, ctypes.c_int64 * n, tuple(at)
+
+
+def _structs(*parts):
+    """The parts' words in one array, and the address of each part (None for an
+    absent tensor)."""
+    pack, array, offsets = _layout(tuple(map(len, parts)))
+    array = array.from_buffer_copy(pack(*[w for p in parts for w in p]))
+    base = ctypes.addressof(array)
+    return array, [base + o if p[0] else None for o, p in zip(offsets, parts)]
+
+
+def _ws(where, ws, device):
+    """(pointer, bytes) of a workspace, or of None."""
+    if ws is None:
+        return None, 0
+    if ws.device != device or not ws.is_contiguous():
+        raise ValueError(f"{where}: ws must be a contiguous tensor on {device}")
+    return ws.data_ptr(), ws.numel() * ws.element_size()
+
+
+@functools.lru_cache(maxsize=1024)
+def _sscan_desc(where, B, T, D, N, G, dtype, softplus):
+    code = _TORCH_DTYPE_CODE.get(dtype)
+    if code is None:
+        raise ValueError(f"{where}: dtype {dtype}")
+    d = SscanDesc(B, T, D, N, G, code, 1 if softplus else 0)
+    return d, ctypes.addressof(d)
+
+
+def _places_of(where, slots, B, states, device):
+    """(slots pointer, number of places) of states whose first dimension is the places."""
+    places = [s.shape[0] for s in states if s is not None]
+    n = places[0] if places else B
+    if any(p != n for p in places):
+        raise ValueError(f"{where}: the states differ in places")
+    if slots is None:
+        if n != B:
+            raise ValueError(f"{where}: without slots the states have one place per sequence")
+        return None, n
+    return _whole(where, "slots", slots, (B,), torch.int32, device), n
+
+
+@functools.lru_cache(maxsize=1024)
+def snn_selective_scan_workspace_bytes(B, T, D, N, G=1, backward=False) -> int:
+    d = SscanDesc(B, T, D, N, G)
+    return load_library().snn_selective_scan_workspace_bytes(ctypes.byref(d), 1 if backward else 0)
+
+
+@functools.lru_cache(maxsize=1024)
+def snn_selective_scan_ckpt_elems(B, T, D, N, G=1) -> int:
+    d = SscanDesc(B, T, D, N, G)
+    return load_library().snn_selective_scan_ckpt_elems(ctypes.byref(d))
+
+
+def snn_selective_scan_fwd(u, delta, A, B, C, y, ws, D=None, z=None, delta_bias=None, softplus=True,
+                           seq_lens=None, state_in=None, state_out=None, slots=None, ckpt=None,
+                           stream=None):
+    """Selective scan over whole sequences, s = softplus(delta + delta_bias), h_t =
+    exp(s A) h_{t-1} + s u B and y = (C h + D u) silu(z): u, delta, z, y [B, T, D] and
+    B, C [B, T, G, N] of one type (fp32, bf16 or fp16, any strides with a contiguous
+    last dimension); A [D, N], D and delta_bias [D], states [places, D, N] fp32.
+    seq_lens and slots: int32 [B].  ws: snn_selective_scan_workspace_bytes of the shape;
+    ckpt: fp32, snn_selective_scan_ckpt_elems of the shape, for the backward."""
+    w = "snn_selective_scan_fwd"
+    dev, (nB, T, nD), (N, G), dt = _device(w, u), u.shape, (A.shape[-1], B.shape[2]), u.dtype
+    _, d = _sscan_desc(w, nB, T, nD, N, G, dt, bool(softplus))
+    ps, n = _places_of(w, slots, nB, (state_in, state_out), dev)
+    seq, grp, f32 = (nB, T, nD), (nB, T, G, N), torch.float32
+    keep, (pu, pd, pB, pC, pz, py) = _structs(
+        _btc(w, "u", u, seq, dt, dev), _btc(w, "delta", delta, seq, dt, dev),
+        _btgn(w, "B", B, grp, dt, dev), _btgn(w, "C", C, grp, dt, dev), _btc(w, "z", z, seq, dt, dev),
+        _btc(w, "y", y, seq, dt, dev))
+    if ckpt is not None and ckpt.numel() < snn_selective_scan_ckpt_elems(nB, T, nD, N, G):
+        raise ValueError(f"{w}: ckpt is smaller than snn_selective_scan_ckpt_elems")
+    pw, nw = _ws(w, ws, dev)
+    _check(load_library().snn_selective_scan_fwd(
+        d, pu, pd, _whole(w, "A", A, (nD, N), f32, dev), pB, pC, _whole(w, "D", D, (nD,), f32, dev), pz,
+        _whole(w, "delta_bias", delta_bias, (nD,), f32, dev),
+        _whole(w, "seq_lens", seq_lens, (nB,), torch.int32, dev),
+        _whole(w, "state_in", state_in, (n, nD, N), f32, dev),
+        _whole(w, "state_out", state_out, (n, nD, N), f32, dev), ps, n,
+        None if ckpt is None else _whole(w, "ckpt", ckpt, ckpt.shape, f32, dev), py, pw, nw,
+        _stream(stream)), w)
+
+
+def snn_selective_scan_bwd(u, delta, A, B, C, grad_y, ckpt, grad_u, grad_delta, grad_A, grad_B, grad_C,
+                           ws, D=None, z=None, delta_bias=None, softplus=True, seq_lens=None,
+                           grad_state_out=None, grad_D=None, grad_z=None, grad_delta_bias=None,
+                           grad_state_in=None, stream=None):
+    """Gradients of snn_selective_scan_fwd from the checkpoints that it left (states
+    [B, D, N], in sequence order); grad_z is given exactly when z is.  ws:
+    snn_selective_scan_workspace_bytes(..., backward=True)."""
+    w = "snn_selective_scan_bwd"
+    dev, (nB, T, nD), (N, G), dt = _device(w, u), u.shape, (A.shape[-1], B.shape[2]), u.dtype
+    _, d = _sscan_desc(w, nB, T, nD, N, G, dt, bool(softplus))
+    seq, grp, f32 = (nB, T, nD), (nB, T, G, N), torch.float32
+    keep, (pu, pd, pB, pC, pz, pgy, pgu, pgd, pgB, pgC, pgz) = _structs(
+        _btc(w, "u", u, seq, dt, dev), _btc(w, "delta", delta, seq, dt, dev),
+        _btgn(w, "B", B, grp, dt, dev), _btgn(w, "C", C, grp, dt, dev), _btc(w, "z", z, seq, dt, dev),
+        _btc(w, "grad_y", grad_y, seq, dt, dev), _btc(w, "grad_u", grad_u, seq, dt, dev),
+        _btc(w, "grad_delta", grad_delta, seq, dt, dev), _btgn(w, "grad_B", grad_B, grp, dt, dev),
+        _btgn(w, "grad_C", grad_C, grp, dt, dev), _btc(w, "grad_z", grad_z, seq, dt, dev))
+    if ckpt.numel() < snn_selective_scan_ckpt_elems(nB, T, nD, N, G):
+        raise ValueError(f"{w}: ckpt is smaller than snn_selective_scan_ckpt_elems")
+    flat = lambda name, t, shape: _whole(w, name, t, shape, f32, dev)
+    pw, nw = _ws(w, ws, dev)
+    _check(load_library().snn_selective_scan_bwd(
+        d, pu, pd, flat("A", A, (nD, N)), pB, pC, flat("D", D, (nD,)), pz,
+        flat("delta_bias", delta_bias, (nD,)), _whole(w, "seq_lens", seq_lens, (nB,), torch.int32, dev),
+        flat("ckpt", ckpt, ckpt.shape), pgy, flat("grad_state_out", grad_state_out, (nB, nD, N)), pgu, pgd,
+        flat("grad_A", grad_A, (nD, N)), pgB, pgC, flat("grad_D", grad_D, (nD,)), pgz,
+        flat("grad_delta_bias", grad_delta_bias, (nD,)),
+        flat("grad_state_in", grad_state_in, (nB, nD, N)), pw, nw, _stream(stream)), w)
+
+
+def snn_selective_scan_step(u, delta, A, B, C, state, y, D=None, z=None, delta_bias=None, softplus=True,
+                            slots=None, stream=None):
+    """One token of each sequence (decoding): u, delta, z, y [B, D], B and C [B, G, N];
+    state fp32 [places, D, N] is updated in place at slots (int32 [B]; default b; outside the
+    range: an empty place of the batch, whose y is zero)."""
+    w = "snn_selective_scan_step"
+    dev, (nB, nD), (N, G), dt = _device(w, u), u.shape, (A.shape[-1], B.shape[1]), u.dtype
+    _, d = _sscan_desc(w, nB, 1, nD, N, G, dt, bool(softplus))
+    seq, grp, f32, n = (nB, nD), (nB, G, N), torch.float32, state.shape[0]
+    keep, (pu, pd, pB, pC, pz, py) = _structs(
+        _btc(w, "u", u, seq, dt, dev), _btc(w, "delta", delta, seq, dt, dev),
+        _btgn(w, "B", B, grp, dt, dev), _btgn(w, "C", C, grp, dt, dev), _btc(w, "z", z, seq, dt, dev),
+        _btc(w, "y", y, seq, dt, dev))
+    _check(load_library().snn_selective_scan_step(
+        d, pu, pd, _whole(w, "A", A, (nD, N), f32, dev), pB, pC, _whole(w, "D", D, (nD,), f32, dev), pz,
+        _whole(w, "delta_bias", delta_bias, (nD,), f32, dev), _whole(w, "state", state, (n, nD, N), f32, dev),
+        _whole(w, "slots", slots, (nB,), torch.int32, dev), n, py, _stream(stream)), w)
+
+
+@functools.lru_cache(maxsize=1024)
+def _conv_desc(where, B, T, C, W, dtype, act):
+    code = _TORCH_DTYPE_CODE.get(dtype)
+    if code is None:
+        raise ValueError(f"{where}: dtype {dtype}")
+    if act not in GATE_CODE:
+        raise ValueError(f"{where}: act {act!r}")
+    d = ConvDesc(B, T, C, W, code, GATE_CODE[act])
+    return d, ctypes.addressof(d)
+
+
+@functools.lru_cache(maxsize=1024)
+def snn_causal_conv_workspace_bytes(B, T, C, W) -> int:
+    d = ConvDesc(B, T, C, W)
+    return load_library().snn_causal_conv_workspace_bytes(ctypes.byref(d))
+
+
+def snn_causal_conv_fwd(x, w, bias, y, act="none", seq_lens=None, state_in=None, state_out=None,
+                        slots=None, stream=None):
+    """Causal convolution of each channel over W = 2, 3 or 4 tokens, y_t = act(bias +
+    sum_j w[j] x_{t-W+1+j}): x, y [B, T, C] (fp32, bf16 or fp16, any strides with contiguous C),
+    w fp32 [C, W], bias fp32 [C] or None, act "none" or "silu".  states [places, W-1, C] of
+    x's type hold the inputs before the sequence, with slots int32 [B] naming the places."""
+    f = "snn_causal_conv_fwd"
+    dev, (B, T, C), W, dt = _device(f, x), x.shape, w.shape[-1], x.dtype
+    _, d = _conv_desc(f, B, T, C, W, dt, act)
+    ps, n = _places_of(f, slots, B, (state_in, state_out), dev)
+    keep, (px, py) = _structs(_btc(f, "x", x, (B, T, C), dt, dev), _btc(f, "y", y, (B, T, C), dt, dev))
+    _check(load_library().snn_causal_conv_fwd(
+        d, px, _whole(f, "w", w, (C, W), torch.float32, dev), _whole(f, "bias", bias, (C,), torch.float32, dev),
+        _whole(f, "seq_lens", seq_lens, (B,), torch.int32, dev),
+        _whole(f, "state_in", state_in, (n, W - 1, C), dt, dev),
+        _whole(f, "state_out", state_out, (n, W - 1, C), dt, dev), ps, n, py, _stream(stream)), f)
+
+
+def snn_causal_conv_bwd(x, w, bias, grad_y, grad_x, grad_w, grad_bias, ws, act="none", seq_lens=None,
+                        state_in=None, grad_state_out=None, grad_state_in=None, stream=None):
+    """Gradients of snn_causal_conv_fwd (states [B, W-1, C], in sequence order); an output
+    None is not computed.  ws: snn_causal_conv_workspace_bytes (None without grad_w and
+    grad_bias)."""
+    f = "snn_causal_conv_bwd"
+    dev, (B, T, C), W, dt = _device(f, x), x.shape, w.shape[-1], x.dtype
+    _, d = _conv_desc(f, B, T, C, W, dt, act)
+    seq = (B, T, C)
+    keep, (px, pgy, pgx) = _structs(_btc(f, "x", x, seq, dt, dev), _btc(f, "grad_y", grad_y, seq, dt, dev),
+                                    _btc(f, "grad_x", grad_x, seq, dt, dev))
+    f32 = lambda name, t, shape: _whole(f, name, t, shape, torch.float32, dev)
+    state = lambda name, t: _whole(f, name, t, (B, W - 1, C), dt, dev)
+    pw, nw = _ws(f, ws, dev)
+    _check(load_library().snn_causal_conv_bwd(
+        d, px, f32("w", w, (C, W)), f32("bias", bias, (C,)),
+        _whole(f, "seq_lens", seq_lens, (B,), torch.int32, dev), state("state_in", state_in), pgy,
+        state("grad_state_out", grad_state_out), pgx, f32("grad_w", grad_w, (C, W)),
+        f32("grad_bias", grad_bias, (C,)), state("grad_state_in", grad_state_in), pw, nw,
+        _stream(stream)), f)
+
+
+def snn_causal_conv_step(x, w, bias, state, y, act="none", slots=None, stream=None):
+    """One token of each sequence (decoding): x, y [B, C]; state [places, W-1, C] of x's
+    type loses its oldest input and takes x, at slots (int32 [B]; default b; outside the
+    range: an empty place of the batch, whose y is zero)."""
+    f = "snn_causal_conv_step"
+    dev, (B, C), W, dt = _device(f, x), x.shape, w.shape[-1], x.dtype
+    _, d = _conv_desc(f, B, 1, C, W, dt, act)
+    n = state.shape[0]
+    keep, (px, py) = _structs(_btc(f, "x", x, (B, C), dt, dev), _btc(f, "y", y, (B, C), dt, dev))
+    _check(load_library().snn_causal_conv_step(
+        d, px, _whole(f, "w", w, (C, W), torch.float32, dev), _whole(f, "bias", bias, (C,), torch.float32, dev),
+        _whole(f, "state", state, (n, W - 1, C), dt, dev), _whole(f, "slots", slots, (B,), torch.int32, dev), n,
+        py, _stream(stream)), f)
+
+
+@functools.lru_cache(maxsize=1024)
+def snn_layer_norm_workspace_bytes(M: int, N: int) -> int:
+    return load_library().snn_layer_norm_workspace_bytes(M, N)
+
+
+@functools.lru_cache(maxsize=1024)
+def _layer_norm_desc(where, M, N, dtype, res_dtype, eps):
+    for dt in (dtype, res_dtype):
+        if dt not in _TORCH_DTYPE_CODE:
+            raise ValueError(f"{where}: dtype {dt}")
+    d = LayerNormDesc(M, N, _TORCH_DTYPE_CODE[dtype], _TORCH_DTYPE_CODE[res_dtype], eps)
+    return d, ctypes.addressof(d)
+
+
+def _matrix(where, name, t, shape, dtype, device):
+    """The words of snn_rows for an [M, N] matrix with contiguous rows, or for None."""
+    if t is None:
+        return 0, 0
+    _on(where, name, t, shape, dtype, device)
+    ld, inner = t.stride()
+    if inner != 1 and shape[1] > 1:
+        raise ValueError(f"{where}: {name} must have contiguous rows")
+    return t.data_ptr(), ld
+
+
+def snn_layer_norm_fwd(x, w, b, y, stats=None, eps=1e-5, stream=None):
+    """y = (x - mean) rsqrt(var + eps) w + b over the rows of [M, N] matrices (rows any stride
+    apart; y of x's type, or 16-bit of an fp32 x); w (None: ones) and b (None: zeros) fp32
+    [N]; stats fp32 [2, M] for the backward, or None."""
+    f = "snn_layer_norm_fwd"
+    dev, (M, N) = _device(f, x), x.shape
+    _, d = _layer_norm_desc(f, M, N, y.dtype, x.dtype, float(eps))
+    keep, (px, py) = _structs(_matrix(f, "x", x, (M, N), x.dtype, dev), _matrix(f, "y", y, (M, N), y.dtype, dev))
+    f32 = lambda name, t, shape: _whole(f, name, t, shape, torch.float32, dev)
+    _check(load_library().snn_layer_norm_fwd(d, px, f32("w", w, (N,)), f32("b", b, (N,)), py,
+                                             f32("stats", stats, (2, M)), _stream(stream)), f)
+
+
+def snn_layer_norm_bwd(x, w, stats, grad_y, grad_x, grad_w, grad_b, ws, stream=None):
+    """Gradients of snn_layer_norm_fwd from its stats; an output None is not computed.  ws:
+    snn_layer_norm_workspace_bytes(M, N) (None without grad_w and grad_b)."""
+    f = "snn_layer_norm_bwd"
+    dev, (M, N) = _device(f, x), x.shape
+    _, d = _layer_norm_desc(f, M, N, grad_y.dtype, x.dtype, 1.0)
+    keep, (px, pgy, pgx) = _structs(
+        _matrix(f, "x", x, (M, N), x.dtype, dev), _matrix(f, "grad_y", grad_y, (M, N), grad_y.dtype, dev),
+        _matrix(f, "grad_x", grad_x, (M, N), x.dtype, dev))
+    f32 = lambda name, t, shape: _whole(f, name, t, shape, torch.float32, dev)
+    pw, nw = _ws(f, ws, dev)
+    _check(load_library().snn_layer_norm_bwd(
+        d, px, f32("w", w, (N,)), f32("stats", stats, (2, M)), pgy, pgx, f32("grad_w", grad_w, (N,)),
+        f32("grad_b", grad_b, (N,)), pw, nw, _stream(stream)), f)
 
 
 # ---------------------------------------------------------------------------
