@@ -61,7 +61,7 @@ def scan_forward(u, delta, A, B, C, D=None, z=None, bias=None, softplus=True, le
 
 def scan_backward(u, delta, A, B, C, gy, D=None, z=None, bias=None, softplus=True, lens=None, state=None,
                   gstate=None, positive=False):
-    """Gradients of <y, gy> + <h, gstate> as a dict."""
+    """Gradients of <y, gy> + <h, gstate> as a dict ("s": that of the step, before softplus)."""
     s, raw = step_sizes(delta, bias, softplus)
     gate, slope = _gate(z)
     k = _p if positive else _f
@@ -102,6 +102,7 @@ def scan_backward(u, delta, A, B, C, gy, D=None, z=None, bias=None, softplus=Tru
             o["u"][b, t] = st * w + skip * dy
             o["delta"][b, t] = ut * w + (q * A_size).sum(-1)
         o["state"][b] = g
+    o["s"] = o["delta"].copy()
     if softplus:
         o["delta"] *= sigmoid(raw)
     o["bias"] = o["delta"].sum((0, 1))

@@ -275,6 +275,18 @@ __global__ void __launch_bounds__(kThreads) scan_bwd(const Args g) {
         store_states(g.grad_state_in + ((int64_t)b * g.D + c) * g.N, g.N, pl * kStates, second, v);
       }
     }
+    // places past the sequence's end
+    if (row < R && pair0 + pr < g.pairs) {
+      const int c = grp * g.Dg + 2 * (pair0 + pr);
+      const bool second = 2 * (pair0 + pr) + 1 < g.Dg;
+      for (int now = first + tiles * kCkpt + row; now < last; now += R) {
+        const int64_t chan = c;
+        put_pair(static_cast<T*>(g.gu.data) + b * g.gu.sb + now * g.gu.st + chan, f2(0.0f), pairs_ok, second);
+        put_pair(static_cast<T*>(g.gdelta.data) + b * g.gdelta.sb + now * g.gdelta.st + chan, f2(0.0f), pairs_ok, second);
+        if (g.z.data)
+          put_pair(static_cast<T*>(g.gz.data) + b * g.gz.sb + now * g.gz.st + chan, f2(0.0f), pairs_ok, second);
+      }
+    }
     // grad_D and grad_delta_bias: the rows of a pair, in order
     __syncthreads();
     if (row == 0 && pr < cp && pair0 + pr < g.pairs) {
