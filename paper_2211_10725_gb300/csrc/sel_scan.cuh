@@ -5,8 +5,10 @@
 //
 // A thread holds four states of two neighbouring channels of a group (a pair), in
 // pairs of floats: one instruction serves both channels.  P = ceil(N / 4) threads
-// side by side hold a pair's states.  The decay of a span of tokens is
-// exp(A sum s), so a cut axis hands on one sum a channel beside the states.
+// side by side hold a pair's states, so that a warp has 32 / P pairs.  It works alone: what
+// its threads exchange lies in shared memory of its own, and no barrier joins it to
+// another warp.  The decay of a span of tokens is exp(A sum s), so a cut axis hands on
+// one sum a channel beside the states.
 #pragma once
 
 #include <cuda_bf16.h>
@@ -15,6 +17,7 @@
 
 #include <cmath>
 #include <cstdint>
+#include <initializer_list>
 
 #include "launch.cuh"
 #include "scan_host.cuh"
@@ -26,7 +29,7 @@ namespace sscan {
 
 constexpr int kStates = 4;        // of a channel in a thread
 constexpr int kMaxN = 64;
-constexpr int kCkpt = 8;          // tokens between checkpoints
+constexpr int kTile = 8;          // tokens of a tile, and between checkpoints
 constexpr float kLog2E = 1.44269504088896340736f;
 
 struct Seq {  // [B, T, channels]
@@ -42,6 +45,7 @@ struct Args {
   int B, T, D, N, G, Dg;   // Dg channels of a group
   int softplus;
   int pair_ok;             // channel pairs lie on their own boundaries in every tensor
+  int quads;               // so do fours of states of B and C
   int P;                   // threads of a pair
   int pairs;               // of a group
   int spans, span;         // cuts of the axis, tokens of each
@@ -79,22 +83,32 @@ __device__ __forceinline__ float rcp(float x) {
   asm("rcp.approx.ftz.f32 %0, %0;" : "+f"(x));
   return x;
 }
+__device__ __forceinline__ float2 rcp(float2 x) { return make_float2(rcp(x.x), rcp(x.y)); }
 
-// log(1 + e^x) = max(x, 0) + log(1 + e), e = e^-|x|, with the area tangent's
-// series: log(1 + e) = 2 atanh(r), r = e / (2 + e) <= 1/3, whose terms past r^13
-// are below 2^-25 of it.
-__device__ __forceinline__ float softplus(float x) {
-  const float e = expf(-fabsf(x));
-  const float r = e * rcp(2.0f + e), q = r * r;
-  float p = 1.0f / 15.0f;
-  p = fmaf(p, q, 1.0f / 13.0f);
-  p = fmaf(p, q, 1.0f / 11.0f);
-  p = fmaf(p, q, 1.0f / 9.0f);
-  p = fmaf(p, q, 1.0f / 7.0f);
-  p = fmaf(p, q, 1.0f / 5.0f);
-  p = fmaf(p, q, 1.0f / 3.0f);
-  p = fmaf(p * q, r, r);
-  return fmaf(2.0f, p, fmaxf(x, 0.0f));
+// softplus and its slope.  With e = e^-|x|: log(1 + e^x) = max(x, 0) + log(1 + e), and
+// log(1 + e) = 2 atanh(r), r = e / (2 + e) <= 1/3: the area tangent's series, whose terms
+// past r^15 are below 2^-27 of it.  The slope is 1 / (1 + e) or e / (1 + e).  e from the
+// power of two, with what the product |x| log2(e) was rounded by put back.
+__device__ __forceinline__ float2 softplus(float2 x, float2* slope) {
+  constexpr float kLog2ELow = 1.92596303e-8f, kLn2 = 0.69314718055994530942f;
+  const float2 a = make_float2(-fabsf(x.x), -fabsf(x.y));
+  const float2 t = mul2(a, f2(kLog2E));
+  const float2 rest = fma2(a, f2(kLog2ELow), fma2(a, f2(kLog2E), make_float2(-t.x, -t.y)));
+  float2 e = ex2(t);
+  e = fma2(e, mul2(rest, f2(kLn2)), e);
+  const float2 r = mul2(e, rcp(add2(e, f2(2.0f)))), q = mul2(r, r);
+  float2 p = fma2(q, f2(1.0f / 15.0f), f2(1.0f / 13.0f));
+  p = fma2(p, q, f2(1.0f / 11.0f));
+  p = fma2(p, q, f2(1.0f / 9.0f));
+  p = fma2(p, q, f2(1.0f / 7.0f));
+  p = fma2(p, q, f2(1.0f / 5.0f));
+  p = fma2(p, q, f2(1.0f / 3.0f));
+  p = fma2(mul2(p, q), r, r);
+  if (slope) {
+    const float2 one = rcp(add2(e, f2(1.0f)));
+    *slope = mul2(make_float2(x.x >= 0.0f ? 1.0f : e.x, x.y >= 0.0f ? 1.0f : e.y), one);
+  }
+  return fma2(f2(2.0f), p, make_float2(fmaxf(x.x, 0.0f), fmaxf(x.y, 0.0f)));
 }
 
 // 1 / (1 + e^-x).  Results rounded to 16 bits take the approximate power of
@@ -106,7 +120,8 @@ __device__ __forceinline__ float sigmoid(float x) {
 }
 template <typename T>
 __device__ __forceinline__ float2 sigmoid(float2 x) {
-  return make_float2(sigmoid<T>(x.x), sigmoid<T>(x.y));
+  if constexpr (sizeof(T) == 4) return make_float2(sigmoid<T>(x.x), sigmoid<T>(x.y));
+  else return rcp(add2(ex2(mul2(x, f2(-kLog2E))), f2(1.0f)));
 }
 
 // The channels c and c + 1 of a token as they lie in memory.
@@ -152,10 +167,11 @@ __device__ __forceinline__ void put_pair(T* p, float2 v, bool pair, bool second)
   }
 }
 
-// s of the two channels of a raw delta.
-__device__ __forceinline__ float2 step_of(float2 raw, float2 bias, bool soft) {
-  raw = add2(raw, bias);
-  return soft ? make_float2(softplus(raw.x), softplus(raw.y)) : raw;
+// s of the two channels of a delta with its bias, and its slope (if asked for).
+__device__ __forceinline__ float2 step_of(float2 raw, bool soft, float2* slope = nullptr) {
+  if (soft) return softplus(raw, slope);
+  if (slope) *slope = f2(1.0f);
+  return raw;
 }
 
 // A thread's states of its pair in an fp32 [.., D, N] array (element (c, n) at
@@ -189,6 +205,32 @@ __device__ __forceinline__ void load_own(const float* p, float2 v[kStates]) {
 __device__ __forceinline__ void store_own(float* p, const float2 v[kStates]) {
   reinterpret_cast<float4*>(p)[0] = make_float4(v[0].x, v[0].y, v[1].x, v[1].y);
   reinterpret_cast<float4*>(p)[1] = make_float4(v[2].x, v[2].y, v[3].x, v[3].y);
+}
+
+// Tile of B or C in shared memory: each value twice (it meets both channels of a
+// pair), [kTile][P][4] float2; zero from token `stop` on and for absent states.  quads: the
+// states can be read in fours.
+template <typename T>
+__device__ __forceinline__ void load_tile(const Args& g, const Mat& m, float2* to, int P, int b, int grp, int t0,
+                                          int stop, int lane) {
+  const T* base = static_cast<const T*>(m.data) + b * m.sb + grp * m.sg + t0 * m.st;
+  if (g.quads) {
+#pragma unroll 2
+    for (int i = lane; i < kTile * P; i += 32) {
+      const int tok = i / P, n = (i - tok * P) * kStates;
+      float v[kStates] = {0.0f, 0.0f, 0.0f, 0.0f};
+      if (t0 + tok < stop) Elem<T>::load4(base + tok * m.st + n, v);
+      reinterpret_cast<float4*>(to)[2 * i] = make_float4(v[0], v[0], v[1], v[1]);
+      reinterpret_cast<float4*>(to)[2 * i + 1] = make_float4(v[2], v[2], v[3], v[3]);
+    }
+  } else {
+    for (int i = lane; i < kTile * P * kStates; i += 32) {
+      const int tok = i / (P * kStates), n = i - tok * (P * kStates);
+      float v = 0.0f;
+      if (n < g.N && t0 + tok < stop) v = Elem<T>::load1(base + tok * m.st + n);
+      to[i] = f2(v);
+    }
+  }
 }
 
 // ---------------------------------------------------------------------------
@@ -240,6 +282,13 @@ inline snn_status_t take(const snn_sscan_desc* d, const snn_bthd* x, Mat* out) {
   out->st = d->T > 1 ? x->stride_t : 0;
   out->sg = d->G > 1 ? x->stride_h : 0;
   return SNN_OK;
+}
+
+inline bool quads(const Args& g, std::initializer_list<const Mat*> ms) {
+  if (g.N % kStates) return false;
+  for (const Mat* m : ms)
+    if ((m->sb | m->st | m->sg) % kStates) return false;
+  return true;
 }
 
 inline Args base_args(const snn_sscan_desc* d) {

@@ -5,12 +5,12 @@
 //   w = sum_n gt B;  q = a_t gt h_{t-1};  r = sum_n q A
 //   grad_u = s w + D dy;   grad_delta = (u w + r) softplus'(delta + bias)
 //   grad_A = sum_t q s;    grad_D = sum_t dy u;   grad_z = grad_y (y before the gate) silu'(z)
-// A block goes backwards through its span of the axis in tiles of the checkpoints'
+// A warp goes backwards through its span of the axis in tiles of the checkpoints'
 // eight tokens, and in each tile in turns through its channel pairs: it takes the states
 // of a turn from the checkpoint through the tile (they stay in registers), then gamma
 // back through it.  A thread has the same states in every turn, so that grad_B and
 // grad_C of the tile gather in its registers over the turns and meet over the
-// threads once a tile; gamma and grad_A of every turn lie in shared memory.  The blocks' shares
+// threads once a tile; gamma and grad_A of every turn lie in shared memory.  The warps' shares
 // of grad_B, grad_C, grad_A, grad_D and grad_delta_bias are added by a second kernel in a
 // fixed order.
 #include "sel_scan.cuh"
@@ -19,65 +19,66 @@
 namespace snn {
 namespace sscan {
 
-constexpr int kAccStride = kThreads + 4;  // floats: rows of the threads' shares, apart by four banks
+constexpr int kTurns = 4;        // of a warp in a tile, at most
+constexpr int kAccStride = 36;   // floats between the rows of the threads' shares: 32 and four banks
 
 struct BwdPlan {
   Plan cut;
-  int per_block, blocks;  // turns of a block; blocks of a group
+  int per_block, blocks;  // turns of a warp; warps of a group
 };
 
 BwdPlan bwd_plan(const Args& g) {
   BwdPlan p;
-  const int turns = (int)ceil_div(g.pairs, kThreads / g.P);
-  p.per_block = turns < 4 ? turns : 4;
+  const int turns = (int)ceil_div(g.pairs, 32 / g.P);
+  p.per_block = turns < kTurns ? turns : kTurns;
   p.blocks = (int)ceil_div(turns, p.per_block);
-  p.cut = cut(g.T, (int64_t)g.B * g.G * p.blocks, kSms * 3);
+  p.cut = cut(g.T, (int64_t)g.B * g.G * p.blocks, kSms * 8, 3);
   return p;
 }
 
-// Shared memory: s and x, dy; B and C; the sums' parts (or the threads' shares of
-// grad_B and grad_C); what stays over the tiles of a span.
-size_t bwd_smem(const Args& g, int per_block) {
-  const int cp = kThreads / g.P;
-  const size_t parts = 3 * kCkpt * kThreads * sizeof(float2), acc = 32 * kAccStride * sizeof(float);
-  return (size_t)kCkpt * cp * (sizeof(float4) + sizeof(float2)) + 2 * (size_t)kCkpt * g.P * 2 * sizeof(float4) +
-         (parts > acc ? parts : acc) + (size_t)per_block * kThreads * (3 * 8 + 4) * sizeof(float);
+// Shared memory of a warp: s and x; slopes; dy; B and C; the sums' parts (or the threads'
+// shares of grad_B and grad_C); what stays over the tiles of a span.
+__host__ __device__ constexpr int bwd_smem(int P, int turns) {
+  return kTile * (32 / P) * (2 * (int)sizeof(float4) + (int)sizeof(float2)) +
+         2 * kTile * P * kStates * (int)sizeof(float2) + 3 * kTile * 32 * (int)sizeof(float2) +
+         turns * 32 * (3 * 8 + 4) * (int)sizeof(float);
 }
 
-template <typename T>
-__global__ void __launch_bounds__(kThreads) scan_bwd(const Args g) {
+template <typename T, int PT>
+__global__ void __launch_bounds__(32) scan_bwd(const Args g) {
   extern __shared__ __align__(16) unsigned char scan_smem[];
+  constexpr int kUnits = units_of(PT);
   grid_dep_wait();
-  const int P = g.P, cp = kThreads / P, R = kThreads / cp, N4 = kStates * P, M = g.per_block;
-  float4* const sx = reinterpret_cast<float4*>(scan_smem);         // [8][cp]: s, x
-  float4* const Bd = sx + kCkpt * cp;                              // [8][P][2]
-  float4* const Cd = Bd + kCkpt * P * 2;
-  float* const keep = reinterpret_cast<float*>(Cd + kCkpt * P * 2);  // [M][3][threads][8]: A, gamma, grad_A
-  float4* const keep2 = reinterpret_cast<float4*>(keep + M * 3 * kThreads * 8);  // [M][threads]: grad_D, grad_delta_bias
-  float2* const dys = reinterpret_cast<float2*>(keep2 + M * kThreads);  // [8][cp]
-  float2* const yp = dys + kCkpt * cp;                             // [8][threads]
-  float2* const wp = yp + kCkpt * kThreads;
-  float2* const rp = wp + kCkpt * kThreads;
+  const int P = PT ? PT : g.P, PW = 32 / P, R = 32 / PW, N4 = kStates * P, M = g.per_block, lane = threadIdx.x;
+  float4* const sx = reinterpret_cast<float4*>(scan_smem);         // [kTile][PW]: s, x
+  float4* const slopes = sx + kTile * PW;                          // [kTile][PW]: softplus', grad_y silu'
+  float2* const Bd = reinterpret_cast<float2*>(slopes + kTile * PW);  // [kTile][P][4]
+  float2* const Cd = Bd + kTile * N4;
+  float* const keep = reinterpret_cast<float*>(Cd + kTile * N4);   // [M][3][32][8]: A, gamma, grad_A
+  float4* const keep2 = reinterpret_cast<float4*>(keep + M * 3 * 32 * 8);  // [M][32]: grad_D, grad_delta_bias
+  float2* const yp = reinterpret_cast<float2*>(keep2 + M * 32);    // [kTile][32]
+  float2* const wp = yp + kTile * 32;
+  float2* const rp = wp + kTile * 32;
+  float2* const dys = rp + kTile * 32;                             // [kTile][PW]
   float* const acc = reinterpret_cast<float*>(yp);                 // [32][kAccStride]
 
-  const int turns = (g.pairs + cp - 1) / cp, nb = (turns + M - 1) / M;
+  const int turns = (g.pairs + PW - 1) / PW, nb = (turns + M - 1) / M;
   const int pb = blockIdx.x % nb, rest = blockIdx.x / nb, grp = rest % g.G, b = rest / g.G;
   const int span = blockIdx.y, len = seq_len(g, b), first = span * g.span;
   const int last = first + g.span < g.T ? first + g.span : g.T;
   const int stop = last < len ? last : len;
-  const int tiles = stop > first ? (stop - first + kCkpt - 1) / kCkpt : 0;
-  const int t = threadIdx.x, pl = t % P, pc = t / P;
-  const int pr = t % cp, row = t / cp;
-  const bool pairs_ok = g.pair_ok;
+  const int tiles = stop > first ? (stop - first + kTile - 1) / kTile : 0;
+  const int pl = lane % P, pc = lane / P, pr = lane % PW, row = lane / PW;
+  const bool pairs_ok = g.pair_ok, gate = g.z.data != nullptr;
   const int64_t own_all = (int64_t)g.B * g.G * g.pairs * P;
-  auto keep_at = [&](int m, int k) { return keep + ((m * 3 + k) * kThreads + t) * 8; };
+  auto keep_at = [&](int m, int k) { return keep + ((m * 3 + k) * 32 + lane) * 8; };
 
   for (int m = 0; m < M; ++m) {
-    const int pair = (pb * M + m) * cp + pc;
+    const int pair = (pb * M + m) * PW + pc;
     float2 A2[kStates], gam[kStates];
 #pragma unroll
     for (int q = 0; q < kStates; ++q) A2[q] = gam[q] = f2(0.0f);
-    if (pc < cp && pair < g.pairs) {
+    if (pc < PW && pair < g.pairs) {
       const int c = grp * g.Dg + 2 * pair;
       const bool second = 2 * pair + 1 < g.Dg;
       const int64_t own = (((int64_t)b * g.G + grp) * g.pairs + pair) * P + pl;
@@ -86,6 +87,7 @@ __global__ void __launch_bounds__(kThreads) scan_bwd(const Args g) {
       for (int q = 0; q < kStates; ++q) A2[q] = mul2(A2[q], f2(kLog2E));
       if (g.grad_state_out)
         load_states(g.grad_state_out + ((int64_t)b * g.D + c) * g.N, g.N, pl * kStates, second, gam);
+#pragma unroll 2
       for (int i = g.spans - 1; i > span; --i) {
         float2 e[kStates];
         load_own(g.ends + ((int64_t)i * own_all + own) * 2 * kStates, e);
@@ -99,172 +101,180 @@ __global__ void __launch_bounds__(kThreads) scan_bwd(const Args g) {
 #pragma unroll
     for (int q = 0; q < kStates; ++q) gam[q] = f2(0.0f);
     store_own(keep_at(m, 2), gam);
-    keep2[m * kThreads + t] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+    keep2[m * 32 + lane] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
   }
 
-  const int n_bc = t % N4, row_bc = t / N4, R_bc = kThreads / N4;
+  const int c0 = grp * g.Dg + 2 * (pb * M * PW + pr);   // the first turn's channel where tokens are loaded and stored
+  auto base = [&](const Seq& x) { return static_cast<T*>(x.data) + b * x.sb + c0; };
+  const T *const pu = base(g.u), *const pd = base(g.delta), *const pg = base(g.gy), *const pz = base(g.z);
+  T *const ou = base(g.gu), *const od = base(g.gdelta), *const oz = base(g.gz);
+  const int64_t ckpt_step = (int64_t)g.G * g.pairs * P * 2 * kStates;
+
   for (int tile = tiles - 1; tile >= 0; --tile) {
-    const int t0 = first + tile * kCkpt;
-    if (row_bc < R_bc) {
-      for (int tok = row_bc; tok < kCkpt; tok += R_bc) {
-        float vb = 0.0f, vc = 0.0f;
-        const int now = t0 + tok;
-        if (n_bc < g.N && now < stop) {
-          vb = Elem<T>::load1(static_cast<const T*>(g.Bm.data) + b * g.Bm.sb + now * g.Bm.st + grp * g.Bm.sg + n_bc);
-          vc = Elem<T>::load1(static_cast<const T*>(g.Cm.data) + b * g.Cm.sb + now * g.Cm.st + grp * g.Cm.sg + n_bc);
-        }
-        reinterpret_cast<float2*>(Bd)[tok * N4 + n_bc] = f2(vb);
-        reinterpret_cast<float2*>(Cd)[tok * N4 + n_bc] = f2(vc);
-      }
-    }
-    float accB[kCkpt][kStates], accC[kCkpt][kStates];
+    const int t0 = first + tile * kTile;
+    load_tile<T>(g, g.Bm, Bd, P, b, grp, t0, stop, lane);
+    load_tile<T>(g, g.Cm, Cd, P, b, grp, t0, stop, lane);
+    const float* const ckpt = g.ckpt + ((int64_t)b * ((g.T + kTile - 1) / kTile) + t0 / kTile) * ckpt_step +
+                              (((int64_t)grp * g.pairs + pb * M * PW + pc) * P + pl) * 2 * kStates;
+    float accB[kTile][kStates], accC[kTile][kStates];
 #pragma unroll
-    for (int i = 0; i < kCkpt; ++i)
+    for (int i = 0; i < kTile; ++i)
 #pragma unroll
       for (int q = 0; q < kStates; ++q) accB[i][q] = accC[i][q] = 0.0f;
 
+#pragma unroll 1
     for (int m = 0; m < M; ++m) {
-      const int pair0 = (pb * M + m) * cp;
+      const int pair0 = (pb * M + m) * PW, off = 2 * m * PW;
       if (pair0 >= g.pairs) break;
-      const bool loads = row < R && pair0 + pr < g.pairs;
-      const int c = grp * g.Dg + 2 * (pair0 + pr);
+      const bool loads = row < R && pair0 + pr < g.pairs, scans = pc < PW && pair0 + pc < g.pairs;
       const bool second = 2 * (pair0 + pr) + 1 < g.Dg;
-      auto at = [&](const Seq& x, int tok) { return static_cast<T*>(x.data) + b * x.sb + tok * x.st + c; };
-      auto value = [&](const Seq& x, int tok) {
-        Raw<T> r;
-        r.load(at(x, tok), pairs_ok, second);
-        return r.get();
-      };
+      float2 h[kTile + 1][kStates];
+      if (scans) load_own(ckpt + (int64_t)m * PW * P * 2 * kStates, h[0]);
+      Raw<T> raw_u[kUnits];
       float2 bias = f2(0.0f), skip = f2(0.0f);
       if (loads) {
+        const int c = c0 + off;
         if (g.bias) bias = make_float2(g.bias[c], second ? g.bias[c + 1] : 0.0f);
         if (g.D_skip) skip = make_float2(g.D_skip[c], second ? g.D_skip[c + 1] : 0.0f);
-        for (int tok = row; tok < kCkpt; tok += R) {
-          float2 s = f2(0.0f), x = f2(0.0f), dy = f2(0.0f);
-          const int now = t0 + tok;
-          if (now < stop) {
-            s = step_of(value(g.delta, now), bias, g.softplus);
-            x = mul2(s, value(g.u, now));
-            dy = value(g.gy, now);
-            if (g.z.data) {
-              const float2 z = value(g.z, now);
-              dy = mul2(dy, mul2(z, sigmoid<T>(z)));
-            }
-            if (!second) s.y = x.y = dy.y = 0.0f;
+        Raw<T> raw_d[kUnits], raw_g[kUnits], raw_z[kUnits];
+#pragma unroll
+        for (int k = 0; k < kUnits; ++k) {
+          const int tok = row + k * R, now = t0 + tok;
+          raw_u[k].clear();
+          raw_d[k].clear();
+          raw_g[k].clear();
+          raw_z[k].clear();
+          if (tok < kTile && now < stop) {
+            raw_u[k].load(pu + now * g.u.st + off, pairs_ok, second);
+            raw_d[k].load(pd + now * g.delta.st + off, pairs_ok, second);
+            raw_g[k].load(pg + now * g.gy.st + off, pairs_ok, second);
+            if (gate) raw_z[k].load(pz + now * g.z.st + off, pairs_ok, second);
           }
-          sx[tok * cp + pr] = make_float4(s.x, s.y, x.x, x.y);
-          dys[tok * cp + pr] = dy;
+        }
+#pragma unroll
+        for (int k = 0; k < kUnits; ++k) {
+          const int tok = row + k * R;
+          if (tok < kTile) {
+            float2 s = f2(0.0f), x = f2(0.0f), dy = f2(0.0f), slope = f2(0.0f), gz = f2(0.0f);
+            if (t0 + tok < stop) {
+              s = step_of(add2(raw_d[k].get(), bias), g.softplus, &slope);
+              x = mul2(s, raw_u[k].get());
+              dy = raw_g[k].get();
+              if (gate) {
+                const float2 z = raw_z[k].get(), sig = sigmoid<T>(z), zs = mul2(z, sig);
+                gz = mul2(dy, fma2(zs, fma2(sig, f2(-1.0f), f2(1.0f)), sig));
+                dy = mul2(dy, zs);
+              }
+              if (!second) s.y = x.y = dy.y = 0.0f;
+            }
+            sx[tok * PW + pr] = make_float4(s.x, s.y, x.x, x.y);
+            slopes[tok * PW + pr] = make_float4(slope.x, slope.y, gz.x, gz.y);
+            dys[tok * PW + pr] = dy;
+          }
         }
       }
-      __syncthreads();
-      const int pair = pair0 + pc;
-      if (pc < cp && pair < g.pairs) {
-        float2 A2[kStates], h[kCkpt + 1][kStates], gam[kStates], dA[kStates];
-        const int64_t at_tile = (int64_t)b * ((g.T + kCkpt - 1) / kCkpt) + t0 / kCkpt;
-        load_own(g.ckpt + (((at_tile * g.G + grp) * g.pairs + pair) * P + pl) * 2 * kStates, h[0]);
+      __syncwarp();
+      if (scans) {
+        float2 A2[kStates], gam[kStates], dA[kStates];
         load_own(keep_at(m, 0), A2);
 #pragma unroll
-        for (int i = 0; i < kCkpt; ++i) {
-          const float4 v = sx[i * cp + pc];
-          const float2 s = make_float2(v.x, v.y), x = make_float2(v.z, v.w), dy = dys[i * cp + pc];
-          const float2* bp = reinterpret_cast<const float2*>(Bd) + (i * P + pl) * 4;
-          const float2* cq = reinterpret_cast<const float2*>(Cd) + (i * P + pl) * 4;
-          float2 y = f2(0.0f);
+        for (int i = 0; i < kTile; ++i) {
+          const float4 v = sx[i * PW + pc];
+          const float2 s = make_float2(v.x, v.y), x = make_float2(v.z, v.w), dy = dys[i * PW + pc];
+          float2 bc[kStates];
+          load_own(reinterpret_cast<const float*>(Bd + (i * P + pl) * kStates), bc);
 #pragma unroll
           for (int q = 0; q < kStates; ++q) {
-            h[i + 1][q] = fma2(ex2(mul2(s, A2[q])), h[i][q], mul2(x, bp[q]));
-            y = fma2(cq[q], h[i + 1][q], y);
+            h[i + 1][q] = fma2(ex2(mul2(s, A2[q])), h[i][q], mul2(x, bc[q]));
             accC[i][q] = fmaf(dy.x, h[i + 1][q].x, accC[i][q]);
             accC[i][q] = fmaf(dy.y, h[i + 1][q].y, accC[i][q]);
           }
-          yp[i * kThreads + t] = y;
+          load_own(reinterpret_cast<const float*>(Cd + (i * P + pl) * kStates), bc);
+          float2 y = mul2(bc[0], h[i + 1][0]);
+#pragma unroll
+          for (int q = 1; q < kStates; ++q) y = fma2(bc[q], h[i + 1][q], y);
+          yp[i * 32 + lane] = y;
         }
         load_own(keep_at(m, 1), gam);
         load_own(keep_at(m, 2), dA);
 #pragma unroll
-        for (int i = kCkpt - 1; i >= 0; --i) {
-          const float4 v = sx[i * cp + pc];
-          const float2 s = make_float2(v.x, v.y), x = make_float2(v.z, v.w), dy = dys[i * cp + pc];
-          const float2* bp = reinterpret_cast<const float2*>(Bd) + (i * P + pl) * 4;
-          const float2* cq = reinterpret_cast<const float2*>(Cd) + (i * P + pl) * 4;
-          float2 w = f2(0.0f), r = f2(0.0f);
+        for (int i = kTile - 1; i >= 0; --i) {
+          const float4 v = sx[i * PW + pc];
+          const float2 s = make_float2(v.x, v.y), x = make_float2(v.z, v.w), dy = dys[i * PW + pc];
+          float2 bc[kStates], w, r;
+          load_own(reinterpret_cast<const float*>(Cd + (i * P + pl) * kStates), bc);
+#pragma unroll
+          for (int q = 0; q < kStates; ++q) gam[q] = fma2(dy, bc[q], gam[q]);
+          load_own(reinterpret_cast<const float*>(Bd + (i * P + pl) * kStates), bc);
 #pragma unroll
           for (int q = 0; q < kStates; ++q) {
-            const float2 gt = fma2(dy, cq[q], gam[q]);
-            accB[i][q] = fmaf(gt.x, x.x, accB[i][q]);
-            accB[i][q] = fmaf(gt.y, x.y, accB[i][q]);
-            w = fma2(gt, bp[q], w);
-            gam[q] = mul2(ex2(mul2(s, A2[q])), gt);
+            accB[i][q] = fmaf(gam[q].x, x.x, accB[i][q]);
+            accB[i][q] = fmaf(gam[q].y, x.y, accB[i][q]);
+            w = q ? fma2(gam[q], bc[q], w) : mul2(gam[q], bc[q]);
+            gam[q] = mul2(ex2(mul2(s, A2[q])), gam[q]);
             const float2 qq = mul2(gam[q], h[i][q]);
-            r = fma2(qq, A2[q], r);
+            r = q ? fma2(qq, A2[q], r) : mul2(qq, A2[q]);
             dA[q] = fma2(qq, s, dA[q]);
           }
-          wp[i * kThreads + t] = w;
-          rp[i * kThreads + t] = r;
+          wp[i * 32 + lane] = w;
+          rp[i * 32 + lane] = r;
         }
         store_own(keep_at(m, 1), gam);
         store_own(keep_at(m, 2), dA);
       }
-      __syncthreads();
+      __syncwarp();
       if (loads) {
-        float4 sums = keep2[m * kThreads + t];
-        for (int tok = row; tok < kCkpt; tok += R) {
-          const int now = t0 + tok;
-          if (now >= last) break;
-          float2 gu = f2(0.0f), gd = f2(0.0f), gz = f2(0.0f);
-          if (now < stop) {
-            const int i = tok * kThreads + pr * P;
-            float2 y = yp[i], w = wp[i], r = rp[i];
-            for (int k = 1; k < P; ++k) y = add2(y, yp[i + k]), w = add2(w, wp[i + k]), r = add2(r, rp[i + k]);
-            const float4 v = sx[tok * cp + pr];
-            const float2 s = make_float2(v.x, v.y), dy = dys[tok * cp + pr], u = value(g.u, now);
-            gu = fma2(s, w, mul2(skip, dy));
-            gd = fma2(u, w, mul2(r, f2(0.69314718055994530942f)));  // r holds A log2(e)
-            if (g.softplus) gd = mul2(gd, sigmoid<T>(add2(value(g.delta, now), bias)));
-            if (g.z.data) {
-              const float2 z = value(g.z, now), sig = sigmoid<T>(z);
-              const float2 slope = fma2(mul2(z, sig), fma2(sig, f2(-1.0f), f2(1.0f)), sig);
-              gz = mul2(mul2(value(g.gy, now), fma2(skip, u, y)), slope);
+        float4 sums = keep2[m * 32 + lane];
+#pragma unroll
+        for (int k = 0; k < kUnits; ++k) {
+          const int tok = row + k * R, now = t0 + tok;
+          if (tok < kTile && now < last) {
+            float2 gu = f2(0.0f), gd = f2(0.0f), gz = f2(0.0f);
+            if (now < stop) {
+              const int i = tok * 32 + pr * P;
+              const float2 w = sum_parts<PT>(wp + i, P), r = sum_parts<PT>(rp + i, P);
+              const float4 v = sx[tok * PW + pr], sl = slopes[tok * PW + pr];
+              const float2 s = make_float2(v.x, v.y), dy = dys[tok * PW + pr], u = raw_u[k].get();
+              gu = fma2(s, w, mul2(skip, dy));
+              gd = fma2(u, w, mul2(r, f2(0.69314718055994530942f)));  // r holds A log2(e)
+              gd = mul2(gd, make_float2(sl.x, sl.y));
+              if (gate) gz = mul2(make_float2(sl.z, sl.w), fma2(skip, u, sum_parts<PT>(yp + i, P)));
+              const float2 d = fma2(dy, u, make_float2(sums.x, sums.y)), e = add2(gd, make_float2(sums.z, sums.w));
+              sums = make_float4(d.x, d.y, e.x, e.y);
             }
-            sums.x = fmaf(dy.x, u.x, sums.x);
-            sums.y = fmaf(dy.y, u.y, sums.y);
-            sums.z += gd.x;
-            sums.w += gd.y;
+            put_pair(ou + now * g.gu.st + off, gu, pairs_ok, second);
+            put_pair(od + now * g.gdelta.st + off, gd, pairs_ok, second);
+            if (gate) put_pair(oz + now * g.gz.st + off, gz, pairs_ok, second);
           }
-          put_pair(at(g.gu, now), gu, pairs_ok, second);
-          put_pair(at(g.gdelta, now), gd, pairs_ok, second);
-          if (g.z.data) put_pair(at(g.gz, now), gz, pairs_ok, second);
         }
-        keep2[m * kThreads + t] = sums;
+        keep2[m * 32 + lane] = sums;
       }
     }
     // grad_B and grad_C of the tile: the threads' shares, pair after pair
 #pragma unroll
     for (int which = 0; which < 2; ++which) {
-      __syncthreads();
+      __syncwarp();
 #pragma unroll
-      for (int i = 0; i < kCkpt; ++i)
+      for (int i = 0; i < kTile; ++i)
 #pragma unroll
-        for (int q = 0; q < kStates; ++q)
-          acc[(i * kStates + q) * kAccStride + t] = pc < cp ? (which ? accC[i][q] : accB[i][q]) : 0.0f;
-      __syncthreads();
-      float* part = which ? g.part_C : g.part_B;
-      for (int o = t; o < kCkpt * N4; o += kThreads) {
+        for (int q = 0; q < kStates; ++q) acc[(i * kStates + q) * kAccStride + lane] = which ? accC[i][q] : accB[i][q];
+      __syncwarp();
+      float* part = (which ? g.part_C : g.part_B) + ((((int64_t)pb * g.B + b) * g.T + t0) * g.G + grp) * g.N;
+      for (int o = lane; o < kTile * N4; o += 32) {
         const int i = o / N4, n = o - i * N4;
         const float* p = acc + (i * kStates + (n & 3)) * kAccStride + (n >> 2);
         float v = p[0];
-        for (int k = 1; k < cp; ++k) v += p[k * P];
-        if (n < g.N && t0 + i < stop)
-          part[((((int64_t)pb * g.B + b) * g.T + t0 + i) * g.G + grp) * g.N + n] = v;
+        for (int k = 1; k < PW; ++k) v += p[k * P];
+        if (n < g.N && t0 + i < stop) part[(int64_t)i * g.G * g.N + n] = v;
       }
     }
-    __syncthreads();
+    __syncwarp();
   }
 
   for (int m = 0; m < M; ++m) {
-    const int pair0 = (pb * M + m) * cp, pair = pair0 + pc;
+    const int pair0 = (pb * M + m) * PW, pair = pair0 + pc, off = 2 * m * PW;
     const int64_t to = (int64_t)span * g.B + b;
-    if (pc < cp && pair < g.pairs) {
+    if (pc < PW && pair < g.pairs) {
       const int c = grp * g.Dg + 2 * pair;
       const bool second = 2 * pair + 1 < g.Dg;
       float2 v[kStates];
@@ -275,39 +285,35 @@ __global__ void __launch_bounds__(kThreads) scan_bwd(const Args g) {
         store_states(g.grad_state_in + ((int64_t)b * g.D + c) * g.N, g.N, pl * kStates, second, v);
       }
     }
-    // places past the sequence's end
+    __syncwarp();
     if (row < R && pair0 + pr < g.pairs) {
-      const int c = grp * g.Dg + 2 * (pair0 + pr);
+      const int c = c0 + off;
       const bool second = 2 * (pair0 + pr) + 1 < g.Dg;
-      for (int now = first + tiles * kCkpt + row; now < last; now += R) {
-        const int64_t chan = c;
-        put_pair(static_cast<T*>(g.gu.data) + b * g.gu.sb + now * g.gu.st + chan, f2(0.0f), pairs_ok, second);
-        put_pair(static_cast<T*>(g.gdelta.data) + b * g.gdelta.sb + now * g.gdelta.st + chan, f2(0.0f), pairs_ok, second);
-        if (g.z.data)
-          put_pair(static_cast<T*>(g.gz.data) + b * g.gz.sb + now * g.gz.st + chan, f2(0.0f), pairs_ok, second);
+      // places past the sequence's end
+      for (int now = first + tiles * kTile + row; now < last; now += R) {
+        put_pair(ou + now * g.gu.st + off, f2(0.0f), pairs_ok, second);
+        put_pair(od + now * g.gdelta.st + off, f2(0.0f), pairs_ok, second);
+        if (gate) put_pair(oz + now * g.gz.st + off, f2(0.0f), pairs_ok, second);
       }
-    }
-    // grad_D and grad_delta_bias: the rows of a pair, in order
-    __syncthreads();
-    if (row == 0 && pr < cp && pair0 + pr < g.pairs) {
-      const int c = grp * g.Dg + 2 * (pair0 + pr);
-      const bool second = 2 * (pair0 + pr) + 1 < g.Dg;
-      float4 v = keep2[m * kThreads + pr];
-      for (int k = 1; k < R; ++k) {
-        const float4 w = keep2[m * kThreads + k * cp + pr];
-        v.x += w.x, v.y += w.y, v.z += w.z, v.w += w.w;
-      }
-      g.part_D[to * g.D + c] = v.x;
-      g.part_bias[to * g.D + c] = v.z;
-      if (second) {
-        g.part_D[to * g.D + c + 1] = v.y;
-        g.part_bias[to * g.D + c + 1] = v.w;
+      // grad_D and grad_delta_bias: the rows of a pair, in order
+      if (row == 0) {
+        float4 v = keep2[m * 32 + pr];
+        for (int k = 1; k < R; ++k) {
+          const float4 w = keep2[m * 32 + k * PW + pr];
+          v.x += w.x, v.y += w.y, v.z += w.z, v.w += w.w;
+        }
+        g.part_D[to * g.D + c] = v.x;
+        g.part_bias[to * g.D + c] = v.z;
+        if (second) {
+          g.part_D[to * g.D + c + 1] = v.y;
+          g.part_bias[to * g.D + c + 1] = v.w;
+        }
       }
     }
   }
 }
 
-// grad_B and grad_C: the blocks' shares in order; zero past a sequence's end.
+// grad_B and grad_C: the warps' shares in order; zero past a sequence's end.
 template <typename T>
 __global__ void __launch_bounds__(256) scan_sum_bc(const Args g, Mat gB, Mat gC, int blocks) {
   grid_dep_wait();
@@ -362,14 +368,19 @@ BwdSpace bwd_space(const Args& g, const BwdPlan& p) {
   return s;
 }
 
+template <typename T, int PT>
+cudaError_t launch_main(const Args& g, const BwdPlan& p, int64_t blocks, cudaStream_t st) {
+  const size_t smem = bwd_smem(g.P, p.per_block);
+  const cudaError_t e = ensure_smem((const void*)scan_bwd<T, PT>, smem);
+  if (e != cudaSuccess) return e;
+  return launch_pdl(scan_bwd<T, PT>, dim3((unsigned)blocks, (unsigned)g.spans), dim3(32), smem, st, g);
+}
+
 template <typename T>
 cudaError_t launch_bwd(const Args& g, const BwdPlan& p, const Mat& gB, const Mat& gC, cudaStream_t st) {
-  const size_t smem = bwd_smem(g, p.per_block);
-  cudaError_t e = ensure_smem((const void*)scan_bwd<T>, smem);
-  if (e != cudaSuccess) return e;
   const int64_t blocks = (int64_t)g.B * g.G * p.blocks, all = (int64_t)g.B * g.T * g.G * g.N;
   if (blocks > 0x7fffffff || ceil_div(all, 256) > 0x7fffffff) return cudaErrorInvalidValue;
-  e = launch_pdl(scan_bwd<T>, dim3((unsigned)blocks, (unsigned)g.spans), dim3(kThreads), smem, st, g);
+  const cudaError_t e = g.P == 4 ? launch_main<T, 4>(g, p, blocks, st) : launch_main<T, 0>(g, p, blocks, st);
   if (e != cudaSuccess || all == 0) return e;
   return launch_pdl(scan_sum_bc<T>, dim3((unsigned)ceil_div(all, 256)), dim3(256), 0, st, g, gB, gC, p.blocks);
 }
@@ -435,6 +446,7 @@ snn_status_t snn_selective_scan_bwd(const snn_sscan_desc* desc, const snn_btc* u
   const BwdSpace space = bwd_space(g, plan);
   if (!ws || ws_bytes < space.total) return SNN_ERR_WORKSPACE;
   g.pair_ok = pair;
+  g.quads = quads(g, {&g.Bm, &g.Cm});
   g.spans = plan.cut.spans;
   g.span = plan.cut.span;
   g.per_block = plan.per_block;

@@ -1,11 +1,11 @@
 // Selective scan over whole sequences, and the spans' ends for it and for its
-// backward.  A block goes through its span of the axis in tiles of a few tokens:
+// backward.  A warp goes through its span of the axis in tiles of eight tokens:
 //   1. its threads turn delta and u of the tile into s and x = s u (shared memory)
 //      and spread B and C, each value twice, so that it meets both channels of a pair;
 //   2. every thread takes its four states of a pair through the tile's tokens and
 //      leaves its part of the sum over states;
 //   3. the parts are added, skipped over by D u, gated and stored.
-// The next tile's inputs are loaded into registers between 1 and 2.
+// The next tile's inputs are loaded into registers before 2.
 #include "sel_scan.cuh"
 #include "sel_scan_plan.cuh"
 
@@ -18,28 +18,34 @@ enum Mode {
   kBack = 2    // what a span adds to the gradient of the state before it
 };
 
-constexpr int kUnits = 4;      // channel pairs of tokens that a thread loads for a tile
+// Shared memory of a warp.
+__host__ __device__ constexpr int fwd_smem(int P, int mode) {
+  return kTile * (32 / P) * (int)sizeof(float4) + (mode == kFull ? 2 : 1) * kTile * P * kStates * (int)sizeof(float2) +
+         (mode == kFull ? kTile * 32 * (int)sizeof(float2) : 0);
+}
 
-template <typename T, int MODE>
-__global__ void __launch_bounds__(kThreads) scan_fwd(const Args g) {
+// PT: threads of a pair, 0 where only the call knows them
+template <typename T, int MODE, int PT>
+__global__ void __launch_bounds__(32) scan_fwd(const Args g) {
   extern __shared__ __align__(16) unsigned char scan_smem[];
+  constexpr int kUnits = units_of(PT);   // channel pairs of tokens that a thread loads for a tile
   grid_dep_wait();
-  const int P = g.P, cp = kThreads / P, R = kThreads / cp, TT = tile_tokens(P), N4 = kStates * P;
-  float4* const sx = reinterpret_cast<float4*>(scan_smem);               // [TT][cp]: s, x
-  float4* const Bd = sx + TT * cp;                                       // [TT][P][2]
-  float4* const Cd = Bd + TT * P * 2;
-  float2* const yp = reinterpret_cast<float2*>(Cd + TT * P * 2);         // [TT][cp P]
+  const int P = PT ? PT : g.P, PW = 32 / P, R = 32 / PW, lane = threadIdx.x;
+  float4* const sx = reinterpret_cast<float4*>(scan_smem);               // [kTile][PW]: s, x
+  float2* const Bd = reinterpret_cast<float2*>(sx + kTile * PW);         // [kTile][P][4]; C where B is not used
+  float2* const Cd = MODE == kFull ? Bd + kTile * P * kStates : Bd;
+  float2* const yp = Cd + kTile * P * kStates;                           // [kTile][32]
 
-  const int nb = (g.pairs + cp - 1) / cp;
+  const int nb = (g.pairs + PW - 1) / PW;
   const int pb = blockIdx.x % nb, rest = blockIdx.x / nb, grp = rest % g.G, b = rest / g.G;
   const int span = blockIdx.y + (MODE == kBack ? 1 : 0);
   const int len = seq_len(g, b), first = span * g.span;
   const int last = first + g.span < g.T ? first + g.span : g.T;
-  const int t = threadIdx.x, pair0 = pb * cp;
+  const int pair0 = pb * PW;
 
   // the thread's states
-  const int pl = t % P, pc = t / P, pair = pair0 + pc;
-  const bool scans = pc < cp && pair < g.pairs;
+  const int pl = lane % P, pc = lane / P, pair = pair0 + pc;
+  const bool scans = pc < PW && pair < g.pairs;
   const int64_t own = (((int64_t)b * g.G + grp) * g.pairs + pair) * P + pl;
   const int64_t own_all = (int64_t)g.B * g.G * g.pairs * P;
   float2 A2[kStates], h[kStates], total = f2(0.0f);
@@ -53,9 +59,9 @@ __global__ void __launch_bounds__(kThreads) scan_fwd(const Args g) {
     load_states(g.A + (int64_t)c_scan * g.N, g.N, pl * kStates, second_scan, A2);
 #pragma unroll
     for (int q = 0; q < kStates; ++q) A2[q] = mul2(A2[q], f2(kLog2E));
-    if (MODE != kBack && span == 0 && g.spans > 1 && MODE == kEnds) {
+    if (MODE == kEnds && span == 0) {
       // the state before the first token, where the last span's end would be: the
-      // kernel after this one may write it while its blocks start from it
+      // kernel after this one may write it while its warps start from it
       float2 h0[kStates] = {f2(0.0f), f2(0.0f), f2(0.0f), f2(0.0f)};
       if (g.state_in && has_place)
         load_states(g.state_in + (place * g.D + c_scan) * g.N, g.N, pl * kStates, second_scan, h0);
@@ -64,6 +70,7 @@ __global__ void __launch_bounds__(kThreads) scan_fwd(const Args g) {
     if (MODE == kFull) {
       if (g.spans > 1) {
         load_own(g.ends + ((int64_t)(g.spans - 1) * own_all + own) * 2 * kStates, h);
+#pragma unroll 4
         for (int i = 0; i < span; ++i) {
           float2 e[kStates];
           load_own(g.ends + ((int64_t)i * own_all + own) * 2 * kStates, e);
@@ -78,17 +85,22 @@ __global__ void __launch_bounds__(kThreads) scan_fwd(const Args g) {
   }
 
   // the thread's channel pair where tokens are loaded and stored
-  const int pr = t % cp, row = t / cp;
+  const int pr = lane % PW, row = lane / PW;
   const bool loads = row < R && pair0 + pr < g.pairs;
   const int c = grp * g.Dg + 2 * (pair0 + pr);
-  const bool second = 2 * (pair0 + pr) + 1 < g.Dg, pairs_ok = g.pair_ok;
+  const bool second = 2 * (pair0 + pr) + 1 < g.Dg, pairs_ok = g.pair_ok, gate = MODE != kEnds && g.z.data;
   float2 bias = f2(0.0f), skip = f2(0.0f);
   if (loads) {
     if (g.bias) bias = make_float2(g.bias[c], second ? g.bias[c + 1] : 0.0f);
     if (MODE == kFull && g.D_skip) skip = make_float2(g.D_skip[c], second ? g.D_skip[c + 1] : 0.0f);
   }
-  auto at = [&](const Seq& m, int tok) { return static_cast<T*>(m.data) + b * m.sb + tok * m.st + c; };
+  const Seq& in = MODE == kBack ? g.gy : g.u;
+  const T* const pu = static_cast<const T*>(in.data) + b * in.sb + c;
+  const T* const pd = static_cast<const T*>(g.delta.data) + b * g.delta.sb + c;
+  const T* const pz = static_cast<const T*>(g.z.data) + b * g.z.sb + c;
+  T* const py = static_cast<T*>(g.y.data) + b * g.y.sb + c;
   Raw<T> raw_u[kUnits], raw_d[kUnits], raw_z[kUnits];
+  const int stop = last < len ? last : len;  // tokens that exist
   auto fetch = [&](int t0) {
 #pragma unroll
     for (int k = 0; k < kUnits; ++k) {
@@ -96,110 +108,93 @@ __global__ void __launch_bounds__(kThreads) scan_fwd(const Args g) {
       raw_u[k].clear();
       raw_d[k].clear();
       raw_z[k].clear();
-      if (loads && tok < TT && now < len && now < last) {
-        raw_u[k].load(at(MODE == kBack ? g.gy : g.u, now), pairs_ok, second);
-        raw_d[k].load(at(g.delta, now), pairs_ok, second);
-        if (MODE != kEnds && g.z.data) raw_z[k].load(at(g.z, now), pairs_ok, second);
+      if (loads && tok < kTile && now < stop) {
+        raw_u[k].load(pu + now * in.st, pairs_ok, second);
+        raw_d[k].load(pd + now * g.delta.st, pairs_ok, second);
+        if (gate) raw_z[k].load(pz + now * g.z.st, pairs_ok, second);
       }
     }
   };
 
-  const int stop = last < len ? last : len;  // tokens that exist
-  const int tiles = stop > first ? (stop - first + TT - 1) / TT : 0;
-  const int n_bc = t % N4, row_bc = t / N4, R_bc = kThreads / N4;
-  if (tiles) fetch(MODE == kBack ? first + (tiles - 1) * TT : first);
+  const int tiles = stop > first ? (stop - first + kTile - 1) / kTile : 0;
+  float* ckpt = nullptr;
+  const int64_t ckpt_step = (int64_t)g.G * g.pairs * P * 2 * kStates;
+  if (MODE == kFull && g.ckpt && scans)
+    ckpt = g.ckpt + ((int64_t)b * ((g.T + kTile - 1) / kTile) + first / kTile) * ckpt_step +
+           (((int64_t)grp * g.pairs + pair) * P + pl) * 2 * kStates;
+  if (tiles) fetch(MODE == kBack ? first + (tiles - 1) * kTile : first);
   for (int tile = 0; tile < tiles; ++tile) {
-    const int t0 = first + (MODE == kBack ? tiles - 1 - tile : tile) * TT;
+    const int t0 = first + (MODE == kBack ? tiles - 1 - tile : tile) * kTile;
+    if (MODE != kBack) load_tile<T>(g, g.Bm, Bd, P, b, grp, t0, stop, lane);
+    if (MODE != kEnds) load_tile<T>(g, g.Cm, Cd, P, b, grp, t0, stop, lane);
     Raw<T> now_u[kUnits], now_z[kUnits];
 #pragma unroll
     for (int k = 0; k < kUnits; ++k) {
       const int tok = row + k * R;
       now_u[k] = raw_u[k];
       now_z[k] = raw_z[k];
-      if (loads && tok < TT) {
+      if (loads && tok < kTile) {
         float2 s = f2(0.0f), x = f2(0.0f);
         if (t0 + tok < stop) {
-          s = step_of(raw_d[k].get(), bias, g.softplus);
+          s = step_of(add2(raw_d[k].get(), bias), g.softplus);
+          x = raw_u[k].get();
           if (MODE == kBack) {
-            x = raw_u[k].get();
-            if (g.z.data) x = mul2(x, mul2(raw_z[k].get(), sigmoid<T>(raw_z[k].get())));
+            if (gate) x = mul2(x, mul2(raw_z[k].get(), sigmoid<T>(raw_z[k].get())));
           } else {
-            x = mul2(s, raw_u[k].get());
+            x = mul2(s, x);
           }
           if (!second) s.y = x.y = 0.0f;
         }
-        sx[tok * cp + pr] = make_float4(s.x, s.y, x.x, x.y);
+        sx[tok * PW + pr] = make_float4(s.x, s.y, x.x, x.y);
       }
     }
-    if (row_bc < R_bc) {
-      for (int tok = row_bc; tok < TT; tok += R_bc) {
-        float vb = 0.0f, vc = 0.0f;
-        const int now = t0 + tok;
-        if (n_bc < g.N && now < stop) {
-          if (MODE != kBack)
-            vb = Elem<T>::load1(static_cast<const T*>(g.Bm.data) + b * g.Bm.sb + now * g.Bm.st + grp * g.Bm.sg + n_bc);
-          if (MODE != kEnds)
-            vc = Elem<T>::load1(static_cast<const T*>(g.Cm.data) + b * g.Cm.sb + now * g.Cm.st + grp * g.Cm.sg + n_bc);
-        }
-        if (MODE != kBack) reinterpret_cast<float2*>(Bd)[tok * N4 + n_bc] = f2(vb);
-        if (MODE != kEnds) reinterpret_cast<float2*>(Cd)[tok * N4 + n_bc] = f2(vc);
-      }
-    }
-    __syncthreads();
-    if (tile + 1 < tiles) fetch(MODE == kBack ? t0 - TT : t0 + TT);
+    __syncwarp();
+    if (tile + 1 < tiles) fetch(MODE == kBack ? t0 - kTile : t0 + kTile);
     if (scans) {
-      for (int k0 = 0; k0 < TT; k0 += 4) {
-        if (MODE == kFull && g.ckpt && ((t0 + k0) & (kCkpt - 1)) == 0 && t0 + k0 < stop) {
-          const int64_t at_tile = (int64_t)b * ((g.T + kCkpt - 1) / kCkpt) + (t0 + k0) / kCkpt;
-          store_own(g.ckpt + (((at_tile * g.G + grp) * g.pairs + pair) * P + pl) * 2 * kStates, h);
+      if (MODE == kFull && ckpt) {
+        store_own(ckpt, h);
+        ckpt += ckpt_step;
+      }
+#pragma unroll
+      for (int i = 0; i < kTile; ++i) {
+        const int tok = MODE == kBack ? kTile - 1 - i : i;
+        const float4 v = sx[tok * PW + pc];
+        const float2 s = make_float2(v.x, v.y), x = make_float2(v.z, v.w);
+        float2 bc[kStates];
+        load_own(reinterpret_cast<const float*>((MODE == kBack ? Cd : Bd) + (tok * P + pl) * kStates), bc);
+#pragma unroll
+        for (int q = 0; q < kStates; ++q) {
+          const float2 a = ex2(mul2(s, A2[q]));
+          if (MODE == kBack) h[q] = mul2(a, fma2(x, bc[q], h[q]));
+          else h[q] = fma2(a, h[q], mul2(x, bc[q]));
         }
+        if (MODE == kFull) {
+          load_own(reinterpret_cast<const float*>(Cd + (tok * P + pl) * kStates), bc);
+          float2 y = mul2(bc[0], h[0]);
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const int tok = MODE == kBack ? TT - 1 - k0 - i : k0 + i;
-          const float4 v = sx[tok * cp + pc];
-          const float2 s = make_float2(v.x, v.y), x = make_float2(v.z, v.w);
-          const float4* bp = (MODE == kBack ? Cd : Bd) + (tok * P + pl) * 2;
-          const float4 b0 = bp[0], b1 = bp[1];
-          const float2 in[kStates] = {make_float2(b0.x, b0.y), make_float2(b0.z, b0.w), make_float2(b1.x, b1.y),
-                                      make_float2(b1.z, b1.w)};
-#pragma unroll
-          for (int q = 0; q < kStates; ++q) {
-            const float2 a = ex2(mul2(s, A2[q]));
-            if (MODE == kBack) h[q] = mul2(a, fma2(x, in[q], h[q]));
-            else h[q] = fma2(a, h[q], mul2(x, in[q]));
-          }
-          if (MODE == kFull) {
-            const float4* cq = Cd + (tok * P + pl) * 2;
-            const float4 c0 = cq[0], c1 = cq[1];
-            float2 y = mul2(make_float2(c0.x, c0.y), h[0]);
-            y = fma2(make_float2(c0.z, c0.w), h[1], y);
-            y = fma2(make_float2(c1.x, c1.y), h[2], y);
-            y = fma2(make_float2(c1.z, c1.w), h[3], y);
-            yp[tok * cp * P + t] = y;
-          } else {
-            total = add2(total, s);
-          }
+          for (int q = 1; q < kStates; ++q) y = fma2(bc[q], h[q], y);
+          yp[tok * 32 + lane] = y;
+        } else {
+          total = add2(total, s);
         }
       }
     }
-    __syncthreads();
+    __syncwarp();
     if (MODE == kFull) {
 #pragma unroll
       for (int k = 0; k < kUnits; ++k) {
         const int tok = row + k * R, now = t0 + tok;
-        if (loads && tok < TT && now < last) {
+        if (loads && tok < kTile && now < last) {
           float2 y = f2(0.0f);
           if (now < stop) {
-            const float2* p = yp + (tok * cp + pr) * P;
-            y = p[0];
-            for (int i = 1; i < P; ++i) y = add2(y, p[i]);
+            y = sum_parts<PT>(yp + tok * 32 + pr * P, P);
             y = fma2(skip, now_u[k].get(), y);
-            if (g.z.data) {
+            if (gate) {
               const float2 z = now_z[k].get();
               y = mul2(y, mul2(z, sigmoid<T>(z)));
             }
           }
-          put_pair(at(g.y, now), y, pairs_ok, second);
+          put_pair(py + now * g.y.st, y, pairs_ok, second);
         }
       }
     }
@@ -207,7 +202,8 @@ __global__ void __launch_bounds__(kThreads) scan_fwd(const Args g) {
   if (MODE == kFull) {
     // places past the sequence's end
     if (loads)
-      for (int now = first + tiles * TT + row; now < last; now += R) put_pair(at(g.y, now), f2(0.0f), pairs_ok, second);
+      for (int now = first + tiles * kTile + row; now < last; now += R)
+        put_pair(py + now * g.y.st, f2(0.0f), pairs_ok, second);
     if (scans && g.state_out && has_place && span == g.spans - 1)
       store_states(g.state_out + (place * g.D + c_scan) * g.N, g.N, pl * kStates, second_scan, h);
   } else if (scans) {
@@ -218,14 +214,12 @@ __global__ void __launch_bounds__(kThreads) scan_fwd(const Args g) {
 
 template <typename T, int MODE>
 cudaError_t launch_mode(const Args& g, int spans, cudaStream_t st) {
-  const int cp = kThreads / g.P, TT = tile_tokens(g.P);
-  const size_t smem = (size_t)TT * (cp * sizeof(float4) + 2 * g.P * 2 * sizeof(float4)) +
-                      (MODE == kFull ? (size_t)TT * cp * g.P * sizeof(float2) : 0);
-  const cudaError_t e = ensure_smem((const void*)scan_fwd<T, MODE>, smem);
-  if (e != cudaSuccess) return e;
-  const int64_t blocks = (int64_t)g.B * g.G * ceil_div(g.pairs, cp);
+  const int64_t blocks = (int64_t)g.B * g.G * ceil_div(g.pairs, 32 / g.P);
   if (blocks > 0x7fffffff) return cudaErrorInvalidValue;
-  return launch_pdl(scan_fwd<T, MODE>, dim3((unsigned)blocks, (unsigned)spans), dim3(kThreads), smem, st, g);
+  const dim3 grid((unsigned)blocks, (unsigned)spans);
+  const size_t smem = fwd_smem(g.P, MODE);
+  if (g.P == 4) return launch_pdl(scan_fwd<T, MODE, 4>, grid, dim3(32), smem, st, g);
+  return launch_pdl(scan_fwd<T, MODE, 0>, grid, dim3(32), smem, st, g);
 }
 
 template <typename T>
@@ -259,7 +253,7 @@ int64_t snn_selective_scan_ckpt_elems(const snn_sscan_desc* desc) {
   d.softplus = 0;
   if (check_desc(&d) != SNN_OK) return 0;
   const Args g = base_args(&d);
-  return snn::ceil_div(d.T, kCkpt) * g.B * g.G * g.pairs * g.P * 2 * kStates;
+  return snn::ceil_div(d.T, kTile) * g.B * g.G * g.pairs * g.P * 2 * kStates;
 }
 
 snn_status_t snn_selective_scan_fwd(const snn_sscan_desc* desc, const snn_btc* u,
@@ -293,6 +287,7 @@ snn_status_t snn_selective_scan_fwd(const snn_sscan_desc* desc, const snn_btc* u
   if (need && (!ws || ws_bytes < need)) return SNN_ERR_WORKSPACE;
   if (desc->B == 0 || (desc->T == 0 && !state_out)) return SNN_OK;
   g.pair_ok = pair;
+  g.quads = quads(g, {&g.Bm, &g.Cm});
   g.A = A;
   g.D_skip = D;
   g.bias = delta_bias;

@@ -69,7 +69,7 @@ __global__ void __launch_bounds__(kStepThreads) scan_step(const StepArgs a) {
   if (g.z.data) z = Elem<T>::load1(static_cast<const T*>(g.z.data) + b * g.z.sb + c);
   if (g.bias) s += g.bias[c];
   const float skip = g.D_skip ? g.D_skip[c] : 0.0f;
-  if (g.softplus) s = softplus(s);
+  if (g.softplus) s = softplus(f2(s), nullptr).x;
   const float x = s * u, s2 = s * kLog2E;
   float y = 0.0f;
 #pragma unroll
@@ -138,7 +138,7 @@ extern "C" snn_status_t snn_selective_scan_step(const snn_sscan_desc* desc, cons
   a.g.slots = slots;
   a.g.num_slots = num_slots;
   a.state = state;
-  a.bc_vec = (a.g.Bm.sb | a.g.Bm.sg | a.g.Cm.sb | a.g.Cm.sg) % 4 == 0;
+  a.bc_vec = quads(a.g, {&a.g.Bm, &a.g.Cm});
   cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
   const cudaError_t e = desc->dtype == SNN_F32    ? launch_step<float>(a, st)
                         : desc->dtype == SNN_BF16 ? launch_step<__nv_bfloat16>(a, st)
