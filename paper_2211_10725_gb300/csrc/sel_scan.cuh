@@ -3,12 +3,16 @@
 //   s = softplus(delta + bias),  x = s u,  a_t = exp(s A)
 //   h_t = a_t h_{t-1} + x_t B_t,   y_t = (sum_n C_t h_t + D u_t) silu(z_t)
 //
-// A thread holds four states of two neighbouring channels of a group (a pair), in
-// pairs of floats: one instruction serves both channels.  P = ceil(N / 4) threads
-// side by side hold a pair's states, so that a warp has 32 / P pairs.  It works alone: what
-// its threads exchange lies in shared memory of its own, and no barrier joins it to
-// another warp.  The decay of a span of tokens is exp(A sum s), so a cut axis hands on
-// one sum a channel beside the states.
+// A thread holds NS states (4, 8, 12 or 16) of two neighbouring channels of a group (a
+// pair), in pairs of floats: one instruction serves both channels.  P threads side by side (1,
+// 2 or 4, P NS >= N) hold a pair's states, so that a warp has 32 / P pairs, and share out its
+// tokens where inputs are made ready and results finished.  A warp works alone: B and C
+// of a few tokens lie in shared memory of its own, and no barrier joins it to another
+// warp.  Shared memory gives an SM 32 words a clock, however many lanes read the
+// same one: a multiply-add that takes its operand from there has to serve several states or
+// channels.
+// The decay of a span of tokens is exp(A sum s), so a cut axis hands on one sum a
+// channel beside the states.
 #pragma once
 
 #include <cuda_bf16.h>
@@ -27,9 +31,8 @@
 namespace snn {
 namespace sscan {
 
-constexpr int kStates = 4;        // of a channel in a thread
 constexpr int kMaxN = 64;
-constexpr int kTile = 8;          // tokens of a tile, and between checkpoints
+constexpr int kTile = 8;          // tokens between checkpoints
 constexpr float kLog2E = 1.44269504088896340736f;
 
 struct Seq {  // [B, T, channels]
@@ -46,8 +49,8 @@ struct Args {
   int softplus;
   int pair_ok;             // channel pairs lie on their own boundaries in every tensor
   int quads;               // so do fours of states of B and C
-  int P;                   // threads of a pair
   int pairs;               // of a group
+  int N2;                  // twos of states
   int spans, span;         // cuts of the axis, tokens of each
   Seq u, delta, z, y, gy, gu, gdelta, gz;
   Mat Bm, Cm;
@@ -56,13 +59,12 @@ struct Args {
   const float* state_in;
   float* state_out;
   int64_t num_slots;
-  float* ckpt;             // [B][ceil(T / 8)][G pairs][P][2 kStates]
-  float* ends;             // [spans][B][G pairs][P][2 kStates]: what a span adds to the state
+  float* ckpt;             // [B][ceil(T / 8)][G][N2][pairs][4]: two states of two channels
+  float* ends;             // [spans][B][G][N2][pairs][4]: what a span adds to the state
   float2* sums;            // [spans][B][G pairs]: of s over a span
   // backward
   const float* grad_state_out;
   float* grad_state_in;
-  int per_block;           // turns of a block over its pairs
   float *part_B, *part_C;  // [blocks of a group][B][T][G][N]
   float* part_A;           // [spans][B][D][N]
   float *part_D, *part_bias;  // [spans][B][D]
@@ -86,23 +88,24 @@ __device__ __forceinline__ float rcp(float x) {
 __device__ __forceinline__ float2 rcp(float2 x) { return make_float2(rcp(x.x), rcp(x.y)); }
 
 // softplus and its slope.  With e = e^-|x|: log(1 + e^x) = max(x, 0) + log(1 + e), and
-// log(1 + e) = 2 atanh(r), r = e / (2 + e) <= 1/3: the area tangent's series, whose terms
-// past r^15 are below 2^-27 of it.  The slope is 1 / (1 + e) or e / (1 + e).  e from the
-// power of two, with what the product |x| log2(e) was rounded by put back.
+// log(1 + e) = 2 atanh(r), r = e / (2 + e) <= 1/3.  The area tangent's series r + r^3 (1/3 + q / 5 +
+// q^2 / 7 + ...), q = r^2 <= 1/9, with the bracket as the cubic that fits it there (Chebyshev): off by
+// a quarter of 2^-24.  The slope is 1 / (1 + e) or e / (1 + e).  For fp32 inputs e gets back what
+// the product |x| log2(e) was rounded by, |x| 2^-25 of it.
+template <typename T>
 __device__ __forceinline__ float2 softplus(float2 x, float2* slope) {
   constexpr float kLog2ELow = 1.92596303e-8f, kLn2 = 0.69314718055994530942f;
-  const float2 a = make_float2(-fabsf(x.x), -fabsf(x.y));
-  const float2 t = mul2(a, f2(kLog2E));
-  const float2 rest = fma2(a, f2(kLog2ELow), fma2(a, f2(kLog2E), make_float2(-t.x, -t.y)));
+  const float2 t = make_float2(-kLog2E * fabsf(x.x), -kLog2E * fabsf(x.y));
   float2 e = ex2(t);
-  e = fma2(e, mul2(rest, f2(kLn2)), e);
+  if constexpr (sizeof(T) == 4) {
+    const float2 a = make_float2(-fabsf(x.x), -fabsf(x.y));
+    const float2 rest = fma2(a, f2(kLog2ELow), fma2(a, f2(kLog2E), make_float2(-t.x, -t.y)));
+    e = fma2(e, mul2(rest, f2(kLn2)), e);
+  }
   const float2 r = mul2(e, rcp(add2(e, f2(2.0f)))), q = mul2(r, r);
-  float2 p = fma2(q, f2(1.0f / 15.0f), f2(1.0f / 13.0f));
-  p = fma2(p, q, f2(1.0f / 11.0f));
-  p = fma2(p, q, f2(1.0f / 9.0f));
-  p = fma2(p, q, f2(1.0f / 7.0f));
-  p = fma2(p, q, f2(1.0f / 5.0f));
-  p = fma2(p, q, f2(1.0f / 3.0f));
+  float2 p = fma2(q, f2(0.13433774f), f2(0.14116979f));
+  p = fma2(p, q, f2(0.20003836f));
+  p = fma2(p, q, f2(0.33333319f));
   p = fma2(mul2(p, q), r, r);
   if (slope) {
     const float2 one = rcp(add2(e, f2(1.0f)));
@@ -168,25 +171,41 @@ __device__ __forceinline__ void put_pair(T* p, float2 v, bool pair, bool second)
 }
 
 // s of the two channels of a delta with its bias, and its slope (if asked for).
+template <typename T>
 __device__ __forceinline__ float2 step_of(float2 raw, bool soft, float2* slope = nullptr) {
-  if (soft) return softplus(raw, slope);
+  if (soft) return softplus<T>(raw, slope);
   if (slope) *slope = f2(1.0f);
   return raw;
 }
 
-// A thread's states of its pair in an fp32 [.., D, N] array (element (c, n) at
-// base + c N + n): `at` is (channel 0's row) + 4 pl; absent states are zero.
-__device__ __forceinline__ void load_states(const float* p, int N, int n0, bool second, float2 v[kStates]) {
+// A thread's states of its pair in an fp32 [.., D, N] array, from channel 0's row on;
+// absent states are zero.
+template <int NS>
+__device__ __forceinline__ void load_states(const float* p, int N, int n0, bool second, float2 (&v)[NS]) {
+  if (N % 4 == 0) {
 #pragma unroll
-  for (int q = 0; q < kStates; ++q) {
-    const bool in = n0 + q < N;
-    v[q].x = in ? p[n0 + q] : 0.0f;
-    v[q].y = in && second ? p[N + n0 + q] : 0.0f;
+    for (int q = 0; q < NS; q += 4) {
+      float a[4] = {0.0f, 0.0f, 0.0f, 0.0f}, b[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+      if (n0 + q < N) {
+        Elem<float>::load4(p + n0 + q, a);
+        if (second) Elem<float>::load4(p + N + n0 + q, b);
+      }
+#pragma unroll
+      for (int i = 0; i < 4; ++i) v[q + i] = make_float2(a[i], b[i]);
+    }
+  } else {
+#pragma unroll
+    for (int q = 0; q < NS; ++q) {
+      const bool in = n0 + q < N;
+      v[q].x = in ? p[n0 + q] : 0.0f;
+      v[q].y = in && second ? p[N + n0 + q] : 0.0f;
+    }
   }
 }
-__device__ __forceinline__ void store_states(float* p, int N, int n0, bool second, const float2 v[kStates]) {
+template <int NS>
+__device__ __forceinline__ void store_states(float* p, int N, int n0, bool second, const float2 (&v)[NS]) {
 #pragma unroll
-  for (int q = 0; q < kStates; ++q) {
+  for (int q = 0; q < NS; ++q) {
     if (n0 + q < N) {
       p[n0 + q] = v[q].x;
       if (second) p[N + n0 + q] = v[q].y;
@@ -194,43 +213,95 @@ __device__ __forceinline__ void store_states(float* p, int N, int n0, bool secon
   }
 }
 
-// A thread's eight floats in an array of its own layout.
-__device__ __forceinline__ void load_own(const float* p, float2 v[kStates]) {
-  const float4 a = reinterpret_cast<const float4*>(p)[0], b = reinterpret_cast<const float4*>(p)[1];
-  v[0] = make_float2(a.x, a.y);
-  v[1] = make_float2(a.z, a.w);
-  v[2] = make_float2(b.x, b.y);
-  v[3] = make_float2(b.z, b.w);
+// The same in [N2][pairs][4] arrays (ends, checkpoints): p at the pair, n0 even.
+template <int NS>
+__device__ __forceinline__ void load_twos(const float* p, const Args& g, int n0, float2 (&v)[NS]) {
+#pragma unroll
+  for (int q = 0; q < NS; q += 2) {
+    float a[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+    const int k = (n0 + q) >> 1;
+    if (k < g.N2) Elem<float>::load4(p + (int64_t)k * g.pairs * 4, a);
+    v[q] = make_float2(a[0], a[1]);
+    v[q + 1] = make_float2(a[2], a[3]);
+  }
 }
-__device__ __forceinline__ void store_own(float* p, const float2 v[kStates]) {
-  reinterpret_cast<float4*>(p)[0] = make_float4(v[0].x, v[0].y, v[1].x, v[1].y);
-  reinterpret_cast<float4*>(p)[1] = make_float4(v[2].x, v[2].y, v[3].x, v[3].y);
+template <int NS>
+__device__ __forceinline__ void store_twos(float* p, const Args& g, int n0, const float2 (&v)[NS]) {
+#pragma unroll
+  for (int q = 0; q < NS; q += 2) {
+    const int k = (n0 + q) >> 1;
+    const float a[4] = {v[q].x, v[q].y, v[q + 1].x, v[q + 1].y};
+    if (k < g.N2) Elem<float>::store4(p + (int64_t)k * g.pairs * 4, a);
+  }
 }
 
-// Tile of B or C in shared memory: each value twice (it meets both channels of a
-// pair), [kTile][P][4] float2; zero from token `stop` on and for absent states.  quads: the
-// states can be read in fours.
+// Four states (n0 ..) of B or C of a token as they lie in memory; zero for absent ones.
 template <typename T>
-__device__ __forceinline__ void load_tile(const Args& g, const Mat& m, float2* to, int P, int b, int grp, int t0,
-                                          int stop, int lane) {
-  const T* base = static_cast<const T*>(m.data) + b * m.sb + grp * m.sg + t0 * m.st;
-  if (g.quads) {
-#pragma unroll 2
-    for (int i = lane; i < kTile * P; i += 32) {
-      const int tok = i / P, n = (i - tok * P) * kStates;
-      float v[kStates] = {0.0f, 0.0f, 0.0f, 0.0f};
-      if (t0 + tok < stop) Elem<T>::load4(base + tok * m.st + n, v);
-      reinterpret_cast<float4*>(to)[2 * i] = make_float4(v[0], v[0], v[1], v[1]);
-      reinterpret_cast<float4*>(to)[2 * i + 1] = make_float4(v[2], v[2], v[3], v[3]);
-    }
-  } else {
-    for (int i = lane; i < kTile * P * kStates; i += 32) {
-      const int tok = i / (P * kStates), n = i - tok * (P * kStates);
-      float v = 0.0f;
-      if (n < g.N && t0 + tok < stop) v = Elem<T>::load1(base + tok * m.st + n);
-      to[i] = f2(v);
+struct Four {
+  uint32_t w[sizeof(T)];
+  __device__ __forceinline__ void clear() {
+#pragma unroll
+    for (int i = 0; i < (int)sizeof(T); ++i) w[i] = 0;
+  }
+  __device__ __forceinline__ void load(const T* p, bool quads, int absent) {  // absent: of the four
+    if (quads) {
+      if constexpr (sizeof(T) == 2) {
+        const uint2 a = *reinterpret_cast<const uint2*>(p);
+        w[0] = a.x, w[1] = a.y;
+      } else {
+        const uint4 a = *reinterpret_cast<const uint4*>(p);
+        w[0] = a.x, w[1] = a.y, w[2] = a.z, w[3] = a.w;
+      }
+    } else {
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        if (q < 4 - absent) {
+          if constexpr (sizeof(T) == 2) w[q >> 1] |= (uint32_t)reinterpret_cast<const uint16_t*>(p)[q] << (16 * (q & 1));
+          else w[q] = reinterpret_cast<const uint32_t*>(p)[q];
+        }
+      }
     }
   }
+  __device__ __forceinline__ void put(float* to) const {  // in 32 bits
+    if constexpr (sizeof(T) == 2) {
+      const float2 a = Elem<T>::to2(w[0]), b = Elem<T>::to2(w[1]);
+      *reinterpret_cast<float4*>(to) = make_float4(a.x, a.y, b.x, b.y);
+    } else {
+      *reinterpret_cast<uint4*>(to) = make_uint4(w[0], w[1], w[2], w[3]);
+    }
+  }
+};
+
+__device__ __forceinline__ float2 from_lane(float2 v, int lane) {
+  return make_float2(__shfl_sync(0xffffffffu, v.x, lane), __shfl_sync(0xffffffffu, v.y, lane));
+}
+
+// Of `tokens` (a multiple of P) tokens' sums over states, a thread's share in each: the whole
+// sums of its own tokens, pl, pl + P, .., in v[0], v[P], ..
+template <int tokens, int P>
+__device__ __forceinline__ void share_out(float2 (&v)[tokens], int pl) {
+#pragma unroll
+  for (int o = P / 2; o > 0; o >>= 1) {
+    const bool up = pl & o;
+#pragma unroll
+    for (int i = 0; i < tokens; ++i) {
+      if (i % P < o) {
+        const float2 give = up ? v[i] : v[i + o], keep = up ? v[i + o] : v[i];
+        v[i] = add2(keep, make_float2(__shfl_xor_sync(0xffffffffu, give.x, o), __shfl_xor_sync(0xffffffffu, give.y, o)));
+      }
+    }
+  }
+}
+
+// Sum over the P threads of a pair; every one gets it.
+template <int P>
+__device__ __forceinline__ float2 sum_pair(float2 v) {
+#pragma unroll
+  for (int o = 1; o < P; o <<= 1) {
+    v.x += __shfl_xor_sync(0xffffffffu, v.x, o);
+    v.y += __shfl_xor_sync(0xffffffffu, v.y, o);
+  }
+  return v;
 }
 
 // ---------------------------------------------------------------------------
@@ -285,9 +356,9 @@ inline snn_status_t take(const snn_sscan_desc* d, const snn_bthd* x, Mat* out) {
 }
 
 inline bool quads(const Args& g, std::initializer_list<const Mat*> ms) {
-  if (g.N % kStates) return false;
+  if (g.N % 4) return false;
   for (const Mat* m : ms)
-    if ((m->sb | m->st | m->sg) % kStates) return false;
+    if ((m->sb | m->st | m->sg) % 4) return false;
   return true;
 }
 
@@ -300,7 +371,7 @@ inline Args base_args(const snn_sscan_desc* d) {
   g.G = (int)d->G;
   g.Dg = (int)(d->D / d->G);
   g.softplus = d->softplus;
-  g.P = (g.N + kStates - 1) / kStates;
+  g.N2 = (g.N + 1) / 2;
   g.pairs = (g.Dg + 1) / 2;
   return g;
 }
@@ -310,9 +381,8 @@ struct Plan {
   int spans, span;
 };
 // What the kernels of a call need beside its tensors.
-inline size_t ends_bytes(const Args& g, int spans) {
-  return round256((size_t)spans * g.B * g.G * g.pairs * g.P * 2 * kStates * sizeof(float));
-}
+inline int64_t state_floats(const Args& g) { return (int64_t)g.B * g.G * g.N2 * g.pairs * 4; }
+inline size_t ends_bytes(const Args& g, int spans) { return round256((size_t)(spans * state_floats(g)) * sizeof(float)); }
 inline size_t sums_bytes(const Args& g, int spans) {
   return round256((size_t)spans * g.B * g.G * g.pairs * sizeof(float2));
 }

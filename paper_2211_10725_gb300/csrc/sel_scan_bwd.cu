@@ -5,312 +5,391 @@
 //   w = sum_n gt B;  q = a_t gt h_{t-1};  r = sum_n q A
 //   grad_u = s w + D dy;   grad_delta = (u w + r) softplus'(delta + bias)
 //   grad_A = sum_t q s;    grad_D = sum_t dy u;   grad_z = grad_y (y before the gate) silu'(z)
-// A warp goes backwards through its span of the axis in tiles of the checkpoints'
-// eight tokens, and in each tile in turns through its channel pairs: it takes the states
-// of a turn from the checkpoint through the tile (they stay in registers), then gamma
-// back through it.  A thread has the same states in every turn, so that grad_B and
-// grad_C of the tile gather in its registers over the turns and meet over the
-// threads once a tile; gamma and grad_A of every turn lie in shared memory.  The warps' shares
-// of grad_B, grad_C, grad_A, grad_D and grad_delta_bias are added by a second kernel in a
-// fixed order.
+// A warp goes backwards through its span of the axis in tiles of the checkpoints' eight
+// tokens: from the checkpoint it takes the states forwards through the tile and leaves them
+// in tensor memory, which serves here as a second register file (a thread's lane of 128
+// words for every four tokens; through shared memory they would be the bound), then
+// gamma back through it.  grad_B and grad_C are summed over the warp's channels as the
+// tokens pass, halving the values a thread holds with every exchange; the warps' shares, and
+// those of grad_A, grad_D and grad_delta_bias, are added by further kernels in a fixed order.
 #include "sel_scan.cuh"
 #include "sel_scan_plan.cuh"
+#include "tcgen05.cuh"
 
 namespace snn {
 namespace sscan {
 
-constexpr int kTurns = 4;        // of a warp in a tile, at most
-constexpr int kAccStride = 36;   // floats between the rows of the threads' shares: 32 and four banks
+using gemm::tc_fence_after;
+using gemm::tc_fence_before;
+using gemm::tmem_alloc;
+using gemm::tmem_dealloc;
+
+constexpr int kWarps = 4;        // of a block, one for each quarter of tensor memory
 
 struct BwdPlan {
+  Lay lay;
+  int blocks;  // warps of a group
   Plan cut;
-  int per_block, blocks;  // turns of a warp; warps of a group
 };
+
+// Columns of tensor memory: a tile's states, allocated in powers of two.
+__host__ __device__ constexpr int columns_of(int NS) { return NS == 4 ? 64 : NS == 8 ? 128 : 256; }
+// Blocks of an SM: what tensor memory and 128 registers a thread (255 for 12 and 16 states) allow.
+__host__ __device__ constexpr int blocks_of(int NS) { return NS <= 8 ? 4 : 2; }
 
 BwdPlan bwd_plan(const Args& g) {
   BwdPlan p;
-  const int turns = (int)ceil_div(g.pairs, 32 / g.P);
-  p.per_block = turns < kTurns ? turns : kTurns;
-  p.blocks = (int)ceil_div(turns, p.per_block);
-  p.cut = cut(g.T, (int64_t)g.B * g.G * p.blocks, kSms * 8, 3);
+  p.lay = lay_of(g.N);
+  p.blocks = (int)ceil_div(g.pairs, 32 / p.lay.P);
+  p.cut = cut(g.T, warps_of(g, p.lay), kSms * kWarps * blocks_of(p.lay.NS), 2);
   return p;
 }
 
-// Shared memory of a warp: s and x; slopes; dy; B and C; the sums' parts (or the threads'
-// shares of grad_B and grad_C); what stays over the tiles of a span.
-__host__ __device__ constexpr int bwd_smem(int P, int turns) {
-  return kTile * (32 / P) * (2 * (int)sizeof(float4) + (int)sizeof(float2)) +
-         2 * kTile * P * kStates * (int)sizeof(float2) + 3 * kTile * 32 * (int)sizeof(float2) +
-         turns * 32 * (3 * 8 + 4) * (int)sizeof(float);
+// Shared memory of a warp: s, u, dy, softplus' and grad_y silu' of a tile's pairs; its B and C.
+__host__ __device__ constexpr int bwd_smem(int NS, int P) {
+  return kTile * (32 / P) * 5 * (int)sizeof(float2) + kTile * 2 * P * NS * (int)sizeof(float);
 }
 
-template <typename T, int PT>
-__global__ void __launch_bounds__(32) scan_bwd(const Args g) {
-  extern __shared__ __align__(16) unsigned char scan_smem[];
-  constexpr int kUnits = units_of(PT);
-  grid_dep_wait();
-  const int P = PT ? PT : g.P, PW = 32 / P, R = 32 / PW, N4 = kStates * P, M = g.per_block, lane = threadIdx.x;
-  float4* const sx = reinterpret_cast<float4*>(scan_smem);         // [kTile][PW]: s, x
-  float4* const slopes = sx + kTile * PW;                          // [kTile][PW]: softplus', grad_y silu'
-  float2* const Bd = reinterpret_cast<float2*>(slopes + kTile * PW);  // [kTile][P][4]
-  float2* const Cd = Bd + kTile * N4;
-  float* const keep = reinterpret_cast<float*>(Cd + kTile * N4);   // [M][3][32][8]: A, gamma, grad_A
-  float4* const keep2 = reinterpret_cast<float4*>(keep + M * 3 * 32 * 8);  // [M][32]: grad_D, grad_delta_bias
-  float2* const yp = reinterpret_cast<float2*>(keep2 + M * 32);    // [kTile][32]
-  float2* const wp = yp + kTile * 32;
-  float2* const rp = wp + kTile * 32;
-  float2* const dys = rp + kTile * 32;                             // [kTile][PW]
-  float* const acc = reinterpret_cast<float*>(yp);                 // [32][kAccStride]
+// Tensor memory as a thread's own: columns of its lane.  What is loaded is there after
+// arrived().
+__device__ __forceinline__ void own_load(uint32_t at, float2* v) {
+  asm volatile("tcgen05.ld.sync.aligned.32x32b.x8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+               : "=f"(v[0].x), "=f"(v[0].y), "=f"(v[1].x), "=f"(v[1].y), "=f"(v[2].x), "=f"(v[2].y), "=f"(v[3].x),
+                 "=f"(v[3].y)
+               : "r"(at));
+}
+template <int NS>
+__device__ __forceinline__ void arrived(float2 (&v)[NS]) {
+  asm volatile("tcgen05.wait::ld.sync.aligned;");
+#pragma unroll
+  for (int q = 0; q < NS; ++q) asm volatile("" : "+f"(v[q].x), "+f"(v[q].y));
+}
+__device__ __forceinline__ void own_store(uint32_t at, const float2* v) {
+  asm volatile("tcgen05.st.sync.aligned.32x32b.x8.b32 [%8], {%0, %1, %2, %3, %4, %5, %6, %7};" ::"f"(v[0].x),
+               "f"(v[0].y), "f"(v[1].x), "f"(v[1].y), "f"(v[2].x), "f"(v[2].y), "f"(v[3].x), "f"(v[3].y), "r"(at));
+}
+__device__ __forceinline__ void stored() { asm volatile("tcgen05.wait::st.sync.aligned;"); }
 
-  const int turns = (g.pairs + PW - 1) / PW, nb = (turns + M - 1) / M;
-  const int pb = blockIdx.x % nb, rest = blockIdx.x / nb, grp = rest % g.G, b = rest / g.G;
-  const int span = blockIdx.y, len = seq_len(g, b), first = span * g.span;
+// Sums of K values (a power of two) over a warp's pairs, whose threads are P apart: with
+// each exchange a thread keeps half of the values.  Left are the first max(1, K P / 32), those
+// from left_at() on (-1 in threads whose sums another one has too).
+template <int K, int P>
+__device__ __forceinline__ void sum_over_pairs(float (&v)[K], int lane) {
+#pragma unroll
+  for (int o = 16; o >= P; o >>= 1) {
+    const int n = K * o / 32;  // left after this exchange
+    const bool up = lane & o;
+    if (n >= 1) {
+#pragma unroll
+      for (int i = 0; i < n; ++i) {
+        const float give = up ? v[i] : v[i + n], keep = up ? v[i + n] : v[i];
+        v[i] = keep + __shfl_xor_sync(0xffffffffu, give, o);
+      }
+    } else {
+      v[0] += __shfl_xor_sync(0xffffffffu, v[0], o);
+    }
+  }
+}
+template <int K, int P>
+__device__ __forceinline__ int left_at(int lane) {
+  int at = 0;
+#pragma unroll
+  for (int o = 16; o >= P; o >>= 1) {
+    const int n = K * o / 32;
+    if (lane & o) {
+      if (n < 1) return -1;
+      at += n;
+    }
+  }
+  return at;
+}
+
+template <typename T, int NS, int P>
+__device__ void scan_back(const Args& g, int64_t work, unsigned char* smem, uint32_t t_h) {
+  constexpr int K = NS == 12 ? 16 : NS, kLeft = K * P / 32 > 1 ? K * P / 32 : 1;   // sums over pairs
+  constexpr int PW = 32 / P, Np = P * NS, U = kTile / P;
+  constexpr int kTokens = 128 / Np, kTurns = (kTile + kTokens - 1) / kTokens;  // whose B and C are loaded at once
+  const int lane = threadIdx.x & 31, pl = lane & (P - 1), pc = lane / P;
+  float2* const ps = reinterpret_cast<float2*>(smem);              // [kTile][PW]
+  float2* const pu = ps + kTile * PW;
+  float2* const pdy = pu + kTile * PW;
+  float2* const pslope = pdy + kTile * PW;
+  float2* const pgz = pslope + kTile * PW;
+  float* const bc = reinterpret_cast<float*>(pgz + kTile * PW);    // [kTile][B, C][Np]
+
+  const int nb = (g.pairs + PW - 1) / PW;
+  const int64_t place = work / g.spans;
+  const int span = (int)(work - place * g.spans);
+  const int pb = (int)(place % nb), rest = (int)(place / nb), grp = rest % g.G, b = rest / g.G;
+  const int len = seq_len(g, b), first = span * g.span;
   const int last = first + g.span < g.T ? first + g.span : g.T;
   const int stop = last < len ? last : len;
   const int tiles = stop > first ? (stop - first + kTile - 1) / kTile : 0;
-  const int pl = lane % P, pc = lane / P, pr = lane % PW, row = lane / PW;
-  const bool pairs_ok = g.pair_ok, gate = g.z.data != nullptr;
-  const int64_t own_all = (int64_t)g.B * g.G * g.pairs * P;
-  auto keep_at = [&](int m, int k) { return keep + ((m * 3 + k) * 32 + lane) * 8; };
+  const int pair = pb * PW + pc, n0 = pl * NS;
+  const bool live = pair < g.pairs, second = 2 * pair + 1 < g.Dg, pairs_ok = g.pair_ok;
+  const bool gate = g.z.data != nullptr, soft = g.softplus;
+  const int c = grp * g.Dg + 2 * pair;
+  const int64_t row_states = (int64_t)g.N2 * g.pairs * 4;
 
-  for (int m = 0; m < M; ++m) {
-    const int pair = (pb * M + m) * PW + pc;
-    float2 A2[kStates], gam[kStates];
+  float2 A2[NS], gam[NS], dA[NS], bias = f2(0.0f), skip = f2(0.0f), sum_D = f2(0.0f), sum_bias = f2(0.0f);
 #pragma unroll
-    for (int q = 0; q < kStates; ++q) A2[q] = gam[q] = f2(0.0f);
-    if (pc < PW && pair < g.pairs) {
-      const int c = grp * g.Dg + 2 * pair;
-      const bool second = 2 * pair + 1 < g.Dg;
-      const int64_t own = (((int64_t)b * g.G + grp) * g.pairs + pair) * P + pl;
-      load_states(g.A + (int64_t)c * g.N, g.N, pl * kStates, second, A2);
+  for (int q = 0; q < NS; ++q) A2[q] = gam[q] = dA[q] = f2(0.0f);
+  if (live) {
+    load_states<NS>(g.A + (int64_t)c * g.N, g.N, n0, second, A2);
 #pragma unroll
-      for (int q = 0; q < kStates; ++q) A2[q] = mul2(A2[q], f2(kLog2E));
-      if (g.grad_state_out)
-        load_states(g.grad_state_out + ((int64_t)b * g.D + c) * g.N, g.N, pl * kStates, second, gam);
-#pragma unroll 2
-      for (int i = g.spans - 1; i > span; --i) {
-        float2 e[kStates];
-        load_own(g.ends + ((int64_t)i * own_all + own) * 2 * kStates, e);
-        const float2 s = g.sums[((int64_t)i * g.B * g.G + rest) * g.pairs + pair];
+    for (int q = 0; q < NS; ++q) A2[q] = mul2(A2[q], f2(kLog2E));
+    if (g.bias) bias = make_float2(g.bias[c], second ? g.bias[c + 1] : 0.0f);
+    if (g.D_skip) skip = make_float2(g.D_skip[c], second ? g.D_skip[c + 1] : 0.0f);
+    if (g.grad_state_out) load_states<NS>(g.grad_state_out + ((int64_t)b * g.D + c) * g.N, g.N, n0, second, gam);
+    for (int i = g.spans - 1; i > span; --i) {
+      float2 e[NS];
+      load_twos<NS>(g.ends + ((int64_t)i * g.B * g.G + rest) * row_states + pair * 4, g, n0, e);
+      const float2 s = g.sums[((int64_t)i * g.B * g.G + rest) * g.pairs + pair];
 #pragma unroll
-        for (int q = 0; q < kStates; ++q) gam[q] = fma2(ex2(mul2(s, A2[q])), gam[q], e[q]);
-      }
+      for (int q = 0; q < NS; ++q) gam[q] = fma2(ex2(mul2(s, A2[q])), gam[q], e[q]);
     }
-    store_own(keep_at(m, 0), A2);
-    store_own(keep_at(m, 1), gam);
-#pragma unroll
-    for (int q = 0; q < kStates; ++q) gam[q] = f2(0.0f);
-    store_own(keep_at(m, 2), gam);
-    keep2[m * 32 + lane] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
   }
 
-  const int c0 = grp * g.Dg + 2 * (pb * M * PW + pr);   // the first turn's channel where tokens are loaded and stored
-  auto base = [&](const Seq& x) { return static_cast<T*>(x.data) + b * x.sb + c0; };
-  const T *const pu = base(g.u), *const pd = base(g.delta), *const pg = base(g.gy), *const pz = base(g.z);
-  T *const ou = base(g.gu), *const od = base(g.gdelta), *const oz = base(g.gz);
-  const int64_t ckpt_step = (int64_t)g.G * g.pairs * P * 2 * kStates;
+  // a thread's own tokens of the last tile, and its fours of states of B and C
+  const int t_last = first + (tiles - 1) * kTile;
+  auto own = [&](const Seq& m) { return static_cast<T*>(m.data) + b * m.sb + (int64_t)(t_last + pl) * m.st + c; };
+  const T *in_u = own(g.u), *in_d = own(g.delta), *in_g = own(g.gy), *in_z = own(g.z);
+  T *out_u = own(g.gu), *out_d = own(g.gdelta), *out_z = own(g.gz);
+  const float* ckpt = g.ckpt + (((int64_t)b * ((g.T + kTile - 1) / kTile) + t_last / kTile) * g.G + grp) * row_states +
+                      pair * 4;
+  const T *pB, *pC;
+  int bc_tok, bc_n;
+  {
+    bc_tok = lane * 4 / Np, bc_n = lane * 4 % Np;   // 128 / Np tokens of B, and of C, a turn
+    pB = static_cast<const T*>(g.Bm.data) + b * g.Bm.sb + (int64_t)(t_last + bc_tok) * g.Bm.st + grp * g.Bm.sg + bc_n;
+    pC = static_cast<const T*>(g.Cm.data) + b * g.Cm.sb + (int64_t)(t_last + bc_tok) * g.Cm.st + grp * g.Cm.sg + bc_n;
+  }
+  const int absent = bc_n + 4 - g.N;
+  // its shares of grad_B and grad_C
+  const int at = left_at<K, P>(lane);
+  const int64_t part_step = (int64_t)g.G * g.N;
+  const int64_t part0 = ((((int64_t)pb * g.B + b) * g.T + t_last) * g.G + grp) * g.N + n0 + at;
+  float *part_B = g.part_B + part0, *part_C = g.part_C + part0;
+  auto put_part = [&](float* p, const float (&v)[K]) {
+    if (at >= 0) {
+#pragma unroll
+      for (int j = 0; j < kLeft; ++j)
+        if (n0 + at + j < g.N && at + j < NS) p[j] = v[j];
+    }
+  };
 
   for (int tile = tiles - 1; tile >= 0; --tile) {
-    const int t0 = first + tile * kTile;
-    load_tile<T>(g, g.Bm, Bd, P, b, grp, t0, stop, lane);
-    load_tile<T>(g, g.Cm, Cd, P, b, grp, t0, stop, lane);
-    const float* const ckpt = g.ckpt + ((int64_t)b * ((g.T + kTile - 1) / kTile) + t0 / kTile) * ckpt_step +
-                              (((int64_t)grp * g.pairs + pb * M * PW + pc) * P + pl) * 2 * kStates;
-    float accB[kTile][kStates], accC[kTile][kStates];
+    const int t0 = first + tile * kTile, tokens = stop - t0 < kTile ? stop - t0 : kTile;
+    float2 h[NS];
 #pragma unroll
-    for (int i = 0; i < kTile; ++i)
+    for (int q = 0; q < NS; ++q) h[q] = f2(0.0f);
+    if (live) load_twos<NS>(ckpt, g, n0, h);
+    ckpt -= g.G * row_states;
+    {  // the tile's inputs: a thread's own tokens, and its fours of B and C
+      Raw<T> ru[U], rd[U], rg[U], rz[U];
+      Four<T> rb[kTurns], rc[kTurns];
 #pragma unroll
-      for (int q = 0; q < kStates; ++q) accB[i][q] = accC[i][q] = 0.0f;
-
+      for (int i = 0; i < kTurns; ++i) {
+        rb[i].clear();
+        rc[i].clear();
+        const int tok = bc_tok + i * kTokens;
+        if (tok < tokens && tok < kTile && bc_tok < kTokens && absent < 4) {
+          rb[i].load(pB + i * kTokens * g.Bm.st, g.quads, absent > 0 ? absent : 0);
+          rc[i].load(pC + i * kTokens * g.Cm.st, g.quads, absent > 0 ? absent : 0);
+        }
+      }
+#pragma unroll
+      for (int j = 0; j < U; ++j) {
+        ru[j].clear();
+        rd[j].clear();
+        rg[j].clear();
+        rz[j].clear();
+        if (live && pl + j * P < tokens) {
+          ru[j].load(in_u + j * P * g.u.st, pairs_ok, second);
+          rd[j].load(in_d + j * P * g.delta.st, pairs_ok, second);
+          rg[j].load(in_g + j * P * g.gy.st, pairs_ok, second);
+          if (gate) rz[j].load(in_z + j * P * g.z.st, pairs_ok, second);
+        }
+      }
+      in_u -= kTile * g.u.st;
+      in_d -= kTile * g.delta.st;
+      in_g -= kTile * g.gy.st;
+      in_z -= kTile * g.z.st;
+      pB -= kTile * g.Bm.st;
+      pC -= kTile * g.Cm.st;
+#pragma unroll
+      for (int i = 0; i < kTurns; ++i) {
+        const int tok = bc_tok + i * kTokens;
+        if (tok < kTile && bc_tok < kTokens) {
+          rb[i].put(bc + tok * 2 * Np + bc_n);
+          rc[i].put(bc + tok * 2 * Np + Np + bc_n);
+        }
+      }
+#pragma unroll
+      for (int j = 0; j < U; ++j) {
+        const int tok = pl + j * P, to = tok * PW + pc;
+        float2 s = f2(0.0f), dy = rg[j].get(), slope = f2(0.0f);
+        if (live && tok < tokens) s = step_of<T>(add2(rd[j].get(), bias), soft, &slope);
+        if (gate) {
+          const float2 z = rz[j].get(), sig = sigmoid<T>(z), zs = mul2(z, sig);
+          pgz[to] = mul2(dy, fma2(zs, fma2(sig, f2(-1.0f), f2(1.0f)), sig));
+          dy = mul2(dy, zs);
+        }
+        if (!second) s.y = dy.y = 0.0f;
+        ps[to] = s;
+        pu[to] = ru[j].get();
+        pdy[to] = dy;
+        pslope[to] = slope;
+      }
+    }
+    __syncwarp();
+    // the states forwards
 #pragma unroll 1
-    for (int m = 0; m < M; ++m) {
-      const int pair0 = (pb * M + m) * PW, off = 2 * m * PW;
-      if (pair0 >= g.pairs) break;
-      const bool loads = row < R && pair0 + pr < g.pairs, scans = pc < PW && pair0 + pc < g.pairs;
-      const bool second = 2 * (pair0 + pr) + 1 < g.Dg;
-      float2 h[kTile + 1][kStates];
-      if (scans) load_own(ckpt + (int64_t)m * PW * P * 2 * kStates, h[0]);
-      Raw<T> raw_u[kUnits];
-      float2 bias = f2(0.0f), skip = f2(0.0f);
-      if (loads) {
-        const int c = c0 + off;
-        if (g.bias) bias = make_float2(g.bias[c], second ? g.bias[c + 1] : 0.0f);
-        if (g.D_skip) skip = make_float2(g.D_skip[c], second ? g.D_skip[c + 1] : 0.0f);
-        Raw<T> raw_d[kUnits], raw_g[kUnits], raw_z[kUnits];
+    for (int i0 = 0; i0 < kTile; i0 += P) {
+      float2 y[P];
 #pragma unroll
-        for (int k = 0; k < kUnits; ++k) {
-          const int tok = row + k * R, now = t0 + tok;
-          raw_u[k].clear();
-          raw_d[k].clear();
-          raw_g[k].clear();
-          raw_z[k].clear();
-          if (tok < kTile && now < stop) {
-            raw_u[k].load(pu + now * g.u.st + off, pairs_ok, second);
-            raw_d[k].load(pd + now * g.delta.st + off, pairs_ok, second);
-            raw_g[k].load(pg + now * g.gy.st + off, pairs_ok, second);
-            if (gate) raw_z[k].load(pz + now * g.z.st + off, pairs_ok, second);
+      for (int k = 0; k < P; ++k) {
+        const int i = i0 + k;
+#pragma unroll
+        for (int q = 0; q < NS; q += 4) own_store(t_h + i * 2 * NS + 2 * q, h + q);
+        const float2 s = ps[i * PW + pc], dy = pdy[i * PW + pc], x = mul2(s, pu[i * PW + pc]);
+        const float* const rb = bc + i * 2 * Np + n0;
+        float2 sum[2] = {f2(0.0f), f2(0.0f)};
+        float dC[K];
+#pragma unroll
+        for (int q = 0; q < NS; q += 4) {
+          float v[4], w[4];
+          Elem<float>::load4(rb + q, v);
+          Elem<float>::load4(rb + Np + q, w);
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            float2& hq = h[q + e];
+            hq = fma2(ex2(mul2(s, A2[q + e])), hq, make_float2(x.x * v[e], x.y * v[e]));
+            float2& to = sum[e & 1];
+            to = make_float2(fmaf(w[e], hq.x, to.x), fmaf(w[e], hq.y, to.y));
+            dC[q + e] = fmaf(dy.x, hq.x, dy.y * hq.y);
           }
         }
+        y[k] = add2(sum[0], sum[1]);
 #pragma unroll
-        for (int k = 0; k < kUnits; ++k) {
-          const int tok = row + k * R;
-          if (tok < kTile) {
-            float2 s = f2(0.0f), x = f2(0.0f), dy = f2(0.0f), slope = f2(0.0f), gz = f2(0.0f);
-            if (t0 + tok < stop) {
-              s = step_of(add2(raw_d[k].get(), bias), g.softplus, &slope);
-              x = mul2(s, raw_u[k].get());
-              dy = raw_g[k].get();
-              if (gate) {
-                const float2 z = raw_z[k].get(), sig = sigmoid<T>(z), zs = mul2(z, sig);
-                gz = mul2(dy, fma2(zs, fma2(sig, f2(-1.0f), f2(1.0f)), sig));
-                dy = mul2(dy, zs);
-              }
-              if (!second) s.y = x.y = dy.y = 0.0f;
-            }
-            sx[tok * PW + pr] = make_float4(s.x, s.y, x.x, x.y);
-            slopes[tok * PW + pr] = make_float4(slope.x, slope.y, gz.x, gz.y);
-            dys[tok * PW + pr] = dy;
-          }
-        }
+        for (int q = NS; q < K; ++q) dC[q] = 0.0f;
+        sum_over_pairs<K, P>(dC, lane);
+        if (i < tokens) put_part(part_C + i * part_step, dC);
       }
-      __syncwarp();
-      if (scans) {
-        float2 A2[kStates], gam[kStates], dA[kStates];
-        load_own(keep_at(m, 0), A2);
-#pragma unroll
-        for (int i = 0; i < kTile; ++i) {
-          const float4 v = sx[i * PW + pc];
-          const float2 s = make_float2(v.x, v.y), x = make_float2(v.z, v.w), dy = dys[i * PW + pc];
-          float2 bc[kStates];
-          load_own(reinterpret_cast<const float*>(Bd + (i * P + pl) * kStates), bc);
-#pragma unroll
-          for (int q = 0; q < kStates; ++q) {
-            h[i + 1][q] = fma2(ex2(mul2(s, A2[q])), h[i][q], mul2(x, bc[q]));
-            accC[i][q] = fmaf(dy.x, h[i + 1][q].x, accC[i][q]);
-            accC[i][q] = fmaf(dy.y, h[i + 1][q].y, accC[i][q]);
-          }
-          load_own(reinterpret_cast<const float*>(Cd + (i * P + pl) * kStates), bc);
-          float2 y = mul2(bc[0], h[i + 1][0]);
-#pragma unroll
-          for (int q = 1; q < kStates; ++q) y = fma2(bc[q], h[i + 1][q], y);
-          yp[i * 32 + lane] = y;
-        }
-        load_own(keep_at(m, 1), gam);
-        load_own(keep_at(m, 2), dA);
-#pragma unroll
-        for (int i = kTile - 1; i >= 0; --i) {
-          const float4 v = sx[i * PW + pc];
-          const float2 s = make_float2(v.x, v.y), x = make_float2(v.z, v.w), dy = dys[i * PW + pc];
-          float2 bc[kStates], w, r;
-          load_own(reinterpret_cast<const float*>(Cd + (i * P + pl) * kStates), bc);
-#pragma unroll
-          for (int q = 0; q < kStates; ++q) gam[q] = fma2(dy, bc[q], gam[q]);
-          load_own(reinterpret_cast<const float*>(Bd + (i * P + pl) * kStates), bc);
-#pragma unroll
-          for (int q = 0; q < kStates; ++q) {
-            accB[i][q] = fmaf(gam[q].x, x.x, accB[i][q]);
-            accB[i][q] = fmaf(gam[q].y, x.y, accB[i][q]);
-            w = q ? fma2(gam[q], bc[q], w) : mul2(gam[q], bc[q]);
-            gam[q] = mul2(ex2(mul2(s, A2[q])), gam[q]);
-            const float2 qq = mul2(gam[q], h[i][q]);
-            r = q ? fma2(qq, A2[q], r) : mul2(qq, A2[q]);
-            dA[q] = fma2(qq, s, dA[q]);
-          }
-          wp[i * 32 + lane] = w;
-          rp[i * 32 + lane] = r;
-        }
-        store_own(keep_at(m, 1), gam);
-        store_own(keep_at(m, 2), dA);
-      }
-      __syncwarp();
-      if (loads) {
-        float4 sums = keep2[m * 32 + lane];
-#pragma unroll
-        for (int k = 0; k < kUnits; ++k) {
-          const int tok = row + k * R, now = t0 + tok;
-          if (tok < kTile && now < last) {
-            float2 gu = f2(0.0f), gd = f2(0.0f), gz = f2(0.0f);
-            if (now < stop) {
-              const int i = tok * 32 + pr * P;
-              const float2 w = sum_parts<PT>(wp + i, P), r = sum_parts<PT>(rp + i, P);
-              const float4 v = sx[tok * PW + pr], sl = slopes[tok * PW + pr];
-              const float2 s = make_float2(v.x, v.y), dy = dys[tok * PW + pr], u = raw_u[k].get();
-              gu = fma2(s, w, mul2(skip, dy));
-              gd = fma2(u, w, mul2(r, f2(0.69314718055994530942f)));  // r holds A log2(e)
-              gd = mul2(gd, make_float2(sl.x, sl.y));
-              if (gate) gz = mul2(make_float2(sl.z, sl.w), fma2(skip, u, sum_parts<PT>(yp + i, P)));
-              const float2 d = fma2(dy, u, make_float2(sums.x, sums.y)), e = add2(gd, make_float2(sums.z, sums.w));
-              sums = make_float4(d.x, d.y, e.x, e.y);
-            }
-            put_pair(ou + now * g.gu.st + off, gu, pairs_ok, second);
-            put_pair(od + now * g.gdelta.st + off, gd, pairs_ok, second);
-            if (gate) put_pair(oz + now * g.gz.st + off, gz, pairs_ok, second);
-          }
-        }
-        keep2[m * 32 + lane] = sums;
+      if (gate) {
+        share_out<P, P>(y, pl);
+        const int i = i0 + pl;
+        if (live && i < tokens)
+          put_pair(out_z + i0 * g.gz.st, mul2(pgz[i * PW + pc], fma2(skip, pu[i * PW + pc], y[0])), pairs_ok, second);
       }
     }
-    // grad_B and grad_C of the tile: the threads' shares, pair after pair
+    stored();
+    // gamma backwards
+#pragma unroll 1
+    for (int i0 = kTile - P; i0 >= 0; i0 -= P) {
+      float2 w[P], r[P];
 #pragma unroll
-    for (int which = 0; which < 2; ++which) {
-      __syncwarp();
+      for (int k = P - 1; k >= 0; --k) {
+        const int i = i0 + k;
+        float2 hv[NS];
 #pragma unroll
-      for (int i = 0; i < kTile; ++i)
+        for (int q = 0; q < NS; q += 4) own_load(t_h + i * 2 * NS + 2 * q, hv + q);
+        const float2 s = ps[i * PW + pc], dy = pdy[i * PW + pc], x = mul2(s, pu[i * PW + pc]);
+        const float* const rb = bc + i * 2 * Np + n0;
+        float2 sw[2] = {f2(0.0f), f2(0.0f)}, sr[2] = {f2(0.0f), f2(0.0f)};
+        float dB[K];
 #pragma unroll
-        for (int q = 0; q < kStates; ++q) acc[(i * kStates + q) * kAccStride + lane] = which ? accC[i][q] : accB[i][q];
-      __syncwarp();
-      float* part = (which ? g.part_C : g.part_B) + ((((int64_t)pb * g.B + b) * g.T + t0) * g.G + grp) * g.N;
-      for (int o = lane; o < kTile * N4; o += 32) {
-        const int i = o / N4, n = o - i * N4;
-        const float* p = acc + (i * kStates + (n & 3)) * kAccStride + (n >> 2);
-        float v = p[0];
-        for (int k = 1; k < PW; ++k) v += p[k * P];
-        if (n < g.N && t0 + i < stop) part[(int64_t)i * g.G * g.N + n] = v;
+        for (int q = 0; q < NS; q += 4) {
+          float vb[4], vc[4];
+          Elem<float>::load4(rb + q, vb);
+          Elem<float>::load4(rb + Np + q, vc);
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            float2& gq = gam[q + e];
+            gq = make_float2(fmaf(dy.x, vc[e], gq.x), fmaf(dy.y, vc[e], gq.y));
+            dB[q + e] = fmaf(gq.x, x.x, gq.y * x.y);
+            float2& to = sw[e & 1];
+            to = make_float2(fmaf(vb[e], gq.x, to.x), fmaf(vb[e], gq.y, to.y));
+            gq = mul2(ex2(mul2(s, A2[q + e])), gq);
+          }
+        }
+        arrived<NS>(hv);
+#pragma unroll
+        for (int q = 0; q < NS; ++q) {
+          const float2 qq = mul2(gam[q], hv[q]);
+          sr[q & 1] = fma2(qq, A2[q], sr[q & 1]);
+          dA[q] = fma2(qq, s, dA[q]);
+        }
+        w[k] = add2(sw[0], sw[1]);
+        r[k] = add2(sr[0], sr[1]);
+#pragma unroll
+        for (int q = NS; q < K; ++q) dB[q] = 0.0f;
+        sum_over_pairs<K, P>(dB, lane);
+        if (i < tokens) put_part(part_B + i * part_step, dB);
+      }
+      share_out<P, P>(w, pl);
+      share_out<P, P>(r, pl);
+      const int i = i0 + pl;
+      if (live && i < tokens) {
+        const float2 s = ps[i * PW + pc], dy = pdy[i * PW + pc], u = pu[i * PW + pc];
+        const float2 du = fma2(s, w[0], mul2(skip, dy));
+        // r holds A log2(e)
+        const float2 dd = mul2(fma2(u, w[0], mul2(r[0], f2(0.69314718055994530942f))), pslope[i * PW + pc]);
+        put_pair(out_u + i0 * g.gu.st, du, pairs_ok, second);
+        put_pair(out_d + i0 * g.gdelta.st, dd, pairs_ok, second);
+        sum_D = fma2(dy, u, sum_D);
+        sum_bias = add2(sum_bias, dd);
       }
     }
+    out_u -= kTile * g.gu.st;
+    out_d -= kTile * g.gdelta.st;
+    out_z -= kTile * g.gz.st;
+    part_B -= kTile * part_step;
+    part_C -= kTile * part_step;
     __syncwarp();
   }
 
-  for (int m = 0; m < M; ++m) {
-    const int pair0 = (pb * M + m) * PW, pair = pair0 + pc, off = 2 * m * PW;
-    const int64_t to = (int64_t)span * g.B + b;
-    if (pc < PW && pair < g.pairs) {
-      const int c = grp * g.Dg + 2 * pair;
-      const bool second = 2 * pair + 1 < g.Dg;
-      float2 v[kStates];
-      load_own(keep_at(m, 2), v);
-      store_states(g.part_A + (to * g.D + c) * g.N, g.N, pl * kStates, second, v);
-      if (span == 0 && g.grad_state_in) {
-        load_own(keep_at(m, 1), v);
-        store_states(g.grad_state_in + ((int64_t)b * g.D + c) * g.N, g.N, pl * kStates, second, v);
-      }
-    }
-    __syncwarp();
-    if (row < R && pair0 + pr < g.pairs) {
-      const int c = c0 + off;
-      const bool second = 2 * (pair0 + pr) + 1 < g.Dg;
-      // places past the sequence's end
-      for (int now = first + tiles * kTile + row; now < last; now += R) {
-        put_pair(ou + now * g.gu.st + off, f2(0.0f), pairs_ok, second);
-        put_pair(od + now * g.gdelta.st + off, f2(0.0f), pairs_ok, second);
-        if (gate) put_pair(oz + now * g.gz.st + off, f2(0.0f), pairs_ok, second);
-      }
-      // grad_D and grad_delta_bias: the rows of a pair, in order
-      if (row == 0) {
-        float4 v = keep2[m * 32 + pr];
-        for (int k = 1; k < R; ++k) {
-          const float4 w = keep2[m * 32 + k * PW + pr];
-          v.x += w.x, v.y += w.y, v.z += w.z, v.w += w.w;
-        }
-        g.part_D[to * g.D + c] = v.x;
-        g.part_bias[to * g.D + c] = v.z;
-        if (second) {
-          g.part_D[to * g.D + c + 1] = v.y;
-          g.part_bias[to * g.D + c + 1] = v.w;
-        }
-      }
+  sum_D = sum_pair<P>(sum_D);
+  sum_bias = sum_pair<P>(sum_bias);
+  if (!live) return;
+  // places past the sequence's end
+  auto base = [&](const Seq& x, int now) { return static_cast<T*>(x.data) + b * x.sb + now * x.st + c; };
+  for (int now = (stop > first ? stop : first) + pl; now < last; now += P) {
+    put_pair(base(g.gu, now), f2(0.0f), pairs_ok, second);
+    put_pair(base(g.gdelta, now), f2(0.0f), pairs_ok, second);
+    if (gate) put_pair(base(g.gz, now), f2(0.0f), pairs_ok, second);
+  }
+  const int64_t to = (int64_t)span * g.B + b;
+  store_states<NS>(g.part_A + (to * g.D + c) * g.N, g.N, n0, second, dA);
+  if (span == 0 && g.grad_state_in)
+    store_states<NS>(g.grad_state_in + ((int64_t)b * g.D + c) * g.N, g.N, n0, second, gam);
+  if (pl == 0) {
+    g.part_D[to * g.D + c] = sum_D.x;
+    g.part_bias[to * g.D + c] = sum_bias.x;
+    if (second) {
+      g.part_D[to * g.D + c + 1] = sum_D.y;
+      g.part_bias[to * g.D + c + 1] = sum_bias.y;
     }
   }
+}
+
+template <typename T, int NS, int P>
+__global__ void __launch_bounds__(32 * kWarps, blocks_of(NS)) scan_bwd(const Args g, int64_t works) {
+  extern __shared__ __align__(16) unsigned char scan_smem[];
+  __shared__ uint32_t tmem_slot;
+  const int warp = threadIdx.x >> 5;
+  if (warp == 0) tmem_alloc(&tmem_slot, columns_of(NS));
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  const uint32_t tmem = tmem_slot;
+  grid_dep_wait();
+  const int64_t work = (int64_t)blockIdx.x * kWarps + warp;
+  if (work < works)
+    scan_back<T, NS, P>(g, work, scan_smem + warp * bwd_smem(NS, P), tmem + ((uint32_t)(warp * 32) << 16));
+  tc_fence_before();
+  __syncthreads();
+  if (warp == 0) tmem_dealloc(tmem, columns_of(NS));
 }
 
 // grad_B and grad_C: the warps' shares in order; zero past a sequence's end.
@@ -326,6 +405,7 @@ __global__ void __launch_bounds__(256) scan_sum_bc(const Args g, Mat gB, Mat gC,
   const int tok = (int)(rest % g.T), b = (int)(rest / g.T);
   float vb = 0.0f, vc = 0.0f;
   if (tok < seq_len(g, b)) {
+#pragma unroll 16
     for (int k = 0; k < blocks; ++k) {
       vb += g.part_B[k * all + i];
       vc += g.part_C[k * all + i];
@@ -368,19 +448,23 @@ BwdSpace bwd_space(const Args& g, const BwdPlan& p) {
   return s;
 }
 
-template <typename T, int PT>
-cudaError_t launch_main(const Args& g, const BwdPlan& p, int64_t blocks, cudaStream_t st) {
-  const size_t smem = bwd_smem(g.P, p.per_block);
-  const cudaError_t e = ensure_smem((const void*)scan_bwd<T, PT>, smem);
+template <typename T, int NS, int P>
+cudaError_t launch_main(const Args& g, int64_t works, cudaStream_t st) {
+  const size_t smem = (size_t)kWarps * bwd_smem(NS, P);
+  // with the kernel's static shared memory, past the limit that needs no asking
+  const size_t ask = smem + 1024 > 48 * 1024 && smem <= 48 * 1024 ? 48 * 1024 + 16 : smem;
+  const cudaError_t e = ensure_smem((const void*)scan_bwd<T, NS, P>, ask);
   if (e != cudaSuccess) return e;
-  return launch_pdl(scan_bwd<T, PT>, dim3((unsigned)blocks, (unsigned)g.spans), dim3(32), smem, st, g);
+  return launch_pdl(scan_bwd<T, NS, P>, dim3((unsigned)ceil_div(works, kWarps)), dim3(32 * kWarps), smem, st, g, works);
 }
 
 template <typename T>
 cudaError_t launch_bwd(const Args& g, const BwdPlan& p, const Mat& gB, const Mat& gC, cudaStream_t st) {
-  const int64_t blocks = (int64_t)g.B * g.G * p.blocks, all = (int64_t)g.B * g.T * g.G * g.N;
-  if (blocks > 0x7fffffff || ceil_div(all, 256) > 0x7fffffff) return cudaErrorInvalidValue;
-  const cudaError_t e = g.P == 4 ? launch_main<T, 4>(g, p, blocks, st) : launch_main<T, 0>(g, p, blocks, st);
+  const int64_t works = warps_of(g, p.lay) * g.spans, all = (int64_t)g.B * g.T * g.G * g.N;
+  if (works > 0x7fffffff || ceil_div(all, 256) > 0x7fffffff) return cudaErrorInvalidValue;
+  const cudaError_t e = with_lay(p.lay, [&](auto NS, auto P) {
+    return launch_main<T, decltype(NS)::value, decltype(P)::value>(g, works, st);
+  });
   if (e != cudaSuccess || all == 0) return e;
   return launch_pdl(scan_sum_bc<T>, dim3((unsigned)ceil_div(all, 256)), dim3(256), 0, st, g, gB, gC, p.blocks);
 }
@@ -449,7 +533,6 @@ snn_status_t snn_selective_scan_bwd(const snn_sscan_desc* desc, const snn_btc* u
   g.quads = quads(g, {&g.Bm, &g.Cm});
   g.spans = plan.cut.spans;
   g.span = plan.cut.span;
-  g.per_block = plan.per_block;
   g.A = A;
   g.D_skip = D;
   g.bias = delta_bias;
@@ -474,7 +557,7 @@ snn_status_t snn_selective_scan_bwd(const snn_sscan_desc* desc, const snn_btc* u
   cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
   cudaError_t e = cudaSuccess;
   if (g.B > 0) {
-    if (g.spans > 1) e = launch_back_ends(g, desc->dtype, st);
+    if (g.spans > 1) e = launch_back_ends(g, plan.lay, desc->dtype, st);
     if (e == cudaSuccess)
       e = desc->dtype == SNN_F32    ? launch_bwd<float>(g, plan, gB, gC, st)
           : desc->dtype == SNN_BF16 ? launch_bwd<__nv_bfloat16>(g, plan, gB, gC, st)

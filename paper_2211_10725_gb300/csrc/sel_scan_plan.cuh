@@ -1,5 +1,7 @@
-// How a selective scan's axis is cut, from the shape alone.
+// How a selective scan is laid on threads and its axis cut, from the shape alone.
 #pragma once
+
+#include <type_traits>
 
 #include "sel_scan.cuh"
 
@@ -7,25 +9,6 @@ namespace snn {
 namespace sscan {
 
 constexpr int kSms = 152;
-
-// Channel pairs of tokens that a thread of a warp loads for a tile, for PT threads of a
-// pair (0: any number).
-__host__ __device__ constexpr int units_of(int PT) {
-  return PT == 0 ? kTile : (kTile + 32 / (32 / PT) - 1) / (32 / (32 / PT));
-}
-
-// Sum of the parts that the P threads of a pair left side by side.
-template <int PT>
-__device__ __forceinline__ float2 sum_parts(const float2* p, int P) {
-  if constexpr (PT == 4) {
-    const float4 a = reinterpret_cast<const float4*>(p)[0], b = reinterpret_cast<const float4*>(p)[1];
-    return add2(add2(make_float2(a.x, a.y), make_float2(a.z, a.w)), add2(make_float2(b.x, b.y), make_float2(b.z, b.w)));
-  } else {
-    float2 v = p[0];
-    for (int i = 1; i < P; ++i) v = add2(v, p[i]);
-    return v;
-  }
-}
 
 // Cuts for `warps` warps of a whole axis: as many as make whole rounds of the
 // `resident` warps that the GPU holds at once, of at least kMinSpan tokens.
@@ -36,10 +19,10 @@ inline Plan cut(int64_t T, int64_t warps, int64_t resident, int rounds) {
   double used = 0.0;
   for (int r = 1; r <= rounds && warps > 0; ++r) {
     int64_t spans = r * resident / warps;
-    if (spans < 1) continue;
     if (spans > most) spans = most;
+    if (spans < 1) continue;
     const double u = (double)(spans * warps) / (double)(ceil_div(spans * warps, resident) * resident);
-    if (spans >= 1 && u > used + 0.03) used = u, best = spans;
+    if (u > used + 0.03) used = u, best = spans;
   }
   Plan p;
   p.span = (int)round_up(T > 0 ? ceil_div(T, best) : 1, kTile);
@@ -47,14 +30,51 @@ inline Plan cut(int64_t T, int64_t warps, int64_t resident, int rounds) {
   return p;
 }
 
-inline Plan fwd_plan(const Args& g) {
-  return cut(g.T, (int64_t)g.B * g.G * ceil_div(g.pairs, 32 / g.P), kSms * 16, 1);
+// States of a thread and threads of a pair.
+struct Lay {
+  int NS, P;
+};
+inline Lay lay_of(int N) {
+  return N <= 4 ? Lay{4, 1} : N <= 8 ? Lay{4, 2} : N <= 16 ? Lay{8, 2} : N <= 24 ? Lay{12, 2}
+       : N <= 32 ? Lay{8, 4} : N <= 48 ? Lay{12, 4} : Lay{16, 4};
 }
-inline size_t fwd_bytes(const Args& g, const Plan& p) {
-  return p.spans > 1 ? ends_bytes(g, p.spans) + sums_bytes(g, p.spans) : 0;
+inline int64_t warps_of(const Args& g, Lay l) { return (int64_t)g.B * g.G * ceil_div(g.pairs, 32 / l.P); }
+
+// f(states, threads) as constants.
+template <typename F>
+cudaError_t with_lay(Lay l, F f) {
+  using std::integral_constant;
+  if (l.P == 1) return f(integral_constant<int, 4>(), integral_constant<int, 1>());
+  if (l.P == 2) {
+    if (l.NS == 4) return f(integral_constant<int, 4>(), integral_constant<int, 2>());
+    if (l.NS == 8) return f(integral_constant<int, 8>(), integral_constant<int, 2>());
+    return f(integral_constant<int, 12>(), integral_constant<int, 2>());
+  }
+  if (l.NS == 4) return f(integral_constant<int, 4>(), integral_constant<int, 4>());
+  if (l.NS == 8) return f(integral_constant<int, 8>(), integral_constant<int, 4>());
+  if (l.NS == 12) return f(integral_constant<int, 12>(), integral_constant<int, 4>());
+  return f(integral_constant<int, 16>(), integral_constant<int, 4>());
 }
 
-cudaError_t launch_back_ends(const Args& g, int dtype, cudaStream_t st);
+struct FwdPlan {
+  Lay lay;
+  Plan cut;
+};
+inline FwdPlan fwd_plan(const Args& g) {
+  FwdPlan p;
+  p.lay = lay_of(g.N);
+  // too few channels and tokens to fill the GPU: more threads to a pair
+  const int64_t spans = g.T >= kMinSpan ? g.T / kMinSpan : 1;
+  if (warps_of(g, p.lay) * spans < kSms * 8 && g.N > 4 && g.N <= 24)
+    p.lay = g.N <= 8 ? Lay{4, 2} : g.N <= 16 ? Lay{4, 4} : Lay{8, 4};
+  p.cut = cut(g.T, warps_of(g, p.lay), kSms * 16, 1);
+  return p;
+}
+inline size_t fwd_bytes(const Args& g, const FwdPlan& p) {
+  return p.cut.spans > 1 ? ends_bytes(g, p.cut.spans) + sums_bytes(g, p.cut.spans) : 0;
+}
+
+cudaError_t launch_back_ends(const Args& g, Lay lay, int dtype, cudaStream_t st);
 
 }  // namespace sscan
 }  // namespace snn

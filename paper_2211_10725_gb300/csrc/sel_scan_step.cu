@@ -69,7 +69,7 @@ __global__ void __launch_bounds__(kStepThreads) scan_step(const StepArgs a) {
   if (g.z.data) z = Elem<T>::load1(static_cast<const T*>(g.z.data) + b * g.z.sb + c);
   if (g.bias) s += g.bias[c];
   const float skip = g.D_skip ? g.D_skip[c] : 0.0f;
-  if (g.softplus) s = softplus(f2(s), nullptr).x;
+  if (g.softplus) s = softplus<T>(f2(s), nullptr).x;
   const float x = s * u, s2 = s * kLog2E;
   float y = 0.0f;
 #pragma unroll
