@@ -5,7 +5,7 @@
 //   d_t = grad_y_t act'(p_t);   grad_x_t = sum_j w[j] d_{t+W-1-j}
 //   grad_w[j] = sum_t d_t x_{t-W+1+j};   grad_bias = sum_t d_t
 // Each tensor is read and written once and a channel-token takes 2 W operations
-// beside its activation, so the bound is HBM.  A thread takes V neighbouring channels
+// beside its activation, so the bound is HBM.  A thread takes four neighbouring channels
 // (one vector access) over a run of tokens and keeps the last W - 1 inputs (the
 // backward: and gradients) in registers; four tokens' loads are started before the first
 // is used.  Neighbouring runs read W - 1 tokens twice, out of L2.  The parameters'
@@ -17,6 +17,7 @@
 
 #include <cmath>
 #include <cstdint>
+#include <type_traits>
 
 #include "launch.cuh"
 #include "scan_host.cuh"
@@ -29,7 +30,7 @@ namespace cconv {
 constexpr int kThreads = 256;
 constexpr int kAhead = 4;      // tokens whose loads are in flight
 constexpr int kMinRun = 4;     // at least W - 1: later runs never look at the state
-constexpr int kBwdV = 4;       // channels of a backward thread
+constexpr int kV = 4;          // channels of a thread
 
 struct Tensor {
   void* data = nullptr;
@@ -52,6 +53,26 @@ struct Args {
   int lanes;      // backward: threads across the channels
 };
 
+// A thread's channels in pairs, one instruction for both (or a single one).
+template <int V>
+using Lane = typename std::conditional<V == 1, float, float2>::type;
+template <int V>
+constexpr int kLanes = V == 1 ? 1 : V / 2;
+__device__ __forceinline__ float fma2(float a, float b, float c) { return fmaf(a, b, c); }
+__device__ __forceinline__ float mul2(float a, float b) { return a * b; }
+__device__ __forceinline__ float add2(float a, float b) { return a + b; }
+using snn::add2;
+using snn::fma2;
+using snn::mul2;
+template <typename L>
+__device__ __forceinline__ L all(float a);
+template <>
+__device__ __forceinline__ float all<float>(float a) { return a; }
+template <>
+__device__ __forceinline__ float2 all<float2>(float a) { return make_float2(a, a); }
+__device__ __forceinline__ float at(float v, int) { return v; }
+__device__ __forceinline__ float at(float2 v, int i) { return i ? v.y : v.x; }
+
 // 1 / (1 + e^-p).  Results rounded to 16 bits take the approximate power of
 // two and reciprocal: the rounding of p log2(e) costs |p| 2^-24 of the result.
 template <typename T>
@@ -63,12 +84,24 @@ __device__ __forceinline__ float sigmoid(float p) {
   asm("rcp.approx.ftz.f32 %0, %0;" : "+f"(e));
   return e;
 }
+template <typename T>
+__device__ __forceinline__ float2 sigmoid(float2 p) {
+  if constexpr (sizeof(T) == 4) return make_float2(sigmoid<T>(p.x), sigmoid<T>(p.y));
+  float2 e = mul2(p, make_float2(-1.44269504088896340736f, -1.44269504088896340736f));
+  asm("ex2.approx.ftz.f32 %0, %0;" : "+f"(e.x));
+  asm("ex2.approx.ftz.f32 %0, %0;" : "+f"(e.y));
+  e = add2(e, make_float2(1.0f, 1.0f));
+  asm("rcp.approx.ftz.f32 %0, %0;" : "+f"(e.x));
+  asm("rcp.approx.ftz.f32 %0, %0;" : "+f"(e.y));
+  return e;
+}
 
-// V channels; V = 1 at any element's address.
+// V channels as they lie in memory; V = 1 at any element's address.
 template <typename T, int V>
 struct Vec {
-  static constexpr int kWords = V * (int)sizeof(T) / 4;
-  uint32_t w[kWords ? kWords : 1];
+  using L = Lane<V>;
+  static constexpr int kWords = V == 1 ? 1 : V * (int)sizeof(T) / 4;
+  uint32_t w[kWords];
   __device__ __forceinline__ void load(const T* p) {
     if constexpr (V == 1) {
       if constexpr (sizeof(T) == 4) w[0] = *reinterpret_cast<const uint32_t*>(p);
@@ -82,22 +115,38 @@ struct Vec {
       w[0] = a.x, w[1] = a.y;
     }
   }
-  __device__ __forceinline__ void clear() {
-#pragma unroll
-    for (int i = 0; i < (kWords ? kWords : 1); ++i) w[i] = 0;
-  }
-  __device__ __forceinline__ void get(float v[V]) const {
+  __device__ __forceinline__ void store(T* p) const {
     if constexpr (V == 1) {
-      v[0] = Elem<T>::load1(reinterpret_cast<const T*>(w));
-    } else if constexpr (V == 8) {
-      Elem<T>::load8(reinterpret_cast<const T*>(w), v);
+      if constexpr (sizeof(T) == 4) *reinterpret_cast<uint32_t*>(p) = w[0];
+      else *reinterpret_cast<uint16_t*>(p) = (uint16_t)w[0];
+    } else if constexpr (kWords == 4) {
+      *reinterpret_cast<uint4*>(p) = make_uint4(w[0], w[1], w[2], w[3]);
     } else {
-      Elem<T>::load4(reinterpret_cast<const T*>(w), v);
+      *reinterpret_cast<uint2*>(p) = make_uint2(w[0], w[1]);
     }
   }
-  __device__ __forceinline__ static void put(T* p, const float v[V]) {
-    if constexpr (V == 1) Elem<T>::store1(p, v[0]);
-    else storev<T, V>(p, v);
+  __device__ __forceinline__ void clear() {
+#pragma unroll
+    for (int i = 0; i < kWords; ++i) w[i] = 0;
+  }
+  __device__ __forceinline__ void get(L (&v)[kLanes<V>]) const {
+    if constexpr (V == 1) {
+      v[0] = Elem<T>::load1(reinterpret_cast<const T*>(w));
+    } else if constexpr (sizeof(T) == 2) {
+#pragma unroll
+      for (int i = 0; i < V / 2; ++i) v[i] = Elem<T>::to2(w[i]);
+    } else {
+#pragma unroll
+      for (int i = 0; i < V / 2; ++i) v[i] = make_float2(__uint_as_float(w[2 * i]), __uint_as_float(w[2 * i + 1]));
+    }
+  }
+  __device__ __forceinline__ static void put(T* p, const L (&v)[kLanes<V>]) {
+    if constexpr (V == 1) {
+      Elem<T>::store1(p, v[0]);
+    } else {
+      const float a[4] = {v[0].x, v[0].y, v[1].x, v[1].y};
+      Elem<T>::store4(p, a);
+    }
   }
 };
 
@@ -131,40 +180,38 @@ struct Run {
 };
 
 template <int V, int W>
-__device__ __forceinline__ void load_params(const Args& g, int c, float (&w)[W][V], float (&bias)[V]) {
-  float flat[V * W];  // a thread's channels' taps lie together
-  const float* p = g.w + (int64_t)c * W;
-  if constexpr (V >= 4) {
+__device__ __forceinline__ void load_params(const Args& g, int c, Lane<V> (&w)[W][kLanes<V>], Lane<V> (&bias)[kLanes<V>]) {
+  const float* p = g.w + (int64_t)c * W;  // a thread's channels' taps lie together
+  if constexpr (V == 1) {
+#pragma unroll
+    for (int j = 0; j < W; ++j) w[j][0] = p[j];
+    bias[0] = g.bias ? g.bias[c] : 0.0f;
+  } else {
+    float flat[V * W], b[V] = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
     for (int i = 0; i < V * W; i += 4) Elem<float>::load4(p + i, flat + i);
-    if (g.bias) {
+    if (g.bias) Elem<float>::load4(g.bias + c, b);
 #pragma unroll
-      for (int i = 0; i < V; i += 4) Elem<float>::load4(g.bias + c + i, bias + i);
+    for (int i = 0; i < V / 2; ++i) {
+#pragma unroll
+      for (int j = 0; j < W; ++j) w[j][i] = make_float2(flat[2 * i * W + j], flat[(2 * i + 1) * W + j]);
+      bias[i] = make_float2(b[2 * i], b[2 * i + 1]);
     }
-  } else {
-#pragma unroll
-    for (int i = 0; i < V * W; ++i) flat[i] = p[i];
-    if (g.bias) bias[0] = g.bias[c];
-  }
-#pragma unroll
-  for (int v = 0; v < V; ++v) {
-#pragma unroll
-    for (int j = 0; j < W; ++j) w[j][v] = flat[v * W + j];
-    if (!g.bias) bias[v] = 0.0f;
   }
 }
 
 template <typename T, int V, int W>
 __global__ void __launch_bounds__(kThreads) conv_fwd(const Args g) {
+  constexpr int N = kLanes<V>;
+  using L = Lane<V>;
   grid_dep_wait();
-  const int cv = g.C / V;
-  const int64_t unit = (int64_t)blockIdx.x * kThreads + threadIdx.x, lane = unit / cv;
-  if (lane >= (int64_t)g.B * g.runs) return;
-  const int b = (int)(lane / g.runs), r = (int)(lane - (int64_t)b * g.runs);
+  const unsigned cv = g.C / V, unit = blockIdx.x * kThreads + threadIdx.x, lane = unit / cv;
+  if (lane >= (unsigned)(g.B * g.runs)) return;
+  const int b = (int)(lane / g.runs), r = (int)(lane - b * g.runs);
   const Run<T, V, W> at{g, b, (int)(unit - lane * cv) * V, seq_len(g, b), g.slots ? (int64_t)g.slots[b] : (int64_t)b};
   const int t0 = r * g.run, t1 = t0 + g.run < g.T ? t0 + g.run : g.T;
   const int len = g.step && !at.has_place() ? 0 : at.len;
-  float win[W][V];  // x of the last W tokens
+  L win[W][N];  // x of the last W tokens
   {
     Vec<T, V> first[W - 1];
 #pragma unroll
@@ -175,35 +222,46 @@ __global__ void __launch_bounds__(kThreads) conv_fwd(const Args g) {
 #pragma unroll
     for (int j = 0; j < W - 1; ++j) first[j].get(win[j + 1]);
   }
-  float w[W][V], bias[V];
+  L w[W][N], bias[N];
   load_params<V, W>(g, at.c, w, bias);
-  for (int t = t0; t < t1; t += kAhead) {
-    Vec<T, V> raw[kAhead];
+  const T* px = at.row(g.x, t0);
+  T* py = at.row_out(g.y, t0);
+  Vec<T, V> raw[kAhead];
+  auto fetch = [&](int t) {
 #pragma unroll
     for (int i = 0; i < kAhead; ++i) {
       raw[i].clear();
-      if (t + i < t1 && t + i < len) raw[i].load(at.row(g.x, t + i));
+      if (t + i < t1 && t + i < len) raw[i].load(px + i * g.x.st);
     }
+    px += kAhead * g.x.st;
+  };
+  fetch(t0);
+  for (int t = t0; t < t1; t += kAhead) {
+    Vec<T, V> now[kAhead];
+#pragma unroll
+    for (int i = 0; i < kAhead; ++i) now[i] = raw[i];
+    fetch(t + kAhead);
 #pragma unroll
     for (int i = 0; i < kAhead; ++i) {
       if (t + i < t1) {
-        float y[V];
+        L y[N];
 #pragma unroll
         for (int j = 0; j < W - 1; ++j)
 #pragma unroll
-          for (int v = 0; v < V; ++v) win[j][v] = win[j + 1][v];
-        raw[i].get(win[W - 1]);
+          for (int v = 0; v < N; ++v) win[j][v] = win[j + 1][v];
+        now[i].get(win[W - 1]);
 #pragma unroll
-        for (int v = 0; v < V; ++v) {
-          float p = bias[v];
+        for (int v = 0; v < N; ++v) {
+          L p = bias[v];
 #pragma unroll
-          for (int j = 0; j < W; ++j) p = fmaf(w[j][v], win[j][v], p);
-          if (g.silu) p *= sigmoid<T>(p);
-          y[v] = t + i < len ? p : 0.0f;
+          for (int j = 0; j < W; ++j) p = fma2(w[j][v], win[j][v], p);
+          if (g.silu) p = mul2(p, sigmoid<T>(p));
+          y[v] = t + i < len ? p : all<L>(0.0f);
         }
-        Vec<T, V>::put(at.row_out(g.y, t + i), y);
+        Vec<T, V>::put(py + i * g.y.st, y);
       }
     }
+    py += kAhead * g.y.st;
   }
   // the last W - 1 inputs; in ascending order, as state_out may be state_in
   if (r == 0 && g.state_out && at.has_place()) {
@@ -211,16 +269,16 @@ __global__ void __launch_bounds__(kThreads) conv_fwd(const Args g) {
     for (int j = 0; j < W - 1; ++j) {
       Vec<T, V> v;
       at.input(at.len - (W - 1) + j, v);
-      float f[V];
-      v.get(f);
-      Vec<T, V>::put(static_cast<T*>(g.state_out) + at.state_at(at.place, j), f);
+      v.store(static_cast<T*>(g.state_out) + at.state_at(at.place, j));
     }
   }
 }
 
 template <typename T, int V, int W>
-__global__ void __launch_bounds__(kThreads) conv_bwd(const Args g) {
+__global__ void __launch_bounds__(kThreads, 2) conv_bwd(const Args g) {
   extern __shared__ float conv_smem[];  // [runs of a block][lanes V][W + 1]
+  constexpr int N = kLanes<V>;
+  using L = Lane<V>;
   grid_dep_wait();
   const int lanes = g.lanes, rows = kThreads / lanes, cv = g.C / V;
   const int cblocks = (cv + lanes - 1) / lanes, rblocks = (g.runs + rows - 1) / rows;
@@ -228,17 +286,19 @@ __global__ void __launch_bounds__(kThreads) conv_bwd(const Args g) {
   const int rb = rest % rblocks, b = rest / rblocks;
   const int lane = threadIdx.x % lanes, ty = threadIdx.x / lanes;
   const int vec = cb * lanes + lane, r = rb * rows + ty;
-  float dw[W][V], db[V];
+  const L zero = all<L>(0.0f);
+  L dw[W][N], db[N];
 #pragma unroll
-  for (int v = 0; v < V; ++v) {
-    db[v] = 0.0f;
+  for (int v = 0; v < N; ++v) {
+    db[v] = zero;
 #pragma unroll
-    for (int j = 0; j < W; ++j) dw[j][v] = 0.0f;
+    for (int j = 0; j < W; ++j) dw[j][v] = zero;
   }
   if (vec < cv && r < g.runs) {
     const Run<T, V, W> at{g, b, vec * V, seq_len(g, b), (int64_t)b};
     const int t0 = r * g.run, t1 = t0 + g.run < g.T ? t0 + g.run : g.T, len = at.len;
-    float w[W][V], bias[V], win[W][V], d[W][V];  // the last W inputs; the last W gradients
+    const int end = t1 + W - 1;  // token t gives grad_x of token t - W + 1
+    L w[W][N], bias[N], win[W][N], d[W][N];  // the last W inputs; the last W gradients
     load_params<V, W>(g, at.c, w, bias);
 #pragma unroll
     for (int j = 0; j < W - 1; ++j) {
@@ -250,50 +310,60 @@ __global__ void __launch_bounds__(kThreads) conv_bwd(const Args g) {
 #pragma unroll
     for (int j = 0; j < W; ++j)
 #pragma unroll
-      for (int v = 0; v < V; ++v) d[j][v] = 0.0f;
-    // token t gives grad_x of token t - W + 1: W - 1 tokens past the run's end
-    for (int t = t0; t < t1 + W - 1; t += kAhead) {
-      Vec<T, V> raw[kAhead], raw_gy[kAhead];
+      for (int v = 0; v < N; ++v) d[j][v] = zero;
+    const T *px = at.row(g.x, t0), *pg = at.row(g.gy, t0);
+    T* po = at.row_out(g.gx, t0) - (W - 1) * g.gx.st;
+    Vec<T, V> raw[kAhead], raw_gy[kAhead];
+    auto fetch = [&](int t) {
 #pragma unroll
       for (int i = 0; i < kAhead; ++i) {
         raw[i].clear();
         raw_gy[i].clear();
-        if (t + i < t1 + W - 1 && t + i < len) {
-          raw[i].load(at.row(g.x, t + i));
-          raw_gy[i].load(at.row(g.gy, t + i));
+        if (t + i < end && t + i < len) {
+          raw[i].load(px + i * g.x.st);
+          raw_gy[i].load(pg + i * g.gy.st);
         }
       }
+      px += kAhead * g.x.st;
+      pg += kAhead * g.gy.st;
+    };
+    fetch(t0);
+    for (int t = t0; t < end; t += kAhead) {
+      Vec<T, V> now_x[kAhead], now_gy[kAhead];
+#pragma unroll
+      for (int i = 0; i < kAhead; ++i) now_x[i] = raw[i], now_gy[i] = raw_gy[i];
+      fetch(t + kAhead);
 #pragma unroll
       for (int i = 0; i < kAhead; ++i) {
         const int now = t + i;
-        if (now < t1 + W - 1) {
-          float gx[V], gy[V];
+        if (now < end) {
+          L gx[N], gy[N];
 #pragma unroll
           for (int j = 0; j < W - 1; ++j)
 #pragma unroll
-            for (int v = 0; v < V; ++v) win[j][v] = win[j + 1][v], d[j][v] = d[j + 1][v];
-          raw[i].get(win[W - 1]);
-          raw_gy[i].get(gy);
+            for (int v = 0; v < N; ++v) win[j][v] = win[j + 1][v], d[j][v] = d[j + 1][v];
+          now_x[i].get(win[W - 1]);
+          now_gy[i].get(gy);
 #pragma unroll
-          for (int v = 0; v < V; ++v) {
-            float p = bias[v];
-#pragma unroll
-            for (int j = 0; j < W; ++j) p = fmaf(w[j][v], win[j][v], p);
-            float slope = 1.0f;
+          for (int v = 0; v < N; ++v) {
+            L dt = gy[v];
             if (g.silu) {
-              const float s = sigmoid<T>(p);
-              slope = fmaf(p * s, 1.0f - s, s);
+              L p = bias[v];
+#pragma unroll
+              for (int j = 0; j < W; ++j) p = fma2(w[j][v], win[j][v], p);
+              const L s = sigmoid<T>(p);
+              dt = mul2(dt, fma2(mul2(p, s), fma2(s, all<L>(-1.0f), all<L>(1.0f)), s));
             }
-            const float dt = now < len ? gy[v] * slope : 0.0f;
+            if (now >= len) dt = zero;
             d[W - 1][v] = dt;
             if (now < t1 && now < len) {
-              db[v] += dt;
+              db[v] = add2(db[v], dt);
 #pragma unroll
-              for (int j = 0; j < W; ++j) dw[j][v] = fmaf(dt, win[j][v], dw[j][v]);
+              for (int j = 0; j < W; ++j) dw[j][v] = fma2(dt, win[j][v], dw[j][v]);
             }
-            gx[v] = 0.0f;
+            gx[v] = mul2(w[0][v], d[W - 1][v]);
 #pragma unroll
-            for (int j = 0; j < W; ++j) gx[v] = fmaf(w[j][v], d[W - 1 - j][v], gx[v]);
+            for (int j = 1; j < W; ++j) gx[v] = fma2(w[j][v], d[W - 1 - j][v], gx[v]);
           }
           const int to = now - (W - 1);
           if (to >= t0 || r == 0) {
@@ -303,19 +373,20 @@ __global__ void __launch_bounds__(kThreads) conv_bwd(const Args g) {
               s.load(static_cast<const T*>(g.grad_state_out) + at.state_at(b, j));
               s.get(gy);
 #pragma unroll
-              for (int v = 0; v < V; ++v) gx[v] += gy[v];
+              for (int v = 0; v < N; ++v) gx[v] = add2(gx[v], gy[v]);
             }
             if (to >= len)
 #pragma unroll
-              for (int v = 0; v < V; ++v) gx[v] = 0.0f;
+              for (int v = 0; v < N; ++v) gx[v] = zero;
             if (to >= 0) {
-              if (g.gx.data) Vec<T, V>::put(at.row_out(g.gx, to), gx);
+              if (g.gx.data) Vec<T, V>::put(po + i * g.gx.st, gx);
             } else if (g.grad_state_in) {
               Vec<T, V>::put(static_cast<T*>(g.grad_state_in) + at.state_at(b, W - 1 + to), gx);
             }
           }
         }
       }
+      po += kAhead * g.gx.st;
     }
   }
   if (!g.part) return;
@@ -324,8 +395,8 @@ __global__ void __launch_bounds__(kThreads) conv_bwd(const Args g) {
   for (int v = 0; v < V; ++v) {
     float* s = conv_smem + ((int64_t)ty * width + lane * V + v) * (W + 1);
 #pragma unroll
-    for (int j = 0; j < W; ++j) s[j] = dw[j][v];
-    s[W] = db[v];
+    for (int j = 0; j < W; ++j) s[j] = cconv::at(dw[j][v / 2], v & 1);
+    s[W] = cconv::at(db[v / 2], v & 1);
   }
   __syncthreads();
   float* part = g.part + (int64_t)rest * g.C * (W + 1);
@@ -369,7 +440,6 @@ __global__ void __launch_bounds__(1024) conv_sum(const float* __restrict__ part,
 constexpr int64_t kMost = int64_t(1) << 28;
 
 bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
-size_t elem_size(int dtype) { return dtype == SNN_F32 ? 4 : 2; }
 
 snn_status_t check_desc(const snn_conv_desc* d) {
   if (!d || d->reserved[0] || d->reserved[1]) return SNN_ERR_INVALID_ARG;
@@ -392,7 +462,7 @@ snn_status_t take(const snn_conv_desc* d, const snn_btc* x, Tensor* out, bool* v
   for (int i = 0; i < 2; ++i) {
     if (ext[i] <= 1) continue;
     if (str[i] <= 0 || str[i] >= (int64_t(1) << 38)) return SNN_ERR_INVALID_ARG;
-    if (str[i] % 8) *vec = false;
+    if (str[i] % kV) *vec = false;
   }
   out->data = x->data;
   out->sb = d->B > 1 ? x->stride_b : 0;
@@ -405,7 +475,7 @@ int lanes_for(int64_t vecs) { return vecs <= 8 ? 8 : vecs <= 16 ? 16 : 32; }
 // Tokens of a run: few enough to fill the GPU with threads, at most `most` (the
 // tokens that two runs share and a run's partial sums cost less in longer ones).
 int run_length(int64_t B, int64_t T, int64_t threads_across, int most) {
-  constexpr int64_t kFill = 152 * 2048;
+  constexpr int64_t kFill = 152 * 768;
   int run = most;
   while (run > kMinRun && B * snn::ceil_div(T, run) * threads_across < kFill) run /= 2;
   return run;
@@ -418,7 +488,7 @@ struct BwdPlan {
 };
 BwdPlan bwd_plan(int64_t B, int64_t T, int64_t C) {
   BwdPlan p;
-  p.run = run_length(B, T, snn::ceil_div(C, kBwdV), 64);
+  p.run = run_length(B, T, snn::ceil_div(C, kV), 64);
   p.runs = T > 0 ? (int)snn::ceil_div(T, p.run) : 1;  // of no tokens: the states' gradients pass through
   return p;
 }
@@ -428,8 +498,8 @@ template <typename T, int V, int W>
 cudaError_t launch_fwd(Args g, cudaStream_t st) {
   g.run = run_length(g.B, g.T, g.C / V, 32);
   g.runs = g.T > 0 ? (int)snn::ceil_div(g.T, g.run) : 1;  // of no tokens: the states pass through
-  const int64_t blocks = snn::ceil_div((int64_t)g.B * g.runs * (g.C / V), kThreads);
-  if (blocks > 0x7fffffff) return cudaErrorInvalidValue;
+  const int64_t units = (int64_t)g.B * g.runs * (g.C / V), blocks = snn::ceil_div(units, kThreads);
+  if (units > 0x7fffff00) return cudaErrorInvalidValue;
   return launch_pdl(conv_fwd<T, V, W>, dim3((unsigned)blocks), dim3(kThreads), 0, st, g);
 }
 
@@ -448,9 +518,8 @@ cudaError_t launch_bwd(Args g, cudaStream_t st) {
 
 template <typename T, int W>
 cudaError_t launch_width(const Args& g, bool bwd, bool vec, cudaStream_t st) {
-  constexpr int V = 16 / sizeof(T);
-  if (bwd) return vec ? launch_bwd<T, kBwdV, W>(g, st) : launch_bwd<T, 1, W>(g, st);
-  return vec ? launch_fwd<T, V, W>(g, st) : launch_fwd<T, 1, W>(g, st);
+  if (bwd) return vec ? launch_bwd<T, kV, W>(g, st) : launch_bwd<T, 1, W>(g, st);
+  return vec ? launch_fwd<T, kV, W>(g, st) : launch_fwd<T, 1, W>(g, st);
 }
 
 template <typename T>
@@ -486,8 +555,7 @@ snn_status_t forward(const snn_conv_desc* d, const snn_btc* x, const float* w, c
   if (!w || num_slots < 0 || num_slots > kMost) return SNN_ERR_INVALID_ARG;
   if ((state_in || state_out) && !slots && num_slots < d->B) return SNN_ERR_INVALID_ARG;
   Args g = base_args(d, w, bias);
-  const size_t e = elem_size(d->dtype);
-  bool vec = d->C % (16 / e) == 0;
+  bool vec = d->C % kV == 0;
   snn_status_t s;
   if (d->B == 0) return SNN_OK;
   if (d->T > 0 && ((s = take(d, x, &g.x, &vec)) != SNN_OK || (s = take(d, y, &g.y, &vec)) != SNN_OK)) return s;
@@ -514,7 +582,7 @@ size_t snn_causal_conv_workspace_bytes(const snn_conv_desc* desc) {
   if (check_desc(desc) != SNN_OK) return 0;
   // the element path has at most as many rows of partials as the vector path has, or more: the larger
   const BwdPlan p = bwd_plan(desc->B, desc->T, desc->C);
-  const int64_t a = bwd_rows(p, desc->B, desc->C), v = bwd_rows(p, desc->B, snn::ceil_div(desc->C, kBwdV));
+  const int64_t a = bwd_rows(p, desc->B, desc->C), v = bwd_rows(p, desc->B, snn::ceil_div(desc->C, kV));
   const size_t b = (size_t)(a > v ? a : v) * (size_t)desc->C * (size_t)(desc->W + 1) * sizeof(float);
   return b < 256 ? 256 : b;
 }
@@ -552,7 +620,7 @@ snn_status_t snn_causal_conv_bwd(const snn_conv_desc* desc, const snn_btc* x, co
   const bool params = grad_w || grad_bias;
   if (params && (!ws || ws_bytes < snn_causal_conv_workspace_bytes(desc))) return SNN_ERR_WORKSPACE;
   Args g = base_args(desc, w, bias);
-  bool vec = desc->C % (16 / elem_size(desc->dtype)) == 0;
+  bool vec = desc->C % kV == 0;
   if (desc->B > 0 && desc->T > 0) {
     if ((s = take(desc, x, &g.x, &vec)) != SNN_OK || (s = take(desc, grad_y, &g.gy, &vec)) != SNN_OK ||
         (grad_x && grad_x->data && (s = take(desc, grad_x, &g.gx, &vec)) != SNN_OK))
@@ -566,7 +634,7 @@ snn_status_t snn_causal_conv_bwd(const snn_conv_desc* desc, const snn_btc* x, co
   g.part = params ? static_cast<float*>(ws) : nullptr;
   cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
   const BwdPlan p = bwd_plan(desc->B, desc->T, desc->C);
-  const int64_t rows = bwd_rows(p, desc->B, vec ? desc->C / kBwdV : desc->C);
+  const int64_t rows = bwd_rows(p, desc->B, vec ? desc->C / kV : desc->C);
   cudaError_t e = cudaSuccess;
   if (rows > 0 && (params || g.gx.data || grad_state_in)) e = launch(desc, g, true, vec, st);
   if (e == cudaSuccess && params) {

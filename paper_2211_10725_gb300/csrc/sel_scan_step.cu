@@ -2,105 +2,171 @@
 //   h <- exp(s A) h + s u B,   y = (sum_n C h + D u) silu(z)
 // on fp32 states [num_slots, D, N] updated in place.  Each state is read and
 // written once (8 bytes for an exponential and five operations), so the bound is
-// HBM: neighbouring threads take neighbouring vectors of the states, one access
-// each, and a channel's sum goes through shuffles.
+// HBM: neighbouring threads take neighbouring vectors of the states, of four
+// sequences each, all on their way before the first is used.  The threads of a channel
+// share out the sequences where inputs are made ready and the outputs finished.
 #include "sel_scan.cuh"
+#include "sel_scan_plan.cuh"
 
 namespace snn {
 namespace sscan {
 
 constexpr int kStepThreads = 256;
+constexpr int kSeqs = 4;  // of a thread
 
 struct StepArgs {
   Args g;
-  int lanes;     // threads of a channel, a power of two up to 32
-  int bc_vec;    // B and C can be read in vectors of four
   float* state;
 };
 
-// V states of a thread; V = 4: N is a multiple of four
-template <typename T, int V>
+// V states of a thread (V = 4: N is a multiple of four), L threads of a channel; with V = 1 and L =
+// 32 a thread has two of up to 64
+template <typename T, int V, int L>
 __global__ void __launch_bounds__(kStepThreads) scan_step(const StepArgs a) {
   const Args& g = a.g;
-  constexpr int kPass = V == 4 ? 1 : 2;  // of V lanes states each; up to 64 states
+  constexpr int kPass = V == 1 && L == 32 ? 2 : 1, U = L < kSeqs ? kSeqs / L : 1;
   grid_dep_wait();
-  const int b = blockIdx.y, N = g.N;
-  const int lane = threadIdx.x & (a.lanes - 1);
-  const int64_t c64 = ((int64_t)blockIdx.x * kStepThreads + threadIdx.x) / a.lanes;
-  const int64_t place = g.slots ? (int64_t)g.slots[b] : (int64_t)b;
-  const bool live = c64 < g.D, used = place >= 0 && place < g.num_slots;
-  const int c = live ? (int)c64 : 0;
-  T* py = static_cast<T*>(g.y.data) + b * g.y.sb + c;
-  if (!used) {  // an empty place of the batch
-    if (live && lane == 0) Elem<T>::store1(py, 0.0f);
-    return;
+  const int b0 = blockIdx.y * kSeqs, N = g.N, l = threadIdx.x & (L - 1);
+  const int64_t c64 = ((int64_t)blockIdx.x * kStepThreads + threadIdx.x) / L;
+  const bool live = c64 < g.D;
+  const int c = live ? (int)c64 : 0, grp = c / g.Dg;
+  int64_t place[kSeqs];
+#pragma unroll
+  for (int j = 0; j < kSeqs; ++j) {
+    place[j] = -1;
+    if (b0 + j < g.B) place[j] = g.slots ? (int64_t)g.slots[b0 + j] : (int64_t)(b0 + j);
+    if (place[j] >= g.num_slots) place[j] = -1;
   }
-  float* st = a.state + (place * g.D + c) * (int64_t)N;
-  const float* pa = g.A + (int64_t)c * N;
-  const int grp = c / g.Dg;
-  const T* pb = static_cast<const T*>(g.Bm.data) + b * g.Bm.sb + grp * g.Bm.sg;
-  const T* pc = static_cast<const T*>(g.Cm.data) + b * g.Cm.sb + grp * g.Cm.sg;
-  float h[kPass][V], A[kPass][V], B[kPass][V], C[kPass][V];
+  float h[kSeqs][kPass][V], A[kPass][V];
+  Four<T> B4[kSeqs], C4[kSeqs];
+  float B1[kSeqs][kPass], C1[kSeqs][kPass];
 #pragma unroll
   for (int k = 0; k < kPass; ++k) {
-    const int n = (k * a.lanes + lane) * V;
-    if (live && n < N) {
-      if constexpr (V == 4) {
-        Elem<float>::load4(st + n, h[k]);
-        Elem<float>::load4(pa + n, A[k]);
-        if (a.bc_vec) {
-          Elem<T>::load4(pb + n, B[k]);
-          Elem<T>::load4(pc + n, C[k]);
+    const int n = (k * L + l) * V;
+    const bool in = live && n < N;
+#pragma unroll
+    for (int v = 0; v < V; ++v) A[k][v] = 0.0f;
+    if (in) {
+      if constexpr (V == 4) Elem<float>::load4(g.A + (int64_t)c * N + n, A[k]);
+      else A[k][0] = g.A[(int64_t)c * N + n];
+    }
+#pragma unroll
+    for (int j = 0; j < kSeqs; ++j) {
+#pragma unroll
+      for (int v = 0; v < V; ++v) h[j][k][v] = 0.0f;
+      if constexpr (V == 4) B4[j].clear(), C4[j].clear();
+      else B1[j][k] = C1[j][k] = 0.0f;
+      if (in && place[j] >= 0) {
+        const float* st = a.state + (place[j] * g.D + c) * (int64_t)N + n;
+        const T* pb = static_cast<const T*>(g.Bm.data) + (b0 + j) * g.Bm.sb + grp * g.Bm.sg + n;
+        const T* pc = static_cast<const T*>(g.Cm.data) + (b0 + j) * g.Cm.sb + grp * g.Cm.sg + n;
+        if constexpr (V == 4) {
+          Elem<float>::load4(st, h[j][k]);
+          B4[j].load(pb, g.quads, 0);
+          C4[j].load(pc, g.quads, 0);
         } else {
-#pragma unroll
-          for (int v = 0; v < V; ++v) B[k][v] = Elem<T>::load1(pb + n + v), C[k][v] = Elem<T>::load1(pc + n + v);
+          h[j][k][0] = *st;
+          B1[j][k] = Elem<T>::load1(pb);
+          C1[j][k] = Elem<T>::load1(pc);
         }
-      } else {
-        h[k][0] = st[n], A[k][0] = pa[n], B[k][0] = Elem<T>::load1(pb + n), C[k][0] = Elem<T>::load1(pc + n);
       }
-    } else {
-#pragma unroll
-      for (int v = 0; v < V; ++v) h[k][v] = A[k][v] = B[k][v] = C[k][v] = 0.0f;
     }
   }
-  const float u = Elem<T>::load1(static_cast<const T*>(g.u.data) + b * g.u.sb + c);
-  float s = Elem<T>::load1(static_cast<const T*>(g.delta.data) + b * g.delta.sb + c);
-  float z = 0.0f;
-  if (g.z.data) z = Elem<T>::load1(static_cast<const T*>(g.z.data) + b * g.z.sb + c);
-  if (g.bias) s += g.bias[c];
-  const float skip = g.D_skip ? g.D_skip[c] : 0.0f;
-  if (g.softplus) s = softplus<T>(f2(s), nullptr).x;
-  const float x = s * u, s2 = s * kLog2E;
-  float y = 0.0f;
+  // the thread's own sequences: l, l + L, ..
+  float s[U], u[U], z[U];
+  const float bias = live && g.bias ? g.bias[c] : 0.0f, skip = live && g.D_skip ? g.D_skip[c] : 0.0f;
 #pragma unroll
-  for (int k = 0; k < kPass; ++k) {
-    const int n = (k * a.lanes + lane) * V;
-    if (live && n < N) {
+  for (int i = 0; i < U; ++i) {
+    const int b = b0 + l + i * L;
+    s[i] = u[i] = z[i] = 0.0f;
+    if (live && l < kSeqs && b < g.B) {
+      u[i] = Elem<T>::load1(static_cast<const T*>(g.u.data) + b * g.u.sb + c);
+      s[i] = Elem<T>::load1(static_cast<const T*>(g.delta.data) + b * g.delta.sb + c);
+      if (g.z.data) z[i] = Elem<T>::load1(static_cast<const T*>(g.z.data) + b * g.z.sb + c);
+    }
+  }
+#pragma unroll
+  for (int i = 0; i < U; ++i) {
+    s[i] += bias;
+    if (g.softplus) s[i] = softplus<T>(f2(s[i]), nullptr).x;
+  }
+  float y[kSeqs];
+#pragma unroll
+  for (int j = 0; j < kSeqs; ++j) {
+    float sj = s[j / L < U ? j / L : 0], xj = sj * u[j / L < U ? j / L : 0];
+    if (L > 1) {
+      const int from = (threadIdx.x & 31 & ~(L - 1)) | (j & (L - 1));
+      sj = __shfl_sync(0xffffffffu, sj, from);
+      xj = __shfl_sync(0xffffffffu, xj, from);
+    }
+    sj *= kLog2E;
+    y[j] = 0.0f;
+#pragma unroll
+    for (int k = 0; k < kPass; ++k) {
+      float B[V], C[V];
+      if constexpr (V == 4) {
+        B4[j].put(B);
+        C4[j].put(C);
+      } else {
+        B[0] = B1[j][k], C[0] = C1[j][k];
+      }
 #pragma unroll
       for (int v = 0; v < V; ++v) {
-        h[k][v] = fmaf(ex2(s2 * A[k][v]), h[k][v], x * B[k][v]);
-        y = fmaf(C[k][v], h[k][v], y);
+        h[j][k][v] = fmaf(ex2(sj * A[k][v]), h[j][k][v], xj * B[v]);
+        y[j] = fmaf(C[v], h[j][k][v], y[j]);
       }
-      if constexpr (V == 4) Elem<float>::store4(st + n, h[k]);
-      else st[n] = h[k][0];
+      const int n = (k * L + l) * V;
+      if (live && n < N && place[j] >= 0) {
+        float* st = a.state + (place[j] * g.D + c) * (int64_t)N + n;
+        if constexpr (V == 4) Elem<float>::store4(st, h[j][k]);
+        else *st = h[j][k][0];
+      }
     }
   }
-  for (int o = 1; o < a.lanes; o <<= 1) y += __shfl_xor_sync(0xffffffffu, y, o);
-  if (live && lane == 0) {
-    y = fmaf(skip, u, y);
-    if (g.z.data) y *= z * sigmoid<T>(z);
-    Elem<T>::store1(py, y);
+  // the sums over a channel's threads: all four while more than four share them, then halves
+#pragma unroll
+  for (int o = L / 2; o > 0; o >>= 1) {
+    if (o >= kSeqs) {
+#pragma unroll
+      for (int j = 0; j < kSeqs; ++j) y[j] += __shfl_xor_sync(0xffffffffu, y[j], o);
+    } else {
+      const bool up = l & o;
+#pragma unroll
+      for (int j = 0; j < kSeqs; ++j) {
+        if (j % (2 * o) < o && (L < kSeqs || j < 2 * o)) {
+          const float give = up ? y[j] : y[j + o], keep = up ? y[j + o] : y[j];
+          y[j] = keep + __shfl_xor_sync(0xffffffffu, give, o);
+        }
+      }
+    }
+  }
+#pragma unroll
+  for (int i = 0; i < U; ++i) {
+    const int b = b0 + l + i * L;
+    if (live && l < kSeqs && b < g.B) {
+      float out = fmaf(skip, u[i], y[L < kSeqs ? i * L : 0]);
+      if (g.z.data) out *= z[i] * sigmoid<T>(z[i]);
+      bool used = false;
+#pragma unroll
+      for (int j = 0; j < kSeqs; ++j)
+        if (j == l + i * L) used = place[j] >= 0;
+      Elem<T>::store1(static_cast<T*>(g.y.data) + b * g.y.sb + c, used ? out : 0.0f);
+    }
   }
 }
 
+template <typename T, int V, int L>
+cudaError_t launch_lanes(const StepArgs& a, int lanes, cudaStream_t st) {
+  if constexpr (V * L < (V == 4 ? 64 : 32))
+    if (lanes > L) return launch_lanes<T, V, 2 * L>(a, lanes, st);
+  const dim3 grid((unsigned)ceil_div((int64_t)a.g.D * L, kStepThreads), (unsigned)ceil_div(a.g.B, kSeqs));
+  return launch_pdl(scan_step<T, V, L>, grid, dim3(kStepThreads), 0, st, a);
+}
+
 template <typename T>
-cudaError_t launch_step(StepArgs a, cudaStream_t st) {
-  const int vecs = a.g.N % 4 == 0 ? a.g.N / 4 : a.g.N;
-  a.lanes = 1;
-  while (a.lanes < vecs && a.lanes < 32) a.lanes *= 2;
-  const dim3 grid((unsigned)ceil_div((int64_t)a.g.D * a.lanes, kStepThreads), (unsigned)a.g.B);
-  if (a.g.N % 4 == 0) return launch_pdl(scan_step<T, 4>, grid, dim3(kStepThreads), 0, st, a);
-  return launch_pdl(scan_step<T, 1>, grid, dim3(kStepThreads), 0, st, a);
+cudaError_t launch_step(const StepArgs& a, cudaStream_t st) {
+  if (a.g.N % 4 == 0) return launch_lanes<T, 4, 1>(a, a.g.N / 4, st);
+  return launch_lanes<T, 1, 1>(a, a.g.N < 32 ? a.g.N : 32, st);
 }
 
 }  // namespace sscan
@@ -119,7 +185,7 @@ extern "C" snn_status_t snn_selective_scan_step(const snn_sscan_desc* desc, cons
   if (s != SNN_OK) return s;
   if (desc->T != 1 || !A || !state || num_slots < 0 || num_slots > kMost) return SNN_ERR_INVALID_ARG;
   if (!slots && num_slots < desc->B) return SNN_ERR_INVALID_ARG;
-  if (desc->B > 65535) return SNN_ERR_UNSUPPORTED;
+  if (desc->B > 65535) return SNN_ERR_UNSUPPORTED;  // a grid's second extent
   const void* ptrs[5] = {A, D, delta_bias, state, slots};
   for (const void* p : ptrs)
     if (!aligned16(p)) return SNN_ERR_ALIGNMENT;
@@ -138,7 +204,7 @@ extern "C" snn_status_t snn_selective_scan_step(const snn_sscan_desc* desc, cons
   a.g.slots = slots;
   a.g.num_slots = num_slots;
   a.state = state;
-  a.bc_vec = quads(a.g, {&a.g.Bm, &a.g.Cm});
+  a.g.quads = quads(a.g, {&a.g.Bm, &a.g.Cm});
   cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
   const cudaError_t e = desc->dtype == SNN_F32    ? launch_step<float>(a, st)
                         : desc->dtype == SNN_BF16 ? launch_step<__nv_bfloat16>(a, st)
