@@ -201,7 +201,7 @@ __device__ __forceinline__ void load_params(const Args& g, int c, Lane<V> (&w)[W
 }
 
 template <typename T, int V, int W>
-__global__ void __launch_bounds__(kThreads) conv_fwd(const Args g) {
+__global__ void __launch_bounds__(kThreads, sizeof(T) == 4 ? 2 : 3) conv_fwd(const Args g) {
   constexpr int N = kLanes<V>;
   using L = Lane<V>;
   grid_dep_wait();
@@ -227,23 +227,29 @@ __global__ void __launch_bounds__(kThreads) conv_fwd(const Args g) {
   const T* px = at.row(g.x, t0);
   T* py = at.row_out(g.y, t0);
   Vec<T, V> raw[kAhead];
+  const int stop = t1 < len ? t1 : len;
   auto fetch = [&](int t) {
+    if (t + kAhead <= stop) {
 #pragma unroll
-    for (int i = 0; i < kAhead; ++i) {
-      raw[i].clear();
-      if (t + i < t1 && t + i < len) raw[i].load(px + i * g.x.st);
+      for (int i = 0; i < kAhead; ++i) raw[i].load(px + i * g.x.st);
+    } else {
+#pragma unroll
+      for (int i = 0; i < kAhead; ++i) {
+        raw[i].clear();
+        if (t + i < stop) raw[i].load(px + i * g.x.st);
+      }
     }
     px += kAhead * g.x.st;
   };
-  fetch(t0);
-  for (int t = t0; t < t1; t += kAhead) {
+  // whole: all the tokens exist
+  auto tokens = [&](int t, auto whole) {
     Vec<T, V> now[kAhead];
 #pragma unroll
     for (int i = 0; i < kAhead; ++i) now[i] = raw[i];
     fetch(t + kAhead);
 #pragma unroll
     for (int i = 0; i < kAhead; ++i) {
-      if (t + i < t1) {
+      if (decltype(whole)::value || t + i < t1) {
         L y[N];
 #pragma unroll
         for (int j = 0; j < W - 1; ++j)
@@ -256,13 +262,17 @@ __global__ void __launch_bounds__(kThreads) conv_fwd(const Args g) {
 #pragma unroll
           for (int j = 0; j < W; ++j) p = fma2(w[j][v], win[j][v], p);
           if (g.silu) p = mul2(p, sigmoid<T>(p));
-          y[v] = t + i < len ? p : all<L>(0.0f);
+          y[v] = decltype(whole)::value || t + i < len ? p : all<L>(0.0f);
         }
         Vec<T, V>::put(py + i * g.y.st, y);
       }
     }
     py += kAhead * g.y.st;
-  }
+  };
+  fetch(t0);
+  int t = t0;
+  for (; t + kAhead <= stop; t += kAhead) tokens(t, std::true_type());
+  for (; t < t1; t += kAhead) tokens(t, std::false_type());
   // the last W - 1 inputs; in ascending order, as state_out may be state_in
   if (r == 0 && g.state_out && at.has_place()) {
 #pragma unroll
@@ -275,7 +285,7 @@ __global__ void __launch_bounds__(kThreads) conv_fwd(const Args g) {
 }
 
 template <typename T, int V, int W>
-__global__ void __launch_bounds__(kThreads, 2) conv_bwd(const Args g) {
+__global__ void __launch_bounds__(kThreads, sizeof(T) == 4 ? 1 : 2) conv_bwd(const Args g) {
   extern __shared__ float conv_smem[];  // [runs of a block][lanes V][W + 1]
   constexpr int N = kLanes<V>;
   using L = Lane<V>;
@@ -314,21 +324,31 @@ __global__ void __launch_bounds__(kThreads, 2) conv_bwd(const Args g) {
     const T *px = at.row(g.x, t0), *pg = at.row(g.gy, t0);
     T* po = at.row_out(g.gx, t0) - (W - 1) * g.gx.st;
     Vec<T, V> raw[kAhead], raw_gy[kAhead];
+    const int stop = end < len ? end : len;
     auto fetch = [&](int t) {
+      if (t + kAhead <= stop) {
 #pragma unroll
-      for (int i = 0; i < kAhead; ++i) {
-        raw[i].clear();
-        raw_gy[i].clear();
-        if (t + i < end && t + i < len) {
+        for (int i = 0; i < kAhead; ++i) {
           raw[i].load(px + i * g.x.st);
           raw_gy[i].load(pg + i * g.gy.st);
+        }
+      } else {
+#pragma unroll
+        for (int i = 0; i < kAhead; ++i) {
+          raw[i].clear();
+          raw_gy[i].clear();
+          if (t + i < stop) {
+            raw[i].load(px + i * g.x.st);
+            raw_gy[i].load(pg + i * g.gy.st);
+          }
         }
       }
       px += kAhead * g.x.st;
       pg += kAhead * g.gy.st;
     };
-    fetch(t0);
-    for (int t = t0; t < end; t += kAhead) {
+    // whole: all the tokens exist and are the run's own, as are those W - 1 before them
+    auto tokens = [&](int t, auto whole_) {
+      constexpr bool whole = decltype(whole_)::value;
       Vec<T, V> now_x[kAhead], now_gy[kAhead];
 #pragma unroll
       for (int i = 0; i < kAhead; ++i) now_x[i] = raw[i], now_gy[i] = raw_gy[i];
@@ -336,7 +356,7 @@ __global__ void __launch_bounds__(kThreads, 2) conv_bwd(const Args g) {
 #pragma unroll
       for (int i = 0; i < kAhead; ++i) {
         const int now = t + i;
-        if (now < end) {
+        if (whole || now < end) {
           L gx[N], gy[N];
 #pragma unroll
           for (int j = 0; j < W - 1; ++j)
@@ -354,9 +374,9 @@ __global__ void __launch_bounds__(kThreads, 2) conv_bwd(const Args g) {
               const L s = sigmoid<T>(p);
               dt = mul2(dt, fma2(mul2(p, s), fma2(s, all<L>(-1.0f), all<L>(1.0f)), s));
             }
-            if (now >= len) dt = zero;
+            if (!whole && now >= len) dt = zero;
             d[W - 1][v] = dt;
-            if (now < t1 && now < len) {
+            if (whole || (now < t1 && now < len)) {
               db[v] = add2(db[v], dt);
 #pragma unroll
               for (int j = 0; j < W; ++j) dw[j][v] = fma2(dt, win[j][v], dw[j][v]);
@@ -366,7 +386,9 @@ __global__ void __launch_bounds__(kThreads, 2) conv_bwd(const Args g) {
             for (int j = 1; j < W; ++j) gx[v] = fma2(w[j][v], d[W - 1 - j][v], gx[v]);
           }
           const int to = now - (W - 1);
-          if (to >= t0 || r == 0) {
+          if (whole) {
+            if (g.gx.data) Vec<T, V>::put(po + i * g.gx.st, gx);
+          } else if (to >= t0 || r == 0) {
             const int j = to - (len - (W - 1));  // the row of the last inputs that this one is
             if (g.grad_state_out && j >= 0 && j < W - 1) {
               Vec<T, V> s;
@@ -387,7 +409,12 @@ __global__ void __launch_bounds__(kThreads, 2) conv_bwd(const Args g) {
         }
       }
       po += kAhead * g.gx.st;
-    }
+    };
+    fetch(t0);
+    int t = t0;
+    for (; t < end && t < t0 + W - 1; t += kAhead) tokens(t, std::false_type());
+    for (; t + kAhead <= t1 && t + kAhead <= len; t += kAhead) tokens(t, std::true_type());
+    for (; t < end; t += kAhead) tokens(t, std::false_type());
   }
   if (!g.part) return;
   const int width = lanes * V;
