@@ -34,8 +34,8 @@ struct BwdPlan {
 
 // Columns of tensor memory: a tile's states, allocated in powers of two.
 __host__ __device__ constexpr int columns_of(int NS) { return NS == 4 ? 64 : NS == 8 ? 128 : 256; }
-// Blocks of an SM: what tensor memory and 128 registers a thread (255 for 12 and 16 states) allow.
-__host__ __device__ constexpr int blocks_of(int NS) { return NS <= 8 ? 4 : 2; }
+// Blocks of an SM: 168 registers a thread, 255 for 12 and 16 states.
+__host__ __device__ constexpr int blocks_of(int NS) { return NS <= 8 ? 3 : 2; }
 
 BwdPlan bwd_plan(const Args& g) {
   BwdPlan p;
@@ -45,10 +45,36 @@ BwdPlan bwd_plan(const Args& g) {
   return p;
 }
 
-// Shared memory of a warp: s, u, dy, softplus' and grad_y silu' of a tile's pairs; its B and C.
-__host__ __device__ constexpr int bwd_smem(int NS, int P) {
-  return kTile * (32 / P) * 5 * (int)sizeof(float2) + kTile * 2 * P * NS * (int)sizeof(float);
+// Values of a sum over the warp's pairs, padded to a power of two.
+__host__ __device__ constexpr int sums_of(int NS) { return NS == 12 ? 16 : NS; }
+// Orders of a four of states (see order_of): whole numbers below this are xor-ed on it.
+__host__ __device__ constexpr int copies_of(int NS, int P) { return NS == 12 ? 1 : NS * P / 32 > 1 ? 2 : 4; }
+// Where order x lies: each in banks of its own.
+__host__ __device__ constexpr int copy_at(int NS, int P, int x) { return x * kTile * 2 * P * NS + (x & 1) * 16 + (x >> 1) * 36; }
+
+// Shared memory of a warp, in bytes.
+template <typename T, int NS, int P>
+struct Smem {
+  static constexpr int PW = 32 / P, Np = P * NS;
+  static constexpr int su = 0;                                                  // float4 [kTile][PW]: s, u
+  static constexpr int sg = su + kTile * PW * 16;                               // float4 [kTile][PW]: softplus', grad_y silu'
+  static constexpr int dy = sg + kTile * PW * 16;                               // float2 [kTile][PW]
+  static constexpr int bc = dy + kTile * PW * 8;                                // [copies][kTile][B, C][Np]
+  static constexpr int raw = bc + (copy_at(NS, P, copies_of(NS, P)) + 16) * 4;    // Raw [u, delta, grad_y, z][kTile][PW]
+  static constexpr int raw_bc = raw + 4 * kTile * PW * (int)sizeof(Raw<T>);     // T [kTile][B, C][Np]
+  static constexpr int h0 = raw_bc + 2 * kTile * Np * (int)sizeof(T);           // float4 [NS / 2][32]
+  static constexpr int bytes = h0 + NS / 2 * 32 * 16;
+};
+
+// To shared memory without passing registers; there after copies_arrived().
+template <int bytes>
+__device__ __forceinline__ void copy_async(void* to, const void* from) {
+  if constexpr (bytes == 16)
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(smem_u32(to)), "l"(from) : "memory");
+  else
+    asm volatile("cp.async.ca.shared.global [%0], [%1], %2;" ::"r"(smem_u32(to)), "l"(from), "n"(bytes) : "memory");
 }
+__device__ __forceinline__ void copies_arrived() { asm volatile("cp.async.wait_all;" ::: "memory"); }
 
 // Tensor memory as a thread's own: columns of its lane.  What is loaded is there after
 // arrived().
@@ -70,10 +96,11 @@ __device__ __forceinline__ void own_store(uint32_t at, const float2* v) {
 }
 __device__ __forceinline__ void stored() { asm volatile("tcgen05.wait::st.sync.aligned;"); }
 
-// Sums of K values (a power of two) over a warp's pairs, whose threads are P apart: with
-// each exchange a thread keeps half of the values.  Left are the first max(1, K P / 32), those
-// from left_at() on (-1 in threads whose sums another one has too).
-template <int K, int P>
+// Sums of K values (a power of two) over a warp's pairs, whose threads are P apart.  With
+// each exchange a thread keeps half of the values; left are the first max(1, K P / 32).  Ordered: a
+// thread's v[i] is value i ^ order_of(lane), so that what it keeps always comes first and nothing
+// has to be selected.
+template <int K, int P, bool kOrdered>
 __device__ __forceinline__ void sum_over_pairs(float (&v)[K], int lane) {
 #pragma unroll
   for (int o = 16; o >= P; o >>= 1) {
@@ -82,40 +109,66 @@ __device__ __forceinline__ void sum_over_pairs(float (&v)[K], int lane) {
     if (n >= 1) {
 #pragma unroll
       for (int i = 0; i < n; ++i) {
-        const float give = up ? v[i] : v[i + n], keep = up ? v[i + n] : v[i];
-        v[i] = keep + __shfl_xor_sync(0xffffffffu, give, o);
+        if (kOrdered) {
+          v[i] += __shfl_xor_sync(0xffffffffu, v[i + n], o);
+        } else {
+          const float give = up ? v[i] : v[i + n], keep = up ? v[i + n] : v[i];
+          v[i] = keep + __shfl_xor_sync(0xffffffffu, give, o);
+        }
       }
     } else {
       v[0] += __shfl_xor_sync(0xffffffffu, v[0], o);
     }
   }
 }
+// The first value that is left, and whether another thread has the same ones.
 template <int K, int P>
-__device__ __forceinline__ int left_at(int lane) {
+__device__ __forceinline__ int left_at(int lane, bool* twice) {
   int at = 0;
+  *twice = false;
 #pragma unroll
   for (int o = 16; o >= P; o >>= 1) {
     const int n = K * o / 32;
     if (lane & o) {
-      if (n < 1) return -1;
+      if (n < 1) *twice = true;
       at += n;
     }
   }
   return at;
 }
+// v[i] <- v[i ^ order]
+template <int NS>
+__device__ __forceinline__ void reorder(float2 (&v)[NS], int order) {
+#pragma unroll
+  for (int n = 1; n < NS; n <<= 1) {
+    const bool up = order & n;
+#pragma unroll
+    for (int i = 0; i < NS; ++i) {
+      if (!(i & n)) {
+        const float2 a = v[i], b = v[i ^ n];
+        v[i] = up ? b : a;
+        v[i ^ n] = up ? a : b;
+      }
+    }
+  }
+}
 
 template <typename T, int NS, int P>
 __device__ void scan_back(const Args& g, int64_t work, unsigned char* smem, uint32_t t_h) {
-  constexpr int K = NS == 12 ? 16 : NS, kLeft = K * P / 32 > 1 ? K * P / 32 : 1;   // sums over pairs
+  using S = Smem<T, NS, P>;
+  constexpr int K = sums_of(NS), kLeft = K * P / 32 > 1 ? K * P / 32 : 1;   // sums over pairs
+  constexpr bool kOrdered = NS != 12;
+  constexpr int kCopies = copies_of(NS, P);
   constexpr int PW = 32 / P, Np = P * NS, U = kTile / P;
   constexpr int kTokens = 128 / Np, kTurns = (kTile + kTokens - 1) / kTokens;  // whose B and C are loaded at once
   const int lane = threadIdx.x & 31, pl = lane & (P - 1), pc = lane / P;
-  float2* const ps = reinterpret_cast<float2*>(smem);              // [kTile][PW]
-  float2* const pu = ps + kTile * PW;
-  float2* const pdy = pu + kTile * PW;
-  float2* const pslope = pdy + kTile * PW;
-  float2* const pgz = pslope + kTile * PW;
-  float* const bc = reinterpret_cast<float*>(pgz + kTile * PW);    // [kTile][B, C][Np]
+  float4* const psu = reinterpret_cast<float4*>(smem + S::su) + pc;
+  float4* const psg = reinterpret_cast<float4*>(smem + S::sg) + pc;
+  float2* const pdy = reinterpret_cast<float2*>(smem + S::dy) + pc;
+  float* const bc = reinterpret_cast<float*>(smem + S::bc);
+  Raw<T>* const raw = reinterpret_cast<Raw<T>*>(smem + S::raw) + pc;
+  T* const raw_bc = reinterpret_cast<T*>(smem + S::raw_bc);
+  float4* const h0 = reinterpret_cast<float4*>(smem + S::h0) + lane;
 
   const int nb = (g.pairs + PW - 1) / PW;
   const int64_t place = work / g.spans;
@@ -126,10 +179,14 @@ __device__ void scan_back(const Args& g, int64_t work, unsigned char* smem, uint
   const int stop = last < len ? last : len;
   const int tiles = stop > first ? (stop - first + kTile - 1) / kTile : 0;
   const int pair = pb * PW + pc, n0 = pl * NS;
-  const bool live = pair < g.pairs, second = 2 * pair + 1 < g.Dg, pairs_ok = g.pair_ok;
+  const bool live = pair < g.pairs, second = 2 * pair + 1 < g.Dg, pairs_ok = g.pair_ok, quads_ok = g.quads;
   const bool gate = g.z.data != nullptr, soft = g.softplus;
   const int c = grp * g.Dg + 2 * pair;
   const int64_t row_states = (int64_t)g.N2 * g.pairs * 4;
+  // its shares of grad_B and grad_C, and the order of its states
+  bool twice;
+  const int at = left_at<K, P>(lane, &twice), order = kOrdered ? at : 0;
+  const bool puts = !twice && at < NS && n0 + at < g.N;
 
   float2 A2[NS], gam[NS], dA[NS], bias = f2(0.0f), skip = f2(0.0f), sum_D = f2(0.0f), sum_bias = f2(0.0f);
 #pragma unroll
@@ -149,6 +206,10 @@ __device__ void scan_back(const Args& g, int64_t work, unsigned char* smem, uint
       for (int q = 0; q < NS; ++q) gam[q] = fma2(ex2(mul2(s, A2[q])), gam[q], e[q]);
     }
   }
+  if (kOrdered) {
+    reorder<NS>(A2, order);
+    reorder<NS>(gam, order);
+  }
 
   // a thread's own tokens of the last tile, and its fours of states of B and C
   const int t_last = first + (tiles - 1) * kTile;
@@ -156,93 +217,128 @@ __device__ void scan_back(const Args& g, int64_t work, unsigned char* smem, uint
   const T *in_u = own(g.u), *in_d = own(g.delta), *in_g = own(g.gy), *in_z = own(g.z);
   T *out_u = own(g.gu), *out_d = own(g.gdelta), *out_z = own(g.gz);
   const float* ckpt = g.ckpt + (((int64_t)b * ((g.T + kTile - 1) / kTile) + t_last / kTile) * g.G + grp) * row_states +
-                      pair * 4;
-  const T *pB, *pC;
-  int bc_tok, bc_n;
-  {
-    bc_tok = lane * 4 / Np, bc_n = lane * 4 % Np;   // 128 / Np tokens of B, and of C, a turn
-    pB = static_cast<const T*>(g.Bm.data) + b * g.Bm.sb + (int64_t)(t_last + bc_tok) * g.Bm.st + grp * g.Bm.sg + bc_n;
-    pC = static_cast<const T*>(g.Cm.data) + b * g.Cm.sb + (int64_t)(t_last + bc_tok) * g.Cm.st + grp * g.Cm.sg + bc_n;
-  }
-  const int absent = bc_n + 4 - g.N;
-  // its shares of grad_B and grad_C
-  const int at = left_at<K, P>(lane);
+                      ((int64_t)(n0 / 2) * g.pairs + pair) * 4;
+  const int bc_tok = lane * 4 / Np, bc_n = lane * 4 % Np, absent = bc_n + 4 - g.N > 0 ? bc_n + 4 - g.N : 0;
+  const T* pB = static_cast<const T*>(g.Bm.data) + b * g.Bm.sb + (int64_t)(t_last + bc_tok) * g.Bm.st + grp * g.Bm.sg + bc_n;
+  const T* pC = static_cast<const T*>(g.Cm.data) + b * g.Cm.sb + (int64_t)(t_last + bc_tok) * g.Cm.st + grp * g.Cm.sg + bc_n;
   const int64_t part_step = (int64_t)g.G * g.N;
   const int64_t part0 = ((((int64_t)pb * g.B + b) * g.T + t_last) * g.G + grp) * g.N + n0 + at;
-  float *part_B = g.part_B + part0, *part_C = g.part_C + part0;
+  float *part_B = g.part_B + part0 + (kTile - 1) * part_step, *part_C = g.part_C + part0;
   auto put_part = [&](float* p, const float (&v)[K]) {
-    if (at >= 0) {
 #pragma unroll
-      for (int j = 0; j < kLeft; ++j)
-        if (n0 + at + j < g.N && at + j < NS) p[j] = v[j];
-    }
+    for (int j = 0; j < kLeft; ++j)
+      if (j == 0 || n0 + at + j < g.N) p[j] = v[j];
   };
 
-  for (int tile = tiles - 1; tile >= 0; --tile) {
-    const int t0 = first + tile * kTile, tokens = stop - t0 < kTile ? stop - t0 : kTile;
-    float2 h[NS];
+  // a tile's inputs on their way to shared memory
+  auto fetch = [&](int tokens) {
 #pragma unroll
-    for (int q = 0; q < NS; ++q) h[q] = f2(0.0f);
-    if (live) load_twos<NS>(ckpt, g, n0, h);
-    ckpt -= g.G * row_states;
-    {  // the tile's inputs: a thread's own tokens, and its fours of B and C
-      Raw<T> ru[U], rd[U], rg[U], rz[U];
-      Four<T> rb[kTurns], rc[kTurns];
-#pragma unroll
-      for (int i = 0; i < kTurns; ++i) {
-        rb[i].clear();
-        rc[i].clear();
-        const int tok = bc_tok + i * kTokens;
-        if (tok < tokens && tok < kTile && bc_tok < kTokens && absent < 4) {
-          rb[i].load(pB + i * kTokens * g.Bm.st, g.quads, absent > 0 ? absent : 0);
-          rc[i].load(pC + i * kTokens * g.Cm.st, g.quads, absent > 0 ? absent : 0);
+    for (int j = 0; j < U; ++j) {
+      const int tok = pl + j * P;
+      Raw<T>* const to = raw + tok * PW;
+      auto one = [&](int k, const T* p) {
+        if (pairs_ok && live && tok < tokens) {
+          copy_async<sizeof(Raw<T>)>(to + k * kTile * PW, p);
+        } else {
+          Raw<T> r;
+          r.clear();
+          if (live && tok < tokens) r.load(p, false, second);
+          to[k * kTile * PW] = r;
         }
-      }
+      };
+      one(0, in_u + j * P * g.u.st);
+      one(1, in_d + j * P * g.delta.st);
+      one(2, in_g + j * P * g.gy.st);
+      if (gate) one(3, in_z + j * P * g.z.st);
+    }
+    in_u -= kTile * g.u.st;
+    in_d -= kTile * g.delta.st;
+    in_g -= kTile * g.gy.st;
+    in_z -= kTile * g.z.st;
 #pragma unroll
-      for (int j = 0; j < U; ++j) {
-        ru[j].clear();
-        rd[j].clear();
-        rg[j].clear();
-        rz[j].clear();
-        if (live && pl + j * P < tokens) {
-          ru[j].load(in_u + j * P * g.u.st, pairs_ok, second);
-          rd[j].load(in_d + j * P * g.delta.st, pairs_ok, second);
-          rg[j].load(in_g + j * P * g.gy.st, pairs_ok, second);
-          if (gate) rz[j].load(in_z + j * P * g.z.st, pairs_ok, second);
-        }
-      }
-      in_u -= kTile * g.u.st;
-      in_d -= kTile * g.delta.st;
-      in_g -= kTile * g.gy.st;
-      in_z -= kTile * g.z.st;
-      pB -= kTile * g.Bm.st;
-      pC -= kTile * g.Cm.st;
-#pragma unroll
-      for (int i = 0; i < kTurns; ++i) {
-        const int tok = bc_tok + i * kTokens;
-        if (tok < kTile && bc_tok < kTokens) {
-          rb[i].put(bc + tok * 2 * Np + bc_n);
-          rc[i].put(bc + tok * 2 * Np + Np + bc_n);
-        }
-      }
-#pragma unroll
-      for (int j = 0; j < U; ++j) {
-        const int tok = pl + j * P, to = tok * PW + pc;
-        float2 s = f2(0.0f), dy = rg[j].get(), slope = f2(0.0f);
-        if (live && tok < tokens) s = step_of<T>(add2(rd[j].get(), bias), soft, &slope);
-        if (gate) {
-          const float2 z = rz[j].get(), sig = sigmoid<T>(z), zs = mul2(z, sig);
-          pgz[to] = mul2(dy, fma2(zs, fma2(sig, f2(-1.0f), f2(1.0f)), sig));
-          dy = mul2(dy, zs);
-        }
-        if (!second) s.y = dy.y = 0.0f;
-        ps[to] = s;
-        pu[to] = ru[j].get();
-        pdy[to] = dy;
-        pslope[to] = slope;
+    for (int i = 0; i < kTurns; ++i) {
+      const int tok = bc_tok + i * kTokens;
+      if (tok < kTile && bc_tok < kTokens) {
+        auto one = [&](int k, const T* p) {
+          T* const to = raw_bc + (tok * 2 + k) * Np + bc_n;
+          if (quads_ok && tok < tokens && absent == 0) {
+            copy_async<4 * sizeof(T)>(to, p);
+          } else {
+            Four<T> r;
+            r.clear();
+            if (tok < tokens && absent < 4) r.load(p, false, absent);
+            *reinterpret_cast<Four<T>*>(to) = r;
+          }
+        };
+        one(0, pB + i * kTokens * g.Bm.st);
+        one(1, pC + i * kTokens * g.Cm.st);
       }
     }
+    pB -= kTile * g.Bm.st;
+    pC -= kTile * g.Cm.st;
+#pragma unroll
+    for (int k = 0; k < NS / 2; ++k) {
+      if (live && n0 / 2 + k < g.N2) copy_async<16>(h0 + k * 32, ckpt + (int64_t)k * g.pairs * 4);
+      else h0[k * 32] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+    }
+    ckpt -= g.G * row_states;
+  };
+  auto tokens_of = [&](int tile) {
+    const int n = stop - (first + tile * kTile);
+    return n < kTile ? n : kTile;
+  };
+  if (tiles) fetch(tokens_of(tiles - 1));
+  const float* const bc_own = bc + copy_at(NS, P, kCopies == 1 ? 0 : kCopies == 2 ? (order >> 1) & 1 : order & 3) + n0;
+  const int first_four = order >> 2;
+
+  for (int tile = tiles - 1; tile >= 0; --tile) {
+    const int tokens = tokens_of(tile);
+    copies_arrived();
     __syncwarp();
+    float2 h[NS];
+#pragma unroll
+    for (int k = 0; k < NS / 2; ++k) {
+      const float4 v = h0[(kOrdered ? k ^ (order >> 1) : k) * 32];
+      const bool swap = kOrdered && (order & 1);
+      h[2 * k] = swap ? make_float2(v.z, v.w) : make_float2(v.x, v.y);
+      h[2 * k + 1] = swap ? make_float2(v.x, v.y) : make_float2(v.z, v.w);
+    }
+#pragma unroll
+    for (int i = 0; i < kTurns; ++i) {
+      const int tok = bc_tok + i * kTokens;
+      if (tok < kTile && bc_tok < kTokens) {
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+          float v[4];
+          reinterpret_cast<const Four<T>*>(raw_bc + (tok * 2 + k) * Np + bc_n)->put(v);
+          float* const to = bc + (tok * 2 + k) * Np + bc_n;
+#pragma unroll
+          for (int x = 0; x < kCopies; ++x) {
+            const int y = kCopies == 2 ? 2 * x : x;
+            *reinterpret_cast<float4*>(to + copy_at(NS, P, x)) = make_float4(v[y], v[1 ^ y], v[2 ^ y], v[3 ^ y]);
+          }
+        }
+      }
+    }
+#pragma unroll
+    for (int j = 0; j < U; ++j) {
+      const int tok = pl + j * P;
+      const Raw<T>* const from = raw + tok * PW;
+      const float2 u = from[0].get();
+      float2 s = f2(0.0f), dy = from[2 * kTile * PW].get(), slope = f2(0.0f), gz = f2(0.0f);
+      if (live && tok < tokens) s = step_of<T>(add2(from[kTile * PW].get(), bias), soft, &slope);
+      if (gate) {
+        const float2 z = from[3 * kTile * PW].get(), sig = sigmoid<T>(z), zs = mul2(z, sig);
+        gz = mul2(dy, fma2(zs, fma2(sig, f2(-1.0f), f2(1.0f)), sig));
+        dy = mul2(dy, zs);
+      }
+      if (!second) s.y = dy.y = 0.0f;
+      psu[tok * PW] = make_float4(s.x, s.y, u.x, u.y);
+      psg[tok * PW] = make_float4(slope.x, slope.y, gz.x, gz.y);
+      pdy[tok * PW] = dy;
+    }
+    __syncwarp();
+    if (tile > 0) fetch(kTile);
     // the states forwards
 #pragma unroll 1
     for (int i0 = 0; i0 < kTile; i0 += P) {
@@ -252,15 +348,17 @@ __device__ void scan_back(const Args& g, int64_t work, unsigned char* smem, uint
         const int i = i0 + k;
 #pragma unroll
         for (int q = 0; q < NS; q += 4) own_store(t_h + i * 2 * NS + 2 * q, h + q);
-        const float2 s = ps[i * PW + pc], dy = pdy[i * PW + pc], x = mul2(s, pu[i * PW + pc]);
-        const float* const rb = bc + i * 2 * Np + n0;
+        const float4 su = psu[i * PW];
+        const float2 s = make_float2(su.x, su.y), x = mul2(s, make_float2(su.z, su.w)), dy = pdy[i * PW];
+        const float* const rb = bc_own + i * 2 * Np;
         float2 sum[2] = {f2(0.0f), f2(0.0f)};
         float dC[K];
 #pragma unroll
         for (int q = 0; q < NS; q += 4) {
           float v[4], w[4];
-          Elem<float>::load4(rb + q, v);
-          Elem<float>::load4(rb + Np + q, w);
+          const int four = kOrdered ? 4 * ((q / 4) ^ first_four) : q;
+          Elem<float>::load4(rb + four, v);
+          Elem<float>::load4(rb + Np + four, w);
 #pragma unroll
           for (int e = 0; e < 4; ++e) {
             float2& hq = h[q + e];
@@ -273,14 +371,18 @@ __device__ void scan_back(const Args& g, int64_t work, unsigned char* smem, uint
         y[k] = add2(sum[0], sum[1]);
 #pragma unroll
         for (int q = NS; q < K; ++q) dC[q] = 0.0f;
-        sum_over_pairs<K, P>(dC, lane);
-        if (i < tokens) put_part(part_C + i * part_step, dC);
+        sum_over_pairs<K, P, kOrdered>(dC, lane);
+        if (puts && i < tokens) put_part(part_C, dC);
+        part_C += part_step;
       }
       if (gate) {
         share_out<P, P>(y, pl);
         const int i = i0 + pl;
-        if (live && i < tokens)
-          put_pair(out_z + i0 * g.gz.st, mul2(pgz[i * PW + pc], fma2(skip, pu[i * PW + pc], y[0])), pairs_ok, second);
+        if (live && i < tokens) {
+          const float4 su = psu[i * PW], sg = psg[i * PW];
+          put_pair(out_z + i0 * g.gz.st,
+                   mul2(make_float2(sg.z, sg.w), fma2(skip, make_float2(su.z, su.w), y[0])), pairs_ok, second);
+        }
       }
     }
     stored();
@@ -294,15 +396,17 @@ __device__ void scan_back(const Args& g, int64_t work, unsigned char* smem, uint
         float2 hv[NS];
 #pragma unroll
         for (int q = 0; q < NS; q += 4) own_load(t_h + i * 2 * NS + 2 * q, hv + q);
-        const float2 s = ps[i * PW + pc], dy = pdy[i * PW + pc], x = mul2(s, pu[i * PW + pc]);
-        const float* const rb = bc + i * 2 * Np + n0;
+        const float4 su = psu[i * PW];
+        const float2 s = make_float2(su.x, su.y), x = mul2(s, make_float2(su.z, su.w)), dy = pdy[i * PW];
+        const float* const rb = bc_own + i * 2 * Np;
         float2 sw[2] = {f2(0.0f), f2(0.0f)}, sr[2] = {f2(0.0f), f2(0.0f)};
         float dB[K];
 #pragma unroll
         for (int q = 0; q < NS; q += 4) {
           float vb[4], vc[4];
-          Elem<float>::load4(rb + q, vb);
-          Elem<float>::load4(rb + Np + q, vc);
+          const int four = kOrdered ? 4 * ((q / 4) ^ first_four) : q;
+          Elem<float>::load4(rb + four, vb);
+          Elem<float>::load4(rb + Np + four, vc);
 #pragma unroll
           for (int e = 0; e < 4; ++e) {
             float2& gq = gam[q + e];
@@ -324,17 +428,19 @@ __device__ void scan_back(const Args& g, int64_t work, unsigned char* smem, uint
         r[k] = add2(sr[0], sr[1]);
 #pragma unroll
         for (int q = NS; q < K; ++q) dB[q] = 0.0f;
-        sum_over_pairs<K, P>(dB, lane);
-        if (i < tokens) put_part(part_B + i * part_step, dB);
+        sum_over_pairs<K, P, kOrdered>(dB, lane);
+        if (puts && i < tokens) put_part(part_B, dB);
+        part_B -= part_step;
       }
       share_out<P, P>(w, pl);
       share_out<P, P>(r, pl);
       const int i = i0 + pl;
       if (live && i < tokens) {
-        const float2 s = ps[i * PW + pc], dy = pdy[i * PW + pc], u = pu[i * PW + pc];
+        const float4 su = psu[i * PW], sg = psg[i * PW];
+        const float2 s = make_float2(su.x, su.y), u = make_float2(su.z, su.w), dy = pdy[i * PW];
         const float2 du = fma2(s, w[0], mul2(skip, dy));
         // r holds A log2(e)
-        const float2 dd = mul2(fma2(u, w[0], mul2(r[0], f2(0.69314718055994530942f))), pslope[i * PW + pc]);
+        const float2 dd = mul2(fma2(u, w[0], mul2(r[0], f2(0.69314718055994530942f))), make_float2(sg.x, sg.y));
         put_pair(out_u + i0 * g.gu.st, du, pairs_ok, second);
         put_pair(out_d + i0 * g.gdelta.st, dd, pairs_ok, second);
         sum_D = fma2(dy, u, sum_D);
@@ -344,8 +450,7 @@ __device__ void scan_back(const Args& g, int64_t work, unsigned char* smem, uint
     out_u -= kTile * g.gu.st;
     out_d -= kTile * g.gdelta.st;
     out_z -= kTile * g.gz.st;
-    part_B -= kTile * part_step;
-    part_C -= kTile * part_step;
+    part_C -= 2 * kTile * part_step;
     __syncwarp();
   }
 
@@ -358,6 +463,10 @@ __device__ void scan_back(const Args& g, int64_t work, unsigned char* smem, uint
     put_pair(base(g.gu, now), f2(0.0f), pairs_ok, second);
     put_pair(base(g.gdelta, now), f2(0.0f), pairs_ok, second);
     if (gate) put_pair(base(g.gz, now), f2(0.0f), pairs_ok, second);
+  }
+  if (kOrdered) {
+    reorder<NS>(dA, order);
+    reorder<NS>(gam, order);
   }
   const int64_t to = (int64_t)span * g.B + b;
   store_states<NS>(g.part_A + (to * g.D + c) * g.N, g.N, n0, second, dA);
@@ -386,7 +495,7 @@ __global__ void __launch_bounds__(32 * kWarps, blocks_of(NS)) scan_bwd(const Arg
   grid_dep_wait();
   const int64_t work = (int64_t)blockIdx.x * kWarps + warp;
   if (work < works)
-    scan_back<T, NS, P>(g, work, scan_smem + warp * bwd_smem(NS, P), tmem + ((uint32_t)(warp * 32) << 16));
+    scan_back<T, NS, P>(g, work, scan_smem + warp * Smem<T, NS, P>::bytes, tmem + ((uint32_t)(warp * 32) << 16));
   tc_fence_before();
   __syncthreads();
   if (warp == 0) tmem_dealloc(tmem, columns_of(NS));
@@ -450,7 +559,7 @@ BwdSpace bwd_space(const Args& g, const BwdPlan& p) {
 
 template <typename T, int NS, int P>
 cudaError_t launch_main(const Args& g, int64_t works, cudaStream_t st) {
-  const size_t smem = (size_t)kWarps * bwd_smem(NS, P);
+  const size_t smem = (size_t)kWarps * Smem<T, NS, P>::bytes;
   // with the kernel's static shared memory, past the limit that needs no asking
   const size_t ask = smem + 1024 > 48 * 1024 && smem <= 48 * 1024 ? 48 * 1024 + 16 : smem;
   const cudaError_t e = ensure_smem((const void*)scan_bwd<T, NS, P>, ask);
