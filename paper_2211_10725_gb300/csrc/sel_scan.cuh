@@ -52,6 +52,7 @@ struct Args {
   int pairs;               // of a group
   int N2;                  // twos of states
   int spans, span;         // cuts of the axis, tokens of each
+  int fine, span_fine;     // parts of a span of which the ends are found, tokens of each
   Seq u, delta, z, y, gy, gu, gdelta, gz;
   Mat Bm, Cm;
   const float *A, *D_skip, *bias;
@@ -60,8 +61,8 @@ struct Args {
   float* state_out;
   int64_t num_slots;
   float* ckpt;             // [B][ceil(T / 8)][G][N2][pairs][4]: two states of two channels
-  float* ends;             // [spans][B][G][N2][pairs][4]: what a span adds to the state
-  float2* sums;            // [spans][B][G pairs]: of s over a span
+  float* ends;             // [spans fine][B][G][N2][pairs][4]: what a part adds to the state
+  float2* sums;            // [spans fine][B][G pairs]: of s over a part
   // backward
   const float* grad_state_out;
   float* grad_state_in;
@@ -378,7 +379,7 @@ inline Args base_args(const snn_sscan_desc* d) {
 
 // How the axis is cut, from the shape alone.
 struct Plan {
-  int spans, span;
+  int spans, span, fine, span_fine;
 };
 // What the kernels of a call need beside its tensors.
 inline int64_t state_floats(const Args& g) { return (int64_t)g.B * g.G * g.N2 * g.pairs * 4; }

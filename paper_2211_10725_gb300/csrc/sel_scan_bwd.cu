@@ -40,8 +40,9 @@ __host__ __device__ constexpr int blocks_of(int NS) { return NS <= 8 ? 3 : 2; }
 BwdPlan bwd_plan(const Args& g) {
   BwdPlan p;
   p.lay = lay_of(g.N);
+  if (p.lay.NS == 12 && p.lay.P == 2) p.lay = Lay{8, 4};
   p.blocks = (int)ceil_div(g.pairs, 32 / p.lay.P);
-  p.cut = cut(g.T, warps_of(g, p.lay), kSms * kWarps * blocks_of(p.lay.NS), 2);
+  p.cut = cut(g.T, warps_of(g, p.lay), kSms * kWarps * blocks_of(p.lay.NS));
   return p;
 }
 
@@ -198,7 +199,7 @@ __device__ void scan_back(const Args& g, int64_t work, unsigned char* smem, uint
     if (g.bias) bias = make_float2(g.bias[c], second ? g.bias[c + 1] : 0.0f);
     if (g.D_skip) skip = make_float2(g.D_skip[c], second ? g.D_skip[c + 1] : 0.0f);
     if (g.grad_state_out) load_states<NS>(g.grad_state_out + ((int64_t)b * g.D + c) * g.N, g.N, n0, second, gam);
-    for (int i = g.spans - 1; i > span; --i) {
+    for (int i = g.spans * g.fine - 1; i >= (span + 1) * g.fine; --i) {
       float2 e[NS];
       load_twos<NS>(g.ends + ((int64_t)i * g.B * g.G + rest) * row_states + pair * 4, g, n0, e);
       const float2 s = g.sums[((int64_t)i * g.B * g.G + rest) * g.pairs + pair];
@@ -501,27 +502,36 @@ __global__ void __launch_bounds__(32 * kWarps, blocks_of(NS)) scan_bwd(const Arg
   if (warp == 0) tmem_dealloc(tmem, columns_of(NS));
 }
 
-// grad_B and grad_C: the warps' shares in order; zero past a sequence's end.
+// grad_B and grad_C: the warps' shares, in eight slices (every eighth, in order), then the
+// slices in order; zero past a sequence's end.
 template <typename T>
 __global__ void __launch_bounds__(256) scan_sum_bc(const Args g, Mat gB, Mat gC, int blocks) {
+  __shared__ float sum[2][8][32];
   grid_dep_wait();
-  const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x, all = (int64_t)g.B * g.T * g.G * g.N;
-  if (i >= all) return;
-  const int n = (int)(i % g.N);
-  int64_t rest = i / g.N;
-  const int grp = (int)(rest % g.G);
-  rest /= g.G;
-  const int tok = (int)(rest % g.T), b = (int)(rest / g.T);
+  const int lane = threadIdx.x & 31, slice = threadIdx.x >> 5;
+  const int64_t i = (int64_t)blockIdx.x * 32 + lane, all = (int64_t)g.B * g.T * g.G * g.N;
+  const int64_t row = i / g.N;
+  const int n = (int)(i - row * g.N);
+  const int64_t token = row / g.G;
+  const int grp = (int)(row - token * g.G), b = (int)(token / g.T), tok = (int)(token - (int64_t)b * g.T);
+  const bool in = i < all;
   float vb = 0.0f, vc = 0.0f;
-  if (tok < seq_len(g, b)) {
-#pragma unroll 16
-    for (int k = 0; k < blocks; ++k) {
+  if (in && tok < seq_len(g, b)) {
+#pragma unroll 8
+    for (int k = slice; k < blocks; k += 8) {
       vb += g.part_B[k * all + i];
       vc += g.part_C[k * all + i];
     }
   }
-  Elem<T>::store1(static_cast<T*>(gB.data) + b * gB.sb + tok * gB.st + grp * gB.sg + n, vb);
-  Elem<T>::store1(static_cast<T*>(gC.data) + b * gC.sb + tok * gC.st + grp * gC.sg + n, vc);
+  sum[0][slice][lane] = vb;
+  sum[1][slice][lane] = vc;
+  __syncthreads();
+  if (slice > 1 || !in) return;
+  float v = sum[slice][0][lane];
+#pragma unroll
+  for (int k = 1; k < 8; ++k) v += sum[slice][k][lane];
+  const Mat& m = slice ? gC : gB;
+  Elem<T>::store1(static_cast<T*>(m.data) + b * m.sb + tok * m.st + grp * m.sg + n, v);
 }
 
 // grad_A, grad_D and grad_delta_bias: the spans' and sequences' shares in order.
@@ -548,8 +558,8 @@ struct BwdSpace {
 };
 BwdSpace bwd_space(const Args& g, const BwdPlan& p) {
   BwdSpace s;
-  s.ends = p.cut.spans > 1 ? ends_bytes(g, p.cut.spans) : 0;
-  s.sums = p.cut.spans > 1 ? sums_bytes(g, p.cut.spans) : 0;
+  s.ends = p.cut.spans > 1 ? ends_bytes(g, p.cut.spans * p.cut.fine) : 0;
+  s.sums = p.cut.spans > 1 ? sums_bytes(g, p.cut.spans * p.cut.fine) : 0;
   s.bc = round256((size_t)p.blocks * g.B * g.T * g.G * g.N * sizeof(float));
   s.a = round256((size_t)p.cut.spans * g.B * g.D * g.N * sizeof(float));
   s.d = round256((size_t)p.cut.spans * g.B * g.D * sizeof(float));
@@ -570,12 +580,12 @@ cudaError_t launch_main(const Args& g, int64_t works, cudaStream_t st) {
 template <typename T>
 cudaError_t launch_bwd(const Args& g, const BwdPlan& p, const Mat& gB, const Mat& gC, cudaStream_t st) {
   const int64_t works = warps_of(g, p.lay) * g.spans, all = (int64_t)g.B * g.T * g.G * g.N;
-  if (works > 0x7fffffff || ceil_div(all, 256) > 0x7fffffff) return cudaErrorInvalidValue;
+  if (works > 0x7fffffff || ceil_div(all, 32) > 0x7fffffff) return cudaErrorInvalidValue;
   const cudaError_t e = with_lay(p.lay, [&](auto NS, auto P) {
     return launch_main<T, decltype(NS)::value, decltype(P)::value>(g, works, st);
   });
   if (e != cudaSuccess || all == 0) return e;
-  return launch_pdl(scan_sum_bc<T>, dim3((unsigned)ceil_div(all, 256)), dim3(256), 0, st, g, gB, gC, p.blocks);
+  return launch_pdl(scan_sum_bc<T>, dim3((unsigned)ceil_div(all, 32)), dim3(256), 0, st, g, gB, gC, p.blocks);
 }
 
 }  // namespace sscan
@@ -640,8 +650,7 @@ snn_status_t snn_selective_scan_bwd(const snn_sscan_desc* desc, const snn_btc* u
   if (!ws || ws_bytes < space.total) return SNN_ERR_WORKSPACE;
   g.pair_ok = pair;
   g.quads = quads(g, {&g.Bm, &g.Cm});
-  g.spans = plan.cut.spans;
-  g.span = plan.cut.span;
+  put_cut(g, plan.cut);
   g.A = A;
   g.D_skip = D;
   g.bias = delta_bias;

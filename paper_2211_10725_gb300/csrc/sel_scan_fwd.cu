@@ -25,9 +25,10 @@ __global__ void __launch_bounds__(32) scan_fwd(const Args g) {
   const int lane = threadIdx.x, pl = lane & (P - 1);
   const int nb = (g.pairs + PW - 1) / PW;
   const int pb = blockIdx.x % nb, rest = blockIdx.x / nb, grp = rest % g.G, b = rest / g.G;
-  const int span = blockIdx.y + (MODE == kBack ? 1 : 0);
-  const int len = seq_len(g, b), first = span * g.span;
-  const int last = first + g.span < g.T ? first + g.span : g.T;
+  // a span, or a part of one (backwards: of the second on)
+  const int span = blockIdx.y + (MODE == kBack ? g.fine : 0), length = MODE == kFull ? g.span : g.span_fine;
+  const int len = seq_len(g, b), first = span * length;
+  const int last = first + length < g.T ? first + length : g.T;
   const int stop = last < len ? last : len;  // tokens that exist
   const int pair = pb * PW + lane / P, n0 = pl * NS;
   const bool live = pair < g.pairs, second = 2 * pair + 1 < g.Dg, pairs_ok = g.pair_ok;
@@ -55,13 +56,13 @@ __global__ void __launch_bounds__(32) scan_fwd(const Args g) {
 #pragma unroll
       for (int q = 0; q < NS; ++q) h0[q] = f2(0.0f);
       if (g.state_in && has_place) load_states<NS>(g.state_in + (place * g.D + c) * g.N, g.N, n0, second, h0);
-      store_twos<NS>(ends + (g.spans - 1) * ends_step, g, n0, h0);
+      store_twos<NS>(ends + (g.spans * g.fine - 1) * ends_step, g, n0, h0);
     }
     if (MODE == kFull) {
       if (g.spans > 1) {
-        load_twos<NS>(ends + (g.spans - 1) * ends_step, g, n0, h);
+        load_twos<NS>(ends + (g.spans * g.fine - 1) * ends_step, g, n0, h);
 #pragma unroll 2
-        for (int i = 0; i < span; ++i) {
+        for (int i = 0; i < span * g.fine; ++i) {
           float2 e[NS];
           load_twos<NS>(ends + i * ends_step, g, n0, e);
           const float2 s = g.sums[((int64_t)i * g.B * g.G + rest) * g.pairs + pair];
@@ -239,16 +240,16 @@ cudaError_t launch_mode(const Args& g, Lay lay, int spans, cudaStream_t st) {
 template <typename T>
 cudaError_t launch_fwd(const Args& g, Lay lay, cudaStream_t st) {
   if (g.spans > 1) {
-    const cudaError_t e = launch_mode<T, kEnds>(g, lay, g.spans - 1, st);
+    const cudaError_t e = launch_mode<T, kEnds>(g, lay, (g.spans - 1) * g.fine, st);
     if (e != cudaSuccess) return e;
   }
   return launch_mode<T, kFull>(g, lay, g.spans, st);
 }
 
 cudaError_t launch_back_ends(const Args& g, Lay lay, int dtype, cudaStream_t st) {
-  if (dtype == SNN_F32) return launch_mode<float, kBack>(g, lay, g.spans - 1, st);
-  if (dtype == SNN_BF16) return launch_mode<__nv_bfloat16, kBack>(g, lay, g.spans - 1, st);
-  return launch_mode<__half, kBack>(g, lay, g.spans - 1, st);
+  if (dtype == SNN_F32) return launch_mode<float, kBack>(g, lay, (g.spans - 1) * g.fine, st);
+  if (dtype == SNN_BF16) return launch_mode<__nv_bfloat16, kBack>(g, lay, (g.spans - 1) * g.fine, st);
+  return launch_mode<__half, kBack>(g, lay, (g.spans - 1) * g.fine, st);
 }
 
 }  // namespace sscan
@@ -295,8 +296,7 @@ snn_status_t snn_selective_scan_fwd(const snn_sscan_desc* desc, const snn_btc* u
       return s;
   }
   const FwdPlan plan = fwd_plan(g);
-  g.spans = plan.cut.spans;
-  g.span = plan.cut.span;
+  put_cut(g, plan.cut);
   const size_t need = fwd_bytes(g, plan);
   if (need && (!ws || ws_bytes < need)) return SNN_ERR_WORKSPACE;
   if (desc->B == 0 || (desc->T == 0 && !state_out)) return SNN_OK;
@@ -313,7 +313,7 @@ snn_status_t snn_selective_scan_fwd(const snn_sscan_desc* desc, const snn_btc* u
   g.ckpt = ckpt;
   unsigned char* w = static_cast<unsigned char*>(ws);
   g.ends = reinterpret_cast<float*>(w);
-  g.sums = reinterpret_cast<float2*>(w + ends_bytes(g, plan.cut.spans));
+  g.sums = reinterpret_cast<float2*>(w + ends_bytes(g, plan.cut.spans * plan.cut.fine));
   cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
   const cudaError_t e = desc->dtype == SNN_F32    ? launch_fwd<float>(g, plan.lay, st)
                         : desc->dtype == SNN_BF16 ? launch_fwd<__nv_bfloat16>(g, plan.lay, st)

@@ -11,21 +11,25 @@ namespace sscan {
 constexpr int kSms = 152;
 
 // Cuts for `warps` warps of a whole axis: as many as make whole rounds of the
-// `resident` warps that the GPU holds at once, of at least kMinSpan tokens.
-constexpr int kMinSpan = 64, kMaxSpans = 64;
-inline Plan cut(int64_t T, int64_t warps, int64_t resident, int rounds) {
-  int64_t most = T / kMinSpan, best = 1;
+// `resident` warps that the GPU holds at once, of at least kMinSpan tokens; and the parts
+// that fill it best with warps of the kernel that finds their ends.
+constexpr int kMinSpan = 64, kMaxSpans = 64, kEndsResident = kSms * 21;
+inline double filled(int64_t warps, int64_t resident) {
+  return warps > 0 ? (double)warps / (double)(ceil_div(warps, resident) * resident) : 0.0;
+}
+inline Plan cut(int64_t T, int64_t warps, int64_t resident) {
+  int64_t most = T / kMinSpan, spans = warps > 0 ? resident / warps : 1;
   if (most > kMaxSpans) most = kMaxSpans;
-  double used = 0.0;
-  for (int r = 1; r <= rounds && warps > 0; ++r) {
-    int64_t spans = r * resident / warps;
-    if (spans > most) spans = most;
-    if (spans < 1) continue;
-    const double u = (double)(spans * warps) / (double)(ceil_div(spans * warps, resident) * resident);
-    if (u > used + 0.03) used = u, best = spans;
-  }
+  if (spans > most) spans = most;
+  if (spans < 1) spans = 1;
+  // (every part costs the second kernel a step at its start: 9 spans in 36 parts 15 us)
+  const bool halves = T / (2 * spans) >= kMinSpan && filled((spans - 1) * 2 * warps, kEndsResident) >
+                                                         filled((spans - 1) * warps, kEndsResident) + 0.2;
+  const int fine = halves ? 2 : 1;
   Plan p;
-  p.span = (int)round_up(T > 0 ? ceil_div(T, best) : 1, kTile);
+  p.fine = fine;
+  p.span_fine = (int)round_up(T > 0 ? ceil_div(T, spans * fine) : 1, kTile);
+  p.span = fine * p.span_fine;
   p.spans = T > 0 ? (int)ceil_div(T, p.span) : 1;
   return p;
 }
@@ -67,11 +71,17 @@ inline FwdPlan fwd_plan(const Args& g) {
   const int64_t spans = g.T >= kMinSpan ? g.T / kMinSpan : 1;
   if (warps_of(g, p.lay) * spans < kSms * 8 && g.N > 4 && g.N <= 24)
     p.lay = g.N <= 8 ? Lay{4, 2} : g.N <= 16 ? Lay{4, 4} : Lay{8, 4};
-  p.cut = cut(g.T, warps_of(g, p.lay), kSms * 16, 1);
+  p.cut = cut(g.T, warps_of(g, p.lay), kSms * 16);
   return p;
 }
+inline void put_cut(Args& g, const Plan& p) {
+  g.spans = p.spans;
+  g.span = p.span;
+  g.fine = p.fine;
+  g.span_fine = p.span_fine;
+}
 inline size_t fwd_bytes(const Args& g, const FwdPlan& p) {
-  return p.cut.spans > 1 ? ends_bytes(g, p.cut.spans) + sums_bytes(g, p.cut.spans) : 0;
+  return p.cut.spans > 1 ? ends_bytes(g, p.cut.spans * p.cut.fine) + sums_bytes(g, p.cut.spans * p.cut.fine) : 0;
 }
 
 cudaError_t launch_back_ends(const Args& g, Lay lay, int dtype, cudaStream_t st);
