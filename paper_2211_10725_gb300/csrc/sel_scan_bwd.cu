@@ -40,7 +40,6 @@ __host__ __device__ constexpr int blocks_of(int NS) { return NS <= 8 ? 3 : 2; }
 BwdPlan bwd_plan(const Args& g) {
   BwdPlan p;
   p.lay = lay_of(g.N);
-  if (p.lay.NS == 12 && p.lay.P == 2) p.lay = Lay{8, 4};
   p.blocks = (int)ceil_div(g.pairs, 32 / p.lay.P);
   p.cut = cut(g.T, warps_of(g, p.lay), kSms * kWarps * blocks_of(p.lay.NS));
   return p;
