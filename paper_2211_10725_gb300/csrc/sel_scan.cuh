@@ -115,6 +115,23 @@ __device__ __forceinline__ float2 softplus(float2 x, float2* slope) {
   return fma2(f2(2.0f), p, make_float2(fmaxf(x.x, 0.0f), fmaxf(x.y, 0.0f)));
 }
 
+// The approximate power of two is low on average, by 0.1 to 0.5 units of 2^-24 for decays
+// between 0.999 and 1/2 (measured, of arguments t with all their bits: about 50 |t| up to
+// |t| = 0.0082, then 0.41), and a state that remembers a thousand tokens multiplies a thousand
+// of them.  Eight tokens' worth of it goes back into the states after every eight, from
+// the sum of their s (2-norms of errors: states of 100 tokens 4e-7, 19e-7 without; grad_A of
+// 4096 tokens 6e-7, 18e-7 without).
+template <int NS>
+__device__ __forceinline__ void settle(float2 (&h)[NS], const float2 (&A2)[NS], float2 s8) {
+  constexpr float kMost = 8.0f * 0.0082f, kUnits = 50.0f / 16777216.0f;
+  const float2 share = mul2(s8, f2(-1.0f / kMost));
+#pragma unroll
+  for (int q = 0; q < NS; ++q) {
+    const float2 of = make_float2(__saturatef(share.x * A2[q].x), __saturatef(share.y * A2[q].y));
+    h[q] = fma2(mul2(of, f2(kMost * kUnits)), h[q], h[q]);
+  }
+}
+
 // 1 / (1 + e^-x).  Results rounded to 16 bits take the approximate power of
 // two and reciprocal: the rounding of x log2(e) costs |x| 2^-24 of the result.
 template <typename T>

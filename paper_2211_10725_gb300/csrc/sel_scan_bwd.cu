@@ -447,6 +447,12 @@ __device__ void scan_back(const Args& g, int64_t work, unsigned char* smem, uint
         sum_bias = add2(sum_bias, dd);
       }
     }
+    {
+      float2 s8 = f2(0.0f);
+#pragma unroll
+      for (int i = 0; i < kTile; ++i) s8 = add2(s8, *reinterpret_cast<const float2*>(psu + i * PW));
+      settle<NS>(gam, A2, s8);
+    }
     out_u -= kTile * g.gu.st;
     out_d -= kTile * g.gdelta.st;
     out_z -= kTile * g.gz.st;

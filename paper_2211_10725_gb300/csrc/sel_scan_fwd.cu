@@ -131,6 +131,7 @@ __global__ void __launch_bounds__(32) scan_fwd(const Args g) {
     fetch(start);
     fetch_bc(start);
   }
+  float2 s8 = f2(0.0f);  // sum of s since the states were settled
   for (int turn = 0; turn < turns; ++turn) {
     const int t0 = start + turn * kStep;
     float* const bc = smem[turn & 1];
@@ -194,8 +195,13 @@ __global__ void __launch_bounds__(32) scan_fwd(const Args g) {
           }
         }
       }
+      s8 = add2(s8, sk);
       if (MODE == kFull) y[k] = add2(sum[0], sum[1]);
-      else total = add2(total, sk);
+    }
+    if (turn & 1) {
+      settle<NS>(h, A2, s8);
+      if (MODE != kFull) total = add2(total, s8);
+      s8 = f2(0.0f);
     }
     if (MODE == kFull) {
       share_out<kFour, P>(y, pl);
@@ -223,6 +229,7 @@ __global__ void __launch_bounds__(32) scan_fwd(const Args g) {
       store_states<NS>(g.state_out + (place * g.D + c) * g.N, g.N, n0, second, h);
   } else {
     store_twos<NS>(ends + span * ends_step, g, n0, h);
+    total = add2(total, s8);
     if (pl == 0) g.sums[((int64_t)span * g.B * g.G + rest) * g.pairs + pair] = total;
   }
 }
