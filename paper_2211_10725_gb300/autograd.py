@@ -242,9 +242,14 @@ def _scratch(n, like):
     return torch.empty(n, dtype=torch.uint8, device=like.device)
 
 
+def _recorded(*tensors):
+    """Whether a backward pass may follow (inside a Function's forward torch no longer says)."""
+    return torch.is_grad_enabled() and any(t is not None and t.requires_grad for t in tensors)
+
+
 class _SelectiveScanFunction(torch.autograd.Function):
     @staticmethod
-    def forward(ctx, u, delta, A, B, C, D, z, delta_bias, state, softplus, seq_lens):
+    def forward(ctx, u, delta, A, B, C, D, z, delta_bias, state, softplus, seq_lens, recorded):
         u, delta, z = (_channels(t, u.dtype) for t in (u, delta, z))
         B, C = _grouped(B), _grouped(C)
         A, D, delta_bias, state, seq_lens = map(_whole, (A, D, delta_bias, state, seq_lens))
@@ -252,7 +257,7 @@ class _SelectiveScanFunction(torch.autograd.Function):
         y = torch.empty(u.shape, dtype=u.dtype, device=u.device)
         end = torch.empty((u.shape[0], *A.shape), dtype=torch.float32, device=u.device)
         ckpt = None
-        if any(ctx.needs_input_grad):
+        if recorded:
             ckpt = torch.empty(snn.snn_selective_scan_ckpt_elems(*shape), dtype=torch.float32, device=u.device)
         snn.snn_selective_scan_fwd(u, delta, A, B, C, y,
                                    _scratch(snn.snn_selective_scan_workspace_bytes(*shape), u), D=D, z=z,
@@ -268,7 +273,7 @@ class _SelectiveScanFunction(torch.autograd.Function):
     def backward(ctx, grad_y, grad_end):
         u, delta, A, B, C, D, z, delta_bias, state, seq_lens, ckpt = ctx.saved_tensors
         if grad_y is None and grad_end is None:
-            return (None,) * 11
+            return (None,) * 12
         shape = (*u.shape, A.shape[1], B.shape[2])
         grad_y = torch.zeros(u.shape, dtype=u.dtype, device=u.device) if grad_y is None \
             else _channels(grad_y, u.dtype)
@@ -279,7 +284,7 @@ class _SelectiveScanFunction(torch.autograd.Function):
                                    D=D, z=z, delta_bias=delta_bias, softplus=ctx.softplus, seq_lens=seq_lens,
                                    grad_state_out=_whole(grad_end), grad_D=gD, grad_z=gz,
                                    grad_delta_bias=gb, grad_state_in=gs)
-        return gu, gd, gA, gB, gC, gD, gz, gb, gs, None, None
+        return gu, gd, gA, gB, gC, gD, gz, gb, gs, None, None, None
 
 
 def selective_scan(u, delta, A, B, C, D=None, z=None, delta_bias=None, softplus=True, state=None,
@@ -292,7 +297,8 @@ def selective_scan(u, delta, A, B, C, D=None, z=None, delta_bias=None, softplus=
         raise ValueError("selective_scan: u must be [B, T, D], B and C [B, T, G, N], A [D, N]")
     if any(t is not None and t.dtype != u.dtype for t in (delta, z, B, C)):
         raise ValueError("selective_scan: u, delta, z, B and C must have one type")
-    return _SelectiveScanFunction.apply(u, delta, A, B, C, D, z, delta_bias, state, bool(softplus), seq_lens)
+    return _SelectiveScanFunction.apply(u, delta, A, B, C, D, z, delta_bias, state, bool(softplus), seq_lens,
+                                        _recorded(u, delta, A, B, C, D, z, delta_bias, state))
 
 
 class _CausalConvFunction(torch.autograd.Function):
@@ -338,13 +344,13 @@ def causal_conv(x, w, bias=None, act="silu", state=None, seq_lens=None):
 
 class _LayerNormFunction(torch.autograd.Function):
     @staticmethod
-    def forward(ctx, x, w, b, eps, dtype):
+    def forward(ctx, x, w, b, eps, dtype, recorded):
         shape, N = x.shape, x.shape[-1]
         x2 = _matrix(x, N, 0)
         w, b = _whole(w), _whole(b)
         y = torch.empty(x2.shape, dtype=dtype, device=x.device)
         stats = torch.empty((2, x2.shape[0]), dtype=torch.float32, device=x.device) \
-            if any(ctx.needs_input_grad) else None
+            if recorded else None
         snn.snn_layer_norm_fwd(x2, w, b, y, stats=stats, eps=eps)
         ctx.save_for_backward(x2, w, b, stats)
         ctx.shape, ctx.dtype = shape, dtype
@@ -358,10 +364,10 @@ class _LayerNormFunction(torch.autograd.Function):
         gx, gw, gb = map(_like, (x, w, b))
         snn.snn_layer_norm_bwd(x, w, stats, _matrix(grad_y, N, 0, ctx.dtype), gx, gw, gb,
                                _scratch(snn.snn_layer_norm_workspace_bytes(M, N), x))
-        return gx.view(ctx.shape), gw, gb, None, None
+        return gx.view(ctx.shape), gw, gb, None, None, None
 
 
 def layer_norm(x, w=None, b=None, eps=1e-5, dtype=None):
     """(x - mean) rsqrt(var + eps) w + b over the last dimension, as `dtype` (x's own, or a
     16-bit type of an fp32 x).  w and b: fp32 or None.  Differentiable in x, w and b."""
-    return _LayerNormFunction.apply(x, w, b, float(eps), dtype or x.dtype)
+    return _LayerNormFunction.apply(x, w, b, float(eps), dtype or x.dtype, _recorded(x, w, b))

@@ -173,9 +173,9 @@ def test_scan_workspaces(lib):
     assert _scan_fwd(lib, long, nws=need - 256 if need % 256 == 0 else need - 1) == WORKSPACE
     assert lib.snn_selective_scan_workspace_bytes(ctypes.byref(long), 1) >= need
     d = _scan()
-    # states before every eighth token, four to a thread and two channels to a pair
+    # states before every eighth token, in twos of two channels of a group
     assert lib.snn_selective_scan_ckpt_elems(ctypes.byref(d)) == 2 * 2 * 64 * 16
-    assert lib.snn_selective_scan_ckpt_elems(ctypes.byref(_scan(D=6, N=5, T=17))) == 2 * 3 * 2 * 2 * 2 * 8
+    assert lib.snn_selective_scan_ckpt_elems(ctypes.byref(_scan(D=6, N=5, T=17))) == 2 * 3 * 2 * 3 * 2 * 4
 
 
 SCAN_BWD = ["u", "delta", "A", "B", "C", "D", "z", "bias", "lens", "ckpt", "gy", "gs_out", "gu", "gdelta", "gA",
