@@ -78,22 +78,33 @@ __global__ void __launch_bounds__(32) scan_fwd(const Args g) {
   const int turns = stop > first ? (stop - first + kFour - 1) / kFour : 0;
   const int start = MODE == kBack ? first + (turns - 1) * kFour : first;
   constexpr int kStep = MODE == kBack ? -kFour : kFour;
-  // a thread's own tokens
+  // a thread's own tokens (past the last pair: that one's)
   const Seq& in = MODE == kBack ? g.gy : g.u;
-  auto own = [&](const Seq& m) { return static_cast<T*>(m.data) + b * m.sb + (int64_t)(start + pl) * m.st + c; };
+  const int c_in = live ? c : grp * g.Dg + 2 * (g.pairs - 1);
+  auto own = [&](const Seq& m) { return static_cast<T*>(m.data) + b * m.sb + (int64_t)(start + pl) * m.st + c_in; };
   const T *pu = own(in), *pd = own(g.delta), *pz = own(g.z);
   T* py = own(g.y);
   Raw<T> raw_u[U], raw_d[U], raw_z[U];
+  const bool quick = pairs_ok && g.quads;
   auto fetch = [&](int t0) {
+    if (quick && t0 + kFour <= stop) {  // all the tokens exist
 #pragma unroll
-    for (int j = 0; j < U; ++j) {
-      raw_u[j].clear();
-      raw_d[j].clear();
-      raw_z[j].clear();
-      if (live && t0 + pl + j * P < stop) {
-        raw_u[j].load(pu + j * P * in.st, pairs_ok, second);
-        raw_d[j].load(pd + j * P * g.delta.st, pairs_ok, second);
-        if (gate) raw_z[j].load(pz + j * P * g.z.st, pairs_ok, second);
+      for (int j = 0; j < U; ++j) {
+        raw_u[j].load(pu + j * P * in.st, true, true);
+        raw_d[j].load(pd + j * P * g.delta.st, true, true);
+        if (gate) raw_z[j].load(pz + j * P * g.z.st, true, true);
+      }
+    } else {
+#pragma unroll
+      for (int j = 0; j < U; ++j) {
+        raw_u[j].clear();
+        raw_d[j].clear();
+        raw_z[j].clear();
+        if (live && t0 + pl + j * P < stop) {
+          raw_u[j].load(pu + j * P * in.st, pairs_ok, second);
+          raw_d[j].load(pd + j * P * g.delta.st, pairs_ok, second);
+          if (gate) raw_z[j].load(pz + j * P * g.z.st, pairs_ok, second);
+        }
       }
     }
     pu += kStep * in.st;
@@ -132,7 +143,9 @@ __global__ void __launch_bounds__(32) scan_fwd(const Args g) {
     fetch_bc(start);
   }
   float2 s8 = f2(0.0f);  // sum of s since the states were settled
-  for (int turn = 0; turn < turns; ++turn) {
+  // whole: all the tokens exist, in pairs
+  auto tokens = [&](int turn, auto whole_) {
+    constexpr bool whole = decltype(whole_)::value;
     const int t0 = start + turn * kStep;
     float* const bc = smem[turn & 1];
 #pragma unroll
@@ -143,7 +156,7 @@ __global__ void __launch_bounds__(32) scan_fwd(const Args g) {
 #pragma unroll
     for (int j = 0; j < U; ++j) {
       s[j] = x[j] = f2(0.0f);
-      if (t0 + pl + j * P < stop) {
+      if (whole || t0 + pl + j * P < stop) {
         s[j] = step_of<T>(add2(raw_d[j].get(), bias), soft);
         x[j] = raw_u[j].get();
         if (MODE == kBack) {
@@ -151,7 +164,7 @@ __global__ void __launch_bounds__(32) scan_fwd(const Args g) {
         } else {
           x[j] = mul2(s[j], x[j]);
         }
-        if (!second) s[j].y = x[j].y = 0.0f;
+        if (!whole && !second) s[j].y = x[j].y = 0.0f;
       }
       now_u[j] = raw_u[j];
       now_z[j] = raw_z[j];
@@ -208,17 +221,26 @@ __global__ void __launch_bounds__(32) scan_fwd(const Args g) {
 #pragma unroll
       for (int j = 0; j < U; ++j) {
         const int now = t0 + pl + j * P;
-        if (live && now < last) {
+        if (live && (whole || now < last)) {
           float2 out = fma2(skip, now_u[j].get(), y[j * P]);
           if (gate) {
             const float2 z = now_z[j].get();
             out = mul2(out, mul2(z, sigmoid<T>(z)));
           }
-          put_pair(py + j * P * g.y.st, now < stop ? out : f2(0.0f), pairs_ok, second);
+          if (whole) put_pair(py + j * P * g.y.st, out, true, true);
+          else put_pair(py + j * P * g.y.st, now < stop ? out : f2(0.0f), pairs_ok, second);
         }
       }
       py += kStep * g.y.st;
     }
+  };
+  {
+    const int part = quick ? (stop - first) % kFour : 0;  // of the last four (backwards: the first turn)
+    int turn = 0;
+    if (MODE == kBack && turns && (!quick || part)) tokens(turn++, std::false_type());
+    const int until = !quick ? 0 : MODE != kBack && part ? turns - 1 : turns;
+    for (; turn < until; ++turn) tokens(turn, std::true_type());
+    for (; turn < turns; ++turn) tokens(turn, std::false_type());
   }
   if (!live) return;
   if (MODE == kFull) {
