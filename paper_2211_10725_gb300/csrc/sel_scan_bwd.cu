@@ -213,11 +213,15 @@ __device__ void scan_back(const Args& g, int64_t work, unsigned char* smem, uint
 
   // a thread's own tokens of the last tile, and its fours of states of B and C
   const int t_last = first + (tiles - 1) * kTile;
-  auto own = [&](const Seq& m) { return static_cast<T*>(m.data) + b * m.sb + (int64_t)(t_last + pl) * m.st + c; };
+  // (past the last pair: that one's inputs, with s and dy of zero)
+  const int pair_in = live ? pair : g.pairs - 1;
+  auto own = [&](const Seq& m) {
+    return static_cast<T*>(m.data) + b * m.sb + (int64_t)(t_last + pl) * m.st + grp * g.Dg + 2 * pair_in;
+  };
   const T *in_u = own(g.u), *in_d = own(g.delta), *in_g = own(g.gy), *in_z = own(g.z);
   T *out_u = own(g.gu), *out_d = own(g.gdelta), *out_z = own(g.gz);
   const float* ckpt = g.ckpt + (((int64_t)b * ((g.T + kTile - 1) / kTile) + t_last / kTile) * g.G + grp) * row_states +
-                      ((int64_t)(n0 / 2) * g.pairs + pair) * 4;
+                      ((int64_t)(n0 / 2) * g.pairs + pair_in) * 4;
   const int bc_tok = lane * 4 / Np, bc_n = lane * 4 % Np, absent = bc_n + 4 - g.N > 0 ? bc_n + 4 - g.N : 0;
   const T* pB = static_cast<const T*>(g.Bm.data) + b * g.Bm.sb + (int64_t)(t_last + bc_tok) * g.Bm.st + grp * g.Bm.sg + bc_n;
   const T* pC = static_cast<const T*>(g.Cm.data) + b * g.Cm.sb + (int64_t)(t_last + bc_tok) * g.Cm.st + grp * g.Cm.sg + bc_n;
@@ -230,63 +234,93 @@ __device__ void scan_back(const Args& g, int64_t work, unsigned char* smem, uint
       if (j == 0 || n0 + at + j < g.N) p[j] = v[j];
   };
 
-  // a tile's inputs on their way to shared memory
+  // a tile's inputs on their way to shared memory; quick: all of them, in whole vectors
+  const bool quick = pairs_ok && quads_ok;
   auto fetch = [&](int tokens) {
+    if (quick && tokens == kTile) {
 #pragma unroll
-    for (int j = 0; j < U; ++j) {
-      const int tok = pl + j * P;
-      Raw<T>* const to = raw + tok * PW;
-      auto one = [&](int k, const T* p) {
-        if (pairs_ok && live && tok < tokens) {
-          copy_async<sizeof(Raw<T>)>(to + k * kTile * PW, p);
-        } else {
+      for (int j = 0; j < U; ++j) {
+        Raw<T>* const to = raw + (pl + j * P) * PW;
+        copy_async<sizeof(Raw<T>)>(to, in_u + j * P * g.u.st);
+        copy_async<sizeof(Raw<T>)>(to + kTile * PW, in_d + j * P * g.delta.st);
+        copy_async<sizeof(Raw<T>)>(to + 2 * kTile * PW, in_g + j * P * g.gy.st);
+        if (gate) copy_async<sizeof(Raw<T>)>(to + 3 * kTile * PW, in_z + j * P * g.z.st);
+      }
+#pragma unroll
+      for (int i = 0; i < kTurns; ++i) {
+        const int tok = bc_tok + i * kTokens;
+        if (tok < kTile && bc_tok < kTokens && absent == 0) {
+          copy_async<4 * sizeof(T)>(raw_bc + tok * 2 * Np + bc_n, pB + i * kTokens * g.Bm.st);
+          copy_async<4 * sizeof(T)>(raw_bc + (tok * 2 + 1) * Np + bc_n, pC + i * kTokens * g.Cm.st);
+        }
+      }
+#pragma unroll
+      for (int k = 0; k < NS / 2; ++k)
+        if (n0 / 2 + k < g.N2) copy_async<16>(h0 + k * 32, ckpt + (int64_t)k * g.pairs * 4);
+    } else {
+#pragma unroll
+      for (int j = 0; j < U; ++j) {
+        const int tok = pl + j * P;
+        Raw<T>* const to = raw + tok * PW;
+        auto one = [&](int k, const T* p) {
           Raw<T> r;
           r.clear();
-          if (live && tok < tokens) r.load(p, false, second);
+          if (live && tok < tokens) r.load(p, pairs_ok, second);
           to[k * kTile * PW] = r;
+        };
+        one(0, in_u + j * P * g.u.st);
+        one(1, in_d + j * P * g.delta.st);
+        one(2, in_g + j * P * g.gy.st);
+        if (gate) one(3, in_z + j * P * g.z.st);
+      }
+#pragma unroll
+      for (int i = 0; i < kTurns; ++i) {
+        const int tok = bc_tok + i * kTokens;
+        if (tok < kTile && bc_tok < kTokens) {
+          auto one = [&](int k, const T* p) {
+            Four<T> r;
+            r.clear();
+            if (tok < tokens && absent < 4) r.load(p, quads_ok, absent);
+            *reinterpret_cast<Four<T>*>(raw_bc + (tok * 2 + k) * Np + bc_n) = r;
+          };
+          one(0, pB + i * kTokens * g.Bm.st);
+          one(1, pC + i * kTokens * g.Cm.st);
         }
-      };
-      one(0, in_u + j * P * g.u.st);
-      one(1, in_d + j * P * g.delta.st);
-      one(2, in_g + j * P * g.gy.st);
-      if (gate) one(3, in_z + j * P * g.z.st);
+      }
+#pragma unroll
+      for (int k = 0; k < NS / 2; ++k) {
+        float4 v = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+        if (live && n0 / 2 + k < g.N2) v = *reinterpret_cast<const float4*>(ckpt + (int64_t)k * g.pairs * 4);
+        h0[k * 32] = v;
+      }
     }
     in_u -= kTile * g.u.st;
     in_d -= kTile * g.delta.st;
     in_g -= kTile * g.gy.st;
     in_z -= kTile * g.z.st;
-#pragma unroll
-    for (int i = 0; i < kTurns; ++i) {
-      const int tok = bc_tok + i * kTokens;
-      if (tok < kTile && bc_tok < kTokens) {
-        auto one = [&](int k, const T* p) {
-          T* const to = raw_bc + (tok * 2 + k) * Np + bc_n;
-          if (quads_ok && tok < tokens && absent == 0) {
-            copy_async<4 * sizeof(T)>(to, p);
-          } else {
-            Four<T> r;
-            r.clear();
-            if (tok < tokens && absent < 4) r.load(p, false, absent);
-            *reinterpret_cast<Four<T>*>(to) = r;
-          }
-        };
-        one(0, pB + i * kTokens * g.Bm.st);
-        one(1, pC + i * kTokens * g.Cm.st);
-      }
-    }
     pB -= kTile * g.Bm.st;
     pC -= kTile * g.Cm.st;
-#pragma unroll
-    for (int k = 0; k < NS / 2; ++k) {
-      if (live && n0 / 2 + k < g.N2) copy_async<16>(h0 + k * 32, ckpt + (int64_t)k * g.pairs * 4);
-      else h0[k * 32] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-    }
     ckpt -= g.G * row_states;
   };
   auto tokens_of = [&](int tile) {
     const int n = stop - (first + tile * kTile);
     return n < kTile ? n : kTile;
   };
+  {  // absent states stay zero
+#pragma unroll
+    for (int k = 0; k < NS / 2; ++k)
+      if (n0 / 2 + k >= g.N2) h0[k * 32] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+#pragma unroll
+    for (int i = 0; i < kTurns; ++i) {
+      const int tok = bc_tok + i * kTokens;
+      if (tok < kTile && bc_tok < kTokens && absent > 0) {
+        Four<T> r;
+        r.clear();
+        *reinterpret_cast<Four<T>*>(raw_bc + tok * 2 * Np + bc_n) = r;
+        *reinterpret_cast<Four<T>*>(raw_bc + (tok * 2 + 1) * Np + bc_n) = r;
+      }
+    }
+  }
   if (tiles) fetch(tokens_of(tiles - 1));
   const float* const bc_own = bc + copy_at(NS, P, kCopies == 1 ? 0 : kCopies == 2 ? (order >> 1) & 1 : order & 3) + n0;
   const int first_four = order >> 2;
@@ -326,12 +360,14 @@ __device__ void scan_back(const Args& g, int64_t work, unsigned char* smem, uint
       const Raw<T>* const from = raw + tok * PW;
       const float2 u = from[0].get();
       float2 s = f2(0.0f), dy = from[2 * kTile * PW].get(), slope = f2(0.0f), gz = f2(0.0f);
-      if (live && tok < tokens) s = step_of<T>(add2(from[kTile * PW].get(), bias), soft, &slope);
+      if (quick && tokens == kTile) s = step_of<T>(add2(from[kTile * PW].get(), bias), soft, &slope);
+      else if (live && tok < tokens) s = step_of<T>(add2(from[kTile * PW].get(), bias), soft, &slope);
       if (gate) {
         const float2 z = from[3 * kTile * PW].get(), sig = sigmoid<T>(z), zs = mul2(z, sig);
         gz = mul2(dy, fma2(zs, fma2(sig, f2(-1.0f), f2(1.0f)), sig));
         dy = mul2(dy, zs);
       }
+      if (!live) s = dy = f2(0.0f);
       if (!second) s.y = dy.y = 0.0f;
       psu[tok * PW] = make_float4(s.x, s.y, u.x, u.y);
       psg[tok * PW] = make_float4(slope.x, slope.y, gz.x, gz.y);
