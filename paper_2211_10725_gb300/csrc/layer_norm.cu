@@ -55,6 +55,13 @@ __host__ __device__ constexpr int bwd_stage(int N, int t_size, int r_size) {
   return slot_bytes(N, r_size) + slot_bytes(N, t_size);
 }
 
+// Rows a team of the backward works on at once: their sums share an exchange
+// (gradients of 16384x2048 bf16: 36 us, 47 with one row at a time).  Not for
+// the longest rows, whose threads have 64 registers, and not forward, where the
+// copies on their way hide the exchange (76 us at 16384x4096 either way).
+template <int TPR>
+constexpr int kBwdRows = TPR == 1024 ? 1 : 2;
+
 extern __shared__ __align__(16) unsigned char ln_smem[];
 
 template <typename T, typename R, bool VEC, int TPR>
@@ -117,44 +124,56 @@ __global__ void __launch_bounds__(kBlockThreads<TPR>, 1024 / kBlockThreads<TPR>)
 template <typename T, typename R, bool VEC, int TPR>
 __global__ void __launch_bounds__(kBlockThreads<TPR>, TPR == 1024 ? 1 : kBwdThreads / kBlockThreads<TPR>)
     ln_bwd(const Args g) {
-  __shared__ __align__(16) float scratch[2][3][32];
+  constexpr int kRows = kBwdRows<TPR>;
+  __shared__ __align__(16) float scratch[2][2 * kRows][32];
   grid_dep_wait();
   constexpr bool kLong = TPR == 1024, kHeld = VEC && !kLong;
   const int t = threadIdx.x % TPR, team = threadIdx.x / TPR, N = g.N;
   const int64_t step = (int64_t)gridDim.x * kTeams<TPR>;
   int64_t row = (int64_t)blockIdx.x * kTeams<TPR> + team;
   const float inv_n = 1.0f / (float)N;
-  RowSum<TPR> row_sum{scratch};
-  const int stage = bwd_stage(N, sizeof(T), sizeof(R));
+  RowSum<TPR, 2 * kRows> row_sum{scratch};
+  const int slot_size = bwd_stage(N, sizeof(T), sizeof(R)), stage = kRows * slot_size;
   unsigned char* const base = ln_smem + team * g.stages * stage;
   const int r_bytes = slot_bytes(N, sizeof(R));
-  auto x_slot = [&](int k) { return Slot<R, VEC, TPR>{base + k * stage}; };
-  auto gy_slot = [&](int k) { return Slot<T, VEC, TPR>{base + k * stage + r_bytes}; };
+  auto x_slot = [&](int k, int j) { return Slot<R, VEC, TPR>{base + k * stage + j * slot_size}; };
+  auto gy_slot = [&](int k, int j) { return Slot<T, VEC, TPR>{base + k * stage + j * slot_size + r_bytes}; };
   auto fetch = [&](int64_t i, int k) {
-    if (i < g.M) {
-      x_slot(k).fetch(g.x, i, g.M, N, t);
-      gy_slot(k).fetch(g.gy, i, g.M, N, t);
+#pragma unroll
+    for (int j = 0; j < kRows; ++j) {
+      if (i + j * step < g.M) {
+        x_slot(k, j).fetch(g.x, i + j * step, g.M, N, t);
+        gy_slot(k, j).fetch(g.gy, i + j * step, g.M, N, t);
+      }
     }
     copies_commit();
   };
   const int ahead = g.stages - 1;
-  Held<R> held_x;
-  Held<T> held_gy;
-  float next_mean = 0.0f, next_rstd = 0.0f;
+  Held<R> held_x[kRows];
+  Held<T> held_gy[kRows];
+  float next_mean[kRows], next_rstd[kRows];
   auto hold = [&](int64_t i) {
-    if (i >= g.M) return;
-    held_x.fetch(g.x, i, N, t);
-    held_gy.fetch(g.gy, i, N, t);
+#pragma unroll
+    for (int j = 0; j < kRows; ++j) {
+      if (i + j * step >= g.M) return;
+      held_x[j].fetch(g.x, i + j * step, N, t);
+      held_gy[j].fetch(g.gy, i + j * step, N, t);
+    }
   };
   auto take_stats = [&](int64_t i) {
-    if (i >= g.M) return;
-    next_mean = g.stats[i];
-    next_rstd = g.stats[g.M + i];
+#pragma unroll
+    for (int j = 0; j < kRows; ++j) {
+      if (i + j * step >= g.M) return;
+      next_mean[j] = g.stats[i + j * step];
+      next_rstd[j] = g.stats[g.M + i + j * step];
+    }
   };
+#pragma unroll
+  for (int j = 0; j < kRows; ++j) next_mean[j] = next_rstd[j] = 0.0f;
   if constexpr (kHeld) {
     hold(row);
   } else {
-    for (int i = 0; i < (ahead ? ahead : 1); ++i) fetch(row + i * step, i);
+    for (int i = 0; i < (ahead ? ahead : 1); ++i) fetch(row + i * kRows * step, i);
   }
   take_stats(row);
   Sums<kLong> sums;  // 0: of grad_y e, 1: of grad_y
@@ -165,40 +184,63 @@ __global__ void __launch_bounds__(kBlockThreads<TPR>, TPR == 1024 ? 1 : kBwdThre
 #pragma unroll
   for (int e = 0; e < E; ++e) one[e] = 1.0f;
   load_param<VEC, TPR>(g.w, N, t, w);
-  for (int k = 0, next = ahead; row < g.M; row += step) {
-    float x[E], gy[E];
+  for (int k = 0, next = ahead; row < g.M; row += kRows * step) {
+    float x[kRows][E], gy[kRows][E];
     if constexpr (kHeld) {
-      held_x.get(N, t, x);
-      held_gy.get(N, t, gy);
-      hold(row + step);
+#pragma unroll
+      for (int j = 0; j < kRows; ++j) {
+        held_x[j].get(N, t, x[j]);
+        held_gy[j].get(N, t, gy[j]);
+      }
+      hold(row + kRows * step);
     } else {
-      if (ahead) fetch(row + ahead * step, next);  // that stage was read before the last row's sums
+      if (ahead) fetch(row + ahead * kRows * step, next);  // that stage was read before the last rows' sums
       copies_wait(ahead);
       if (!VEC) team_sync<TPR>();
-      x_slot(k).get(g.x, row, N, t, x);
-      gy_slot(k).get(g.gy, row, N, t, gy);
-    }
-    const float mean = next_mean, rstd = next_rstd;
-    take_stats(row + step);
-    float v[E];
 #pragma unroll
-    for (int e = 0; e < E; e += 2) {
-      put2(x, e, mul2(add2(two(x, e), both(-mean)), both(rstd)));
-      put2(v, e, mul2(two(gy, e), two(w, e)));
+      for (int j = 0; j < kRows; ++j) {
+        x_slot(k, j).get(g.x, row + j * step, N, t, x[j]);
+        gy_slot(k, j).get(g.gy, row + j * step, N, t, gy[j]);
+      }
     }
-    // past N: v is zero, so the x there enters nothing
-    float ss[2] = {sum(v), dot(v, x)};
-    sums.add(0, gy, x);
-    sums.add(1, gy, one);
+    float mean[kRows], rstd[kRows], ss[2 * kRows];
+#pragma unroll
+    for (int j = 0; j < kRows; ++j) {
+      mean[j] = next_mean[j];
+      rstd[j] = next_rstd[j];
+    }
+    take_stats(row + kRows * step);
+#pragma unroll
+    for (int j = 0; j < kRows; ++j) {
+      float v[E];
+#pragma unroll
+      for (int e = 0; e < E; e += 2) {
+        put2(x[j], e, mul2(add2(two(x[j], e), both(-mean[j])), both(rstd[j])));
+        put2(v, e, mul2(two(gy[j], e), two(w, e)));
+      }
+      // past N: v is zero, so the x there enters nothing; a row past M enters no sum
+      if (row + j * step < g.M) {
+        sums.add(0, gy[j], x[j]);
+        sums.add(1, gy[j], one);
+      }
+      ss[2 * j] = sum(v);
+      ss[2 * j + 1] = dot(v, x[j]);
+#pragma unroll
+      for (int e = 0; e < E; ++e) gy[j][e] = v[e];
+    }
     row_sum(ss);
     if (!VEC && TPR == 32) team_sync<TPR>();
-    if (!kHeld && !ahead) fetch(row + step, 0);  // the row is read: its stage is free
+    if (!kHeld && !ahead) fetch(row + kRows * step, 0);  // the rows are read: their stage is free
     if (g.gx.data) {
-      const float m0 = ss[0] * inv_n, m1 = ss[1] * inv_n;
 #pragma unroll
-      for (int e = 0; e < E; e += 2)
-        put2(v, e, mul2(both(rstd), fma2(two(x, e), both(-m1), add2(two(v, e), both(-m0)))));
-      store_row<R, VEC, TPR>(g.gx, row, N, t, v);
+      for (int j = 0; j < kRows; ++j) {
+        if (row + j * step >= g.M) break;
+        const float m0 = ss[2 * j] * inv_n, m1 = ss[2 * j + 1] * inv_n;
+#pragma unroll
+        for (int e = 0; e < E; e += 2)
+          put2(gy[j], e, mul2(both(rstd[j]), fma2(two(x[j], e), both(-m1), add2(two(gy[j], e), both(-m0)))));
+        store_row<R, VEC, TPR>(g.gx, row + j * step, N, t, gy[j]);
+      }
     }
     k = k + 1 == g.stages ? 0 : k + 1;
     next = next + 1 == g.stages ? 0 : next + 1;
@@ -320,7 +362,7 @@ cudaError_t launch_tpr(const Launch& l) {
     return launch_staged(ln_fwd<T, R, VEC, TPR>, l, kThreads, kTeams<TPR>, slot_bytes(l.g.N, sizeof(R)), 0,
                          1024 / kThreads, 2);
   return launch_staged(ln_bwd<T, R, VEC, TPR>, l, kThreads, kTeams<TPR>,
-                       VEC && TPR < 1024 ? 0 : bwd_stage(l.g.N, sizeof(T), sizeof(R)),
+                       VEC && TPR < 1024 ? 0 : kBwdRows<TPR> * bwd_stage(l.g.N, sizeof(T), sizeof(R)),
                        TPR == 1024 ? 2 * E * sizeof(float) * TPR : 0,
                        TPR == 1024 ? 1 : kBwdThreads / kThreads, 1);
 }

@@ -207,9 +207,9 @@ __device__ __forceinline__ void load_param(const float* p, int N, int t, float v
 // Sums of K values over the TPR threads of a row; every thread gets them.
 // Successive sums alternate between two scratch buffers, so one barrier a sum
 // is enough: a warp cannot be two sums ahead.
-template <int TPR>
+template <int TPR, int MOST = 3>
 struct RowSum {
-  float (*scratch)[3][32];  // [2][value][warp]
+  float (*scratch)[MOST][32];  // [2][value][warp]
   int turn = 0;
   // in_group: the last value's sum over a group's `lanes` neighbouring threads
   template <int K>
