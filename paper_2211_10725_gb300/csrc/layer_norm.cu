@@ -4,8 +4,11 @@
 //   grad_x = rstd (g - mean(g) - e mean(g e));   grad_w = sum grad_y e;   grad_b = sum grad_y
 // Every tensor is read and written once, so the bound is HBM.  The plan is that
 // of the block norms (norm_rows.cuh): a warp or a block to a row, eight channels
-// to a thread, the next rows on their way to shared memory (the backward's, in
-// registers) while the present one is worked on.  The variance is the sum of
+// to a thread, the next two rows on their way to its registers while the present
+// ones are worked on (through shared memory, 16384x4096 bf16 on an fp32 stream took 77 us
+// for 70: its copies of 16 bytes each touch half a sector of a 32-bit row; three rows on
+// their way 69 for 68).  Rows that are not whole 16-byte vectors, and
+// the longest rows' backward, pass through shared memory.  The variance is the sum of
 // squares about the mean, from the registers: a row far from zero loses no
 // bits.  The backward takes mean and rstd as the forward stored them (8 bytes a
 // row), so that its two sums over a row meet in one exchange; grad_w and grad_b gather
@@ -55,10 +58,14 @@ __host__ __device__ constexpr int bwd_stage(int N, int t_size, int r_size) {
   return slot_bytes(N, r_size) + slot_bytes(N, t_size);
 }
 
-// Rows a team of the backward works on at once: their sums share an exchange
-// (gradients of 16384x2048 bf16: 36 us, 47 with one row at a time).  Not for
-// the longest rows, whose threads have 64 registers, and not forward, where the
-// copies on their way hide the exchange (76 us at 16384x4096 either way).
+// Rows that a team works on at once, their sums in one exchange.  Forward where
+// a row is several warps' (16384x4096 bf16 on an fp32 stream: 63 us, 68 with one
+// row at a time; 16384x2048 bf16: 24.8 and 27.9), but one by one where it is one
+// warp's (no barrier to share: 40000x200 23.7 against 21.6, with its gradients)
+// or a whole block's (8192x8192: 82.6 against 77.8).  Backward for all but the longest rows,
+// whose threads have 64 registers (16384x2048 bf16: 38 us, 47).
+template <int TPR>
+constexpr bool kPaired = TPR > 32 && TPR < 1024;
 template <int TPR>
 constexpr int kBwdRows = TPR == 1024 ? 1 : 2;
 
@@ -88,37 +95,85 @@ __global__ void __launch_bounds__(kBlockThreads<TPR>, 1024 / kBlockThreads<TPR>)
     if (i < g.M) slot(k).fetch(g.x, i, g.M, N, t);
     copies_commit();
   };
-  const int ahead = g.stages - 1;  // at least one
-  for (int i = 0; i < ahead; ++i) fetch(row + i * step, i);
-  for (int k = 0, next = ahead; row < g.M; row += step) {
-    fetch(row + ahead * step, next);  // that stage was read before the last row's sums
-    copies_wait(ahead);
-    if (!VEC) team_sync<TPR>();
-    float x[E];
-    slot(k).get(g.x, row, N, t, x);
-    float s[1] = {sum(x)};
-    row_sum(s);
-    const float mean = s[0] * inv_n;
+  auto work = [&](int64_t first, auto& x) {  // x: [rows][E]
+    constexpr int kRows = sizeof(x) / sizeof(x[0]);
+    float s[kRows], mean[kRows];
 #pragma unroll
-    for (int e = 0; e < E; ++e) {
-      const int c = VEC ? t * E + e : e * TPR + t;
-      x[e] = c < N ? x[e] - mean : 0.0f;
-    }
-    s[0] = square_sum(x);
+    for (int j = 0; j < kRows; ++j) s[j] = sum(x[j]);
     row_sum(s);
-    if (TPR == 32) team_sync<TPR>();
-    const float rstd = rsqrtf(fmaf(s[0], inv_n, g.eps));
-    if (g.stats && t == 0) {
-      g.stats[row] = mean;
-      g.stats[g.M + row] = rstd;
-    }
 #pragma unroll
-    for (int e = 0; e < E; e += 2) put2(x, e, fma2(mul2(two(x, e), both(rstd)), two(w, e), two(b, e)));
-    store_row<T, VEC, TPR>(g.y, row, N, t, x);
-    k = k + 1 == g.stages ? 0 : k + 1;
-    next = next + 1 == g.stages ? 0 : next + 1;
+    for (int j = 0; j < kRows; ++j) {
+      mean[j] = s[j] * inv_n;
+      if constexpr (VEC) {  // past N: zero less zero
+        const float off = t * E < N ? -mean[j] : 0.0f;
+#pragma unroll
+        for (int e = 0; e < E; e += 2) put2(x[j], e, add2(two(x[j], e), both(off)));
+      } else {
+#pragma unroll
+        for (int e = 0; e < E; ++e) x[j][e] = e * TPR + t < N ? x[j][e] - mean[j] : 0.0f;
+      }
+      s[j] = square_sum(x[j]);
+    }
+    row_sum(s);
+#pragma unroll
+    for (int j = 0; j < kRows; ++j) {
+      const int64_t row = first + j * step;
+      if (j && row >= g.M) break;
+      const float rstd = rsqrtf(fmaf(s[j], inv_n, g.eps));
+      if (g.stats && t == 0) {
+        g.stats[row] = mean[j];
+        g.stats[g.M + row] = rstd;
+      }
+#pragma unroll
+      for (int e = 0; e < E; e += 2)
+        put2(x[j], e, fma2(mul2(two(x[j], e), both(rstd)), two(w, e), two(b, e)));
+      store_row<T, VEC, TPR>(g.y, row, N, t, x[j]);
+    }
+  };
+  if constexpr (VEC) {
+    Held<R> held[2];
+    auto take = [&](int64_t i, Held<R>& h, float (&x)[E]) {  // row i, and two rows on on its way
+      h.get(N, t, x);
+      if (i + 2 * step < g.M) h.fetch(g.x, i + 2 * step, N, t);
+    };
+#pragma unroll
+    for (int j = 0; j < 2; ++j)
+      if (row + j * step < g.M) held[j].fetch(g.x, row + j * step, N, t);
+    while (row < g.M) {
+      if constexpr (kPaired<TPR>) {
+        float x[2][E];  // (the second row past M: whatever its registers hold, never stored)
+#pragma unroll
+        for (int j = 0; j < 2; ++j) take(row + j * step, held[j], x[j]);
+        work(row, x);
+        row += 2 * step;
+      } else {
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+          if (row < g.M) {
+            float x[1][E];
+            take(row, held[j], x[0]);
+            work(row, x);
+          }
+          row += step;
+        }
+      }
+    }
+  } else {
+    const int ahead = g.stages - 1;  // at least one
+    for (int i = 0; i < ahead; ++i) fetch(row + i * step, i);
+    for (int k = 0, next = ahead; row < g.M; row += step) {
+      fetch(row + ahead * step, next);  // that stage was read before the last row's sums
+      copies_wait(ahead);
+      team_sync<TPR>();
+      float x[1][E];
+      slot(k).get(g.x, row, N, t, x[0]);
+      if (TPR == 32) team_sync<TPR>();
+      work(row, x);
+      k = k + 1 == g.stages ? 0 : k + 1;
+      next = next + 1 == g.stages ? 0 : next + 1;
+    }
+    copies_wait(0);
   }
-  copies_wait(0);
 }
 
 template <typename T, typename R, bool VEC, int TPR>
@@ -359,8 +414,8 @@ template <typename T, typename R, bool VEC, int TPR>
 cudaError_t launch_tpr(const Launch& l) {
   constexpr int kThreads = kBlockThreads<TPR>;
   if (!l.bwd)
-    return launch_staged(ln_fwd<T, R, VEC, TPR>, l, kThreads, kTeams<TPR>, slot_bytes(l.g.N, sizeof(R)), 0,
-                         1024 / kThreads, 2);
+    return launch_staged(ln_fwd<T, R, VEC, TPR>, l, kThreads, kTeams<TPR>,
+                         VEC ? 0 : slot_bytes(l.g.N, sizeof(R)), 0, 1024 / kThreads, 2);
   return launch_staged(ln_bwd<T, R, VEC, TPR>, l, kThreads, kTeams<TPR>,
                        VEC && TPR < 1024 ? 0 : kBwdRows<TPR> * bwd_stage(l.g.N, sizeof(T), sizeof(R)),
                        TPR == 1024 ? 2 * E * sizeof(float) * TPR : 0,
