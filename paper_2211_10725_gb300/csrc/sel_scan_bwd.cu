@@ -622,7 +622,7 @@ template <typename T>
 cudaError_t launch_bwd(const Args& g, const BwdPlan& p, const Mat& gB, const Mat& gC, cudaStream_t st) {
   const int64_t works = warps_of(g, p.lay) * g.spans, all = (int64_t)g.B * g.T * g.G * g.N;
   if (works > 0x7fffffff || ceil_div(all, 32) > 0x7fffffff) return cudaErrorInvalidValue;
-  const cudaError_t e = with_lay(p.lay, [&](auto NS, auto P) {
+  const cudaError_t e = with_lay<false>(p.lay, [&](auto NS, auto P) {
     return launch_main<T, decltype(NS)::value, decltype(P)::value>(g, works, st);
   });
   if (e != cudaSuccess || all == 0) return e;

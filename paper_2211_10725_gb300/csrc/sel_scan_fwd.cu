@@ -260,7 +260,7 @@ template <typename T, int MODE>
 cudaError_t launch_mode(const Args& g, Lay lay, int spans, cudaStream_t st) {
   const int64_t blocks = warps_of(g, lay);
   if (blocks > 0x7fffffff) return cudaErrorInvalidValue;
-  return with_lay(lay, [&](auto NS, auto P) {
+  return with_lay<MODE != kBack>(lay, [&](auto NS, auto P) {
     return launch_pdl(scan_fwd<T, MODE, decltype(NS)::value, decltype(P)::value>, dim3((unsigned)blocks, (unsigned)spans),
                       dim3(32), 0, st, g);
   });

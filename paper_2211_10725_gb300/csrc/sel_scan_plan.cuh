@@ -44,8 +44,9 @@ inline Lay lay_of(int N) {
 }
 inline int64_t warps_of(const Args& g, Lay l) { return (int64_t)g.B * g.G * ceil_div(g.pairs, 32 / l.P); }
 
-// f(states, threads) as constants.
-template <typename F>
+// f(states, threads) as constants (kNarrow: of a forward pass, whose plan may take four
+// threads for 9 to 16 states).
+template <bool kNarrow, typename F>
 cudaError_t with_lay(Lay l, F f) {
   using std::integral_constant;
   if (l.P == 1) return f(integral_constant<int, 4>(), integral_constant<int, 1>());
@@ -54,7 +55,8 @@ cudaError_t with_lay(Lay l, F f) {
     if (l.NS == 8) return f(integral_constant<int, 8>(), integral_constant<int, 2>());
     return f(integral_constant<int, 12>(), integral_constant<int, 2>());
   }
-  if (l.NS == 4) return f(integral_constant<int, 4>(), integral_constant<int, 4>());
+  if constexpr (kNarrow)
+    if (l.NS == 4) return f(integral_constant<int, 4>(), integral_constant<int, 4>());
   if (l.NS == 8) return f(integral_constant<int, 8>(), integral_constant<int, 4>());
   if (l.NS == 12) return f(integral_constant<int, 12>(), integral_constant<int, 4>());
   return f(integral_constant<int, 16>(), integral_constant<int, 4>());
@@ -69,8 +71,8 @@ inline FwdPlan fwd_plan(const Args& g) {
   p.lay = lay_of(g.N);
   // too few channels and tokens to fill the GPU: more threads to a pair
   const int64_t spans = g.T >= kMinSpan ? g.T / kMinSpan : 1;
-  if (warps_of(g, p.lay) * spans < kSms * 8 && g.N > 4 && g.N <= 24)
-    p.lay = g.N <= 8 ? Lay{4, 2} : g.N <= 16 ? Lay{4, 4} : Lay{8, 4};
+  if (warps_of(g, p.lay) * spans < kSms * 8 && g.N > 8 && g.N <= 24)
+    p.lay = g.N <= 16 ? Lay{4, 4} : Lay{8, 4};
   p.cut = cut(g.T, warps_of(g, p.lay), kSms * 16);
   return p;
 }

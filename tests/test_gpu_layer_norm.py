@@ -117,6 +117,32 @@ def test_many_rows_repeat_and_no_rows(cuda_device):
     assert torch.count_nonzero(gw) == 0 and torch.count_nonzero(gb) == 0
 
 
+# rows of several warps are worked on two at a time: teams with an odd count, the last rows alone
+@pytest.mark.parametrize("dtype,res", [(BF, F32), (HF, HF), (F32, F32)])
+@pytest.mark.parametrize("M,N", [(2000, 1024), (1001, 2048), (461, 4096), (305, 4090), (306, 8192), (4100, 512)])
+def test_several_rows_of_a_team(M, N, dtype, res, cuda_device):
+    Case(cuda_device, M, N, dtype, res).check()
+
+
+@pytest.mark.parametrize("N", [1024, 1001, 200])
+def test_a_row_without_values_stays_alone(N, cuda_device):
+    """Whatever lies in some rows, the others' results are the same bits."""
+    c = Case(cuda_device, 2500, N, F32, F32)
+    got = []
+    for bad in (None, NAN, float("inf")):
+        if bad is not None:
+            c.x[5::100] = bad
+        y, stats, gx = torch.empty_like(c.x), torch.empty(2, 2500, device=cuda_device), torch.empty_like(c.x)
+        snn.snn_layer_norm_fwd(c.x, c.w, c.b, y, stats=stats, eps=EPS)
+        snn.snn_layer_norm_bwd(c.x, c.w, stats, c.gy, gx, None, None, None)
+        got.append((y, gx))
+    good = torch.ones(2500, dtype=torch.bool, device=cuda_device)
+    good[5::100] = False
+    for y, gx in got[1:]:
+        assert torch.equal(y[good], got[0][0][good]) and torch.equal(gx[good], got[0][1][good])
+        assert torch.isnan(y[~good]).all() and torch.isnan(gx[~good]).all()
+
+
 def test_in_place(cuda_device):
     for N in (64, 61):
         c = Case(cuda_device, 700, N, F32, F32)
