@@ -4,7 +4,9 @@
 //   h_t = a_t h_{t-1} + x_t B_t,   y_t = (sum_n C_t h_t + D u_t) silu(z_t)
 //
 // A thread holds NS states (4, 8, 12 or 16) of two neighbouring channels of a group (a
-// pair), in pairs of floats: one instruction serves both channels.  P threads side by side (1,
+// pair), in pairs of floats: v[2 k + j] is the states 2 k and 2 k + 1 of channel j, and one
+// instruction serves both.  (B and C come in such pairs from where they lie; with the
+// channels paired instead, what B or C enters took two instructions.)  P threads side by side (1,
 // 2 or 4, P NS >= N) hold a pair's states, so that a warp has 32 / P pairs, and share out its
 // tokens where inputs are made ready and results finished.  A warp works alone: B and C
 // of a few tokens lie in shared memory of its own, and no barrier joins it to another
@@ -60,7 +62,7 @@ struct Args {
   const float* state_in;
   float* state_out;
   int64_t num_slots;
-  float* ckpt;             // [B][ceil(T / 8)][G][N2][pairs][4]: two states of two channels
+  float* ckpt;             // [B][ceil(T / 8)][G][N2][pairs][4]: two states of one channel, then the other
   float* ends;             // [spans fine][B][G][N2][pairs][4]: what a part adds to the state
   float2* sums;            // [spans fine][B][G pairs]: of s over a part
   // backward
@@ -81,6 +83,9 @@ __device__ __forceinline__ float ex2(float x) {
   asm("ex2.approx.ftz.f32 %0, %0;" : "+f"(x));
   return x;
 }
+// A channel's value, for both of its states.
+__device__ __forceinline__ float2 of_channel(float2 v, int j) { return f2(j & 1 ? v.y : v.x); }
+__device__ __forceinline__ float2 across(float2 a, float2 b) { return make_float2(a.x + a.y, b.x + b.y); }
 __device__ __forceinline__ float2 ex2(float2 x) { return make_float2(ex2(x.x), ex2(x.y)); }
 __device__ __forceinline__ float rcp(float x) {
   asm("rcp.approx.ftz.f32 %0, %0;" : "+f"(x));
@@ -127,7 +132,8 @@ __device__ __forceinline__ void settle(float2 (&h)[NS], const float2 (&A2)[NS], 
   const float2 share = mul2(s8, f2(-1.0f / kMost));
 #pragma unroll
   for (int q = 0; q < NS; ++q) {
-    const float2 of = make_float2(__saturatef(share.x * A2[q].x), __saturatef(share.y * A2[q].y));
+    const float by = q & 1 ? share.y : share.x;
+    const float2 of = make_float2(__saturatef(by * A2[q].x), __saturatef(by * A2[q].y));
     h[q] = fma2(mul2(of, f2(kMost * kUnits)), h[q], h[q]);
   }
 }
@@ -209,24 +215,31 @@ __device__ __forceinline__ void load_states(const float* p, int N, int n0, bool 
         if (second) Elem<float>::load4(p + N + n0 + q, b);
       }
 #pragma unroll
-      for (int i = 0; i < 4; ++i) v[q + i] = make_float2(a[i], b[i]);
+      for (int i = 0; i < 4; i += 2) {
+        v[q + i] = make_float2(a[i], a[i + 1]);
+        v[q + i + 1] = make_float2(b[i], b[i + 1]);
+      }
     }
   } else {
 #pragma unroll
-    for (int q = 0; q < NS; ++q) {
-      const bool in = n0 + q < N;
-      v[q].x = in ? p[n0 + q] : 0.0f;
-      v[q].y = in && second ? p[N + n0 + q] : 0.0f;
+    for (int q = 0; q < NS; q += 2) {
+      const bool in = n0 + q < N, in2 = n0 + q + 1 < N;
+      v[q] = make_float2(in ? p[n0 + q] : 0.0f, in2 ? p[n0 + q + 1] : 0.0f);
+      v[q + 1] = make_float2(in && second ? p[N + n0 + q] : 0.0f, in2 && second ? p[N + n0 + q + 1] : 0.0f);
     }
   }
 }
 template <int NS>
 __device__ __forceinline__ void store_states(float* p, int N, int n0, bool second, const float2 (&v)[NS]) {
 #pragma unroll
-  for (int q = 0; q < NS; ++q) {
+  for (int q = 0; q < NS; q += 2) {
     if (n0 + q < N) {
       p[n0 + q] = v[q].x;
-      if (second) p[N + n0 + q] = v[q].y;
+      if (second) p[N + n0 + q] = v[q + 1].x;
+    }
+    if (n0 + q + 1 < N) {
+      p[n0 + q + 1] = v[q].y;
+      if (second) p[N + n0 + q + 1] = v[q + 1].y;
     }
   }
 }

@@ -136,11 +136,13 @@ __device__ __forceinline__ int left_at(int lane, bool* twice) {
   }
   return at;
 }
-// v[i] <- v[i ^ order]
+// State i <- state i ^ order.
 template <int NS>
 __device__ __forceinline__ void reorder(float2 (&v)[NS], int order) {
 #pragma unroll
-  for (int n = 1; n < NS; n <<= 1) {
+  for (int i = 0; i < NS; ++i) v[i] = order & 1 ? make_float2(v[i].y, v[i].x) : v[i];
+#pragma unroll
+  for (int n = 2; n < NS; n <<= 1) {
     const bool up = order & n;
 #pragma unroll
     for (int i = 0; i < NS; ++i) {
@@ -153,11 +155,24 @@ __device__ __forceinline__ void reorder(float2 (&v)[NS], int order) {
   }
 }
 
+// A channel's value times a pair of states (plus c): as two instructions where four
+// threads' turns leave no registers for the value twice.
+template <bool kTwice>
+__device__ __forceinline__ float2 times(float a, float2 v) {
+  if constexpr (kTwice) return mul2(f2(a), v);
+  else return make_float2(a * v.x, a * v.y);
+}
+template <bool kTwice>
+__device__ __forceinline__ float2 times(float a, float2 v, float2 c) {
+  if constexpr (kTwice) return fma2(f2(a), v, c);
+  else return make_float2(fmaf(a, v.x, c.x), fmaf(a, v.y, c.y));
+}
+
 template <typename T, int NS, int P>
 __device__ void scan_back(const Args& g, int64_t work, unsigned char* smem, uint32_t t_h) {
   using S = Smem<T, NS, P>;
   constexpr int K = sums_of(NS), kLeft = K * P / 32 > 1 ? K * P / 32 : 1;   // sums over pairs
-  constexpr bool kOrdered = NS != 12;
+  constexpr bool kOrdered = NS != 12, kTwice = P < 4;
   constexpr int kCopies = copies_of(NS, P);
   constexpr int PW = 32 / P, Np = P * NS, U = kTile / P;
   constexpr int kTokens = 128 / Np, kTurns = (kTile + kTokens - 1) / kTokens;  // whose B and C are loaded at once
@@ -203,7 +218,7 @@ __device__ void scan_back(const Args& g, int64_t work, unsigned char* smem, uint
       load_twos<NS>(g.ends + ((int64_t)i * g.B * g.G + rest) * row_states + pair * 4, g, n0, e);
       const float2 s = g.sums[((int64_t)i * g.B * g.G + rest) * g.pairs + pair];
 #pragma unroll
-      for (int q = 0; q < NS; ++q) gam[q] = fma2(ex2(mul2(s, A2[q])), gam[q], e[q]);
+      for (int q = 0; q < NS; ++q) gam[q] = fma2(ex2(mul2(of_channel(s, q), A2[q])), gam[q], e[q]);
     }
   }
   if (kOrdered) {
@@ -334,8 +349,8 @@ __device__ void scan_back(const Args& g, int64_t work, unsigned char* smem, uint
     for (int k = 0; k < NS / 2; ++k) {
       const float4 v = h0[(kOrdered ? k ^ (order >> 1) : k) * 32];
       const bool swap = kOrdered && (order & 1);
-      h[2 * k] = swap ? make_float2(v.z, v.w) : make_float2(v.x, v.y);
-      h[2 * k + 1] = swap ? make_float2(v.x, v.y) : make_float2(v.z, v.w);
+      h[2 * k] = swap ? make_float2(v.y, v.x) : make_float2(v.x, v.y);
+      h[2 * k + 1] = swap ? make_float2(v.w, v.z) : make_float2(v.z, v.w);
     }
 #pragma unroll
     for (int i = 0; i < kTurns; ++i) {
@@ -386,6 +401,7 @@ __device__ void scan_back(const Args& g, int64_t work, unsigned char* smem, uint
         for (int q = 0; q < NS; q += 4) own_store(t_h + i * 2 * NS + 2 * q, h + q);
         const float4 su = psu[i * PW];
         const float2 s = make_float2(su.x, su.y), x = mul2(s, make_float2(su.z, su.w)), dy = pdy[i * PW];
+        const float sj[2] = {s.x, s.y}, xj[2] = {x.x, x.y}, dyj[2] = {dy.x, dy.y};
         const float* const rb = bc_own + i * 2 * Np;
         float2 sum[2] = {f2(0.0f), f2(0.0f)};
         float dC[K];
@@ -396,15 +412,20 @@ __device__ void scan_back(const Args& g, int64_t work, unsigned char* smem, uint
           Elem<float>::load4(rb + four, v);
           Elem<float>::load4(rb + Np + four, w);
 #pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            float2& hq = h[q + e];
-            hq = fma2(ex2(mul2(s, A2[q + e])), hq, make_float2(x.x * v[e], x.y * v[e]));
-            float2& to = sum[e & 1];
-            to = make_float2(fmaf(w[e], hq.x, to.x), fmaf(w[e], hq.y, to.y));
-            dC[q + e] = fmaf(dy.x, hq.x, dy.y * hq.y);
+          for (int e = 0; e < 4; e += 2) {
+            const float2 v2 = make_float2(v[e], v[e + 1]), w2 = make_float2(w[e], w[e + 1]);
+            float2 *const hq = h + q + e, d = f2(0.0f);
+#pragma unroll
+            for (int j = 0; j < 2; ++j) {
+              hq[j] = fma2(ex2(times<kTwice>(sj[j], A2[q + e + j])), hq[j], times<kTwice>(xj[j], v2));
+              sum[j] = fma2(w2, hq[j], sum[j]);
+              d = j ? times<kTwice>(dyj[j], hq[j], d) : times<kTwice>(dyj[j], hq[j]);
+            }
+            dC[q + e] = d.x;
+            dC[q + e + 1] = d.y;
           }
         }
-        y[k] = add2(sum[0], sum[1]);
+        y[k] = across(sum[0], sum[1]);
 #pragma unroll
         for (int q = NS; q < K; ++q) dC[q] = 0.0f;
         sum_over_pairs<K, P, kOrdered>(dC, lane);
@@ -434,6 +455,7 @@ __device__ void scan_back(const Args& g, int64_t work, unsigned char* smem, uint
         for (int q = 0; q < NS; q += 4) own_load(t_h + i * 2 * NS + 2 * q, hv + q);
         const float4 su = psu[i * PW];
         const float2 s = make_float2(su.x, su.y), x = mul2(s, make_float2(su.z, su.w)), dy = pdy[i * PW];
+        const float sj[2] = {s.x, s.y}, xj[2] = {x.x, x.y}, dyj[2] = {dy.x, dy.y};
         const float* const rb = bc_own + i * 2 * Np;
         float2 sw[2] = {f2(0.0f), f2(0.0f)}, sr[2] = {f2(0.0f), f2(0.0f)};
         float dB[K];
@@ -444,13 +466,18 @@ __device__ void scan_back(const Args& g, int64_t work, unsigned char* smem, uint
           Elem<float>::load4(rb + four, vb);
           Elem<float>::load4(rb + Np + four, vc);
 #pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            float2& gq = gam[q + e];
-            gq = make_float2(fmaf(dy.x, vc[e], gq.x), fmaf(dy.y, vc[e], gq.y));
-            dB[q + e] = fmaf(gq.x, x.x, gq.y * x.y);
-            float2& to = sw[e & 1];
-            to = make_float2(fmaf(vb[e], gq.x, to.x), fmaf(vb[e], gq.y, to.y));
-            gq = mul2(ex2(mul2(s, A2[q + e])), gq);
+          for (int e = 0; e < 4; e += 2) {
+            const float2 b2 = make_float2(vb[e], vb[e + 1]), c2 = make_float2(vc[e], vc[e + 1]);
+            float2 *const gq = gam + q + e, d = f2(0.0f);
+#pragma unroll
+            for (int j = 0; j < 2; ++j) {
+              gq[j] = times<kTwice>(dyj[j], c2, gq[j]);
+              d = j ? times<kTwice>(xj[j], gq[j], d) : times<kTwice>(xj[j], gq[j]);
+              sw[j] = fma2(b2, gq[j], sw[j]);
+              gq[j] = mul2(ex2(times<kTwice>(sj[j], A2[q + e + j])), gq[j]);
+            }
+            dB[q + e] = d.x;
+            dB[q + e + 1] = d.y;
           }
         }
         arrived<NS>(hv);
@@ -458,10 +485,10 @@ __device__ void scan_back(const Args& g, int64_t work, unsigned char* smem, uint
         for (int q = 0; q < NS; ++q) {
           const float2 qq = mul2(gam[q], hv[q]);
           sr[q & 1] = fma2(qq, A2[q], sr[q & 1]);
-          dA[q] = fma2(qq, s, dA[q]);
+          dA[q] = times<kTwice>(sj[q & 1], qq, dA[q]);
         }
-        w[k] = add2(sw[0], sw[1]);
-        r[k] = add2(sr[0], sr[1]);
+        w[k] = across(sw[0], sw[1]);
+        r[k] = across(sr[0], sr[1]);
 #pragma unroll
         for (int q = NS; q < K; ++q) dB[q] = 0.0f;
         sum_over_pairs<K, P, kOrdered>(dB, lane);

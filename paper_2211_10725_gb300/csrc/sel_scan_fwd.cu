@@ -67,7 +67,7 @@ __global__ void __launch_bounds__(32) scan_fwd(const Args g) {
           load_twos<NS>(ends + i * ends_step, g, n0, e);
           const float2 s = g.sums[((int64_t)i * g.B * g.G + rest) * g.pairs + pair];
 #pragma unroll
-          for (int q = 0; q < NS; ++q) h[q] = fma2(ex2(mul2(s, A2[q])), h[q], e[q]);
+          for (int q = 0; q < NS; ++q) h[q] = fma2(ex2(mul2(of_channel(s, q), A2[q])), h[q], e[q]);
         }
       } else if (g.state_in && has_place) {
         load_states<NS>(g.state_in + (place * g.D + c) * g.N, g.N, n0, second, h);
@@ -190,7 +190,8 @@ __global__ void __launch_bounds__(32) scan_fwd(const Args g) {
       }
       const float* const rb = bc + k * Np + n0;
       const float* const rc = bc + (kFour + k) * Np + n0;
-      float2 sum[2] = {f2(0.0f), f2(0.0f)};
+      const float2 s2[2] = {f2(sk.x), f2(sk.y)}, x2[2] = {f2(xk.x), f2(xk.y)};
+      float2 sum[2] = {f2(0.0f), f2(0.0f)};  // of a channel
 #pragma unroll
       for (int q = 0; q < NS; q += 4) {
         float v[4], w[4];
@@ -199,17 +200,14 @@ __global__ void __launch_bounds__(32) scan_fwd(const Args g) {
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
           float2& hq = h[q + e];
-          const float2 a = ex2(mul2(sk, A2[q + e]));
-          if (MODE == kBack) hq = mul2(a, make_float2(fmaf(xk.x, v[e], hq.x), fmaf(xk.y, v[e], hq.y)));
-          else hq = fma2(a, hq, make_float2(xk.x * v[e], xk.y * v[e]));
-          if (MODE == kFull) {
-            float2& to = sum[e & 1];
-            to = make_float2(fmaf(w[e], hq.x, to.x), fmaf(w[e], hq.y, to.y));
-          }
+          const float2 a = ex2(mul2(s2[e & 1], A2[q + e])), in2 = make_float2(v[e & 2], v[(e & 2) + 1]);
+          if (MODE == kBack) hq = mul2(a, fma2(x2[e & 1], in2, hq));
+          else hq = fma2(a, hq, mul2(x2[e & 1], in2));
+          if (MODE == kFull) sum[e & 1] = fma2(make_float2(w[e & 2], w[(e & 2) + 1]), hq, sum[e & 1]);
         }
       }
       s8 = add2(s8, sk);
-      if (MODE == kFull) y[k] = add2(sum[0], sum[1]);
+      if (MODE == kFull) y[k] = across(sum[0], sum[1]);
     }
     if (turn & 1) {
       settle<NS>(h, A2, s8);
