@@ -236,9 +236,9 @@ _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (
     lambda device: torch.cuda.current_stream(device).cuda_stream)
 
 
-def _stream(stream) -> Optional[int]:
-    if stream is None:
-        return _raw_stream(torch.cuda.current_device())
+def _stream(stream, device=None) -> Optional[int]:
+    if stream is None:  # the current device's (`device`, where that is known)
+        return _raw_stream(torch.cuda.current_device() if device is None else device.index)
     if isinstance(stream, int):
         return stream
     return stream.cuda_stream
@@ -740,30 +740,33 @@ def _device(where, t):
     return t.device
 
 
-def _on(where, name, t, shape, dtype, device):
+def _refuse(where, name, t, shape, dtype, device, last):
+    """Why a tensor was refused (`last`: of the layout)."""
     if t.shape != shape or t.dtype != dtype or t.device != device:
         raise ValueError(f"{where}: {name} must be a {dtype} tensor of shape {shape} on {device}")
+    raise ValueError(f"{where}: {name} must {last}")
 
+
+# The checks stand in each function, not in one of their own: a call per tensor is
+# a tenth of a small kernel's way through here.
 
 def _btc(where, name, t, shape, dtype, device):
     """The words of snn_btc for a [B, T, C] tensor (a [B, C] one for a single
     token) with contiguous C, or for None."""
     if t is None:
         return 0, 0, 0
-    _on(where, name, t, shape, dtype, device)
     st = t.stride()
-    if st[-1] != 1 and shape[-1] > 1:
-        raise ValueError(f"{where}: {name} must have a contiguous last dimension")
+    if t.shape != shape or t.dtype != dtype or t.device != device or (st[-1] != 1 and shape[-1] > 1):
+        _refuse(where, name, t, shape, dtype, device, "have a contiguous last dimension")
     return t.data_ptr(), st[0], st[-2]
 
 
 def _btgn(where, name, t, shape, dtype, device):
     """The words of snn_bthd for a [B, T, G, N] tensor (a [B, G, N] one for a single
     token) with contiguous N."""
-    _on(where, name, t, shape, dtype, device)
     st = t.stride()
-    if st[-1] != 1 and shape[-1] > 1:
-        raise ValueError(f"{where}: {name} must have a contiguous last dimension")
+    if t.shape != shape or t.dtype != dtype or t.device != device or (st[-1] != 1 and shape[-1] > 1):
+        _refuse(where, name, t, shape, dtype, device, "have a contiguous last dimension")
     return t.data_ptr(), st[0], st[1], st[-2]
 
 
@@ -771,9 +774,8 @@ def _whole(where, name, t, shape, dtype, device):
     """Pointer of a contiguous tensor, or None."""
     if t is None:
         return None
-    _on(where, name, t, shape, dtype, device)
-    if not t.is_contiguous():
-        raise ValueError(f"{where}: {name} must be contiguous")
+    if t.shape != shape or t.dtype != dtype or t.device != device or not t.is_contiguous():
+        _refuse(where, name, t, shape, dtype, device, "be contiguous")
     return t.data_ptr()
 
 
@@ -866,7 +868,7 @@ def snn_selective_scan_fwd(u, delta, A, B, C, y, ws, D=None, z=None, delta_bias=
         _whole(w, "state_in", state_in, (n, nD, N), f32, dev),
         _whole(w, "state_out", state_out, (n, nD, N), f32, dev), ps, n,
         None if ckpt is None else _whole(w, "ckpt", ckpt, ckpt.shape, f32, dev), py, pw, nw,
-        _stream(stream)), w)
+        _stream(stream, dev)), w)
 
 
 def snn_selective_scan_bwd(u, delta, A, B, C, grad_y, ckpt, grad_u, grad_delta, grad_A, grad_B, grad_C,
@@ -896,7 +898,7 @@ def snn_selective_scan_bwd(u, delta, A, B, C, grad_y, ckpt, grad_u, grad_delta, 
         flat("ckpt", ckpt, ckpt.shape), pgy, flat("grad_state_out", grad_state_out, (nB, nD, N)), pgu, pgd,
         flat("grad_A", grad_A, (nD, N)), pgB, pgC, flat("grad_D", grad_D, (nD,)), pgz,
         flat("grad_delta_bias", grad_delta_bias, (nD,)),
-        flat("grad_state_in", grad_state_in, (nB, nD, N)), pw, nw, _stream(stream)), w)
+        flat("grad_state_in", grad_state_in, (nB, nD, N)), pw, nw, _stream(stream, dev)), w)
 
 
 def snn_selective_scan_step(u, delta, A, B, C, state, y, D=None, z=None, delta_bias=None, softplus=True,
@@ -915,7 +917,7 @@ def snn_selective_scan_step(u, delta, A, B, C, state, y, D=None, z=None, delta_b
     _check(load_library().snn_selective_scan_step(
         d, pu, pd, _whole(w, "A", A, (nD, N), f32, dev), pB, pC, _whole(w, "D", D, (nD,), f32, dev), pz,
         _whole(w, "delta_bias", delta_bias, (nD,), f32, dev), _whole(w, "state", state, (n, nD, N), f32, dev),
-        _whole(w, "slots", slots, (nB,), torch.int32, dev), n, py, _stream(stream)), w)
+        _whole(w, "slots", slots, (nB,), torch.int32, dev), n, py, _stream(stream, dev)), w)
 
 
 @functools.lru_cache(maxsize=1024)
@@ -950,7 +952,7 @@ def snn_causal_conv_fwd(x, w, bias, y, act="none", seq_lens=None, state_in=None,
         d, px, _whole(f, "w", w, (C, W), torch.float32, dev), _whole(f, "bias", bias, (C,), torch.float32, dev),
         _whole(f, "seq_lens", seq_lens, (B,), torch.int32, dev),
         _whole(f, "state_in", state_in, (n, W - 1, C), dt, dev),
-        _whole(f, "state_out", state_out, (n, W - 1, C), dt, dev), ps, n, py, _stream(stream)), f)
+        _whole(f, "state_out", state_out, (n, W - 1, C), dt, dev), ps, n, py, _stream(stream, dev)), f)
 
 
 def snn_causal_conv_bwd(x, w, bias, grad_y, grad_x, grad_w, grad_bias, ws, act="none", seq_lens=None,
@@ -972,7 +974,7 @@ def snn_causal_conv_bwd(x, w, bias, grad_y, grad_x, grad_w, grad_bias, ws, act="
         _whole(f, "seq_lens", seq_lens, (B,), torch.int32, dev), state("state_in", state_in), pgy,
         state("grad_state_out", grad_state_out), pgx, f32("grad_w", grad_w, (C, W)),
         f32("grad_bias", grad_bias, (C,)), state("grad_state_in", grad_state_in), pw, nw,
-        _stream(stream)), f)
+        _stream(stream, dev)), f)
 
 
 def snn_causal_conv_step(x, w, bias, state, y, act="none", slots=None, stream=None):
@@ -987,7 +989,7 @@ def snn_causal_conv_step(x, w, bias, state, y, act="none", slots=None, stream=No
     _check(load_library().snn_causal_conv_step(
         d, px, _whole(f, "w", w, (C, W), torch.float32, dev), _whole(f, "bias", bias, (C,), torch.float32, dev),
         _whole(f, "state", state, (n, W - 1, C), dt, dev), _whole(f, "slots", slots, (B,), torch.int32, dev), n,
-        py, _stream(stream)), f)
+        py, _stream(stream, dev)), f)
 
 
 @functools.lru_cache(maxsize=1024)
@@ -1008,11 +1010,10 @@ def _matrix(where, name, t, shape, dtype, device):
     """The words of snn_rows for an [M, N] matrix with contiguous rows, or for None."""
     if t is None:
         return 0, 0
-    _on(where, name, t, shape, dtype, device)
-    ld, inner = t.stride()
-    if inner != 1 and shape[1] > 1:
-        raise ValueError(f"{where}: {name} must have contiguous rows")
-    return t.data_ptr(), ld
+    st = t.stride()
+    if t.shape != shape or t.dtype != dtype or t.device != device or (st[-1] != 1 and shape[1] > 1):
+        _refuse(where, name, t, shape, dtype, device, "have contiguous rows")
+    return t.data_ptr(), st[0]
 
 
 def snn_layer_norm_fwd(x, w, b, y, stats=None, eps=1e-5, stream=None):
@@ -1025,7 +1026,7 @@ def snn_layer_norm_fwd(x, w, b, y, stats=None, eps=1e-5, stream=None):
     keep, (px, py) = _structs(_matrix(f, "x", x, (M, N), x.dtype, dev), _matrix(f, "y", y, (M, N), y.dtype, dev))
     f32 = lambda name, t, shape: _whole(f, name, t, shape, torch.float32, dev)
     _check(load_library().snn_layer_norm_fwd(d, px, f32("w", w, (N,)), f32("b", b, (N,)), py,
-                                             f32("stats", stats, (2, M)), _stream(stream)), f)
+                                             f32("stats", stats, (2, M)), _stream(stream, dev)), f)
 
 
 def snn_layer_norm_bwd(x, w, stats, grad_y, grad_x, grad_w, grad_b, ws, stream=None):
@@ -1041,7 +1042,7 @@ def snn_layer_norm_bwd(x, w, stats, grad_y, grad_x, grad_w, grad_b, ws, stream=N
     pw, nw = _ws(f, ws, dev)
     _check(load_library().snn_layer_norm_bwd(
         d, px, f32("w", w, (N,)), f32("stats", stats, (2, M)), pgy, pgx, f32("grad_w", grad_w, (N,)),
-        f32("grad_b", grad_b, (N,)), pw, nw, _stream(stream)), f)
+        f32("grad_b", grad_b, (N,)), pw, nw, _stream(stream, dev)), f)
 
 
 # ---------------------------------------------------------------------------
