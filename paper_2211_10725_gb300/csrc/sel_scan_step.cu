@@ -6,8 +6,10 @@
 // sequences each, all on their way before the first is used.  The threads of a channel
 // share out the sequences where inputs are made ready and the outputs finished.
 //
-// 192 sequences of 5120 channels, 16 states, bf16: 21 us in a graph, 0.75 of the copy rate (one
-// sequence a thread: 35); issue is the bound there, 0.73 a clock.  One sequence of 1024 channels: 2.7 us.
+// 192 sequences of 5120 channels, 16 states, bf16: 18.5 us in a graph, 0.87 of the copy rate (one
+// sequence a thread: 35; 64-bit products for the addresses: 21); issue is near its bound there, 0.68 a
+// clock.  Four blocks an SM, or three of fp32 (without: 19.6, and fp32 28.2 for 25.8).  One
+// sequence of 1024 channels: 2.7 us.
 #include "sel_scan.cuh"
 #include "sel_scan_plan.cuh"
 
@@ -25,7 +27,7 @@ struct StepArgs {
 // V states of a thread (V = 4: N is a multiple of four), L threads of a channel; with V = 1 and L =
 // 32 a thread has two of up to 64
 template <typename T, int V, int L>
-__global__ void __launch_bounds__(kStepThreads) scan_step(const StepArgs a) {
+__global__ void __launch_bounds__(kStepThreads, sizeof(T) == 4 ? 3 : 4) scan_step(const StepArgs a) {
   const Args& g = a.g;
   constexpr int kPass = V == 1 && L == 32 ? 2 : 1, U = L < kSeqs ? kSeqs / L : 1;
   grid_dep_wait();
@@ -33,13 +35,19 @@ __global__ void __launch_bounds__(kStepThreads) scan_step(const StepArgs a) {
   const int64_t c64 = ((int64_t)blockIdx.x * kStepThreads + threadIdx.x) / L;
   const bool live = c64 < g.D;
   const int c = live ? (int)c64 : 0, grp = c / g.Dg;
-  int64_t place[kSeqs];
+  int place[kSeqs];
 #pragma unroll
   for (int j = 0; j < kSeqs; ++j) {
     place[j] = -1;
-    if (b0 + j < g.B) place[j] = g.slots ? (int64_t)g.slots[b0 + j] : (int64_t)(b0 + j);
+    if (b0 + j < g.B) place[j] = g.slots ? g.slots[b0 + j] : b0 + j;
     if (place[j] >= g.num_slots) place[j] = -1;
   }
+  // addresses by one 32-bit product, or by steps, each (a place's D N states are below 2^28)
+  const uint32_t row = (uint32_t)g.D * (uint32_t)N;
+  float* const states = a.state + (int64_t)c * N + l * V;
+  auto of_place = [&](int j) { return states + (uint64_t)(uint32_t)place[j] * row; };
+  const T* const B0 = static_cast<const T*>(g.Bm.data) + b0 * g.Bm.sb + grp * g.Bm.sg + l * V;
+  const T* const C0 = static_cast<const T*>(g.Cm.data) + b0 * g.Cm.sb + grp * g.Cm.sg + l * V;
   float h[kSeqs][kPass][V], A[kPass][V];
   Four<T> B4[kSeqs], C4[kSeqs];
   float B1[kSeqs][kPass], C1[kSeqs][kPass];
@@ -53,16 +61,15 @@ __global__ void __launch_bounds__(kStepThreads) scan_step(const StepArgs a) {
       if constexpr (V == 4) Elem<float>::load4(g.A + (int64_t)c * N + n, A[k]);
       else A[k][0] = g.A[(int64_t)c * N + n];
     }
+    const T *pb = B0 + k * L * V, *pc = C0 + k * L * V;
 #pragma unroll
-    for (int j = 0; j < kSeqs; ++j) {
+    for (int j = 0; j < kSeqs; ++j, pb += g.Bm.sb, pc += g.Cm.sb) {
 #pragma unroll
       for (int v = 0; v < V; ++v) h[j][k][v] = 0.0f;
       if constexpr (V == 4) B4[j].clear(), C4[j].clear();
       else B1[j][k] = C1[j][k] = 0.0f;
       if (in && place[j] >= 0) {
-        const float* st = a.state + (place[j] * g.D + c) * (int64_t)N + n;
-        const T* pb = static_cast<const T*>(g.Bm.data) + (b0 + j) * g.Bm.sb + grp * g.Bm.sg + n;
-        const T* pc = static_cast<const T*>(g.Cm.data) + (b0 + j) * g.Cm.sb + grp * g.Cm.sg + n;
+        const float* st = of_place(j) + k * L * V;
         if constexpr (V == 4) {
           Elem<float>::load4(st, h[j][k]);
           B4[j].load(pb, g.quads, 0);
@@ -120,7 +127,7 @@ __global__ void __launch_bounds__(kStepThreads) scan_step(const StepArgs a) {
       }
       const int n = (k * L + l) * V;
       if (live && n < N && place[j] >= 0) {
-        float* st = a.state + (place[j] * g.D + c) * (int64_t)N + n;
+        float* st = of_place(j) + k * L * V;
         if constexpr (V == 4) Elem<float>::store4(st, h[j][k]);
         else *st = h[j][k][0];
       }

@@ -157,6 +157,18 @@ def test_in_place(cuda_device):
         assert torch.equal(g2, gx) and torch.equal(x2, y)
 
 
+@pytest.mark.parametrize("M,N", [(1500, 1024), (700, 2048), (400, 8192), (700, 4095)])
+def test_in_place_with_rows_on_their_way(M, N, cuda_device):
+    c = Case(cuda_device, M, N, BF, BF)
+    y, stats, gx = torch.empty_like(c.x), torch.empty(2, M, device=cuda_device), torch.empty_like(c.x)
+    snn.snn_layer_norm_fwd(c.x, c.w, c.b, y, stats=stats, eps=EPS)
+    snn.snn_layer_norm_bwd(c.x, c.w, stats, c.gy, gx, None, None, None)
+    g2, x2 = c.gy.clone(), c.x.clone()
+    snn.snn_layer_norm_bwd(c.x, c.w, stats, g2, g2, None, None, None)
+    snn.snn_layer_norm_fwd(x2, c.w, c.b, x2, eps=EPS)
+    assert torch.equal(g2, gx) and torch.equal(x2, y)
+
+
 def test_refusals_of_the_binding(cuda_device):
     c = Case(cuda_device, 4, 32, BF, F32)
     y = torch.empty(4, 32, dtype=BF, device=cuda_device)

@@ -194,6 +194,16 @@ def test_spans(B, T, D, N, G, lens, dtype, cuda_device):
     c.check_backward()
 
 
+@pytest.mark.parametrize("T", [127, 128, 129, 255, 1030])
+@pytest.mark.parametrize("N", [5, 20, 64])
+def test_short_spans(T, N, cuda_device):
+    """Where cutting begins, spans that are no multiple of a tile, sequences that end in
+    the first, in the middle of one, at a cut and in the last."""
+    c = Case(cuda_device, 4, T, 10, N, F32, lens=[T, 16, 1, T - 3])
+    c.check_forward()
+    c.check_backward()
+
+
 def test_tokens_of_no_length(cuda_device):
     c = Case(cuda_device, 2, 0, 8, 16, F32)
     _, end = c.forward(ckpt=True)
