@@ -731,6 +731,8 @@ int64_t snn_selective_scan_ckpt_elems(const snn_sscan_desc* desc);
 /*
  * Forward over whole sequences (prompts, training).
  *   A          fp32 [D, N]; finite.  Decays are those of negative values.
+ *   delta      any value: -infinity, and any other far below zero, is a token whose s
+ *              is zero under softplus, over which the states pass unchanged
  *   Bm, Cm     [B, T, G, N], states contiguous; strides positive, of any
  *              number of elements (stride_h of snn_bthd is the groups')
  *   D          fp32 [D] or NULL (zeros)

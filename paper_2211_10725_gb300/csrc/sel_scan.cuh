@@ -97,14 +97,21 @@ __device__ __forceinline__ float2 rcp(float2 x) { return make_float2(rcp(x.x), r
 // log(1 + e) = 2 atanh(r), r = e / (2 + e) <= 1/3.  The area tangent's series r + r^3 (1/3 + q / 5 +
 // q^2 / 7 + ...), q = r^2 <= 1/9, with the bracket as the cubic that fits it there (Chebyshev): off by
 // a quarter of 2^-24.  The slope is 1 / (1 + e) or e / (1 + e).  For fp32 inputs e gets back what
-// the product |x| log2(e) was rounded by, |x| 2^-25 of it.
+// the product |x| log2(e) was rounded by, |x| 2^-25 of it.  From |x| = 128 on, where e is zero
+// (its power is flushed), |x| stays there: past 2.36e38 the product would be infinite and the rest of its
+// rounding no number, with x = -inf, whose s is zero, among them.  A NaN stays one.
+__device__ __forceinline__ float at_most_128(float x) {
+  asm("min.NaN.f32 %0, %0, %1;" : "+f"(x) : "f"(128.0f));
+  return x;
+}
 template <typename T>
 __device__ __forceinline__ float2 softplus(float2 x, float2* slope) {
   constexpr float kLog2ELow = 1.92596303e-8f, kLn2 = 0.69314718055994530942f;
-  const float2 t = make_float2(-kLog2E * fabsf(x.x), -kLog2E * fabsf(x.y));
+  float2 a = make_float2(-fabsf(x.x), -fabsf(x.y));
+  if constexpr (sizeof(T) == 4) a = make_float2(-at_most_128(fabsf(x.x)), -at_most_128(fabsf(x.y)));
+  const float2 t = mul2(a, f2(kLog2E));
   float2 e = ex2(t);
   if constexpr (sizeof(T) == 4) {
-    const float2 a = make_float2(-fabsf(x.x), -fabsf(x.y));
     const float2 rest = fma2(a, f2(kLog2ELow), fma2(a, f2(kLog2E), make_float2(-t.x, -t.y)));
     e = fma2(e, mul2(rest, f2(kLn2)), e);
   }
