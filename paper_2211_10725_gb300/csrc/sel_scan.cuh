@@ -127,6 +127,17 @@ __device__ __forceinline__ float2 softplus(float2 x, float2* slope) {
   return fma2(f2(2.0f), p, make_float2(fmaxf(x.x, 0.0f), fmaxf(x.y, 0.0f)));
 }
 
+// A state over a part of the axis that adds e to it, s the sum of the part's steps.  Large steps can
+// add up past fp32; that sum stays finite, as the infinite one times an A of zero (that of
+// a state that is absent, too) is no number.
+template <int NS>
+__device__ __forceinline__ void join(float2 (&h)[NS], const float2 (&A2)[NS], float2 s, const float2 (&e)[NS]) {
+  constexpr float kMost = 3.402823466e38f;
+  s = make_float2(fminf(fmaxf(s.x, -kMost), kMost), fminf(fmaxf(s.y, -kMost), kMost));
+#pragma unroll
+  for (int q = 0; q < NS; ++q) h[q] = fma2(ex2(mul2(of_channel(s, q), A2[q])), h[q], e[q]);
+}
+
 // The approximate power of two is low on average, by 0.1 to 0.5 units of 2^-24 for decays
 // between 0.999 and 1/2 (measured, of arguments t with all their bits: about 50 |t| up to
 // |t| = 0.0082, then 0.41), and a state that remembers a thousand tokens multiplies a thousand

@@ -225,9 +225,7 @@ __device__ void scan_back(const Args& g, int64_t work, unsigned char* smem, uint
     for (int i = g.spans * g.fine - 1; i >= (span + 1) * g.fine; --i) {
       float2 e[NS];
       load_twos<NS>(g.ends + ((int64_t)i * g.B * g.G + rest) * row_states + pair * 4, g, n0, e);
-      const float2 s = g.sums[((int64_t)i * g.B * g.G + rest) * g.pairs + pair];
-#pragma unroll
-      for (int q = 0; q < NS; ++q) gam[q] = fma2(ex2(mul2(of_channel(s, q), A2[q])), gam[q], e[q]);
+      join<NS>(gam, A2, g.sums[((int64_t)i * g.B * g.G + rest) * g.pairs + pair], e);
     }
   }
   if (kOrdered) {

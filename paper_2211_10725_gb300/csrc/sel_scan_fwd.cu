@@ -72,9 +72,7 @@ __global__ void __launch_bounds__(32) scan_fwd(const Args g) {
         for (int i = 0; i < span * g.fine; ++i) {
           float2 e[NS];
           load_twos<NS>(ends + i * ends_step, g, n0, e);
-          const float2 s = g.sums[((int64_t)i * g.B * g.G + rest) * g.pairs + pair];
-#pragma unroll
-          for (int q = 0; q < NS; ++q) h[q] = fma2(ex2(mul2(of_channel(s, q), A2[q])), h[q], e[q]);
+          join<NS>(h, A2, g.sums[((int64_t)i * g.B * g.G + rest) * g.pairs + pair], e);
         }
       } else if (g.state_in && has_place) {
         load_states<NS>(g.state_in + (place * g.D + c) * g.N, g.N, n0, second, h);

@@ -46,7 +46,7 @@ def _far_close(name, got, want, size, units, lost=0.0):
 
 
 @pytest.mark.parametrize("dtype", [F32, BF, HF])
-@pytest.mark.parametrize("T,N,pad", [(24, 16, 0), (300, 16, 1)])
+@pytest.mark.parametrize("T,N,pad", [(24, 16, 0), (300, 16, 1), (300, 5, 0), (700, 20, 0)])
 def test_far_steps(T, N, pad, dtype, cuda_device, monkeypatch):
     monkeypatch.setattr(scan_tests, "close", _far_close)
     c = _far(Case(cuda_device, 2, T, 22, N, dtype, pad=pad))
