@@ -730,7 +730,8 @@ int64_t snn_selective_scan_ckpt_elems(const snn_sscan_desc* desc);
 
 /*
  * Forward over whole sequences (prompts, training).
- *   A          fp32 [D, N]; finite.  Decays are those of negative values.
+ *   A          fp32 [D, N]; finite.  Decays are those of negative values; where s A is
+ *              positive a state grows, and is infinite where it is past fp32
  *   delta      any value: -infinity, and any other far below zero, is a token whose s
  *              is zero under softplus, over which the states pass unchanged
  *   Bm, Cm     [B, T, G, N], states contiguous; strides positive, of any

@@ -129,13 +129,20 @@ __device__ __forceinline__ float2 softplus(float2 x, float2* slope) {
 
 // A state over a part of the axis that adds e to it, s the sum of the part's steps.  Large steps can
 // add up past fp32; that sum stays finite, as the infinite one times an A of zero (that of
-// a state that is absent, too) is no number.
+// a state that is absent, too) is no number.  The power is taken as the square of its root, at most
+// 2^127: a growing state's (of a negative sum) can be past fp32 while the state is not, and
+// so zero stays zero and a state becomes infinite where its value is past fp32.  (No branch: the
+// next part's loads go past it; with one, 777 tokens of 1001 channels took 28 us for 23.)
 template <int NS>
 __device__ __forceinline__ void join(float2 (&h)[NS], const float2 (&A2)[NS], float2 s, const float2 (&e)[NS]) {
   constexpr float kMost = 3.402823466e38f;
-  s = make_float2(fminf(fmaxf(s.x, -kMost), kMost), fminf(fmaxf(s.y, -kMost), kMost));
+  s = mul2(make_float2(fminf(fmaxf(s.x, -kMost), kMost), fminf(fmaxf(s.y, -kMost), kMost)), f2(0.5f));
 #pragma unroll
-  for (int q = 0; q < NS; ++q) h[q] = fma2(ex2(mul2(of_channel(s, q), A2[q])), h[q], e[q]);
+  for (int q = 0; q < NS; ++q) {
+    const float2 t = mul2(of_channel(s, q), A2[q]);
+    const float2 root = ex2(make_float2(fminf(t.x, 127.0f), fminf(t.y, 127.0f)));
+    h[q] = fma2(root, mul2(root, h[q]), e[q]);
+  }
 }
 
 // The approximate power of two is low on average, by 0.1 to 0.5 units of 2^-24 for decays

@@ -83,3 +83,23 @@ def test_a_nan_step_stays_one(T, dtype, cuda_device):
     hit[1, 9:, 3] = True
     assert torch.equal(torch.isnan(y), hit)
     assert torch.isnan(end[1, 3]).all() and torch.isfinite(end[0]).all()
+
+
+@pytest.mark.parametrize("T,N", [(100, 8), (600, 8), (603, 5)])
+def test_growing_states(T, N, cuda_device):
+    """Negative steps, over whose spans the decays alone are past fp32 while the states are not:
+    states of zero, and small ones that grow by up to e^115 in 12 tokens near
+    the first or the last."""
+    c = Case(cuda_device, 2, T, 12, N, F32, softplus=False, bias=False)
+    for x in (c.u, c.gy):
+        x[:, :, :8] = 0
+    c.delta[:, :, :8] = 0
+    c.state[:, :4] = c.gs[:, :4] = 0
+    c.delta[:, :, :4] = -0.6
+    c.state[:, 4:8] = c.gs[:, 4:8] = 1e-30
+    c.delta[:, 2:14, 4:6] = -1.2
+    c.delta[:, T - 14:T - 2, 6:8] = -1.2
+    c.A[:, :] = -torch.arange(1, N + 1, device=cuda_device)
+    c.check_forward()
+    for name, x in c.check_backward().items():
+        assert x is None or torch.isfinite(x).all(), name
