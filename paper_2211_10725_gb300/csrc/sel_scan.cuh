@@ -35,6 +35,7 @@ namespace sscan {
 
 constexpr int kMaxN = 64;
 constexpr int kTile = 8;          // tokens between checkpoints
+constexpr int kSettle = 16;       // tokens between settle()s, whole tiles
 constexpr float kLog2E = 1.44269504088896340736f;
 
 struct Seq {  // [B, T, channels]
@@ -92,6 +93,11 @@ __device__ __forceinline__ float rcp(float x) {
   return x;
 }
 __device__ __forceinline__ float2 rcp(float2 x) { return make_float2(rcp(x.x), rcp(x.y)); }
+__device__ __forceinline__ float2 root(float2 x) {
+  asm("sqrt.approx.ftz.f32 %0, %0;" : "+f"(x.x));
+  asm("sqrt.approx.ftz.f32 %0, %0;" : "+f"(x.y));
+  return x;
+}
 
 // softplus and its slope.  With e = e^-|x|: log(1 + e^x) = max(x, 0) + log(1 + e), and
 // log(1 + e) = 2 atanh(r), r = e / (2 + e) <= 1/3.  The area tangent's series r + r^3 (1/3 + q / 5 +
@@ -145,21 +151,36 @@ __device__ __forceinline__ void join(float2 (&h)[NS], const float2 (&A2)[NS], fl
   }
 }
 
-// The approximate power of two is low on average, by 0.1 to 0.5 units of 2^-24 for decays
-// between 0.999 and 1/2 (measured, of arguments t with all their bits: about 50 |t| up to
-// |t| = 0.0082, then 0.41), and a state that remembers a thousand tokens multiplies a thousand
-// of them.  Eight tokens' worth of it goes back into the states after every eight, from
-// the sum of their s (2-norms of errors: states of 100 tokens 4e-7, 19e-7 without; grad_A of
-// 4096 tokens 6e-7, 18e-7 without).
+// The approximate power of two of an argument t below zero is low on average (measured, of arguments with
+// all their bits): by 0.11 units of 2^-24 up to |t| = 0.002, by 0.4 from 0.008 to 1/2.  A state
+// that remembers a thousand tokens multiplies a thousand of them.  The 0.11 units are a larger t
+// (one of zero still gives exactly one); what is left, about 0.33 min(|t| / 0.0082, 1)^2 units, goes back
+// into the states for kSettle tokens at a time: 0.33 min((|A| / 0.0082)^2 sum s^2, n) units, n = (sum s)^2 / sum s^2
+// the number of tokens that the sum consists of: all of equal steps, one where one step stands
+// among steps near zero.
+constexpr float kLift = 0.11f / 16777216.0f / 0.69314718055994530942f;
+struct alignas(16) Steps {
+  float2 sum = {0.0f, 0.0f}, squares = {0.0f, 0.0f};
+  __device__ __forceinline__ void add(float2 s) {
+    sum = add2(sum, s);
+    squares = fma2(s, s, squares);
+  }
+  __device__ __forceinline__ void add(const Steps& o) {
+    sum = add2(sum, o.sum);
+    squares = add2(squares, o.squares);
+  }
+};
 template <int NS>
-__device__ __forceinline__ void settle(float2 (&h)[NS], const float2 (&A2)[NS], float2 s8) {
-  constexpr float kMost = 8.0f * 0.0082f, kUnits = 50.0f / 16777216.0f;
-  const float2 share = mul2(s8, f2(-1.0f / kMost));
+__device__ __forceinline__ void settle(float2 (&h)[NS], const float2 (&A2)[NS], const Steps& s) {
+  constexpr float kMost = kSettle, kCap = 0.0082f, kUnits = 0.33f / 16777216.0f;
+  // (n of no steps, and of steps past fp32, is no number: kMost)
+  const float2 n = mul2(mul2(s.sum, s.sum), rcp(s.squares)), by = root(mul2(s.squares, f2(kUnits / (kCap * kCap))));
+  const float2 most = mul2(make_float2(fminf(n.x, kMost), fminf(n.y, kMost)), f2(kUnits));
 #pragma unroll
   for (int q = 0; q < NS; ++q) {
-    const float by = q & 1 ? share.y : share.x;
-    const float2 of = make_float2(__saturatef(by * A2[q].x), __saturatef(by * A2[q].y));
-    h[q] = fma2(mul2(of, f2(kMost * kUnits)), h[q], h[q]);
+    const float2 of = mul2(A2[q], of_channel(by, q)), part = mul2(of, of);
+    const float cap = q & 1 ? most.y : most.x;
+    h[q] = fma2(make_float2(fminf(part.x, cap), fminf(part.y, cap)), h[q], h[q]);
   }
 }
 

@@ -23,8 +23,14 @@ enum Mode {
 
 constexpr int kFour = 4;  // tokens
 
+// Blocks of an SM that the registers are held to (0: as they come).  Without: 128 and 91 registers for 96 and 80, and
+// the gradient's ends of 2 x 4096 tokens of 4096 channels 142 us for 136 (16 states), 123 for 98 (8); 32-bit inputs
+// have no room for it (backward 879 us for 825).
 template <typename T, int MODE, int NS, int P>
-__global__ void __launch_bounds__(32) scan_fwd(const Args g) {
+constexpr int kBlocks = MODE == kBack && P == 2 && sizeof(T) == 2 ? (NS == 4 ? 24 : NS == 8 ? 20 : 0) : 0;
+
+template <typename T, int MODE, int NS, int P>
+__global__ void __launch_bounds__(32, kBlocks<T, MODE, NS, P>) scan_fwd(const Args g) {
   constexpr int PW = 32 / P, Np = P * NS, U = kFour / P;  // a thread's own tokens of four
   constexpr int kJobs = (MODE == kFull ? 2 : 1) * Np, kTurns = (kJobs + 31) / 32;  // fours of states to load
   __shared__ __align__(16) float smem[2][kJobs * 4];      // [B, C][kFour][Np]
@@ -147,7 +153,7 @@ __global__ void __launch_bounds__(32) scan_fwd(const Args g) {
     fetch(start);
     fetch_bc(start);
   }
-  float2 s8 = f2(0.0f);  // sum of s since the states were settled
+  Steps s8;  // since the states were settled
   // whole: all the tokens exist, in pairs
   auto tokens = [&](int turn, auto whole_) {
     constexpr bool whole = decltype(whole_)::value;
@@ -205,19 +211,19 @@ __global__ void __launch_bounds__(32) scan_fwd(const Args g) {
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
           float2& hq = h[q + e];
-          const float2 a = ex2(mul2(s2[e & 1], A2[q + e])), in2 = make_float2(v[e & 2], v[(e & 2) + 1]);
+          const float2 a = ex2(fma2(s2[e & 1], A2[q + e], f2(kLift))), in2 = make_float2(v[e & 2], v[(e & 2) + 1]);
           if (MODE == kBack) hq = mul2(a, fma2(x2[e & 1], in2, hq));
           else hq = fma2(a, hq, mul2(x2[e & 1], in2));
           if (MODE == kFull) sum[e & 1] = fma2(make_float2(w[e & 2], w[(e & 2) + 1]), hq, sum[e & 1]);
         }
       }
-      s8 = add2(s8, sk);
+      s8.add(sk);
       if (MODE == kFull) y[k] = across(sum[0], sum[1]);
     }
-    if (turn & 1) {
+    if (turn % (kSettle / kFour) == kSettle / kFour - 1) {
       settle<NS>(h, A2, s8);
-      if (MODE != kFull) total = add2(total, s8);
-      s8 = f2(0.0f);
+      if (MODE != kFull) total = add2(total, s8.sum);
+      s8 = Steps();
     }
     if (MODE == kFull) {
       share_out<kFour, P>(y, pl);
@@ -254,7 +260,7 @@ __global__ void __launch_bounds__(32) scan_fwd(const Args g) {
       store_states<NS>(g.state_out + (place * g.D + c) * g.N, g.N, n0, second, h);
   } else {
     store_twos<NS>(ends + span * ends_step, g, n0, h);
-    total = add2(total, s8);
+    total = add2(total, s8.sum);
     if (pl == 0) g.sums[((int64_t)span * g.B * g.G + rest) * g.pairs + pair] = total;
   }
 }

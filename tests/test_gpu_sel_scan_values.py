@@ -103,3 +103,90 @@ def test_growing_states(T, N, cuda_device):
     c.check_forward()
     for name, x in c.check_backward().items():
         assert x is None or torch.isfinite(x).all(), name
+
+
+# Long memories.  A state that remembers m tokens (|s A| = 1 / m) is a product of m rounded
+# decays.  A decay errs by 0.6 units of 2^-24 (root mean square; a rounding to fp32 between 1/2 and
+# 1 alone by 0.29 to 0.58), the addition to the state by 0.42, independently from token to
+# token where the steps differ: 0.73 sqrt(m / 2) of the state, 8.7 units for the longest memory
+# here, m = 286.  What is left of the approximate power's bias after its correction adds
+# at most 15 units where steps differ most, and 2 where they are alike: their root of squares is
+# below 20 units, which is a state's tolerance in the 2-norm over channels (no
+# correction: 51 units for steps alike; one from the sum of eight unequal steps: 45).  A gradient that is a sum of
+# products of two such states: sqrt(2) of that, 28, and for its own additions in order, 0.2 sqrt(terms) units for
+# random signs, up to 10: 30.  That of A is a sum over sequences whose own sums have random signs too, so that
+# what it is off by is measured on the square root of the sum of their squares.  Of only two channels it
+# is the 2-norm of two normal numbers, above sqrt(x) of what is expected with a chance of e^-x: sqrt(7.4) = 2.7 for
+# one in a hundred among 16 states.
+UNIT = 2.0 ** -24
+
+
+def _memories(dev, B, T, D, kind):
+    """A case with |s A| of 0.0035 to 0.056 on average: steps alike (spread by 30%), or one in eight
+    of eight times that among steps near zero, or one of each eight among steps of zero."""
+    c = Case(dev, B, T, D, 16, F32, gate=False, softplus=False, bias=False)
+    g = torch.Generator().manual_seed(17)
+    n = torch.randn(B, T, D, generator=g)
+    s = 0.056 * torch.exp(0.3 * n - 0.045)
+    if kind == "sparse":
+        s = s * torch.where(torch.rand(B, T, D, generator=g) < 1 / 8, 8.0, 1e-3)
+    if kind == "single":
+        s = 8 * s * (torch.arange(T) % 8 == torch.randint(0, 8, (B, T // 8, 1), generator=g).repeat_interleave(8, 1)[..., 0])[..., None]
+    c.delta.copy_(s)
+    c.A.copy_(-(torch.arange(1, 17) / 16.0).expand(D, 16) * torch.exp(0.02 * torch.randn(D, 16, generator=g)))
+    c.kw["delta_bias"] = None
+    return c
+
+
+def _definition(c):
+    """y, the last state and the gradients in 64 bits (G = 1, no gate, steps as they are)."""
+    d = lambda x: x.double()
+    u, s, A, Bm, Cm, gy, skip = map(d, (c.u, c.delta, c.A, c.Bm[:, :, 0], c.Cm[:, :, 0], c.gy, c.D_skip))
+    h, hs, y = d(c.state), [d(c.state)], torch.empty_like(u)
+    for t in range(c.T):
+        h = torch.exp(s[:, t, :, None] * A) * h + (s[:, t] * u[:, t])[..., None] * Bm[:, t, None]
+        y[:, t] = (h * Cm[:, t, None]).sum(-1) + skip * u[:, t]
+        hs.append(h)
+    g, o = d(c.gs), {k: torch.zeros_like(v) for k, v in (("u", u), ("delta", s), ("B", Bm), ("C", Cm), ("A", h))}
+    for t in range(c.T - 1, -1, -1):
+        a = torch.exp(s[:, t, :, None] * A)
+        o["C"][:, t] = (gy[:, t, :, None] * hs[t + 1]).sum(1)
+        g = g + gy[:, t, :, None] * Cm[:, t, None]
+        o["B"][:, t] = (g * (s[:, t] * u[:, t])[..., None]).sum(1)
+        w, q = (g * Bm[:, t, None]).sum(-1), a * g * hs[t]
+        o["A"] += q * s[:, t, :, None]
+        o["u"][:, t] = s[:, t] * w + skip * gy[:, t]
+        o["delta"][:, t] = u[:, t] * w + (q * A).sum(-1)
+        g = a * g
+    o["state"] = g
+    return y, h, o
+
+
+def _off(got, want, dims=None):
+    """Units of 2^-24 of the 2-norm that a result is off by (dims: of each of its other places)."""
+    e = (got.double() - want).square()
+    if dims is None:
+        return float((e.sum() / want.square().sum()).sqrt()) / UNIT
+    return float((e.sum(dims) / want.square().sum(dims)).sqrt().max()) / UNIT
+
+
+def _sum_off(got, parts):
+    """The same of a sum over sequences, on their 2-norm."""
+    e = (got.double() - parts.sum(0)).square().sum(0)
+    return float((e / parts.square().sum((0, 1))).sqrt().max()) / UNIT
+
+
+# a cut axis, and sequences enough for whole ones
+@pytest.mark.parametrize("B,T,D", [(2, 4096, 64), (1300, 1024, 2)])
+@pytest.mark.parametrize("kind", ["alike", "sparse", "single"])
+def test_long_memories(B, T, D, kind, cuda_device):
+    c = _memories(cuda_device, B, T, D, kind)
+    y, end = c.forward(ckpt=True)
+    got = c.backward()
+    want_y, want_end, want = _definition(c)
+    off = {"y": _off(y, want_y), "end": _off(end, want_end, (0, 1)), "state": _off(got["state"], want["state"], (0, 1)),
+           "A": _sum_off(got["A"], want["A"]) / (1.5 * (2.7 if D == 2 else 1.0)), "B": _off(got["B"][:, :, 0], want["B"]),
+           "C": _off(got["C"][:, :, 0], want["C"])}
+    for name in ("u", "delta"):
+        off[name] = _off(got[name], want[name]) / 1.5
+    assert max(off.values()) < 20, off
