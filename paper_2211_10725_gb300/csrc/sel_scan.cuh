@@ -36,7 +36,7 @@ namespace sscan {
 constexpr int kMaxN = 64;
 constexpr int kTile = 8;          // tokens between checkpoints
 constexpr int kSettle = 16;       // tokens between settle()s, whole tiles
-constexpr float kLog2E = 1.44269504088896340736f;
+constexpr float kLog2E = 1.44269504088896340736f, kLn2 = 0.69314718055994530942f;
 
 struct Seq {  // [B, T, channels]
   void* data = nullptr;
@@ -112,7 +112,7 @@ __device__ __forceinline__ float at_most_128(float x) {
 }
 template <typename T>
 __device__ __forceinline__ float2 softplus(float2 x, float2* slope) {
-  constexpr float kLog2ELow = 1.92596303e-8f, kLn2 = 0.69314718055994530942f;
+  constexpr float kLog2ELow = 1.92596303e-8f;
   float2 a = make_float2(-fabsf(x.x), -fabsf(x.y));
   if constexpr (sizeof(T) == 4) a = make_float2(-at_most_128(fabsf(x.x)), -at_most_128(fabsf(x.y)));
   const float2 t = mul2(a, f2(kLog2E));
@@ -158,7 +158,7 @@ __device__ __forceinline__ void join(float2 (&h)[NS], const float2 (&A2)[NS], fl
 // into the states for kSettle tokens at a time: 0.33 min((|A| / 0.0082)^2 sum s^2, n) units, n = (sum s)^2 / sum s^2
 // the number of tokens that the sum consists of: all of equal steps, one where one step stands
 // among steps near zero.
-constexpr float kLift = 0.11f / 16777216.0f / 0.69314718055994530942f;
+constexpr float kLift = 0.11f / 16777216.0f / kLn2, kCap = 0.0082f, kUnits = 0.33f / 16777216.0f;
 struct alignas(16) Steps {
   float2 sum = {0.0f, 0.0f}, squares = {0.0f, 0.0f};
   __device__ __forceinline__ void add(float2 s) {
@@ -172,7 +172,7 @@ struct alignas(16) Steps {
 };
 template <int NS>
 __device__ __forceinline__ void settle(float2 (&h)[NS], const float2 (&A2)[NS], const Steps& s) {
-  constexpr float kMost = kSettle, kCap = 0.0082f, kUnits = 0.33f / 16777216.0f;
+  constexpr float kMost = kSettle;
   // (n of no steps, and of steps past fp32, is no number: kMost)
   const float2 n = mul2(mul2(s.sum, s.sum), rcp(s.squares)), by = root(mul2(s.squares, f2(kUnits / (kCap * kCap))));
   const float2 most = mul2(make_float2(fminf(n.x, kMost), fminf(n.y, kMost)), f2(kUnits));

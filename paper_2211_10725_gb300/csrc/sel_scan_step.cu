@@ -24,6 +24,14 @@ struct StepArgs {
   float* state;
 };
 
+// Decays of a single token, s with log2(e): what the approximate power lacks (sel_scan.cuh) is all
+// in its argument, as no settle() follows.
+__device__ __forceinline__ float2 decay(float2 s, float2 A) {
+  const float2 t = fma2(s, A, f2(kLift));
+  const float2 part = make_float2(__saturatef(t.x * (-1.0f / kCap)), __saturatef(t.y * (-1.0f / kCap)));
+  return ex2(fma2(mul2(part, part), f2(kUnits / kLn2), t));
+}
+
 // V states of a thread (V = 4: N is a multiple of four), L threads of a channel; with V = 1 and L =
 // 32 a thread has two of up to 64
 template <typename T, int V, int L>
@@ -120,10 +128,19 @@ __global__ void __launch_bounds__(kStepThreads, sizeof(T) == 4 ? 3 : 4) scan_ste
       } else {
         B[0] = B1[j][k], C[0] = C1[j][k];
       }
+      if constexpr (V == 4) {
 #pragma unroll
-      for (int v = 0; v < V; ++v) {
-        h[j][k][v] = fmaf(ex2(sj * A[k][v]), h[j][k][v], xj * B[v]);
-        y[j] = fmaf(C[v], h[j][k][v], y[j]);
+        for (int v = 0; v < V; v += 2) {
+          const float2 a = decay(f2(sj), make_float2(A[k][v], A[k][v + 1]));
+          const float2 now = fma2(a, make_float2(h[j][k][v], h[j][k][v + 1]), mul2(f2(xj), make_float2(B[v], B[v + 1])));
+          h[j][k][v] = now.x;
+          h[j][k][v + 1] = now.y;
+          y[j] = fmaf(C[v], now.x, y[j]);
+          y[j] = fmaf(C[v + 1], now.y, y[j]);
+        }
+      } else {
+        h[j][k][0] = fmaf(decay(f2(sj), f2(A[k][0])).x, h[j][k][0], xj * B[0]);
+        y[j] = fmaf(C[0], h[j][k][0], y[j]);
       }
       const int n = (k * L + l) * V;
       if (live && n < N && place[j] >= 0) {

@@ -190,3 +190,24 @@ def test_long_memories(B, T, D, kind, cuda_device):
     for name in ("u", "delta"):
         off[name] = _off(got[name], want[name]) / 1.5
     assert max(off.values()) < 20, off
+
+
+@pytest.mark.parametrize("N", [16, 7])
+@pytest.mark.parametrize("kind", ["alike", "single"])
+def test_long_memories_of_single_tokens(kind, N, cuda_device):
+    """700 tokens one by one, as far from the definition as a sequence may be."""
+    c = _memories(cuda_device, 4, 704, 64, kind)
+    c.A, c.state = c.A[:, :N].contiguous(), c.state[..., :N].contiguous()
+    c.Bm, c.Cm = c.Bm[..., :N], c.Cm[..., :N]   # (of rows of 16: every token's start on 16 bytes)
+    pool, y = c.state.clone(), c.new(c.u)
+    h, want = c.state.double(), torch.empty_like(c.u, dtype=torch.float64)
+    d = lambda x, t: x[:, t].double()
+    for t in range(c.T):
+        one = lambda x: x[:, t]
+        snn.snn_selective_scan_step(one(c.u), one(c.delta), c.A, one(c.Bm), one(c.Cm), pool, y[:, t], D=c.D_skip,
+                                    softplus=False)
+        h = torch.exp(d(c.delta, t)[..., None] * c.A.double()) * h \
+            + (d(c.delta, t) * d(c.u, t))[..., None] * d(c.Bm, t)
+        want[:, t] = (h * d(c.Cm, t)).sum(-1) + c.D_skip.double() * d(c.u, t)
+    off = {"y": _off(y, want), "pool": _off(pool, h, (0, 1))}
+    assert max(off.values()) < 20, off
