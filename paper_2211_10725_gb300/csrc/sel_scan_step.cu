@@ -24,7 +24,7 @@ struct StepArgs {
   float* state;
 };
 
-// Decays of a single token, s with log2(e): what the approximate power lacks (sel_scan.cuh) is all
+// Decays of a single token, A with log2(e) (a large step with it would be past fp32): what the approximate power lacks (sel_scan.cuh) is all
 // in its argument, as no settle() follows.
 __device__ __forceinline__ float2 decay(float2 s, float2 A) {
   const float2 t = fma2(s, A, f2(kLift));
@@ -68,6 +68,8 @@ __global__ void __launch_bounds__(kStepThreads, sizeof(T) == 4 ? 3 : 4) scan_ste
     if (in) {
       if constexpr (V == 4) Elem<float>::load4(g.A + (int64_t)c * N + n, A[k]);
       else A[k][0] = g.A[(int64_t)c * N + n];
+#pragma unroll
+      for (int v = 0; v < V; ++v) A[k][v] *= kLog2E;
     }
     const T *pb = B0 + k * L * V, *pc = C0 + k * L * V;
 #pragma unroll
@@ -117,7 +119,6 @@ __global__ void __launch_bounds__(kStepThreads, sizeof(T) == 4 ? 3 : 4) scan_ste
       sj = __shfl_sync(0xffffffffu, sj, from);
       xj = __shfl_sync(0xffffffffu, xj, from);
     }
-    sj *= kLog2E;
     y[j] = 0.0f;
 #pragma unroll
     for (int k = 0; k < kPass; ++k) {

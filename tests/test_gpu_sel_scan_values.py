@@ -211,3 +211,22 @@ def test_long_memories_of_single_tokens(kind, N, cuda_device):
         want[:, t] = (h * d(c.Cm, t)).sum(-1) + c.D_skip.double() * d(c.u, t)
     off = {"y": _off(y, want), "pool": _off(pool, h, (0, 1))}
     assert max(off.values()) < 20, off
+
+
+@pytest.mark.parametrize("dtype", [F32, BF])
+@pytest.mark.parametrize("N", [16, 20, 6, 50])
+def test_the_largest_steps_of_single_tokens(N, dtype, cuda_device):
+    """A step near the largest number forgets all: with log2(e) it is past fp32, and no state,
+    absent ones among them, may become infinity times zero."""
+    c = Case(cuda_device, 2, 1, 24, N, dtype, bias=False)
+    c.delta[:] = 3e38
+    c.u[:] *= 1e-38
+    pool = c.state.clone()
+    one = lambda x: x[:, 0]
+    y = c.new(c.u)[:, 0]
+    snn.snn_selective_scan_step(one(c.u), one(c.delta), c.A, one(c.Bm), one(c.Cm), pool, y, D=c.D_skip, z=one(c.z))
+    args, kw = c.oracle_args()
+    want, h = O.scan_forward(*args, **kw)
+    size, hs = O.scan_forward(*args, positive=True, **kw)
+    close("y", y, want[:, 0], size[:, 0], 160 + N)
+    close("pool", pool, h, hs, 80)
