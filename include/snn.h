@@ -858,7 +858,8 @@ snn_status_t snn_causal_conv_bwd(const snn_conv_desc* desc, const snn_btc* x, co
                                  snn_stream_t stream);
 
 /* One token for each of B sequences (decoding, desc->T = 1): state [num_slots, W-1, C] of
- * dtype loses its oldest input and takes x; slots as in snn_selective_scan_step. */
+ * dtype loses its oldest input and takes x; slots as in snn_selective_scan_step.  y may be x
+ * itself (the same rows). */
 snn_status_t snn_causal_conv_step(const snn_conv_desc* desc, const snn_btc* x, const float* w,
                                   const float* bias, void* state, const int32_t* slots,
                                   int64_t num_slots, const snn_btc* y, snn_stream_t stream);

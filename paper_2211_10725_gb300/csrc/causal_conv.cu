@@ -276,10 +276,8 @@ __global__ void __launch_bounds__(kThreads, sizeof(T) == 4 ? 2 : 3) conv_fwd(con
     py += kAhead * g.y.st;
   };
   fetch(t0);
-  int t = t0;
-  for (; t + kAhead <= stop; t += kAhead) tokens(t, std::true_type());
-  for (; t < t1; t += kAhead) tokens(t, std::false_type());
-  // the last W - 1 inputs; in ascending order, as state_out may be state_in
+  // the last W - 1 inputs; in ascending order, as state_out may be state_in, and before y,
+  // which a step's x may be
   if (r == 0 && g.state_out && at.has_place()) {
 #pragma unroll
     for (int j = 0; j < W - 1; ++j) {
@@ -288,6 +286,9 @@ __global__ void __launch_bounds__(kThreads, sizeof(T) == 4 ? 2 : 3) conv_fwd(con
       v.store(static_cast<T*>(g.state_out) + at.state_at(at.place, j));
     }
   }
+  int t = t0;
+  for (; t + kAhead <= stop; t += kAhead) tokens(t, std::true_type());
+  for (; t < t1; t += kAhead) tokens(t, std::false_type());
 }
 
 template <typename T, int V, int W>

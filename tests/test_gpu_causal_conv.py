@@ -178,3 +178,20 @@ def test_refusals_of_the_binding(cuda_device):
             snn.snn_causal_conv_fwd(**kw)
     with pytest.raises(snn.SnnError):
         snn.snn_causal_conv_fwd(c.x, c.w, c.bias, y, act="sigmoid")
+
+
+@pytest.mark.parametrize("dtype", [F32, BF, HF])
+@pytest.mark.parametrize("W", [2, 3, 4])
+@pytest.mark.parametrize("B,C", [(5, 40), (3, 33)])
+def test_steps_over_their_input(B, C, W, dtype, cuda_device):
+    """y may be x itself: the state takes the inputs, as with a y of its own."""
+    c = Case(cuda_device, B, 1, C, W, dtype)
+    slots = torch.tensor([B - b for b in range(B - 1)] + [-1], dtype=torch.int32, device=cuda_device)
+    pools = [torch.randn(B + 2, W - 1, C, device=cuda_device).to(dtype)]
+    pools.append(pools[0].clone())
+    y, x = c.new(c.x), c.x.clone()
+    for t in range(W + 1):
+        snn.snn_causal_conv_step(c.x[:, 0], c.w, c.bias, pools[0], y[:, 0], act="silu", slots=slots)
+        snn.snn_causal_conv_step(x[:, 0], c.w, c.bias, pools[1], x[:, 0], act="silu", slots=slots)
+        assert torch.equal(x, y) and torch.equal(*pools)
+        c.x.copy_(y)
