@@ -230,3 +230,26 @@ def test_the_largest_steps_of_single_tokens(N, dtype, cuda_device):
     size, hs = O.scan_forward(*args, positive=True, **kw)
     close("y", y, want[:, 0], size[:, 0], 160 + N)
     close("pool", pool, h, hs, 80)
+
+
+def test_two_backward_passes_at_once(cuda_device):
+    """On streams of their own, each with its tensor memory (of two sizes) on the same SMs."""
+    cases = [Case(cuda_device, 2, 2000, 256, N, BF, seed=N) for N in (16, 64)]
+    want = []
+    for c in cases:
+        c.forward(ckpt=True)
+        want.append(c.backward())
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in cases]
+    got = [[], []]
+    for i in range(3):
+        for c, s, g in zip(cases, streams, got):
+            if i == 0:
+                s.wait_stream(torch.cuda.current_stream())
+            with torch.cuda.stream(s):
+                g.append(c.backward())
+    torch.cuda.synchronize()
+    for w, g in zip(want, got):
+        for x in g:
+            for name in w:
+                assert torch.equal(w[name], x[name]), name
