@@ -12,10 +12,10 @@
 // gradients gather in registers over a run, in shared memory over the runs of a
 // block, and a second kernel adds the blocks in their order (no atomics).
 //
-// 2 x 4096 tokens of 4096 channels, width 4, silu, bf16: forward 32 us (4.2 TB/s), backward
-// 57 (3.5) and 6 for the sums; issue at 0.45 and 0.5 a clock, the rest the latency of the loads at 20 and 14 warps
+// 2 x 4096 tokens of 4096 channels, width 4, silu, bf16: forward 30 us (4.5 TB/s), backward
+// 57 (3.5) and 6 for the sums; issue at 0.48 and 0.49 a clock, the rest the latency of the loads at 20 and 14 warps
 // an SM (one channel's runs of 16 tokens first: 242 us for the three; channels in pairs,
-// longer runs: 156; whole fours of tokens without checks: 92).  Eight channels a thread, two or eight tokens ahead
+// longer runs: 156; whole fours of tokens without checks: 92; the state read before the tokens: 91).  Eight channels a thread, two or eight tokens ahead
 // and other block counts were no faster.  4095 channels, element by element: 163 for 92.
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
@@ -617,7 +617,7 @@ size_t snn_conv_desc_size(void) { return sizeof(snn_conv_desc); }
 
 size_t snn_causal_conv_workspace_bytes(const snn_conv_desc* desc) {
   if (check_desc(desc) != SNN_OK) return 0;
-  // the element path has at most as many rows of partials as the vector path has, or more: the larger
+  // rows of partials of the element path and of the vector path: the larger
   const BwdPlan p = bwd_plan(desc->B, desc->T, desc->C);
   const int64_t a = bwd_rows(p, desc->B, desc->C), v = bwd_rows(p, desc->B, snn::ceil_div(desc->C, kV));
   const size_t b = (size_t)(a > v ? a : v) * (size_t)desc->C * (size_t)(desc->W + 1) * sizeof(float);

@@ -13,10 +13,10 @@
 // tokens pass, halving the values a thread holds with every exchange; the warps' shares, and
 // those of grad_A, grad_D and grad_delta_bias, are added by further kernels in a fixed order.
 //
-// 2 x 4096 tokens of 4096 channels, 16 states, bf16: 555 us, the gradient's ends of the spans
-// 137 before it, the sums 25 and 7 after it.  The formulas are 15 operations and two
+// 2 x 4096 tokens of 4096 channels, 16 states, bf16: 552 us, the gradient's ends of the spans
+// 140 before it, the sums 25 and 6 after it.  The formulas are 15 operations and two
 // powers of two a state, 200 us at the rate of fp32; a thread issues 24 instructions for each
-// state, 0.58 a clock and scheduler, and what keeps it there is the latency of dependent
+// state, 0.59 a clock and scheduler, and what keeps it there is the latency of dependent
 // instructions at three warps a scheduler (168 registers; a fourth warp at 128: 661 us, the token loops
 // unrolled by two: 640).  Tiles of a whole block between barriers took 2752, warps that
 // work alone with four states to a thread and the sums through shared memory 879, eight states
@@ -351,7 +351,8 @@ __device__ void scan_back(const Args& g, int64_t work, unsigned char* smem, uint
   const int first_four = order >> 2;
 
   // gamma, after kSettleTiles tiles: of 16-bit inputs at the end of the last of them, of 32-bit ones
-  // at the start of the next (2 x 4096 tokens of 4096 channels: bf16 721 us, fp32 825 and 807)
+  // at the start of the next (2 x 4096 tokens of 4096 channels, 16 states: fp32 807 us, 825 at the end; bf16 of 24 states
+  // 575 at the end and 589)
   auto settle_all = [&]() {
     Steps all;
 #pragma unroll

@@ -3,8 +3,8 @@
 // four come to its shared memory, the tokens' inputs to the registers of the pairs'
 // threads, each while the four before are worked on.
 //
-// 2 x 4096 tokens of 4096 channels, 16 states, bf16 with checkpoints: 189 us, the spans' ends 131
-// before it; a prompt of 16384 tokens of 2048 channels 294 for both.  A state of a token is four fp32
+// 2 x 4096 tokens of 4096 channels, 16 states, bf16 with checkpoints: 187 us, the spans' ends 129
+// before it; a prompt of 16384 tokens of 2048 channels 296 for both.  A state of a token is four fp32
 // operations and a power of two, 53 us in either unit; a cut axis needs the powers twice.  A thread issues
 // eight instructions for each state, 0.61 a clock and scheduler at four warps:
 // bound by the latency of dependent instructions and the two units in turn.  (Registers capped for 18, 20 or
@@ -23,11 +23,10 @@ enum Mode {
 
 constexpr int kFour = 4;  // tokens
 
-// Blocks of an SM that the registers are held to (0: as they come).  Without: 128 and 91 registers for 96 and 80, and
-// the gradient's ends of 2 x 4096 tokens of 4096 channels 142 us for 136 (16 states), 123 for 98 (8); 32-bit inputs
-// have no room for it (backward 879 us for 825).
+// Blocks of an SM that the registers are held to (0: as they come): without, the gradient's ends take 91
+// for 80 with 8 states, 123 us for 101 at 2 x 4096 tokens of 4096 channels.
 template <typename T, int MODE, int NS, int P>
-constexpr int kBlocks = MODE == kBack && P == 2 && sizeof(T) == 2 ? (NS == 4 ? 24 : NS == 8 ? 20 : 0) : 0;
+constexpr int kBlocks = MODE == kBack && P == 2 && sizeof(T) == 2 ? (NS == 4 ? 24 : 0) : 0;
 
 template <typename T, int MODE, int NS, int P>
 __global__ void __launch_bounds__(32, kBlocks<T, MODE, NS, P>) scan_fwd(const Args g) {

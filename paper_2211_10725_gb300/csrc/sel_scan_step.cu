@@ -6,10 +6,11 @@
 // sequences each, all on their way before the first is used.  The threads of a channel
 // share out the sequences where inputs are made ready and the outputs finished.
 //
-// 192 sequences of 5120 channels, 16 states, bf16: 18.5 us in a graph, 0.87 of the copy rate (one
-// sequence a thread: 35; 64-bit products for the addresses: 21); issue is near its bound there, 0.68 a
-// clock.  Four blocks an SM, or three of fp32 (without: 19.6, and fp32 28.2 for 25.8).  One
-// sequence of 1024 channels: 2.7 us.
+// 192 sequences of 5120 channels, 16 states, from HBM: bf16 24.6 us (0.65 of the copy rate), fp32 29.0 (0.73);
+// 256 of 4096 channels of 64 states 94.6 (0.86) and 112 (0.73).  Instructions bound it, 0.65 a clock: with the states
+// in L2 the first still takes 19.1 us (18.5 without the decays' correction; when the kernel was first
+// made one sequence a thread took 35, 64-bit products for the addresses 21, and without four blocks an SM, or three of fp32, it was
+// 19.6 for 18.5 and 28.2 for 25.8).  One sequence of 1024 channels: 2.7 us.
 #include "sel_scan.cuh"
 #include "sel_scan_plan.cuh"
 
